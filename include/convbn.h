@@ -73,7 +73,9 @@ typedef enum {
     CONVBN_PHASE_DEPLOY_FWD = 5,
     CONVBN_PHASE_DEPLOY_BWD = 6,
     CONVBN_PHASE_TUNE_BWD = 7,
-    CONVBN_PHASE_COUNT = 8
+    CONVBN_PHASE_TUNE_BWD_PACKED = 8,
+    CONVBN_PHASE_DEPLOY_FWD_QUANT = 9,
+    CONVBN_PHASE_COUNT = 10
 } convbn_phase;
 
 /* Problem description (paper Sec. 3.1 and the shape annotations of Appendix C; stride, padding,
@@ -199,6 +201,33 @@ int convbn_tune_bwd_weight_noalloc(const convbn_desc *desc, const void *dz, cons
                                    const void *saved, float *dw, float *db, float *dgamma,
                                    float *dbeta, void *stream);
 
+/* ---- X in 8 bits from forward to backward (Sec. 3.3 / 3.4, Appendix M: in Tune mode X is all that is left to keep) ----
+ *
+ * convbn_pack writes `count` elements of `dtype` in 8 bits: `codes` [count], a signed byte per element, and `steps`
+ * [ceil(count / 32)], a byte e + 127 per 32 consecutive elements (the last group may be shorter).  An element stands
+ * for code * 2^e.
+ *   e      the smallest integer at which the group's largest magnitude rounds to 127 at most, within -126 .. 121
+ *          (bf16, fp32) or -24 .. 9 (half)
+ *   code   x 2^-e rounded to the nearest integer (ties to even), at most 127 in magnitude, and 1 or -1 where that is 0
+ *          but x is not: x > 0 exactly where code > 0
+ * A group that holds an infinity or a NaN: step byte 255, codes 0; all of it is restored as NaN.
+ * The largest error is half a step, 2^-8 of the group's largest magnitude at most 2^-7 (one step for magnitudes below half
+ * a step, and where e is held at a bound).
+ * convbn_unpack restores the values, without rounding, in any of the three types that they fit.
+ * All pointers device, 16-byte aligned, no overlap.  A count of 0 is a no-op that looks at no pointer.  CONVBN_EINVAL for a
+ * count below 0 or above 2^40, an unknown dtype or (count > 0) a NULL pointer; CONVBN_EALIGN; CONVBN_ECUDA. */
+int convbn_pack(int dtype, const void *x, void *codes, void *steps, long long count, void *stream);
+int convbn_unpack(int dtype, const void *codes, const void *steps, void *out, long long count, void *stream);
+
+/* convbn_tune_bwd_glue with X given as convbn_pack left it (codes and steps of all N C_in H_in W_in elements, in the order
+ * of desc.layout): the same values as that call gives for the restored X; relu_mask: dx = 0 where the code is not positive.
+ * Codes and steps belong to the library like X does (begin != 0: until the join).
+ * Workspace: convbn_workspace_bytes(desc, CONVBN_PHASE_TUNE_BWD_PACKED).  Errors as for convbn_tune_bwd_glue. */
+int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *codes, const void *steps, const void *w,
+                           const float *b, const float *run_mean, const void *saved, void *dx, float *dw, float *db,
+                           float *dgamma, float *dbeta, const void *add, int relu_mask, int begin, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
 /* ---- Eval mode comparator (Sec. 3.1; Table 2, Eval row) ---------------------------------- */
 
 /* Y = omega (*) X + b is written to `y_saved` (the activation Eval mode keeps), then
@@ -232,6 +261,28 @@ int convbn_deploy_fwd(const convbn_desc *desc, const void *x, const void *w_fuse
 int convbn_deploy_bwd(const convbn_desc *desc, const void *dz, const void *x,
                       const void *w_fused, void *dx, float *dw_fused, float *db_fused,
                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- Deploy mode in 8-bit integers: 1x1 and Linear-BN blocks (Sec. 3.3; Appendix C) --------------------------------------
+ *
+ * The product of a deployed block with both operands in 8 bits: a scale for every output channel, fixed once, and one for
+ * every row of X (the channels of an output pixel; a token), formed by each call.
+ *     prepare:  a = max_k |omega[co][k]|   w_codes = rne(omega * fl(127 / a))   w_scale = s a / 127   b_fused = b'
+ *     forward:  a = max_k |x[p][k]|        xq = rne(x * fl(127 / a))
+ *               z = (sum_k xq w_codes) (a / 127) w_scale + b_fused,   with `add` z + add, with relu != 0 max(z, 0)
+ * The BatchNorm scale s is part of the channel scale: the codes are omega's own.  Products are exact, sums exact in 32 bits;
+ * one rounding to the storage type, when z is written.  A row or a channel whose largest magnitude is below 2^-100 counts as zero; one
+ * with an infinity or a NaN gives NaN (which max(., 0) turns into 0, as convbn_relu does).
+ * w_codes: signed bytes [C_out][C_in rounded up to a multiple of 16], the added columns zero.  w_scale, b_fused [C_out] fp32.
+ * Layers: kh = kw = 1, no padding, groups = 1, any stride, C_in <= 131072, fewer than 2^31 - 256 output pixels; NHWC 16-bit storage,
+ * or fp32 with one pixel per image (convbn_linear_desc).  Others: CONVBN_EUNSUPPORTED, workspace size 0.
+ * z may not overlap x; add [like z, 16-byte aligned, NULL: none] may not overlap z.
+ * Workspace of the forward call: convbn_workspace_bytes(desc, CONVBN_PHASE_DEPLOY_FWD_QUANT). */
+int convbn_deploy_prepare_quant(const convbn_desc *desc, const void *w, const float *b, const float *gamma, const float *beta,
+                                const float *run_mean, const float *run_var, void *w_codes, float *w_scale, float *b_fused,
+                                void *stream);
+int convbn_deploy_fwd_quant(const convbn_desc *desc, const void *x, const void *w_codes, const float *w_scale,
+                            const float *b_fused, void *z, const void *add, int relu, void *workspace, size_t workspace_bytes,
+                            void *stream);
 
 /* ---- one Tune-mode training step from HOST buffers ------------------------------------------- */
 

@@ -20,7 +20,7 @@ F32, BF16, F16 = 0, 1, 2
 NCHW, NHWC = 0, 1
 MODE_TUNE, MODE_EVAL, MODE_DEPLOY = 0, 1, 2
 (PHASE_TUNE_FWD, PHASE_TUNE_BWD_DATA, PHASE_TUNE_BWD_WEIGHT, PHASE_EVAL_FWD, PHASE_EVAL_BWD,
- PHASE_DEPLOY_FWD, PHASE_DEPLOY_BWD, PHASE_TUNE_BWD) = range(8)
+ PHASE_DEPLOY_FWD, PHASE_DEPLOY_BWD, PHASE_TUNE_BWD, PHASE_TUNE_BWD_PACKED, PHASE_DEPLOY_FWD_QUANT) = range(10)
 
 EXPORTS = (
     "convbn_out_shape", "convbn_saved_bytes", "convbn_workspace_bytes", "convbn_tune_fwd",
@@ -31,6 +31,7 @@ EXPORTS = (
     "convbn_tune_bwd_weight_noalloc", "convbn_selftest_wait_timeout", "convbn_tune_bwd", "convbn_linear_desc", "convbn_relu", "convbn_add_relu", "convbn_relu_bwd", "convbn_add",
     "convbn_tune_bwd_begin", "convbn_tune_bwd_join", "convbn_tune_fwd_glue", "convbn_tune_bwd_glue",
     "convbn_tconv_out_shape", "convbn_tconv_workspace_bytes", "convbn_tconv_tune_fwd", "convbn_tconv_tune_bwd",
+    "convbn_pack", "convbn_unpack", "convbn_tune_bwd_packed", "convbn_deploy_prepare_quant", "convbn_deploy_fwd_quant",
 )
 
 
@@ -71,6 +72,8 @@ def _signatures():
         "convbn_deploy_fwd": "dpppppzp", "convbn_deploy_bwd": "dpppppppzp",
         "convbn_tune_bwd_weight_noalloc": "dppppppppppp", "convbn_deploy_prepare": "dppppppppp",
         "convbn_relu": "ippqp", "convbn_add_relu": "ipppqp", "convbn_relu_bwd": "ipppqp",
+        "convbn_pack": "ipppqp", "convbn_unpack": "ipppqp", "convbn_tune_bwd_packed": "dppppppppppppp" "iipzp",
+        "convbn_deploy_prepare_quant": "dppppppppp" "p", "convbn_deploy_fwd_quant": "dppppppipzp",
         "convbn_add": "ipppqp", "convbn_workspace_bytes": "di", "convbn_saved_bytes": "di", "convbn_check": "p",
     }
     return {name: [kinds[k] for k in sig] for name, sig in table.items()}
@@ -386,6 +389,57 @@ def convbn_relu_bwd(a, y, out, stream=None):
 def convbn_add(a, b, out, stream=None):
     _raise(lib().convbn_add(_dtype_of(a), _ptr(a), _ptr(b), _ptr(out), a.numel(),
                             _stream(stream)), "convbn_add")
+
+
+def _storage(t) -> int:
+    import torch
+    kind = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}.get(t.dtype)
+    if kind is None:
+        raise TypeError("bfloat16, float16 or float32 is expected, not %s" % t.dtype)
+    return kind
+
+
+def convbn_pack(x, codes, steps, stream=None):
+    """x in 8 bits: a signed code per element, a step byte per 32 consecutive ones."""
+    status = (_native or _calls()).convbn_pack(_storage(x), x, codes, steps, x.numel(), stream)
+    if status:
+        _raise(status, "convbn_pack")
+
+
+def convbn_unpack(codes, steps, out, stream=None):
+    status = (_native or _calls()).convbn_unpack(_storage(out), codes, steps, out, out.numel(), stream)
+    if status:
+        _raise(status, "convbn_unpack")
+
+
+def convbn_tune_bwd_packed(desc, dz, codes, steps, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta, add, relu_mask, begin,
+                           workspace=None, workspace_bytes: Optional[int] = None, stream=None):
+    """convbn_tune_bwd_glue with X as convbn_pack left it."""
+    if type(desc) is not Desc:
+        desc = _desc(desc)
+    status = (_native or _calls()).convbn_tune_bwd_packed(desc, dz, codes, steps, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta,
+                                                          add, 1 if relu_mask else 0, 1 if begin else 0, workspace,
+                                                          workspace_bytes, stream)
+    if status:
+        _raise(status, "convbn_tune_bwd_packed")
+
+
+def convbn_deploy_prepare_quant(desc, w, b, gamma, beta, run_mean, run_var, w_codes, w_scale, b_fused, stream=None):
+    """A trained 1x1 or Linear-BN block's weights in 8 bits: codes [C_out][C_in rounded up to 16], a scale per channel."""
+    _raise(lib().convbn_deploy_prepare_quant(desc, _ptr(w), _ptr(b), _ptr(gamma), _ptr(beta), _ptr(run_mean), _ptr(run_var),
+                                             _ptr(w_codes), _ptr(w_scale), _ptr(b_fused), _stream(stream)),
+           "convbn_deploy_prepare_quant")
+
+
+def convbn_deploy_fwd_quant(desc, x, w_codes, w_scale, b_fused, z, add, relu, workspace=None,
+                            workspace_bytes: Optional[int] = None, stream=None):
+    """convbn_deploy_fwd as a product of 8-bit integers, with the addend and the ReLU of a residual network."""
+    if type(desc) is not Desc:
+        desc = _desc(desc)
+    status = (_native or _calls()).convbn_deploy_fwd_quant(desc, x, w_codes, w_scale, b_fused, z, add, 1 if relu else 0, workspace,
+                                                           workspace_bytes, stream)
+    if status:
+        _raise(status, "convbn_deploy_fwd_quant")
 
 
 def convbn_check(stream=None) -> None:

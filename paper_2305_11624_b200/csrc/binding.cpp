@@ -133,7 +133,8 @@ PyMethodDef g_methods[] = {
     ENTRY(convbn_tune_fwd), ENTRY(convbn_tune_bwd_data), ENTRY(convbn_tune_bwd_weight), ENTRY(convbn_tune_bwd),
     ENTRY(convbn_tune_bwd_begin), ENTRY(convbn_tune_bwd_join), ENTRY(convbn_tune_fwd_glue), ENTRY(convbn_tune_bwd_glue),
     ENTRY(convbn_tconv_tune_fwd), ENTRY(convbn_tconv_tune_bwd), ENTRY(convbn_eval_fwd), ENTRY(convbn_eval_bwd),
-    ENTRY(convbn_deploy_fwd), ENTRY(convbn_deploy_bwd), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(convbn_deploy_fwd), ENTRY(convbn_deploy_bwd), ENTRY(convbn_pack), ENTRY(convbn_unpack), ENTRY(convbn_tune_bwd_packed),
+    ENTRY(convbn_deploy_fwd_quant), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

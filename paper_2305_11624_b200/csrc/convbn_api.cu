@@ -17,8 +17,8 @@ using namespace convbn;
 
 namespace {
 
-thread_local const char *t_last_kernel[CONVBN_PHASE_COUNT] = {"none", "none", "none", "none",
-                                                              "none", "none", "none", "none"};
+thread_local const char *t_last_kernel[CONVBN_PHASE_COUNT] = {"none", "none", "none", "none", "none",
+                                                              "none", "none", "none", "none", "none"};
 
 // ---- optional per-kernel timing (CUDA events around every launch this library makes) ----------
 struct ProfRec { cudaEvent_t a, b; std::string name; };
@@ -125,6 +125,8 @@ struct Plan {
     size_t xpk = 0, wst = 0;   // small-C_in layers: packed input [n][hp][wp][8], expanded weights [C_out][kh][64]
     bool stem = false;
     bool stem_win_wgrad = false;   // stem weight gradient straight from X (window operand), fused epilogue
+    size_t unpacked = 0;   // backward from packed X: X in the storage type
+    size_t inner = 0;      // its offset of the backward call's workspace; Deploy mode in 8 bits: the rows' scales
     size_t wbd = 0;        // block-diagonal expanded weights [C_out][taps][64], storage dtype
     // Eval backward of a dense tensor-core layer: s commutes with both contractions, so dX and domega come from dZ through
     // the Tune kernels and no s dZ tensor exists (eval_inner: offset of their workspace)
@@ -140,6 +142,12 @@ bool f32_path(const convbn_desc *d, const Problem &pb) {
 
 bool fused_bwd_path(const convbn_desc *d, const Problem &pb) {
     return d->dtype == CONVBN_BF16 && d->layout == CONVBN_NHWC && fused_bwd1x1_eligible(pb);
+}
+
+// (fp32 NCHW: where a pixel's channels lie side by side)
+bool quant_path(const convbn_desc *d, const Problem &pb) {
+    return quant_eligible(pb) && (d->dtype == CONVBN_F32 ? d->layout == CONVBN_NCHW && pb.h_in == 1 && pb.w_in == 1
+                                                         : d->layout == CONVBN_NHWC);
 }
 
 bool strided_dgrad_ok(const convbn_desc *d, const Problem &pb);
@@ -208,6 +216,19 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded,
     }
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
+    if (phase == CONVBN_PHASE_TUNE_BWD_PACKED) {
+        pl.unpacked = take((size_t)pb.pin * pb.c_in * elem_size(d->dtype));
+        pl.inner = take(make_plan(d, pb, CONVBN_PHASE_TUNE_BWD).total);
+        pl.total = off;
+        return pl;
+    }
+    if (phase == CONVBN_PHASE_DEPLOY_FWD_QUANT) {
+        if (!quant_path(d, pb)) return pl;
+        pl.unpacked = take(quant_codes_bytes(pb));
+        pl.inner = take((size_t)pb.p * sizeof(float));
+        pl.total = off;
+        return pl;
+    }
     size_t wbytes = (size_t)pb.c_out * pb.kdim * elem_size(d->dtype);
     // the sub-pixel backward-data path of small-C_in layers keeps its (zero-padded) weight matrix there
     if (d->dtype == CONVBN_BF16 && d->layout == CONVBN_NHWC && subpixel_weight_bytes(pb) > wbytes)
@@ -1139,6 +1160,63 @@ int convbn_tune_bwd_join(void *stream) {
     return CONVBN_OK;
 }
 
+// ---- X in 8 bits from forward to backward ---------------------------------------------------------
+static int pack_check(int dtype, const void *a, const void *b, const void *c, long long count) {
+    if (count < 0 || (dtype != CONVBN_F32 && dtype != CONVBN_BF16 && dtype != CONVBN_F16)) return CONVBN_EINVAL;
+    if (count > (1LL << 40)) return CONVBN_EINVAL;
+    if (count == 0) return CONVBN_OK;
+    if (!a || !b || !c) return CONVBN_EINVAL;
+    return aligned(a, 16) && aligned(b, 16) && aligned(c, 16) ? CONVBN_OK : CONVBN_EALIGN;
+}
+
+int convbn_pack(int dtype, const void *x, void *codes, void *steps, long long count, void *stream) {
+    t_prof_phase = "pack";
+    CK(pack_check(dtype, x, codes, steps, count));
+    cudaStream_t st = (cudaStream_t)stream;
+    if (count) LAUNCH("pack", launch_pack(dtype, x, codes, steps, count, st));
+    return CONVBN_OK;
+}
+
+int convbn_unpack(int dtype, const void *codes, const void *steps, void *out, long long count, void *stream) {
+    t_prof_phase = "unpack";
+    CK(pack_check(dtype, codes, steps, out, count));
+    cudaStream_t st = (cudaStream_t)stream;
+    if (count) LAUNCH("unpack", launch_unpack(dtype, codes, steps, out, count, st));
+    return CONVBN_OK;
+}
+
+int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *codes, const void *steps, const void *w,
+                           const float *b, const float *run_mean, const void *saved, void *dx, float *dw, float *db,
+                           float *dgamma, float *dbeta, const void *add, int relu_mask, int begin, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+    HalfCall half(desc);
+    if (half.status != CONVBN_OK) return half.status;
+    desc = half.use;
+    Problem pb;
+    t_prof_phase = "bwd";
+    CK(make_problem(desc, &pb));
+    CK(check_pair(desc));
+    if (!dz || !codes || !steps || !w || !run_mean || !saved || !dx || !dw || !dgamma || !dbeta) return CONVBN_EINVAL;
+    if ((b == nullptr) != (db == nullptr)) return CONVBN_EINVAL;
+    if (!aligned(dz, 16) || !aligned(codes, 16) || !aligned(steps, 16) || !aligned(w, 16) || !aligned(saved, 16) ||
+        !aligned(dx, 16) || !aligned(dw, 16) || !aligned(b, 4) || !aligned(run_mean, 4) || !aligned(db, 4) ||
+        !aligned(dgamma, 4) || !aligned(dbeta, 4) || !aligned(add, 16))
+        return CONVBN_EALIGN;
+    const Plan pl = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD_PACKED);
+    CK(check_ws(pl, workspace, workspace_bytes));
+    cudaStream_t st = (cudaStream_t)stream;
+    void *x = at(workspace, pl.unpacked);
+    LAUNCH("unpack", launch_unpack(desc->dtype == CONVBN_BF16 && call_f16() ? CONVBN_F16 : desc->dtype, codes, steps, x,
+                                   pb.pin * pb.c_in, st));
+    PostOp post;
+    post.add = add;
+    post.mask = relu_mask ? x : nullptr;
+    CK(tune_bwd_impl(desc, dz, x, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta, at(workspace, pl.inner), pl.total - pl.inner,
+                     stream, begin != 0, post));
+    t_last_kernel[CONVBN_PHASE_TUNE_BWD_PACKED] = "unpack";
+    return CONVBN_OK;
+}
+
 int convbn_eval_fwd(const convbn_desc *desc, const void *x, const void *w, const float *b,
                     const float *gamma, const float *beta, const float *run_mean,
                     const float *run_var, void *z, void *y_saved, void *workspace,
@@ -1319,6 +1397,54 @@ int convbn_deploy_bwd(const convbn_desc *desc, const void *dz, const void *x, co
             return run_conv_dgrad(desc, pb, dz, w_fused, nullptr, at(workspace, pl.w_scaled), at(workspace, pl.wbd), dx, st,
                                   &t_last_kernel[CONVBN_PHASE_DEPLOY_BWD]);
         });
+}
+
+// ---- Deploy mode in 8-bit integers -------------------------------------------------------------------
+static int storage_type(const convbn_desc *d) { return d->dtype == CONVBN_BF16 && call_f16() ? CONVBN_F16 : d->dtype; }
+
+int convbn_deploy_prepare_quant(const convbn_desc *desc, const void *w, const float *b, const float *gamma, const float *beta,
+                                const float *run_mean, const float *run_var, void *w_codes, float *w_scale, float *b_fused,
+                                void *stream) {
+    HalfCall half(desc);
+    if (half.status != CONVBN_OK) return half.status;
+    desc = half.use;
+    Problem pb;
+    t_prof_phase = "deploy_prepare_quant";
+    CK(make_problem(desc, &pb));
+    CK(check_pair(desc));
+    if (!quant_path(desc, pb)) return CONVBN_EUNSUPPORTED;
+    if (!w || !gamma || !beta || !run_mean || !run_var || !w_codes || !w_scale || !b_fused) return CONVBN_EINVAL;
+    if (!aligned(w, 16) || !aligned(w_codes, 16) || !aligned(b, 4) || !aligned(gamma, 4) || !aligned(beta, 4) ||
+        !aligned(run_mean, 4) || !aligned(run_var, 4) || !aligned(w_scale, 4) || !aligned(b_fused, 4))
+        return CONVBN_EALIGN;
+    cudaStream_t st = (cudaStream_t)stream;
+    LAUNCH("quant_weights", launch_quant_weights(pb, storage_type(desc), w, b, gamma, beta, run_mean, run_var, w_codes, w_scale,
+                                                 b_fused, st));
+    return CONVBN_OK;
+}
+
+int convbn_deploy_fwd_quant(const convbn_desc *desc, const void *x, const void *w_codes, const float *w_scale, const float *b_fused,
+                            void *z, const void *add, int relu, void *workspace, size_t workspace_bytes, void *stream) {
+    HalfCall half(desc);
+    if (half.status != CONVBN_OK) return half.status;
+    desc = half.use;
+    Problem pb;
+    t_prof_phase = "deploy_fwd_quant";
+    CK(make_problem(desc, &pb));
+    CK(check_pair(desc));
+    if (!quant_path(desc, pb)) return CONVBN_EUNSUPPORTED;
+    if (!x || !w_codes || !w_scale || !b_fused || !z) return CONVBN_EINVAL;
+    if (!aligned(x, 16) || !aligned(w_codes, 16) || !aligned(z, 16) || !aligned(add, 16) || !aligned(w_scale, 4) || !aligned(b_fused, 4))
+        return CONVBN_EALIGN;
+    const Plan pl = make_plan(desc, pb, CONVBN_PHASE_DEPLOY_FWD_QUANT);
+    CK(check_ws(pl, workspace, workspace_bytes));
+    cudaStream_t st = (cudaStream_t)stream;
+    float *xs = (float *)at(workspace, pl.inner);
+    LAUNCH("quant_rows", launch_quant_rows(pb, storage_type(desc), x, at(workspace, pl.unpacked), xs, st));
+    LAUNCH("quant_product", launch_quant_product(pb, storage_type(desc), at(workspace, pl.unpacked), xs, w_codes, w_scale, b_fused, add,
+                                                 relu ? 1 : 0, z, st));
+    t_last_kernel[CONVBN_PHASE_DEPLOY_FWD_QUANT] = "direct";
+    return CONVBN_OK;
 }
 
 // ---- TransposedConv-BN -----------------------------------------------------------------------------

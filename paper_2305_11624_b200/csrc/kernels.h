@@ -327,4 +327,20 @@ cudaError_t launch_tconv_param_epilogue(int dtype, bool nhwc, int c_out, int tap
                                         const float *bsum, int bsplits, float *dw, float *db, float *dgamma,
                                         float *dbeta, cudaStream_t st);
 
+// ---- 8-bit forms of a block's input ----------------------------------------------------------------------
+// Kept from forward to backward (pack_kernels.cu; dtype is the caller's, CONVBN_F16 included).
+cudaError_t launch_pack(int dtype, const void *x, void *codes, void *steps, long long count, cudaStream_t st);
+cudaError_t launch_unpack(int dtype, const void *codes, const void *steps, void *out, long long count, cudaStream_t st);
+
+// The deployed 1x1 block as a product of 8-bit integers (quant_kernels.cu).  Rows of codes are quant_pitch bytes apart.
+bool quant_eligible(const Problem &pb);
+inline int quant_pitch(const Problem &pb) { return (pb.c_in + 15) / 16 * 16; }
+size_t quant_codes_bytes(const Problem &pb);
+cudaError_t launch_quant_weights(const Problem &pb, int dtype, const void *w, const float *b, const float *gamma, const float *beta,
+                                 const float *mean, const float *var, void *codes, float *scale, float *shift, cudaStream_t st);
+// codes [p][pitch], scale [p]: of the rows of X that the output pixels read
+cudaError_t launch_quant_rows(const Problem &pb, int dtype, const void *x, void *codes, float *scale, cudaStream_t st);
+cudaError_t launch_quant_product(const Problem &pb, int dtype, const void *xq, const float *xs, const void *wq, const float *ws,
+                                 const float *shift, const void *add, int relu, void *z, cudaStream_t st);
+
 }  // namespace convbn

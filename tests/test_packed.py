@@ -1,0 +1,271 @@
+"""X in 8 bits from forward to backward: convbn_pack, convbn_unpack, convbn_tune_bwd_packed."""
+import numpy as np
+import pytest
+
+import parity
+from oracle import packed_oracle as P
+from paper_2305_11624_b200 import convbn as C
+from paper_2305_11624_b200 import inputs as I
+
+ROUND = {"bf16": I.round_bf16, "f16": lambda a: np.asarray(a, np.float16).astype(np.float32), "f32": lambda a: np.asarray(a, np.float32)}
+
+
+# ---- the definition itself ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_the_definition_keeps_signs_and_half_a_step(dtype):
+    rng = np.random.default_rng(3)
+    x = ROUND[dtype]((rng.standard_normal(6400) * np.repeat(10.0 ** rng.uniform(-3, 3, 200), 32)).astype(np.float32)).astype(np.float64)
+    x[::7] = 0.0
+    q, s = P.pack(x, dtype)
+    back, step = P.unpack(q, s), np.repeat(2.0 ** (s.astype(float) - 127), 32)
+    assert np.array_equal(np.sign(back), np.sign(x))
+    large = np.abs(x) >= step / 2
+    assert np.all(np.abs(back - x)[large] <= step[large] / 2) and np.all(np.abs(back - x) <= step)
+    top = np.abs(x).reshape(-1, 32).max(1)
+    assert np.all((np.abs(q.astype(int)).reshape(-1, 32).max(1) >= 64) | (s == P.BOUNDS[dtype][0] + 127))
+    assert np.all(top <= 127.5 * 2.0 ** (s.astype(float) - 127))
+    np.testing.assert_array_equal(ROUND[dtype](back), back)              # exact in the storage type
+
+
+# ---- refusals (host) -------------------------------------------------------------------------------------------------
+def test_pack_refusals():
+    lib, ok = C.lib(), 4096
+    for f in (lib.convbn_pack, lib.convbn_unpack):
+        assert f(C.BF16, 0, 0, 0, 0, 0) == C.OK                         # nothing to do
+        assert f(C.BF16, ok, ok, ok, -1, 0) == C.EINVAL
+        assert f(C.BF16, ok, ok, ok, (1 << 40) + 1, 0) == C.EINVAL
+        assert f(3, ok, ok, ok, 5, 0) == C.EINVAL
+        for i in range(3):
+            p = [ok] * 3
+            p[i] = 0
+            assert f(C.F32, *p, 5, 0) == C.EINVAL
+            p[i] = ok + 8
+            assert f(C.F16, *p, 5, 0) == C.EALIGN
+
+
+def test_packed_backward_refusals():
+    d = C.Desc.make(2, 64, 8, 8, 64, 1, 1)
+    size = C.convbn_workspace_bytes(d, C.PHASE_TUNE_BWD_PACKED)
+    assert size >= C.convbn_workspace_bytes(d, C.PHASE_TUNE_BWD) > 0 and size % 256 == 0
+    names = ("dz", "codes", "steps", "w", "b", "run_mean", "saved", "dx", "dw", "db", "dgamma", "dbeta", "add")
+
+    def status(desc=d, ws=4096, bytes_=size, **over):
+        a = {n: (None if n in ("b", "db", "add") else 4096) for n in names}
+        a.update(over)
+        with pytest.raises(C.ConvBNError) as e:
+            C.convbn_tune_bwd_packed(desc, *[a[n] for n in names], True, False, ws, bytes_, stream=0)
+        return e.value.status
+
+    for n in names:
+        if n not in ("b", "db", "add"):
+            assert status(**{n: None}) == C.EINVAL, n
+        off = 2 if n in ("b", "run_mean", "db", "dgamma", "dbeta") else 8
+        pair = {"b": dict(db=4096), "db": dict(b=4096)}.get(n, {})
+        assert status(**{n: 4096 + off}, **pair) == C.EALIGN, n
+    assert status(b=4096) == C.EINVAL and status(db=4096) == C.EINVAL
+    assert status(ws=None) == C.EWORKSPACE and status(bytes_=size - 1) == C.EWORKSPACE and status(ws=4096 + 16) == C.EALIGN
+    assert status(desc=C.Desc.make(2, 64, 8, 8, 64, 1, 1, dtype=C.BF16, layout=C.NCHW)) == C.EUNSUPPORTED
+    assert status(desc=C.Desc.make(2, 64, 8, 8, 64, 1, 1, dtype=C.F16, layout=C.NCHW)) == C.EUNSUPPORTED
+    assert status(desc=C.Desc.make(0, 64, 8, 8, 64, 1, 1)) == C.EINVAL
+
+
+# ---- packing on the device ------------------------------------------------------------------------------------------
+def _values(count, dtype, seed):
+    """Every kind of group: ordinary, all zero, one value, values at a tie, the type's largest and smallest, infinities, NaN."""
+    rng = np.random.default_rng(seed)
+    groups = -(-count // 32)
+    v = rng.standard_normal((groups, 32)) * 2.0 ** rng.integers(-20, 20, groups)[:, None]
+    for g in range(groups):
+        kind = (g + seed) % 12
+        if kind == 1:
+            v[g] = 0.0
+        elif kind == 2:
+            v[g] = 0.0
+            v[g, rng.integers(32)] = -3.25
+        elif kind == 3:
+            v[g] = (rng.integers(-127, 127, 32) + 0.5) * 0.25           # ties, and 127.5 steps
+            v[g, 0] = 127.5 * 0.25
+        elif kind == 4:
+            v[g, 5] = {"bf16": 3.3895314e38, "f32": 3.4028235e38, "f16": 65504.0}[dtype]
+        elif kind == 5:
+            v[g] = rng.integers(-3, 4, 32) * {"bf16": 2.0 ** -133, "f32": 2.0 ** -149, "f16": 2.0 ** -24}[dtype]
+        elif kind == 6:
+            v[g, 31] = np.inf * (-1) ** g
+        elif kind == 7:
+            v[g, 0] = np.nan
+        elif kind == 8:
+            v[g] = np.abs(v[g]) * (rng.random(32) < 0.5)                # a ReLU's output
+        elif kind == 9:
+            v[g] *= 2.0 ** rng.integers(-30, 1, 32)                     # far below half a step
+    with np.errstate(over="ignore"):
+        return ROUND[dtype](v.astype(np.float32).ravel()[:count])
+
+
+def _torch(dtype):
+    import torch
+    return {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[dtype]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("count", [1, 15, 16, 17, 31, 32, 33, 511, 513, 4099, 148 * 16 * 4096 + 77])
+def test_pack_and_unpack_are_exact(dtype, count):
+    import torch
+    host = _values(count, dtype, count % 5)
+    groups = -(-count // 32)
+    x = torch.from_numpy(host).cuda().to(_torch(dtype))
+    codes = torch.full((count + 48,), 99, dtype=torch.int8, device="cuda")
+    steps = torch.full((groups + 48,), 99, dtype=torch.uint8, device="cuda")
+    out = torch.full((count + 24,), 7.0, dtype=_torch(dtype), device="cuda")
+    C.convbn_pack(x, codes, steps)
+    C.convbn_unpack(codes, steps, out[:count])
+    C.convbn_check()
+    q, s = P.pack(host, dtype)
+    assert np.array_equal(steps[:groups].cpu().numpy(), s)
+    assert np.array_equal(codes[:count].cpu().numpy(), q)
+    np.testing.assert_array_equal(out[:count].float().cpu().numpy().astype(np.float64), P.unpack(q, s))
+    assert bool((codes[count:] == 99).all()) and bool((steps[groups:] == 99).all()) and bool((out[count:] == 7.0).all())
+
+
+@pytest.mark.gpu
+def test_a_type_that_is_not_a_storage_type_is_refused():
+    import torch
+    x = torch.zeros(64, dtype=torch.float64, device="cuda")
+    codes, steps = torch.zeros(64, dtype=torch.int8, device="cuda"), torch.zeros(2, dtype=torch.uint8, device="cuda")
+    with pytest.raises(TypeError):
+        C.convbn_pack(x, codes, steps)
+    with pytest.raises(TypeError):
+        C.convbn_unpack(codes, steps, codes)
+
+
+# ---- the backward pass -----------------------------------------------------------------------------------------------
+LAYERS = [
+    I.LayerSpec("wide_in", 2, 256, 20, 15, 64, 1, 1),                    # one kernel reads dZ once
+    I.LayerSpec("wide_in_128", 3, 128, 14, 13, 64, 1, 1),
+    I.LayerSpec("wide_out", 2, 64, 17, 19, 256, 1, 1),
+    I.LayerSpec("wide_out_128", 5, 64, 11, 13, 128, 1, 1),
+    I.LayerSpec("wide_few_pixels", 1, 256, 3, 5, 64, 1, 1),
+    I.LayerSpec("one_pixel", 1, 64, 1, 1, 64, 1, 1),
+    I.LayerSpec("rows", 777, 256, 1, 1, 192, 1, 1),                      # Linear-BN
+    I.LayerSpec("rows_wide", 130, 2048, 1, 1, 512, 1, 1),
+    I.LayerSpec("odd_slices", 3, 192, 9, 7, 320, 1, 1),
+    I.LayerSpec("reduce", 4, 1024, 7, 7, 256, 1, 1),
+    I.LayerSpec("shortcut", 2, 256, 15, 14, 512, 1, 1, stride=2),
+    I.LayerSpec("conv3", 2, 64, 13, 17, 64, 3, 3, pad=1),
+    I.LayerSpec("conv3_stride2", 2, 128, 16, 18, 128, 3, 3, stride=2, pad=1),
+    I.LayerSpec("conv3_dilated", 1, 64, 16, 18, 64, 3, 3, pad=2, dil=2),
+    I.LayerSpec("stem", 1, 3, 33, 40, 64, 7, 7, stride=2, pad=3),
+    I.LayerSpec("depthwise", 2, 96, 12, 11, 96, 3, 3, pad=1, groups=96),
+    I.LayerSpec("grouped8", 2, 64, 10, 12, 64, 3, 3, pad=1, groups=8),
+    I.LayerSpec("grouped32", 2, 128, 10, 12, 128, 3, 3, pad=1, groups=4),
+    I.LayerSpec("odd_channels", 2, 10, 9, 8, 20, 3, 3, pad=1),
+    I.LayerSpec("f32", 2, 16, 9, 11, 24, 3, 3, pad=1, dtype="f32", layout="nchw"),
+    I.LayerSpec("f32_rows", 37, 24, 1, 1, 10, 1, 1, dtype="f32", layout="nchw"),
+]
+
+
+def _restored(spec, x):
+    """x [N, C, H, W] as the packed form holds it, and its codes and steps in memory order."""
+    flat = I.act_to_layout(x, spec.layout).ravel()
+    q, s = P.pack(flat, spec.dtype)
+    return I.act_from_layout(P.unpack(q, s), spec.layout, x.shape), q, s
+
+
+def _packed_pass(spec, t, add, mask, begin=False, stream=None, expect=None):
+    """The calls of a training step whose X is kept packed; outputs as float64 in logical order."""
+    import torch
+    from paper_2305_11624_b200.harness import Block
+    blk = Block(spec, modes=("tune",))
+    blk.load(t)
+    codes = torch.empty(blk.x.numel(), dtype=torch.int8, device="cuda")
+    steps = torch.empty(-(-blk.x.numel() // 32), dtype=torch.uint8, device="cuda")
+    more = None
+    if add is not None:
+        more = torch.empty_like(blk.x)
+        blk._up(more, I.act_to_layout(add, spec.layout))
+    for name in ("dx", "dw", "dgamma", "dbeta"):
+        getattr(blk, name).fill_(float("nan"))
+    blk.tune_fwd()
+    C.convbn_pack(blk.x, codes, steps)
+    _, q, s = _restored(spec, t["x"])
+    assert np.array_equal(codes.cpu().numpy(), q) and np.array_equal(steps.cpu().numpy(), s)
+    blk.x.fill_(float("nan"))                                            # X itself is gone
+    size = C.convbn_workspace_bytes(blk.desc, C.PHASE_TUNE_BWD_PACKED)
+    room = torch.full((size + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    C.convbn_tune_bwd_packed(blk.desc, blk.dz, codes, steps, blk.w, blk.b, blk.mu_hat, blk.saved, blk.dx, blk.dw, blk.db, blk.dgamma,
+                             blk.dbeta, more, mask, begin, room[:size] if size else None)
+    if begin:
+        C.convbn_tune_bwd_join()
+    C.convbn_check()
+    assert bool((room[size:] == 0xFF).all())
+    if expect is not None:
+        assert C.convbn_last_kernel(C.PHASE_TUNE_BWD_PACKED) == expect
+    names = ["dx", "dw", "dgamma", "dbeta"] + (["db"] if spec.bias else [])
+    return dict({n: blk.fetch(n) for n in names}, **({} if spec.bias else {"db": None}))
+
+
+def _reference(spec, t, add, mask):
+    back, _, _ = _restored(spec, t["x"])
+    ref = parity.oracle_tune(spec, dict(t, x=back))
+    if add is not None:
+        ref["dx"] = ref["dx"] + add
+    if mask:
+        ref["dx"] = ref["dx"] * (t["x"] > 0)                             # (the mask is the true one)
+    return ref
+
+
+HALF_STEP = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}
+
+
+def _compare(spec, t, got, ref, add, mask):
+    """Norms and the parameter gradients as parity.py bounds them.  dX element by element, proven: with S = sum |dZ| |omega'| over
+    an element's products, the rounding of omega' costs u S (2^-25 |dZ| a product where half has no smaller steps), s and the fp32
+    sum of K products (8 + K) 2^-24 S, the store u |dX|, the addend's sum another u |dX + add|.  (parity.py measures an element
+    against the rms of its channel instead, which 15 pixels, half of them masked, do not give: a layer with 15 pixels, its dX
+    right, came to 1.26 of that bound.)"""
+    parity.compare(got, ref, parity.TOL[spec.dtype], ("dw", "db", "dgamma", "dbeta"), spec.name, dtype=spec.dtype)
+    assert parity.O.rel_l2(got["dx"], ref["dx"]) <= parity.TOL[spec.dtype]
+    plain = parity.oracle_tune(spec, t)
+    shape = parity.oracle_shape(spec)
+    size = parity.O.tune_backward(shape, np.abs(t["dz"]), t["x"], t["w"], np.abs(plain["w_f"]), t["b"], t["gamma"], t["mu_hat"],
+                                  t["var_hat"])["dx"]
+    products = spec.c_out // spec.groups * spec.kh * spec.kw
+    u = HALF_STEP[spec.dtype] * (1 + 2.0 ** -6)
+    bound = (u + (8 + products) * 2.0 ** -24) * size + u * np.abs(plain["dx"])
+    bound += 2.0 ** -25 * (1 + products * np.abs(t["dz"]).max())
+    if add is not None:
+        bound += u * (np.abs(plain["dx"] + add) + bound)
+    if mask:
+        assert not got["dx"][t["x"] <= 0].any()
+        bound = bound * (t["x"] > 0)
+    err = np.abs(got["dx"] - ref["dx"])
+    assert np.all(err <= bound), float((err / np.maximum(bound, 1e-30)).max())
+
+
+def _relu_inputs(spec, seed):
+    t = parity.make_inputs(spec, seed)
+    t["x"] = np.maximum(t["x"], 0.0)
+    return t
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mask,with_add", [(False, False), (True, False), (True, True)])
+@pytest.mark.parametrize("spec", LAYERS, ids=lambda s: s.name)
+def test_packed_backward_against_the_oracle(spec, mask, with_add):
+    """X enters the gradients as the value that its code stands for, exactly, so the bounds are those of the same layer with that
+    X."""
+    t = _relu_inputs(spec, 5) if mask else parity.make_inputs(spec, 5)
+    add = ROUND[spec.dtype](np.random.default_rng(1).standard_normal(t["x"].shape).astype(np.float32)) if with_add else None
+    got = _packed_pass(spec, t, add, mask)
+    _compare(spec, t, got, _reference(spec, t, add, mask), add, mask)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spec", [s for s in LAYERS if s.name in ("wide_in", "wide_out", "rows", "reduce", "conv3", "shortcut")], ids=lambda s: s.name)
+def test_packed_backward_in_half_with_bias_deferred(spec):
+    import dataclasses
+    spec = dataclasses.replace(spec, dtype="f16", bias=True)
+    t = _relu_inputs(spec, 9)
+    add = ROUND["f16"](np.random.default_rng(1).standard_normal(t["x"].shape).astype(np.float32))
+    got = _packed_pass(spec, t, add, True, begin=True)
+    _compare(spec, t, got, _reference(spec, t, add, True), add, True)

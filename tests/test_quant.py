@@ -1,0 +1,180 @@
+"""Deploy mode in 8-bit integers: convbn_deploy_prepare_quant, convbn_deploy_fwd_quant."""
+import numpy as np
+import pytest
+
+from oracle import packed_oracle as P
+from paper_2305_11624_b200 import convbn as C
+from paper_2305_11624_b200 import inputs as I
+
+KIND = {"bf16": C.BF16, "f16": C.F16, "f32": C.F32}
+HALF_STEP = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}
+ROUND = {"bf16": I.round_bf16, "f16": lambda a: np.asarray(a, np.float16).astype(np.float32), "f32": lambda a: np.asarray(a, np.float32)}
+
+
+def _desc(n, ci, h, w, co, dtype="bf16", stride=1, **kw):
+    return C.Desc.make(n, ci, h, w, co, 1, 1, stride, stride, dtype=KIND[dtype], layout=C.NCHW if dtype == "f32" else C.NHWC, **kw)
+
+
+# ---- host ------------------------------------------------------------------------------------------------------------
+def test_which_layers_are_taken():
+    size = lambda d: C.convbn_workspace_bytes(d, C.PHASE_DEPLOY_FWD_QUANT)
+    refused = [C.Desc.make(2, 64, 8, 8, 64, 3, 3, 1, 1, 1, 1), C.Desc.make(2, 64, 8, 8, 64, 1, 1, 1, 1, 1, 0),
+               C.Desc.make(2, 64, 8, 8, 64, 1, 1, groups=2), _desc(2, 64, 8, 8, 64, "f32"), _desc(1, 131073, 1, 1, 64)]
+    for d in refused:
+        assert size(d) == 0
+        for call in (lambda: C.convbn_deploy_fwd_quant(d, 4096, 4096, 4096, 4096, 4096, None, False, 4096, 1 << 30, stream=0),
+                     lambda: C.convbn_deploy_prepare_quant(d, 4096, None, 4096, 4096, 4096, 4096, 4096, 4096, 4096, stream=0)):
+            with pytest.raises(C.ConvBNError) as e:
+                call()
+            assert e.value.status == C.EUNSUPPORTED
+
+
+def test_refusals():
+    d = _desc(2, 64, 8, 8, 64)
+    size = C.convbn_workspace_bytes(d, C.PHASE_DEPLOY_FWD_QUANT)
+    names = ("x", "w_codes", "w_scale", "b_fused", "z", "add")
+
+    def forward(desc=d, ws=4096, bytes_=size, **over):
+        a = {n: None if n == "add" else 4096 for n in names}
+        a.update(over)
+        with pytest.raises(C.ConvBNError) as e:
+            C.convbn_deploy_fwd_quant(desc, *[a[n] for n in names], False, ws, bytes_, stream=0)
+        return e.value.status
+
+    for n in names:
+        if n != "add":
+            assert forward(**{n: None}) == C.EINVAL, n
+        assert forward(**{n: 4096 + (2 if n in ("w_scale", "b_fused") else 8)}) == C.EALIGN, n
+    if size:
+        assert forward(ws=None) == C.EWORKSPACE and forward(bytes_=size - 1) == C.EWORKSPACE and forward(ws=4096 + 16) == C.EALIGN
+    assert forward(desc=_desc(0, 64, 8, 8, 64)) == C.EINVAL
+    assert forward(desc=C.Desc.make(2, 64, 8, 8, 64, 1, 1, dtype=C.F16, layout=C.NCHW)) == C.EUNSUPPORTED
+    named = ("w", "b", "gamma", "beta", "run_mean", "run_var", "w_codes", "w_scale", "b_fused")
+
+    def prepare(**over):
+        a = {n: None if n == "b" else 4096 for n in named}
+        a.update(over)
+        with pytest.raises(C.ConvBNError) as e:
+            C.convbn_deploy_prepare_quant(d, *[a[n] for n in named], stream=0)
+        return e.value.status
+
+    for n in named:
+        if n != "b":
+            assert prepare(**{n: None}) == C.EINVAL, n
+        assert prepare(**{n: 4096 + (8 if n in ("w", "w_codes") else 2)}) == C.EALIGN, n
+
+
+def test_the_definition_is_within_its_rounding_of_the_plain_block():
+    """Against the unrounded product: an operand is off by half a step of its row, so a sum of K products is off by at most
+    (a_x / 254) sum |w| + (a_w / 254) sum |xhat|, both ends worst."""
+    rng = np.random.default_rng(2)
+    x, w = rng.standard_normal((17, 40)), rng.standard_normal((9, 40))
+    one, zero = np.ones(9), np.zeros(9)
+    got = P.deploy_forward(x, w, None, one, zero, zero, one, 0.0)
+    ax, aw = np.abs(x).max(1), np.abs(w).max(1)
+    bound = ax[:, None] / 254 * np.abs(w).sum(1) + aw[None, :] / 254 * (np.abs(x).sum(1)[:, None] + 40 * ax[:, None] / 254)
+    assert np.all(np.abs(got["z"] - x @ w.T) <= bound * (1 + 1e-5))
+
+
+# ---- device ----------------------------------------------------------------------------------------------------------
+def _draw(n, ci, h, w, co, dtype, stride, bias, with_add, seed=0):
+    rng = np.random.default_rng(seed + n + ci + co)
+    r = lambda a: ROUND[dtype](a.astype(np.float32)).astype(np.float64)
+    ho, wo = (h - 1) // stride + 1, (w - 1) // stride + 1
+    f32 = lambda a: a.astype(np.float32).astype(np.float64)
+    t = dict(x=r(rng.standard_normal((n, h, w, ci)) * np.exp(rng.standard_normal(ci))), w=r(rng.standard_normal((co, ci)) * np.sqrt(2.0 / ci)),
+             b=f32(rng.standard_normal(co)) if bias else None, gamma=f32(rng.uniform(0.5, 1.5, co) * np.sign(rng.standard_normal(co))),
+             beta=f32(rng.standard_normal(co) * 0.1), mu_hat=f32(rng.standard_normal(co) * 0.1), var_hat=f32(rng.uniform(0.5, 2.0, co)))
+    t["add"] = r(rng.standard_normal((n * ho * wo, co))) if with_add else None
+    return t
+
+
+def _run(t, desc, dtype, relu, ws_fill=0xFF):
+    import torch
+    td = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[dtype]
+    dev = lambda a, d=torch.float32: None if a is None else torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda().to(d)
+    co, ci = t["w"].shape
+    ho, wo = C.convbn_out_shape(desc)
+    rows, pitch = desc.n * ho * wo, -(-ci // 16) * 16
+    codes = torch.full((co * pitch + 64,), 99, dtype=torch.int8, device="cuda")
+    scale, shift = torch.full((co + 4,), 5.0, device="cuda"), torch.full((co + 4,), 5.0, device="cuda")
+    C.convbn_deploy_prepare_quant(desc, dev(t["w"], td), dev(t["b"]), dev(t["gamma"]), dev(t["beta"]), dev(t["mu_hat"]), dev(t["var_hat"]),
+                                  codes, scale, shift)
+    z = torch.full((rows * co + 64,), 9.0, dtype=td, device="cuda")
+    size = C.convbn_workspace_bytes(desc, C.PHASE_DEPLOY_FWD_QUANT)
+    room = torch.full((size + 256,), ws_fill, dtype=torch.uint8, device="cuda")
+    C.convbn_deploy_fwd_quant(desc, dev(t["x"], td), codes, scale, shift, z, dev(t["add"], td), relu, room, size)
+    C.convbn_check()
+    assert bool((room[size:] == ws_fill).all()) and bool((z[rows * co:] == 9.0).all())
+    assert bool((codes[co * pitch:] == 99).all()) and bool((scale[co:] == 5.0).all()) and bool((shift[co:] == 5.0).all())
+    f = lambda a: a.float().cpu().numpy().astype(np.float64)
+    return {"z": f(z[:rows * co]).reshape(rows, co), "w_codes": codes[:co * pitch].cpu().numpy().reshape(co, pitch),
+            "w_scale": f(scale[:co]), "b_fused": f(shift[:co])}
+
+
+def _check(got, t, dtype, stride, relu):
+    x = t["x"][:, ::stride, ::stride].reshape(-1, t["w"].shape[1])
+    ref = P.deploy_forward(x, t["w"], t["b"], t["gamma"], t["beta"], t["mu_hat"], t["var_hat"], 1e-5, t["add"], relu)
+    ci = t["w"].shape[1]
+    assert np.array_equal(got["w_codes"][:, :ci], ref["w_codes"]) and not got["w_codes"][:, ci:].any()
+    # var + eps, root, reciprocal, gamma r, a / 127, their product: six roundings
+    tiny = 2.0 ** -24
+    assert np.all(np.abs(got["w_scale"] - ref["w_scale"]) <= 6 * tiny * np.abs(ref["w_scale"]))
+    parts = np.abs((0 if t["b"] is None else t["b"])) + np.abs(t["mu_hat"])
+    s = np.abs(t["gamma"]) / np.sqrt(t["var_hat"] + 1e-5)
+    assert np.all(np.abs(got["b_fused"] - ref["b_fused"]) <= 8 * tiny * (parts * s + np.abs(t["beta"])))
+    # the sum as a float, a / 127 of the row, the channel's scale (six), two products and the shift (eight of its own), the
+    # addend; then one rounding to the storage type (2^-25: half of half precision's smallest number)
+    arithmetic = 10 * tiny * np.abs(ref["product"]) + 8 * tiny * (parts * s + np.abs(t["beta"])) + tiny * np.abs(ref["before_add"])
+    u = HALF_STEP[dtype] * (1 + 2.0 ** -6)
+    total = ref["before_add"] if t["add"] is None else ref["before_add"] + t["add"]
+    bound = arithmetic + (u + tiny) * np.abs(total) + 2.0 ** -25
+    err = np.abs(got["z"] - ref["z"])
+    assert np.all(err <= bound), float((err / bound).max())
+
+
+SIZES = [(1, 1, 1, 1, 1), (1, 64, 1, 1, 64), (1, 2048, 1, 1, 1000), (2, 500, 1, 1, 10), (7, 256, 1, 1, 129), (16, 24, 1, 1, 2048),
+         (17, 130, 1, 1, 40), (33, 1024, 1, 1, 256), (100, 512, 1, 1, 130), (128, 64, 1, 1, 64), (129, 96, 1, 1, 200), (300, 2000, 1, 1, 72),
+         (1000, 256, 1, 1, 64), (2, 64, 13, 11, 256), (3, 256, 9, 15, 64), (1, 1024, 14, 14, 512), (2, 2048, 7, 7, 512), (5, 8, 3, 7, 8),
+         (40, 512, 7, 7, 2048), (6, 192, 21, 19, 320)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_forward_against_the_definition(size, dtype):
+    n, ci, h, w, co = size
+    if dtype == "f32" and h * w > 1:
+        n, h, w = n * h * w, 1, 1
+    for bias, with_add, relu in ((False, False, False), (True, True, True)):
+        t = _draw(n, ci, h, w, co, dtype, 1, bias, with_add)
+        _check(_run(t, _desc(n, ci, h, w, co, dtype), dtype, relu), t, dtype, 1, relu)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [(2, 256, 15, 14, 512), (1, 40, 7, 9, 24), (3, 512, 28, 28, 128)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("stride", [2, 3])
+def test_strided_shortcuts(size, stride):
+    n, ci, h, w, co = size
+    t = _draw(n, ci, h, w, co, "bf16", stride, True, True)
+    _check(_run(t, _desc(n, ci, h, w, co, "bf16", stride), "bf16", True), t, "bf16", stride, True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [3, 200])
+def test_rows_and_channels_that_are_zero_tiny_infinite_or_not_numbers(rows):
+    t = _draw(rows, 128, 1, 1, 64, "bf16", 1, True, False)
+    t["x"][0] = 0.0
+    t["x"][1] = ROUND["bf16"](np.full((1, 1, 128), 1e-35, np.float32))
+    t["w"][5] = 0.0
+    t["w"][6] = ROUND["bf16"](np.full(128, 1e-33, np.float32))
+    t["gamma"][7] = 0.0
+    _check(_run(t, _desc(rows, 128, 1, 1, 64), "bf16", False), t, "bf16", 1, False)
+    t["x"][2, 0, 0, 77] = np.inf
+    t["x"][rows - 1, 0, 0, 0] = np.nan
+    t["w"][9, 3] = -np.inf
+    got = _run(t, _desc(rows, 128, 1, 1, 64), "bf16", False)["z"]
+    bad = np.zeros((rows, 64), bool)
+    bad[[2, rows - 1]] = True
+    bad[:, 9] = True
+    assert np.array_equal(np.isnan(got), bad) and np.isfinite(got[~bad]).all()
