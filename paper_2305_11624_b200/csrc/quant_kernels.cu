@@ -8,28 +8,15 @@
 // rounded.  The sum is exact in 32 bits up to C_in = 131072; a code is the rounding of the exact product x * fl(127 / a), formed
 // by one fused multiply-add, so it does not depend on how a compiler or a library rounds in between.
 #include "kernels.h"
+#include "quant8.cuh"
 
 namespace convbn {
 
 namespace {
 
-// Largest magnitudes below this count as zero: 127 / a would not be finite.
-constexpr float kTiny = 7.8886091e-31f;      // 2^-100
-
 // |x| as bits: the largest one is the largest magnitude, and an infinity or a NaN is above every number.
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-
-struct RowScale { float inv, scale; };       // 127 / a, a / 127
-__device__ __forceinline__ RowScale row_scale(uint32_t top) {
-    const float a = __uint_as_float(top);
-    if (top >= 0x7F800000u) return {0.f, __uint_as_float(0x7FC00000u)};     // (codes 0, scale NaN: so is every result)
-    if (a < kTiny) return {0.f, 0.f};
-    return {__fdiv_rn(127.f, a), __fdiv_rn(a, 127.f)};
-}
-// The code in the low byte: |x inv| <= 127 (1 + 2^-24), so no clamp.
-__device__ __forceinline__ uint32_t code_of(float x, float inv) {
-    return inv == 0.f ? 0u : __float_as_uint(fmaf(x, inv, 12582912.f)) & 0xFFu;
-}
+__device__ __forceinline__ uint32_t code_of(float x, float inv) { return inv == 0.f ? 0u : code_bits(x, inv) & 0xFFu; }
 
 template <class T>
 __global__ void __launch_bounds__(256) quant_weights_kernel(int c_in, int pitch, const T *__restrict__ w, const float *__restrict__ b,

@@ -15,6 +15,8 @@ namespace convbn {
 // Row-major matrix [rows][cols], box = box_rows x box_cols.
 bool make_tmap_matrix_bf16(CUtensorMap *tm, const void *base, long long rows, long long cols, int box_rows,
                            int box_cols);
+// Row-major matrix of 1-, 2- or 4-byte elements, rows multiples of 16 bytes: box = box_rows x 128 bytes.
+bool make_tmap_matrix_bytes(CUtensorMap *tm, const void *base, long long rows, long long cols, int elem_bytes, int box_rows);
 // NHWC tensor in im2col mode: `pixels` output positions x `channels` channels per load.
 bool make_tmap_im2col_bf16(CUtensorMap *tm, const void *base, int n, int h, int w, int c, int lower_h,
                            int lower_w, int upper_h, int upper_w, int stride_h, int stride_w, int pixels,
