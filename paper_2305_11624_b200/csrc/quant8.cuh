@@ -2,6 +2,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "packed_f32.cuh"
 #include "sm100_ptx.cuh"
 
 namespace convbn {
@@ -38,6 +39,11 @@ struct Eight {
             w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
         }
     }
+    __device__ __forceinline__ void load_shared(uint32_t at) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(at + 4u * i) : "memory");
+    }
     __device__ __forceinline__ void load_some(const T *p, int count) {      // any alignment, the rest zero
         zero();
 #pragma unroll
@@ -47,38 +53,49 @@ struct Eight {
             else w[i] = __ldg((const unsigned int *)p + i);
         }
     }
-    // Largest magnitude as bits: |x| as an integer, in two halves for 16-bit types (see top_f32).
+    // Largest magnitude as bits (16-bit types: the same in both halves); a NaN stays, and lies above every number.
     __device__ __forceinline__ uint32_t top() const {
-        uint32_t m = 0;
+        if constexpr (sizeof(T) == 2) {
+            uint32_t m = w[0];
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            if constexpr (sizeof(T) == 2) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
-            else m = max(m, w[i] & 0x7FFFFFFFu);
+            for (int i = 1; i < kWords; ++i) m = larger(m, w[i]);
+            return merge(m);
+        } else {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
+            return m;
         }
-        return m;
     }
-    static __device__ __forceinline__ uint32_t max_top(uint32_t a, uint32_t b) {
-        if constexpr (sizeof(T) == 2) return __vmaxu2(a, b);
-        else return max(a, b);
+    // of the larger magnitudes of two words' halves (16-bit types; the signs are any)
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        uint32_t r;
+        if constexpr (__is_same(T, __half)) asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
     }
-    // ... as an fp32 number's bits
+    static __device__ __forceinline__ uint32_t merge(uint32_t m) {
+        return larger(m, __byte_perm(m, m, 0x1032)) & 0x7FFF7FFFu;
+    }
+    // of a largest magnitude as bits, that number's bits as fp32
     static __device__ __forceinline__ uint32_t top_f32(uint32_t m) {
         if constexpr (sizeof(T) == 4) return m;
-        m = max(m & 0xFFFFu, m >> 16);
-        if constexpr (__is_same(T, __half)) return __float_as_uint(unpack_h16((uint16_t)m, 1));
-        else return m << 16;
+        else if constexpr (__is_same(T, __half)) return __float_as_uint(unpack_h16((uint16_t)m, 1));
+        else return m & 0xFFFF0000u;
     }
+    // (inv = 0: codes 0, but of an infinity or a NaN, whose row's scale is NaN)
     __device__ __forceinline__ uint2 codes(float inv) const {
+        const f32x2 by = pair(inv, inv), magic = pair(12582912.f, 12582912.f);
         uint32_t t[8];
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            float a, b;
-            if constexpr (sizeof(T) == 2) unpack2_t<__is_same(T, __half)>(w[i / 2], a, b);
-            else { a = __uint_as_float(w[i]); b = __uint_as_float(w[i + 1]); }
-            t[i] = code_bits(a, inv);
-            t[i + 1] = code_bits(b, inv);
+            f32x2 v;
+            if constexpr (sizeof(T) == 2) v = widen_t<__is_same(T, __half)>(w[i / 2]);
+            else v = pair(__uint_as_float(w[i]), __uint_as_float(w[i + 1]));
+            v = fma2(v, by, magic);
+            t[i] = (uint32_t)v;
+            t[i + 1] = (uint32_t)(v >> 32);
         }
-        if (inv == 0.f) return make_uint2(0u, 0u);
         return make_uint2(pack_bytes(t[0], t[1], t[2], t[3]), pack_bytes(t[4], t[5], t[6], t[7]));
     }
 };

@@ -2,11 +2,13 @@
 // memory, the product runs on the tensor cores (tcgen05, 8-bit operands, 32-bit integer sums in tensor memory), scales, shift,
 // addend and ReLU are applied to the sums.  X is read once in its storage type, Z written once; codes exist on chip only.
 //
-// CTA = 18 warps: 0 weight tiles (TMA), 1 MMA issuer and owner of tensor memory, 2-9 epilogue (two groups of four, an accumulator
-// each), 10-17 rows to codes.  A unit of work is 128 rows (and a span of channel tiles where there are few rows): the last eight
-// warps read its rows whole, a row by 8, 16 or 32 lanes, find the largest magnitude, and write the codes as the K-major A operand
-// (128-byte swizzle); the next rows are requested before these are converted.
+// CTA = 19 warps: 0 weight tiles (TMA), 1 MMA issuer and owner of tensor memory, 2-9 epilogue (two groups of four, an accumulator
+// each), 10-17 rows to codes, 18 brings the rows.  A unit of work is 128 rows (and a span of channel tiles where there are few rows): eight warps
+// read its rows whole, a row by 8, 16 or 32 lanes, find the largest magnitude, and write the codes as the K-major A operand
+// (128-byte swizzle).  Rows on 16-byte boundaries arrive by bulk copies of up to
+// 16 KB in a ring (by loads into registers, a batch ahead, 256 -> 64 at 56 x 56, N = 256 took 143 us).
 #include "kernels.h"
+#include "mma_sync.cuh"
 #include "quant8.cuh"
 
 namespace convbn {
@@ -17,11 +19,13 @@ namespace {
 
 constexpr int kQRows = 128;                      // rows of a unit (UMMA M)
 constexpr uint32_t kQBlock = kQRows * 128;       // [128 rows][128 codes] of the A operand
-constexpr int kQThreads = 576;
+constexpr int kQThreads = 608;
 constexpr int kQLoadWarp = 10;                   // first of the eight warps that make codes
+constexpr int kQRowWarp = 18;                    // brings the rows
 constexpr int kQMaxStages = 8;
 constexpr uint32_t kQStage = 32 * 128;           // an epilogue warp's box: [32 rows][128 bytes]
 constexpr int kQSlots = 4;                       // row scales of so many units
+constexpr int kQMaxDepth = 8;                    // slots of the ring of rows
 
 struct QuantFused {
     RowMap rows;
@@ -30,11 +34,12 @@ struct QuantFused {
     uint32_t units, n_tiles, per_part;           // per_part: channel tiles of a unit
     FastDiv by_parts;                            // units of the same rows
     int abufs, stages, nbuf, resident;           // A buffers, slots of streamed weights, boxes of an epilogue warp
+    int depth;                                   // slots of the ring of rows
     int vec, dense, relu;                        // rows of X (of Z) start on 16-byte boundaries
 };
 
 struct QuantCtl {
-    uint64_t full[kQMaxStages], empty[kQMaxStages], wfull, a_full[2], a_empty[2], xs_full[kQSlots], acc_full[2], acc_empty[2], add_full[8];
+    uint64_t rows_full[kQMaxDepth], rows_empty[kQMaxDepth], full[kQMaxStages], empty[kQMaxStages], wfull, a_full[2], a_empty[2], xs_full[kQSlots], acc_full[2], acc_empty[2], add_full[8];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -53,8 +58,16 @@ __device__ __forceinline__ void umma_s8(uint32_t d, uint32_t a_lo, uint32_t a_hi
         : "memory");
 }
 
-// LPR lanes read a row, 8 CPL LPR elements at most.
-template <class T, int LPR, int CPL>
+// A converting warp's rows of a unit: RPI of them an instruction (a set), BATCH sets at a time, at most 4 KB.  Half a batch of all
+// eight warps, side by side, is a slot of the ring.
+template <class T, int LPR, int CPL> struct RowSets {
+    static constexpr int RPI = 32 / LPR, SETS = 16 / RPI, SET_BYTES = 256 * CPL * (int)sizeof(T);
+    static constexpr int BATCH = SETS * SET_BYTES <= 4096 ? SETS : 4096 / SET_BYTES, BATCHES = SETS / BATCH;
+};
+template <class T, int LPR, int CPL> constexpr uint32_t kSlotBytes = (uint32_t)(8 * RowSets<T, LPR, CPL>::BATCH * RowSets<T, LPR, CPL>::SET_BYTES / 2);
+
+// LPR lanes read a row, 8 CPL LPR elements at most.  RING: rows start on 16-byte boundaries.
+template <class T, int LPR, int CPL, bool RING>
 __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_z,
                                                                 const __grid_constant__ CUtensorMap tm_add, const QuantFused g,
                                                                 const T *__restrict__ x, const float *__restrict__ ws,
@@ -65,8 +78,9 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
     const uint32_t a_bytes = (uint32_t)g.kb * kQBlock, w_bytes = (uint32_t)g.bn * 128;
     uint8_t *w_tiles = a_tiles + (size_t)g.abufs * a_bytes;
     uint8_t *staging = w_tiles + (size_t)(g.resident ? g.n_tiles * g.kb : g.stages) * w_bytes;
-    float *params = (float *)(staging + (size_t)8 * g.nbuf * kQStage);          // 8 warps x [scale 64 | shift 64]
-    float *xs_s = params + 8 * 128;                                             // [kQSlots][128]
+    uint8_t *ring = staging + (size_t)8 * g.nbuf * kQStage;
+    float *scale_s = (float *)(ring + (size_t)g.depth * kSlotBytes<T, LPR, CPL>), *shift_s = scale_s + g.n_tiles * g.bn;
+    float *xs_s = shift_s + g.n_tiles * g.bn;                                   // [kQSlots][128]
     QuantCtl *ctl = (QuantCtl *)(xs_s + kQSlots * kQRows);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *abort_flag = &ctl->abort_flag;
@@ -80,7 +94,11 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             mbar_init(&ctl->acc_full[s], 1); mbar_init(&ctl->acc_empty[s], 4);
         }
         for (int s = 0; s < kQSlots; ++s) mbar_init(&ctl->xs_full[s], 8);
-        for (int s = 0; s < 8; ++s) mbar_init(&ctl->add_full[s], 1);
+        for (int s = 0; s < 8; ++s) {
+            mbar_init(&ctl->add_full[s], 1);
+            mbar_init(&ctl->rows_full[s], 1);
+            mbar_init(&ctl->rows_empty[s], 8);
+        }
         ctl->abort_flag = 0;
         fence_barrier_init();
     }
@@ -162,81 +180,129 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     }
                     if (ok) umma_commit(&ctl->acc_full[acc]);
                 }
-                if (ok) umma_commit(&ctl->a_empty[ab]);
+                if (ok && u + g.abufs * gridDim.x < g.units) umma_commit(&ctl->a_empty[ab]);
             }
             if (!ok) give_up();
         }
-    } else if (warp >= kQLoadWarp) {
-        // ---- rows to codes: warp qw has rows 16 qw .. 16 qw + 15 of a unit, RPI of them an instruction, RB such sets a batch ----
-        constexpr int RPI = 32 / LPR, SETS = 16 / RPI;
-        constexpr int ROOM = (sizeof(T) == 2 ? 8 : 4) / CPL, RB = ROOM < SETS ? ROOM : SETS, BATCHES = SETS / RB;
-        const int qw = warp - kQLoadWarp, sub = lane & (LPR - 1), row_l = lane / LPR;
-        Eight<T> next[RB][CPL];
-        auto fetch = [&](uint32_t u, int batch) {
-            uint32_t m, a, b;
-            unit(u, m, a, b);
-#pragma unroll
-            for (int j = 0; j < RB; ++j) {
-                const uint32_t row = m * kQRows + qw * 16 + (batch * RB + j) * RPI + row_l;
-                const T *src = x + (row < g.p ? g.rows.at(row) : 0);
-#pragma unroll
-                for (int c = 0; c < CPL; ++c) {
-                    const int at = (c * LPR + sub) * 8;
-                    if (row >= g.p || at >= g.k) next[j][c].zero();
-                    else if (g.vec) next[j][c].load(src + at);
-                    else next[j][c].load_some(src + at, g.k - at);
+    } else if (warp == kQRowWarp) {
+        // ---- rows of X into the ring, a slot at a time: side by side one copy, otherwise one a row ----
+        if constexpr (RING) {
+            using R = RowSets<T, LPR, CPL>;
+            constexpr uint32_t ROWS = 8 * (R::BATCH / 2) * R::RPI;
+            const uint32_t row_bytes = (uint32_t)g.k * sizeof(T);
+            uint32_t slot = 0, ph = 1, asked = 0;
+            bool ok = true;
+            for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x) {
+                const uint32_t end = min((g.by_parts.div(u) + 1) * kQRows, g.p);
+                for (uint32_t first = g.by_parts.div(u) * kQRows; first < end; first += ROWS) {
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_empty[slot], ph, abort_flag));
+                    if (!ok) break;
+                    const uint32_t rows = min(ROWS, end - first);
+                    uint8_t *to = ring + (size_t)slot * kSlotBytes<T, LPR, CPL>;
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(&ctl->rows_full[slot], rows * row_bytes);
+                        if (!g.rows.strided) bulk_load(to, x + (size_t)first * g.k, rows * row_bytes, &ctl->rows_full[slot]);
+                    }
+                    if (g.rows.strided) {
+                        __syncwarp();
+                        for (uint32_t r = lane; r < rows; r += 32) bulk_load(to + (size_t)r * row_bytes, x + g.rows.at(first + r), row_bytes, &ctl->rows_full[slot]);
+                    }
+                    ++asked;
+                    if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
                 }
             }
-        };
+            if (!ok && lane == 0) {
+                give_up();
+                for (uint32_t j = asked > (uint32_t)g.depth ? asked - g.depth : 0; j < asked; ++j)        // let the copies in flight land
+                    mbar_wait_bounded(&ctl->rows_full[j % g.depth], (j / g.depth) & 1u, nullptr, 200000000ull);
+            }
+        }
+    } else if (warp >= kQLoadWarp) {
+        // ---- rows to codes: warp qw has the rows qw HALF RPI .. of every slot ----
+        // A batch's rows are read twice: for their largest magnitudes, and after these have become scales, which each lane works out
+        // for one row (a scale per four rows, and the rows kept in registers between: 1900 instructions a warp and unit instead of
+        // 700, 256 -> 64 at 56 x 56, N = 256 192 us).
+        using R = RowSets<T, LPR, CPL>;
+        constexpr int RPI = R::RPI, BATCH = R::BATCH, BATCHES = R::BATCHES, HALF = BATCH / 2;
+        constexpr int SLOT_ROWS = 8 * HALF * RPI;
+        const int qw = warp - kQLoadWarp, sub = lane & (LPR - 1), row_l = lane / LPR, own = qw * HALF * RPI + row_l;     // row in a slot
+        const uint32_t row_bytes = (uint32_t)g.k * sizeof(T), ring0 = smem_u32(ring);
+        uint32_t slot = 0, ph = 0;
+        // set j of a batch in its unit, as this lane has it
+        auto row_of = [&](int batch, int j) { return (2 * batch + j / HALF) * SLOT_ROWS + own + j % HALF * RPI; };
         bool ok = true;
         uint32_t i = 0;
-        if (blockIdx.x < g.units) fetch(blockIdx.x, 0);
         for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
             const uint32_t ab = g.abufs == 2 ? (i & 1u) : 0u, use = g.abufs == 2 ? (i >> 1) : i;
             uint8_t *tile = a_tiles + (size_t)ab * a_bytes;
-            float *xs = xs_s + (i % kQSlots) * kQRows + qw * 16;
+            float *xs = xs_s + (i % kQSlots) * kQRows;
+            const uint32_t first = g.by_parts.div(u) * kQRows;
 #pragma unroll 1
             for (int batch = 0; batch < BATCHES; ++batch) {
-                Eight<T> now[RB][CPL];
+                // set j of the batch as this lane has it
+                auto read = [&](Eight<T> (&v)[CPL], int j, uint32_t base) {
+                    const T *src = nullptr;
+                    if constexpr (!RING) src = x + g.rows.at(min(first + (uint32_t)row_of(batch, j), g.p - 1));
 #pragma unroll
-                for (int j = 0; j < RB; ++j)
+                    for (int c = 0; c < CPL; ++c) {
+                        const int at = (c * LPR + sub) * 8;
+                        if (at >= g.k) v[c].zero();
+                        else if (RING) v[c].load_shared(base + (uint32_t)(own + j % HALF * RPI) * row_bytes + (uint32_t)at * (uint32_t)sizeof(T));
+                        else if (g.vec) v[c].load(src + at);
+                        else v[c].load_some(src + at, g.k - at);
+                    }
+                };
+                uint32_t mine = 0, base[2], bar[2];
+                bool there[2];
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c) now[j][c] = next[j][c];
-                if (batch + 1 < BATCHES) fetch(u, batch + 1);
-                else if (u + gridDim.x < g.units) fetch(u + gridDim.x, 0);
-                uint32_t top[RB];
+                for (int h = 0; h < 2; ++h) {
+                    there[h] = !RING || first + (uint32_t)((2 * batch + h) * SLOT_ROWS) < g.p;       // (a slot past the last row never comes)
+                    base[h] = ring0 + slot * kSlotBytes<T, LPR, CPL>;
+                    bar[h] = slot;
+                    if (!there[h]) continue;
+                    if constexpr (RING) {
+                        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_full[slot], ph, abort_flag));
+                        if (!ok) break;
+                        if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
+                    }
 #pragma unroll
-                for (int j = 0; j < RB; ++j) {
-                    uint32_t t = now[j][0].top();
+                    for (int j = h * HALF; j < (h + 1) * HALF; ++j) {
+                        Eight<T> v[CPL];
+                        read(v, j, base[h]);
+                        uint32_t t = v[0].top();
+                        if constexpr (CPL == 2) t = max(t, v[1].top());
+                        if constexpr (LPR == 32) t = __reduce_max_sync(0xffffffffu, t);
+                        else
 #pragma unroll
-                    for (int c = 1; c < CPL; ++c) t = Eight<T>::max_top(t, now[j][c].top());
-                    t = Eight<T>::top_f32(t);
-                    if constexpr (LPR == 32) t = __reduce_max_sync(0xffffffffu, t);
-                    else
-#pragma unroll
-                        for (int o = LPR / 2; o > 0; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
-                    top[j] = t;
+                            for (int o = LPR / 2; o > 0; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
+                        mine = sub == j ? t : mine;           // lane j of a row's lanes has set j
+                    }
                 }
-                // lane j of a row's lanes works out the scales of its set j
-                uint32_t mine = top[0];
-#pragma unroll
-                for (int j = 1; j < RB; ++j) mine = (sub & (RB - 1)) == j ? top[j] : mine;
-                const RowScale rs = row_scale(mine);
+                if (!ok) break;
+                const RowScale rs = row_scale(Eight<T>::top_f32(mine));
                 if (batch == 0) {
                     ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->a_empty[ab], (use & 1u) ^ 1u, abort_flag));
                     if (!ok) break;
                 }
-                if (sub < RB) xs[(batch * RB + sub) * RPI + row_l] = rs.scale;
+                if (sub < BATCH) xs[row_of(batch, sub)] = rs.scale;
 #pragma unroll
-                for (int j = 0; j < RB; ++j) {
-                    const float inv = __shfl_sync(0xffffffffu, rs.inv, (lane & ~(LPR - 1)) + j);
-                    const int r = qw * 16 + (batch * RB + j) * RPI + row_l;
+                for (int h = 0; h < 2; ++h) {
+                    if (!there[h]) continue;
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c) {
-                        const int at = (c * LPR + sub) * 8;
-                        if (at < g.kb * 128)
-                            *(uint2 *)(tile + (size_t)(at >> 7) * kQBlock + r * 128 + ((((at >> 4) ^ r) & 7) << 4) + (at & 8)) = now[j][c].codes(inv);
+                    for (int j = h * HALF; j < (h + 1) * HALF; ++j) {
+                        Eight<T> v[CPL];
+                        read(v, j, base[h]);
+                        const float inv = __shfl_sync(0xffffffffu, rs.inv, (lane & ~(LPR - 1)) + j);
+                        const int r = row_of(batch, j);
+#pragma unroll
+                        for (int c = 0; c < CPL; ++c) {
+                            const int at = (c * LPR + sub) * 8;
+                            if (at < g.kb * 128)
+                                *(uint2 *)(tile + (size_t)(at >> 7) * kQBlock + r * 128 + ((((at >> 4) ^ r) & 7) << 4) + (at & 8)) = v[c].codes(inv);
+                        }
                     }
+                    __syncwarp();                             // every lane has read this half
+                    if (RING && lane == 0) mbar_arrive(&ctl->rows_empty[bar[h]]);
                 }
             }
             if (!ok) break;
@@ -247,12 +313,27 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         if (!ok && lane == 0) give_up();
     } else {
         // ---- epilogue ----
-        constexpr int CH = 128 / sizeof(T);                  // columns of a box
+        constexpr int CH = 128 / sizeof(T), PER = 16 / sizeof(T);      // columns of a box, of 16 bytes
         const int quarter = warp & 3, ew = warp - 2;
         const uint32_t egroup = (uint32_t)ew >> 2;
         uint8_t *boxes = staging + (size_t)ew * g.nbuf * kQStage;
-        float *par = params + ew * 128;
         uint64_t *add_bar = &ctl->add_full[ew];
+        for (int c = (int)threadIdx.x - 64; c < (int)g.n_tiles * g.bn; c += 256) {
+            scale_s[c] = c < g.n ? ws[c] : 0.f;
+            shift_s[c] = c < g.n ? shift[c] : 0.f;
+        }
+        named_bar_sync(1, 256);
+        // fragments of the accumulator (16-bit types): see umma_conv.cu
+        const uint32_t frag_row = (uint32_t)((lane & 7) + (lane & 8)) * 128u, frag_chunk = (uint32_t)(((lane >> 4) ^ (lane & 7)) << 4);
+        const f32x2 one = pair(1.f, 1.f), away = pair(-12582912.f, -12582912.f), none = pair(-0.f, -0.f);
+        // Sums times the row's scale.  Up to 256 products of codes lie below 2^22: added to the bits of 1.5 2^23 they are its low bits,
+        // and the conversion unit, a quarter as fast, is left alone.
+        auto scaled = [&](uint32_t a, uint32_t b, f32x2 xs2) {
+            if constexpr (LPR * CPL <= 32)
+                return fma2(fma2(pair(__uint_as_float(a + 0x4B400000u), __uint_as_float(b + 0x4B400000u)), one, away), xs2, none);
+            else
+                return fma2(pair((float)(int)a, (float)(int)b), xs2, none);
+        };
         bool ok = true;
         uint32_t i = 0, s = 0, m, nt, last, turn = 0, add_ph = 0;
         const bool boxed = g.dense && add;
@@ -275,7 +356,13 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                 };
                 if (g.dense) fetch_add(0);
                 ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->xs_full[i % kQSlots], (i / kQSlots) & 1u, abort_flag));
-                const float xs = ok ? xs_s[(i % kQSlots) * kQRows + quarter * 32 + lane] : 0.f;
+                const float *xs = xs_s + (i % kQSlots) * kQRows + quarter * 32;
+                f32x2 xs2[4];                    // 16-bit types: rows lane / 4 + 8 k, otherwise row `lane`
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float v1 = ok ? xs[g.dense && sizeof(T) == 2 ? lane / 4 + 8 * k : lane] : 0.f;
+                    xs2[k] = pair(v1, v1);
+                }
                 ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->acc_full[s & 1u], (s >> 1) & 1u, abort_flag));
                 if (!ok) {
                     if (boxed) { if (lane == 0) mbar_wait_bounded(add_bar, add_ph, nullptr, 200000000ull); __syncwarp(); }
@@ -285,64 +372,83 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                 const uint32_t t_row = tmem_base + (s & 1u) * (uint32_t)g.bn + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
                 for (int c0 = 0; c0 < cols; c0 += CH) {
-                    uint8_t *buf = box(), *brow = buf + lane * 128;
-#pragma unroll
-                    for (int c = lane; c < CH; c += 32) {
-                        const int col = n0 + c0 + c;
-                        par[c] = col < g.n ? __ldg(ws + col) : 0.f;
-                        par[64 + c] = col < g.n ? __ldg(shift + col) : 0.f;
-                    }
-                    __syncwarp();
+                    uint8_t *buf = box();
                     if (boxed) {
                         ok = __all_sync(0xffffffffu, mbar_wait_bounded(add_bar, add_ph, abort_flag));
                         add_ph ^= 1u;
                         if (!ok) break;
                     }
-#pragma unroll 1
-                    for (int h = 0; h < CH; h += 32) {
-                        uint32_t v[32];
-                        tmem_ld_32x32(t_row + (uint32_t)(c0 + h), v);
-                        tmem_ld_wait();
-                        float f[32];
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            const float4 w4 = *(const float4 *)(par + h + j), b4 = *(const float4 *)(par + 64 + h + j);
-                            f[j] = fmaf((float)(int)v[j] * xs, w4.x, b4.x);
-                            f[j + 1] = fmaf((float)(int)v[j + 1] * xs, w4.y, b4.y);
-                            f[j + 2] = fmaf((float)(int)v[j + 2] * xs, w4.z, b4.z);
-                            f[j + 3] = fmaf((float)(int)v[j + 3] * xs, w4.w, b4.w);
-                        }
+                    const float *ws_c = scale_s + n0 + c0, *b_c = shift_s + n0 + c0;
+                    bool boxed_done = false;
+                    if constexpr (sizeof(T) == 2) {
                         if (g.dense) {
-                            constexpr int PER = 16 / sizeof(T);
+                            boxed_done = true;
+                            constexpr bool H = __is_same(T, __half);
+                            const uint32_t ws_at = smem_u32(ws_c) + (uint32_t)(lane & 3) * 8u, b_at = smem_u32(b_c) + (uint32_t)(lane & 3) * 8u;
+                            const uint32_t frag = smem_u32(buf) + frag_row;
+                            auto rows16 = [&](auto add_tag, auto relu_tag) {
+                                constexpr bool ADD = decltype(add_tag)::value, RELU = decltype(relu_tag)::value;
 #pragma unroll
-                            for (int j = 0; j < 32; j += PER) {
-                                uint4 *at = (uint4 *)(brow + ((((h + j) / PER ^ lane) & 7) << 4));
-                                uint4 q = boxed ? *at : make_uint4(0u, 0u, 0u, 0u);
-                                uint32_t *w = (uint32_t *)&q;
+                                for (int h = 0; h < 2; ++h) {
+                                    uint32_t v[32];
+                                    tmem_ld_16x64(t_row + ((uint32_t)(16 * h) << 16) + (uint32_t)c0, v);
+                                    tmem_ld_wait();
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    if constexpr (sizeof(T) == 2) {
-                                        constexpr bool H = __is_same(T, __half);
-                                        float lo = f[j + 2 * e], hi = f[j + 2 * e + 1], al, ah;
-                                        if (boxed) { unpack2_t<H>(w[e], al, ah); lo += al; hi += ah; }
-                                        if (g.relu) { lo = fmaxf(lo, 0.f); hi = fmaxf(hi, 0.f); }
-                                        w[e] = pack2_t<H>(lo, hi);
-                                    } else {
-                                        float v1 = f[j + e];
+                                    for (int q = 0; q < 8; q += 2) {
+                                        uint32_t o[4], a[4];           // columns 8 q and 8 q + 8: rows 0-7, 8-15 of each
+                                        const uint32_t at16 = (uint32_t)h * 2048u + (((uint32_t)q << 4) ^ frag_chunk);
+                                        if constexpr (ADD) ldmatrix_x4(a[0], a[1], a[2], a[3], frag + at16);
+#pragma unroll
+                                        for (int e = 0; e < 4; ++e) {
+                                            const uint32_t *p2 = &v[(q + (e >> 1)) * 4 + (e & 1) * 2], off = (uint32_t)(8 * (q + (e >> 1))) * 4u;
+                                            f32x2 f = fma2(scaled(p2[0], p2[1], xs2[2 * h + (e & 1)]), lds_f32x2(ws_at + off), lds_f32x2(b_at + off));
+                                            if constexpr (ADD) f = fma2(f, one, widen_t<H>(a[e]));
+                                            o[e] = narrow_t<H>(f);
+                                            if constexpr (RELU) o[e] = post_pair<H>(o[e], false, 0u, true, false, 0u);
+                                        }
+                                        stmatrix_x4(frag + at16, o[0], o[1], o[2], o[3]);
+                                    }
+                                }
+                            };
+                            if (boxed) { if (g.relu) rows16(std::true_type(), std::true_type()); else rows16(std::true_type(), std::false_type()); }
+                            else { if (g.relu) rows16(std::false_type(), std::true_type()); else rows16(std::false_type(), std::false_type()); }
+                        }
+                    }
+                    if (!boxed_done) {
+#pragma unroll 1
+                        for (int h = 0; h < CH; h += 32) {
+                            uint32_t v[32];
+                            tmem_ld_32x32(t_row + (uint32_t)(c0 + h), v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 32; j += 2) {
+                                const f32x2 f2 = fma2(scaled(v[j], v[j + 1], xs2[0]), *(const f32x2 *)(ws_c + h + j), *(const f32x2 *)(b_c + h + j));
+                                v[j] = (uint32_t)f2;
+                                v[j + 1] = (uint32_t)(f2 >> 32);
+                            }
+                            if (sizeof(T) == 4 && g.dense) {
+#pragma unroll
+                                for (int j = 0; j < 32; j += PER) {
+                                    uint4 *at = (uint4 *)(buf + lane * 128 + ((((j / PER) ^ lane) & 7) << 4));
+                                    uint4 q = boxed ? *at : make_uint4(0u, 0u, 0u, 0u);
+                                    uint32_t *w = (uint32_t *)&q;
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        float v1 = __uint_as_float(v[j + e]);
                                         if (boxed) v1 += __uint_as_float(w[e]);
                                         w[e] = __float_as_uint(g.relu ? fmaxf(v1, 0.f) : v1);
                                     }
+                                    *at = q;
                                 }
-                                *at = q;
-                            }
-                        } else if (row < g.p) {
+                            } else if (row < g.p) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                if (c0 + h + j >= cols) continue;
-                                const size_t at = (size_t)row * g.n + n0 + c0 + h + j;
-                                float v1 = f[j];
-                                if (add) v1 += to_f32(add[at]);
-                                z[at] = from_f32<T>(g.relu ? fmaxf(v1, 0.f) : v1);
+                                for (int j = 0; j < 32; ++j) {
+                                    if (c0 + h + j >= cols) continue;
+                                    const size_t at = (size_t)row * g.n + n0 + c0 + h + j;
+                                    float v1 = __uint_as_float(v[j]);
+                                    if (add) v1 += to_f32(add[at]);
+                                    z[at] = from_f32<T>(g.relu ? fmaxf(v1, 0.f) : v1);
+                                }
                             }
                         }
                     }
@@ -361,7 +467,6 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                         turn ^= 1u;
                         if (c0 + CH < cols) fetch_add(c0 + CH);
                     }
-                    __syncwarp();
                 }
             }
         }
@@ -374,14 +479,15 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
 }
 
 // Shared memory of a choice of buffers; 0: they do not fit.
-size_t fused_smem(const QuantFused &g) {
+size_t fused_smem(const QuantFused &g, size_t slot) {
     const size_t w = (size_t)(g.resident ? (int)g.n_tiles * g.kb : g.stages) * g.bn * 128;
-    return 1024 + (size_t)g.abufs * g.kb * kQBlock + w + (size_t)8 * g.nbuf * kQStage + 8 * 512 + kQSlots * kQRows * 4 + sizeof(QuantCtl) + 16;
+    return 1024 + (size_t)g.abufs * g.kb * kQBlock + w + (size_t)8 * g.nbuf * kQStage + g.depth * slot + 8 * (size_t)g.n_tiles * g.bn +
+           kQSlots * kQRows * 4 + sizeof(QuantCtl) + 16;
 }
 
 }  // namespace
 
-bool quant_fused_eligible(const Problem &pb) { return pb.c_in <= 1024; }
+bool quant_fused_eligible(const Problem &pb) { return pb.c_in <= 512 && pb.c_out <= 2048; }
 
 RowMap quant_row_map(const Problem &pb) {
     RowMap r;
@@ -416,29 +522,33 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
         g.by_parts = FastDiv(parts);
         g.units = m_tiles * parts;
     };
-    // Buffers, the most wanted first: two of the A operand (rows are converted while others are multiplied), the weights resident
-    // or at least three slots of them, wide tiles, two boxes per epilogue warp.
-    const size_t room = 227 * 1024;
+    // Buffers, the most wanted first: two of the A operand (rows are converted while others are multiplied) and six slots of
+    // rows (two are in use, the others on their way), then two boxes per epilogue warp; the weights
+    // resident where a CTA has all of them to itself, otherwise at least three slots; wide tiles.
+    const size_t room = 227 * 1024, lanes = pb.c_in <= 64 ? 8 : (pb.c_in <= 128 ? 16 : 32), set = 256 * es * (pb.c_in > 256 ? 2 : 1);
+    const size_t slot = 8 * (lanes / 2 * set <= 4096 ? lanes / 2 * set : 4096) / 2;         // (kSlotBytes)
+    const struct { int abufs, nbuf, depth; } wanted[] = {{2, 2, 6}, {2, 1, 6}, {2, 1, 4}, {1, 2, 6}, {1, 1, 4}, {1, 1, 2}};
     size_t smem = 0;
-    for (g.abufs = 2; g.abufs > 0 && !smem; --g.abufs)
+    for (const auto &c : wanted) {
+        g.abufs = c.abufs; g.nbuf = c.nbuf; g.depth = g.vec ? c.depth : 0; g.stages = 3;
         for (int widest = many ? 256 : 64; widest >= (many && g.abufs == 2 ? 128 : 64) && !smem; widest /= 2) {
             tiles(widest);
-            for (int choice = 0; choice < 4 && !smem; ++choice) {
-                g.resident = choice < 2;
-                g.nbuf = 2 - (choice & 1);
-                g.stages = 3;
-                if (g.resident && (g.by_parts.d != 1 || m_tiles < (uint32_t)sms)) continue;
-                if (fused_smem(g) > room) continue;
-                while (!g.resident && g.stages < kQMaxStages) {
-                    ++g.stages;
-                    if (fused_smem(g) > room) { --g.stages; break; }
-                }
-                smem = fused_smem(g);
-            }
+            for (g.resident = g.by_parts.d == 1 && m_tiles >= (uint32_t)sms; g.resident >= 0 && !smem; --g.resident)
+                if (fused_smem(g, slot) <= room) { smem = fused_smem(g, slot); break; }
             if (smem) break;
         }
+        if (smem) break;
+    }
     if (!smem) return cudaErrorInvalidValue;
-    ++g.abufs;                                         // (the loop's last step)
+    while (!g.resident && g.stages < 4) {
+        ++g.stages;
+        if (fused_smem(g, slot) > room) { --g.stages; break; }
+    }
+    while (g.vec && g.depth < kQMaxDepth) {
+        ++g.depth;
+        if (fused_smem(g, slot) > room) { --g.depth; break; }
+    }
+    smem = fused_smem(g, slot);
     const unsigned grid = g.units < (uint32_t)sms ? g.units : (unsigned)sms;
     CUtensorMap tw, tz, ta;
     if (!make_tmap_matrix_bytes(&tw, wq, pb.c_out, quant_pitch(pb), 1, g.bn)) return cudaErrorInvalidValue;
@@ -449,21 +559,24 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
     }
     int *err = nullptr;
     if (cudaError_t e = error_word_address(&err); e != cudaSuccess) return e;
-    auto go = [&](auto tag, auto lpr, auto cpl) {
+    auto go = [&](auto tag, auto lpr, auto cpl, auto rows) {
         using T = decltype(tag);
-        auto kernel = quant_fused_kernel<T, decltype(lpr)::value, decltype(cpl)::value>;
+        auto kernel = quant_fused_kernel<T, decltype(lpr)::value, decltype(cpl)::value, decltype(rows)::value>;
         static PerDevice attr, carve;
         if (cudaError_t e = max_dynamic_smem_once(kernel, 227 * 1024, &attr); e != cudaSuccess) return e;
         prefer_max_shared_once(kernel, &carve);
         return launch_pdl(kernel, dim3(grid), dim3(kQThreads), smem, st, tw, tz, ta, g, (const T *)x, ws, shift, (const T *)add, (T *)z, err);
     };
+    auto sized = [&](auto tag, auto lpr, auto cpl) {
+        if (g.vec) return go(tag, lpr, cpl, std::true_type());
+        return go(tag, lpr, cpl, std::false_type());
+    };
     auto typed = [&](auto tag) {
         using std::integral_constant;
-        if (pb.c_in <= 64) return go(tag, integral_constant<int, 8>(), integral_constant<int, 1>());
-        if (pb.c_in <= 128) return go(tag, integral_constant<int, 16>(), integral_constant<int, 1>());
-        if (pb.c_in <= 256) return go(tag, integral_constant<int, 32>(), integral_constant<int, 1>());
-        if (pb.c_in <= 512) return go(tag, integral_constant<int, 32>(), integral_constant<int, 2>());
-        return go(tag, integral_constant<int, 32>(), integral_constant<int, 4>());
+        if (pb.c_in <= 64) return sized(tag, integral_constant<int, 8>(), integral_constant<int, 1>());
+        if (pb.c_in <= 128) return sized(tag, integral_constant<int, 16>(), integral_constant<int, 1>());
+        if (pb.c_in <= 256) return sized(tag, integral_constant<int, 32>(), integral_constant<int, 1>());
+        return sized(tag, integral_constant<int, 32>(), integral_constant<int, 2>());
     };
     return dtype == CONVBN_F32 ? typed(float()) : (dtype == CONVBN_F16 ? typed(__half()) : typed(__nv_bfloat16()));
 }
