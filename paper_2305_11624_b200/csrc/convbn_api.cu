@@ -1446,9 +1446,9 @@ int convbn_deploy_fwd_quant(const convbn_desc *desc, const void *x, const void *
     }
     float *xs = (float *)at(workspace, pl.inner);
     LAUNCH("quant_rows", launch_quant_rows(pb, storage_type(desc), x, at(workspace, pl.unpacked), xs, st));
-    LAUNCH("quant_product", launch_quant_product(pb, storage_type(desc), at(workspace, pl.unpacked), xs, w_codes, w_scale, b_fused, add,
-                                                 relu ? 1 : 0, z, st));
-    t_last_kernel[CONVBN_PHASE_DEPLOY_FWD_QUANT] = "direct";
+    LAUNCH("quant_gemm", launch_quant_gemm(pb, storage_type(desc), at(workspace, pl.unpacked), xs, w_codes, w_scale, b_fused, add,
+                                           relu ? 1 : 0, z, st));
+    t_last_kernel[CONVBN_PHASE_DEPLOY_FWD_QUANT] = "umma";
     return CONVBN_OK;
 }
 

@@ -338,13 +338,14 @@ inline int quant_pitch(const Problem &pb) { return (pb.c_in + 15) / 16 * 16; }
 size_t quant_codes_bytes(const Problem &pb);
 cudaError_t launch_quant_weights(const Problem &pb, int dtype, const void *w, const float *b, const float *gamma, const float *beta,
                                  const float *mean, const float *var, void *codes, float *scale, float *shift, cudaStream_t st);
-// codes [p][pitch], scale [p]: of the rows of X that the output pixels read
-cudaError_t launch_quant_rows(const Problem &pb, int dtype, const void *x, void *codes, float *scale, cudaStream_t st);
 // Rows to codes and product in one kernel (quant_fused.cu).
 bool quant_fused_eligible(const Problem &pb);
 cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, const void *wq, const float *ws, const float *shift,
                                const void *add, int relu, void *z, cudaStream_t st);
-cudaError_t launch_quant_product(const Problem &pb, int dtype, const void *xq, const float *xs, const void *wq, const float *ws,
-                                 const float *shift, const void *add, int relu, void *z, cudaStream_t st);
+// The two as kernels of their own (quant_gemm.cu).
+// codes [p][pitch], scale [p]: of the rows of X that the output pixels read
+cudaError_t launch_quant_rows(const Problem &pb, int dtype, const void *x, void *codes, float *scale, cudaStream_t st);
+cudaError_t launch_quant_gemm(const Problem &pb, int dtype, const void *xq, const float *xs, const void *wq, const float *ws,
+                              const float *shift, const void *add, int relu, void *z, cudaStream_t st);
 
 }  // namespace convbn

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "mma_sync.cuh"
 #include "packed_f32.cuh"
 #include "sm100_ptx.cuh"
 
@@ -112,5 +113,119 @@ struct RowMap {
         return (long long)img * image + (long long)(t - img * by_h.d) * line + (long long)(p - t * by_w.d) * pixel;
     }
 };
+
+RowMap quant_row_map(const Problem &pb);      // (quant_fused.cu)
+
+// ---- tensor-core product of codes ---------------------------------------------------------------------------------------
+// tcgen05.mma instruction descriptor of kind::i8: bits 4-5 D format (2 = s32), 7-9 and 10-12 operand formats (1 = s8), 17-22 N >> 3,
+// 24-28 M >> 4.
+__host__ __device__ constexpr uint32_t idesc_s8(int m, int n) {
+    return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+template <int CTAS = 1>
+__device__ __forceinline__ void umma_s8(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
+        "setp.ne.u32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::%7.kind::i8 [%0], da, db, %5, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "n"(CTAS)
+        : "memory");
+}
+
+// What an epilogue warp does with 32 rows and 128 bytes of columns of Z: sums times the row's and the channel's scale, shift,
+// addend, ReLU, into its box (which holds the addend's) or, where rows of Z do not start on 16-byte boundaries, straight into Z.
+template <class T>
+struct QuantOut {
+    T *z;
+    const T *add;
+    uint32_t p;
+    int n, dense, relu;        // dense: boxes
+};
+// xs2: scales of rows lane / 4 + 8 k (16-bit boxes), otherwise of row `lane`.  SMALL: |sums| below 2^22: added to the bits of 1.5 2^23
+// they are its low bits, and the conversion unit, a quarter as fast, is left alone.
+template <class T, bool SMALL>
+__device__ __forceinline__ void quant_chunk(const QuantOut<T> &o, uint8_t *buf, bool boxed, uint32_t t_row, const float *ws_c, const float *b_c,
+                                            const f32x2 (&xs2)[4], uint32_t row, int col0, int cols, int lane) {
+    constexpr int CH = 128 / sizeof(T), PER = 16 / sizeof(T);
+    const f32x2 one = pair(1.f, 1.f), away = pair(-12582912.f, -12582912.f), none = pair(-0.f, -0.f);
+    auto scaled = [&](uint32_t a, uint32_t b, f32x2 xs) {
+        if constexpr (SMALL)
+            return fma2(fma2(pair(__uint_as_float(a + 0x4B400000u), __uint_as_float(b + 0x4B400000u)), one, away), xs, none);
+        else
+            return fma2(pair((float)(int)a, (float)(int)b), xs, none);
+    };
+    if constexpr (sizeof(T) == 2) {
+        if (o.dense) {
+            // the accumulator as matrix fragments: see umma_conv.cu
+            constexpr bool H = __is_same(T, __half);
+            const uint32_t ws_at = ptx::smem_u32(ws_c) + (uint32_t)(lane & 3) * 8u, b_at = ptx::smem_u32(b_c) + (uint32_t)(lane & 3) * 8u;
+            const uint32_t frag = ptx::smem_u32(buf) + (uint32_t)((lane & 7) + (lane & 8)) * 128u;
+            const uint32_t frag_chunk = (uint32_t)(((lane >> 4) ^ (lane & 7)) << 4);
+            auto rows16 = [&](auto add_tag, auto relu_tag) {
+                constexpr bool ADD = decltype(add_tag)::value, RELU = decltype(relu_tag)::value;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t v[32];
+                    ptx::tmem_ld_16x64(t_row + ((uint32_t)(16 * h) << 16), v);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int q = 0; q < 8; q += 2) {
+                        uint32_t r[4], a[4];           // columns 8 q and 8 q + 8: rows 0-7, 8-15 of each
+                        const uint32_t at16 = (uint32_t)h * 2048u + (((uint32_t)q << 4) ^ frag_chunk);
+                        if constexpr (ADD) ldmatrix_x4(a[0], a[1], a[2], a[3], frag + at16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t *s = &v[(q + (e >> 1)) * 4 + (e & 1) * 2], off = (uint32_t)(8 * (q + (e >> 1))) * 4u;
+                            f32x2 f = fma2(scaled(s[0], s[1], xs2[2 * h + (e & 1)]), lds_f32x2(ws_at + off), lds_f32x2(b_at + off));
+                            if constexpr (ADD) f = fma2(f, one, widen_t<H>(a[e]));
+                            r[e] = narrow_t<H>(f);
+                            if constexpr (RELU) r[e] = post_pair<H>(r[e], false, 0u, true, false, 0u);
+                        }
+                        stmatrix_x4(frag + at16, r[0], r[1], r[2], r[3]);
+                    }
+                }
+            };
+            if (boxed) { if (o.relu) rows16(std::true_type(), std::true_type()); else rows16(std::true_type(), std::false_type()); }
+            else { if (o.relu) rows16(std::false_type(), std::true_type()); else rows16(std::false_type(), std::false_type()); }
+            return;
+        }
+    }
+#pragma unroll 1
+    for (int h = 0; h < CH; h += 32) {
+        uint32_t v[32];
+        ptx::tmem_ld_32x32(t_row + (uint32_t)h, v);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            const f32x2 f = fma2(scaled(v[j], v[j + 1], xs2[0]), *(const f32x2 *)(ws_c + h + j), *(const f32x2 *)(b_c + h + j));
+            v[j] = (uint32_t)f;
+            v[j + 1] = (uint32_t)(f >> 32);
+        }
+        if (sizeof(T) == 4 && o.dense) {
+#pragma unroll
+            for (int j = 0; j < 32; j += PER) {
+                uint4 *at = (uint4 *)(buf + lane * 128 + ((((j / PER) ^ lane) & 7) << 4));
+                uint4 q = boxed ? *at : make_uint4(0u, 0u, 0u, 0u);
+                uint32_t *w = (uint32_t *)&q;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float f = __uint_as_float(v[j + e]);
+                    if (boxed) f += __uint_as_float(w[e]);
+                    w[e] = __float_as_uint(o.relu ? fmaxf(f, 0.f) : f);
+                }
+                *at = q;
+            }
+        } else if (row < o.p) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                if (h + j >= cols) continue;
+                const size_t at = (size_t)row * o.n + col0 + h + j;
+                float f = __uint_as_float(v[j]);
+                if (o.add) f += to_f32(o.add[at]);
+                o.z[at] = from_f32<T>(o.relu ? fmaxf(f, 0.f) : f);
+            }
+        }
+    }
+}
 
 }  // namespace convbn

@@ -8,7 +8,6 @@
 // (128-byte swizzle).  Rows on 16-byte boundaries arrive by bulk copies of up to
 // 16 KB in a ring (by loads into registers, a batch ahead, 256 -> 64 at 56 x 56, N = 256 took 143 us).
 #include "kernels.h"
-#include "mma_sync.cuh"
 #include "quant8.cuh"
 
 namespace convbn {
@@ -43,20 +42,6 @@ struct QuantCtl {
     uint32_t tmem_base;
     int abort_flag;
 };
-
-// tcgen05.mma instruction descriptor of kind::i8: bits 4-5 D format (2 = s32), 7-9 and 10-12 operand formats (1 = s8), 17-22 N >> 3,
-// 24-28 M >> 4.
-__host__ __device__ constexpr uint32_t idesc_s8(int m, int n) {
-    return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
-}
-__device__ __forceinline__ void umma_s8(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
-        "setp.ne.u32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::i8 [%0], da, db, %5, p;\n\t}"
-        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
 
 // A converting warp's rows of a unit: RPI of them an instruction (a set), BATCH sets at a time, at most 4 KB.  Half a batch of all
 // eight warps, side by side, is a slot of the ring.
@@ -313,7 +298,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         if (!ok && lane == 0) give_up();
     } else {
         // ---- epilogue ----
-        constexpr int CH = 128 / sizeof(T), PER = 16 / sizeof(T);      // columns of a box, of 16 bytes
+        constexpr int CH = 128 / sizeof(T);                  // columns of a box
         const int quarter = warp & 3, ew = warp - 2;
         const uint32_t egroup = (uint32_t)ew >> 2;
         uint8_t *boxes = staging + (size_t)ew * g.nbuf * kQStage;
@@ -323,17 +308,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             shift_s[c] = c < g.n ? shift[c] : 0.f;
         }
         named_bar_sync(1, 256);
-        // fragments of the accumulator (16-bit types): see umma_conv.cu
-        const uint32_t frag_row = (uint32_t)((lane & 7) + (lane & 8)) * 128u, frag_chunk = (uint32_t)(((lane >> 4) ^ (lane & 7)) << 4);
-        const f32x2 one = pair(1.f, 1.f), away = pair(-12582912.f, -12582912.f), none = pair(-0.f, -0.f);
-        // Sums times the row's scale.  Up to 256 products of codes lie below 2^22: added to the bits of 1.5 2^23 they are its low bits,
-        // and the conversion unit, a quarter as fast, is left alone.
-        auto scaled = [&](uint32_t a, uint32_t b, f32x2 xs2) {
-            if constexpr (LPR * CPL <= 32)
-                return fma2(fma2(pair(__uint_as_float(a + 0x4B400000u), __uint_as_float(b + 0x4B400000u)), one, away), xs2, none);
-            else
-                return fma2(pair((float)(int)a, (float)(int)b), xs2, none);
-        };
+        const QuantOut<T> out{z, add, g.p, g.n, g.dense, g.relu};
         bool ok = true;
         uint32_t i = 0, s = 0, m, nt, last, turn = 0, add_ph = 0;
         const bool boxed = g.dense && add;
@@ -378,80 +353,8 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                         add_ph ^= 1u;
                         if (!ok) break;
                     }
-                    const float *ws_c = scale_s + n0 + c0, *b_c = shift_s + n0 + c0;
-                    bool boxed_done = false;
-                    if constexpr (sizeof(T) == 2) {
-                        if (g.dense) {
-                            boxed_done = true;
-                            constexpr bool H = __is_same(T, __half);
-                            const uint32_t ws_at = smem_u32(ws_c) + (uint32_t)(lane & 3) * 8u, b_at = smem_u32(b_c) + (uint32_t)(lane & 3) * 8u;
-                            const uint32_t frag = smem_u32(buf) + frag_row;
-                            auto rows16 = [&](auto add_tag, auto relu_tag) {
-                                constexpr bool ADD = decltype(add_tag)::value, RELU = decltype(relu_tag)::value;
-#pragma unroll
-                                for (int h = 0; h < 2; ++h) {
-                                    uint32_t v[32];
-                                    tmem_ld_16x64(t_row + ((uint32_t)(16 * h) << 16) + (uint32_t)c0, v);
-                                    tmem_ld_wait();
-#pragma unroll
-                                    for (int q = 0; q < 8; q += 2) {
-                                        uint32_t o[4], a[4];           // columns 8 q and 8 q + 8: rows 0-7, 8-15 of each
-                                        const uint32_t at16 = (uint32_t)h * 2048u + (((uint32_t)q << 4) ^ frag_chunk);
-                                        if constexpr (ADD) ldmatrix_x4(a[0], a[1], a[2], a[3], frag + at16);
-#pragma unroll
-                                        for (int e = 0; e < 4; ++e) {
-                                            const uint32_t *p2 = &v[(q + (e >> 1)) * 4 + (e & 1) * 2], off = (uint32_t)(8 * (q + (e >> 1))) * 4u;
-                                            f32x2 f = fma2(scaled(p2[0], p2[1], xs2[2 * h + (e & 1)]), lds_f32x2(ws_at + off), lds_f32x2(b_at + off));
-                                            if constexpr (ADD) f = fma2(f, one, widen_t<H>(a[e]));
-                                            o[e] = narrow_t<H>(f);
-                                            if constexpr (RELU) o[e] = post_pair<H>(o[e], false, 0u, true, false, 0u);
-                                        }
-                                        stmatrix_x4(frag + at16, o[0], o[1], o[2], o[3]);
-                                    }
-                                }
-                            };
-                            if (boxed) { if (g.relu) rows16(std::true_type(), std::true_type()); else rows16(std::true_type(), std::false_type()); }
-                            else { if (g.relu) rows16(std::false_type(), std::true_type()); else rows16(std::false_type(), std::false_type()); }
-                        }
-                    }
-                    if (!boxed_done) {
-#pragma unroll 1
-                        for (int h = 0; h < CH; h += 32) {
-                            uint32_t v[32];
-                            tmem_ld_32x32(t_row + (uint32_t)(c0 + h), v);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int j = 0; j < 32; j += 2) {
-                                const f32x2 f2 = fma2(scaled(v[j], v[j + 1], xs2[0]), *(const f32x2 *)(ws_c + h + j), *(const f32x2 *)(b_c + h + j));
-                                v[j] = (uint32_t)f2;
-                                v[j + 1] = (uint32_t)(f2 >> 32);
-                            }
-                            if (sizeof(T) == 4 && g.dense) {
-#pragma unroll
-                                for (int j = 0; j < 32; j += PER) {
-                                    uint4 *at = (uint4 *)(buf + lane * 128 + ((((j / PER) ^ lane) & 7) << 4));
-                                    uint4 q = boxed ? *at : make_uint4(0u, 0u, 0u, 0u);
-                                    uint32_t *w = (uint32_t *)&q;
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        float v1 = __uint_as_float(v[j + e]);
-                                        if (boxed) v1 += __uint_as_float(w[e]);
-                                        w[e] = __float_as_uint(g.relu ? fmaxf(v1, 0.f) : v1);
-                                    }
-                                    *at = q;
-                                }
-                            } else if (row < g.p) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) {
-                                    if (c0 + h + j >= cols) continue;
-                                    const size_t at = (size_t)row * g.n + n0 + c0 + h + j;
-                                    float v1 = __uint_as_float(v[j]);
-                                    if (add) v1 += to_f32(add[at]);
-                                    z[at] = from_f32<T>(g.relu ? fmaxf(v1, 0.f) : v1);
-                                }
-                            }
-                        }
-                    }
+                    quant_chunk<T, LPR * CPL <= 32>(out, buf, boxed, t_row + (uint32_t)c0, scale_s + n0 + c0, shift_s + n0 + c0, xs2, row, n0 + c0,
+                                                    cols - c0, lane);
                     if (c0 + CH >= cols) {
                         tc_fence_before_sync();
                         __syncwarp();

@@ -136,7 +136,7 @@ def _check(got, t, dtype, stride, relu):
 SIZES = [(1, 1, 1, 1, 1), (1, 64, 1, 1, 64), (1, 2048, 1, 1, 1000), (2, 500, 1, 1, 10), (7, 256, 1, 1, 129), (16, 24, 1, 1, 2048),
          (17, 130, 1, 1, 40), (33, 1024, 1, 1, 256), (100, 512, 1, 1, 130), (128, 64, 1, 1, 64), (129, 96, 1, 1, 200), (300, 2000, 1, 1, 72),
          (1000, 256, 1, 1, 64), (2, 64, 13, 11, 256), (3, 256, 9, 15, 64), (1, 1024, 14, 14, 512), (2, 2048, 7, 7, 512), (5, 8, 3, 7, 8),
-         (40, 512, 7, 7, 2048), (6, 192, 21, 19, 320)]
+         (40, 512, 7, 7, 2048), (6, 192, 21, 19, 320), (9500, 520, 1, 1, 1032), (1700, 1032, 1, 1, 1500), (300, 4104, 1, 1, 2056)]
 
 
 @pytest.mark.gpu
