@@ -223,7 +223,7 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded,
         return pl;
     }
     if (phase == CONVBN_PHASE_DEPLOY_FWD_QUANT) {
-        if (!quant_path(d, pb) || quant_fused_eligible(pb)) return pl;
+        if (!quant_path(d, pb) || quant_fused_eligible(pb, (int)elem_size(d->dtype))) return pl;
         pl.unpacked = take(quant_codes_bytes(pb));
         pl.inner = take((size_t)pb.p * sizeof(float));
         pl.total = off;
@@ -1439,7 +1439,7 @@ int convbn_deploy_fwd_quant(const convbn_desc *desc, const void *x, const void *
     const Plan pl = make_plan(desc, pb, CONVBN_PHASE_DEPLOY_FWD_QUANT);
     CK(check_ws(pl, workspace, workspace_bytes));
     cudaStream_t st = (cudaStream_t)stream;
-    if (quant_fused_eligible(pb)) {
+    if (quant_fused_eligible(pb, (int)elem_size(desc->dtype))) {
         LAUNCH("quant_fused", launch_quant_fused(pb, storage_type(desc), x, w_codes, w_scale, b_fused, add, relu ? 1 : 0, z, st));
         t_last_kernel[CONVBN_PHASE_DEPLOY_FWD_QUANT] = "umma";
         return CONVBN_OK;

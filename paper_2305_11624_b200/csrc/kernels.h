@@ -339,7 +339,7 @@ size_t quant_codes_bytes(const Problem &pb);
 cudaError_t launch_quant_weights(const Problem &pb, int dtype, const void *w, const float *b, const float *gamma, const float *beta,
                                  const float *mean, const float *var, void *codes, float *scale, float *shift, cudaStream_t st);
 // Rows to codes and product in one kernel (quant_fused.cu).
-bool quant_fused_eligible(const Problem &pb);
+bool quant_fused_eligible(const Problem &pb, int elem_bytes);
 cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, const void *wq, const float *ws, const float *shift,
                                const void *add, int relu, void *z, cudaStream_t st);
 // The two as kernels of their own (quant_gemm.cu).

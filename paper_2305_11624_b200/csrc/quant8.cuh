@@ -164,25 +164,34 @@ __device__ __forceinline__ void quant_chunk(const QuantOut<T> &o, uint8_t *buf, 
             auto rows16 = [&](auto add_tag, auto relu_tag) {
                 constexpr bool ADD = decltype(add_tag)::value, RELU = decltype(relu_tag)::value;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t v[32];
-                    ptx::tmem_ld_16x64(t_row + ((uint32_t)(16 * h) << 16), v);
+                for (int c = 0; c < 64; c += 32) {     // 32 columns of all rows at a time: their parameters are read once
+                    uint32_t v[2][16];
+                    ptx::tmem_ld_16x32(t_row + (uint32_t)c, v[0]);
+                    ptx::tmem_ld_16x32(t_row + (16u << 16) + (uint32_t)c, v[1]);
+                    f32x2 sc[4], sh[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        sc[q] = lds_f32x2(ws_at + (uint32_t)(c + 8 * q) * 4u);
+                        sh[q] = lds_f32x2(b_at + (uint32_t)(c + 8 * q) * 4u);
+                    }
                     ptx::tmem_ld_wait();
 #pragma unroll
-                    for (int q = 0; q < 8; q += 2) {
-                        uint32_t r[4], a[4];           // columns 8 q and 8 q + 8: rows 0-7, 8-15 of each
-                        const uint32_t at16 = (uint32_t)h * 2048u + (((uint32_t)q << 4) ^ frag_chunk);
-                        if constexpr (ADD) ldmatrix_x4(a[0], a[1], a[2], a[3], frag + at16);
+                    for (int q = 0; q < 4; q += 2)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t *s = &v[(q + (e >> 1)) * 4 + (e & 1) * 2], off = (uint32_t)(8 * (q + (e >> 1))) * 4u;
-                            f32x2 f = fma2(scaled(s[0], s[1], xs2[2 * h + (e & 1)]), lds_f32x2(ws_at + off), lds_f32x2(b_at + off));
-                            if constexpr (ADD) f = fma2(f, one, widen_t<H>(a[e]));
-                            r[e] = narrow_t<H>(f);
-                            if constexpr (RELU) r[e] = post_pair<H>(r[e], false, 0u, true, false, 0u);
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t r[4], a[4];       // columns c + 8 q and the next 8: rows 0-7, 8-15 of each
+                            const uint32_t at16 = (uint32_t)h * 2048u + (((uint32_t)(c / 8 + q) << 4) ^ frag_chunk);
+                            if constexpr (ADD) ldmatrix_x4(a[0], a[1], a[2], a[3], frag + at16);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const uint32_t *s = &v[h][(q + (e >> 1)) * 4 + (e & 1) * 2];
+                                f32x2 f = fma2(scaled(s[0], s[1], xs2[2 * h + (e & 1)]), sc[q + (e >> 1)], sh[q + (e >> 1)]);
+                                if constexpr (ADD) f = fma2(f, one, widen_t<H>(a[e]));
+                                r[e] = narrow_t<H>(f);
+                                if constexpr (RELU) r[e] = post_pair<H>(r[e], false, 0u, true, false, 0u);
+                            }
+                            stmatrix_x4(frag + at16, r[0], r[1], r[2], r[3]);
                         }
-                        stmatrix_x4(frag + at16, r[0], r[1], r[2], r[3]);
-                    }
                 }
             };
             if (boxed) { if (o.relu) rows16(std::true_type(), std::true_type()); else rows16(std::true_type(), std::false_type()); }

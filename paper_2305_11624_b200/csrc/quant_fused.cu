@@ -3,8 +3,7 @@
 // addend and ReLU are applied to the sums.  X is read once in its storage type, Z written once; codes exist on chip only.
 //
 // CTA = 19 warps: 0 weight tiles (TMA), 1 MMA issuer and owner of tensor memory, 2-9 epilogue (two groups of four, an accumulator
-// each), 10-17 rows to codes, 18 brings the rows.  A unit of work is 128 rows (and a span of channel tiles where there are few rows): eight warps
-// read its rows whole, a row by 8, 16 or 32 lanes, find the largest magnitude, and write the codes as the K-major A operand
+// each), 10-17 rows to codes, 18 brings the rows.  A unit of work is 128 rows: eight warps read them whole, a row by 8, 16 or 32 lanes, find the largest magnitude, and write the codes as the K-major A operand
 // (128-byte swizzle).  Rows on 16-byte boundaries arrive by bulk copies of up to
 // 16 KB in a ring (by loads into registers, a batch ahead, 256 -> 64 at 56 x 56, N = 256 took 143 us).
 #include "kernels.h"
@@ -30,11 +29,10 @@ struct QuantFused {
     RowMap rows;
     uint32_t p;
     int k, kb, n, bn;                            // C_in, its blocks of 128, C_out, channels of a tile
-    uint32_t units, n_tiles, per_part;           // per_part: channel tiles of a unit
-    FastDiv by_parts;                            // units of the same rows
+    uint32_t units, n_tiles;
     int abufs, stages, nbuf, resident;           // A buffers, slots of streamed weights, boxes of an epilogue warp
     int depth;                                   // slots of the ring of rows
-    int vec, dense, relu;                        // rows of X (of Z) start on 16-byte boundaries
+    int dense, relu;                             // rows of Z start on 16-byte boundaries
 };
 
 struct QuantCtl {
@@ -45,14 +43,14 @@ struct QuantCtl {
 
 // A converting warp's rows of a unit: RPI of them an instruction (a set), BATCH sets at a time, at most 4 KB.  Half a batch of all
 // eight warps, side by side, is a slot of the ring.
-template <class T, int LPR, int CPL> struct RowSets {
-    static constexpr int RPI = 32 / LPR, SETS = 16 / RPI, SET_BYTES = 256 * CPL * (int)sizeof(T);
+template <class T, int LPR> struct RowSets {
+    static constexpr int RPI = 32 / LPR, SETS = 16 / RPI, SET_BYTES = 256 * (int)sizeof(T);
     static constexpr int BATCH = SETS * SET_BYTES <= 4096 ? SETS : 4096 / SET_BYTES, BATCHES = SETS / BATCH;
 };
-template <class T, int LPR, int CPL> constexpr uint32_t kSlotBytes = (uint32_t)(8 * RowSets<T, LPR, CPL>::BATCH * RowSets<T, LPR, CPL>::SET_BYTES / 2);
+template <class T, int LPR> constexpr uint32_t kSlotBytes = (uint32_t)(8 * RowSets<T, LPR>::BATCH * RowSets<T, LPR>::SET_BYTES / 2);
 
-// LPR lanes read a row, 8 CPL LPR elements at most.  RING: rows start on 16-byte boundaries.
-template <class T, int LPR, int CPL, bool RING>
+// LPR lanes read a row, eight elements each.
+template <class T, int LPR>
 __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_z,
                                                                 const __grid_constant__ CUtensorMap tm_add, const QuantFused g,
                                                                 const T *__restrict__ x, const float *__restrict__ ws,
@@ -64,7 +62,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
     uint8_t *w_tiles = a_tiles + (size_t)g.abufs * a_bytes;
     uint8_t *staging = w_tiles + (size_t)(g.resident ? g.n_tiles * g.kb : g.stages) * w_bytes;
     uint8_t *ring = staging + (size_t)8 * g.nbuf * kQStage;
-    float *scale_s = (float *)(ring + (size_t)g.depth * kSlotBytes<T, LPR, CPL>), *shift_s = scale_s + g.n_tiles * g.bn;
+    float *scale_s = (float *)(ring + (size_t)g.depth * kSlotBytes<T, LPR>), *shift_s = scale_s + g.n_tiles * g.bn;
     float *xs_s = shift_s + g.n_tiles * g.bn;                                   // [kQSlots][128]
     QuantCtl *ctl = (QuantCtl *)(xs_s + kQSlots * kQRows);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -100,25 +98,19 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
     pdl_launch_dependents();
     const uint32_t tmem_base = ctl->tmem_base;
     auto give_up = [&]() { atomicOr(err, ERRW_TIMEOUT); ctl->abort_flag = 1; };
-    // channel tiles [first, last) of unit u, whose rows start at 128 m
-    auto unit = [&](uint32_t u, uint32_t &m, uint32_t &first, uint32_t &last) {
-        m = g.by_parts.div(u);
-        first = (u - m * g.by_parts.d) * g.per_part;
-        last = min(first + g.per_part, g.n_tiles);
-    };
 
     if (warp == 0) {
         if (elect_one()) {
             bool ok = true;
-            uint32_t it = 0, m, nt, last;
+            uint32_t it = 0;
             if (g.resident) {
                 mbar_arrive_expect_tx(&ctl->wfull, g.n_tiles * g.kb * w_bytes);
-                for (nt = 0; nt < g.n_tiles; ++nt)
+                for (uint32_t nt = 0; nt < g.n_tiles; ++nt)
                     for (int kb = 0; kb < g.kb; ++kb)
                         tma_load_2d(w_tiles + (size_t)(nt * g.kb + kb) * w_bytes, &tm_w, &ctl->wfull, kb * 128, (int)nt * g.bn);
             } else {
                 for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x)
-                    for (unit(u, m, nt, last); ok && nt < last; ++nt)
+                    for (uint32_t nt = 0; ok && nt < g.n_tiles; ++nt)
                         for (int kb = 0; kb < g.kb; ++kb, ++it) {
                             const uint32_t s = it % g.stages, ph = (it / g.stages) & 1u;
                             ok = mbar_wait_bounded(&ctl->empty[s], ph ^ 1u, abort_flag);
@@ -141,11 +133,11 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             const uint32_t a0 = smem_desc_lo(smem_u32(a_tiles), 16), w0 = smem_desc_lo(smem_u32(w_tiles), 16);
             const int tail = (g.k - (g.kb - 1) * 128 + 31) / 32;              // steps of 32 codes of the last block
             bool ok = !g.resident || mbar_wait_bounded(&ctl->wfull, 0, abort_flag);
-            uint32_t i = 0, s = 0, it = 0, m, nt, last;
+            uint32_t i = 0, s = 0, it = 0;
             for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
                 const uint32_t ab = g.abufs == 2 ? (i & 1u) : 0u, use = g.abufs == 2 ? (i >> 1) : i;
                 ok = mbar_wait_bounded(&ctl->a_full[ab], use & 1u, abort_flag);
-                for (unit(u, m, nt, last); ok && nt < last; ++nt, ++s) {
+                for (uint32_t nt = 0; ok && nt < g.n_tiles; ++nt, ++s) {
                     const uint32_t acc = s & 1u, d = tmem_base + acc * (uint32_t)g.bn;
                     ok = mbar_wait_bounded(&ctl->acc_empty[acc], ((s >> 1) & 1u) ^ 1u, abort_flag);
                     if (!ok) break;
@@ -171,43 +163,41 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         }
     } else if (warp == kQRowWarp) {
         // ---- rows of X into the ring, a slot at a time: side by side one copy, otherwise one a row ----
-        if constexpr (RING) {
-            using R = RowSets<T, LPR, CPL>;
-            constexpr uint32_t ROWS = 8 * (R::BATCH / 2) * R::RPI;
-            const uint32_t row_bytes = (uint32_t)g.k * sizeof(T);
-            uint32_t slot = 0, ph = 1, asked = 0;
-            bool ok = true;
-            for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x) {
-                const uint32_t end = min((g.by_parts.div(u) + 1) * kQRows, g.p);
-                for (uint32_t first = g.by_parts.div(u) * kQRows; first < end; first += ROWS) {
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_empty[slot], ph, abort_flag));
-                    if (!ok) break;
-                    const uint32_t rows = min(ROWS, end - first);
-                    uint8_t *to = ring + (size_t)slot * kSlotBytes<T, LPR, CPL>;
-                    if (lane == 0) {
-                        mbar_arrive_expect_tx(&ctl->rows_full[slot], rows * row_bytes);
-                        if (!g.rows.strided) bulk_load(to, x + (size_t)first * g.k, rows * row_bytes, &ctl->rows_full[slot]);
-                    }
-                    if (g.rows.strided) {
-                        __syncwarp();
-                        for (uint32_t r = lane; r < rows; r += 32) bulk_load(to + (size_t)r * row_bytes, x + g.rows.at(first + r), row_bytes, &ctl->rows_full[slot]);
-                    }
-                    ++asked;
-                    if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
+        using R = RowSets<T, LPR>;
+        constexpr uint32_t ROWS = 8 * (R::BATCH / 2) * R::RPI;
+        const uint32_t row_bytes = (uint32_t)g.k * sizeof(T);
+        uint32_t slot = 0, ph = 1, asked = 0;
+        bool ok = true;
+        for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x) {
+            const uint32_t end = min((u + 1) * kQRows, g.p);
+            for (uint32_t first = u * kQRows; first < end; first += ROWS) {
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_empty[slot], ph, abort_flag));
+                if (!ok) break;
+                const uint32_t rows = min(ROWS, end - first);
+                uint8_t *to = ring + (size_t)slot * kSlotBytes<T, LPR>;
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(&ctl->rows_full[slot], rows * row_bytes);
+                    if (!g.rows.strided) bulk_load(to, x + (size_t)first * g.k, rows * row_bytes, &ctl->rows_full[slot]);
                 }
+                if (g.rows.strided) {
+                    __syncwarp();
+                    for (uint32_t r = lane; r < rows; r += 32) bulk_load(to + (size_t)r * row_bytes, x + g.rows.at(first + r), row_bytes, &ctl->rows_full[slot]);
+                }
+                ++asked;
+                if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
             }
-            if (!ok && lane == 0) {
-                give_up();
-                for (uint32_t j = asked > (uint32_t)g.depth ? asked - g.depth : 0; j < asked; ++j)        // let the copies in flight land
-                    mbar_wait_bounded(&ctl->rows_full[j % g.depth], (j / g.depth) & 1u, nullptr, 200000000ull);
-            }
+        }
+        if (!ok && lane == 0) {
+            give_up();
+            for (uint32_t j = asked > (uint32_t)g.depth ? asked - g.depth : 0; j < asked; ++j)        // let the copies in flight land
+                mbar_wait_bounded(&ctl->rows_full[j % g.depth], (j / g.depth) & 1u, nullptr, 200000000ull);
         }
     } else if (warp >= kQLoadWarp) {
         // ---- rows to codes: warp qw has the rows qw HALF RPI .. of every slot ----
         // A batch's rows are read twice: for their largest magnitudes, and after these have become scales, which each lane works out
         // for one row (a scale per four rows, and the rows kept in registers between: 1900 instructions a warp and unit instead of
         // 700, 256 -> 64 at 56 x 56, N = 256 192 us).
-        using R = RowSets<T, LPR, CPL>;
+        using R = RowSets<T, LPR>;
         constexpr int RPI = R::RPI, BATCH = R::BATCH, BATCHES = R::BATCHES, HALF = BATCH / 2;
         constexpr int SLOT_ROWS = 8 * HALF * RPI;
         const int qw = warp - kQLoadWarp, sub = lane & (LPR - 1), row_l = lane / LPR, own = qw * HALF * RPI + row_l;     // row in a slot
@@ -221,41 +211,29 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             const uint32_t ab = g.abufs == 2 ? (i & 1u) : 0u, use = g.abufs == 2 ? (i >> 1) : i;
             uint8_t *tile = a_tiles + (size_t)ab * a_bytes;
             float *xs = xs_s + (i % kQSlots) * kQRows;
-            const uint32_t first = g.by_parts.div(u) * kQRows;
+            const uint32_t first = u * kQRows;
 #pragma unroll 1
             for (int batch = 0; batch < BATCHES; ++batch) {
-                // set j of the batch as this lane has it
-                auto read = [&](Eight<T> (&v)[CPL], int j, uint32_t base) {
-                    const T *src = nullptr;
-                    if constexpr (!RING) src = x + g.rows.at(min(first + (uint32_t)row_of(batch, j), g.p - 1));
-#pragma unroll
-                    for (int c = 0; c < CPL; ++c) {
-                        const int at = (c * LPR + sub) * 8;
-                        if (at >= g.k) v[c].zero();
-                        else if (RING) v[c].load_shared(base + (uint32_t)(own + j % HALF * RPI) * row_bytes + (uint32_t)at * (uint32_t)sizeof(T));
-                        else if (g.vec) v[c].load(src + at);
-                        else v[c].load_some(src + at, g.k - at);
-                    }
+                auto read = [&](Eight<T> &v, int j, uint32_t base) {       // set j of the batch as this lane has it
+                    if (sub * 8 >= g.k) v.zero();
+                    else v.load_shared(base + (uint32_t)(own + j % HALF * RPI) * row_bytes + (uint32_t)sub * 8u * (uint32_t)sizeof(T));
                 };
                 uint32_t mine = 0, base[2], bar[2];
                 bool there[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    there[h] = !RING || first + (uint32_t)((2 * batch + h) * SLOT_ROWS) < g.p;       // (a slot past the last row never comes)
-                    base[h] = ring0 + slot * kSlotBytes<T, LPR, CPL>;
+                    there[h] = first + (uint32_t)((2 * batch + h) * SLOT_ROWS) < g.p;       // (a slot past the last row never comes)
+                    base[h] = ring0 + slot * kSlotBytes<T, LPR>;
                     bar[h] = slot;
                     if (!there[h]) continue;
-                    if constexpr (RING) {
-                        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_full[slot], ph, abort_flag));
-                        if (!ok) break;
-                        if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
-                    }
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_full[slot], ph, abort_flag));
+                    if (!ok) break;
+                    if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
 #pragma unroll
                     for (int j = h * HALF; j < (h + 1) * HALF; ++j) {
-                        Eight<T> v[CPL];
+                        Eight<T> v;
                         read(v, j, base[h]);
-                        uint32_t t = v[0].top();
-                        if constexpr (CPL == 2) t = max(t, v[1].top());
+                        uint32_t t = v.top();
                         if constexpr (LPR == 32) t = __reduce_max_sync(0xffffffffu, t);
                         else
 #pragma unroll
@@ -275,19 +253,15 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     if (!there[h]) continue;
 #pragma unroll
                     for (int j = h * HALF; j < (h + 1) * HALF; ++j) {
-                        Eight<T> v[CPL];
+                        Eight<T> v;
                         read(v, j, base[h]);
                         const float inv = __shfl_sync(0xffffffffu, rs.inv, (lane & ~(LPR - 1)) + j);
-                        const int r = row_of(batch, j);
-#pragma unroll
-                        for (int c = 0; c < CPL; ++c) {
-                            const int at = (c * LPR + sub) * 8;
-                            if (at < g.kb * 128)
-                                *(uint2 *)(tile + (size_t)(at >> 7) * kQBlock + r * 128 + ((((at >> 4) ^ r) & 7) << 4) + (at & 8)) = v[c].codes(inv);
-                        }
+                        const int r = row_of(batch, j), at = sub * 8;
+                        if (at < g.kb * 128)
+                            *(uint2 *)(tile + (size_t)(at >> 7) * kQBlock + r * 128 + ((((at >> 4) ^ r) & 7) << 4) + (at & 8)) = v.codes(inv);
                     }
                     __syncwarp();                             // every lane has read this half
-                    if (RING && lane == 0) mbar_arrive(&ctl->rows_empty[bar[h]]);
+                    if (lane == 0) mbar_arrive(&ctl->rows_empty[bar[h]]);
                 }
             }
             if (!ok) break;
@@ -310,12 +284,12 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         named_bar_sync(1, 256);
         const QuantOut<T> out{z, add, g.p, g.n, g.dense, g.relu};
         bool ok = true;
-        uint32_t i = 0, s = 0, m, nt, last, turn = 0, add_ph = 0;
+        uint32_t i = 0, s = 0, turn = 0, add_ph = 0;
         const bool boxed = g.dense && add;
         for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
-            for (unit(u, m, nt, last); ok && nt < last; ++nt, ++s) {
+            for (uint32_t nt = 0; ok && nt < g.n_tiles; ++nt, ++s) {
                 if ((s & 1u) != egroup) continue;
-                const uint32_t row0 = m * kQRows + quarter * 32, row = row0 + lane;
+                const uint32_t row0 = u * kQRows + quarter * 32, row = row0 + lane;
                 const int n0 = (int)nt * g.bn, cols = min(g.bn, g.n - n0);
                 auto box = [&]() { return boxes + (g.nbuf == 2 ? turn * kQStage : 0u); };
                 // the addend's box goes where the results will be; the box's last store has been read
@@ -353,7 +327,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                         add_ph ^= 1u;
                         if (!ok) break;
                     }
-                    quant_chunk<T, LPR * CPL <= 32>(out, buf, boxed, t_row + (uint32_t)c0, scale_s + n0 + c0, shift_s + n0 + c0, xs2, row, n0 + c0,
+                    quant_chunk<T, true>(out, buf, boxed, t_row + (uint32_t)c0, scale_s + n0 + c0, shift_s + n0 + c0, xs2, row, n0 + c0,
                                                     cols - c0, lane);
                     if (c0 + CH >= cols) {
                         tc_fence_before_sync();
@@ -390,7 +364,14 @@ size_t fused_smem(const QuantFused &g, size_t slot) {
 
 }  // namespace
 
-bool quant_fused_eligible(const Problem &pb) { return pb.c_in <= 512 && pb.c_out <= 2048; }
+// Rows enough for every SM, and short ones that start on 16-byte boundaries.  This kernel and the two of quant_gemm.cu, us: 100352
+// rows 64 -> 256 20.5 and 27.7, 256 -> 64 23.3 and 28.0, 256 -> 1024 78.7 and 79.8, but (as it was for longer rows) 512 -> 64 41.6 and
+// 43.8, 512 -> 1024 122.9 and 100.8; 6272 rows 64 -> 256 6.1 and 5.9, 256 -> 64 7.2 and 6.1; 1000 rows 256 -> 64 7.0 and 5.6: below a
+// unit per SM a warp per row beats sixteen rows a warp one after the other.
+bool quant_fused_eligible(const Problem &pb, int elem_bytes) {
+    return pb.c_in <= 256 && pb.c_in % 8 == 0 && (size_t)pb.c_in * elem_bytes % 16 == 0 && pb.c_out <= 2048 &&
+           pb.p >= (long long)kQRows * device_sm_count();
+}
 
 RowMap quant_row_map(const Problem &pb) {
     RowMap r;
@@ -410,44 +391,29 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
     QuantFused g;
     g.rows = quant_row_map(pb);
     g.p = (uint32_t)pb.p; g.k = pb.c_in; g.kb = (pb.c_in + 127) / 128; g.n = pb.c_out; g.relu = relu;
-    g.vec = (size_t)pb.c_in * es % 16 == 0 && pb.c_in % 8 == 0;
     g.dense = (size_t)pb.c_out * es % 16 == 0;
-    const uint32_t m_tiles = (uint32_t)((pb.p + kQRows - 1) / kQRows);
-    // Enough rows for every SM: wide tiles.  Fewer: tiles of 64 channels, and the channels cut into parts.
-    const bool many = m_tiles * 2 > (uint32_t)sms;
-    auto tiles = [&](int widest) {
-        g.n_tiles = (uint32_t)((pb.c_out + widest - 1) / widest);
-        g.bn = (int)(((pb.c_out + g.n_tiles - 1) / g.n_tiles + 63) / 64 * 64);
-        uint32_t parts = many ? 1 : (uint32_t)sms / m_tiles;
-        if (parts > g.n_tiles) parts = g.n_tiles;
-        g.per_part = (g.n_tiles + parts - 1) / parts;
-        parts = (g.n_tiles + g.per_part - 1) / g.per_part;
-        g.by_parts = FastDiv(parts);
-        g.units = m_tiles * parts;
-    };
+    g.units = (uint32_t)((pb.p + kQRows - 1) / kQRows);
     // Buffers, the most wanted first: two of the A operand (rows are converted while others are multiplied) and six slots of
-    // rows (two are in use, the others on their way), then two boxes per epilogue warp; the weights
-    // resident where a CTA has all of them to itself, otherwise at least three slots; wide tiles.
-    const size_t room = 227 * 1024, lanes = pb.c_in <= 64 ? 8 : (pb.c_in <= 128 ? 16 : 32), set = 256 * es * (pb.c_in > 256 ? 2 : 1);
-    const size_t slot = 8 * (lanes / 2 * set <= 4096 ? lanes / 2 * set : 4096) / 2;         // (kSlotBytes)
-    const struct { int abufs, nbuf, depth; } wanted[] = {{2, 2, 6}, {2, 1, 6}, {2, 1, 4}, {1, 2, 6}, {1, 1, 4}, {1, 1, 2}};
+    // rows (two are in use, the others on their way), then two boxes per epilogue warp; the weights resident, otherwise at least
+    // three slots of them; wide tiles.
+    const size_t room = 227 * 1024, sets = pb.c_in <= 64 ? 4 : (pb.c_in <= 128 ? 8 : 16), set = 256 * es;
+    const size_t slot = 8 * (sets * set <= 4096 ? sets * set : 4096) / 2;                   // (kSlotBytes)
+    const struct { int abufs, nbuf, depth; } wanted[] = {{2, 2, 6}, {2, 1, 6}, {2, 1, 4}, {1, 1, 4}, {1, 1, 2}};
     size_t smem = 0;
     for (const auto &c : wanted) {
-        g.abufs = c.abufs; g.nbuf = c.nbuf; g.depth = g.vec ? c.depth : 0; g.stages = 3;
-        for (int widest = many ? 256 : 64; widest >= (many && g.abufs == 2 ? 128 : 64) && !smem; widest /= 2) {
-            tiles(widest);
-            for (g.resident = g.by_parts.d == 1 && m_tiles >= (uint32_t)sms; g.resident >= 0 && !smem; --g.resident)
-                if (fused_smem(g, slot) <= room) { smem = fused_smem(g, slot); break; }
+        g.abufs = c.abufs; g.nbuf = c.nbuf; g.depth = c.depth; g.stages = 3;
+        for (int widest = 256; widest >= 64 && !smem; widest /= 2) {
+            g.n_tiles = (uint32_t)((pb.c_out + widest - 1) / widest);
+            g.bn = (int)(((pb.c_out + g.n_tiles - 1) / g.n_tiles + 63) / 64 * 64);
+            for (g.resident = 1; g.resident >= 0; --g.resident)
+                if ((smem = fused_smem(g, slot)) <= room) break;
+                else smem = 0;
             if (smem) break;
         }
         if (smem) break;
     }
     if (!smem) return cudaErrorInvalidValue;
-    while (!g.resident && g.stages < 4) {
-        ++g.stages;
-        if (fused_smem(g, slot) > room) { --g.stages; break; }
-    }
-    while (g.vec && g.depth < kQMaxDepth) {
+    while (g.depth < kQMaxDepth) {
         ++g.depth;
         if (fused_smem(g, slot) > room) { --g.depth; break; }
     }
@@ -462,24 +428,19 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
     }
     int *err = nullptr;
     if (cudaError_t e = error_word_address(&err); e != cudaSuccess) return e;
-    auto go = [&](auto tag, auto lpr, auto cpl, auto rows) {
+    auto go = [&](auto tag, auto lpr) {
         using T = decltype(tag);
-        auto kernel = quant_fused_kernel<T, decltype(lpr)::value, decltype(cpl)::value, decltype(rows)::value>;
+        auto kernel = quant_fused_kernel<T, decltype(lpr)::value>;
         static PerDevice attr, carve;
         if (cudaError_t e = max_dynamic_smem_once(kernel, 227 * 1024, &attr); e != cudaSuccess) return e;
         prefer_max_shared_once(kernel, &carve);
         return launch_pdl(kernel, dim3(grid), dim3(kQThreads), smem, st, tw, tz, ta, g, (const T *)x, ws, shift, (const T *)add, (T *)z, err);
     };
-    auto sized = [&](auto tag, auto lpr, auto cpl) {
-        if (g.vec) return go(tag, lpr, cpl, std::true_type());
-        return go(tag, lpr, cpl, std::false_type());
-    };
     auto typed = [&](auto tag) {
         using std::integral_constant;
-        if (pb.c_in <= 64) return sized(tag, integral_constant<int, 8>(), integral_constant<int, 1>());
-        if (pb.c_in <= 128) return sized(tag, integral_constant<int, 16>(), integral_constant<int, 1>());
-        if (pb.c_in <= 256) return sized(tag, integral_constant<int, 32>(), integral_constant<int, 1>());
-        return sized(tag, integral_constant<int, 32>(), integral_constant<int, 2>());
+        if (pb.c_in <= 64) return go(tag, integral_constant<int, 8>());
+        if (pb.c_in <= 128) return go(tag, integral_constant<int, 16>());
+        return go(tag, integral_constant<int, 32>());
     };
     return dtype == CONVBN_F32 ? typed(float()) : (dtype == CONVBN_F16 ? typed(__half()) : typed(__nv_bfloat16()));
 }

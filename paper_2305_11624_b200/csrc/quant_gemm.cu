@@ -237,43 +237,58 @@ __global__ void __launch_bounds__(kGThreads) quant_gemm_kernel(const __grid_cons
     if (warp == 1) tmem_dealloc<CTAS>(tmem_base, 2 * BN);
 }
 
-// Rows to codes: a warp per row, read for its largest magnitude and again (from L1 or L2) for its codes.
-template <class T, bool VEC>
+// Rows to codes.  LPR lanes a row, KEEP chunks of eight elements a lane kept from the search for the largest magnitude to the codes
+// (what lies beyond is read again, from L1 or L2); short rows several to a lane, so that a warp has at least four requests out.
+template <class T, int LPR, int KEEP, bool VEC>
 __global__ void __launch_bounds__(256) quant_rows_kernel(const RowMap rows, uint32_t p, int k, int pitch, const T *__restrict__ x,
                                                          uint8_t *__restrict__ codes, float *__restrict__ scale) {
-    constexpr int KEEP = 8;             // chunks of eight elements that a lane keeps between the readings
+    constexpr int RPI = 32 / LPR, SETS = KEEP < 4 ? 4 / KEEP : 1;
     pdl_wait();
     pdl_launch_dependents();
-    const int lane = threadIdx.x & 31;
-    for (uint32_t row = blockIdx.x * 8 + (threadIdx.x >> 5); row < p; row += gridDim.x * 8) {
-        const T *src = x + rows.at(row);
-        auto read = [&](Eight<T> &v, int at) {
-            if (at >= k) v.zero();
-            else if constexpr (VEC) v.load(src + at);
-            else v.load_some(src + at, k - at);
-        };
-        Eight<T> kept[KEEP];
-        uint32_t top = 0;
+    const int lane = threadIdx.x & 31, sub = lane & (LPR - 1);
+    const uint32_t first = (blockIdx.x * 8 + (threadIdx.x >> 5)) * (RPI * SETS) + lane / LPR;
+    auto read = [&](Eight<T> &v, const T *src, int at) {
+        if (at >= k) v.zero();
+        else if constexpr (VEC) v.load(src + at);
+        else v.load_some(src + at, k - at);
+    };
+    Eight<T> kept[SETS][KEEP];
 #pragma unroll
-        for (int c = 0; c < KEEP; ++c) read(kept[c], (c * 32 + lane) * 8);
+    for (int s = 0; s < SETS; ++s) {
+        const T *src = x + rows.at(min(first + s * RPI, p - 1));
 #pragma unroll
-        for (int c = 0; c < KEEP; ++c) top = max(top, kept[c].top());
-        for (int at = (KEEP * 32 + lane) * 8; at < k; at += 256) {
-            Eight<T> v;
-            read(v, at);
-            top = max(top, v.top());
-        }
-        const RowScale rs = row_scale(Eight<T>::top_f32(__reduce_max_sync(0xffffffffu, top)));
+        for (int c = 0; c < KEEP; ++c) read(kept[s][c], src, (c * LPR + sub) * 8);
+    }
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+        const uint32_t row = first + s * RPI;
+        const T *src = x + rows.at(min(row, p - 1));
+        uint32_t top = kept[s][0].top();
+#pragma unroll
+        for (int c = 1; c < KEEP; ++c) top = max(top, kept[s][c].top());
+        if constexpr (LPR == 32)
+            for (int at = (KEEP * 32 + lane) * 8; at < k; at += 256) {
+                Eight<T> v;
+                read(v, src, at);
+                top = max(top, v.top());
+            }
+        if constexpr (LPR == 32) top = __reduce_max_sync(0xffffffffu, top);
+        else
+#pragma unroll
+            for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const RowScale rs = row_scale(Eight<T>::top_f32(top));
+        if (row >= p) continue;
         uint8_t *dst = codes + (size_t)row * pitch;
 #pragma unroll
         for (int c = 0; c < KEEP; ++c)
-            if ((c * 32 + lane) * 8 < pitch) *(uint2 *)(dst + (c * 32 + lane) * 8) = kept[c].codes(rs.inv);
-        for (int at = (KEEP * 32 + lane) * 8; at < pitch; at += 256) {
-            Eight<T> v;
-            read(v, at);
-            *(uint2 *)(dst + at) = v.codes(rs.inv);
-        }
-        if (lane == 0) scale[row] = rs.scale;
+            if ((c * LPR + sub) * 8 < pitch) *(uint2 *)(dst + (c * LPR + sub) * 8) = kept[s][c].codes(rs.inv);
+        if constexpr (LPR == 32)
+            for (int at = (KEEP * 32 + lane) * 8; at < pitch; at += 256) {
+                Eight<T> v;
+                read(v, src, at);
+                *(uint2 *)(dst + at) = v.codes(rs.inv);
+            }
+        if (sub == 0) scale[row] = rs.scale;
     }
 }
 
@@ -314,13 +329,22 @@ cudaError_t launch_gemm(const Problem &pb, const void *xq, const float *xs, cons
 }  // namespace
 
 cudaError_t launch_quant_rows(const Problem &pb, int dtype, const void *x, void *codes, float *scale, cudaStream_t st) {
-    const long long cap = (long long)device_sm_count() * 8, blocks = (pb.p + 7) / 8;
     const RowMap rows = quant_row_map(pb);
-    auto go = [&](auto tag) {
+    auto sized = [&](auto tag, auto lpr, auto keep) {
         using T = decltype(tag);
-        auto kernel = pb.c_in % 8 == 0 ? quant_rows_kernel<T, true> : quant_rows_kernel<T, false>;
-        return launch_pdl(kernel, dim3((unsigned)(blocks < cap ? blocks : cap)), dim3(256), 0, st, rows, (uint32_t)pb.p, pb.c_in,
-                          quant_pitch(pb), (const T *)x, (uint8_t *)codes, scale);
+        constexpr int LPR = decltype(lpr)::value, KEEP = decltype(keep)::value, PER = 8 * (32 / LPR) * (KEEP < 4 ? 4 / KEEP : 1);
+        auto kernel = pb.c_in % 8 == 0 ? quant_rows_kernel<T, LPR, KEEP, true> : quant_rows_kernel<T, LPR, KEEP, false>;
+        return launch_pdl(kernel, dim3((unsigned)((pb.p + PER - 1) / PER)), dim3(256), 0, st, rows, (uint32_t)pb.p, pb.c_in, quant_pitch(pb),
+                          (const T *)x, (uint8_t *)codes, scale);
+    };
+    auto go = [&](auto tag) {
+        using std::integral_constant;
+        if (pb.c_in <= 64) return sized(tag, integral_constant<int, 8>(), integral_constant<int, 1>());
+        if (pb.c_in <= 128) return sized(tag, integral_constant<int, 16>(), integral_constant<int, 1>());
+        if (pb.c_in <= 256) return sized(tag, integral_constant<int, 32>(), integral_constant<int, 1>());
+        if (pb.c_in <= 512) return sized(tag, integral_constant<int, 32>(), integral_constant<int, 2>());
+        if (pb.c_in <= 1024) return sized(tag, integral_constant<int, 32>(), integral_constant<int, 4>());
+        return sized(tag, integral_constant<int, 32>(), integral_constant<int, 8>());
     };
     return dtype == CONVBN_F32 ? go(float()) : (dtype == CONVBN_F16 ? go(__half()) : go(__nv_bfloat16()));
 }

@@ -136,7 +136,10 @@ def _check(got, t, dtype, stride, relu):
 SIZES = [(1, 1, 1, 1, 1), (1, 64, 1, 1, 64), (1, 2048, 1, 1, 1000), (2, 500, 1, 1, 10), (7, 256, 1, 1, 129), (16, 24, 1, 1, 2048),
          (17, 130, 1, 1, 40), (33, 1024, 1, 1, 256), (100, 512, 1, 1, 130), (128, 64, 1, 1, 64), (129, 96, 1, 1, 200), (300, 2000, 1, 1, 72),
          (1000, 256, 1, 1, 64), (2, 64, 13, 11, 256), (3, 256, 9, 15, 64), (1, 1024, 14, 14, 512), (2, 2048, 7, 7, 512), (5, 8, 3, 7, 8),
-         (40, 512, 7, 7, 2048), (6, 192, 21, 19, 320), (9500, 520, 1, 1, 1032), (1700, 1032, 1, 1, 1500), (300, 4104, 1, 1, 2056)]
+         (40, 512, 7, 7, 2048), (6, 192, 21, 19, 320), (9500, 520, 1, 1, 1032), (1700, 1032, 1, 1, 1500), (300, 4104, 1, 1, 2056),
+         # rows enough for the kernel that makes codes on its way (148 units of 128)
+         (19000, 256, 1, 1, 64), (20001, 64, 1, 1, 256), (19500, 128, 1, 1, 200), (25000, 192, 1, 1, 320), (19001, 40, 1, 1, 129),
+         (40000, 16, 1, 1, 8), (19200, 256, 1, 1, 1032), (31, 64, 27, 28, 640)]
 
 
 @pytest.mark.gpu
@@ -152,7 +155,7 @@ def test_forward_against_the_definition(size, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("size", [(2, 256, 15, 14, 512), (1, 40, 7, 9, 24), (3, 512, 28, 28, 128)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("size", [(2, 256, 15, 14, 512), (1, 40, 7, 9, 24), (3, 512, 28, 28, 128), (14, 256, 111, 114, 64), (7, 96, 160, 161, 40)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("stride", [2, 3])
 def test_strided_shortcuts(size, stride):
     n, ci, h, w, co = size
