@@ -266,9 +266,10 @@ int convbn_deploy_bwd(const convbn_desc *desc, const void *dz, const void *x,
  *
  * The product of a deployed block with both operands in 8 bits: a scale for every output channel, fixed once, and one for
  * every row of X (the channels of an output pixel; a token), formed by each call.
- *     prepare:  a = max_k |omega[co][k]|   w_codes = rne(omega * fl(127 / a))   w_scale = s a / 127   b_fused = b'
- *     forward:  a = max_k |x[p][k]|        xq = rne(x * fl(127 / a))
+ *     prepare:  a = max_k |omega[co][k]|   w_codes = rne(omega i)   w_scale = s a / 127   b_fused = b'
+ *     forward:  a = max_k |x[p][k]|        xq = rne(x i)
  *               z = (sum_k xq w_codes) (a / 127) w_scale + b_fused,   with `add` z + add, with relu != 0 max(z, 0)
+ * with i = fl(127 fl(1 / a)) in fp32 and the product rounded once, to the nearest integer (ties to even).
  * The BatchNorm scale s is part of the channel scale: the codes are omega's own.  Products are exact, sums exact in 32 bits;
  * one rounding to the storage type, when z is written.  A row or a channel whose largest magnitude is below 2^-100 counts as zero; one
  * with an infinity or a NaN gives NaN (which max(., 0) turns into 0, as convbn_relu does).

@@ -31,15 +31,16 @@ def unpack(codes, steps):
 
 
 def row_codes(x):
-    """(codes, scale) of every row of a matrix of values of the storage type; the factor is the fp32 quotient."""
+    """(codes, scale) of every row of a matrix of values of the storage type; the factor is 127 times the
+    reciprocal, each rounded to fp32."""
     x = np.asarray(x, np.float64)
     finite = np.isfinite(x).all(1)
     v = np.where(finite[:, None], x, 0.0)
     top = np.abs(v).max(1).astype(np.float32)
     live = finite & (top >= 2.0 ** -100)
     with np.errstate(divide="ignore", over="ignore"):
-        inv = np.where(live, np.float32(127) / np.where(live, top, np.float32(1)), np.float32(0)).astype(np.float64)
-    scale = np.where(finite, np.where(live, top / np.float32(127), np.float32(0)), np.nan).astype(np.float64)
+        inv = np.where(live, np.float32(127) * (np.float32(1) / np.where(live, top, np.float32(1))), np.float32(0)).astype(np.float64)
+    scale = np.where(finite, np.where(live, top.astype(np.float64) / 127, 0.0), np.nan)
     return np.rint(v * inv[:, None]), scale
 
 

@@ -223,7 +223,7 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded,
         return pl;
     }
     if (phase == CONVBN_PHASE_DEPLOY_FWD_QUANT) {
-        if (!quant_path(d, pb) || quant_fused_eligible(pb, (int)elem_size(d->dtype))) return pl;
+        if (!quant_path(d, pb) || quant_fused_eligible(pb, (int)elem_size(d->dtype)) || quant_small_eligible(pb)) return pl;
         pl.unpacked = take(quant_codes_bytes(pb));
         pl.inner = take((size_t)pb.p * sizeof(float));
         pl.total = off;
@@ -1442,6 +1442,11 @@ int convbn_deploy_fwd_quant(const convbn_desc *desc, const void *x, const void *
     if (quant_fused_eligible(pb, (int)elem_size(desc->dtype))) {
         LAUNCH("quant_fused", launch_quant_fused(pb, storage_type(desc), x, w_codes, w_scale, b_fused, add, relu ? 1 : 0, z, st));
         t_last_kernel[CONVBN_PHASE_DEPLOY_FWD_QUANT] = "umma";
+        return CONVBN_OK;
+    }
+    if (quant_small_eligible(pb)) {
+        LAUNCH("quant_small", launch_quant_small(pb, storage_type(desc), x, w_codes, w_scale, b_fused, add, relu ? 1 : 0, z, st));
+        t_last_kernel[CONVBN_PHASE_DEPLOY_FWD_QUANT] = "mma";
         return CONVBN_OK;
     }
     float *xs = (float *)at(workspace, pl.inner);

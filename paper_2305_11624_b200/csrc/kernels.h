@@ -342,6 +342,10 @@ cudaError_t launch_quant_weights(const Problem &pb, int dtype, const void *w, co
 bool quant_fused_eligible(const Problem &pb, int elem_bytes);
 cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, const void *wq, const float *ws, const float *shift,
                                const void *add, int relu, void *z, cudaStream_t st);
+// The same for few rows (quant_small.cu).
+bool quant_small_eligible(const Problem &pb);
+cudaError_t launch_quant_small(const Problem &pb, int dtype, const void *x, const void *wq, const float *ws, const float *shift,
+                               const void *add, int relu, void *z, cudaStream_t st);
 // The two as kernels of their own (quant_gemm.cu).
 // codes [p][pitch], scale [p]: of the rows of X that the output pixels read
 cudaError_t launch_quant_rows(const Problem &pb, int dtype, const void *x, void *codes, float *scale, cudaStream_t st);

@@ -11,14 +11,16 @@ namespace convbn {
 // Largest magnitudes below this count as zero: 127 / a would not be finite.
 constexpr float kQuantTiny = 7.8886091e-31f;      // 2^-100
 
+// The factor is 127 times the rounded reciprocal (two roundings, and part of the definition: x times it may lie on a half), the
+// scale a times the rounded 1 / 127.
 struct RowScale { float inv, scale; };            // 127 / a, a / 127
 __device__ __forceinline__ RowScale row_scale(uint32_t top) {      // bits of the largest magnitude as fp32
     const float a = __uint_as_float(top);
     if (top >= 0x7F800000u) return {0.f, __uint_as_float(0x7FC00000u)};     // (codes 0, scale NaN: so is every result)
     if (a < kQuantTiny) return {0.f, 0.f};
-    return {__fdiv_rn(127.f, a), __fdiv_rn(a, 127.f)};
+    return {__fmul_rn(__frcp_rn(a), 127.f), __fmul_rn(a, 1.f / 127.f)};
 }
-// 1.5 2^23 + code: the code is the low byte.  |x inv| <= 127 (1 + 2^-24), so no clamp; the product is exact inside the fma.
+// 1.5 2^23 + code: the code is the low byte.  |x inv| <= 127 (1 + 2^-23), so no clamp; the product is exact inside the fma.
 __device__ __forceinline__ uint32_t code_bits(float x, float inv) { return __float_as_uint(fmaf(x, inv, 12582912.f)); }
 __device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);

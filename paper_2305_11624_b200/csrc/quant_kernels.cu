@@ -5,8 +5,8 @@
 //     z[p][co] = (sum_k xq wq) xs[p] ws[co] + b'[co]
 //
 // The BatchNorm scale s goes into the channel scale, so the weights' codes are those of omega itself and no folded weight is
-// rounded.  The sum is exact in 32 bits up to C_in = 131072; a code is the rounding of the exact product x * fl(127 / a), formed
-// by one fused multiply-add, so it does not depend on how a compiler or a library rounds in between.
+// rounded.  The sum is exact in 32 bits up to C_in = 131072; a code is the rounding of the exact product of x
+// and fl(127 fl(1 / a)), formed by one fused multiply-add, so it does not depend on how a compiler or a library rounds in between.
 #include "kernels.h"
 #include "quant8.cuh"
 
