@@ -217,7 +217,7 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded,
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
     if (phase == CONVBN_PHASE_TUNE_BWD_PACKED) {
-        pl.unpacked = take((size_t)pb.pin * pb.c_in * elem_size(d->dtype));
+        if (!fused_bwd_path(d, pb)) pl.unpacked = take((size_t)pb.pin * pb.c_in * elem_size(d->dtype));
         pl.inner = take(make_plan(d, pb, CONVBN_PHASE_TUNE_BWD).total);
         pl.total = off;
         return pl;
@@ -1040,6 +1040,25 @@ int side_by_side(cudaStream_t st, Side &&side, Main &&main_pass) {
 }  // namespace
 
 extern "C" {
+// The parameter gradients of a single-kernel backward pass from its partial sums: on the caller's stream, or, deferred, on the side
+// lane (dX is complete on the caller's stream).
+static int finish_fused_bwd(const Problem &pb, const Plan &pl, const float *partials, const float *bsum, const void *w, const float *vec3,
+                            const float *b, const float *run_mean, float *dw, float *db, float *dgamma, float *dbeta, cudaStream_t st,
+                            bool defer_join) {
+    if (defer_join && !g_prof.on) {
+        SideLane *lane = nullptr;
+        CK(side_lane(&lane));
+        CU(cudaEventRecord(lane->fork, st));
+        CU(cudaStreamWaitEvent(lane->stream, lane->fork, 0));
+        cudaStream_t st = lane->stream;
+        LAUNCH("wgrad_rows", launch_wgrad_rows(pb, pl.uw.splits, partials, bsum, w, vec3, b, run_mean, dw, db, dgamma, dbeta, true, st));
+        lane->pending = true;
+        return CONVBN_OK;
+    }
+    LAUNCH("wgrad_rows", launch_wgrad_rows(pb, pl.uw.splits, partials, bsum, w, vec3, b, run_mean, dw, db, dgamma, dbeta, true, st));
+    return CONVBN_OK;
+}
+
 static int tune_bwd_impl(const convbn_desc *desc, const void *dz, const void *x, const void *w, const float *b,
                          const float *run_mean, const void *saved, void *dx, float *dw, float *db, float *dgamma,
                          float *dbeta, void *workspace, size_t workspace_bytes, void *stream, bool defer_join,
@@ -1107,19 +1126,7 @@ static int tune_bwd_impl(const convbn_desc *desc, const void *dz, const void *x,
     const float *vec3 = (const float *)saved;
     LAUNCH("umma_bwd", launch_fused_bwd1x1(pb, dz, x, w, vec3, dx, partials, bsum, st, &post));
     t_last_kernel[CONVBN_PHASE_TUNE_BWD] = "umma-fused-bwd";
-    if (defer_join && !g_prof.on) {
-        // dX is complete on the caller's stream; the parameter gradients are finished on the side lane
-        SideLane *lane = nullptr;
-        CK(side_lane(&lane));
-        CU(cudaEventRecord(lane->fork, st));
-        CU(cudaStreamWaitEvent(lane->stream, lane->fork, 0));
-        cudaStream_t st = lane->stream;
-        LAUNCH("wgrad_rows", launch_wgrad_rows(pb, pl.uw.splits, partials, bsum, w, vec3, b, run_mean, dw, db, dgamma, dbeta, true, st));
-        lane->pending = true;
-        return CONVBN_OK;
-    }
-    LAUNCH("wgrad_rows", launch_wgrad_rows(pb, pl.uw.splits, partials, bsum, w, vec3, b, run_mean, dw, db, dgamma, dbeta, true, st));
-    return CONVBN_OK;
+    return finish_fused_bwd(pb, pl, partials, bsum, w, vec3, b, run_mean, dw, db, dgamma, dbeta, st, defer_join);
 }
 
 int convbn_tune_bwd(const convbn_desc *desc, const void *dz, const void *x, const void *w, const float *b,
@@ -1205,6 +1212,14 @@ int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *
     const Plan pl = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD_PACKED);
     CK(check_ws(pl, workspace, workspace_bytes));
     cudaStream_t st = (cudaStream_t)stream;
+    if (fused_bwd_path(desc, pb)) {
+        const Plan pt = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD);
+        float *partials = (float *)at(workspace, pl.inner + pt.partials), *bsum = (float *)at(workspace, pl.inner + pt.bsum);
+        const float *vec3 = (const float *)saved;
+        LAUNCH("packed_bwd", launch_packed_bwd1x1(pb, dz, codes, steps, w, vec3, dx, partials, bsum, add, relu_mask != 0, st));
+        t_last_kernel[CONVBN_PHASE_TUNE_BWD_PACKED] = "umma-fused-bwd";
+        return finish_fused_bwd(pb, pt, partials, bsum, w, vec3, b, run_mean, dw, db, dgamma, dbeta, st, begin != 0);
+    }
     void *x = at(workspace, pl.unpacked);
     LAUNCH("unpack", launch_unpack(desc->dtype == CONVBN_BF16 && call_f16() ? CONVBN_F16 : desc->dtype, codes, steps, x,
                                    pb.pin * pb.c_in, st));

@@ -332,6 +332,11 @@ cudaError_t launch_tconv_param_epilogue(int dtype, bool nhwc, int c_out, int tap
 cudaError_t launch_pack(int dtype, const void *x, void *codes, void *steps, long long count, cudaStream_t st);
 cudaError_t launch_unpack(int dtype, const void *codes, const void *steps, void *out, long long count, cudaStream_t st);
 
+// The fused backward of a 1x1 layer (fused_bwd1x1_eligible) from packed X: umma_bwd1x1_packed.cu.  partials, bsum: as for
+// launch_fused_bwd1x1.
+cudaError_t launch_packed_bwd1x1(const Problem &pb, const void *dz, const void *codes, const void *steps, const void *w, const float *vec3,
+                                 void *dx, float *partials, float *bsum, const void *add, bool mask, cudaStream_t st);
+
 // The deployed 1x1 block as a product of 8-bit integers (quant_kernels.cu).  Rows of codes are quant_pitch bytes apart.
 bool quant_eligible(const Problem &pb);
 inline int quant_pitch(const Problem &pb) { return (pb.c_in + 15) / 16 * 16; }

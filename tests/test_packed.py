@@ -144,6 +144,8 @@ LAYERS = [
     I.LayerSpec("wide_in_128", 3, 128, 14, 13, 64, 1, 1),
     I.LayerSpec("wide_out", 2, 64, 17, 19, 256, 1, 1),
     I.LayerSpec("wide_out_128", 5, 64, 11, 13, 128, 1, 1),
+    I.LayerSpec("wide_in_many_tiles", 13, 256, 56, 55, 64, 1, 1),        # several tiles a CTA, the last one short
+    I.LayerSpec("wide_out_many_tiles", 13, 64, 56, 55, 128, 1, 1),
     I.LayerSpec("wide_few_pixels", 1, 256, 3, 5, 64, 1, 1),
     I.LayerSpec("one_pixel", 1, 64, 1, 1, 64, 1, 1),
     I.LayerSpec("rows", 777, 256, 1, 1, 192, 1, 1),                      # Linear-BN
