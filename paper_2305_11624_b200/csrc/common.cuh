@@ -81,6 +81,13 @@ __device__ __forceinline__ void unpack2_t(uint32_t bits, float &lo, float &hi) {
     if constexpr (F16) { const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&bits)); lo = f.x; hi = f.y; }
     else { lo = __uint_as_float(bits << 16); hi = __uint_as_float(bits & 0xFFFF0000u); }
 }
+// prmt with its sign mode, which __byte_perm leaves out: nibble i + 8 of SEL is eight times the sign of byte i.
+template <uint32_t SEL>
+__device__ __forceinline__ uint32_t sign_bytes(uint32_t v) {
+    uint32_t r;
+    asm("prmt.b32 %0, %1, 0, %2;" : "=r"(r) : "r"(v), "n"(SEL));
+    return r;
+}
 // What a residual network does next with a block's result, on eight 16-bit values: v + a (rounded again, as an add of two
 // stored tensors is), max(v, 0), v where m > 0 and 0 elsewhere.  Two values per instruction: the 16-bit sum is the rounded
 // exact one, which an fp32 sum rounded to 16 bits is too (24 >= 2 * 11 + 2 significant bits).

@@ -57,6 +57,9 @@ struct ProfScope {
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 inline size_t elem_size(int dtype) { return dtype == CONVBN_F32 ? 4 : 2; }
 
+// The caller's storage type inside a call that runs as its bf16 twin (HalfCall).
+inline int storage_type(const convbn_desc *d) { return d->dtype == CONVBN_BF16 && call_f16() ? CONVBN_F16 : d->dtype; }
+
 int make_problem(const convbn_desc *d, Problem *pb) {
     if (!d) return CONVBN_EINVAL;
     if (d->n <= 0 || d->c_in <= 0 || d->h_in <= 0 || d->w_in <= 0 || d->c_out <= 0 || d->kh <= 0 ||
@@ -152,6 +155,7 @@ bool quant_path(const convbn_desc *d, const Problem &pb) {
 
 bool strided_dgrad_ok(const convbn_desc *d, const Problem &pb);
 bool umma_dgrad_shape(const convbn_desc *d, const Problem &pb, UmmaConvShape *s);
+bool packed_path(const convbn_desc *d, const Problem &pb);
 
 // bounded: the tensor-core weight gradient in the slices of a call with a fixed scratch, a stem's without a packed copy of X;
 // sums: what it sums beside.
@@ -217,7 +221,7 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded,
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
     if (phase == CONVBN_PHASE_TUNE_BWD_PACKED) {
-        if (!fused_bwd_path(d, pb)) pl.unpacked = take((size_t)pb.pin * pb.c_in * elem_size(d->dtype));
+        if (!fused_bwd_path(d, pb) && !packed_path(d, pb)) pl.unpacked = take((size_t)pb.pin * pb.c_in * elem_size(d->dtype));
         pl.inner = take(make_plan(d, pb, CONVBN_PHASE_TUNE_BWD).total);
         pl.total = off;
         return pl;
@@ -404,6 +408,21 @@ bool umma_dgrad_shape(const convbn_desc *d, const Problem &pb, UmmaConvShape *s)
                        pb.pad_h - (pb.kh - 1) * pb.dil_h, pb.pad_w - (pb.kw - 1) * pb.dil_w, 1, 1, pb.dil_h,
                        pb.dil_w};
     return umma_conv_eligible(*s);
+}
+
+// Whether the backward pass takes packed X as it is: dense tensor-core layers, the weight gradient restores it on its way, and the data
+// pass, which wants it as a mask alone, reads that from the codes (the kernel of umma_conv.cu does).  The weight gradient restores X once
+// for every tap and every 128 output channels: whole calls that way and with X restored in the workspace first, us: one such pass 1x1
+// 512 -> 128 at 28 x 28, N = 32 31.5 and 38.0, 64 -> 64 at 56 x 56, N = 256 96 and 121; two 1024 -> 256 at 14 x 14, N = 32 25.6 and 28.5;
+// four 2048 -> 512 at 7 x 7, N = 64 32.5 and 34.2, 20000 rows 1024 -> 512 98.7 and 103.2, but 128 -> 512 at 28 x 28,
+// N = 32 32.1 and 28.1; eight 256 -> 1024 at 14 x 14, N = 32 23.9 and
+// 20.6; nine 3x3 64 -> 64 at 56 x 56, N = 32 43.9 and 38.0; sixteen 2048 -> 512 the other way, N = 64 33.2 and 27.1.  (X restored on
+// the side lane while the data pass runs gains nothing over restoring it first: 38.5, 22.6, 27.5 for the last three.)
+bool packed_path(const convbn_desc *d, const Problem &pb) {
+    UmmaConvShape s;
+    return d->dtype == CONVBN_BF16 && d->layout == CONVBN_NHWC && umma_wgrad_eligible(pb) &&
+           (long long)pb.kh * pb.kw * ((pb.c_out + 127) / 128) <= (pb.c_in >= 1024 ? 4 : 2) && umma_dgrad_shape(d, pb, &s) && !umma_strip_eligible(s) &&
+           pb.pin < (1LL << 31);
 }
 
 // Taps of one residue class of a strided backward-data pass (unit dilation): r = r_max - stride m for
@@ -721,7 +740,8 @@ int run_f32_bwd(const convbn_desc *d, const Problem &pb, int groups, float *part
 //   scale_only          : dw = s domega' alone, s the first C_out floats of vec3 (dense tensor-core path)
 int run_param_grads(const convbn_desc *d, const Problem &pb, const Plan &pl, const void *dz, const void *x,
                     const void *w, const float *vec3, const float *b, const float *mean, float *dw, float *db,
-                    float *dgamma, float *dbeta, void *ws, cudaStream_t st, const char **which, bool scale_only = false) {
+                    float *dgamma, float *dbeta, void *ws, cudaStream_t st, const char **which, bool scale_only = false,
+                    const PackedTensor *packed_x = nullptr) {
     float *partials = (float *)at(ws, pl.partials), *bsum = (float *)at(ws, pl.bsum);
     const bool need_bsum = (vec3 || db) && !scale_only;
     if (f32_path(d, pb))
@@ -756,7 +776,7 @@ int run_param_grads(const convbn_desc *d, const Problem &pb, const Plan &pl, con
                                                              dgamma, dbeta, st));
         *which = "grouped-umma";
     } else if (pl.umma_wgrad) {
-        LAUNCH("umma_wgrad", launch_umma_wgrad(pb, pl.uw, dz, x, partials, bsum, st));
+        LAUNCH("umma_wgrad", launch_umma_wgrad(pb, pl.uw, dz, x, partials, bsum, st, nullptr, 0, WgradSums::kDz, packed_x));
         LAUNCH("wgrad_rows", launch_wgrad_rows(pb, pl.uw.splits, partials, bsum, w, vec3, b, mean, dw, db, dgamma, dbeta, need_bsum, st));
         *which = "umma";
     } else if (pl.dw_tma_wgrad) {
@@ -944,7 +964,8 @@ int convbn_tune_bwd_data(const convbn_desc *desc, const void *dz, const void *w,
 
 static int tune_bwd_weight_impl(const convbn_desc *desc, const void *dz, const void *x, const void *w, const float *b,
                                 const float *run_mean, const void *saved, float *dw, float *db, float *dgamma, float *dbeta,
-                                void *workspace, size_t workspace_bytes, void *stream, bool bounded) {
+                                void *workspace, size_t workspace_bytes, void *stream, bool bounded,
+                                const PackedTensor *packed_x = nullptr) {
     HalfCall half(desc);              // CONVBN_F16: checked here, then run as the 16-bit path with the half flag set
     if (half.status != CONVBN_OK) return half.status;
     desc = half.use;
@@ -952,7 +973,7 @@ static int tune_bwd_weight_impl(const convbn_desc *desc, const void *dz, const v
     t_prof_phase = "bwd_weight";
     CK(make_problem(desc, &pb));
     CK(check_pair(desc));
-    if (!dz || !x || !w || !run_mean || !saved || !dw || !dgamma || !dbeta) return CONVBN_EINVAL;
+    if (!dz || !(x || packed_x) || !w || !run_mean || !saved || !dw || !dgamma || !dbeta) return CONVBN_EINVAL;
     if ((b == nullptr) != (db == nullptr)) return CONVBN_EINVAL;
     if (!aligned(dz, 16) || !aligned(x, 16) || !aligned(w, 16) || !aligned(saved, 16) ||
         !aligned(dw, 16) || !aligned(b, 4) || !aligned(run_mean, 4) || !aligned(db, 4) ||
@@ -962,7 +983,7 @@ static int tune_bwd_weight_impl(const convbn_desc *desc, const void *dz, const v
     CK(check_ws(pl, workspace, workspace_bytes));
     cudaStream_t st = (cudaStream_t)stream;
     CK(run_param_grads(desc, pb, pl, dz, x, w, (const float *)saved, b, run_mean, dw, db, dgamma, dbeta,
-                       workspace, st, &t_last_kernel[CONVBN_PHASE_TUNE_BWD_WEIGHT]));
+                       workspace, st, &t_last_kernel[CONVBN_PHASE_TUNE_BWD_WEIGHT], false, packed_x));
     return CONVBN_OK;
 }
 
@@ -1062,7 +1083,7 @@ static int finish_fused_bwd(const Problem &pb, const Plan &pl, const float *part
 static int tune_bwd_impl(const convbn_desc *desc, const void *dz, const void *x, const void *w, const float *b,
                          const float *run_mean, const void *saved, void *dx, float *dw, float *db, float *dgamma,
                          float *dbeta, void *workspace, size_t workspace_bytes, void *stream, bool defer_join,
-                         const PostOp &post = PostOp()) {
+                         const PostOp &post = PostOp(), const PackedTensor *packed_x = nullptr) {
     HalfCall half(desc);              // CONVBN_F16: checked here, then run as the 16-bit path with the half flag set
     if (half.status != CONVBN_OK) return half.status;
     desc = half.use;
@@ -1070,7 +1091,7 @@ static int tune_bwd_impl(const convbn_desc *desc, const void *dz, const void *x,
     t_prof_phase = "bwd";
     CK(make_problem(desc, &pb));
     CK(check_pair(desc));
-    if (!dz || !x || !w || !run_mean || !saved || !dx || !dw || !dgamma || !dbeta) return CONVBN_EINVAL;
+    if (!dz || !(x || packed_x) || !w || !run_mean || !saved || !dx || !dw || !dgamma || !dbeta) return CONVBN_EINVAL;
     if ((b == nullptr) != (db == nullptr)) return CONVBN_EINVAL;
     if (!aligned(dz, 16) || !aligned(x, 16) || !aligned(w, 16) || !aligned(saved, 16) || !aligned(dx, 16) ||
         !aligned(dw, 16) || !aligned(b, 4) || !aligned(run_mean, 4) || !aligned(db, 4) || !aligned(dgamma, 4) ||
@@ -1095,24 +1116,26 @@ static int tune_bwd_impl(const convbn_desc *desc, const void *dz, const void *x,
         void *ws_w = workspace ? at(workspace, pl.w_scaled) : nullptr;
         const size_t bytes_d = pl.w_scaled, bytes_w = pl.total - pl.w_scaled;
         t_last_kernel[CONVBN_PHASE_TUNE_BWD] = "two-calls";
+        auto weight_pass = [&](void *on) -> int {
+            return tune_bwd_weight_impl(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, ws_w, bytes_w, on, false, packed_x);
+        };
         if (g_prof.on) {                 // per-kernel timing wants one stream, deferred or not
             CK(tune_bwd_data_impl(desc, dz, w, saved, dx, post, workspace, bytes_d, stream));
-            return convbn_tune_bwd_weight(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, ws_w, bytes_w, stream);
+            return weight_pass(stream);
         }
         if (!defer_join && !data_pass_first(desc, pb, (cudaStream_t)stream))
             return side_by_side(
                 (cudaStream_t)stream,
                 [&](cudaStream_t lane) { return tune_bwd_data_impl(desc, dz, w, saved, dx, post, workspace, bytes_d, lane); },
                 [&]() {
-                    return convbn_tune_bwd_weight(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, ws_w, bytes_w, stream);
+                    return weight_pass(stream);
                 });
         SideLane *lane = nullptr;
         CK(side_lane(&lane));
         cudaStream_t st = (cudaStream_t)stream;
         CU(cudaEventRecord(lane->fork, st));
         CU(cudaStreamWaitEvent(lane->stream, lane->fork, 0));
-        const int sw = convbn_tune_bwd_weight(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, ws_w, bytes_w,
-                                              lane->stream);
+        const int sw = weight_pass(lane->stream);
         // whatever happened on the lane, the caller's stream joins it again (a capture must not be left forked)
         const bool joined = defer_join || cudaEventRecord(lane->join, lane->stream) == cudaSuccess;
         const int sd = tune_bwd_data_impl(desc, dz, w, saved, dx, post, workspace, bytes_d, stream);
@@ -1220,9 +1243,18 @@ int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *
         t_last_kernel[CONVBN_PHASE_TUNE_BWD_PACKED] = "umma-fused-bwd";
         return finish_fused_bwd(pb, pt, partials, bsum, w, vec3, b, run_mean, dw, db, dgamma, dbeta, st, begin != 0);
     }
+    if (packed_path(desc, pb)) {
+        const PackedTensor px{codes, steps};
+        PostOp post;
+        post.add = add;
+        post.mask_codes = relu_mask ? codes : nullptr;
+        CK(tune_bwd_impl(desc, dz, nullptr, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta, at(workspace, pl.inner),
+                         pl.total - pl.inner, stream, begin != 0, post, &px));
+        t_last_kernel[CONVBN_PHASE_TUNE_BWD_PACKED] = "umma";
+        return CONVBN_OK;
+    }
     void *x = at(workspace, pl.unpacked);
-    LAUNCH("unpack", launch_unpack(desc->dtype == CONVBN_BF16 && call_f16() ? CONVBN_F16 : desc->dtype, codes, steps, x,
-                                   pb.pin * pb.c_in, st));
+    LAUNCH("unpack", launch_unpack(storage_type(desc), codes, steps, x, pb.pin * pb.c_in, st));
     PostOp post;
     post.add = add;
     post.mask = relu_mask ? x : nullptr;
@@ -1415,7 +1447,6 @@ int convbn_deploy_bwd(const convbn_desc *desc, const void *dz, const void *x, co
 }
 
 // ---- Deploy mode in 8-bit integers -------------------------------------------------------------------
-static int storage_type(const convbn_desc *d) { return d->dtype == CONVBN_BF16 && call_f16() ? CONVBN_F16 : d->dtype; }
 
 int convbn_deploy_prepare_quant(const convbn_desc *desc, const void *w, const float *b, const float *gamma, const float *beta,
                                 const float *run_mean, const float *run_var, void *w_codes, float *w_scale, float *b_fused,

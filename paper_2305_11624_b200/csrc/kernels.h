@@ -36,7 +36,12 @@ cudaError_t launch_direct_wgrad(const Problem &pb, int dtype, int layout, const 
 struct PostOp {
     const void *add = nullptr, *mask = nullptr;
     int relu = 0;
-    bool any() const { return add || mask || relu; }
+    const void *mask_codes = nullptr;      // the mask as a packed tensor's codes (dense outputs of umma_conv.cu only)
+    bool any() const { return add || mask || relu || mask_codes; }
+};
+// A tensor as convbn_pack leaves it.
+struct PackedTensor {
+    const void *codes = nullptr, *steps = nullptr;
 };
 // BatchNorm parameters for in-kernel reparameterisation: the kernel forms s and b' per output channel,
 // computes out = s * (wmat (*) act) + b' and (CTA 0) writes [s | b' | r] to vec3 (3 cn floats, may be NULL).
@@ -147,7 +152,8 @@ UmmaWgradPlan umma_wgrad_plan_bounded(const Problem &pb);     // for calls with 
 // counters: `ncounters` words zeroed for an epilogue that counts its blocks (may be NULL)
 cudaError_t launch_umma_wgrad(const Problem &pb, const UmmaWgradPlan &pl, const void *dz, const void *x,
                               float *partials, float *bsum, cudaStream_t st, unsigned int *counters = nullptr,
-                              int ncounters = 0, WgradSums sums = WgradSums::kDz);
+                              int ncounters = 0, WgradSums sums = WgradSums::kDz,
+                              const PackedTensor *packed_x = nullptr);
 // Everything after the GEMM: dw[co][k] = scale[co] * sum_splits partials (scale = first
 // C_out floats of vec3, 1 if NULL); with need_sums also dbeta, db, dgamma (vec3 given) or db = sum dZ.
 cudaError_t launch_wgrad_rows(const Problem &pb, int splits, const float *partials, const float *bsum, const void *w,

@@ -99,28 +99,28 @@ __global__ void __launch_bounds__(256) unpack_kernel(const uint8_t *__restrict__
     const long long turns = (count + kPer - 1) / kPer;
     for (long long i = blockIdx.x * (long long)blockDim.x + threadIdx.x; i < turns; i += (long long)gridDim.x * blockDim.x) {
         const long long at = i * kPer;
-        const float step = pack_step(__ldg(steps + (i >> 1)));
+        const uint32_t byte = __ldg(steps + (i >> 1));
         if (at + kPer <= count) {
+            const float step = pack_step(byte);
+            const f32x2 by = pair(step, step);
             const uint4 q = __ldg((const uint4 *)(codes + at));
             const uint32_t w[4] = {q.x, q.y, q.z, q.w};
             uint4 o[kPer * sizeof(T) / 16];
             uint32_t *r = (uint32_t *)o;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                float f[4];
-                codes_to_f32(w[k], f);
-                if constexpr (sizeof(T) == 2) {
-                    r[2 * k] = pack2_t<!__is_same(T, __nv_bfloat16)>(f[0] * step, f[1] * step);
-                    r[2 * k + 1] = pack2_t<!__is_same(T, __nv_bfloat16)>(f[2] * step, f[3] * step);
-                } else {
+                f32x2 f[2];
+                restore4(w[k], by, f);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) r[4 * k + j] = __float_as_uint(f[j] * step);
+                for (int j = 0; j < 2; ++j) {
+                    if constexpr (sizeof(T) == 2) r[2 * k + j] = narrow_t<!__is_same(T, __nv_bfloat16)>(f[j]);
+                    else { r[4 * k + 2 * j] = (uint32_t)f[j]; r[4 * k + 2 * j + 1] = (uint32_t)(f[j] >> 32); }
                 }
             }
 #pragma unroll
             for (int k = 0; k < (int)(kPer * sizeof(T) / 16); ++k) ((uint4 *)(out + at))[k] = o[k];
         } else {
-            for (int k = 0; at + k < count; ++k) out[at + k] = from_f32<T>((float)(int8_t)codes[at + k] * step);
+            for (int k = 0; at + k < count; ++k) out[at + k] = from_f32<T>((float)(int8_t)codes[at + k] * pack_step(byte));
         }
     }
 }

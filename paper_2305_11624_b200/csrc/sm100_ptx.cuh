@@ -22,6 +22,11 @@ bool make_tmap_im2col_bf16(CUtensorMap *tm, const void *base, int n, int h, int 
                            int lower_w, int upper_h, int upper_w, int stride_h, int stride_w, int pixels,
                            int channels);
 
+// The same two over a packed tensor's codes (64 of them side by side, 64-byte swizzle).
+bool make_tmap_im2col_codes(CUtensorMap *tm, const void *base, int n, int h, int w, int c, int lower_h, int lower_w, int upper_h,
+                            int upper_w, int stride_h, int stride_w, int pixels, int channels);
+bool make_tmap_codes(CUtensorMap *tm, const void *base, long long rows, long long cols, int box_rows);
+
 // General tiled map over bf16 data: rank <= 5, dims / byte strides (strides[0] unused) / box, 128-byte swizzle.
 bool make_tmap_tiled_bf16(CUtensorMap *tm, const void *base, int rank, const unsigned long long *dims,
                           const unsigned long long *strides_bytes, const unsigned int *box);

@@ -208,14 +208,15 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
             for (int a = 0; a < AHEAD; ++a) {
                 const int idx = a * 32 + lane, r = qw * 16 + idx / CHUNKS, c = idx % CHUNKS;
                 const float step = pack_step(next_step[a]);
+                const f32x2 by = pair(step, step);
                 const uint32_t word[4] = {next[a].x, next[a].y, next[a].z, next[a].w};
                 uint32_t o[8];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    float f[4];
-                    codes_to_f32(word[k], f);
-                    o[2 * k] = pack2_t<H>(f[0] * step, f[1] * step);
-                    o[2 * k + 1] = pack2_t<H>(f[2] * step, f[3] * step);
+                    f32x2 f[2];
+                    restore4(word[k], by, f);
+                    o[2 * k] = narrow_t<H>(f[0]);
+                    o[2 * k + 1] = narrow_t<H>(f[1]);
                 }
                 uint8_t *row = tile + (size_t)(c >> 2) * kPbBox + r * 128;
                 const int c16 = (c & 3) * 2;

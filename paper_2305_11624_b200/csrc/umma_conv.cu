@@ -61,6 +61,7 @@ struct ConvGemm {
     FastDiv by_n, by_wo, by_ho;                     // by the tiles of a row of tiles, wo, ho
     const __nv_bfloat16 *post_add, *post_mask;      // at the output's offsets
     int post_relu;
+    int mask_codes;                                 // kPost: the mask's box is of 8-bit codes (post_mask is not NULL)
 };
 
 struct ConvSmemCtl {
@@ -453,7 +454,7 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
             post_pending = extra > 0;
             if (!post_pending || lane != 0) return;
             uint64_t *bar = &ctl->post_full[warp - 2];
-            mbar_arrive_expect_tx(bar, (uint32_t)extra * kStagingWarpBytes);
+            mbar_arrive_expect_tx(bar, (uint32_t)extra * kStagingWarpBytes - (g.mask_codes ? kStagingWarpBytes / 2 : 0u));
             const int x = (int)n * BN + c0, y = (int)(m * kBM) + quarter * 32;
             if (g.post_add) tma_load_2d(add_buf, &tm_out2, bar, x, y);
             if (g.post_mask) tma_load_2d(mask_buf, &tm_mask, bar, x, y);
@@ -532,6 +533,25 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
                             post_ph ^= 1u;
                             if (!here && lane == 0) { atomicOr(err, ERRW_TIMEOUT); ctl->abort_flag = 1; }
                             __syncwarp();
+                            if (g.mask_codes) {
+                                // codes [32 rows][64 bytes] become 16-bit words of the same signs in the place of the mask's box (a
+                                // negative word is negative or no number, either way not above zero)
+                                const uint32_t from = smem_u32(mask_buf) + (uint32_t)lane * 64u, to = smem_u32(mask_buf) + (uint32_t)lane * 128u;
+                                uint32_t cw[16];
+#pragma unroll
+                                for (uint32_t q = 0; q < 4; ++q)
+                                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                                 : "=r"(cw[4 * q]), "=r"(cw[4 * q + 1]), "=r"(cw[4 * q + 2]), "=r"(cw[4 * q + 3])
+                                                 : "r"(from + ((q ^ ((uint32_t)(lane >> 1) & 3u)) << 4)) : "memory");
+                                __syncwarp();
+#pragma unroll
+                                for (uint32_t q = 0; q < 8; ++q)
+                                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
+                                                 ::"r"(to + ((q ^ ((uint32_t)lane & 7u)) << 4)), "r"(sign_bytes<0x9180>(cw[2 * q])),
+                                                   "r"(sign_bytes<0xB3A2>(cw[2 * q])), "r"(sign_bytes<0x9180>(cw[2 * q + 1])),
+                                                   "r"(sign_bytes<0xB3A2>(cw[2 * q + 1])) : "memory");
+                                __syncwarp();
+                            }
                         }
                     }
                     // (what follows the rounding is fixed outside the loop over the columns: one uniform branch per chunk)
@@ -772,6 +792,29 @@ bool make_tmap_im2col_bf16(CUtensorMap *tm, const void *base, int n, int h, int 
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_tmap_im2col_codes(CUtensorMap *tm, const void *base, int n, int h, int w, int c, int lower_h, int lower_w, int upper_h,
+                            int upper_w, int stride_h, int stride_w, int pixels, int channels) {
+    if (!load_encoders()) return false;
+    cuuint64_t dims[4] = {(cuuint64_t)c, (cuuint64_t)w, (cuuint64_t)h, (cuuint64_t)n};
+    cuuint64_t strides[3] = {(cuuint64_t)c, (cuuint64_t)w * c, (cuuint64_t)h * w * c};
+    int lower[2] = {lower_w, lower_h}, upper[2] = {upper_w, upper_h};
+    cuuint32_t estr[4] = {1, (cuuint32_t)stride_w, (cuuint32_t)stride_h, 1};
+    return g_encode_im2col(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(base), dims, strides, lower, upper, (cuuint32_t)channels,
+                           (cuuint32_t)pixels, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Row-major bytes [rows][cols] -> box of box_rows x 64 bytes, 64-byte swizzle.
+bool make_tmap_codes(CUtensorMap *tm, const void *base, long long rows, long long cols, int box_rows) {
+    if (!load_encoders()) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)cols};
+    cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    return g_encode_tiled(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 static bool encode_tiled_bf16(CUtensorMap *tm, const void *base, int rank, const unsigned long long *dims,
                               const unsigned long long *strides_bytes, const unsigned int *box, CUtensorMapSwizzle sw) {
     if (!load_encoders() || rank < 1 || rank > 5) return false;
@@ -905,7 +948,9 @@ cudaError_t launch_umma_conv(const UmmaConvShape &s, const void *act, const void
     g.out_sn = s.out_sn; g.out_sh = s.out_sh; g.out_sw = s.out_sw;
     const bool with_post = post && post->any();
     g.post_add = with_post ? (const __nv_bfloat16 *)post->add : nullptr;
-    g.post_mask = with_post ? (const __nv_bfloat16 *)post->mask : nullptr;
+    g.post_mask = with_post ? (const __nv_bfloat16 *)(post->mask_codes ? post->mask_codes : post->mask) : nullptr;
+    g.mask_codes = with_post && post->mask_codes;
+    if (g.mask_codes && (s.out_sw || s.cn % 64)) return cudaErrorInvalidValue;
     g.post_relu = with_post ? post->relu : 0;
     g.tap_c = s.tap_c; g.tap_kw = s.tap_kw; g.tap_sh = s.tap_sh; g.tap_sw = s.tap_sw;
     // The bounding box of base pixels has ho x wo positions: upper = lower + (out-1) stride - (in-1).
@@ -936,7 +981,9 @@ cudaError_t launch_umma_conv(const UmmaConvShape &s, const void *act, const void
     CUtensorMap tmask = tout;
     if (with_post && !s.out_sw) {
         if (g.post_add && !make_tmap_matrix_bf16(&tout2, post->add, g.p, s.cn, 32, 64)) return cudaErrorInvalidValue;
-        if (g.post_mask && !make_tmap_matrix_bf16(&tmask, post->mask, g.p, s.cn, 32, 64)) return cudaErrorInvalidValue;
+        if (g.post_mask && !(g.mask_codes ? make_tmap_codes(&tmask, post->mask_codes, g.p, s.cn, 32)
+                                          : make_tmap_matrix_bf16(&tmask, post->mask, g.p, s.cn, 32, 64)))
+            return cudaErrorInvalidValue;
         if (!g.post_add && !g.post_mask) return launch_mode<kRelu>(bn, pair, ta, tw, tout, tout2, tmask, g, bias, err, st);
         return launch_mode<kPost>(bn, pair, ta, tw, tout, tout2, tmask, g, bias, err, st);
     }
@@ -953,7 +1000,7 @@ cudaError_t launch_stem_fwd(const Problem &pb, const void *x_packed, const void 
     const int krows = stem_krows(pb);
     ConvGemm g;
     g.chunk_outer = 0;
-    g.tap_c = 0; g.post_add = g.post_mask = nullptr; g.post_relu = 0;
+    g.tap_c = 0; g.post_add = g.post_mask = nullptr; g.post_relu = 0; g.mask_codes = 0;
     g.ho = pb.h_out; g.wo = pb.w_out; g.cn = pb.c_out; g.ca = 64; g.taps_h = krows; g.taps_w = 1;
     g.lower_h = g.lower_w = 0; g.stride_h = g.stride_w = g.dil_h = g.dil_w = 1;
     g.stem = 1; g.stem_tw = 16; g.stem_th = 8;

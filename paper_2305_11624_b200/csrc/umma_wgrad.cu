@@ -9,6 +9,8 @@
 // fp32 partial tile, in the weights' layout part[split][co][k].  A second kernel adds the slices in fixed order and forms
 // domega, dgamma, ... from the fp32 sums (never from rounded values).
 #include "kernels.h"
+#include "pack8.cuh"
+#include "packed_f32.cuh"
 #include "sm100_ptx.cuh"
 
 namespace convbn {
@@ -45,6 +47,8 @@ struct WgradGemm {
     int sums;
     int f16;                // 16-bit storage type: 0 bf16, 1 IEEE half
     int rows;               // 1: partials are [split][C_out][kdim], 0: [split][k][C_out]
+    const uint8_t *steps;   // packed X: the steps, and the extent of X
+    int h_in, w_in;
 };
 
 enum { kSumNone, kSumSlice, kSumX };
@@ -54,10 +58,15 @@ struct WgradSmemCtl {
     uint64_t tmem_full;
     uint32_t tmem_base;
     int abort_flag;
+    uint64_t raw[kWMaxStages];       // PACKED: the codes of a stage have landed
 };
 
 // X_SUMS: g.sums is kSumX.
-template <int BN, bool X_SUMS>
+// PACKED: X comes as 8-bit codes (tm_x: a map of bytes) and steps.  A slice's codes land in the first half of its place, 64 bytes a
+// pixel; the epilogue warps, two per slice, take them into registers, meet, and write the 16-bit values (code * step, exact) over the
+// whole of it while earlier stages are multiplied.  (Which layers: packed_path in
+// convbn_api.cu.)
+template <int BN, bool X_SUMS, bool PACKED>
 __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_constant__ CUtensorMap tm_x,
                                                               const __grid_constant__ CUtensorMap tm_dz,
                                                               const WgradGemm g, float *__restrict__ partials,
@@ -104,7 +113,11 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
         ho0 = (int)(t0 - img * (uint32_t)g.ho);
     }
     if (threadIdx.x == 64) {
-        for (int s = 0; s < stages; ++s) { mbar_init(&ctl->full[s], 2); mbar_init(&ctl->empty[s], adds ? 5 : 1); }
+        for (int s = 0; s < stages; ++s) {
+            mbar_init(&ctl->full[s], PACKED ? 1 + 2 * a_chunks : 2);       // (PACKED: dZ and the warps that restore X)
+            mbar_init(&ctl->empty[s], adds ? 5 : 1);
+            if constexpr (PACKED) mbar_init(&ctl->raw[s], 1);
+        }
         mbar_init(&ctl->tmem_full, 1);
         ctl->abort_flag = 0;
         fence_barrier_init();
@@ -142,7 +155,8 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
         atomicOr(err, ERRW_TIMEOUT);
         ctl->abort_flag = 1;
         for (int kb = issued > stages ? issued - stages : 0; kb < issued; ++kb)     // let the copies in flight land
-            mbar_wait_bounded(&ctl->full[kb % stages], (uint32_t)(kb / stages) & 1u, nullptr, 200000000ull);
+            mbar_wait_bounded(PACKED && warp == 0 ? &ctl->raw[kb % stages] : &ctl->full[kb % stages], (uint32_t)(kb / stages) & 1u, nullptr,
+                              200000000ull);
     };
     // stem: pixel block -> (image, patch row, patch column) of 4 x 16 output pixels
     auto patch = [&](uint32_t blk, int &pw, int &phh, int &im) {
@@ -158,13 +172,14 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
         // Weight phase with its second kernel, graph replay: 3x3 512 at 7 x 7, N = 64 29.5 -> 25.5 us, N = 32 22.6 -> 20.6,
         // 3x3 64 at 56 x 56, N = 32 21.9 -> 19.4.
         if (elect_one()) {
-            const uint32_t tx_bytes = (uint32_t)a_chunks * kChunkBytes;
+            const uint32_t tx_bytes = (uint32_t)a_chunks * (PACKED ? kChunkBytes / 2 : kChunkBytes);
+            const uint32_t full_x = PACKED ? smem_u32(&ctl->raw[0]) : full0;
             const uint32_t blk0 = (uint32_t)(p0 / kWP);
 #pragma unroll 4
-            for (int kb = 0; kb < num_kb; ++kb) {
+            for (int kb = 0; kb < (PACKED && a_chunks == 0 ? 0 : num_kb); ++kb) {
                 if (!free) ok = mbar_wait_bounded(empty0 + sb, ph, abort_flag);
                 if (!ok) break;
-                const uint32_t bar = full0 + sb, dst = slot;
+                const uint32_t bar = full_x + sb, dst = slot;
                 ++issued; sb += 8; slot += kStageBytes;
                 if (sb == sb_end) { sb = 0; slot = tiles0; ph ^= 1u; }
                 free = mbar_test_wait(empty0 + sb, ph);
@@ -270,6 +285,66 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
             }
             const int k = k0 + slice * 64 + 2 * lane;
             if (slice < a_chunks) *(float2 *)(bsum + ((size_t)blockIdx.z * 2 + half) * g.kdim + k) = make_float2(lo, hi);
+        }
+        if constexpr (PACKED) {
+            const int slice = quarter >> 1, r = (quarter & 1) * 32 + lane;          // this lane's pixel of a stage
+            if (slice < a_chunks) {
+                const int kk = k0 + slice * 64, tap = (int)g.by_ci.div((uint32_t)kk), tr = (int)g.by_tw.div((uint32_t)tap);
+                const int c = kk - tap * g.c_in, dh = g.lower_h + tr * g.dil_h, dw = g.lower_w + (tap - tr * g.taps_w) * g.dil_w;
+                auto steps_of = [&](int kb) -> uint32_t {                           // both groups of 32 channels
+                    const long long at = p0 + (long long)kb * kWP + r;
+                    if (kb >= num_kb || at >= p1) return 0u;
+                    const uint32_t pp = (uint32_t)at, t0 = g.by_wo.div(pp), im = g.by_ho.div(t0);
+                    const int hi = dh + (int)(t0 - im * (uint32_t)g.ho) * g.stride_h, wi = dw + (int)(pp - t0 * (uint32_t)g.wo) * g.stride_w;
+                    if ((unsigned)hi >= (unsigned)g.h_in || (unsigned)wi >= (unsigned)g.w_in) return 0u;      // (codes 0 there)
+                    return __ldg((const unsigned short *)(g.steps + ((((size_t)im * g.h_in + hi) * g.w_in + wi) * g.c_in + c) / kPackGroup));
+                };
+                const uint32_t raw0 = smem_u32(&ctl->raw[0]), row = tiles0 + (uint32_t)slice * kChunkBytes;
+                // 64-byte swizzle of the codes, 128-byte swizzle of the values
+                const uint32_t codes_at = row + (uint32_t)r * 64u, values_at = row + (uint32_t)r * 128u, cx = (uint32_t)(r >> 1) & 3u, vx = (uint32_t)r & 7u;
+                uint32_t at = 0, sb2 = 0, ph2 = 0, now = steps_of(0), next = steps_of(1), after = steps_of(2);
+                bool fine = true;
+                auto restore = [&](auto half_tag) {
+                    constexpr bool H = decltype(half_tag)::value;
+                    for (int kb = 0; kb < num_kb; ++kb) {
+                        const uint32_t st = now;
+                        now = next; next = after; after = steps_of(kb + 3);
+                        fine = __all_sync(0xffffffffu, mbar_wait_bounded(raw0 + sb2, ph2, abort_flag));
+                        uint32_t w[16];
+#pragma unroll
+                        for (uint32_t q = 0; q < 4; ++q)
+                            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(w[4 * q]), "=r"(w[4 * q + 1]), "=r"(w[4 * q + 2]), "=r"(w[4 * q + 3])
+                                         : "r"(codes_at + at + ((q ^ cx) << 4)) : "memory");
+                        // (both warps of the slice have its codes; after a give-up they leave together)
+                        fine = named_bar_all(1 + slice, 64, fine);
+                        if (!fine) return;
+                        const float step0 = pack_step(st & 255u), step1 = pack_step(st >> 8);
+                        const f32x2 group0 = pair(step0, step0), group1 = pair(step1, step1);
+#pragma unroll
+                        for (uint32_t q = 0; q < 8; ++q) {
+                            const f32x2 by = q < 4 ? group0 : group1;
+                            uint32_t o[4];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                f32x2 f[2];
+                                restore4(w[2 * q + h], by, f);
+                                o[2 * h] = narrow_t<H>(f[0]);
+                                o[2 * h + 1] = narrow_t<H>(f[1]);
+                            }
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(values_at + at + ((q ^ vx) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+                                         : "memory");
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(full0 + sb2);
+                        sb2 += 8; at += kStageBytes;
+                        if (sb2 == sb_end) { sb2 = 0; at = 0; ph2 ^= 1u; }
+                    }
+                };
+                if (g.f16) restore(std::true_type{}); else restore(std::false_type{});
+                if (!fine && lane == 0) { atomicOr(err, ERRW_TIMEOUT); ctl->abort_flag = 1; }
+            }
         }
         const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->tmem_full, 0, abort_flag));
         if (!ok && lane == 0) { atomicOr(err, ERRW_TIMEOUT); ctl->abort_flag = 1; }
@@ -385,7 +460,7 @@ UmmaWgradPlan umma_wgrad_plan_bounded(const Problem &pb) {
 
 int wgrad_kmajor_rows(const Problem &pb) { return (pb.kdim + 1) / 2; }
 
-template <int BN, bool X_SUMS = false>
+template <int BN, bool X_SUMS = false, bool PACKED = false>
 static cudaError_t launch_w(const CUtensorMap &tx, const CUtensorMap &tdz, WgradGemm g, const UmmaWgradPlan &pl,
                             const Problem &pb, float *partials, float *bsum, int *err, cudaStream_t st,
                             unsigned int *counters = nullptr, int ncounters = 0) {
@@ -399,22 +474,25 @@ static cudaError_t launch_w(const CUtensorMap &tx, const CUtensorMap &tdz, Wgrad
     const size_t floor_smem = (size_t)(228 * 1024) / (512 / BN + 1) + 1024;
     if (smem < floor_smem) smem = floor_smem;
     static PerDevice attr_done;
-    if (cudaError_t e = max_dynamic_smem_once(umma_wgrad_kernel<BN, X_SUMS>, 210 * 1024, &attr_done); e != cudaSuccess) return e;
+    if (cudaError_t e = max_dynamic_smem_once(umma_wgrad_kernel<BN, X_SUMS, PACKED>, 210 * 1024, &attr_done); e != cudaSuccess) return e;
     static PerDevice carve;
-    prefer_max_shared_once(umma_wgrad_kernel<BN, X_SUMS>, &carve);
+    prefer_max_shared_once(umma_wgrad_kernel<BN, X_SUMS, PACKED>, &carve);
     dim3 grid((unsigned)((g.kdim / 64 + (g.sums == kSumSlice ? 2 : 1)) / 2), (unsigned)((pb.c_out + BN - 1) / BN),
               (unsigned)pl.splits);
-    return launch_pdl(umma_wgrad_kernel<BN, X_SUMS>, grid, dim3(kWThreads), smem, st, tx, tdz, g, partials, bsum, counters,
+    return launch_pdl(umma_wgrad_kernel<BN, X_SUMS, PACKED>, grid, dim3(kWThreads), smem, st, tx, tdz, g, partials, bsum, counters,
                       ncounters, err);
 }
 
 cudaError_t launch_umma_wgrad(const Problem &pb, const UmmaWgradPlan &pl, const void *dz, const void *x,
-                              float *partials, float *bsum, cudaStream_t st, unsigned int *counters, int ncounters, WgradSums sums) {
+                              float *partials, float *bsum, cudaStream_t st, unsigned int *counters, int ncounters, WgradSums sums,
+                              const PackedTensor *packed_x) {
     WgradGemm g;
     g.ho = pb.h_out; g.wo = pb.w_out; g.c_in = pb.c_in; g.c_out = pb.c_out; g.taps_w = pb.kw;
     g.lower_h = -pb.pad_h; g.lower_w = -pb.pad_w; g.stride_h = pb.stride_h; g.stride_w = pb.stride_w;
     g.dil_h = pb.dil_h; g.dil_w = pb.dil_w; g.kdim = pb.kdim; g.p = pb.p; g.per_split = pl.per_split; g.stages = 1;
     g.blockdiag = pb.groups > 1 ? 1 : 0;
+    g.steps = packed_x ? (const uint8_t *)packed_x->steps : nullptr; g.h_in = pb.h_in; g.w_in = pb.w_in;
+    if (packed_x && (g.blockdiag || sums != WgradSums::kDz)) return cudaErrorInvalidValue;
     g.rows = g.blockdiag ? 0 : 1;
     g.stem = 0; g.stem_tiles_w = g.stem_tiles_h = 1; g.f16 = call_f16();
     g.sums = sums == WgradSums::kX ? kSumX : (sums == WgradSums::kNone ? kSumNone : kSumSlice);
@@ -422,7 +500,9 @@ cudaError_t launch_umma_wgrad(const Problem &pb, const UmmaWgradPlan &pl, const 
     const int upper_h = g.lower_h + (pb.h_out - 1) * pb.stride_h - (pb.h_in - 1);
     const int upper_w = g.lower_w + (pb.w_out - 1) * pb.stride_w - (pb.w_in - 1);
     CUtensorMap tx, tdz;
-    if (!make_tmap_im2col_bf16(&tx, x, pb.n, pb.h_in, pb.w_in, pb.c_in, g.lower_h, g.lower_w, upper_h, upper_w,
+    if (packed_x ? !make_tmap_im2col_codes(&tx, packed_x->codes, pb.n, pb.h_in, pb.w_in, pb.c_in, g.lower_h, g.lower_w, upper_h, upper_w,
+                                           pb.stride_h, pb.stride_w, kWP, 64)
+                 : !make_tmap_im2col_bf16(&tx, x, pb.n, pb.h_in, pb.w_in, pb.c_in, g.lower_h, g.lower_w, upper_h, upper_w,
                                pb.stride_h, pb.stride_w, kWP, 64))
         return cudaErrorInvalidValue;
     const int bn = g.blockdiag ? 64 : wgrad_bn(pb);
@@ -435,6 +515,9 @@ cudaError_t launch_umma_wgrad(const Problem &pb, const UmmaWgradPlan &pl, const 
     int *err = nullptr;
     cudaError_t e = error_word_address(&err);
     if (e != cudaSuccess) return e;
+    if (packed_x)
+        return bn == 64 ? launch_w<64, false, true>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters)
+                        : launch_w<128, false, true>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters);
     if (g.sums == kSumX)
         return bn == 64 ? launch_w<64, true>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters)
                         : launch_w<128, true>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters);
