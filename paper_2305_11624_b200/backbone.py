@@ -7,7 +7,7 @@ last of a bottleneck, the skip connection and its ReLU at the end of each bottle
 ReLU and every add runs through `libconvbn.so`; this module only owns buffers and the order of the calls.
 
 What is kept from forward to backward is what a framework would keep: each convolution's input (the previous
-ReLU's output), the mode's extra state (Tune: three vectors per block; Eval: the pre-normalisation tensor Y of
+ReLU's output; with `packed`, Tune mode, in 8 bits), the mode's extra state (Tune: three vectors per block; Eval: the pre-normalisation tensor Y of
 every block; Deploy: nothing), and nothing else.  Buffers are allocated with torch inside the pass and dropped
 as soon as the backward pass has used them, so `torch.cuda.max_memory_allocated` sees the peak a training
 framework would see.
@@ -24,7 +24,7 @@ import torch
 
 from . import convbn as C
 from . import inputs as I
-from .harness import Block
+from .harness import Block, packed_buffers
 
 
 @dataclass
@@ -52,7 +52,7 @@ def resnet50_plan(size: int = 224) -> Tuple[Optional[Tuple[int, int]], List[Bott
 class _Layer:
     """One ConvBN block of the chain: parameters, gradients, the calls of the chosen mode."""
 
-    def __init__(self, name, n, c_in, hw, c_out, k, stride, mode, device, seed, dtype="bf16"):
+    def __init__(self, name, n, c_in, hw, c_out, k, stride, mode, device, seed, dtype="bf16", packed=False):
         spec = I.LayerSpec(name, n, c_in, hw[0], hw[1], c_out, k, k, stride=stride, pad=k // 2, dtype=dtype)
         self.blk = Block(spec, device=device, modes=(mode,), allocate="params")
         self.blk.randomize_params(seed)
@@ -61,7 +61,7 @@ class _Layer:
             with torch.cuda.device(self.blk.device):
                 self.saved_bytes = max(16, C.convbn_saved_bytes(self.blk.desc, C.MODE_TUNE))
                 self.fwd_bytes = max(256, C.convbn_workspace_bytes(self.blk.desc, C.PHASE_TUNE_FWD))
-                self.bwd_bytes = max(256, C.convbn_workspace_bytes(self.blk.desc, C.PHASE_TUNE_BWD))
+                self.bwd_bytes = max(256, C.convbn_workspace_bytes(self.blk.desc, C.PHASE_TUNE_BWD_PACKED if packed else C.PHASE_TUNE_BWD))
         if mode == "deploy":
             b = self.blk
             b.w_fused = torch.empty_like(b.w)
@@ -96,15 +96,21 @@ class _Layer:
             C.convbn_relu(z, z)
         return z
 
-    def backward(self, dz, held=None, add=None, relu_mask=False, saved=None, scratch=None):
+    def backward(self, dz, held=None, add=None, relu_mask=False, saved=None, scratch=None, packed=None):
         """Gradient with respect to the block's input, plus `add`, and with `relu_mask` zero where the input (the output
         of a ReLU) is not positive; drops what the block kept for it.  With `held` (a list, Tune mode) the
         parameter-gradient pass stays on the library's side stream: what it still reads of the tensors allocated here (dZ, X)
         is parked in `held` until the caller has joined.  saved, scratch (Tune mode): addresses of the forward pass's
-        vectors and of bwd_bytes, both in use until the pass is joined."""
+        vectors and of bwd_bytes, both in use until the pass is joined.  packed: (codes, steps) of the input, in its place."""
         b = self.blk
         dx = torch.empty(self.in_elems, dtype=b.tdtype, device=b.device)
         x, b.x = b.x, None
+        if packed is not None:
+            C.convbn_tune_bwd_packed(b.desc, dz, packed[0], packed[1], b.w, b.b, b.mu_hat, saved, dx, b.dw, b.db, b.dgamma, b.dbeta,
+                                     add, relu_mask, held is not None, scratch, self.bwd_bytes)
+            if held is not None:
+                held.append((packed, dz))
+            return dx
         if self.mode == "tune":
             C.convbn_tune_bwd_glue(b.desc, dz, x, b.w, b.b, b.mu_hat, saved, dx, b.dw, b.db, b.dgamma, b.dbeta, add,
                                    relu_mask, held is not None, scratch, self.bwd_bytes)
@@ -131,8 +137,11 @@ def _aligned(n):
 
 class BackboneReplay:
     def __init__(self, batch: int, plan: List[Bottleneck], mode: str, stem_hw: Optional[Tuple[int, int]] = None,
-                 device="cuda:0", seed: int = 0, async_param_grads: bool = False, dtype: str = "bf16"):
-        assert mode in ("tune", "eval", "deploy") and dtype in ("bf16", "f16")
+                 device="cuda:0", seed: int = 0, async_param_grads: bool = False, dtype: str = "bf16", packed: bool = False):
+        """packed (Tune mode): the inputs of the bottlenecks' convolutions are kept for the backward pass in 8 bits
+        (C.convbn_pack); their ReLUs decide as before, parameter gradients see the restored values."""
+        assert mode in ("tune", "eval", "deploy") and dtype in ("bf16", "f16") and (mode == "tune" or not packed)
+        self.packed = packed
         self.async_param_grads = async_param_grads
         self.mode, self.batch, self.device = mode, batch, torch.device(device)
         self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float16
@@ -147,12 +156,12 @@ class BackboneReplay:
             hw3 = (bt.hw[0] // bt.stride, bt.hw[1] // bt.stride) if bt.stride > 1 else bt.hw
             if bt.stride > 1:      # floor convention of a 3x3 stride-2 pad-1 convolution
                 hw3 = ((bt.hw[0] - 1) // bt.stride + 1, (bt.hw[1] - 1) // bt.stride + 1)
-            c1 = _Layer("b%d.c1" % i, n, bt.c_in, bt.hw, bt.width, 1, 1, mode, device, k, dtype)
-            c2 = _Layer("b%d.c2" % i, n, bt.width, hw2, bt.width, 3, bt.stride, mode, device, k + 1, dtype)
-            c3 = _Layer("b%d.c3" % i, n, bt.width, hw3, bt.c_out, 1, 1, mode, device, k + 2, dtype)
+            c1 = _Layer("b%d.c1" % i, n, bt.c_in, bt.hw, bt.width, 1, 1, mode, device, k, dtype, packed)
+            c2 = _Layer("b%d.c2" % i, n, bt.width, hw2, bt.width, 3, bt.stride, mode, device, k + 1, dtype, packed)
+            c3 = _Layer("b%d.c3" % i, n, bt.width, hw3, bt.c_out, 1, 1, mode, device, k + 2, dtype, packed)
             ds = None
             if bt.stride > 1 or bt.c_in != bt.c_out:
-                ds = _Layer("b%d.ds" % i, n, bt.c_in, bt.hw, bt.c_out, 1, bt.stride, mode, device, k + 3, dtype)
+                ds = _Layer("b%d.ds" % i, n, bt.c_in, bt.hw, bt.c_out, 1, bt.stride, mode, device, k + 3, dtype, packed)
             k += 4
             self.blocks.append((c1, c2, c3, ds))
         self.first = plan[0]
@@ -177,6 +186,11 @@ class BackboneReplay:
                         at += _aligned(l.bwd_bytes)
                 self.bwd_at.append(off)
                 self.bwd_total.append(at or max(l.bwd_bytes for l in blk if l is not None))
+
+    def _pack(self, x):
+        codes, steps = packed_buffers(x)
+        C.convbn_pack(x, codes, steps)
+        return codes, steps
 
     # ---- one iteration ---------------------------------------------------------------------------------
     def make_inputs(self, seed: int = 1):
@@ -210,9 +224,19 @@ class BackboneReplay:
         for c1, c2, c3, ds in self.blocks:
             a = c1.forward(x, None, True, *fwd.get(c1, none))
             b = c2.forward(a, None, True, *fwd.get(c2, none))
+            if self.packed:               # a tensor goes as soon as its last reader of the forward pass is queued
+                c2.blk.x, pa = None, self._pack(a)
+                if keep is None:
+                    del a
             # out = relu(c3(b) + identity)
             c = c3.forward(b, ds.forward(x, None, False, *fwd.get(ds, none)) if ds is not None else x, True, *fwd.get(c3, none))
-            relu_outs.append((x, a, b, c))
+            if self.packed:
+                for layer in (c1, c3, ds):
+                    if layer is not None:
+                        layer.blk.x = None
+                relu_outs.append((self._pack(x), pa, self._pack(b)))
+            else:
+                relu_outs.append((x, a, b, c))
             if keep is not None:
                 keep.setdefault("relu_outputs", []).append((a.clone(), b.clone(), c.clone()))
             x = c
@@ -221,26 +245,29 @@ class BackboneReplay:
         scratch = None
         g = torch.empty_like(ins["g"])
         C.convbn_relu_bwd(ins["g"], x, g)                      # through the last block's ReLU
-        del x, a, b, c
+        x = a = b = c = pa = None
         # Tune mode: the parameter gradients of a bottleneck's blocks run beside its input-gradient chain and are
         # joined once per bottleneck, after which what they were reading can be released
         held = [] if self.mode == "tune" and self.async_param_grads else None
         for i in range(len(self.blocks) - 1, -1, -1):
             c1, c2, c3, ds = self.blocks[i]
-            relu_outs.pop()
+            kept_inputs = relu_outs.pop()
+            px, pa, pb = kept_inputs if self.packed else (None, None, None)
+            del kept_inputs
             at = none * 2
             if tune:
                 scratch = raw(self.bwd_total[i])
                 base = scratch.data_ptr()
                 at = [base + o for o in self.bwd_at[i]]
             kept = lambda l: fwd.get(l, none)[0]
-            gb = c3.backward(g, held, None, True, kept(c3), at[2])
-            ga = c2.backward(gb, held, None, True, kept(c2), at[1])
+            gb = c3.backward(g, held, None, True, kept(c3), at[2], pb)
+            ga = c2.backward(gb, held, None, True, kept(c2), at[1], pa)
             del gb
-            gs = ds.backward(g, held, None, False, kept(ds), at[3]) if ds is not None else g
+            gs = ds.backward(g, held, None, False, kept(ds), at[3], px) if ds is not None else g
             # the two branches meet; the input of every block but the first is the ReLU output of the block below
-            g = c1.backward(ga, held, gs, i > 0, kept(c1), at[0])
+            g = c1.backward(ga, held, gs, i > 0, kept(c1), at[0], px)
             del ga, gs
+            px = pa = pb = None
             if held is not None:
                 C.convbn_tune_bwd_join()
                 held.clear()

@@ -18,6 +18,12 @@ def make_desc(spec: I.LayerSpec) -> C.Desc:
                        **spec.dims())
 
 
+def packed_buffers(x: torch.Tensor):
+    """(codes, steps) of a tensor of x's size, for C.convbn_pack."""
+    return (torch.empty(x.numel(), dtype=torch.int8, device=x.device),
+            torch.empty(-(-x.numel() // 32), dtype=torch.uint8, device=x.device))
+
+
 class Block:
     """Buffers of one layer on one device plus the calls of each mode."""
 
@@ -61,6 +67,13 @@ class Block:
             self.b_fused = f()
             self.dw_fused = e(self.w_shape, torch.float32)
             self.db_fused = f()
+        if "packed" in modes:            # (beside "tune": X in 8 bits from forward to backward)
+            phases.append(C.PHASE_TUNE_BWD_PACKED)
+            self.x_codes, self.x_steps = packed_buffers(self.x)
+        if "quant" in modes:             # Deploy mode in 8-bit integers
+            phases.append(C.PHASE_DEPLOY_FWD_QUANT)
+            self.w_codes = torch.empty(spec.c_out * (-(-cg // 16) * 16), dtype=torch.int8, device=self.device)
+            self.w_scale, self.b_fused = f(), f()
         ws = max([C.convbn_workspace_bytes(self.desc, p) for p in phases] + [256])
         self.workspace = torch.empty(ws, dtype=torch.uint8, device=self.device)
 
@@ -148,6 +161,15 @@ class Block:
         C.convbn_tune_bwd_begin(self.desc, self.dz, self.x, self.w, self.b, self.mu_hat, self.saved, self.dx, self.dw,
                                 self.db, self.dgamma, self.dbeta, self.workspace, stream=stream)
 
+    def pack_x(self, stream=None):
+        """What the backward pass needs of X, in 8 bits: X itself may go."""
+        C.convbn_pack(self.x, self.x_codes, self.x_steps, stream=stream)
+
+    def tune_bwd_packed(self, stream=None, add=None, relu_mask=False, defer_join=False):
+        C.convbn_tune_bwd_packed(self.desc, self.dz, self.x_codes, self.x_steps, self.w, self.b, self.mu_hat, self.saved, self.dx,
+                                 self.dw, self.db, self.dgamma, self.dbeta, add, relu_mask, defer_join, self.workspace,
+                                 stream=stream)
+
     def tune_step(self, stream=None, defer_join=False):
         self.tune_fwd(stream)
         if defer_join:
@@ -178,14 +200,23 @@ class Block:
         C.convbn_deploy_bwd(self.desc, self.dz, self.x, self.w_fused, self.dx, self.dw_fused,
                             self.db_fused, self.workspace, stream=stream)
 
+    def deploy_prepare_quant(self, stream=None):
+        C.convbn_deploy_prepare_quant(self.desc, self.w, self.b, self.gamma, self.beta, self.mu_hat, self.var_hat, self.w_codes,
+                                      self.w_scale, self.b_fused, stream=stream)
+
+    def deploy_fwd_quant(self, stream=None, add=None, relu=False):
+        C.convbn_deploy_fwd_quant(self.desc, self.x, self.w_codes, self.w_scale, self.b_fused, self.z, add, relu, self.workspace,
+                                  stream=stream)
+
     # ---- accounting ------------------------------------------------------------------------
     def flops_per_phase(self) -> float:
         sp = self.spec
         return 2.0 * sp.n * self.h_out * self.w_out * sp.c_out * (sp.c_in // sp.groups) * sp.kh * sp.kw
 
     def saved_bytes(self, mode: str) -> int:
-        """Bytes kept from forward to backward beside nothing else: X plus the mode's extra."""
+        """Bytes kept from forward to backward beside nothing else: X (mode "packed": its codes and steps) plus the mode's extra."""
         es = 2 if self.spec.dtype in ("bf16", "f16") else 4
-        xb = int(np.prod(self.x_shape)) * es
-        m = {"tune": C.MODE_TUNE, "eval": C.MODE_EVAL, "deploy": C.MODE_DEPLOY}[mode]
+        elements = int(np.prod(self.x_shape))
+        xb = elements + -(-elements // 32) if mode == "packed" else elements * es
+        m = {"tune": C.MODE_TUNE, "packed": C.MODE_TUNE, "eval": C.MODE_EVAL, "deploy": C.MODE_DEPLOY}[mode]
         return xb + C.convbn_saved_bytes(self.desc, m)

@@ -271,3 +271,87 @@ def test_packed_backward_in_half_with_bias_deferred(spec):
     add = ROUND["f16"](np.random.default_rng(1).standard_normal(t["x"].shape).astype(np.float32))
     got = _packed_pass(spec, t, add, True, begin=True)
     _compare(spec, t, got, _reference(spec, t, add, True), add, True)
+
+
+# ---- together, as a training iteration uses them -----------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("deferred", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_a_backbone_that_keeps_its_inputs_packed(dtype, deferred):
+    """The forward pass is the same, bit for bit; input gradients do not depend on what is kept (a ReLU's decision is the sign of
+    the code), within the rounding of the layers' other kernels; the parameter gradients of the last block are those of the
+    restored input."""
+    import torch
+    from oracle import oracle as O
+    from paper_2305_11624_b200.backbone import BackboneReplay, Bottleneck
+    plan = [Bottleneck(64, 64, 256, 1, (12, 12)), Bottleneck(256, 64, 256, 1, (12, 12)), Bottleneck(256, 128, 512, 2, (12, 12))]
+    runs = []
+    for packed in (False, True):
+        rp = BackboneReplay(4, plan, "tune", seed=3, dtype=dtype, async_param_grads=deferred, packed=packed)
+        ins = rp.make_inputs(5)
+        keep = {}
+        rp.forward_backward(ins, keep)
+        torch.cuda.synchronize()
+        C.convbn_check()
+        runs.append((rp, ins, keep))
+    (_, _, plain), (rp, ins, keep) = runs
+    assert torch.equal(plain["out"], keep["out"])
+    f = lambda t: t.float().cpu().numpy().astype(np.float64)
+    assert O.rel_l2(f(keep["dx"]), f(plain["dx"])) <= parity.TOL[dtype] * 3
+    # the last 1x1 convolution: dZ = g where the output is above zero, X = the restored ReLU output in front of it
+    c3 = rp.blocks[-1][2].blk
+    spec = c3.spec
+    shape = (4, 512, 6, 6)
+    dz = I.act_from_layout(f(ins["g"]) * (f(keep["out"]) > 0), "nhwc", shape)
+    q, s = P.pack(f(keep["relu_outputs"][-1][1]).ravel(), dtype)
+    x = I.act_from_layout(P.unpack(q, s), "nhwc", (4, 128, 6, 6))
+    t = {k: c3.fetch(k) for k in ("w", "gamma", "beta", "mu_hat", "var_hat")}
+    ref = parity.oracle_tune(spec, dict(t, x=x, dz=dz, b=None))
+    got = {k: c3.fetch(k) for k in ("dw", "dgamma", "dbeta")}
+    parity.compare(got, ref, parity.TOL["f32"], ("dw", "dgamma", "dbeta"), "c3", dtype="f32")
+
+
+@pytest.mark.gpu
+def test_a_packed_backbone_needs_less_memory():
+    """Of what an iteration holds, the kept inputs shrink from 2 bytes an element to 33 / 32, gradients and scratch do not: over
+    six identical bottlenecks of 256 channels at 56 x 56 the inputs (384 elements a pixel and bottleneck) are most of it."""
+    from paper_2305_11624_b200.backbone import BackboneReplay, Bottleneck
+    plan = [Bottleneck(256, 64, 256, 1, (56, 56))] * 6
+    peaks = [BackboneReplay(8, plan, "tune", seed=1, packed=packed).measure(iters=1, warmup=1)[1] for packed in (False, True)]
+    assert peaks[1] < 0.75 * peaks[0], peaks
+
+
+@pytest.mark.gpu
+def test_packed_calls_are_captured_and_replayed_on_other_inputs():
+    import torch
+    from paper_2305_11624_b200.harness import Block
+    spec = I.LayerSpec("captured", 3, 256, 14, 13, 64, 1, 1)
+    blk = Block(spec, modes=("tune", "packed"))
+    for seed in (1, 2):
+        t = _relu_inputs(spec, seed)
+        if seed == 1:
+            blk.load(t)
+            blk.tune_fwd(); blk.pack_x(); blk.tune_bwd_packed(relu_mask=True, defer_join=True); C.convbn_tune_bwd_join()
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                blk.tune_fwd()
+                blk.pack_x()
+                blk.tune_bwd_packed(relu_mask=True, defer_join=True)
+                C.convbn_tune_bwd_join()
+        blk.load(t)
+        graph.replay()
+        C.convbn_check()
+        got = dict({n: blk.fetch(n) for n in ("dx", "dw", "dgamma", "dbeta")}, db=None)
+        _compare(spec, t, got, _reference(spec, t, None, True), None, True)
+
+
+@pytest.mark.gpu
+def test_a_group_that_is_no_number_shows_in_the_gradients():
+    """An infinity in X: its group is restored as NaN, so every gradient of its channels' weights is, and dX is masked there."""
+    spec = I.LayerSpec("inf", 1, 256, 6, 5, 64, 1, 1)
+    t = parity.make_inputs(spec, 4)
+    t["x"][0, 40, 2, 3] = np.inf
+    got = _packed_pass(spec, t, None, True)
+    assert np.isnan(got["dw"][:, 32:64]).all() and np.isfinite(np.delete(got["dw"], np.s_[32:64], 1)).all()
+    assert not got["dx"][0, 32:64, 2, 3].any() and np.isfinite(got["dx"]).all() and np.isfinite(got["dbeta"]).all()
