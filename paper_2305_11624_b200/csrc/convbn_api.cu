@@ -1247,6 +1247,7 @@ int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *
         const PackedTensor px{codes, steps};
         PostOp post;
         post.add = add;
+        post.add_once = 1;
         post.mask_codes = relu_mask ? codes : nullptr;
         CK(tune_bwd_impl(desc, dz, nullptr, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta, at(workspace, pl.inner),
                          pl.total - pl.inner, stream, begin != 0, post, &px));
@@ -1257,6 +1258,7 @@ int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *
     LAUNCH("unpack", launch_unpack(storage_type(desc), codes, steps, x, pb.pin * pb.c_in, st));
     PostOp post;
     post.add = add;
+    post.add_once = 1;
     post.mask = relu_mask ? x : nullptr;
     CK(tune_bwd_impl(desc, dz, x, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta, at(workspace, pl.inner), pl.total - pl.inner,
                      stream, begin != 0, post));

@@ -36,6 +36,7 @@ cudaError_t launch_direct_wgrad(const Problem &pb, int dtype, int layout, const 
 struct PostOp {
     const void *add = nullptr, *mask = nullptr;
     int relu = 0;
+    int add_once = 0;                      // the sum with `add` may be rounded once
     const void *mask_codes = nullptr;      // the mask as a packed tensor's codes (dense outputs of umma_conv.cu only)
     bool any() const { return add || mask || relu || mask_codes; }
 };

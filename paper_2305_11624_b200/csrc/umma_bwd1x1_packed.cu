@@ -311,7 +311,9 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
                                     const uint32_t *p2 = &v[h][(q + (e >> 1)) * 4 + (e & 1) * 2];
-                                    r[e] = post_pair<H>(pack2_t<H>(__uint_as_float(p2[0]), __uint_as_float(p2[1])), ADD, a[e], false, MASK, m[e]);
+                                    f32x2 f = pair(__uint_as_float(p2[0]), __uint_as_float(p2[1]));
+                                    if constexpr (ADD) f = fma2(f, pair(1.f, 1.f), widen_t<H>(a[e]));
+                                    r[e] = post_pair<H>(narrow_t<H>(f), false, 0u, false, MASK, m[e]);
                                 }
                                 stmatrix_x4(out + at16, r[0], r[1], r[2], r[3]);
                             }

@@ -62,6 +62,7 @@ struct ConvGemm {
     const __nv_bfloat16 *post_add, *post_mask;      // at the output's offsets
     int post_relu;
     int mask_codes;                                 // kPost: the mask's box is of 8-bit codes (post_mask is not NULL)
+    int add_once;                                   // kPost: the sum with post_add (not NULL, no ReLU) is rounded once
 };
 
 struct ConvSmemCtl {
@@ -556,7 +557,9 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
                     }
                     // (what follows the rounding is fixed outside the loop over the columns: one uniform branch per chunk)
                     auto pack_rows = [&](auto half_tag, auto add_tag, auto relu_tag, auto mask_tag) {
-                        constexpr bool H = decltype(half_tag)::value, ADD = decltype(add_tag)::value;
+                        // ADD 1: the result is rounded and their sum again, 2: the sum alone
+                        constexpr int ADD = decltype(add_tag)::value;
+                        constexpr bool H = decltype(half_tag)::value;
                         constexpr bool RELU = decltype(relu_tag)::value, MASK = decltype(mask_tag)::value;
 #pragma unroll
                         for (int i = 0; i < 8; i += 2) {
@@ -564,21 +567,24 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 uint32_t o[4];                 // columns 8 i and 8 i + 8: rows 0-7, 8-15 of each
+                                uint32_t a[4] = {0u, 0u, 0u, 0u}, m[4] = {0u, 0u, 0u, 0u};
+                                const uint32_t at16 = (uint32_t)h * 2048u + (((uint32_t)i << 4) ^ frag_chunk);
+                                if constexpr (POST && ADD == 2) ldmatrix_x4(a[0], a[1], a[2], a[3], smem_u32(add_buf) + frag_row + at16);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
                                     const uint32_t *q = &v[h][(i + (e >> 1)) * 4 + (e & 1) * 2];
                                     const f32x2 f = pair(__uint_as_float(q[0]), __uint_as_float(q[1]));
                                     const f32x2 shift = sh[(i & 3) + (e >> 1)];
-                                    o[e] = narrow_t<H>(DUAL ? fma2(f, one, shift) : mul_add2(f, sc[(i & 3) + (e >> 1)], shift, one));
+                                    f32x2 r = DUAL ? fma2(f, one, shift) : mul_add2(f, sc[(i & 3) + (e >> 1)], shift, one);
+                                    if constexpr (POST && ADD == 2) r = fma2(r, one, widen_t<H>(a[e]));
+                                    o[e] = narrow_t<H>(r);
                                     if constexpr (MODE == kRelu) o[e] = post_pair<H>(o[e], false, 0u, true, false, 0u);
                                 }
-                                const uint32_t at16 = (uint32_t)h * 2048u + (((uint32_t)i << 4) ^ frag_chunk);
                                 if constexpr (POST) {
-                                    uint32_t a[4] = {0u, 0u, 0u, 0u}, m[4] = {0u, 0u, 0u, 0u};
-                                    if constexpr (ADD) ldmatrix_x4(a[0], a[1], a[2], a[3], smem_u32(add_buf) + frag_row + at16);
+                                    if constexpr (ADD == 1) ldmatrix_x4(a[0], a[1], a[2], a[3], smem_u32(add_buf) + frag_row + at16);
                                     if constexpr (MASK) ldmatrix_x4(m[0], m[1], m[2], m[3], smem_u32(mask_buf) + frag_row + at16);
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) o[e] = post_pair<H>(o[e], ADD, a[e], RELU, MASK, m[e]);
+                                    for (int e = 0; e < 4; ++e) o[e] = post_pair<H>(o[e], ADD == 1, a[e], RELU, MASK, m[e]);
                                 }
                                 stmatrix_x4(frag + at16, o[0], o[1], o[2], o[3]);
                                 if constexpr (DUAL) {          // kept for the second output, in the accumulator's registers
@@ -594,7 +600,9 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
                     };
                     constexpr std::true_type yes{};
                     constexpr std::false_type no{};
+                    constexpr std::integral_constant<int, 2> once{};
                     if constexpr (!POST) pack(no, no, no);
+                    else if (g.add_once) { if (g.post_mask) pack(once, no, yes); else pack(once, no, no); }
                     else if (g.post_mask) { if (g.post_add) pack(yes, no, yes); else pack(no, no, yes); }
                     else if (g.post_relu) pack(yes, yes, no);
                     else pack(yes, no, no);
@@ -950,6 +958,7 @@ cudaError_t launch_umma_conv(const UmmaConvShape &s, const void *act, const void
     g.post_add = with_post ? (const __nv_bfloat16 *)post->add : nullptr;
     g.post_mask = with_post ? (const __nv_bfloat16 *)(post->mask_codes ? post->mask_codes : post->mask) : nullptr;
     g.mask_codes = with_post && post->mask_codes;
+    g.add_once = with_post && post->add && post->add_once && !post->relu && !s.out_sw;
     if (g.mask_codes && (s.out_sw || s.cn % 64)) return cudaErrorInvalidValue;
     g.post_relu = with_post ? post->relu : 0;
     g.tap_c = s.tap_c; g.tap_kw = s.tap_kw; g.tap_sh = s.tap_sh; g.tap_sw = s.tap_sw;
@@ -1000,7 +1009,7 @@ cudaError_t launch_stem_fwd(const Problem &pb, const void *x_packed, const void 
     const int krows = stem_krows(pb);
     ConvGemm g;
     g.chunk_outer = 0;
-    g.tap_c = 0; g.post_add = g.post_mask = nullptr; g.post_relu = 0; g.mask_codes = 0;
+    g.tap_c = 0; g.post_add = g.post_mask = nullptr; g.post_relu = 0; g.mask_codes = g.add_once = 0;
     g.ho = pb.h_out; g.wo = pb.w_out; g.cn = pb.c_out; g.ca = 64; g.taps_h = krows; g.taps_w = 1;
     g.lower_h = g.lower_w = 0; g.stride_h = g.stride_w = g.dil_h = g.dil_w = 1;
     g.stem = 1; g.stem_tw = 16; g.stem_th = 8;
