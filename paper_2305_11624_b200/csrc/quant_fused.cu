@@ -23,31 +23,34 @@ constexpr int kQRowWarp = 18;                    // brings the rows
 constexpr int kQMaxStages = 8;
 constexpr uint32_t kQStage = 32 * 128;           // an epilogue warp's box: [32 rows][128 bytes]
 constexpr int kQSlots = 4;                       // row scales of so many units
-constexpr int kQMaxDepth = 8;                    // slots of the ring of rows
+constexpr int kQMaxDepth = 8;                    // slots of a ring of rows
 
 struct QuantFused {
     RowMap rows;
     uint32_t p;
     int k, kb, n, bn;                            // C_in, its blocks of 128, C_out, channels of a tile
     uint32_t units, n_tiles;
-    int abufs, stages, nbuf, resident;           // A buffers, slots of streamed weights, boxes of an epilogue warp
-    int depth;                                   // slots of the ring of rows
+    int stages, nbuf, resident;                  // slots of streamed weights, boxes of an epilogue warp
+    int rings, depth;                            // rings of rows (one per converting group), their slots
     int dense, relu;                             // rows of Z start on 16-byte boundaries
 };
 
 struct QuantCtl {
-    uint64_t rows_full[kQMaxDepth], rows_empty[kQMaxDepth], full[kQMaxStages], empty[kQMaxStages], wfull, a_full[2], a_empty[2], xs_full[kQSlots], acc_full[2], acc_empty[2], add_full[8];
+    uint64_t rows_full[2][kQMaxDepth], rows_empty[2][kQMaxDepth], full[kQMaxStages], empty[kQMaxStages], wfull, a_full[2], a_empty[2], xs_full[kQSlots], acc_full[2], acc_empty[2], add_full[8];
     uint32_t tmem_base;
     int abort_flag;
 };
 
-// A converting warp's rows of a unit: RPI of them an instruction (a set), BATCH sets at a time, at most 4 KB.  Half a batch of all
-// eight warps, side by side, is a slot of the ring.
+// The eight converting warps work on a unit together, or, rows of up to 64 elements, in two groups that take the units in turn (GROUPS).
+// A warp has ROWS of its group's units, RPI of them an instruction (a set), BATCH sets at a time, at most 4 KB.  Half a batch of a group's
+// warps, side by side, is a slot of the group's ring.
 template <class T, int LPR> struct RowSets {
-    static constexpr int RPI = 32 / LPR, SETS = 16 / RPI, SET_BYTES = 256 * (int)sizeof(T);
-    static constexpr int BATCH = SETS * SET_BYTES <= 4096 ? SETS : 4096 / SET_BYTES, BATCHES = SETS / BATCH;
+    static constexpr int GROUPS = LPR == 8 ? 2 : 1, WARPS = 8 / GROUPS, ROWS = kQRows / WARPS;
+    static constexpr int RPI = 32 / LPR, SETS = ROWS / RPI, SET_BYTES = 256 * (int)sizeof(T);
+    static constexpr int BATCH = SETS * SET_BYTES <= 4096 ? SETS : 4096 / SET_BYTES, BATCHES = SETS / BATCH, HALF = BATCH / 2;
+    static constexpr int SLOT_ROWS = WARPS * HALF * RPI;
+    static constexpr uint32_t SLOT_BYTES = (uint32_t)(WARPS * HALF * SET_BYTES);
 };
-template <class T, int LPR> constexpr uint32_t kSlotBytes = (uint32_t)(8 * RowSets<T, LPR>::BATCH * RowSets<T, LPR>::SET_BYTES / 2);
 
 // LPR lanes read a row, eight elements each.
 template <class T, int LPR>
@@ -59,10 +62,10 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
     extern __shared__ uint8_t smem_raw[];
     uint8_t *a_tiles = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t a_bytes = (uint32_t)g.kb * kQBlock, w_bytes = (uint32_t)g.bn * 128;
-    uint8_t *w_tiles = a_tiles + (size_t)g.abufs * a_bytes;
+    uint8_t *w_tiles = a_tiles + 2 * (size_t)a_bytes;
     uint8_t *staging = w_tiles + (size_t)(g.resident ? g.n_tiles * g.kb : g.stages) * w_bytes;
     uint8_t *ring = staging + (size_t)8 * g.nbuf * kQStage;
-    float *scale_s = (float *)(ring + (size_t)g.depth * kSlotBytes<T, LPR>), *shift_s = scale_s + g.n_tiles * g.bn;
+    float *scale_s = (float *)(ring + RowSets<T, LPR>::GROUPS * (size_t)g.depth * RowSets<T, LPR>::SLOT_BYTES), *shift_s = scale_s + g.n_tiles * g.bn;
     float *xs_s = shift_s + g.n_tiles * g.bn;                                   // [kQSlots][128]
     QuantCtl *ctl = (QuantCtl *)(xs_s + kQSlots * kQRows);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -73,15 +76,14 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         for (int s = 0; s < kQMaxStages; ++s) { mbar_init(&ctl->full[s], 1); mbar_init(&ctl->empty[s], 1); }
         mbar_init(&ctl->wfull, 1);
         for (int s = 0; s < 2; ++s) {
-            mbar_init(&ctl->a_full[s], 8); mbar_init(&ctl->a_empty[s], 1);
+            mbar_init(&ctl->a_full[s], RowSets<T, LPR>::WARPS); mbar_init(&ctl->a_empty[s], 1);
             mbar_init(&ctl->acc_full[s], 1); mbar_init(&ctl->acc_empty[s], 4);
         }
-        for (int s = 0; s < kQSlots; ++s) mbar_init(&ctl->xs_full[s], 8);
+        for (int s = 0; s < kQSlots; ++s) mbar_init(&ctl->xs_full[s], RowSets<T, LPR>::WARPS);
         for (int s = 0; s < 8; ++s) {
             mbar_init(&ctl->add_full[s], 1);
-            mbar_init(&ctl->rows_full[s], 1);
-            mbar_init(&ctl->rows_empty[s], 8);
         }
+        for (int s = 0; s < 2 * kQMaxDepth; ++s) { mbar_init(&ctl->rows_full[0][0] + s, 1); mbar_init(&ctl->rows_empty[0][0] + s, RowSets<T, LPR>::WARPS); }
         ctl->abort_flag = 0;
         fence_barrier_init();
     }
@@ -135,7 +137,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             bool ok = !g.resident || mbar_wait_bounded(&ctl->wfull, 0, abort_flag);
             uint32_t i = 0, s = 0, it = 0;
             for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
-                const uint32_t ab = g.abufs == 2 ? (i & 1u) : 0u, use = g.abufs == 2 ? (i >> 1) : i;
+                const uint32_t ab = i & 1u, use = i >> 1;
                 ok = mbar_wait_bounded(&ctl->a_full[ab], use & 1u, abort_flag);
                 for (uint32_t nt = 0; ok && nt < g.n_tiles; ++nt, ++s) {
                     const uint32_t acc = s & 1u, d = tmem_base + acc * (uint32_t)g.bn;
@@ -157,58 +159,62 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     }
                     if (ok) umma_commit(&ctl->acc_full[acc]);
                 }
-                if (ok && u + g.abufs * gridDim.x < g.units) umma_commit(&ctl->a_empty[ab]);
+                if (ok && u + 2 * gridDim.x < g.units) umma_commit(&ctl->a_empty[ab]);
             }
             if (!ok) give_up();
         }
     } else if (warp == kQRowWarp) {
-        // ---- rows of X into the ring, a slot at a time: side by side one copy, otherwise one a row ----
+        // ---- rows of X, a slot at a time, into the ring of the group that converts the unit: side by side one copy, otherwise one a row ----
         using R = RowSets<T, LPR>;
-        constexpr uint32_t ROWS = 8 * (R::BATCH / 2) * R::RPI;
+        constexpr uint32_t ROWS = R::SLOT_ROWS;
         const uint32_t row_bytes = (uint32_t)g.k * sizeof(T);
-        uint32_t slot = 0, ph = 1, asked = 0;
+        uint32_t asked[2] = {0, 0}, i = 0;
         bool ok = true;
-        for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x) {
-            const uint32_t end = min((u + 1) * kQRows, g.p);
+        for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
+            const uint32_t end = min((u + 1) * kQRows, g.p), qg = R::GROUPS == 2 ? i & 1u : 0u;
             for (uint32_t first = u * kQRows; first < end; first += ROWS) {
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_empty[slot], ph, abort_flag));
+                const uint32_t n = qg ? asked[1] : asked[0], turn = n / (uint32_t)g.depth, slot = n - turn * (uint32_t)g.depth;
+                uint64_t *full = &ctl->rows_full[qg][slot];
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_empty[qg][slot], (turn & 1u) ^ 1u, abort_flag));
                 if (!ok) break;
                 const uint32_t rows = min(ROWS, end - first);
-                uint8_t *to = ring + (size_t)slot * kSlotBytes<T, LPR>;
+                uint8_t *to = ring + ((size_t)qg * g.depth + slot) * RowSets<T, LPR>::SLOT_BYTES;
                 if (lane == 0) {
-                    mbar_arrive_expect_tx(&ctl->rows_full[slot], rows * row_bytes);
-                    if (!g.rows.strided) bulk_load(to, x + (size_t)first * g.k, rows * row_bytes, &ctl->rows_full[slot]);
+                    mbar_arrive_expect_tx(full, rows * row_bytes);
+                    if (!g.rows.strided) bulk_load(to, x + (size_t)first * g.k, rows * row_bytes, full);
                 }
                 if (g.rows.strided) {
                     __syncwarp();
-                    for (uint32_t r = lane; r < rows; r += 32) bulk_load(to + (size_t)r * row_bytes, x + g.rows.at(first + r), row_bytes, &ctl->rows_full[slot]);
+                    for (uint32_t r = lane; r < rows; r += 32) bulk_load(to + (size_t)r * row_bytes, x + g.rows.at(first + r), row_bytes, full);
                 }
-                ++asked;
-                if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
+                if (qg) ++asked[1]; else ++asked[0];
             }
         }
         if (!ok && lane == 0) {
             give_up();
-            for (uint32_t j = asked > (uint32_t)g.depth ? asked - g.depth : 0; j < asked; ++j)        // let the copies in flight land
-                mbar_wait_bounded(&ctl->rows_full[j % g.depth], (j / g.depth) & 1u, nullptr, 200000000ull);
+            for (int qg = 0; qg < 2; ++qg)
+                for (uint32_t j = asked[qg] > (uint32_t)g.depth ? asked[qg] - g.depth : 0; j < asked[qg]; ++j)    // let the copies in flight land
+                    mbar_wait_bounded(&ctl->rows_full[qg][j % g.depth], (j / g.depth) & 1u, nullptr, 200000000ull);
         }
     } else if (warp >= kQLoadWarp) {
-        // ---- rows to codes: warp qw has the rows qw HALF RPI .. of every slot ----
-        // A batch's rows are read twice: for their largest magnitudes, and after these have become scales, which each lane works out
-        // for one row (a scale per four rows, and the rows kept in registers between: 1900 instructions a warp and unit instead of
-        // 700, 256 -> 64 at 56 x 56, N = 256 192 us).
+        // ---- rows to codes ----
+        // What a unit costs beside its elements (waits, scales, the hand-over) is most of it where rows are short: two groups, each with an A
+        // buffer of its own, halve that and run beside each other, 64 -> 64 at 56 x 56, N = 256 62 -> 51 us; longer rows want the ring in
+        // one piece, 256 -> 64 132 us and 157 by groups.  A batch's rows are read twice: for their largest magnitudes, and after these
+        // have become scales, which each lane works out for one row (a scale per four rows, and the rows kept in registers between: 192).
         using R = RowSets<T, LPR>;
-        constexpr int RPI = R::RPI, BATCH = R::BATCH, BATCHES = R::BATCHES, HALF = BATCH / 2;
-        constexpr int SLOT_ROWS = 8 * HALF * RPI;
-        const int qw = warp - kQLoadWarp, sub = lane & (LPR - 1), row_l = lane / LPR, own = qw * HALF * RPI + row_l;     // row in a slot
-        const uint32_t row_bytes = (uint32_t)g.k * sizeof(T), ring0 = smem_u32(ring);
+        constexpr int RPI = R::RPI, BATCH = R::BATCH, BATCHES = R::BATCHES, HALF = R::HALF, SLOT_ROWS = R::SLOT_ROWS;
+        const int qg = R::GROUPS == 2 ? (warp - kQLoadWarp) >> 2 : 0, qw = (warp - kQLoadWarp) & (R::WARPS - 1);
+        const int sub = lane & (LPR - 1), row_l = lane / LPR, own = qw * HALF * RPI + row_l;     // row in a slot
+        const uint32_t row_bytes = (uint32_t)g.k * sizeof(T), ring0 = smem_u32(ring) + (uint32_t)(qg * g.depth) * RowSets<T, LPR>::SLOT_BYTES;
         uint32_t slot = 0, ph = 0;
         // set j of a batch in its unit, as this lane has it
         auto row_of = [&](int batch, int j) { return (2 * batch + j / HALF) * SLOT_ROWS + own + j % HALF * RPI; };
         bool ok = true;
         uint32_t i = 0;
         for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
-            const uint32_t ab = g.abufs == 2 ? (i & 1u) : 0u, use = g.abufs == 2 ? (i >> 1) : i;
+            const uint32_t ab = i & 1u, use = i >> 1;
+            if (R::GROUPS == 2 && (int)ab != qg) continue;    // (the other group's)
             uint8_t *tile = a_tiles + (size_t)ab * a_bytes;
             float *xs = xs_s + (i % kQSlots) * kQRows;
             const uint32_t first = u * kQRows;
@@ -223,10 +229,10 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     there[h] = first + (uint32_t)((2 * batch + h) * SLOT_ROWS) < g.p;       // (a slot past the last row never comes)
-                    base[h] = ring0 + slot * kSlotBytes<T, LPR>;
+                    base[h] = ring0 + slot * RowSets<T, LPR>::SLOT_BYTES;
                     bar[h] = slot;
                     if (!there[h]) continue;
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_full[slot], ph, abort_flag));
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_full[qg][slot], ph, abort_flag));
                     if (!ok) break;
                     if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
 #pragma unroll
@@ -261,7 +267,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                             *(uint2 *)(tile + (size_t)(at >> 7) * kQBlock + r * 128 + ((((at >> 4) ^ r) & 7) << 4) + (at & 8)) = v.codes(inv);
                     }
                     __syncwarp();                             // every lane has read this half
-                    if (lane == 0) mbar_arrive(&ctl->rows_empty[bar[h]]);
+                    if (lane == 0) mbar_arrive(&ctl->rows_empty[qg][bar[h]]);
                 }
             }
             if (!ok) break;
@@ -358,7 +364,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
 // Shared memory of a choice of buffers; 0: they do not fit.
 size_t fused_smem(const QuantFused &g, size_t slot) {
     const size_t w = (size_t)(g.resident ? (int)g.n_tiles * g.kb : g.stages) * g.bn * 128;
-    return 1024 + (size_t)g.abufs * g.kb * kQBlock + w + (size_t)8 * g.nbuf * kQStage + g.depth * slot + 8 * (size_t)g.n_tiles * g.bn +
+    return 1024 + 2 * (size_t)g.kb * kQBlock + w + (size_t)8 * g.nbuf * kQStage + (size_t)g.rings * g.depth * slot + 8 * (size_t)g.n_tiles * g.bn +
            kQSlots * kQRows * 4 + sizeof(QuantCtl) + 16;
 }
 
@@ -393,15 +399,16 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
     g.p = (uint32_t)pb.p; g.k = pb.c_in; g.kb = (pb.c_in + 127) / 128; g.n = pb.c_out; g.relu = relu;
     g.dense = (size_t)pb.c_out * es % 16 == 0;
     g.units = (uint32_t)((pb.p + kQRows - 1) / kQRows);
-    // Buffers, the most wanted first: two of the A operand (rows are converted while others are multiplied) and six slots of
-    // rows (two are in use, the others on their way), then two boxes per epilogue warp; the weights resident, otherwise at least
-    // three slots of them; wide tiles.
-    const size_t room = 227 * 1024, sets = pb.c_in <= 64 ? 4 : (pb.c_in <= 128 ? 8 : 16), set = 256 * es;
-    const size_t slot = 8 * (sets * set <= 4096 ? sets * set : 4096) / 2;                   // (kSlotBytes)
-    const struct { int abufs, nbuf, depth; } wanted[] = {{2, 2, 6}, {2, 1, 6}, {2, 1, 4}, {1, 1, 4}, {1, 1, 2}};
+    // Buffers: two boxes per epilogue warp, the weights resident, otherwise at least three slots of them, wide tiles, and slots of rows,
+    // four for each group if there is room (two are in use, the others on their way).
+    const size_t room = 227 * 1024, set = 256 * es;
+    g.rings = pb.c_in <= 64 ? 2 : 1;                                                         // (RowSets)
+    const size_t warps = 8 / g.rings, sets = kQRows / warps / (pb.c_in <= 64 ? 4 : (pb.c_in <= 128 ? 2 : 1));
+    const size_t slot = warps * (sets * set <= 4096 ? sets * set : 4096) / 2;
+    const struct { int nbuf, depth; } wanted[] = {{2, 4}, {1, 6}, {1, 4}, {1, 3}, {1, 2}};
     size_t smem = 0;
     for (const auto &c : wanted) {
-        g.abufs = c.abufs; g.nbuf = c.nbuf; g.depth = c.depth; g.stages = 3;
+        g.nbuf = c.nbuf; g.depth = c.depth; g.stages = 3;
         for (int widest = 256; widest >= 64 && !smem; widest /= 2) {
             g.n_tiles = (uint32_t)((pb.c_out + widest - 1) / widest);
             g.bn = (int)(((pb.c_out + g.n_tiles - 1) / g.n_tiles + 63) / 64 * 64);
@@ -413,7 +420,7 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
         if (smem) break;
     }
     if (!smem) return cudaErrorInvalidValue;
-    while (g.depth < kQMaxDepth) {
+    while (g.rings == 1 && g.depth < kQMaxDepth) {                                           // the rest for longer rows
         ++g.depth;
         if (fused_smem(g, slot) > room) { --g.depth; break; }
     }
