@@ -42,10 +42,12 @@ struct Eight {
             w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
         }
     }
-    __device__ __forceinline__ void load_shared(uint32_t at) {
+    // from a row of 128 bytes in shared memory, chunk (of 16 bytes) c and the next ones at c ^ swizzle
+    __device__ __forceinline__ void load_swizzled(uint32_t row, uint32_t c, uint32_t swizzle) {
 #pragma unroll
         for (int i = 0; i < kWords; i += 4)
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(at + 4u * i) : "memory");
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(row + (((c + i / 4) ^ swizzle) << 4)) : "memory");
     }
     __device__ __forceinline__ void load_some(const T *p, int count) {      // any alignment, the rest zero
         zero();

@@ -26,7 +26,9 @@ constexpr int kQSlots = 4;                       // row scales of so many units
 constexpr int kQMaxDepth = 8;                    // slots of a ring of rows
 
 struct QuantFused {
-    RowMap rows;
+    int strided, stride_h, stride_w;             // rows of X that are not side by side: im2col boxes
+    FastDiv by_w, by_h;                          // output extent
+    int boxes;                                   // of 128 bytes of a row of X
     uint32_t p;
     int k, kb, n, bn;                            // C_in, its blocks of 128, C_out, channels of a tile
     uint32_t units, n_tiles;
@@ -54,9 +56,10 @@ template <class T, int LPR> struct RowSets {
 
 // LPR lanes read a row, eight elements each.
 template <class T, int LPR>
-__global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_z,
+__global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_constant__ CUtensorMap tm_x,
+                                                                const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_z,
                                                                 const __grid_constant__ CUtensorMap tm_add, const QuantFused g,
-                                                                const T *__restrict__ x, const float *__restrict__ ws,
+                                                                const float *__restrict__ ws,
                                                                 const float *__restrict__ shift, const T *__restrict__ add,
                                                                 T *__restrict__ z, int *err) {
     extern __shared__ uint8_t smem_raw[];
@@ -72,7 +75,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
     volatile int *abort_flag = &ctl->abort_flag;
 
     if (threadIdx.x == 0) {
-        prefetch_tensormap(&tm_w);
+        prefetch_tensormap(&tm_x); prefetch_tensormap(&tm_w);
         for (int s = 0; s < kQMaxStages; ++s) { mbar_init(&ctl->full[s], 1); mbar_init(&ctl->empty[s], 1); }
         mbar_init(&ctl->wfull, 1);
         for (int s = 0; s < 2; ++s) {
@@ -164,33 +167,37 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             if (!ok) give_up();
         }
     } else if (warp == kQRowWarp) {
-        // ---- rows of X, a slot at a time, into the ring of the group that converts the unit: side by side one copy, otherwise one a row ----
+        // ---- rows of X, a slot at a time, into the ring of the group that converts the unit: boxes of [SLOT_ROWS][128 bytes] ----
         using R = RowSets<T, LPR>;
-        constexpr uint32_t ROWS = R::SLOT_ROWS;
-        const uint32_t row_bytes = (uint32_t)g.k * sizeof(T);
+        constexpr int COLS = 128 / sizeof(T);                 // columns of a box
         uint32_t asked[2] = {0, 0}, i = 0;
         bool ok = true;
-        for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
-            const uint32_t end = min((u + 1) * kQRows, g.p), qg = R::GROUPS == 2 ? i & 1u : 0u;
-            for (uint32_t first = u * kQRows; first < end; first += ROWS) {
-                const uint32_t n = qg ? asked[1] : asked[0], turn = n / (uint32_t)g.depth, slot = n - turn * (uint32_t)g.depth;
-                uint64_t *full = &ctl->rows_full[qg][slot];
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_empty[qg][slot], (turn & 1u) ^ 1u, abort_flag));
-                if (!ok) break;
-                const uint32_t rows = min(ROWS, end - first);
-                uint8_t *to = ring + ((size_t)qg * g.depth + slot) * RowSets<T, LPR>::SLOT_BYTES;
-                if (lane == 0) {
-                    mbar_arrive_expect_tx(full, rows * row_bytes);
-                    if (!g.rows.strided) bulk_load(to, x + (size_t)first * g.k, rows * row_bytes, full);
+        if (elect_one()) {
+            for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
+                const uint32_t end = min((u + 1) * kQRows, g.p), qg = R::GROUPS == 2 ? i & 1u : 0u;
+                for (uint32_t first = u * kQRows; first < end; first += R::SLOT_ROWS) {
+                    const uint32_t n = qg ? asked[1] : asked[0], turn = n / (uint32_t)g.depth, slot = n - turn * (uint32_t)g.depth;
+                    uint64_t *full = &ctl->rows_full[qg][slot];
+                    ok = mbar_wait_bounded(&ctl->rows_empty[qg][slot], (turn & 1u) ^ 1u, abort_flag);
+                    if (!ok) break;
+                    uint8_t *to = ring + ((size_t)qg * g.depth + slot) * R::SLOT_BYTES;
+                    mbar_arrive_expect_tx(full, (uint32_t)g.boxes * (R::SLOT_ROWS * 128));
+                    int img = 0, ho = 0, wo = 0;
+                    if (g.strided) {
+                        const uint32_t t = g.by_w.div(first);
+                        img = (int)g.by_h.div(t);
+                        ho = (int)(t - (uint32_t)img * g.by_h.d) * g.stride_h;
+                        wo = (int)(first - t * g.by_w.d) * g.stride_w;
+                    }
+                    for (int c = 0; c < g.boxes; ++c, to += R::SLOT_ROWS * 128) {
+                        if (g.strided) tma_load_im2col_4d(to, &tm_x, full, c * COLS, wo, ho, img, 0, 0);
+                        else tma_load_2d(to, &tm_x, full, c * COLS, (int)first);
+                    }
+                    if (qg) ++asked[1]; else ++asked[0];
                 }
-                if (g.rows.strided) {
-                    __syncwarp();
-                    for (uint32_t r = lane; r < rows; r += 32) bulk_load(to + (size_t)r * row_bytes, x + g.rows.at(first + r), row_bytes, full);
-                }
-                if (qg) ++asked[1]; else ++asked[0];
             }
         }
-        if (!ok && lane == 0) {
+        if (!ok) {                                            // (the thread that asked)
             give_up();
             for (int qg = 0; qg < 2; ++qg)
                 for (uint32_t j = asked[qg] > (uint32_t)g.depth ? asked[qg] - g.depth : 0; j < asked[qg]; ++j)    // let the copies in flight land
@@ -206,7 +213,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         constexpr int RPI = R::RPI, BATCH = R::BATCH, BATCHES = R::BATCHES, HALF = R::HALF, SLOT_ROWS = R::SLOT_ROWS;
         const int qg = R::GROUPS == 2 ? (warp - kQLoadWarp) >> 2 : 0, qw = (warp - kQLoadWarp) & (R::WARPS - 1);
         const int sub = lane & (LPR - 1), row_l = lane / LPR, own = qw * HALF * RPI + row_l;     // row in a slot
-        const uint32_t row_bytes = (uint32_t)g.k * sizeof(T), ring0 = smem_u32(ring) + (uint32_t)(qg * g.depth) * RowSets<T, LPR>::SLOT_BYTES;
+        const uint32_t ring0 = smem_u32(ring) + (uint32_t)(qg * g.depth) * RowSets<T, LPR>::SLOT_BYTES;
         uint32_t slot = 0, ph = 0;
         // set j of a batch in its unit, as this lane has it
         auto row_of = [&](int batch, int j) { return (2 * batch + j / HALF) * SLOT_ROWS + own + j % HALF * RPI; };
@@ -221,8 +228,9 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
 #pragma unroll 1
             for (int batch = 0; batch < BATCHES; ++batch) {
                 auto read = [&](Eight<T> &v, int j, uint32_t base) {       // set j of the batch as this lane has it
-                    if (sub * 8 >= g.k) v.zero();
-                    else v.load_shared(base + (uint32_t)(own + j % HALF * RPI) * row_bytes + (uint32_t)sub * 8u * (uint32_t)sizeof(T));
+                    if (sub * 8 >= g.boxes * (int)(128 / sizeof(T))) { v.zero(); return; }         // (no box there)
+                    const uint32_t r = (uint32_t)(own + j % HALF * RPI), chunk = (uint32_t)sub * (sizeof(T) / 2);     // of 16 bytes
+                    v.load_swizzled(base + (chunk >> 3) * (SLOT_ROWS * 128) + r * 128u, chunk & 7u, r & 7u);
                 };
                 uint32_t mine = 0, base[2], bar[2];
                 bool there[2];
@@ -235,17 +243,25 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_full[qg][slot], ph, abort_flag));
                     if (!ok) break;
                     if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
+                    // (a half batch's rows are loaded before the first is used: row by row a unit of 256 channels took 1634 clocks here
+                    // and 2690 below, of 5800; now LATERD)
+                    Eight<T> v[HALF];
+                    uint32_t t[HALF];
 #pragma unroll
-                    for (int j = h * HALF; j < (h + 1) * HALF; ++j) {
-                        Eight<T> v;
-                        read(v, j, base[h]);
-                        uint32_t t = v.top();
-                        if constexpr (LPR == 32) t = __reduce_max_sync(0xffffffffu, t);
-                        else
+                    for (int j = 0; j < HALF; ++j) read(v[j], j, base[h]);
 #pragma unroll
-                            for (int o = LPR / 2; o > 0; o >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, o));
-                        mine = sub == j ? t : mine;           // lane j of a row's lanes has set j
+                    for (int j = 0; j < HALF; ++j) t[j] = v[j].top();
+                    if constexpr (LPR == 32) {
+#pragma unroll
+                        for (int j = 0; j < HALF; ++j) t[j] = __reduce_max_sync(0xffffffffu, t[j]);
+                    } else {
+#pragma unroll
+                        for (int o = LPR / 2; o > 0; o >>= 1)
+#pragma unroll
+                            for (int j = 0; j < HALF; ++j) t[j] = max(t[j], __shfl_xor_sync(0xffffffffu, t[j], o));
                     }
+#pragma unroll
+                    for (int j = 0; j < HALF; ++j) mine = sub == h * HALF + j ? t[j] : mine;      // lane j of a row's lanes has set j
                 }
                 if (!ok) break;
                 const RowScale rs = row_scale(Eight<T>::top_f32(mine));
@@ -257,14 +273,22 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (!there[h]) continue;
+                    Eight<T> v[HALF];
+                    float inv[HALF];
+                    uint2 c[HALF];
 #pragma unroll
-                    for (int j = h * HALF; j < (h + 1) * HALF; ++j) {
-                        Eight<T> v;
-                        read(v, j, base[h]);
-                        const float inv = __shfl_sync(0xffffffffu, rs.inv, (lane & ~(LPR - 1)) + j);
-                        const int r = row_of(batch, j), at = sub * 8;
-                        if (at < g.kb * 128)
-                            *(uint2 *)(tile + (size_t)(at >> 7) * kQBlock + r * 128 + ((((at >> 4) ^ r) & 7) << 4) + (at & 8)) = v.codes(inv);
+                    for (int j = 0; j < HALF; ++j) read(v[j], j, base[h]);
+#pragma unroll
+                    for (int j = 0; j < HALF; ++j) inv[j] = __shfl_sync(0xffffffffu, rs.inv, (lane & ~(LPR - 1)) + h * HALF + j);
+#pragma unroll
+                    for (int j = 0; j < HALF; ++j) c[j] = v[j].codes(inv[j]);
+                    if (sub * 8 < g.kb * 128) {
+                        const int at = sub * 8;
+#pragma unroll
+                        for (int j = 0; j < HALF; ++j) {
+                            const int r = row_of(batch, h * HALF + j);
+                            *(uint2 *)(tile + (size_t)(at >> 7) * kQBlock + r * 128 + ((((at >> 4) ^ r) & 7) << 4) + (at & 8)) = c[j];
+                        }
                     }
                     __syncwarp();                             // every lane has read this half
                     if (lane == 0) mbar_arrive(&ctl->rows_empty[qg][bar[h]]);
@@ -376,7 +400,7 @@ size_t fused_smem(const QuantFused &g, size_t slot) {
 // unit per SM a warp per row beats sixteen rows a warp one after the other.
 bool quant_fused_eligible(const Problem &pb, int elem_bytes) {
     return pb.c_in <= 256 && pb.c_in % 8 == 0 && (size_t)pb.c_in * elem_bytes % 16 == 0 && pb.c_out <= 2048 &&
-           pb.p >= (long long)kQRows * device_sm_count();
+           (pb.stride_h == 1 && pb.stride_w == 1 ? true : pb.c_in % 64 == 0 && pb.stride_h <= 8 && pb.stride_w <= 8) && pb.p >= (long long)kQRows * device_sm_count();
 }
 
 RowMap quant_row_map(const Problem &pb) {
@@ -395,7 +419,10 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
                                const void *add, int relu, void *z, cudaStream_t st) {
     const int es = dtype == CONVBN_F32 ? 4 : 2, sms = device_sm_count();
     QuantFused g;
-    g.rows = quant_row_map(pb);
+    g.strided = pb.stride_h != 1 || pb.stride_w != 1;
+    g.stride_h = pb.stride_h; g.stride_w = pb.stride_w;
+    g.by_w = FastDiv((uint32_t)pb.w_out); g.by_h = FastDiv((uint32_t)pb.h_out);
+    g.boxes = (pb.c_in * es + 127) / 128;
     g.p = (uint32_t)pb.p; g.k = pb.c_in; g.kb = (pb.c_in + 127) / 128; g.n = pb.c_out; g.relu = relu;
     g.dense = (size_t)pb.c_out * es % 16 == 0;
     g.units = (uint32_t)((pb.p + kQRows - 1) / kQRows);
@@ -426,7 +453,13 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
     }
     smem = fused_smem(g, slot);
     const unsigned grid = g.units < (uint32_t)sms ? g.units : (unsigned)sms;
-    CUtensorMap tw, tz, ta;
+    CUtensorMap tx, tw, tz, ta;
+    const int slot_rows = (int)(slot / (set / (pb.c_in <= 64 ? 4 : (pb.c_in <= 128 ? 2 : 1))));
+    // (the box of base pixels has h_out x w_out positions: upper = (out - 1) stride - (in - 1))
+    if (g.strided ? !make_tmap_im2col_bf16(&tx, x, pb.n, pb.h_in, pb.w_in, pb.c_in, 0, 0, (pb.h_out - 1) * pb.stride_h - (pb.h_in - 1),
+                                           (pb.w_out - 1) * pb.stride_w - (pb.w_in - 1), pb.stride_h, pb.stride_w, slot_rows, 64)
+                  : !make_tmap_matrix_bytes(&tx, x, pb.p, pb.c_in, es, slot_rows))
+        return cudaErrorInvalidValue;
     if (!make_tmap_matrix_bytes(&tw, wq, pb.c_out, quant_pitch(pb), 1, g.bn)) return cudaErrorInvalidValue;
     tz = ta = tw;
     if (g.dense) {
@@ -441,7 +474,7 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
         static PerDevice attr, carve;
         if (cudaError_t e = max_dynamic_smem_once(kernel, 227 * 1024, &attr); e != cudaSuccess) return e;
         prefer_max_shared_once(kernel, &carve);
-        return launch_pdl(kernel, dim3(grid), dim3(kQThreads), smem, st, tw, tz, ta, g, (const T *)x, ws, shift, (const T *)add, (T *)z, err);
+        return launch_pdl(kernel, dim3(grid), dim3(kQThreads), smem, st, tx, tw, tz, ta, g, ws, shift, (const T *)add, (T *)z, err);
     };
     auto typed = [&](auto tag) {
         using std::integral_constant;

@@ -196,13 +196,6 @@ __device__ __forceinline__ void tma_load_3d(Dst smem_dst, const CUtensorMap *map
         ::"r"(smem_u32(smem_dst)), "l"((uint64_t)map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
         : "memory");
 }
-// `bytes` side by side: both addresses and the count multiples of 16.
-template <class Dst, class Bar>
-__device__ __forceinline__ void bulk_load(Dst smem_dst, const void *src, uint32_t bytes, Bar bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem_u32(smem_dst)), "l"((uint64_t)__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
-                 : "memory");
-}
 // Tiled 4-D box (c, w, h, n); coordinates outside the tensor read zeros (c must stay 16-byte aligned).
 template <class Dst, class Bar>
 __device__ __forceinline__ void tma_load_4d(Dst smem_dst, const CUtensorMap *map, Bar bar, int c, int w,
