@@ -42,12 +42,12 @@ struct Eight {
             w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
         }
     }
-    // from a row of 128 bytes in shared memory, chunk (of 16 bytes) c and the next ones at c ^ swizzle
-    __device__ __forceinline__ void load_swizzled(uint32_t row, uint32_t c, uint32_t swizzle) {
+    // from shared memory; the second 16 bytes of fp32 lie in the neighbouring chunk of a swizzled row
+    __device__ __forceinline__ void load_shared(uint32_t at) {
 #pragma unroll
         for (int i = 0; i < kWords; i += 4)
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(row + (((c + i / 4) ^ swizzle) << 4)) : "memory");
+                         : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(at ^ (uint32_t)(4 * i)) : "memory");
     }
     __device__ __forceinline__ void load_some(const T *p, int count) {      // any alignment, the rest zero
         zero();
@@ -119,6 +119,24 @@ struct RowMap {
 };
 
 RowMap quant_row_map(const Problem &pb);      // (quant_fused.cu)
+
+// mbar_wait_bounded whose attempts may last up to 4 us each: a waiting warp leaves the issue slots to those that convert.
+template <class Bar>
+__device__ __forceinline__ bool mbar_wait_parked(Bar bar, uint32_t parity, volatile int *abort_flag, uint64_t limit_ns = 2000000000ull) {
+    auto attempt = [&]() {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(ptx::smem_u32(bar)), "r"(parity), "r"(4000u) : "memory");
+        return ok != 0;
+    };
+    if (attempt()) return true;
+    const uint64_t t0 = ptx::globaltimer_ns();
+    while (true) {
+        if (attempt()) return true;
+        if (abort_flag && *abort_flag) return false;
+        if (ptx::globaltimer_ns() - t0 > limit_ns) return false;
+    }
+}
 
 // ---- tensor-core product of codes ---------------------------------------------------------------------------------------
 // tcgen05.mma instruction descriptor of kind::i8: bits 4-5 D format (2 = s32), 7-9 and 10-12 operand formats (1 = s8), 17-22 N >> 3,

@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     for (uint32_t nt = 0; ok && nt < g.n_tiles; ++nt)
                         for (int kb = 0; kb < g.kb; ++kb, ++it) {
                             const uint32_t s = it % g.stages, ph = (it / g.stages) & 1u;
-                            ok = mbar_wait_bounded(&ctl->empty[s], ph ^ 1u, abort_flag);
+                            ok = mbar_wait_parked(&ctl->empty[s], ph ^ 1u, abort_flag);
                             if (!ok) break;
                             mbar_arrive_expect_tx(&ctl->full[s], w_bytes);
                             tma_load_2d(w_tiles + (size_t)s * w_bytes, &tm_w, &ctl->full[s], kb * 128, (int)nt * g.bn);
@@ -127,9 +127,9 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             if (!ok) {
                 give_up();
                 for (uint32_t j = it > (uint32_t)g.stages ? it - g.stages : 0; j < it; ++j)      // let the copies in flight land
-                    mbar_wait_bounded(&ctl->full[j % g.stages], (j / g.stages) & 1u, nullptr, 200000000ull);
+                    mbar_wait_parked(&ctl->full[j % g.stages], (j / g.stages) & 1u, nullptr, 200000000ull);
             } else if (g.resident) {
-                mbar_wait_bounded(&ctl->wfull, 0, nullptr, 200000000ull);
+                mbar_wait_parked(&ctl->wfull, 0, nullptr, 200000000ull);
             }
         }
     } else if (warp == 1) {
@@ -137,21 +137,21 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             const uint32_t idesc = idesc_s8(kQRows, g.bn), hi = smem_desc_hi_sw128(1024);
             const uint32_t a0 = smem_desc_lo(smem_u32(a_tiles), 16), w0 = smem_desc_lo(smem_u32(w_tiles), 16);
             const int tail = (g.k - (g.kb - 1) * 128 + 31) / 32;              // steps of 32 codes of the last block
-            bool ok = !g.resident || mbar_wait_bounded(&ctl->wfull, 0, abort_flag);
+            bool ok = !g.resident || mbar_wait_parked(&ctl->wfull, 0, abort_flag);
             uint32_t i = 0, s = 0, it = 0;
             for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
                 const uint32_t ab = i & 1u, use = i >> 1;
-                ok = mbar_wait_bounded(&ctl->a_full[ab], use & 1u, abort_flag);
+                ok = mbar_wait_parked(&ctl->a_full[ab], use & 1u, abort_flag);
                 for (uint32_t nt = 0; ok && nt < g.n_tiles; ++nt, ++s) {
                     const uint32_t acc = s & 1u, d = tmem_base + acc * (uint32_t)g.bn;
-                    ok = mbar_wait_bounded(&ctl->acc_empty[acc], ((s >> 1) & 1u) ^ 1u, abort_flag);
+                    ok = mbar_wait_parked(&ctl->acc_empty[acc], ((s >> 1) & 1u) ^ 1u, abort_flag);
                     if (!ok) break;
                     tc_fence_after_sync();
                     for (int kb = 0; kb < g.kb; ++kb) {
                         uint32_t slot = nt * g.kb + kb;
                         if (!g.resident) {
                             slot = it % g.stages;
-                            ok = mbar_wait_bounded(&ctl->full[slot], (it / g.stages) & 1u, abort_flag);
+                            ok = mbar_wait_parked(&ctl->full[slot], (it / g.stages) & 1u, abort_flag);
                             if (!ok) break;
                             ++it;
                         }
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                 for (uint32_t first = u * kQRows; first < end; first += R::SLOT_ROWS) {
                     const uint32_t n = qg ? asked[1] : asked[0], turn = n / (uint32_t)g.depth, slot = n - turn * (uint32_t)g.depth;
                     uint64_t *full = &ctl->rows_full[qg][slot];
-                    ok = mbar_wait_bounded(&ctl->rows_empty[qg][slot], (turn & 1u) ^ 1u, abort_flag);
+                    ok = mbar_wait_parked(&ctl->rows_empty[qg][slot], (turn & 1u) ^ 1u, abort_flag);
                     if (!ok) break;
                     uint8_t *to = ring + ((size_t)qg * g.depth + slot) * R::SLOT_BYTES;
                     mbar_arrive_expect_tx(full, (uint32_t)g.boxes * (R::SLOT_ROWS * 128));
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             give_up();
             for (int qg = 0; qg < 2; ++qg)
                 for (uint32_t j = asked[qg] > (uint32_t)g.depth ? asked[qg] - g.depth : 0; j < asked[qg]; ++j)    // let the copies in flight land
-                    mbar_wait_bounded(&ctl->rows_full[qg][j % g.depth], (j / g.depth) & 1u, nullptr, 200000000ull);
+                    mbar_wait_parked(&ctl->rows_full[qg][j % g.depth], (j / g.depth) & 1u, nullptr, 200000000ull);
         }
     } else if (warp >= kQLoadWarp) {
         // ---- rows to codes ----
@@ -215,23 +215,29 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         const int sub = lane & (LPR - 1), row_l = lane / LPR, own = qw * HALF * RPI + row_l;     // row in a slot
         const uint32_t ring0 = smem_u32(ring) + (uint32_t)(qg * g.depth) * RowSets<T, LPR>::SLOT_BYTES;
         uint32_t slot = 0, ph = 0;
-        // set j of a batch in its unit, as this lane has it
+        // Where set j of a half batch is for this lane, in its slot and in its unit's A operand (slots and their rows in the unit start on
+        // multiples of eight rows).  Formed for every row anew, from pointers whose kind the compiler cannot see, these took as many
+        // instructions as all else.
+        uint32_t from[HALF], to[HALF];
+#pragma unroll
+        for (int j = 0; j < HALF; ++j) {
+            const uint32_t r = (uint32_t)(own + j * RPI), chunk = (uint32_t)sub * (sizeof(T) / 2), at = (uint32_t)sub * 8u;
+            from[j] = (chunk >> 3) * (SLOT_ROWS * 128) + r * 128u + (((chunk ^ r) & 7u) << 4);
+            to[j] = (at >> 7) * kQBlock + r * 128u + ((((at >> 4) ^ r) & 7u) << 4) + (at & 8u);
+        }
+        const bool there_is = sub * 8 < g.boxes * (int)(128 / sizeof(T));                          // (a box with these elements)
+        auto read = [&](Eight<T> &v, uint32_t at) { if (there_is) v.load_shared(at); else v.zero(); };
+        // set j of a batch in its unit
         auto row_of = [&](int batch, int j) { return (2 * batch + j / HALF) * SLOT_ROWS + own + j % HALF * RPI; };
         bool ok = true;
         uint32_t i = 0;
         for (uint32_t u = blockIdx.x; ok && u < g.units; u += gridDim.x, ++i) {
             const uint32_t ab = i & 1u, use = i >> 1;
             if (R::GROUPS == 2 && (int)ab != qg) continue;    // (the other group's)
-            uint8_t *tile = a_tiles + (size_t)ab * a_bytes;
-            float *xs = xs_s + (i % kQSlots) * kQRows;
+            const uint32_t tile = smem_u32(a_tiles) + ab * a_bytes, xs = smem_u32(xs_s) + (i % kQSlots) * (kQRows * 4u);
             const uint32_t first = u * kQRows;
 #pragma unroll 1
             for (int batch = 0; batch < BATCHES; ++batch) {
-                auto read = [&](Eight<T> &v, int j, uint32_t base) {       // set j of the batch as this lane has it
-                    if (sub * 8 >= g.boxes * (int)(128 / sizeof(T))) { v.zero(); return; }         // (no box there)
-                    const uint32_t r = (uint32_t)(own + j % HALF * RPI), chunk = (uint32_t)sub * (sizeof(T) / 2);     // of 16 bytes
-                    v.load_swizzled(base + (chunk >> 3) * (SLOT_ROWS * 128) + r * 128u, chunk & 7u, r & 7u);
-                };
                 uint32_t mine = 0, base[2], bar[2];
                 bool there[2];
 #pragma unroll
@@ -240,7 +246,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     base[h] = ring0 + slot * RowSets<T, LPR>::SLOT_BYTES;
                     bar[h] = slot;
                     if (!there[h]) continue;
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->rows_full[qg][slot], ph, abort_flag));
+                    ok = __all_sync(0xffffffffu, mbar_wait_parked(&ctl->rows_full[qg][slot], ph, abort_flag));
                     if (!ok) break;
                     if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
                     // (a half batch's rows are loaded before the first is used: row by row a unit of 256 channels took 1634 clocks here
@@ -248,7 +254,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     Eight<T> v[HALF];
                     uint32_t t[HALF];
 #pragma unroll
-                    for (int j = 0; j < HALF; ++j) read(v[j], j, base[h]);
+                    for (int j = 0; j < HALF; ++j) read(v[j], base[h] + from[j]);
 #pragma unroll
                     for (int j = 0; j < HALF; ++j) t[j] = v[j].top();
                     if constexpr (LPR == 32) {
@@ -266,10 +272,10 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                 if (!ok) break;
                 const RowScale rs = row_scale(Eight<T>::top_f32(mine));
                 if (batch == 0) {
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->a_empty[ab], (use & 1u) ^ 1u, abort_flag));
+                    ok = __all_sync(0xffffffffu, mbar_wait_parked(&ctl->a_empty[ab], (use & 1u) ^ 1u, abort_flag));
                     if (!ok) break;
                 }
-                if (sub < BATCH) xs[row_of(batch, sub)] = rs.scale;
+                if (sub < BATCH) asm volatile("st.shared.f32 [%0], %1;" ::"r"(xs + (uint32_t)row_of(batch, sub) * 4u), "f"(rs.scale) : "memory");
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (!there[h]) continue;
@@ -277,18 +283,16 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     float inv[HALF];
                     uint2 c[HALF];
 #pragma unroll
-                    for (int j = 0; j < HALF; ++j) read(v[j], j, base[h]);
+                    for (int j = 0; j < HALF; ++j) read(v[j], base[h] + from[j]);
 #pragma unroll
                     for (int j = 0; j < HALF; ++j) inv[j] = __shfl_sync(0xffffffffu, rs.inv, (lane & ~(LPR - 1)) + h * HALF + j);
 #pragma unroll
                     for (int j = 0; j < HALF; ++j) c[j] = v[j].codes(inv[j]);
                     if (sub * 8 < g.kb * 128) {
-                        const int at = sub * 8;
+                        const uint32_t rows_at = tile + (uint32_t)((2 * batch + h) * SLOT_ROWS) * 128u;
 #pragma unroll
-                        for (int j = 0; j < HALF; ++j) {
-                            const int r = row_of(batch, h * HALF + j);
-                            *(uint2 *)(tile + (size_t)(at >> 7) * kQBlock + r * 128 + ((((at >> 4) ^ r) & 7) << 4) + (at & 8)) = c[j];
-                        }
+                        for (int j = 0; j < HALF; ++j)
+                            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(rows_at + to[j]), "r"(c[j].x), "r"(c[j].y) : "memory");
                     }
                     __syncwarp();                             // every lane has read this half
                     if (lane == 0) mbar_arrive(&ctl->rows_empty[qg][bar[h]]);
@@ -334,7 +338,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     __syncwarp();
                 };
                 if (g.dense) fetch_add(0);
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->xs_full[i % kQSlots], (i / kQSlots) & 1u, abort_flag));
+                ok = __all_sync(0xffffffffu, mbar_wait_parked(&ctl->xs_full[i % kQSlots], (i / kQSlots) & 1u, abort_flag));
                 const float *xs = xs_s + (i % kQSlots) * kQRows + quarter * 32;
                 f32x2 xs2[4];                    // 16-bit types: rows lane / 4 + 8 k, otherwise row `lane`
 #pragma unroll
@@ -342,9 +346,9 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     const float v1 = ok ? xs[g.dense && sizeof(T) == 2 ? lane / 4 + 8 * k : lane] : 0.f;
                     xs2[k] = pair(v1, v1);
                 }
-                ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->acc_full[s & 1u], (s >> 1) & 1u, abort_flag));
+                ok = ok && __all_sync(0xffffffffu, mbar_wait_parked(&ctl->acc_full[s & 1u], (s >> 1) & 1u, abort_flag));
                 if (!ok) {
-                    if (boxed) { if (lane == 0) mbar_wait_bounded(add_bar, add_ph, nullptr, 200000000ull); __syncwarp(); }
+                    if (boxed) { if (lane == 0) mbar_wait_parked(add_bar, add_ph, nullptr, 200000000ull); __syncwarp(); }
                     break;
                 }
                 tc_fence_after_sync();
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                 for (int c0 = 0; c0 < cols; c0 += CH) {
                     uint8_t *buf = box();
                     if (boxed) {
-                        ok = __all_sync(0xffffffffu, mbar_wait_bounded(add_bar, add_ph, abort_flag));
+                        ok = __all_sync(0xffffffffu, mbar_wait_parked(add_bar, add_ph, abort_flag));
                         add_ph ^= 1u;
                         if (!ok) break;
                     }
