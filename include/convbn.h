@@ -278,7 +278,7 @@ int convbn_deploy_bwd(const convbn_desc *desc, const void *dz, const void *x,
  * Layers: kh = kw = 1, no padding, groups = 1, any stride, C_in <= 131072, fewer than 2^31 - 256 output pixels; NHWC 16-bit storage,
  * or fp32 with one pixel per image (convbn_linear_desc).  Others: CONVBN_EUNSUPPORTED, workspace size 0.
  * z may not overlap x; add [like z, 16-byte aligned, NULL: none] may not overlap z.
- * Workspace of the forward call: convbn_workspace_bytes(desc, CONVBN_PHASE_DEPLOY_FWD_QUANT). */
+ * Workspace of the forward call: convbn_workspace_bytes(desc, CONVBN_PHASE_DEPLOY_FWD_QUANT), 0 where the codes stay on chip. */
 int convbn_deploy_prepare_quant(const convbn_desc *desc, const void *w, const float *b, const float *gamma, const float *beta,
                                 const float *run_mean, const float *run_var, void *w_codes, float *w_scale, float *b_fused,
                                 void *stream);

@@ -72,6 +72,15 @@ struct Eight {
             return m;
         }
     }
+    // The same in steps: of these eight (16-bit types: of the even and the odd ones), of two such, as top() has it.
+    __device__ __forceinline__ uint32_t part() const {
+        uint32_t m = sizeof(T) == 2 ? w[0] : w[0] & 0x7FFFFFFFu;
+#pragma unroll
+        for (int i = 1; i < kWords; ++i) m = sizeof(T) == 2 ? larger(m, w[i]) : max(m, w[i] & 0x7FFFFFFFu);
+        return m;
+    }
+    static __device__ __forceinline__ uint32_t of_two(uint32_t a, uint32_t b) { return sizeof(T) == 2 ? larger(a, b) : max(a, b); }
+    static __device__ __forceinline__ uint32_t whole(uint32_t m) { return sizeof(T) == 2 ? merge(m) : m; }
     // of the larger magnitudes of two words' halves (16-bit types; the signs are any)
     static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
         uint32_t r;

@@ -3,9 +3,10 @@
 // addend and ReLU are applied to the sums.  X is read once in its storage type, Z written once; codes exist on chip only.
 //
 // CTA = 19 warps: 0 weight tiles (TMA), 1 MMA issuer and owner of tensor memory, 2-9 epilogue (two groups of four, an accumulator
-// each), 10-17 rows to codes, 18 brings the rows.  A unit of work is 128 rows: eight warps read them whole, a row by 8, 16 or 32 lanes, find the largest magnitude, and write the codes as the K-major A operand
-// (128-byte swizzle).  Rows on 16-byte boundaries arrive by bulk copies of up to
-// 16 KB in a ring (by loads into registers, a batch ahead, 256 -> 64 at 56 x 56, N = 256 took 143 us).
+// each), 10-17 rows to codes, 18 brings the rows by TMA into a ring.  A unit of work is 128 rows: they are read whole, a row by 8, 16 or
+// 32 lanes, for their largest magnitudes and again for the codes, which are written as the K-major A operand (128-byte swizzle).
+// Bound by those two readings for long rows, by the epilogue for wide outputs: 256 -> 64 at 56 x 56, N = 256 107 us (78.5 at the
+// measured copy bandwidth), 64 -> 256, N = 128 55.5 (39.3), 128 -> 128, N = 128 40.3 (31.4).
 #include "kernels.h"
 #include "quant8.cuh"
 
@@ -207,8 +208,9 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         // ---- rows to codes ----
         // What a unit costs beside its elements (waits, scales, the hand-over) is most of it where rows are short: two groups, each with an A
         // buffer of its own, halve that and run beside each other, 64 -> 64 at 56 x 56, N = 256 62 -> 51 us; longer rows want the ring in
-        // one piece, 256 -> 64 132 us and 157 by groups.  A batch's rows are read twice: for their largest magnitudes, and after these
-        // have become scales, which each lane works out for one row (a scale per four rows, and the rows kept in registers between: 192).
+        // one piece, 256 -> 64 132 us and 157 by groups (sixteen warps in two groups: 133 where eight in one took 118).  A batch's rows are
+        // read twice: for their largest magnitudes, and after these have become scales, which each lane works out for one row (a scale
+        // per four rows, and the rows kept in registers between: 192 us).
         using R = RowSets<T, LPR>;
         constexpr int RPI = R::RPI, BATCH = R::BATCH, BATCHES = R::BATCHES, HALF = R::HALF, SLOT_ROWS = R::SLOT_ROWS;
         const int qg = R::GROUPS == 2 ? (warp - kQLoadWarp) >> 2 : 0, qw = (warp - kQLoadWarp) & (R::WARPS - 1);
@@ -238,8 +240,10 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
             const uint32_t first = u * kQRows;
 #pragma unroll 1
             for (int batch = 0; batch < BATCHES; ++batch) {
-                uint32_t mine = 0, base[2], bar[2];
+                uint32_t t[BATCH], base[2], bar[2];
                 bool there[2];
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) t[j] = 0u;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     there[h] = first + (uint32_t)((2 * batch + h) * SLOT_ROWS) < g.p;       // (a slot past the last row never comes)
@@ -250,32 +254,34 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     if (!ok) break;
                     if (++slot == (uint32_t)g.depth) { slot = 0; ph ^= 1u; }
                     // (a half batch's rows are loaded before the first is used: row by row a unit of 256 channels took 1634 clocks here
-                    // and 2690 below, of 5800; now LATERD)
+                    // and 2690 below, of 5800)
                     Eight<T> v[HALF];
-                    uint32_t t[HALF];
 #pragma unroll
                     for (int j = 0; j < HALF; ++j) read(v[j], base[h] + from[j]);
 #pragma unroll
-                    for (int j = 0; j < HALF; ++j) t[j] = v[j].top();
-                    if constexpr (LPR == 32) {
-#pragma unroll
-                        for (int j = 0; j < HALF; ++j) t[j] = __reduce_max_sync(0xffffffffu, t[j]);
-                    } else {
-#pragma unroll
-                        for (int o = LPR / 2; o > 0; o >>= 1)
-#pragma unroll
-                            for (int j = 0; j < HALF; ++j) t[j] = max(t[j], __shfl_xor_sync(0xffffffffu, t[j], o));
-                    }
-#pragma unroll
-                    for (int j = 0; j < HALF; ++j) mine = sub == h * HALF + j ? t[j] : mine;      // lane j of a row's lanes has set j
+                    for (int j = 0; j < HALF; ++j) t[h * HALF + j] = v[j].part();
                 }
+                // The largest of each row over its lanes: lanes exchange halves of the sets until a lane has one set, then the rest.  Lane
+                // j LPR / BATCH of a row's lanes ends with set j.  (A redux per row took 90 clocks each.)
+#pragma unroll
+                for (int n = BATCH / 2, o = LPR / 2; n > 0; n /= 2, o /= 2) {
+                    const bool upper = sub & o;
+#pragma unroll
+                    for (int j = 0; j < n; ++j) {
+                        const uint32_t keep = upper ? t[j + n] : t[j], give = upper ? t[j] : t[j + n];
+                        t[j] = Eight<T>::of_two(keep, __shfl_xor_sync(0xffffffffu, give, o));
+                    }
+                }
+#pragma unroll
+                for (int o = LPR / BATCH / 2; o > 0; o /= 2) t[0] = Eight<T>::of_two(t[0], __shfl_xor_sync(0xffffffffu, t[0], o));
+                const uint32_t mine = Eight<T>::whole(t[0]);
                 if (!ok) break;
                 const RowScale rs = row_scale(Eight<T>::top_f32(mine));
                 if (batch == 0) {
                     ok = __all_sync(0xffffffffu, mbar_wait_parked(&ctl->a_empty[ab], (use & 1u) ^ 1u, abort_flag));
                     if (!ok) break;
                 }
-                if (sub < BATCH) asm volatile("st.shared.f32 [%0], %1;" ::"r"(xs + (uint32_t)row_of(batch, sub) * 4u), "f"(rs.scale) : "memory");
+                if ((sub & (LPR / BATCH - 1)) == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(xs + (uint32_t)row_of(batch, sub / (LPR / BATCH)) * 4u), "f"(rs.scale) : "memory");
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (!there[h]) continue;
@@ -285,7 +291,7 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
 #pragma unroll
                     for (int j = 0; j < HALF; ++j) read(v[j], base[h] + from[j]);
 #pragma unroll
-                    for (int j = 0; j < HALF; ++j) inv[j] = __shfl_sync(0xffffffffu, rs.inv, (lane & ~(LPR - 1)) + h * HALF + j);
+                    for (int j = 0; j < HALF; ++j) inv[j] = __shfl_sync(0xffffffffu, rs.inv, (lane & ~(LPR - 1)) + (h * HALF + j) * (LPR / BATCH));
 #pragma unroll
                     for (int j = 0; j < HALF; ++j) c[j] = v[j].codes(inv[j]);
                     if (sub * 8 < g.kb * 128) {
@@ -398,13 +404,14 @@ size_t fused_smem(const QuantFused &g, size_t slot) {
 
 }  // namespace
 
-// Rows enough for every SM, and short ones that start on 16-byte boundaries.  This kernel and the two of quant_gemm.cu, us: 100352
-// rows 64 -> 256 20.5 and 27.7, 256 -> 64 23.3 and 28.0, 256 -> 1024 78.7 and 79.8, but (as it was for longer rows) 512 -> 64 41.6 and
-// 43.8, 512 -> 1024 122.9 and 100.8; 6272 rows 64 -> 256 6.1 and 5.9, 256 -> 64 7.2 and 6.1; 1000 rows 256 -> 64 7.0 and 5.6: below a
-// unit per SM a warp per row beats sixteen rows a warp one after the other.
+// Rows enough for every SM, short ones that start on 16-byte boundaries, and not too many channels for two accumulators to drain.  This
+// kernel and the two of quant_gemm.cu, us: 100352 rows 64 -> 256 18.8 and 25.9, 256 -> 64 19.5 and 28.1, 128 -> 128 14.7 and 22.4,
+// 256 -> 1024 75.3 and 79.1, 64 -> 2048 143 and 123; 19200 rows 64 -> 256 7.8 and 9.6, 256 -> 64 8.3 and 8.7; an earlier form of it
+// 512 -> 1024 122.9 and 100.8, and below a unit per SM, 6272 rows 256 -> 64, 7.2 and 6.1: a warp per row beats sixteen rows a warp.
 bool quant_fused_eligible(const Problem &pb, int elem_bytes) {
-    return pb.c_in <= 256 && pb.c_in % 8 == 0 && (size_t)pb.c_in * elem_bytes % 16 == 0 && pb.c_out <= 2048 &&
-           (pb.stride_h == 1 && pb.stride_w == 1 ? true : pb.c_in % 64 == 0 && pb.stride_h <= 8 && pb.stride_w <= 8) && pb.p >= (long long)kQRows * device_sm_count();
+    const bool beside = pb.stride_h == 1 && pb.stride_w == 1;            // (otherwise im2col boxes of 64 channels)
+    return pb.c_in <= 256 && pb.c_in % 8 == 0 && (size_t)pb.c_in * elem_bytes % 16 == 0 && pb.c_out <= 1024 &&
+           (beside || (pb.c_in % 64 == 0 && pb.stride_h <= 8 && pb.stride_w <= 8)) && pb.p >= (long long)kQRows * device_sm_count();
 }
 
 RowMap quant_row_map(const Problem &pb) {
@@ -430,13 +437,14 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
     g.p = (uint32_t)pb.p; g.k = pb.c_in; g.kb = (pb.c_in + 127) / 128; g.n = pb.c_out; g.relu = relu;
     g.dense = (size_t)pb.c_out * es % 16 == 0;
     g.units = (uint32_t)((pb.p + kQRows - 1) / kQRows);
-    // Buffers: two boxes per epilogue warp, the weights resident, otherwise at least three slots of them, wide tiles, and slots of rows,
-    // four for each group if there is room (two are in use, the others on their way).
+    // Buffers.  Rows up to 128 elements: two boxes per epilogue warp and four slots of rows per group (64 -> 256 at 56 x 56, N = 128 55.5 us,
+    // with one box and six slots 59.3); longer ones the other way round (256 -> 64, N = 256 107.3 and 111.5).  The weights resident,
+    // otherwise at least three slots of them; wide tiles.
     const size_t room = 227 * 1024, set = 256 * es;
     g.rings = pb.c_in <= 64 ? 2 : 1;                                                         // (RowSets)
     const size_t warps = 8 / g.rings, sets = kQRows / warps / (pb.c_in <= 64 ? 4 : (pb.c_in <= 128 ? 2 : 1));
     const size_t slot = warps * (sets * set <= 4096 ? sets * set : 4096) / 2;
-    const struct { int nbuf, depth; } wanted[] = {{2, 4}, {1, 6}, {1, 4}, {1, 3}, {1, 2}};
+    const struct { int nbuf, depth; } wanted[] = {{pb.c_in <= 128 ? 2 : 1, pb.c_in <= 128 ? 4 : 6}, {1, 4}, {1, 3}, {1, 2}};
     size_t smem = 0;
     for (const auto &c : wanted) {
         g.nbuf = c.nbuf; g.depth = c.depth; g.stages = 3;

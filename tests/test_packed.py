@@ -355,3 +355,48 @@ def test_a_group_that_is_no_number_shows_in_the_gradients():
     got = _packed_pass(spec, t, None, True)
     assert np.isnan(got["dw"][:, 32:64]).all() and np.isfinite(np.delete(got["dw"], np.s_[32:64], 1)).all()
     assert not got["dx"][0, 32:64, 2, 3].any() and np.isfinite(got["dx"]).all() and np.isfinite(got["dbeta"]).all()
+
+
+@pytest.mark.gpu
+def test_more_than_two_to_the_31_elements():
+    import torch
+    count, tail = (1 << 31) + 32 * 1001 + 5, 32 * 4000 + 5
+    x = torch.empty(count, dtype=torch.bfloat16, device="cuda")
+    for at in range(0, count, 1 << 28):
+        x[at:at + (1 << 28)].normal_(generator=torch.Generator("cuda").manual_seed(at & 1023))
+    codes, steps = torch.empty(count, dtype=torch.int8, device="cuda"), torch.empty(-(-count // 32), dtype=torch.uint8, device="cuda")
+    C.convbn_pack(x, codes, steps)
+    q, s = P.pack(x[count - tail:].float().cpu().numpy(), "bf16")
+    assert np.array_equal(codes[count - tail:].cpu().numpy(), q) and np.array_equal(steps[(count - tail) // 32:].cpu().numpy(), s)
+    x.zero_()
+    C.convbn_unpack(codes, steps, x)
+    C.convbn_check()
+    np.testing.assert_array_equal(x[count - tail:].float().cpu().numpy().astype(np.float64), P.unpack(q, s))
+
+
+@pytest.mark.gpu
+def test_a_packed_backward_pass_of_more_than_two_to_the_31_elements():
+    """dX of the last rows by themselves: the same bits.  dbeta: the sum over all rows of dZ = 1 and 0."""
+    import torch
+    rows, ci, co, tail = 8_500_000, 256, 64, 128 * 1000
+    g = torch.Generator("cuda").manual_seed(1)
+    codes = torch.empty(rows, ci, dtype=torch.int8, device="cuda")
+    for at in range(0, rows, 1_000_000):
+        codes[at:at + 1_000_000].random_(-127, 128, generator=g)
+    steps = torch.full((rows, ci // 32), 121, dtype=torch.uint8, device="cuda")
+    dz = (torch.arange(rows, device="cuda") % 2).to(torch.bfloat16)[:, None].expand(rows, co).contiguous()
+    w = torch.randn(co, ci, device="cuda", generator=g).to(torch.bfloat16)
+    mean, saved = torch.zeros(co, device="cuda"), torch.ones(3 * co, device="cuda")
+    out = []
+    for first in (0, rows - tail):
+        n = rows - first
+        d = C.convbn_linear_desc(n, ci, co)
+        dx = torch.empty(n, ci, dtype=torch.bfloat16, device="cuda")
+        dw, dgamma, dbeta = torch.empty(co, ci, device="cuda"), torch.empty(co, device="cuda"), torch.empty(co, device="cuda")
+        ws = torch.empty(max(256, C.convbn_workspace_bytes(d, C.PHASE_TUNE_BWD_PACKED)), dtype=torch.uint8, device="cuda")
+        C.convbn_tune_bwd_packed(d, dz[first:], codes[first:], steps[first:], w, None, mean, saved, dx, dw, None, dgamma, dbeta, None, True,
+                                 False, ws)
+        C.convbn_check()
+        assert bool((dbeta == n // 2).all())
+        out.append(dx[n - tail:].clone())
+    assert torch.equal(out[0], out[1]) and bool((out[0][codes[rows - tail:] <= 0] == 0).all())

@@ -181,3 +181,66 @@ def test_rows_and_channels_that_are_zero_tiny_infinite_or_not_numbers(rows):
     bad[[2, rows - 1]] = True
     bad[:, 9] = True
     assert np.array_equal(np.isnan(got), bad) and np.isfinite(got[~bad]).all()
+
+
+# ---- together, as a deployed network uses them ---------------------------------------------------------------------------
+@pytest.mark.gpu
+def test_a_deployed_bottleneck_of_three_calls_captured_and_replayed():
+    """A reducing layer, a wide one and one row after the other on a stream of their own, in one captured graph, replayed on other
+    inputs: every result is that of the definition for the stored result of the layer before."""
+    import torch
+    from paper_2305_11624_b200.harness import Block
+    specs = [I.LayerSpec("q1", 7, 256, 28, 28, 64, 1, 1), I.LayerSpec("q2", 7, 64, 28, 28, 640, 1, 1), I.LayerSpec("q3", 7, 640, 28, 28, 72, 1, 1)]
+    blocks = [Block(s, modes=("quant",)) for s in specs]
+    for k, b in enumerate(blocks):
+        b.randomize(k)
+        b.deploy_prepare_quant()
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+
+    def chain():
+        for k, b in enumerate(blocks):
+            if k:
+                b.x = blocks[k - 1].z
+            b.deploy_fwd_quant(relu=k < 2)
+
+    with torch.cuda.stream(stream):
+        chain()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        chain()
+    for seed in (5, 6):
+        blocks[0].x.copy_(torch.randn(blocks[0].x.numel(), generator=torch.Generator("cuda").manual_seed(seed), device="cuda").to(torch.bfloat16))
+        graph.replay()
+        C.convbn_check()
+        for k, b in enumerate(blocks):
+            f = lambda t: t.float().cpu().numpy().astype(np.float64)
+            t = dict(x=f(b.x).reshape(7, 28, 28, -1), w=f(b.w).reshape(b.spec.c_out, -1), b=None, gamma=f(b.gamma), beta=f(b.beta), mu_hat=f(b.mu_hat),
+                     var_hat=f(b.var_hat), add=None)
+            got = {"z": f(b.z).reshape(-1, b.spec.c_out), "w_codes": b.w_codes.cpu().numpy().reshape(b.spec.c_out, -1), "w_scale": f(b.w_scale),
+                   "b_fused": f(b.b_fused)}
+            _check(got, t, "bf16", 1, k < 2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,ci,co", [(9_000_000, 256, 64), (1_100_000, 2048, 64)])
+def test_inputs_of_more_than_two_to_the_31_elements(rows, ci, co):
+    """The last rows by themselves give the same bits: they are the same rows, by the same kernel."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(1)
+    x = torch.empty(rows, ci, dtype=torch.bfloat16, device="cuda")
+    for at in range(0, rows, 500_000):
+        x[at:at + 500_000].normal_(generator=g)
+    pitch, tail = -(-ci // 16) * 16, 150_000
+    codes = torch.randint(-127, 128, (co, pitch), dtype=torch.int8, device="cuda", generator=g)
+    scale, shift = torch.rand(co, device="cuda", generator=g), torch.rand(co, device="cuda", generator=g)
+    out = []
+    for part in (x, x[rows - tail:]):
+        d = C.convbn_linear_desc(part.shape[0], ci, co)
+        z = torch.empty(part.shape[0], co, dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(max(256, C.convbn_workspace_bytes(d, C.PHASE_DEPLOY_FWD_QUANT)), dtype=torch.uint8, device="cuda")
+        C.convbn_deploy_fwd_quant(d, part, codes, scale, shift, z, None, False, ws)
+        C.convbn_check()
+        out.append(z[part.shape[0] - tail:].clone())
+    assert torch.equal(out[0], out[1]) and bool(out[0].float().abs().sum() > 0)
