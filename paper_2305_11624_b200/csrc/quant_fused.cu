@@ -364,8 +364,12 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     uint8_t *buf = box();
                     if (boxed) {
                         ok = __all_sync(0xffffffffu, mbar_wait_parked(add_bar, add_ph, abort_flag));
+                        if (!ok) {                              // (the copy in flight lands before the block ends)
+                            if (lane == 0) mbar_wait_parked(add_bar, add_ph, nullptr, 200000000ull);
+                            __syncwarp();
+                            break;
+                        }
                         add_ph ^= 1u;
-                        if (!ok) break;
                     }
                     quant_chunk<T, true>(out, buf, boxed, t_row + (uint32_t)c0, scale_s + n0 + c0, shift_s + n0 + c0, xs2, row, n0 + c0,
                                                     cols - c0, lane);
@@ -404,12 +408,15 @@ size_t fused_smem(const QuantFused &g, size_t slot) {
 
 }  // namespace
 
+// Strides that leave pixels out; otherwise rows of X are side by side, whatever the strides.
+static bool skips_pixels(const Problem &pb) { return pb.h_out != pb.h_in || pb.w_out != pb.w_in; }
+
 // Rows enough for every SM, short ones that start on 16-byte boundaries, and not too many channels for two accumulators to drain.  This
 // kernel and the two of quant_gemm.cu, us: 100352 rows 64 -> 256 18.8 and 25.9, 256 -> 64 19.5 and 28.1, 128 -> 128 14.7 and 22.4,
 // 256 -> 1024 75.3 and 79.1, 64 -> 2048 143 and 123; 19200 rows 64 -> 256 7.8 and 9.6, 256 -> 64 8.3 and 8.7; an earlier form of it
 // 512 -> 1024 122.9 and 100.8, and below a unit per SM, 6272 rows 256 -> 64, 7.2 and 6.1: a warp per row beats sixteen rows a warp.
 bool quant_fused_eligible(const Problem &pb, int elem_bytes) {
-    const bool beside = pb.stride_h == 1 && pb.stride_w == 1;            // (otherwise im2col boxes of 64 channels)
+    const bool beside = !skips_pixels(pb);                               // (otherwise im2col boxes of 64 channels)
     return pb.c_in <= 256 && pb.c_in % 8 == 0 && (size_t)pb.c_in * elem_bytes % 16 == 0 && pb.c_out <= 1024 &&
            (beside || (pb.c_in % 64 == 0 && pb.stride_h <= 8 && pb.stride_w <= 8)) && pb.p >= (long long)kQRows * device_sm_count();
 }
@@ -417,7 +424,7 @@ bool quant_fused_eligible(const Problem &pb, int elem_bytes) {
 RowMap quant_row_map(const Problem &pb) {
     RowMap r;
     r.step = pb.c_in;
-    r.strided = pb.stride_h != 1 || pb.stride_w != 1;
+    r.strided = skips_pixels(pb);
     r.pixel = (long long)pb.stride_w * pb.c_in;
     r.image = (long long)pb.h_in * pb.w_in * pb.c_in;
     r.line = (long long)pb.stride_h * pb.w_in * pb.c_in;
@@ -430,7 +437,7 @@ cudaError_t launch_quant_fused(const Problem &pb, int dtype, const void *x, cons
                                const void *add, int relu, void *z, cudaStream_t st) {
     const int es = dtype == CONVBN_F32 ? 4 : 2, sms = device_sm_count();
     QuantFused g;
-    g.strided = pb.stride_h != 1 || pb.stride_w != 1;
+    g.strided = skips_pixels(pb);
     g.stride_h = pb.stride_h; g.stride_w = pb.stride_w;
     g.by_w = FastDiv((uint32_t)pb.w_out); g.by_h = FastDiv((uint32_t)pb.h_out);
     g.boxes = (pb.c_in * es + 127) / 128;

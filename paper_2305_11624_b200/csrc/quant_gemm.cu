@@ -203,8 +203,12 @@ __global__ void __launch_bounds__(kGThreads) quant_gemm_kernel(const __grid_cons
             for (int c0 = 0; ok && c0 < cols; c0 += CH) {
                 if (boxed) {
                     ok = __all_sync(0xffffffffu, mbar_wait_bounded(add_bar, add_ph, abort_flag));
+                    if (!ok) {                              // (the copy in flight lands before the block ends)
+                        if (lane == 0) mbar_wait_bounded(add_bar, add_ph, nullptr, 200000000ull);
+                        __syncwarp();
+                        break;
+                    }
                     add_ph ^= 1u;
-                    if (!ok) break;
                 }
                 quant_chunk<T, false>(out, buf, boxed, t_row + (uint32_t)c0, scale_s + c0, shift_s + c0, xs2, row0 + lane, n0 + c0, cols - c0, lane);
                 if (c0 + CH >= cols) {

@@ -164,6 +164,19 @@ def test_strided_shortcuts(size, stride):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,ci", [(40, 64), (20000, 64), (20000, 256), (3000, 512)])
+def test_strides_that_leave_no_pixel_out(rows, ci, dtype):
+    """One pixel per image, or one line of them and a stride across lines: the rows of X are side by side all the same."""
+    t = _draw(rows, ci, 1, 1, 64, dtype, 1, True, True)
+    _check(_run(t, _desc(rows, ci, 1, 1, 64, dtype, 2), dtype, True), t, dtype, 1, True)
+    if dtype != "f32":
+        t["x"] = t["x"].reshape(rows // 20, 1, 20, ci)
+        desc = C.Desc.make(rows // 20, ci, 1, 20, 64, 1, 1, 9, 1, dtype=C.BF16, layout=C.NHWC)
+        _check(_run(t, desc, dtype, True), t, dtype, 1, True)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows", [3, 200])
 def test_rows_and_channels_that_are_zero_tiny_infinite_or_not_numbers(rows):
     t = _draw(rows, 128, 1, 1, 64, "bf16", 1, True, False)
