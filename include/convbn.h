@@ -211,8 +211,8 @@ int convbn_tune_bwd_weight_noalloc(const convbn_desc *desc, const void *dz, cons
  *   code   x 2^-e rounded to the nearest integer (ties to even), at most 127 in magnitude, and 1 or -1 where that is 0
  *          but x is not: x > 0 exactly where code > 0
  * A group that holds an infinity or a NaN: step byte 255, codes 0; all of it is restored as NaN.
- * The largest error is half a step, 2^-8 of the group's largest magnitude at most 2^-7 (one step for magnitudes below half
- * a step, and where e is held at a bound).
+ * An element is off by half a step at most, which is between 2^-8 and 2^-7 of the group's largest magnitude; a magnitude below
+ * half a step is off by less than one step (it stands for a whole one), and where e is held at a bound the step is that bound's.
  * convbn_unpack restores the values, without rounding, in any of the three types that they fit.
  * All pointers device, 16-byte aligned, no overlap.  A count of 0 is a no-op that looks at no pointer.  CONVBN_EINVAL for a
  * count below 0 or above 2^40, an unknown dtype or (count > 0) a NULL pointer; CONVBN_EALIGN; CONVBN_ECUDA. */
@@ -417,7 +417,8 @@ const char *convbn_status_string(int status);
  * "direct" (the plain-ALU kernels, those of small fp32 layers among them), "umma", "umma-strip", "umma-strided",
  * "umma-subpixel", "umma-stem", "stem-mma", "depthwise", "grouped-mma", "grouped-umma", and for
  * CONVBN_PHASE_TUNE_BWD "umma-fused-bwd" (the 1x1 kernel that reads dZ once) or "two-calls" (everything else, whatever
- * the number of launches).
+ * the number of launches); CONVBN_PHASE_TUNE_BWD_PACKED "umma-fused-bwd" (that kernel from codes), "umma" (the weight gradient
+ * restores X on its way) or "unpack" (X restored into the workspace first); CONVBN_PHASE_DEPLOY_FWD_QUANT "umma" or "mma" (few rows).
  * Static string, never NULL. */
 const char *convbn_last_kernel(int phase);
 

@@ -7,6 +7,8 @@
 // into the swizzled 16-bit boxes that the weight-gradient MMAs read (code * step, exact).  The same boxes are the mask of dX: the
 // epilogue reads them as matrix fragments beside its accumulator.  Its boxes of the addend arrive by TMA where the results will
 // leave from.  Warps: 0 dZ by TMA, 1 MMA issuer and owner of tensor memory, 2-9 epilogue, 10-17 codes to X.
+// Measured (launch to launch, inputs cold, bf16): 256 -> 64 at 56 x 56, N = 256 with addend and mask 197-203 us, 0.87 of the copy
+// bandwidth on the bytes above (the kernel that reads X itself: 275); 64 -> 256 at N = 32 26.4 us (29.4).
 #include "kernels.h"
 #include "mma_sync.cuh"
 #include "pack8.cuh"
@@ -289,8 +291,12 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
                 const uint32_t taddr = tmem_base + buf * (uint32_t)CI + (uint32_t)c0 + lane_sel;
                 if (g.add) {
                     ok = __all_sync(0xffffffffu, mbar_wait_bounded(add_bar, add_ph, abort_flag));
+                    if (!ok) {                          // (the copy in flight lands before the block ends)
+                        if (lane == 0) mbar_wait_bounded(add_bar, add_ph, nullptr, 200000000ull);
+                        __syncwarp();
+                        break;
+                    }
                     add_ph ^= 1u;
-                    if (!ok) break;
                 }
                 auto rows = [&](auto add_tag, auto mask_tag) {
                     constexpr bool ADD = decltype(add_tag)::value, MASK = decltype(mask_tag)::value;

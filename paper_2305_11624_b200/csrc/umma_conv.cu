@@ -607,6 +607,7 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
                     else if (g.post_relu) pack(yes, yes, no);
                     else pack(yes, no, no);
                     if constexpr (POST) {
+                        if (g.mask_codes) fence_proxy_async_smem();      // (words were written where the next box of codes lands)
                         __syncwarp();                          // every lane has read its rows of the boxes
                         if (c0 + 64 < c_hi) fetch_post(mt, nt, c0 + 64); else fetch_from(i + 1);
                     }
