@@ -220,8 +220,8 @@ int convbn_pack(int dtype, const void *x, void *codes, void *steps, long long co
 int convbn_unpack(int dtype, const void *codes, const void *steps, void *out, long long count, void *stream);
 
 /* convbn_tune_bwd_glue with X given as convbn_pack left it (codes and steps of all N C_in H_in W_in elements, in the order
- * of desc.layout): the same values as that call gives for the restored X, but that dX + add may
- * be rounded once instead of twice; relu_mask: dx = 0 where the code is not positive.
+ * of desc.layout): the values of that call for the restored X, but that dX + add may be rounded once instead of twice, and that
+ * the parameter gradients' sums over many pixels are cut into shorter ones; relu_mask: dx = 0 where the code is not positive.
  * Codes and steps belong to the library like X does (begin != 0: until the join).
  * Workspace: convbn_workspace_bytes(desc, CONVBN_PHASE_TUNE_BWD_PACKED).  Errors as for convbn_tune_bwd_glue. */
 int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *codes, const void *steps, const void *w,

@@ -157,15 +157,18 @@ bool strided_dgrad_ok(const convbn_desc *d, const Problem &pb);
 bool umma_dgrad_shape(const convbn_desc *d, const Problem &pb, UmmaConvShape *s);
 bool packed_path(const convbn_desc *d, const Problem &pb);
 
-// bounded: the tensor-core weight gradient in the slices of a call with a fixed scratch, a stem's without a packed copy of X;
-// sums: what it sums beside.
-Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded, WgradSums sums);
+// The slices of the tensor-core weight gradient: the fastest; those of a call with a fixed scratch (a stem's without a packed copy of
+// X); of at most kExactPixels pixels.
+enum Slicing { kSlicesFastest, kSlicesBounded, kSlicesExact };
+
+// sums: what the weight gradient sums beside.
+Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, Slicing slicing, WgradSums sums);
 
 // The plans of the last layers of this thread: a function of the descriptor, the phase and the device (its SM count).  A
 // backward call asks for five of them, 2 us together.
 struct PlanKey {
     convbn_desc d;
-    int phase, bounded, sums, device, f16;
+    int phase, slicing, sums, device, f16;
 };
 struct PlanSlot { PlanKey key; Plan plan; bool used = false; };
 constexpr int kPlanSlots = 256;
@@ -173,24 +176,24 @@ thread_local PlanSlot *t_plans = nullptr;        // made on first use and kept f
 struct PlanOwner { ~PlanOwner() { delete[] t_plans; t_plans = nullptr; } };
 thread_local PlanOwner t_plan_owner;
 
-Plan make_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded = false, WgradSums sums = WgradSums::kDz) {
+Plan make_plan(const convbn_desc *d, const Problem &pb, int phase, Slicing slicing = kSlicesFastest, WgradSums sums = WgradSums::kDz) {
     PlanKey k;
     memset(&k, 0, sizeof(k));
     k.d.n = d->n; k.d.c_in = d->c_in; k.d.h_in = d->h_in; k.d.w_in = d->w_in; k.d.c_out = d->c_out; k.d.kh = d->kh; k.d.kw = d->kw;
     k.d.stride_h = d->stride_h; k.d.stride_w = d->stride_w; k.d.pad_h = d->pad_h; k.d.pad_w = d->pad_w; k.d.dil_h = d->dil_h;
     k.d.dil_w = d->dil_w; k.d.groups = d->groups; k.d.dtype = d->dtype; k.d.layout = d->layout;      // (no plan depends on eps)
-    k.phase = phase; k.bounded = bounded; k.sums = (int)sums; k.device = current_device_slot(); k.f16 = call_f16();
+    k.phase = phase; k.slicing = slicing; k.sums = (int)sums; k.device = current_device_slot(); k.f16 = call_f16();
     unsigned long long h = 1469598103934665603ull;
     const int *word = (const int *)&k;
     for (size_t i = 0; i < sizeof(k) / sizeof(int); ++i) h = (h ^ (unsigned)word[i]) * 1099511628211ull;
     if (!t_plans) {
         (void)&t_plan_owner;
         t_plans = new (std::nothrow) PlanSlot[kPlanSlots];
-        if (!t_plans) return form_plan(d, pb, phase, bounded, sums);
+        if (!t_plans) return form_plan(d, pb, phase, slicing, sums);
     }
     const unsigned at = (unsigned)(h >> 40) % kPlanSlots;
     if (!t_plans[at].used || memcmp(&t_plans[at].key, &k, sizeof(k)) != 0) {
-        const Plan pl = form_plan(d, pb, phase, bounded, sums);       // (it asks for other plans, which may take this slot)
+        const Plan pl = form_plan(d, pb, phase, slicing, sums);       // (it asks for other plans, which may take this slot)
         t_plans[at].key = k;
         t_plans[at].plan = pl;
         t_plans[at].used = true;
@@ -199,19 +202,23 @@ Plan make_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded 
     return t_plans[at].plan;
 }
 
-Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded, WgradSums sums) {
+Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, Slicing slicing, WgradSums sums) {
     Plan pl;
+    const bool bounded = slicing == kSlicesBounded;
+    auto sliced = [&](WgradSums beside) {
+        return bounded ? umma_wgrad_plan_bounded(pb) : umma_wgrad_plan(pb, beside, slicing == kSlicesExact ? kExactPixels : 0);
+    };
     UmmaConvShape us;
     if (phase == CONVBN_PHASE_TUNE_BWD) {
         if (!fused_bwd_path(d, pb)) {       // the two passes run side by side: each has its own region
-            const Plan a = make_plan(d, pb, CONVBN_PHASE_TUNE_BWD_DATA), b2 = make_plan(d, pb, CONVBN_PHASE_TUNE_BWD_WEIGHT);
+            const Plan a = make_plan(d, pb, CONVBN_PHASE_TUNE_BWD_DATA), b2 = make_plan(d, pb, CONVBN_PHASE_TUNE_BWD_WEIGHT, slicing);
             pl.w_scaled = align_up(a.total, 256);          // here: offset of the backward-weight region
             pl.total = pl.w_scaled + b2.total;
             return pl;
         }
         size_t o = 0;
         auto put = [&](size_t bytes) { size_t r = o; o = align_up(o + bytes, 256); return r; };
-        pl.uw.splits = fused_bwd1x1_ctas(pb);
+        pl.uw.splits = slicing == kSlicesExact ? packed_bwd1x1_ctas(pb) : fused_bwd1x1_ctas(pb);
         pl.bsplits = pl.uw.splits;
         pl.partials = put((size_t)pl.uw.splits * pb.c_out * pb.kdim * sizeof(float));
         pl.bsum = put((size_t)pl.uw.splits * pb.c_out * sizeof(float));
@@ -222,7 +229,7 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded,
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
     if (phase == CONVBN_PHASE_TUNE_BWD_PACKED) {
         if (!fused_bwd_path(d, pb) && !packed_path(d, pb)) pl.unpacked = take((size_t)pb.pin * pb.c_in * elem_size(d->dtype));
-        pl.inner = take(make_plan(d, pb, CONVBN_PHASE_TUNE_BWD).total);
+        pl.inner = take(make_plan(d, pb, CONVBN_PHASE_TUNE_BWD, kSlicesExact).total);
         pl.total = off;
         return pl;
     }
@@ -261,7 +268,7 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded,
     const size_t wbd_bytes = grouped ? (size_t)pb.c_out * pb.kh * pb.kw * 64 * elem_size(d->dtype) : 0;
     pl.grouped_wgrad = grouped;
     if (grouped) {
-        pl.uw = bounded ? umma_wgrad_plan_bounded(pb) : umma_wgrad_plan(pb);
+        pl.uw = sliced(WgradSums::kDz);
         pl.bsplits = pl.uw.splits;
         part_bytes = (size_t)pl.uw.splits * (pb.c_out / 64) * pb.kh * pb.kw * 64 * 64 * sizeof(float);
         const int slots = grouped8_eligible(pb) ? grouped8_wgrad_slots(pb) : 0;
@@ -286,7 +293,7 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, bool bounded,
         }
     }
     if (pl.umma_wgrad) {
-        pl.uw = bounded ? umma_wgrad_plan_bounded(pb) : umma_wgrad_plan(pb, sums);
+        pl.uw = sliced(sums);
         pl.bsplits = pl.uw.splits;
         part_bytes = wrows * pl.uw.splits * sizeof(float);
     }
@@ -603,8 +610,13 @@ int run_conv_dgrad(const convbn_desc *d, const Problem &pb, const void *dz, cons
         bool any_empty = false;
         for (int a = 0; a < pb.stride_h && !any_empty; ++a) any_empty = class_taps(a, pb.pad_h, pb.kh, pb.stride_h).count == 0;
         for (int b2 = 0; b2 < pb.stride_w && !any_empty; ++b2) any_empty = class_taps(b2, pb.pad_w, pb.kw, pb.stride_w).count == 0;
-        if (any_empty &&
-            cudaMemsetAsync(dx, 0, (size_t)pb.pin * pb.c_in * elem_size(d->dtype), st) != cudaSuccess)
+        // positions that no class writes: zero, or, where each sum is rounded once, the (masked) addend
+        const bool filled = any_empty && post && post->add && post->add_once && !post->relu;
+        const size_t dx_bytes = (size_t)pb.pin * pb.c_in * elem_size(d->dtype);
+        if (filled && post->mask)
+            LAUNCH("glue", launch_glue(2, storage_type(d), post->add, post->mask, dx, pb.pin * pb.c_in, st));
+        else if (filled ? post->add != dx && cudaMemcpyAsync(dx, post->add, dx_bytes, cudaMemcpyDeviceToDevice, st) != cudaSuccess
+                        : any_empty && cudaMemsetAsync(dx, 0, dx_bytes, st) != cudaSuccess)
             return CONVBN_ECUDA;
         // one launch writes every class's weight matrix (when the kernel has at most 64 taps)
         const bool merged = pb.kh * pb.kw <= 64;
@@ -629,7 +641,7 @@ int run_conv_dgrad(const convbn_desc *d, const Problem &pb, const void *dz, cons
             LAUNCH("reparam_dgrad", launch_reparam_dgrad_classes(pb, w, scale, w_scratch, where, st));
         }
         // (positions that no class writes keep the zero of the memset: a mask leaves it, an addend would not)
-        const bool here = post && post->any() && !(any_empty && (post->add || post->relu));
+        const bool here = post && post->any() && (filled || !(any_empty && (post->add || post->relu)));
         if (post_done) *post_done = here;
         size_t woff = 0;
         for (int a = 0; a < pb.stride_h && a < pb.h_in; ++a)
@@ -964,7 +976,7 @@ int convbn_tune_bwd_data(const convbn_desc *desc, const void *dz, const void *w,
 
 static int tune_bwd_weight_impl(const convbn_desc *desc, const void *dz, const void *x, const void *w, const float *b,
                                 const float *run_mean, const void *saved, float *dw, float *db, float *dgamma, float *dbeta,
-                                void *workspace, size_t workspace_bytes, void *stream, bool bounded,
+                                void *workspace, size_t workspace_bytes, void *stream, Slicing slicing,
                                 const PackedTensor *packed_x = nullptr) {
     HalfCall half(desc);              // CONVBN_F16: checked here, then run as the 16-bit path with the half flag set
     if (half.status != CONVBN_OK) return half.status;
@@ -979,7 +991,7 @@ static int tune_bwd_weight_impl(const convbn_desc *desc, const void *dz, const v
         !aligned(dw, 16) || !aligned(b, 4) || !aligned(run_mean, 4) || !aligned(db, 4) ||
         !aligned(dgamma, 4) || !aligned(dbeta, 4))
         return CONVBN_EALIGN;
-    const Plan pl = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD_WEIGHT, bounded);
+    const Plan pl = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD_WEIGHT, slicing);
     CK(check_ws(pl, workspace, workspace_bytes));
     cudaStream_t st = (cudaStream_t)stream;
     CK(run_param_grads(desc, pb, pl, dz, x, w, (const float *)saved, b, run_mean, dw, db, dgamma, dbeta,
@@ -990,7 +1002,7 @@ static int tune_bwd_weight_impl(const convbn_desc *desc, const void *dz, const v
 int convbn_tune_bwd_weight(const convbn_desc *desc, const void *dz, const void *x, const void *w, const float *b,
                            const float *run_mean, const void *saved, float *dw, float *db, float *dgamma, float *dbeta,
                            void *workspace, size_t workspace_bytes, void *stream) {
-    return tune_bwd_weight_impl(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, workspace, workspace_bytes, stream, false);
+    return tune_bwd_weight_impl(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, workspace, workspace_bytes, stream, kSlicesFastest);
 }
 
 }  // extern "C"
@@ -1083,7 +1095,7 @@ static int finish_fused_bwd(const Problem &pb, const Plan &pl, const float *part
 static int tune_bwd_impl(const convbn_desc *desc, const void *dz, const void *x, const void *w, const float *b,
                          const float *run_mean, const void *saved, void *dx, float *dw, float *db, float *dgamma,
                          float *dbeta, void *workspace, size_t workspace_bytes, void *stream, bool defer_join,
-                         const PostOp &post = PostOp(), const PackedTensor *packed_x = nullptr) {
+                         const PostOp &post = PostOp(), Slicing slicing = kSlicesFastest, const PackedTensor *packed_x = nullptr) {
     HalfCall half(desc);              // CONVBN_F16: checked here, then run as the 16-bit path with the half flag set
     if (half.status != CONVBN_OK) return half.status;
     desc = half.use;
@@ -1097,13 +1109,13 @@ static int tune_bwd_impl(const convbn_desc *desc, const void *dz, const void *x,
         !aligned(dw, 16) || !aligned(b, 4) || !aligned(run_mean, 4) || !aligned(db, 4) || !aligned(dgamma, 4) ||
         !aligned(dbeta, 4) || !aligned(post.add, 16))
         return CONVBN_EALIGN;
-    const Plan pl = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD);
+    const Plan pl = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD, slicing);
     CK(check_ws(pl, workspace, workspace_bytes));
     if (const int groups = f32_path(desc, pb) ? f32_wgrad_groups(pb, true) : 0; groups > 0) {            // both passes in one launch
         cudaStream_t st = (cudaStream_t)stream;
         float *partials = nullptr, *bsum = nullptr;
         if (groups > 1) {
-            const Plan pw = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD_WEIGHT);
+            const Plan pw = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD_WEIGHT, slicing);
             partials = (float *)at(workspace, pl.w_scaled + pw.partials);
             bsum = (float *)at(workspace, pl.w_scaled + pw.bsum);
         }
@@ -1117,7 +1129,7 @@ static int tune_bwd_impl(const convbn_desc *desc, const void *dz, const void *x,
         const size_t bytes_d = pl.w_scaled, bytes_w = pl.total - pl.w_scaled;
         t_last_kernel[CONVBN_PHASE_TUNE_BWD] = "two-calls";
         auto weight_pass = [&](void *on) -> int {
-            return tune_bwd_weight_impl(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, ws_w, bytes_w, on, false, packed_x);
+            return tune_bwd_weight_impl(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, ws_w, bytes_w, on, slicing, packed_x);
         };
         if (g_prof.on) {                 // per-kernel timing wants one stream, deferred or not
             CK(tune_bwd_data_impl(desc, dz, w, saved, dx, post, workspace, bytes_d, stream));
@@ -1236,7 +1248,7 @@ int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *
     CK(check_ws(pl, workspace, workspace_bytes));
     cudaStream_t st = (cudaStream_t)stream;
     if (fused_bwd_path(desc, pb)) {
-        const Plan pt = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD);
+        const Plan pt = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD, kSlicesExact);
         float *partials = (float *)at(workspace, pl.inner + pt.partials), *bsum = (float *)at(workspace, pl.inner + pt.bsum);
         const float *vec3 = (const float *)saved;
         LAUNCH("packed_bwd", launch_packed_bwd1x1(pb, dz, codes, steps, w, vec3, dx, partials, bsum, add, relu_mask != 0, st));
@@ -1250,7 +1262,7 @@ int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *
         post.add_once = 1;
         post.mask_codes = relu_mask ? codes : nullptr;
         CK(tune_bwd_impl(desc, dz, nullptr, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta, at(workspace, pl.inner),
-                         pl.total - pl.inner, stream, begin != 0, post, &px));
+                         pl.total - pl.inner, stream, begin != 0, post, kSlicesExact, &px));
         t_last_kernel[CONVBN_PHASE_TUNE_BWD_PACKED] = "umma";
         return CONVBN_OK;
     }
@@ -1261,7 +1273,7 @@ int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *
     post.add_once = 1;
     post.mask = relu_mask ? x : nullptr;
     CK(tune_bwd_impl(desc, dz, x, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta, at(workspace, pl.inner), pl.total - pl.inner,
-                     stream, begin != 0, post));
+                     stream, begin != 0, post, kSlicesExact));
     t_last_kernel[CONVBN_PHASE_TUNE_BWD_PACKED] = "unpack";
     return CONVBN_OK;
 }
@@ -1548,7 +1560,7 @@ int tconv_view(const convbn_desc *d, TconvView *v) {
     v->sums = d->kh == d->stride_h && d->kw == d->stride_w && !d->pad_h && !d->pad_w && d->dil_h == 1 &&
                       d->dil_w == 1
                   ? WgradSums::kX : WgradSums::kNone;
-    v->bwd = make_plan(&v->conv, v->pb, CONVBN_PHASE_DEPLOY_BWD, false, v->sums);
+    v->bwd = make_plan(&v->conv, v->pb, CONVBN_PHASE_DEPLOY_BWD, kSlicesFastest, v->sums);
     v->gemm_sums = v->bwd.umma_wgrad && v->sums == WgradSums::kX;
     if (v->gemm_sums) v->bsplits = v->bwd.uw.splits * 2 * d->kh * d->kw;
     v->wcount = (size_t)d->c_in * (d->c_out / d->groups) * d->kh * d->kw;
@@ -1957,13 +1969,13 @@ int convbn_tune_bwd_weight_noalloc(const convbn_desc *desc, const void *dz, cons
     CK(check_pair(desc));
     const size_t room = (size_t)CONVBN_NOALLOC_SCRATCH_BYTES;
     const bool bounded = make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD_WEIGHT).total > room;
-    if (bounded && make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD_WEIGHT, true).total > room) return CONVBN_ECAPACITY;
+    if (bounded && make_plan(desc, pb, CONVBN_PHASE_TUNE_BWD_WEIGHT, kSlicesBounded).total > room) return CONVBN_ECAPACITY;
     void *scratch = nullptr;
     CK(noalloc_scratch_address(&scratch));
     // Same kernels as convbn_tune_bwd_weight, with the built-in array standing in for the caller's
     // workspace, and in the same slices wherever those fit.  Every scratch word those kernels read is written earlier in the same call, so
     // nothing left over from a previous call has to be cleared.
-    return tune_bwd_weight_impl(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, scratch, room, stream, bounded);
+    return tune_bwd_weight_impl(desc, dz, x, w, b, run_mean, saved, dw, db, dgamma, dbeta, scratch, room, stream, bounded ? kSlicesBounded : kSlicesFastest);
 }
 
 const char *convbn_status_string(int status) {

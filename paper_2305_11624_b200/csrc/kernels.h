@@ -145,7 +145,8 @@ struct UmmaWgradPlan {
 };
 enum class WgradSums { kDz, kX, kNone };         // what a call wants the GEMM to sum over the pixels
 bool umma_wgrad_eligible(const Problem &pb);
-UmmaWgradPlan umma_wgrad_plan(const Problem &pb, WgradSums sums = WgradSums::kDz);
+// most: pixels that a slice may have, 0: any number
+UmmaWgradPlan umma_wgrad_plan(const Problem &pb, WgradSums sums = WgradSums::kDz, long long most = 0);
 UmmaWgradPlan umma_wgrad_plan_bounded(const Problem &pb);     // for calls with a fixed scratch
 // partials: [splits][C_out][kdim] fp32 (the layout of the weights; block-diagonal: [splits][block][k][64])
 // bsum    : [splits][C_out] fp32 per-slice sums of dZ over pixels (from a ones row in the GEMM); with kX
@@ -339,8 +340,14 @@ cudaError_t launch_tconv_param_epilogue(int dtype, bool nhwc, int c_out, int tap
 cudaError_t launch_pack(int dtype, const void *x, void *codes, void *steps, long long count, cudaStream_t st);
 cudaError_t launch_unpack(int dtype, const void *codes, const void *steps, void *out, long long count, cudaStream_t st);
 
-// The fused backward of a 1x1 layer (fused_bwd1x1_eligible) from packed X: umma_bwd1x1_packed.cu.  partials, bsum: as for
-// launch_fused_bwd1x1.
+// Pixels that one fp32 accumulator of a weight gradient from packed X adds up, at most.  The tensor core's sums drift with their length:
+// against 64 bits, half values, relative error of domega per 1000 pixels of a slice 0.7 to 1.2e-6 (1024 -> 512 at 63 x 100: N = 4,
+// 2800 pixels 1.9e-6; N = 23, 16100 pixels 2.0e-5).  Slices themselves are added in order by launch_wgrad_rows.
+constexpr long long kExactPixels = 6144;
+
+// The fused backward of a 1x1 layer (fused_bwd1x1_eligible) from packed X: umma_bwd1x1_packed.cu.  partials, bsum: one per CTA
+// (packed_bwd1x1_ctas of them), as for launch_fused_bwd1x1.
+int packed_bwd1x1_ctas(const Problem &pb);
 cudaError_t launch_packed_bwd1x1(const Problem &pb, const void *dz, const void *codes, const void *steps, const void *w, const float *vec3,
                                  void *dx, float *partials, float *bsum, const void *add, bool mask, cudaStream_t st);
 

@@ -412,6 +412,13 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
 
 }  // namespace
 
+// One CTA per SM, or as many rounds of them as keep an accumulator's sums short (1.56 M pixels 64 -> 128: two).
+int packed_bwd1x1_ctas(const Problem &pb) {
+    const long long tiles = (pb.p + 127) / 128, sms = device_sm_count(), most = sms * (kExactPixels / 128);
+    const long long ctas = (tiles + most - 1) / most * sms;
+    return (int)(tiles < ctas ? tiles : ctas);
+}
+
 cudaError_t launch_packed_bwd1x1(const Problem &pb, const void *dz, const void *codes, const void *steps, const void *w, const float *vec3,
                                  void *dx, float *partials, float *bsum, const void *add, bool mask, cudaStream_t st) {
     if (!fused_bwd1x1_eligible(pb)) return cudaErrorInvalidValue;
@@ -438,7 +445,7 @@ cudaError_t launch_packed_bwd1x1(const Problem &pb, const void *dz, const void *
         static PerDevice attr, carve;
         if (cudaError_t e = max_dynamic_smem_once(kernel, 227 * 1024, &attr); e != cudaSuccess) return e;
         prefer_max_shared_once(kernel, &carve);
-        return launch_pdl(kernel, dim3((unsigned)fused_bwd1x1_ctas(pb)), dim3(kPbThreads), smem, st, tdz, tdx, tadd, g,
+        return launch_pdl(kernel, dim3((unsigned)packed_bwd1x1_ctas(pb)), dim3(kPbThreads), smem, st, tdz, tdx, tadd, g,
                           (const __nv_bfloat16 *)w, partials, bsum, err);
     };
     auto typed = [&](auto ci, auto co) { return g.f16 ? go(ci, co, std::true_type()) : go(ci, co, std::false_type()); };

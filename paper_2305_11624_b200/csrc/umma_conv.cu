@@ -62,7 +62,7 @@ struct ConvGemm {
     const __nv_bfloat16 *post_add, *post_mask;      // at the output's offsets
     int post_relu;
     int mask_codes;                                 // kPost: the mask's box is of 8-bit codes (post_mask is not NULL)
-    int add_once;                                   // kPost: the sum with post_add (not NULL, no ReLU) is rounded once
+    int add_once;                                   // kPost, kPostStrided: the sum with post_add (not NULL, no ReLU) is rounded once
 };
 
 struct ConvSmemCtl {
@@ -569,14 +569,14 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
                                 uint32_t o[4];                 // columns 8 i and 8 i + 8: rows 0-7, 8-15 of each
                                 uint32_t a[4] = {0u, 0u, 0u, 0u}, m[4] = {0u, 0u, 0u, 0u};
                                 const uint32_t at16 = (uint32_t)h * 2048u + (((uint32_t)i << 4) ^ frag_chunk);
-                                if constexpr (POST && ADD == 2) ldmatrix_x4(a[0], a[1], a[2], a[3], smem_u32(add_buf) + frag_row + at16);
+                                if constexpr (ADD == 2) ldmatrix_x4(a[0], a[1], a[2], a[3], (POST ? smem_u32(add_buf) + frag_row : frag) + at16);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
                                     const uint32_t *q = &v[h][(i + (e >> 1)) * 4 + (e & 1) * 2];
                                     const f32x2 f = pair(__uint_as_float(q[0]), __uint_as_float(q[1]));
                                     const f32x2 shift = sh[(i & 3) + (e >> 1)];
                                     f32x2 r = DUAL ? fma2(f, one, shift) : mul_add2(f, sc[(i & 3) + (e >> 1)], shift, one);
-                                    if constexpr (POST && ADD == 2) r = fma2(r, one, widen_t<H>(a[e]));
+                                    if constexpr (ADD == 2) r = fma2(r, one, widen_t<H>(a[e]));
                                     o[e] = narrow_t<H>(r);
                                     if constexpr (MODE == kRelu) o[e] = post_pair<H>(o[e], false, 0u, true, false, 0u);
                                 }
@@ -601,7 +601,25 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
                     constexpr std::true_type yes{};
                     constexpr std::false_type no{};
                     constexpr std::integral_constant<int, 2> once{};
-                    if constexpr (!POST) pack(no, no, no);
+                    if constexpr (POST_STRIDED) {
+                        if (g.add_once) {
+                            // the addend of this chunk's pixels, where the results will be
+                            const int ch = lane & 7;
+#pragma unroll 4
+                            for (int it = 0; it < 8; ++it) {
+                                const int rr = it * 4 + (lane >> 3);
+                                const __nv_bfloat16 *dst = (const __nv_bfloat16 *)__shfl_sync(0xffffffffu, (unsigned long long)srow, rr);
+                                uint4 q = make_uint4(0u, 0u, 0u, 0u);
+                                if (dst && c0 + ch * 8 < c_hi) q = *(const uint4 *)(g.post_add + (dst - g.out_strided) + c0 + ch * 8);
+                                *(uint4 *)(buf + rr * 128 + (((ch ^ (rr & 7)) & 7) << 4)) = q;
+                            }
+                            __syncwarp();
+                            pack(once, no, no);
+                        } else {
+                            pack(no, no, no);
+                        }
+                    }
+                    else if constexpr (!POST) pack(no, no, no);
                     else if (g.add_once) { if (g.post_mask) pack(once, no, yes); else pack(once, no, no); }
                     else if (g.post_mask) { if (g.post_add) pack(yes, no, yes); else pack(no, no, yes); }
                     else if (g.post_relu) pack(yes, yes, no);
@@ -615,6 +633,7 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
                         // as below, with the other tensors' values of four pixels requested before the first is used
                         __syncwarp();
                         const int ch = lane & 7;
+                        const bool add_late = g.post_add && !g.add_once;
 #pragma unroll 1
                         for (int i0 = 0; i0 < 8; i0 += 4) {
                             uint4 av[4], mv[4];
@@ -626,15 +645,15 @@ __global__ void __launch_bounds__(MODE == kPlain || MODE == kRelu || MODE == kTa
                                 const bool on = dst && c0 + ch * 8 < c_hi;
                                 at8[k] = on ? dst - g.out_strided + c0 + ch * 8 : -1;
                                 av[k] = mv[k] = make_uint4(0u, 0u, 0u, 0u);
-                                if (on && g.post_add) av[k] = *(const uint4 *)(g.post_add + at8[k]);
+                                if (on && add_late) av[k] = *(const uint4 *)(g.post_add + at8[k]);
                                 if (on && g.post_mask) mv[k] = *(const uint4 *)(g.post_mask + at8[k]);
                             }
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
                                 const int rr = (i0 + k) * 4 + (lane >> 3);
                                 const uint4 q = *(const uint4 *)(buf + rr * 128 + (((ch ^ (rr & 7)) & 7) << 4));
-                                const uint4 o = g.f16 ? post_chunk<true>(q, g.post_add, av[k], g.post_relu, g.post_mask, mv[k])
-                                                      : post_chunk<false>(q, g.post_add, av[k], g.post_relu, g.post_mask, mv[k]);
+                                const uint4 o = g.f16 ? post_chunk<true>(q, add_late, av[k], g.post_relu, g.post_mask, mv[k])
+                                                      : post_chunk<false>(q, add_late, av[k], g.post_relu, g.post_mask, mv[k]);
                                 if (at8[k] >= 0) *(uint4 *)(g.out_strided + at8[k]) = o;
                             }
                         }
@@ -959,7 +978,7 @@ cudaError_t launch_umma_conv(const UmmaConvShape &s, const void *act, const void
     g.post_add = with_post ? (const __nv_bfloat16 *)post->add : nullptr;
     g.post_mask = with_post ? (const __nv_bfloat16 *)(post->mask_codes ? post->mask_codes : post->mask) : nullptr;
     g.mask_codes = with_post && post->mask_codes;
-    g.add_once = with_post && post->add && post->add_once && !post->relu && !s.out_sw;
+    g.add_once = with_post && post->add && post->add_once && !post->relu;
     if (g.mask_codes && (s.out_sw || s.cn % 64)) return cudaErrorInvalidValue;
     g.post_relu = with_post ? post->relu : 0;
     g.tap_c = s.tap_c; g.tap_kw = s.tap_kw; g.tap_sh = s.tap_sh; g.tap_sw = s.tap_sw;

@@ -419,17 +419,20 @@ static long long wgrad_tiles(const Problem &pb, int bn, bool ones_slice) {
 
 // The slice count minimises  rounds over the resident slots x (pixels per slice + a fixed cost per
 // CTA, in pixels) + a small cost per slice for the epilogue that adds the slices up (four pixels, set when a block added a whole
-// channel); a grid a few CTAs larger than the slots would otherwise run a second, nearly empty round.
-static UmmaWgradPlan wgrad_slices(const Problem &pb, long long tiles, long long slots) {
+// channel); a grid a few CTAs larger than the slots would otherwise run a second, nearly empty round.  most: pixels that a slice may
+// have (0: any).
+static UmmaWgradPlan wgrad_slices(const Problem &pb, long long tiles, long long slots, long long most = 0) {
     UmmaWgradPlan pl;
     const long long max_splits = (pb.p + 4 * kWP - 1) / (4 * kWP);     // at least 256 pixels per slice
-    long long splits = 1;
+    long long least = most ? (pb.p + most - 1) / most : 1;
+    if (least > 32768) least = 32768;                                   // (a grid's extent)
+    long long splits = least;
     double best_cost = -1.0;
-    for (long long sp = 1; sp <= max_splits; ++sp) {
+    for (long long sp = least; sp <= max_splits; ++sp) {
         const long long rounds = (tiles * sp + slots - 1) / slots;
         const double cost = (double)rounds * ((double)pb.p / (double)sp + 384.0) + 4.0 * (double)sp;
         if (best_cost < 0 || cost < best_cost) { best_cost = cost; splits = sp; }
-        if (tiles * sp > 4 * slots) break;
+        if (tiles * sp > 4 * slots && (!most || 2 * sp > 3 * least)) break;
     }
     long long per = (pb.p + splits - 1) / splits;
     per = (per + kWP - 1) / kWP * kWP;
@@ -438,7 +441,7 @@ static UmmaWgradPlan wgrad_slices(const Problem &pb, long long tiles, long long 
     return pl;
 }
 
-UmmaWgradPlan umma_wgrad_plan(const Problem &pb, WgradSums sums) {
+UmmaWgradPlan umma_wgrad_plan(const Problem &pb, WgradSums sums, long long most) {
     // Resident CTAs: two per SM (the stage rings are sized for it, launch_w): one's partial tile leaves while the other
     // multiplies.  A deeper ring for one CTA gains nothing.
     // Few tiles mean many slices, and where those are short the partial tensors weigh more than what a second CTA hides: up to
@@ -448,7 +451,7 @@ UmmaWgradPlan umma_wgrad_plan(const Problem &pb, WgradSums sums) {
     // arrive pixel by pixel and a second CTA hides that (29173 rows, 1024 -> 64: 44.5 and 27.4 us; 2 x 2 about even; from
     // 4 x 4 on one CTA is the faster).
     const long long tiles = wgrad_tiles(pb, pb.groups > 1 ? 64 : wgrad_bn(pb), sums == WgradSums::kDz), sms = device_sm_count();
-    return wgrad_slices(pb, tiles, sms * (tiles <= 24 && pb.p * tiles <= 2048 * sms && pb.w_out >= 4 ? 1 : 2));
+    return wgrad_slices(pb, tiles, sms * (tiles <= 24 && pb.p * tiles <= 2048 * sms && pb.w_out >= 4 ? 1 : 2), most);
 }
 
 // The slices of a call whose scratch is bounded, where the plan above wants more than there is: 256 columns count as one tile

@@ -69,6 +69,13 @@ def test_packed_backward_refusals():
     assert status(desc=C.Desc.make(0, 64, 8, 8, 64, 1, 1)) == C.EINVAL
 
 
+def test_room_for_slices_that_keep_sums_short():
+    """A weight gradient's fp32 accumulators add up 6144 pixels at most: a partial tensor for each slice of so many."""
+    size = lambda rows, ci, co: C.convbn_workspace_bytes(C.convbn_linear_desc(rows, ci, co), C.PHASE_TUNE_BWD_PACKED)
+    for rows, ci, co in ((100000, 1024, 512), (144900, 1024, 512), (1560000, 64, 128), (1200000, 256, 64)):
+        assert size(rows, ci, co) >= -(-rows // 6144) * ci * co * 4, (rows, ci, co)
+
+
 # ---- packing on the device ------------------------------------------------------------------------------------------
 def _values(count, dtype, seed):
     """Every kind of group: ordinary, all zero, one value, values at a tie, the type's largest and smallest, infinities, NaN."""
@@ -400,3 +407,66 @@ def test_a_packed_backward_pass_of_more_than_two_to_the_31_elements():
         assert bool((dbeta == n // 2).all())
         out.append(dx[n - tail:].clone())
     assert torch.equal(out[0], out[1]) and bool((out[0][codes[rows - tail:] <= 0] == 0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,ci,co", [(144900, 1024, 512), (100000, 512, 1024), (1560000, 64, 128)])
+def test_sums_over_many_pixels(rows, ci, co, dtype):
+    """Against 64 bits.  A slice is at most 6144 pixels, 384 additions of 16 products to an fp32 accumulator.  An addition that cuts what
+    does not fit is off by half a last place on average, 2^-24 of the sum so far or less, always towards zero; sums of random signs have
+    2/3 of their last size on average, which gives 384 2/3 2^-24 = 1.5e-5 of a slice, 2^-24 for each of the few sums over slices.
+    Products are exact (8 or 11 bits by 7)."""
+    import torch
+    kind, td = (C.BF16, torch.bfloat16) if dtype == "bf16" else (C.F16, torch.float16)
+    g = torch.Generator("cuda").manual_seed(3)
+    x = torch.randn(rows, ci, device="cuda", generator=g).to(td)
+    codes, steps = torch.empty(rows, ci, dtype=torch.int8, device="cuda"), torch.empty(rows, ci // 32, dtype=torch.uint8, device="cuda")
+    C.convbn_pack(x, codes, steps)
+    dz, w = torch.randn(rows, co, device="cuda", generator=g).to(td), torch.randn(co, ci, device="cuda", generator=g).to(td)
+    d = C.Desc.make(rows, ci, 1, 1, co, 1, 1, dtype=kind, layout=C.NHWC)
+    mean, saved = torch.zeros(co, device="cuda"), torch.ones(3 * co, device="cuda")
+    dw, dgamma, dbeta = torch.empty(co, ci, device="cuda"), torch.empty(co, device="cuda"), torch.empty(co, device="cuda")
+    ws = torch.empty(C.convbn_workspace_bytes(d, C.PHASE_TUNE_BWD_PACKED), dtype=torch.uint8, device="cuda")
+    C.convbn_tune_bwd_packed(d, dz, codes, steps, w, None, mean, saved, x, dw, None, dgamma, dbeta, None, False, False, ws)
+    C.convbn_check()
+    exact, total = torch.zeros(co, ci, dtype=torch.float64, device="cuda"), torch.zeros(co, dtype=torch.float64, device="cuda")
+    for at in range(0, rows, 1 << 17):
+        part = slice(at, at + (1 << 17))
+        step = torch.exp2(steps[part].double() - 127.0).repeat_interleave(32, 1)
+        exact += dz[part].double().t() @ (codes[part].double() * step)
+        total += dz[part].double().sum(0)
+    rel = lambda a, b: float((a.double() - b).norm() / b.norm())
+    bound = 384 * 2 / 3 * 2.0 ** -24 + 2.0 ** -22
+    assert rel(dw, exact) <= bound and rel(dbeta, total) <= bound
+    assert rel(dgamma, (exact * w.double()).sum(1)) <= bound * 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,ci,hw,co,stride,mask", [(3, 128, 15, 256, 2, True), (2, 512, 9, 192, 2, False), (3, 64, 14, 64, 3, True),
+                                                     (4, 512, 12, 128, 1, True), (2, 256, 17, 64, 1, True)])
+def test_an_addend_is_rounded_with_the_sum(n, ci, hw, co, stride, mask, dtype):
+    """Whole numbers whose products add up without rounding in fp32, to more bits than the storage type has: dX is the sum with the
+    addend, rounded, bit for bit."""
+    import torch
+    kind, td = (C.BF16, torch.bfloat16) if dtype == "bf16" else (C.F16, torch.float16)
+    g = torch.Generator("cuda").manual_seed(n + ci)
+    whole = lambda most, *shape: torch.randint(-most, most + 1, shape, device="cuda", generator=g).float()
+    ho = (hw - 1) // stride + 1
+    x, dz, w = whole(7, n, hw, hw, ci), whole(9, n, ho, ho, co), whole(9, co, ci)
+    add = (whole(4000, n, hw, hw, ci) / 3).to(td)
+    codes, steps = torch.empty(x.numel(), dtype=torch.int8, device="cuda"), torch.empty(x.numel() // 32, dtype=torch.uint8, device="cuda")
+    C.convbn_pack(x.to(td), codes, steps)
+    d = C.Desc.make(n, ci, hw, hw, co, 1, 1, stride, stride, dtype=kind, layout=C.NHWC)
+    dx = torch.empty(n, hw, hw, ci, dtype=td, device="cuda")
+    dw, dgamma, dbeta = torch.empty(co, ci, device="cuda"), torch.empty(co, device="cuda"), torch.empty(co, device="cuda")
+    ws = torch.empty(max(256, C.convbn_workspace_bytes(d, C.PHASE_TUNE_BWD_PACKED)), dtype=torch.uint8, device="cuda")
+    C.convbn_tune_bwd_packed(d, dz.to(td), codes, steps, w.to(td), None, torch.zeros(co, device="cuda"), torch.ones(3 * co, device="cuda"),
+                             dx, dw, None, dgamma, dbeta, add, mask, False, ws)
+    C.convbn_check()
+    conv = torch.zeros(n, hw, hw, ci, dtype=torch.float64, device="cuda")
+    conv[:, ::stride, ::stride] = dz.double() @ w.double()
+    want = (conv + add.double()).float().to(td)                       # (to fp32 first, as an fp32 sum is)
+    want = torch.where(x > 0, want, torch.zeros_like(want)).float() if mask else want.float()
+    assert int((dx.float() != want).sum()) == 0
