@@ -142,6 +142,7 @@ cudaError_t launch_reparam_dgrad_class(const Problem &pb, const void *w, const f
 struct UmmaWgradPlan {
     int splits = 1;           // pixel slices = partial tiles
     long long per_split = 0;  // pixels per slice
+    bool segments = false;    // sums of 1024 pixels, added up between them (umma_wgrad.cu)
 };
 enum class WgradSums { kDz, kX, kNone };         // what a call wants the GEMM to sum over the pixels
 bool umma_wgrad_eligible(const Problem &pb);
@@ -342,7 +343,9 @@ cudaError_t launch_unpack(int dtype, const void *codes, const void *steps, void 
 
 // Pixels that one fp32 accumulator of a weight gradient from packed X adds up, at most.  The tensor core's sums drift with their length:
 // against 64 bits, half values, relative error of domega per 1000 pixels of a slice 0.7 to 1.2e-6 (1024 -> 512 at 63 x 100: N = 4,
-// 2800 pixels 1.9e-6; N = 23, 16100 pixels 2.0e-5).  Slices themselves are added in order by launch_wgrad_rows.
+// 2800 pixels 1.9e-6; N = 23, 16100 pixels 2.0e-5), a quarter of that for bf16.  Slices themselves are added in order by
+// launch_wgrad_rows.  With half values the accumulators are emptied every 1024 pixels besides (umma_wgrad.cu, SEG;
+// umma_bwd1x1_packed.cu): 5e-7, as fp32 additions that round have it.
 constexpr long long kExactPixels = 6144;
 
 // The fused backward of a 1x1 layer (fused_bwd1x1_eligible) from packed X: umma_bwd1x1_packed.cu.  partials, bsum: one per CTA

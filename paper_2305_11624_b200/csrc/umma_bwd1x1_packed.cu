@@ -24,6 +24,10 @@ namespace {
 constexpr int kPbThreads = 576;
 constexpr uint32_t kPbBox = 128 * 128;        // [128 pixels][64 channels] of 16 bits
 constexpr uint32_t kPbOut = 32 * 128;         // an epilogue warp's box: [32 pixels][64 channels]
+// Half values: the accumulators of domega and sum dZ are added to the CTA's partial, which stays in L2, every eight tiles, by additions
+// that round (those of the tensor core cut off, and drift: see kExactPixels).  256 -> 64 at 56 x 56, N = 256 204 -> 214 us, 64 -> 128 at
+// 100 x 65, N = 240 129 -> 144; read back and stored instead 245 and 332, by as many more CTAs 251 and 230.
+constexpr uint32_t kPbSegment = 8;
 
 struct PackedBwd {
     long long p;
@@ -35,7 +39,7 @@ struct PackedBwd {
 };
 
 struct PbCtl {
-    uint64_t dz_full[2], dz_empty[2], x_full[2], x_empty[2], dx_full[2], dx_empty[2], add_full[8], acc_done;
+    uint64_t dz_full[2], dz_empty[2], x_full[2], x_empty[2], dx_full[2], dx_empty[2], add_full[8], seg_full, seg_empty, acc_done;
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -83,6 +87,7 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
             mbar_init(&ctl->dx_full[s], 1); mbar_init(&ctl->dx_empty[s], S::kDxBufs == 2 ? 4 : 8);
         }
         for (int s = 0; s < 8; ++s) mbar_init(&ctl->add_full[s], 1);
+        mbar_init(&ctl->seg_full, 1); mbar_init(&ctl->seg_empty, 8);
         mbar_init(&ctl->acc_done, 1);
         ctl->abort_flag = 0;
         fence_barrier_init();
@@ -154,13 +159,15 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
                 }
                 umma_commit(&ctl->dx_full[buf]);
                 // domega' and sum dZ: K = the tile's 128 pixels in steps of 16 (two groups of 8 rows, 2048 bytes)
-                ok = mbar_wait_bounded(&ctl->x_full[s], ph, abort_flag);
+                const bool fresh = H ? i % kPbSegment == 0 : i == 0;
+                ok = mbar_wait_bounded(&ctl->x_full[s], ph, abort_flag) &&
+                     (!fresh || i == 0 || mbar_wait_bounded(&ctl->seg_empty, (i / kPbSegment - 1) & 1u, abort_flag));
                 if (!ok) break;
                 tc_fence_after_sync();
 #pragma unroll 1
                 for (int kt = 0; kt < 8; ++kt) {
                     const uint32_t koff = (uint32_t)kt * 128u;
-                    const bool first = i == 0 && kt == 0;
+                    const bool first = fresh && kt == 0;
 #pragma unroll
                     for (int mb = 0; mb < S::kMBlocks; ++mb) {
                         const uint32_t d = tmem_base + (uint32_t)(S::kDwCol0 + mb * S::kNarrow);
@@ -174,6 +181,7 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
                 }
                 umma_commit(&ctl->dz_empty[s]);
                 umma_commit(&ctl->x_empty[s]);
+                if (H && (i + 1) % kPbSegment == 0 && t + 1 < tile_hi) umma_commit(&ctl->seg_full);
             }
             if (ok) umma_commit(&ctl->acc_done);
             else give_up();
@@ -259,8 +267,85 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
         const uint32_t frag_row = (uint32_t)((lane & 7) + (lane & 8)) * 128u, frag_chunk = (uint32_t)(((lane >> 4) ^ (lane & 7)) << 4);
         bool ok = true;
         uint32_t i = 0, turn = 0, add_ph = 0;
-        for (int t = tile_lo; t < tile_hi && ok; ++t, ++i) {
+        for (int t = tile_lo; t <= tile_hi && ok; ++t, ++i) {
             const uint32_t s = i & 1u, buf = S::kDxBufs == 2 ? s : 0u, use = S::kDxBufs == 2 ? (i >> 1) : i;
+            const bool last = t == tile_hi;
+            if (last || (H && i && i % kPbSegment == 0)) {
+                // ---- the CTA's partial of domega' as part[cta][co][ci] and its row of sums of dZ: 128 contiguous bytes per store, of later
+                // segments added to what is there.  Both groups, before either waits for this tile: the issuer goes on when all eight
+                // warps are through ----
+                const bool more = H && i > kPbSegment;
+                ok = __all_sync(0xffffffffu, last ? mbar_wait_bounded(&ctl->acc_done, 0, abort_flag)
+                                                  : mbar_wait_bounded(&ctl->seg_full, (i / kPbSegment - 1) & 1u, abort_flag));
+                if (last) pdl_launch_dependents();                     // (see umma_wgrad.cu)
+                if (!ok) break;
+                if (lane == 0) tma_store_wait_read<0>();               // (the boxes are free)
+                __syncwarp();
+                tc_fence_after_sync();
+                float *part = partials + (size_t)blockIdx.x * CI * CO;
+                // (added in L2, without a reading: each number has one thread, so the order is that of the segments)
+                auto put = [&](float *at, uint32_t bits) {
+                    if (more) atomicAdd(at, __uint_as_float(bits));
+                    else *at = __uint_as_float(bits);
+                };
+                if (S::kWideIn) {
+                    // accumulator row = ci (M block mb, lane), columns = co
+                    for (int mb = egroup; mb < S::kMBlocks; mb += 2) {
+                        float *ocol = part + mb * 128 + quarter * 32 + lane;
+#pragma unroll 1
+                        for (int c0 = 0; c0 < CO; c0 += 32) {
+                            uint32_t v[32];
+                            tmem_ld_32x32(tmem_base + (uint32_t)(S::kDwCol0 + mb * CO + c0) + lane_sel, v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) put(ocol + (size_t)(c0 + j) * CI, v[j]);
+                        }
+                    }
+                    if (warp == 2) {                               // every row of the sums tile is sum dZ: take this warp's first
+                        float *brow = bsum + (size_t)blockIdx.x * CO;
+#pragma unroll 1
+                        for (int c0 = 0; c0 < CO; c0 += 32) {
+                            uint32_t v[32];
+                            tmem_ld_32x32(tmem_base + (uint32_t)(S::kSumCol0 + c0) + lane_sel, v);
+                            tmem_ld_wait();
+                            if (lane == 0) {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) put(brow + c0 + j, v[j]);
+                            }
+                        }
+                    }
+                } else {
+                    // accumulator row = co, columns = ci (64): 32 x 32 blocks are transposed in the warp's box (word (row, column) at row
+                    // 32 + (column ^ row): no bank conflicts either way), then lane = ci
+                    uint32_t *tr = (uint32_t *)boxes;
+                    for (int mb = egroup; mb < S::kMBlocks; mb += 2) {
+                        const int co0 = mb * 128 + quarter * 32;
+#pragma unroll 1
+                        for (int c0 = 0; c0 < CI; c0 += 32) {
+                            uint32_t v[32];
+                            int here = lane;
+                            asm volatile("" : "+r"(here));    // (64 addresses that else are kept through all tiles)
+                            tmem_ld_32x32(tmem_base + (uint32_t)(S::kDwCol0 + mb * CI + c0) + lane_sel, v);
+                            tmem_ld_wait();
+                            __syncwarp();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) tr[here * 32 + (j ^ here)] = v[j];
+                            __syncwarp();
+#pragma unroll 8
+                            for (int r = 0; r < 32; ++r) put(part + (size_t)(co0 + r) * CI + c0 + lane, tr[r * 32 + (here ^ r)]);
+                        }
+                        uint32_t sv[16];
+                        tmem_ld_32x16(tmem_base + (uint32_t)(S::kSumCol0 + mb * 16) + lane_sel, sv);
+                        tmem_ld_wait();
+                        put(bsum + (size_t)blockIdx.x * CO + co0 + lane, sv[0]);
+                    }
+                }
+                if (last) break;
+                tc_fence_before_sync();
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl->seg_empty);
+            }
             if (S::kDxBufs == 2 && (int)buf != egroup) continue;        // the two groups take alternate tiles ...
             // ... or halve the columns of the one accumulator
             const int c_lo = S::kDxBufs == 2 ? 0 : egroup * (CI / 2), c_hi = S::kDxBufs == 2 ? CI : c_lo + CI / 2;
@@ -345,64 +430,6 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
             }
         }
         if (lane == 0) tma_store_wait_all<0>();
-        // ---- the CTA's partial of domega' as part[cta][co][ci] and its row of sums of dZ: 128 contiguous bytes per store ----
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->acc_done, 0, abort_flag));
-        pdl_launch_dependents();                               // (see umma_wgrad.cu)
-        if (ok) {
-            tc_fence_after_sync();
-            float *part = partials + (size_t)blockIdx.x * CI * CO;
-            if (S::kWideIn) {
-                // accumulator row = ci (M block mb, lane), columns = co
-                for (int mb = egroup; mb < S::kMBlocks; mb += 2) {
-                    float *ocol = part + mb * 128 + quarter * 32 + lane;
-#pragma unroll 1
-                    for (int c0 = 0; c0 < CO; c0 += 32) {
-                        uint32_t v[32];
-                        tmem_ld_32x32(tmem_base + (uint32_t)(S::kDwCol0 + mb * CO + c0) + lane_sel, v);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) ocol[(size_t)(c0 + j) * CI] = __uint_as_float(v[j]);
-                    }
-                }
-                if (warp == 2) {                               // every row of the sums tile is sum dZ: take this warp's first
-                    float *brow = bsum + (size_t)blockIdx.x * CO;
-#pragma unroll 1
-                    for (int c0 = 0; c0 < CO; c0 += 32) {
-                        uint32_t v[32];
-                        tmem_ld_32x32(tmem_base + (uint32_t)(S::kSumCol0 + c0) + lane_sel, v);
-                        tmem_ld_wait();
-                        if (lane == 0) {
-#pragma unroll
-                            for (int j = 0; j < 32; j += 4) *(uint4 *)(brow + c0 + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                        }
-                    }
-                }
-            } else {
-                // accumulator row = co, columns = ci (64): 32 x 32 blocks are transposed in the warp's box (word (row, column) at row
-                // 32 + (column ^ row): no bank conflicts either way), then lane = ci
-                uint32_t *tr = (uint32_t *)boxes;
-                for (int mb = egroup; mb < S::kMBlocks; mb += 2) {
-                    const int co0 = mb * 128 + quarter * 32;
-#pragma unroll 1
-                    for (int c0 = 0; c0 < CI; c0 += 32) {
-                        uint32_t v[32];
-                        tmem_ld_32x32(tmem_base + (uint32_t)(S::kDwCol0 + mb * CI + c0) + lane_sel, v);
-                        tmem_ld_wait();
-                        __syncwarp();
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) tr[lane * 32 + (j ^ lane)] = v[j];
-                        __syncwarp();
-#pragma unroll
-                        for (int r = 0; r < 32; ++r)
-                            part[(size_t)(co0 + r) * CI + c0 + lane] = __uint_as_float(tr[r * 32 + (lane ^ r)]);
-                    }
-                    uint32_t sv[16];
-                    tmem_ld_32x16(tmem_base + (uint32_t)(S::kSumCol0 + mb * 16) + lane_sel, sv);
-                    tmem_ld_wait();
-                    bsum[(size_t)blockIdx.x * CO + co0 + lane] = __uint_as_float(sv[0]);
-                }
-            }
-        }
         if (!ok && lane == 0) give_up();
     }
     tc_fence_before_sync();

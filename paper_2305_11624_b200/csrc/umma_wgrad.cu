@@ -19,6 +19,7 @@ using namespace ptx;
 
 constexpr int kWM = 128;          // k rows per tile (two 64-channel slices)
 constexpr int kWP = 64;           // pixels per stage (reduction depth per stage)
+constexpr int kWSegment = 16;            // blocks of kWP pixels that an accumulator adds up (SEG)
 constexpr int kWUmmaK = 16;
 constexpr int kWMaxStages = 8;
 constexpr int kWThreads = 224;    // X loads, MMA, 4 epilogue warps, dZ loads
@@ -59,6 +60,7 @@ struct WgradSmemCtl {
     uint32_t tmem_base;
     int abort_flag;
     uint64_t raw[kWMaxStages];       // PACKED: the codes of a stage have landed
+    uint64_t seg_full, seg_empty;    // SEG
 };
 
 // X_SUMS: g.sums is kSumX.
@@ -66,7 +68,11 @@ struct WgradSmemCtl {
 // pixel; the epilogue warps, two per slice, take them into registers, meet, and write the 16-bit values (code * step, exact) over the
 // whole of it while earlier stages are multiplied.  (Which layers: packed_path in
 // convbn_api.cu.)
-template <int BN, bool X_SUMS, bool PACKED>
+// SEG: the accumulator is emptied every kWSegment blocks of pixels into a second one, by additions that round (those of the tensor core cut
+// off, and drift: see kExactPixels).  The epilogue warps do it, 32 columns at a time, while the CTA beside this one multiplies.  Whole
+// backward calls from packed X, bf16 (without) and half (with): 512 -> 128 at 28 x 28, N = 64 54.2 and 54.1 us, 1024 -> 512 at 63 x 100,
+// N = 23 414 and 453, 100000 rows 2048 -> 1024 1486 and 1513.
+template <int BN, bool X_SUMS, bool PACKED, bool SEG>
 __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_constant__ CUtensorMap tm_x,
                                                               const __grid_constant__ CUtensorMap tm_dz,
                                                               const WgradGemm g, float *__restrict__ partials,
@@ -118,12 +124,13 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
             mbar_init(&ctl->empty[s], adds ? 5 : 1);
             if constexpr (PACKED) mbar_init(&ctl->raw[s], 1);
         }
+        if constexpr (SEG) { mbar_init(&ctl->seg_full, 1); mbar_init(&ctl->seg_empty, 4); }
         mbar_init(&ctl->tmem_full, 1);
         ctl->abort_flag = 0;
         fence_barrier_init();
     }
     if (warp == 1) {
-        tmem_alloc(&ctl->tmem_base, BN);
+        tmem_alloc(&ctl->tmem_base, SEG ? 2 * BN : BN);
         tmem_relinquish();
     }
     pdl_wait();                 // global memory only after every earlier kernel has finished
@@ -232,6 +239,17 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
             ph = 0;
 #pragma unroll 4
             for (int kb = 0; kb < num_kb; ++kb) {
+                if constexpr (SEG)
+                    if (kb && kb % kWSegment == 0) {
+                        umma_commit(&ctl->seg_full);
+                        if (!mbar_wait_bounded(&ctl->seg_empty, (uint32_t)(kb / kWSegment - 1) & 1u, abort_flag)) {
+                            atomicOr(err, ERRW_TIMEOUT);
+                            ctl->abort_flag = 1;
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after_sync();
+                    }
                 if (!free && !mbar_wait_bounded(full0 + sb, ph, abort_flag)) {
                     atomicOr(err, ERRW_TIMEOUT);
                     ctl->abort_flag = 1;
@@ -244,7 +262,7 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
                 sb += 8; a_lo += kStageBytes >> 4;
                 if (sb == sb_end) { sb = 0; a_lo = tiles_lo; ph ^= 1u; }
                 free = mbar_test_wait(full0 + sb, ph);
-                umma_bf16_ss_sel(tmem_base, a0, hi, b0, hi, idesc, (uint32_t)kb);
+                umma_bf16_ss_sel(tmem_base, a0, hi, b0, hi, idesc, (uint32_t)(SEG ? kb % kWSegment : kb));
 #pragma unroll
                 for (int k = 1; k < kWP / kWUmmaK; ++k)
                     umma_bf16_ss_halves<true>(tmem_base, a0 + (uint32_t)k * (kWUmmaK * 128 >> 4), hi,
@@ -286,6 +304,34 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
             const int k = k0 + slice * 64 + 2 * lane;
             if (slice < a_chunks) *(float2 *)(bsum + ((size_t)blockIdx.z * 2 + half) * g.kdim + k) = make_float2(lo, hi);
         }
+        // SEG: this warp's rows of the accumulator, added to the second one (of the first segment: copied)
+        int emptied = 0;
+        const int segments = SEG ? (num_kb - 1) / kWSegment : 0;
+        const uint32_t acc_at = tmem_base + ((uint32_t)(quarter * 32) << 16), sum_at = acc_at + BN;
+        auto empty_segment = [&]() {
+            const bool there = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->seg_full, (uint32_t)emptied & 1u, abort_flag));
+            if (!there) { if (lane == 0) { atomicOr(err, ERRW_TIMEOUT); ctl->abort_flag = 1; } }
+            else {
+                tc_fence_after_sync();
+#pragma unroll 1
+                for (int c0 = 0; c0 < BN; c0 += 32) {
+                    uint32_t v[32], sum[32];
+                    tmem_ld_32x32(acc_at + (uint32_t)c0, v);
+                    if (emptied) tmem_ld_32x32(sum_at + (uint32_t)c0, sum);
+                    tmem_ld_wait();
+                    if (emptied) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(sum[j]));
+                    }
+                    tmem_st_32x32(sum_at + (uint32_t)c0, v);
+                }
+                tmem_st_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl->seg_empty);
+            }
+            ++emptied;
+        };
         if constexpr (PACKED) {
             const int slice = quarter >> 1, r = (quarter & 1) * 32 + lane;          // this lane's pixel of a stage
             if (slice < a_chunks) {
@@ -340,12 +386,16 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
                         if (lane == 0) mbar_arrive(full0 + sb2);
                         sb2 += 8; at += kStageBytes;
                         if (sb2 == sb_end) { sb2 = 0; at = 0; ph2 ^= 1u; }
+                        // a segment is emptied when two blocks of the next are ready (the ring has three at least)
+                        if (SEG && kb > kWSegment && kb % kWSegment == 1) empty_segment();
                     }
                 };
                 if (g.f16) restore(std::true_type{}); else restore(std::false_type{});
                 if (!fine && lane == 0) { atomicOr(err, ERRW_TIMEOUT); ctl->abort_flag = 1; }
             }
         }
+        if constexpr (SEG)
+            while (emptied < segments) empty_segment();
         const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->tmem_full, 0, abort_flag));
         if (!ok && lane == 0) { atomicOr(err, ERRW_TIMEOUT); ctl->abort_flag = 1; }
         // The adding kernel is let go only here: its blocks, waiting for this grid, would take the shared memory that the
@@ -365,8 +415,15 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
             for (int c0 = 0; c0 < BN; c0 += 32) {
                 if (n0 + c0 >= g.c_out) break;
                 uint32_t v[32];
-                tmem_ld_32x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0, v);
+                tmem_ld_32x32(acc_at + (uint32_t)c0, v);
                 tmem_ld_wait();
+                if (SEG && segments) {
+                    uint32_t sum[32];
+                    tmem_ld_32x32(sum_at + (uint32_t)c0, sum);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(sum[j]));
+                }
                 if (row_ok && g.rows) {
                     // lanes are consecutive k: each store is 128 contiguous bytes of a weight row
                     float *wrow = partials + ((size_t)blockIdx.z * g.c_out + n0 + c0) * g.kdim + k;
@@ -386,7 +443,7 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 1) tmem_dealloc(tmem_base, BN);
+    if (warp == 1) tmem_dealloc(tmem_base, SEG ? 2 * BN : BN);
 }
 
 bool grouped_bd_eligible(const Problem &pb) {
@@ -451,7 +508,9 @@ UmmaWgradPlan umma_wgrad_plan(const Problem &pb, WgradSums sums, long long most)
     // arrive pixel by pixel and a second CTA hides that (29173 rows, 1024 -> 64: 44.5 and 27.4 us; 2 x 2 about even; from
     // 4 x 4 on one CTA is the faster).
     const long long tiles = wgrad_tiles(pb, pb.groups > 1 ? 64 : wgrad_bn(pb), sums == WgradSums::kDz), sms = device_sm_count();
-    return wgrad_slices(pb, tiles, sms * (tiles <= 24 && pb.p * tiles <= 2048 * sms && pb.w_out >= 4 ? 1 : 2), most);
+    UmmaWgradPlan pl = wgrad_slices(pb, tiles, sms * (tiles <= 24 && pb.p * tiles <= 2048 * sms && pb.w_out >= 4 ? 1 : 2), most);
+    pl.segments = most && call_f16() && sums == WgradSums::kDz && pl.per_split > kWSegment * kWP;
+    return pl;
 }
 
 // The slices of a call whose scratch is bounded, where the plan above wants more than there is: 256 columns count as one tile
@@ -463,7 +522,7 @@ UmmaWgradPlan umma_wgrad_plan_bounded(const Problem &pb) {
 
 int wgrad_kmajor_rows(const Problem &pb) { return (pb.kdim + 1) / 2; }
 
-template <int BN, bool X_SUMS = false, bool PACKED = false>
+template <int BN, bool X_SUMS = false, bool PACKED = false, bool SEG = false>
 static cudaError_t launch_w(const CUtensorMap &tx, const CUtensorMap &tdz, WgradGemm g, const UmmaWgradPlan &pl,
                             const Problem &pb, float *partials, float *bsum, int *err, cudaStream_t st,
                             unsigned int *counters = nullptr, int ncounters = 0) {
@@ -474,15 +533,15 @@ static cudaError_t launch_w(const CUtensorMap &tx, const CUtensorMap &tdz, Wgrad
     if (stages > max_kb) stages = (int)max_kb;
     g.stages = stages;
     size_t smem = stages * stage + 1024 + sizeof(WgradSmemCtl);
-    const size_t floor_smem = (size_t)(228 * 1024) / (512 / BN + 1) + 1024;
+    const size_t floor_smem = (size_t)(228 * 1024) / (512 / (SEG ? 2 * BN : BN) + 1) + 1024;
     if (smem < floor_smem) smem = floor_smem;
     static PerDevice attr_done;
-    if (cudaError_t e = max_dynamic_smem_once(umma_wgrad_kernel<BN, X_SUMS, PACKED>, 210 * 1024, &attr_done); e != cudaSuccess) return e;
+    if (cudaError_t e = max_dynamic_smem_once(umma_wgrad_kernel<BN, X_SUMS, PACKED, SEG>, 210 * 1024, &attr_done); e != cudaSuccess) return e;
     static PerDevice carve;
-    prefer_max_shared_once(umma_wgrad_kernel<BN, X_SUMS, PACKED>, &carve);
+    prefer_max_shared_once(umma_wgrad_kernel<BN, X_SUMS, PACKED, SEG>, &carve);
     dim3 grid((unsigned)((g.kdim / 64 + (g.sums == kSumSlice ? 2 : 1)) / 2), (unsigned)((pb.c_out + BN - 1) / BN),
               (unsigned)pl.splits);
-    return launch_pdl(umma_wgrad_kernel<BN, X_SUMS, PACKED>, grid, dim3(kWThreads), smem, st, tx, tdz, g, partials, bsum, counters,
+    return launch_pdl(umma_wgrad_kernel<BN, X_SUMS, PACKED, SEG>, grid, dim3(kWThreads), smem, st, tx, tdz, g, partials, bsum, counters,
                       ncounters, err);
 }
 
@@ -518,9 +577,13 @@ cudaError_t launch_umma_wgrad(const Problem &pb, const UmmaWgradPlan &pl, const 
     int *err = nullptr;
     cudaError_t e = error_word_address(&err);
     if (e != cudaSuccess) return e;
-    if (packed_x)
-        return bn == 64 ? launch_w<64, false, true>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters)
-                        : launch_w<128, false, true>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters);
+    auto go = [&](auto packed, auto seg) {
+        constexpr bool P = decltype(packed)::value, S = decltype(seg)::value;
+        return bn == 64 ? launch_w<64, false, P, S>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters)
+                        : launch_w<128, false, P, S>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters);
+    };
+    if (pl.segments) return packed_x ? go(std::true_type{}, std::true_type{}) : go(std::false_type{}, std::true_type{});
+    if (packed_x) return go(std::true_type{}, std::false_type{});
     if (g.sums == kSumX)
         return bn == 64 ? launch_w<64, true>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters)
                         : launch_w<128, true>(tx, tdz, g, pl, pb, partials, bsum, err, st, counters, ncounters);
