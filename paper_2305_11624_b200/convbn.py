@@ -399,15 +399,38 @@ def _storage(t) -> int:
     return kind
 
 
+def _packed_room(codes, steps, count, where):
+    """EINVAL unless codes and steps, where they are tensors, have room for `count` elements: the library takes addresses."""
+    for t, name, least in ((codes, "codes", count), (steps, "steps", -(-count // 32))):
+        if t is None or isinstance(t, int):
+            continue
+        if t.element_size() != 1 or t.numel() < least or not t.is_contiguous():
+            _raise(EINVAL, "%s: %s, %d bytes in one piece are needed" % (where, name, least))
+
+
+def _packed_pair(x, codes, steps, where):
+    """The same, and x (`out`) in one piece too, contiguous or channels last, all of them on one GPU."""
+    import torch
+    if not (x.is_contiguous() or (x.dim() == 4 and x.is_contiguous(memory_format=torch.channels_last))):
+        _raise(EINVAL, "%s: a tensor in one piece is needed" % where)
+    _packed_room(codes, steps, x.numel(), where)
+    if not x.is_cuda or any(not (t is None or isinstance(t, int)) and t.device != x.device for t in (codes, steps)):
+        _raise(EINVAL, "%s: tensors of one GPU are needed" % where)
+
+
 def convbn_pack(x, codes, steps, stream=None):
-    """x in 8 bits: a signed code per element, a step byte per 32 consecutive ones."""
-    status = (_native or _calls()).convbn_pack(_storage(x), x, codes, steps, x.numel(), stream)
+    """x in 8 bits: a signed code per element, a step byte per 32 consecutive ones, in the order of x in memory."""
+    kind = _storage(x)
+    _packed_pair(x, codes, steps, "convbn_pack")
+    status = (_native or _calls()).convbn_pack(kind, x, codes, steps, x.numel(), stream)
     if status:
         _raise(status, "convbn_pack")
 
 
 def convbn_unpack(codes, steps, out, stream=None):
-    status = (_native or _calls()).convbn_unpack(_storage(out), codes, steps, out, out.numel(), stream)
+    kind = _storage(out)
+    _packed_pair(out, codes, steps, "convbn_unpack")
+    status = (_native or _calls()).convbn_unpack(kind, codes, steps, out, out.numel(), stream)
     if status:
         _raise(status, "convbn_unpack")
 
@@ -417,6 +440,8 @@ def convbn_tune_bwd_packed(desc, dz, codes, steps, w, b, run_mean, saved, dx, dw
     """convbn_tune_bwd_glue with X as convbn_pack left it."""
     if type(desc) is not Desc:
         desc = _desc(desc)
+    if desc is not None:
+        _packed_room(codes, steps, desc.n * desc.c_in * desc.h_in * desc.w_in, "convbn_tune_bwd_packed")
     status = (_native or _calls()).convbn_tune_bwd_packed(desc, dz, codes, steps, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta,
                                                           add, 1 if relu_mask else 0, 1 if begin else 0, workspace,
                                                           workspace_bytes, stream)

@@ -69,6 +69,42 @@ def test_packed_backward_refusals():
     assert status(desc=C.Desc.make(0, 64, 8, 8, 64, 1, 1)) == C.EINVAL
 
 
+def test_tensors_that_do_not_hold_what_is_read_or_written_are_refused():
+    """The library takes addresses and a count, so what is too short, of another width, or has gaps is refused before the call."""
+    import torch
+    x = torch.zeros(100, 64, dtype=torch.bfloat16)
+    codes, steps = torch.zeros(6400, dtype=torch.int8), torch.zeros(200, dtype=torch.uint8)
+
+    def refused(what, x=x, codes=codes, steps=steps):
+        for call in (lambda: C.convbn_pack(x, codes, steps, stream=0), lambda: C.convbn_unpack(codes, steps, x, stream=0)):
+            with pytest.raises(C.ConvBNError, match=what) as e:
+                call()
+            assert e.value.status == C.EINVAL
+
+    refused("codes", codes=codes[:6399])
+    refused("steps", steps=steps[:199])
+    refused("codes", codes=codes.view(100, 64)[:, :32])
+    refused("codes", codes=torch.zeros(128, 64, dtype=torch.int8).t())
+    refused("codes", codes=torch.zeros(6400, dtype=torch.int32))
+    refused("steps", steps=torch.zeros(400, dtype=torch.uint8)[::2])
+    refused("steps", steps=torch.zeros(200, dtype=torch.float32))
+    refused("one piece", x=x[:, ::2])
+    refused("one piece", x=x.t())
+    refused("one piece", x=torch.zeros(64, dtype=torch.bfloat16).expand(100, 64))
+    refused("one GPU")                                                   # (nothing else is wrong, in any of the three)
+    refused("one GPU", x=torch.zeros(2, 8, 20, 20, dtype=torch.bfloat16).to(memory_format=torch.channels_last))
+    refused("codes", codes=codes[:2 * 64 * 8 * 8 - 1], x=torch.zeros(2, 8, 8, 64, dtype=torch.float32))
+
+    d = C.Desc.make(2, 64, 8, 8, 64, 1, 1)
+    for c, s in ((codes, torch.zeros(256, dtype=torch.uint8)), (torch.zeros(8191, dtype=torch.int8), torch.zeros(256, dtype=torch.uint8)),
+                 (torch.zeros(8192, dtype=torch.int8), torch.zeros(255, dtype=torch.uint8)),
+                 (torch.zeros(8192, dtype=torch.int8), torch.zeros(512, dtype=torch.uint8)[::2])):
+        with pytest.raises(C.ConvBNError, match="codes|steps") as e:
+            C.convbn_tune_bwd_packed(d, 4096, c, s, 4096, None, 4096, 4096, 4096, 4096, None, 4096, 4096, None, True, False, 4096, 1 << 30,
+                                     stream=0)
+        assert e.value.status == C.EINVAL
+
+
 def test_room_for_slices_that_keep_sums_short():
     """A weight gradient's fp32 accumulators add up 6144 pixels at most: a partial tensor for each slice of so many."""
     size = lambda rows, ci, co: C.convbn_workspace_bytes(C.convbn_linear_desc(rows, ci, co), C.PHASE_TUNE_BWD_PACKED)
