@@ -205,9 +205,8 @@ Plan make_plan(const convbn_desc *d, const Problem &pb, int phase, Slicing slici
 Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, Slicing slicing, WgradSums sums) {
     Plan pl;
     const bool bounded = slicing == kSlicesBounded;
-    auto sliced = [&](WgradSums beside) {
-        return bounded ? umma_wgrad_plan_bounded(pb) : umma_wgrad_plan(pb, beside, slicing == kSlicesExact ? kExactPixels : 0);
-    };
+    const long long most = slicing == kSlicesExact ? kExactPixels : 0;
+    auto sliced = [&](WgradSums beside) { return bounded ? umma_wgrad_plan_bounded(pb) : umma_wgrad_plan(pb, beside, most); };
     UmmaConvShape us;
     if (phase == CONVBN_PHASE_TUNE_BWD) {
         if (!fused_bwd_path(d, pb)) {       // the two passes run side by side: each has its own region
@@ -271,7 +270,7 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, Slicing slici
         pl.uw = sliced(WgradSums::kDz);
         pl.bsplits = pl.uw.splits;
         part_bytes = (size_t)pl.uw.splits * (pb.c_out / 64) * pb.kh * pb.kw * 64 * 64 * sizeof(float);
-        const int slots = grouped8_eligible(pb) ? grouped8_wgrad_slots(pb) : 0;
+        const int slots = grouped8_eligible(pb) ? grouped8_wgrad_slots(pb, most) : 0;
         if (slots > 0) {
             pl.grouped8_wgrad = true;
             pl.bsplits = slots;
@@ -280,13 +279,13 @@ Plan form_plan(const convbn_desc *d, const Problem &pb, int phase, Slicing slici
     }
     if (pl.stem) {
         pl.umma_wgrad = false;
-        pl.uw = stem_wgrad_plan(pb);
+        pl.uw = stem_wgrad_plan(pb, most != 0);
         pl.bsplits = pl.uw.splits;
         part_bytes = (size_t)pl.uw.splits * stem_krows(pb) * 64 * pb.c_out * sizeof(float);
         if (stem_window_wgrad_eligible(pb, bounded)) {
             pl.stem_win_wgrad = true;
             pl.uw = UmmaWgradPlan();
-            pl.uw.splits = stem_window_wgrad_ctas(pb);
+            pl.uw.splits = stem_window_wgrad_ctas(pb, most);
             pl.bsplits = pl.uw.splits;
             part_bytes = wrows * pl.uw.splits * sizeof(float);
             dot_bytes = (size_t)wgrad_kmajor_rows(pb) * pb.c_out * sizeof(float);
@@ -766,7 +765,7 @@ int run_param_grads(const convbn_desc *d, const Problem &pb, const Plan &pl, con
         LAUNCH("channel_sum", launch_channel_sum_partial(pb, d->dtype, d->layout, dz, bsum, pl.bsplits, st));
     if (pl.stem_win_wgrad) {
         float *dotpart = (float *)at(ws, pl.dotpart);
-        LAUNCH("stem_wgrad", launch_stem_window_wgrad(pb, dz, x, partials, bsum, st));
+        LAUNCH("stem_wgrad", launch_stem_window_wgrad(pb, pl.uw.splits, dz, x, partials, bsum, st));
         LAUNCH("wgrad_kmajor", launch_wgrad_epilogue_kmajor(pb, pl.uw.splits, partials, bsum, w, vec3, b, mean, dw, dotpart, db,
                                                           dgamma, dbeta, need_bsum, st));
         *which = "umma-stem";
@@ -777,8 +776,8 @@ int run_param_grads(const convbn_desc *d, const Problem &pb, const Plan &pl, con
                                                                  dgamma, dbeta, need_bsum, st));
         *which = "umma-stem";
     } else if (pl.grouped8_wgrad) {
-        LAUNCH("grouped_wgrad", launch_grouped8_wgrad(pb, dz, x, partials, bsum, st));
-        LAUNCH("grouped_wgrad_finish", launch_grouped8_wgrad_finish(pb, partials, bsum, w, vec3, b, mean, dw, db,
+        LAUNCH("grouped_wgrad", launch_grouped8_wgrad(pb, pl.bsplits, dz, x, partials, bsum, st));
+        LAUNCH("grouped_wgrad_finish", launch_grouped8_wgrad_finish(pb, pl.bsplits, partials, bsum, w, vec3, b, mean, dw, db,
                                                                     dgamma, dbeta, st));
         *which = "grouped-mma";
     } else if (pl.grouped_wgrad) {

@@ -533,7 +533,7 @@ cudaError_t launch_grouped8_dgrad(const Problem &pb, const void *dz, const void 
 }
 
 // Blocks per 64-channel chunk of the backward-weight kernel = partial rows it writes.
-static GroupedPlan plan_grouped8_wgrad(const Problem &pb, int *slots) {
+static GroupedPlan plan_grouped8_wgrad(const Problem &pb, long long most, int *slots) {
     GroupedPlan pl = plan_grouped8(pb.n, pb.h_in, pb.w_in, pb.c_in, pb.h_out, pb.w_out, pb.kh, pb.kw, -pb.pad_h, -pb.pad_w,
                                    true);
     if (!pl.ok) return pl;
@@ -541,6 +541,10 @@ static GroupedPlan plan_grouped8_wgrad(const Problem &pb, int *slots) {
     const int chunks = pb.c_in / 64;
     long long per_chunk = (long long)sms * pl.bps / chunks;
     const long long bands = (long long)pb.n * pl.g.tiles_h;
+    if (most) {                                          // (a band's pixels are fewer than what a block stages)
+        const long long band = (long long)pl.g.R * pb.w_out, each = most > band ? most / band : 1, least = (bands + each - 1) / each;
+        if (per_chunk < least) per_chunk = least;
+    }
     if (per_chunk > bands) per_chunk = bands;
     if (per_chunk < 1) per_chunk = 1;
     *slots = (int)per_chunk;
@@ -548,17 +552,18 @@ static GroupedPlan plan_grouped8_wgrad(const Problem &pb, int *slots) {
     return pl;
 }
 
-int grouped8_wgrad_slots(const Problem &pb) {
+int grouped8_wgrad_slots(const Problem &pb, long long most) {
     int slots = 0;
-    return plan_grouped8_wgrad(pb, &slots).ok ? slots : 0;
+    return plan_grouped8_wgrad(pb, most, &slots).ok ? slots : 0;
 }
 
-// part: [slots][C][taps 8] floats, bsum: [slots][C] floats (slots = grouped8_wgrad_slots)
-cudaError_t launch_grouped8_wgrad(const Problem &pb, const void *dz, const void *x, float *part, float *bsum,
+// part: [slots][C][taps 8] floats, bsum: [slots][C] floats
+cudaError_t launch_grouped8_wgrad(const Problem &pb, int slots, const void *dz, const void *x, float *part, float *bsum,
                                   cudaStream_t st) {
-    int slots = 0;
-    const GroupedPlan pl = plan_grouped8_wgrad(pb, &slots);
-    if (!pl.ok) return cudaErrorInvalidValue;
+    int fastest = 0;
+    GroupedPlan pl = plan_grouped8_wgrad(pb, 0, &fastest);
+    if (!pl.ok || slots <= 0) return cudaErrorInvalidValue;
+    pl.grid = (unsigned)slots * (unsigned)(pb.c_in / 64);
     CUtensorMap tx, tdz;
     {
         const unsigned long long dims[4] = {(unsigned long long)pb.c_in, (unsigned long long)pb.w_in,
@@ -590,10 +595,9 @@ cudaError_t launch_grouped8_wgrad(const Problem &pb, const void *dz, const void 
                       slots, part, bsum, err);
 }
 
-cudaError_t launch_grouped8_wgrad_finish(const Problem &pb, const float *part, const float *bsum, const void *w,
+cudaError_t launch_grouped8_wgrad_finish(const Problem &pb, int slots, const float *part, const float *bsum, const void *w,
                                          const float *vec3, const float *b, const float *mean, float *dw, float *db,
                                          float *dgamma, float *dbeta, cudaStream_t st) {
-    const int slots = grouped8_wgrad_slots(pb);
     if (slots <= 0) return cudaErrorInvalidValue;
     // With 256 threads five blocks share an SM.  512 where a thread would go through more than six batches of slots (C = 256,
     // 56 x 16, N = 31, 111 slots: 19.5 and 17.2 us with the GEMM); 1024, which many slots want alone, cost 1.3 to 3.8 times the

@@ -188,8 +188,9 @@ bool stem_dgrad_eligible(const Problem &pb);
 cudaError_t launch_stem_dgrad(const Problem &pb, const void *dz, const void *w, const float *s_vec, void *dx,
                               cudaStream_t st);
 // Weight gradient of a stem layer on the packed input: partials [splits][krows * 64][C_out] (padded k rows),
-// bsum [splits][C_out]; the epilogue gathers the real kh x kw x C_in entries.
-UmmaWgradPlan stem_wgrad_plan(const Problem &pb);
+// bsum [splits][C_out]; the epilogue gathers the real kh x kw x C_in entries.  segments: accumulators of long slices are emptied
+// every 1024 pixels (umma_wgrad.cu, SEG).
+UmmaWgradPlan stem_wgrad_plan(const Problem &pb, bool segments = false);
 cudaError_t launch_stem_wgrad(const Problem &pb, const UmmaWgradPlan &pl, const void *dz, const void *x_packed,
                               float *partials, float *bsum, cudaStream_t st);
 cudaError_t launch_wgrad_epilogue_stem(const Problem &pb, const UmmaWgradPlan &pl, const float *partials,
@@ -202,11 +203,11 @@ bool stem_window_eligible(const Problem &pb);
 cudaError_t launch_stem_window_fwd(const Problem &pb, const void *x, const void *w, const float *bias, void *z,
                                    cudaStream_t st, const BnFold *fold = nullptr, int relu = 0);
 // Weight gradient of the same layers (C_in <= 3, C_out = 64) straight from X and dZ: one fp32 partial
-// [kdim][C_out] and one row of sums of dZ per CTA (stem_window_wgrad_ctas of them), for
-// launch_wgrad_epilogue_kmajor.
+// [kdim][C_out] and one row of sums of dZ per CTA (as many as stem_window_wgrad_ctas says), for
+// launch_wgrad_epilogue_kmajor.  most: pixels that an accumulator may add up, 0: any number.
 bool stem_window_wgrad_eligible(const Problem &pb, bool any_width = false);
-int stem_window_wgrad_ctas(const Problem &pb);
-cudaError_t launch_stem_window_wgrad(const Problem &pb, const void *dz, const void *x, float *partials, float *bsum,
+int stem_window_wgrad_ctas(const Problem &pb, long long most = 0);
+cudaError_t launch_stem_window_wgrad(const Problem &pb, int ctas, const void *dz, const void *x, float *partials, float *bsum,
                                      cudaStream_t st);
 // Backward data of the same layers (C_out = 64, W_out <= 128) as a scatter GEMM with the overlap-add of the
 // window positions done on chip (see stem_window_dgrad.cu); s_vec (NULL = 1) is folded into the weights.
@@ -250,11 +251,12 @@ cudaError_t launch_grouped8_fwd(const Problem &pb, const void *x, const void *w,
                                 cudaStream_t st, const BnFold *fold = nullptr);
 cudaError_t launch_grouped8_dgrad(const Problem &pb, const void *dz, const void *w, const float *s_vec, void *dx,
                                   cudaStream_t st);
-// backward weight: part [slots][C][taps 8] and bsum [slots][C] floats, slots = grouped8_wgrad_slots(pb)
-int grouped8_wgrad_slots(const Problem &pb);
-cudaError_t launch_grouped8_wgrad(const Problem &pb, const void *dz, const void *x, float *part, float *bsum,
+// backward weight: part [slots][C][taps 8] and bsum [slots][C] floats, slots = grouped8_wgrad_slots(pb, most); most: pixels that
+// a slot may have, 0: any number
+int grouped8_wgrad_slots(const Problem &pb, long long most = 0);
+cudaError_t launch_grouped8_wgrad(const Problem &pb, int slots, const void *dz, const void *x, float *part, float *bsum,
                                   cudaStream_t st);
-cudaError_t launch_grouped8_wgrad_finish(const Problem &pb, const float *part, const float *bsum, const void *w,
+cudaError_t launch_grouped8_wgrad_finish(const Problem &pb, int slots, const float *part, const float *bsum, const void *w,
                                          const float *vec3, const float *b, const float *mean, float *dw, float *db,
                                          float *dgamma, float *dbeta, cudaStream_t st);
 // wbd[co][tap][64]: omega (scaled by s_vec[co] if given) placed at its group's columns, zeros elsewhere.
@@ -341,11 +343,13 @@ cudaError_t launch_tconv_param_epilogue(int dtype, bool nhwc, int c_out, int tap
 cudaError_t launch_pack(int dtype, const void *x, void *codes, void *steps, long long count, cudaStream_t st);
 cudaError_t launch_unpack(int dtype, const void *codes, const void *steps, void *out, long long count, cudaStream_t st);
 
-// Pixels that one fp32 accumulator of a weight gradient from packed X adds up, at most.  The tensor core's sums drift with their length:
-// against 64 bits, half values, relative error of domega per 1000 pixels of a slice 0.7 to 1.2e-6 (1024 -> 512 at 63 x 100: N = 4,
-// 2800 pixels 1.9e-6; N = 23, 16100 pixels 2.0e-5), a quarter of that for bf16.  Slices themselves are added in order by
-// launch_wgrad_rows.  With half values the accumulators are emptied every 1024 pixels besides (umma_wgrad.cu, SEG;
-// umma_bwd1x1_packed.cu): 5e-7, as fp32 additions that round have it.
+// Pixels that one fp32 accumulator of a tensor-core weight gradient from packed X adds up, at most.  The tensor core's sums drift with their
+// length: against 64 bits, relative error of domega per 1000 pixels of a slice 0.7 to 1.5e-6 for half values (1024 -> 512 at 63 x 100: N = 4,
+// 2800 pixels 1.9e-6; N = 23, 16100 pixels 2.0e-5), a quarter of that for bf16.  Slices themselves are added in order by the finishing
+// kernels.  Where accumulators are emptied every 1024 pixels besides, by additions that round, it is 3e-7 (bf16) to 8e-7: with half values
+// in umma_wgrad.cu (SEG) and umma_bwd1x1_packed.cu, with both types for stems on a packed copy (3 -> 64 at 225 x 225, N = 256: 43000 pixels
+// a slice 5.0e-5 before in half, 2.6e-5 in bf16).  A stem's window kernel and groups of eight stay at this limit: 5.2e-6 in half (3 -> 64
+// at 224 x 224, N = 256; one accumulator per SM for all rows 1.1e-5; 350 -> 360 us a call).
 constexpr long long kExactPixels = 6144;
 
 // The fused backward of a 1x1 layer (fused_bwd1x1_eligible) from packed X: umma_bwd1x1_packed.cu.  partials, bsum: one per CTA

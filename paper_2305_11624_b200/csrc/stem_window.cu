@@ -809,12 +809,21 @@ static cudaError_t launch_window_wgrad(const CUtensorMap &tdz, const WinWgrad &g
                       (const __nv_bfloat16 *)x, partials, bsum, err);
 }
 
-int stem_window_wgrad_ctas(const Problem &pb) {
+// One CTA per SM, or as many rounds of them as keep an accumulator's sums within `most` pixels.  It adds up one row of every pair
+// of a chunk of kWgR, and the last row of a chunk that has an odd number: L rows of images of H have at most L / H + 3 of those,
+// so that (L + L / H + 3) / 2 rows are an accumulator's at most.
+int stem_window_wgrad_ctas(const Problem &pb, long long most) {
     const long long rows = (long long)pb.n * pb.h_out, sms = device_sm_count();
-    return (int)(rows < sms ? rows : sms);
+    long long ctas = sms;
+    if (most) {
+        long long each = (2 * (most / pb.w_out) - 3) * pb.h_out / (pb.h_out + 1);      // (w_out is 256 at most)
+        if (each < 1) each = 1;
+        ctas = ((rows + each - 1) / each + sms - 1) / sms * sms;
+    }
+    return (int)(rows < ctas ? rows : ctas);
 }
 
-cudaError_t launch_stem_window_wgrad(const Problem &pb, const void *dz, const void *x, float *partials, float *bsum,
+cudaError_t launch_stem_window_wgrad(const Problem &pb, int ctas, const void *dz, const void *x, float *partials, float *bsum,
                                      cudaStream_t st) {
     const WinWgPlan pl = plan_window_wgrad(pb, true);
     if (!pl.ok) return cudaErrorInvalidValue;
@@ -835,7 +844,7 @@ cudaError_t launch_stem_window_wgrad(const Problem &pb, const void *dz, const vo
     int *err = nullptr;
     cudaError_t e = error_word_address(&err);
     if (e != cudaSuccess) return e;
-    const unsigned grid = (unsigned)stem_window_wgrad_ctas(pb);
+    const unsigned grid = (unsigned)ctas;
     switch (pb.c_in) {
         case 1: return launch_window_wgrad<1>(tdz, g, pl.smem, grid, x, partials, bsum, err, st);
         case 2: return launch_window_wgrad<2>(tdz, g, pl.smem, grid, x, partials, bsum, err, st);

@@ -867,7 +867,7 @@ cudaError_t launch_wgrad_epilogue_kmajor(const Problem &pb, int splits, const fl
 }
 
 // ---- small-C_in ("stem") layers -------------------------------------------------------------------
-UmmaWgradPlan stem_wgrad_plan(const Problem &pb) {
+UmmaWgradPlan stem_wgrad_plan(const Problem &pb, bool segments) {
     UmmaWgradPlan pl;
     const int bn = stem_wgrad_bn(pb);
     const long long patches = (long long)pb.n * ((pb.h_out + 3) / 4) * ((pb.w_out + 15) / 16);
@@ -878,6 +878,7 @@ UmmaWgradPlan stem_wgrad_plan(const Problem &pb) {
     const long long per = (patches + splits - 1) / splits;
     pl.per_split = per * kWP;                       // in pixels of 4 x 16 patches
     pl.splits = (int)((patches + per - 1) / per);
+    pl.segments = segments && pl.per_split > kWSegment * kWP;
     return pl;
 }
 
@@ -919,9 +920,13 @@ cudaError_t launch_stem_wgrad(const Problem &pb, const UmmaWgradPlan &pl, const 
     Problem q = pb;
     q.kdim = g.kdim;                                   // grid: (kh + 2) / 2 row tiles
     const int bn = stem_wgrad_bn(pb);
-    if (bn == 64) return launch_w<64>(tx, tdz, g, pl, q, partials, bsum, err, st);
-    if (bn == 128) return launch_w<128>(tx, tdz, g, pl, q, partials, bsum, err, st);
-    return launch_w<256>(tx, tdz, g, pl, q, partials, bsum, err, st);
+    auto go = [&](auto seg) {
+        constexpr bool S = decltype(seg)::value;
+        if (bn == 64) return launch_w<64, false, false, S>(tx, tdz, g, pl, q, partials, bsum, err, st);
+        if (bn == 128) return launch_w<128, false, false, S>(tx, tdz, g, pl, q, partials, bsum, err, st);
+        return launch_w<256, false, false, S>(tx, tdz, g, pl, q, partials, bsum, err, st);
+    };
+    return pl.segments ? go(std::true_type{}) : go(std::false_type{});
 }
 
 // One block per output channel: gathers the kh x kw x C_in real entries out of the krows x 64 padded rows,

@@ -112,6 +112,19 @@ def test_room_for_slices_that_keep_sums_short():
         assert size(rows, ci, co) >= -(-rows // 6144) * ci * co * 4, (rows, ci, co)
 
 
+def test_room_for_the_short_sums_of_stems_and_groups_of_eight():
+    """The same for the kernels whose accumulators stay with a block: a stem's read straight from X (3 -> 64, two accumulators a block,
+    224 pixels a row: 14400 rows and more), groups of eight channels."""
+    def partials(d, elements):
+        return (C.convbn_workspace_bytes(d, C.PHASE_TUNE_BWD_PACKED) - elements * 2 - C.convbn_workspace_bytes(d, C.PHASE_TUNE_BWD_DATA))
+    for kind in (C.BF16, C.F16):
+        for n in (256, 1024):
+            d = C.Desc.make(n, 3, 224, 224, 64, 7, 7, 2, 2, 3, 3, dtype=kind)
+            assert partials(d, n * 224 * 224 * 3) >= n * 112 * 112 // (2 * 6144) * 147 * 64 * 4
+        d = C.Desc.make(256, 2048, 28, 28, 2048, 3, 3, 1, 1, 1, 1, groups=256, dtype=kind)
+        assert partials(d, 256 * 28 * 28 * 2048) >= 256 * 28 * 28 // 6144 * 2048 * 72 * 4
+
+
 # ---- packing on the device ------------------------------------------------------------------------------------------
 def _values(count, dtype, seed):
     """Every kind of group: ordinary, all zero, one value, values at a tie, the type's largest and smallest, infinities, NaN."""
@@ -506,3 +519,61 @@ def test_an_addend_is_rounded_with_the_sum(n, ci, hw, co, stride, mask, dtype):
     want = (conv + add.double()).float().to(td)                       # (to fp32 first, as an fp32 sum is)
     want = torch.where(x > 0, want, torch.zeros_like(want)).float() if mask else want.float()
     assert int((dx.float() != want).sum()) == 0
+
+
+def _exact_weight_gradient(x, dz, k, stride, pad, groups):
+    """domega' [C_out, k, k, C_in / groups] of NHWC tensors in 64 bits, some images at a time."""
+    import torch
+    n, h, w, ci = x.shape
+    ho, wo, co = dz.shape[1:]
+    cg = ci // groups
+    exact = torch.zeros(co, k, k, cg, dtype=torch.float64, device="cuda")
+    some = max(1, int(2e8 // (h * w * ci + ho * wo * co)))
+    for at in range(0, n, some):
+        xp = torch.nn.functional.pad(x[at:at + some].double(), (0, 0, pad, pad, pad, pad))
+        z = dz[at:at + some].double().reshape(-1, groups, co // groups).permute(1, 2, 0)
+        for r in range(k):
+            for q in range(k):
+                v = xp[:, r:r + (ho - 1) * stride + 1:stride, q:q + (wo - 1) * stride + 1:stride]
+                exact[:, r, q] += torch.bmm(z, v.reshape(-1, groups, cg).permute(1, 0, 2)).reshape(co, cg)
+    return exact
+
+
+# name, n, C_in, h, w, C_out, k, stride, groups, kernel, whether the accumulators are emptied every 1024 pixels: half, bf16
+LONG_SUMS = [("stem_window", 512, 3, 224, 224, 64, 7, 2, 1, "umma-stem", (False, False)),
+             ("stem_packed", 256, 3, 225, 225, 64, 7, 2, 1, "umma-stem", (True, True)),
+             ("stem_packed_wide", 256, 3, 64, 64, 256, 5, 2, 1, "umma-stem", (True, True)),
+             ("groups_of_8", 256, 2048, 28, 28, 2048, 3, 1, 256, "grouped-mma", (False, False)),
+             ("groups_of_32", 128, 64, 56, 56, 64, 3, 1, 2, "grouped-umma", (True, False)),
+             ("conv3", 64, 128, 56, 56, 128, 3, 1, 1, "umma", (True, False))]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("layer", LONG_SUMS, ids=lambda l: l[0])
+def test_sums_over_many_pixels_of_other_layers(layer, dtype):
+    """As test_sums_over_many_pixels, with its bounds: 6144 pixels (384 additions of 16 products) where an accumulator is not emptied, 1024
+    (64) where it is; partial sums of a CTA and of the CTAs after that, fewer than 512 roundings one after the other."""
+    import torch
+    name, n, ci, h, w, co, k, stride, groups, kernel, emptied = layer
+    kind, td = (C.BF16, torch.bfloat16) if dtype == "bf16" else (C.F16, torch.float16)
+    d = C.Desc.make(n, ci, h, w, co, k, k, stride, stride, k // 2, k // 2, groups=groups, dtype=kind, layout=C.NHWC)
+    ho, wo = C.convbn_out_shape(d)
+    g = torch.Generator("cuda").manual_seed(7)
+    rand = lambda *shape: torch.randn(shape, device="cuda", generator=g).to(td)
+    x, dz, wt = rand(n, h, w, ci), rand(n, ho, wo, co), rand(co, k, k, ci // groups)
+    codes, steps = torch.empty(x.numel(), dtype=torch.int8, device="cuda"), torch.empty(-(-x.numel() // 32), dtype=torch.uint8, device="cuda")
+    C.convbn_pack(x, codes, steps)
+    mean, saved = torch.zeros(co, device="cuda"), torch.ones(3 * co, device="cuda")
+    dx = torch.empty_like(x)
+    dw, dgamma, dbeta = torch.empty(co, k, k, ci // groups, device="cuda"), torch.empty(co, device="cuda"), torch.empty(co, device="cuda")
+    ws = torch.empty(C.convbn_workspace_bytes(d, C.PHASE_TUNE_BWD_PACKED), dtype=torch.uint8, device="cuda")
+    C.convbn_tune_bwd_packed(d, dz, codes, steps, wt, None, mean, saved, dx, dw, None, dgamma, dbeta, None, False, False, ws)
+    C.convbn_check()
+    assert C.convbn_last_kernel(C.PHASE_TUNE_BWD_WEIGHT) == kernel
+    C.convbn_unpack(codes, steps, x)
+    exact, total = _exact_weight_gradient(x, dz, k, stride, k // 2, groups), dz.double().sum((0, 1, 2))
+    rel = lambda a, b: float((a.double() - b).norm() / b.norm())
+    bound = (64 if emptied[0 if dtype == "f16" else 1] else 384) * 2 / 3 * 2.0 ** -24 + 2.0 ** -20
+    assert rel(dw, exact) <= bound and rel(dbeta, total) <= bound, (rel(dw, exact), rel(dbeta, total), bound)
+    assert rel(dgamma, (exact * wt.double()).sum((1, 2, 3))) <= bound * 2
