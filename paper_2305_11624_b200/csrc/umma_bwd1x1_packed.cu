@@ -26,7 +26,7 @@ constexpr uint32_t kPbBox = 128 * 128;        // [128 pixels][64 channels] of 16
 constexpr uint32_t kPbOut = 32 * 128;         // an epilogue warp's box: [32 pixels][64 channels]
 // Half values: the accumulators of domega and sum dZ are added to the CTA's partial, which stays in L2, every eight tiles, by additions
 // that round (those of the tensor core cut off, and drift: see kExactPixels).  256 -> 64 at 56 x 56, N = 256 204 -> 214 us, 64 -> 128 at
-// 100 x 65, N = 240 129 -> 144; read back and stored instead 245 and 332, by as many more CTAs 251 and 230.
+// 100 x 65, N = 240 129 -> 139 (144 in two rounds of CTAs); read back and stored instead 245 and 332, by as many more CTAs 251 and 230.
 constexpr uint32_t kPbSegment = 8;
 
 struct PackedBwd {
@@ -439,10 +439,11 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
 
 }  // namespace
 
-// One CTA per SM, or as many rounds of them as keep an accumulator's sums short (1.56 M pixels 64 -> 128: two).
+// One CTA per SM, or, where accumulators are not emptied on the way, as many rounds of them as keep their sums short (1.56 M pixels
+// 64 -> 128: two).
 int packed_bwd1x1_ctas(const Problem &pb) {
     const long long tiles = (pb.p + 127) / 128, sms = device_sm_count(), most = sms * (kExactPixels / 128);
-    const long long ctas = (tiles + most - 1) / most * sms;
+    const long long ctas = call_f16() ? sms : (tiles + most - 1) / most * sms;
     return (int)(tiles < ctas ? tiles : ctas);
 }
 

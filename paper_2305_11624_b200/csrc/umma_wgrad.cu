@@ -66,12 +66,12 @@ struct WgradSmemCtl {
 // X_SUMS: g.sums is kSumX.
 // PACKED: X comes as 8-bit codes (tm_x: a map of bytes) and steps.  A slice's codes land in the first half of its place, 64 bytes a
 // pixel; the epilogue warps, two per slice, take them into registers, meet, and write the 16-bit values (code * step, exact) over the
-// whole of it while earlier stages are multiplied.  (Which layers: packed_path in
-// convbn_api.cu.)
+// whole of it while earlier stages are multiplied.  (Which layers: packed_path in convbn_api.cu.)
 // SEG: the accumulator is emptied every kWSegment blocks of pixels into a second one, by additions that round (those of the tensor core cut
 // off, and drift: see kExactPixels).  The epilogue warps do it, 32 columns at a time, while the CTA beside this one multiplies.  Whole
-// backward calls from packed X, bf16 (without) and half (with): 512 -> 128 at 28 x 28, N = 64 54.2 and 54.1 us, 1024 -> 512 at 63 x 100,
-// N = 23 414 and 453, 100000 rows 2048 -> 1024 1486 and 1513.
+// backward calls from packed X, half, with slices of at most 6144 pixels besides and without: 1024 -> 512 at 63 x 100, N = 23 381 and 377
+// us, 100000 rows 2048 -> 1024 1430 and 1470 (and 125 MB less of partial tensors), 3x3 512 at 28 x 28, N = 128 761 and 702 (151 MB), 3x3 128
+// in groups of 32 at 56 x 56, N = 256 596 and 377.
 template <int BN, bool X_SUMS, bool PACKED, bool SEG>
 __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_constant__ CUtensorMap tm_x,
                                                               const __grid_constant__ CUtensorMap tm_dz,
@@ -508,8 +508,10 @@ UmmaWgradPlan umma_wgrad_plan(const Problem &pb, WgradSums sums, long long most)
     // arrive pixel by pixel and a second CTA hides that (29173 rows, 1024 -> 64: 44.5 and 27.4 us; 2 x 2 about even; from
     // 4 x 4 on one CTA is the faster).
     const long long tiles = wgrad_tiles(pb, pb.groups > 1 ? 64 : wgrad_bn(pb), sums == WgradSums::kDz), sms = device_sm_count();
-    UmmaWgradPlan pl = wgrad_slices(pb, tiles, sms * (tiles <= 24 && pb.p * tiles <= 2048 * sms && pb.w_out >= 4 ? 1 : 2), most);
-    pl.segments = most && call_f16() && sums == WgradSums::kDz && pl.per_split > kWSegment * kWP;
+    // half values: an accumulator that is emptied every kWSegment blocks needs no short slices, each with a partial tensor of its own
+    const bool emptied = most && call_f16() && sums == WgradSums::kDz;
+    UmmaWgradPlan pl = wgrad_slices(pb, tiles, sms * (tiles <= 24 && pb.p * tiles <= 2048 * sms && pb.w_out >= 4 ? 1 : 2), emptied ? 0 : most);
+    pl.segments = emptied && pl.per_split > kWSegment * kWP;
     return pl;
 }
 

@@ -125,6 +125,17 @@ def test_room_for_the_short_sums_of_stems_and_groups_of_eight():
         assert partials(d, 256 * 28 * 28 * 2048) >= 256 * 28 * 28 // 6144 * 2048 * 72 * 4
 
 
+def test_half_values_need_no_more_room_than_the_other_call():
+    """Their accumulators are emptied on the way, so the slices, and the partial tensors, are those of convbn_tune_bwd: beside those, X
+    restored where the weight gradient does not do that itself."""
+    for args in ((100000, 2048, 1, 1, 2048, 1), (100000, 2048, 1, 1, 1024, 1), (23, 1024, 63, 100, 512, 1), (240, 64, 100, 65, 128, 1),
+                 (64, 2048, 7, 7, 512, 1), (256, 64, 56, 56, 64, 3), (128, 512, 28, 28, 512, 3), (17, 256, 15, 14, 512, 1)):
+        n, ci, h, w, co, k = args
+        d = C.Desc.make(n, ci, h, w, co, k, k, 1, 1, k // 2, k // 2, dtype=C.F16)
+        packed, plain = (C.convbn_workspace_bytes(d, p) for p in (C.PHASE_TUNE_BWD_PACKED, C.PHASE_TUNE_BWD))
+        assert plain <= packed <= plain + n * h * w * ci * 2 + 256, args
+
+
 # ---- packing on the device ------------------------------------------------------------------------------------------
 def _values(count, dtype, seed):
     """Every kind of group: ordinary, all zero, one value, values at a tie, the type's largest and smallest, infinities, NaN."""
