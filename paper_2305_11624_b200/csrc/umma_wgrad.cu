@@ -508,10 +508,15 @@ UmmaWgradPlan umma_wgrad_plan(const Problem &pb, WgradSums sums, long long most)
     // arrive pixel by pixel and a second CTA hides that (29173 rows, 1024 -> 64: 44.5 and 27.4 us; 2 x 2 about even; from
     // 4 x 4 on one CTA is the faster).
     const long long tiles = wgrad_tiles(pb, pb.groups > 1 ? 64 : wgrad_bn(pb), sums == WgradSums::kDz), sms = device_sm_count();
-    // half values: an accumulator that is emptied every kWSegment blocks needs no short slices, each with a partial tensor of its own
-    const bool emptied = most && call_f16() && sums == WgradSums::kDz;
-    UmmaWgradPlan pl = wgrad_slices(pb, tiles, sms * (tiles <= 24 && pb.p * tiles <= 2048 * sms && pb.w_out >= 4 ? 1 : 2), emptied ? 0 : most);
-    pl.segments = emptied && pl.per_split > kWSegment * kWP;
+    // An accumulator that is emptied every kWSegment blocks needs no short slices, each with a partial tensor of its own.  Half values: always.
+    // bf16, which drifts a quarter as much: where the fastest slices are longer than `most` and the weights have several taps (emptied and in
+    // short slices, whole backward calls: 3x3 512 at 28 x 28, N = 128 690 and 745 us, 126 and 277 MB of workspace; 64 at 56 x 56, N = 256 187
+    // and 203, 112 and 129 MB; 128 in groups of 32 at 56 x 56, N = 256 377 and 592, 214 and 249 MB); 1x1 layers keep short slices, which
+    // are the faster ones there (half values: 100000 rows 2048 -> 1024 1470 and 1430).
+    const long long slots = sms * (tiles <= 24 && pb.p * tiles <= 2048 * sms && pb.w_out >= 4 ? 1 : 2);
+    const bool half = call_f16(), emptied = most && sums == WgradSums::kDz && (half || pb.kh * pb.kw > 1);
+    UmmaWgradPlan pl = wgrad_slices(pb, tiles, slots, emptied ? 0 : most);
+    pl.segments = emptied && pl.per_split > (half ? (long long)kWSegment * kWP : most);
     return pl;
 }
 

@@ -136,6 +136,14 @@ def test_half_values_need_no_more_room_than_the_other_call():
         assert plain <= packed <= plain + n * h * w * ci * 2 + 256, args
 
 
+def test_layers_of_several_taps_need_no_more_room_than_the_other_call():
+    """The same in bf16, whose 1x1 layers alone have slices instead."""
+    for n, c, hw, groups in ((256, 64, 56, 1), (128, 512, 28, 1), (256, 128, 56, 4), (64, 256, 14, 1)):
+        d = C.Desc.make(n, c, hw, hw, c, 3, 3, 1, 1, 1, 1, groups=groups, dtype=C.BF16)
+        packed, plain = (C.convbn_workspace_bytes(d, p) for p in (C.PHASE_TUNE_BWD_PACKED, C.PHASE_TUNE_BWD))
+        assert plain <= packed <= plain + n * hw * hw * c * 2 + 256, (n, c, hw, groups)
+
+
 # ---- packing on the device ------------------------------------------------------------------------------------------
 def _values(count, dtype, seed):
     """Every kind of group: ordinary, all zero, one value, values at a tie, the type's largest and smallest, infinities, NaN."""
