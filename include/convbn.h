@@ -418,7 +418,8 @@ const char *convbn_status_string(int status);
  * "umma-subpixel", "umma-stem", "stem-mma", "depthwise", "grouped-mma", "grouped-umma", and for
  * CONVBN_PHASE_TUNE_BWD "umma-fused-bwd" (the 1x1 kernel that reads dZ once) or "two-calls" (everything else, whatever
  * the number of launches); CONVBN_PHASE_TUNE_BWD_PACKED "umma-fused-bwd" (that kernel from codes), "umma" (the weight gradient
- * restores X on its way) or "unpack" (X restored into the workspace first); CONVBN_PHASE_DEPLOY_FWD_QUANT "umma" or "mma" (few rows).
+ * restores X on its way) or "unpack" (X restored into the workspace first); CONVBN_PHASE_DEPLOY_FWD_QUANT "umma-fused" (codes stay on chip),
+ * "umma" (codes in the workspace) or "mma" (few rows).
  * Static string, never NULL. */
 const char *convbn_last_kernel(int phase);
 

@@ -1500,7 +1500,7 @@ int convbn_deploy_fwd_quant(const convbn_desc *desc, const void *x, const void *
     cudaStream_t st = (cudaStream_t)stream;
     if (quant_fused_eligible(pb, (int)elem_size(desc->dtype))) {
         LAUNCH("quant_fused", launch_quant_fused(pb, storage_type(desc), x, w_codes, w_scale, b_fused, add, relu ? 1 : 0, z, st));
-        t_last_kernel[CONVBN_PHASE_DEPLOY_FWD_QUANT] = "umma";
+        t_last_kernel[CONVBN_PHASE_DEPLOY_FWD_QUANT] = "umma-fused";
         return CONVBN_OK;
     }
     if (quant_small_eligible(pb)) {

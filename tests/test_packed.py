@@ -337,6 +337,38 @@ def test_packed_backward_against_the_oracle(spec, mask, with_add):
     _compare(spec, t, got, _reference(spec, t, add, mask), add, mask)
 
 
+# which kernels take X as it is packed (the single kernel from 512 pixels on); the others restore it first
+PATHS = dict({s.name: "umma-fused-bwd" for s in LAYERS[:6]}, wide_few_pixels="umma", one_pixel="umma", rows="umma", rows_wide="umma", reduce="umma")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("spec", LAYERS, ids=lambda s: s.name)
+def test_which_kernels_a_layer_takes(spec, dtype):
+    import dataclasses
+    if spec.dtype == "bf16":
+        spec = dataclasses.replace(spec, dtype=dtype)
+    _packed_pass(spec, parity.make_inputs(spec, 2), None, False, expect=PATHS.get(spec.name, "unpack"))
+
+
+# few taps, borders and dilations in the weight gradient that restores X on its way
+FEW_TAPS = [I.LayerSpec("pair", 2, 64, 9, 11, 64, 1, 2), I.LayerSpec("column", 2, 1024, 9, 7, 64, 3, 1),
+            I.LayerSpec("dilated_row", 3, 1024, 6, 10, 128, 1, 3, dil=2), I.LayerSpec("four", 1, 1024, 8, 7, 128, 2, 2),
+            I.LayerSpec("four_with_border", 2, 1024, 6, 5, 64, 2, 2, pad=1), I.LayerSpec("border_1x1", 2, 64, 6, 9, 128, 1, 1, pad=1)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("spec", FEW_TAPS, ids=lambda s: s.name)
+def test_few_taps_against_the_oracle(spec, dtype):
+    import dataclasses
+    spec = dataclasses.replace(spec, dtype=dtype, bias=True)
+    t = _relu_inputs(spec, 3)
+    add = ROUND[dtype](np.random.default_rng(1).standard_normal(t["x"].shape).astype(np.float32))
+    got = _packed_pass(spec, t, add, True, expect="umma")
+    _compare(spec, t, got, _reference(spec, t, add, True), add, True)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("spec", [s for s in LAYERS if s.name in ("wide_in", "wide_out", "rows", "reduce", "conv3", "shortcut")], ids=lambda s: s.name)
 def test_packed_backward_in_half_with_bias_deferred(spec):

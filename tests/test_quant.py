@@ -154,6 +154,48 @@ def test_forward_against_the_definition(size, dtype):
         _check(_run(t, _desc(n, ci, h, w, co, dtype), dtype, relu), t, dtype, 1, relu)
 
 
+# rows to codes on the way to the product; codes in the workspace first (the others: few rows, one launch)
+FUSED = [(19000, 256, 1, 1, 64), (20001, 64, 1, 1, 256), (19500, 128, 1, 1, 200), (25000, 192, 1, 1, 320), (19001, 40, 1, 1, 129),
+         (40000, 16, 1, 1, 8), (31, 64, 27, 28, 640)]
+TWO_KERNELS = [(300, 2000, 1, 1, 72), (2, 2048, 7, 7, 512), (40, 512, 7, 7, 2048), (6, 192, 21, 19, 320), (9500, 520, 1, 1, 1032),
+               (1700, 1032, 1, 1, 1500), (300, 4104, 1, 1, 2056), (19200, 256, 1, 1, 1032)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_which_kernels_a_size_takes(dtype):
+    import torch
+    units = 128 * torch.cuda.get_device_properties(0).multi_processor_count      # rows that give every SM a unit
+    td = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[dtype]
+    zeros = lambda count, t=torch.float32: torch.zeros(count, dtype=t, device="cuda")
+
+    def taken(n, ci, h, w, co, stride=1):
+        d = _desc(n, ci, h, w, co, dtype, stride)
+        ho, wo = C.convbn_out_shape(d)
+        size = C.convbn_workspace_bytes(d, C.PHASE_DEPLOY_FWD_QUANT)
+        C.convbn_deploy_fwd_quant(d, zeros(n * h * w * ci, td), zeros(co * (-(-ci // 16) * 16), torch.int8), zeros(co), zeros(co),
+                                  zeros(n * ho * wo * co, td), None, False, zeros(max(256, size), torch.uint8))
+        C.convbn_check()
+        name = C.convbn_last_kernel(C.PHASE_DEPLOY_FWD_QUANT)
+        assert (size > 0) == (name == "umma")
+        return name, n * ho * wo
+
+    for size in SIZES:
+        n, ci, h, w, co = size
+        if dtype == "f32" and h * w > 1:
+            n, h, w = n * h * w, 1, 1
+        name, rows = taken(n, ci, h, w, co)
+        if size in FUSED:
+            assert rows < units or name == "umma-fused", (size, name)
+        else:
+            assert name == ("umma" if size in TWO_KERNELS else "mma"), (size, name)
+    if dtype == "f32":
+        return
+    for size, fused in (((14, 256, 111, 114, 64), True), ((7, 96, 160, 161, 40), False)):
+        name, rows = taken(*size, stride=2)
+        assert rows >= units and name == ("umma-fused" if fused else "umma"), (size, name)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("size", [(2, 256, 15, 14, 512), (1, 40, 7, 9, 24), (3, 512, 28, 28, 128), (14, 256, 111, 114, 64), (7, 96, 160, 161, 40)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("stride", [2, 3])
