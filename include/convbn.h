@@ -211,8 +211,9 @@ int convbn_tune_bwd_weight_noalloc(const convbn_desc *desc, const void *dz, cons
  *   code   x 2^-e rounded to the nearest integer (ties to even), at most 127 in magnitude, and 1 or -1 where that is 0
  *          but x is not: x > 0 exactly where code > 0
  * A group that holds an infinity or a NaN: step byte 255, codes 0; all of it is restored as NaN.
- * An element is off by half a step at most, which is between 2^-8 and 2^-7 of the group's largest magnitude; a magnitude below
- * half a step is off by less than one step (it stands for a whole one), and where e is held at a bound the step is that bound's.
+ * An element is off by half a step at most, which is between 1/255 and 1/127.5 of the group's largest magnitude (where e is held at
+ * its lower bound, the step is 2^-126 or 2^-24).  Off by less than one step are a magnitude below half a step, which stands for a whole
+ * one, and, where e is held at its upper bound, one above 127.5 steps, which stands for 127 (fp32 above 127.5 2^121, half above 65280).
  * convbn_unpack restores the values, without rounding, in any of the three types that they fit.
  * All pointers device, 16-byte aligned, no overlap.  A count of 0 is a no-op that looks at no pointer.  CONVBN_EINVAL for a
  * count below 0 or above 2^40, an unknown dtype or (count > 0) a NULL pointer; CONVBN_EALIGN; CONVBN_ECUDA. */

@@ -27,6 +27,33 @@ def test_the_definition_keeps_signs_and_half_a_step(dtype):
     np.testing.assert_array_equal(ROUND[dtype](back), back)              # exact in the storage type
 
 
+@pytest.mark.parametrize("dtype,largest,step", [("bf16", 255 * 2.0 ** 120, 2.0 ** 121), ("f32", float(np.float32(3.4028235e38)), 2.0 ** 121),
+                                                ("f16", 65504.0, 512.0)])
+def test_the_definition_at_the_largest_values(dtype, largest, step):
+    """Steps are held at their upper bound there: what is above 127.5 of them stands for 127, less than one step away."""
+    rng = np.random.default_rng(5)
+    for top in (largest, 127.5 * step, 127.4 * step, 64 * step, 63.75 * step):
+        x = ROUND[dtype]((rng.uniform(-1, 1, 32) * top).astype(np.float32)).astype(np.float64)
+        x[7] = ROUND[dtype](np.float32(top)) * (-1) ** int(rng.integers(2))
+        q, s = P.pack(x, dtype)
+        assert 2.0 ** (int(s[0]) - 127) == step and np.abs(q.astype(int)).max() <= 127
+        err = np.abs(P.unpack(q, s) - x)
+        cut, small = np.abs(x) > 127.5 * step, np.abs(x) < step / 2
+        assert np.all(err[cut] < step) and np.all(err[small] < step) and np.all(err[~cut & ~small] <= step / 2)
+        assert dtype != "bf16" or not cut.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_half_a_step_against_the_largest_magnitude(dtype):
+    """Between 1/255 and 1/127.5 of it, and as near to both as the type has values."""
+    tops = np.unique(ROUND[dtype](np.append(np.linspace(60, 128, 20000), 63.75).astype(np.float32))).astype(np.float64)
+    x = np.zeros((tops.size, 32))
+    x[:, 3] = tops
+    _, s = P.pack(x.ravel(), dtype)
+    share = 2.0 ** (s.astype(float) - 128) / tops
+    assert share.min() > 1 / 255 and share.max() == 1 / 127.5 and share.min() < 1.01 / 255
+
+
 # ---- refusals (host) -------------------------------------------------------------------------------------------------
 def test_pack_refusals():
     lib, ok = C.lib(), 4096
