@@ -273,7 +273,8 @@ int convbn_deploy_bwd(const convbn_desc *desc, const void *dz, const void *x,
  *               z = (sum_k xq w_codes) (a / 127) w_scale + b_fused,   with `add` z + add, with relu != 0 max(z, 0)
  * with i = fl(127 fl(1 / a)) in fp32 and the product rounded once, to the nearest integer (ties to even).
  * The BatchNorm scale s is part of the channel scale: the codes are omega's own.  Products are exact, sums exact in 32 bits;
- * one rounding to the storage type, when z is written.  A row or a channel whose largest magnitude is below 2^-100 counts as zero; one
+ * one rounding to the storage type, when z is written.  z is formed in fp32 from the left to the right: where |sum| (a / 127) passes
+ * fp32's range it is infinite, whatever w_scale is.  A row or a channel whose largest magnitude is below 2^-100 counts as zero; one
  * with an infinity or a NaN gives NaN (which max(., 0) turns into 0, as convbn_relu does).
  * w_codes: signed bytes [C_out][C_in rounded up to a multiple of 16], the added columns zero.  w_scale, b_fused [C_out] fp32.
  * Layers: kh = kw = 1, no padding, groups = 1, any stride, C_in <= 131072, fewer than 2^31 - 256 output pixels; NHWC 16-bit storage,

@@ -20,7 +20,9 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top) {      // bits of th
     if (a < kQuantTiny) return {0.f, 0.f};
     return {__fmul_rn(__frcp_rn(a), 127.f), __fmul_rn(a, 1.f / 127.f)};
 }
-// 1.5 2^23 + code: the code is the low byte.  |x inv| <= 127 (1 + 2^-23), so no clamp; the product is exact inside the fma.
+// 1.5 2^23 + code: the code is the low byte; the product is exact inside the fma.  No clamp: |x inv| is at most 127 (1 + 2^-23), and
+// 127 (1 + 2^-21) for maxima above 2^126, whose reciprocals are subnormal (they must not be flushed) and have 21 bits or more; from 127.5
+// on it would be 128.
 __device__ __forceinline__ uint32_t code_bits(float x, float inv) { return __float_as_uint(fmaf(x, inv, 12582912.f)); }
 __device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);

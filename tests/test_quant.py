@@ -238,6 +238,36 @@ def test_rows_and_channels_that_are_zero_tiny_infinite_or_not_numbers(rows):
     assert np.array_equal(np.isnan(got), bad) and np.isfinite(got[~bad]).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,largest", [("bf16", 255 * 2.0 ** 120), ("f32", 1.9 * 2.0 ** 127), ("f16", 65504.0)])
+@pytest.mark.parametrize("rows,ci,kernel", [(5, 128, "mma"), (64, 2048, "umma"), (19008, 128, "umma-fused")])
+def test_rows_and_channels_near_the_largest_value(rows, ci, kernel, dtype, largest):
+    """Reciprocals of maxima above 2^126 are subnormal.  Channel c has its largest weight where rows are zero and code 1 at one other
+    place, so z is a row's code there, one after the other, times the scales: no sum passes the range."""
+    rng = np.random.default_rng(9)
+    t = _draw(rows, ci, 1, 1, 64, dtype, 1, False, False)
+    t["beta"], t["mu_hat"] = t["beta"] * 0, t["mu_hat"] * 0
+    t["w"] = np.zeros((64, ci))
+    t["w"][:, 1] = ROUND[dtype](rng.uniform(0.5, 1.0, 64).astype(np.float32))
+    t["w"][np.arange(64), 2 + np.arange(64)] = ROUND[dtype]((t["w"][:, 1] * 0.0082).astype(np.float32))
+    t["x"][..., 1] = 0.0
+    plain = t["x"].copy()
+    for r, top in enumerate((largest, largest / 2, largest / 1.9, 1.01 * largest / 2)):
+        t["x"][r] = ROUND[dtype]((rng.uniform(-1, 1, ci) * top).astype(np.float32))
+        t["x"][r, 0, 0, :2] = float(ROUND[dtype](np.float32(-top))), 0.0
+    got = _run(t, _desc(rows, ci, 1, 1, 64, dtype), dtype, False)
+    assert C.convbn_last_kernel(C.PHASE_DEPLOY_FWD_QUANT) == kernel and np.isfinite(got["z"]).all()
+    assert set(np.unique(got["w_codes"])) == {0, 1, 127}
+    _check(got, t, dtype, 1, False)
+    # channels of such weights
+    t["x"] = plain
+    scale = largest / t["w"][:4, 1] / np.array([1.0, 2.0, 1.9, 1.98])
+    t["w"][:4] = ROUND[dtype]((t["w"][:4] * scale[:, None]).astype(np.float32))
+    got = _run(t, _desc(rows, ci, 1, 1, 64, dtype), dtype, False)
+    assert np.isfinite(got["w_scale"]).all()
+    _check(got, t, dtype, 1, False)
+
+
 # ---- together, as a deployed network uses them ---------------------------------------------------------------------------
 @pytest.mark.gpu
 def test_a_deployed_bottleneck_of_three_calls_captured_and_replayed():
