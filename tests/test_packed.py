@@ -655,3 +655,129 @@ def test_sums_over_many_pixels_of_other_layers(layer, dtype):
     bound = (64 if emptied[0 if dtype == "f16" else 1] else 384) * 2 / 3 * 2.0 ** -24 + 2.0 ** -20
     assert rel(dw, exact) <= bound and rel(dbeta, total) <= bound, (rel(dw, exact), rel(dbeta, total), bound)
     assert rel(dgamma, (exact * wt.double()).sum((1, 2, 3))) <= bound * 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("ci,co", [(256, 64), (64, 256)])
+def test_no_number_in_the_single_kernel(ci, co, dtype):
+    """test_a_group_that_is_no_number_shows_in_the_gradients with pixels enough for the kernel that reads dZ once."""
+    spec = I.LayerSpec("inf", 3, ci, 30, 20, co, 1, 1, dtype=dtype)
+    t = parity.make_inputs(spec, 4)
+    t["x"][2, 40, 29, 18], t["x"][1, 5, 2, 3] = -np.inf, np.nan
+    got = _packed_pass(spec, t, None, True, expect="umma-fused-bwd")
+    assert np.isnan(got["dw"][:, :64]).all() and np.isfinite(got["dw"][:, 64:]).all()
+    assert not got["dx"][2, 32:64, 29, 18].any() and not got["dx"][1, :32, 2, 3].any()
+    assert np.isfinite(got["dx"]).all() and np.isfinite(got["dbeta"]).all()
+
+
+@pytest.mark.gpu
+def test_a_weight_gradient_that_restores_more_than_two_to_the_31_elements():
+    """Only rows beyond the 2^31st element have a dZ that is not zero; whole numbers, so the sums are exact in fp32 in any order."""
+    import torch
+    rows, ci, co, tail = 2_200_000, 1024, 64, 100_000
+    g = torch.Generator("cuda").manual_seed(1)
+    codes = torch.empty(rows, ci, dtype=torch.int8, device="cuda")
+    for at in range(0, rows, 500_000):
+        codes[at:at + 500_000].random_(-3, 4, generator=g)
+    steps = torch.full((rows, ci // 32), 127, dtype=torch.uint8, device="cuda")
+    assert (rows - tail) * ci > 1 << 31
+    dz = torch.zeros(rows, co, dtype=torch.bfloat16, device="cuda")
+    dz[rows - tail:] = torch.randint(-2, 3, (tail, co), device="cuda", generator=g).to(torch.bfloat16)
+    w = torch.randint(-2, 3, (co, ci), device="cuda", generator=g).to(torch.bfloat16)
+    d = C.convbn_linear_desc(rows, ci, co)
+    mean, saved = torch.zeros(co, device="cuda"), torch.ones(3 * co, device="cuda")
+    dx = torch.full((rows, ci), 7.0, dtype=torch.bfloat16, device="cuda")
+    dw, dgamma, dbeta = torch.empty(co, ci, device="cuda"), torch.empty(co, device="cuda"), torch.empty(co, device="cuda")
+    ws = torch.empty(C.convbn_workspace_bytes(d, C.PHASE_TUNE_BWD_PACKED), dtype=torch.uint8, device="cuda")
+    C.convbn_tune_bwd_packed(d, dz, codes, steps, w, None, mean, saved, dx, dw, None, dgamma, dbeta, None, True, False, ws)
+    C.convbn_check()
+    assert C.convbn_last_kernel(C.PHASE_TUNE_BWD_PACKED) == "umma"
+    last, q = dz[rows - tail:].double(), codes[rows - tail:]
+    assert torch.equal(dw.double(), last.t() @ q.double()) and torch.equal(dbeta.double(), last.sum(0))
+    want = (last @ w.double()).to(torch.bfloat16) * (q > 0)
+    assert torch.equal(dx[rows - tail:], want) and not bool(dx[:rows - tail].any())
+
+
+def _call(spec, seed):
+    """A packed backward call on tensors of its own: (call, outputs)."""
+    import torch
+    from paper_2305_11624_b200.harness import Block
+    blk = Block(spec, modes=("tune", "packed"))
+    blk.randomize(seed)
+    blk.tune_fwd()
+    blk.pack_x()
+    outputs = [o for o in (blk.dx, blk.dw, blk.db, blk.dgamma, blk.dbeta) if o is not None]
+    return lambda defer=False: blk.tune_bwd_packed(relu_mask=True, defer_join=defer), outputs
+
+
+AT_ONCE = [("wide_in", 8, 256, 40, 41, 64, 1, 1), ("restoring", 8, 512, 28, 28, 128, 1, 1), ("shortcut", 4, 256, 28, 28, 512, 1, 2),
+           ("conv3", 9, 64, 56, 56, 64, 3, 1)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_the_same_call_gives_the_same_bits(dtype):
+    import torch
+    more = [("many_rows", 150000, 64, 1, 1, 128, 1, 1), ("wide_rows", 60000, 1024, 1, 1, 64, 1, 1), ("conv3_long", 64, 64, 112, 112, 64, 3, 1)]
+    for name, n, ci, h, w, co, k, stride in AT_ONCE + more:
+        call, outputs = _call(I.LayerSpec(name, n, ci, h, w, co, k, k, stride=stride, pad=k // 2, dtype=dtype), 3)
+        call()
+        first = [o.clone() for o in outputs]
+        for o in outputs:
+            o.fill_(float("nan"))
+        call()
+        C.convbn_check()
+        assert all(torch.equal(a, b) for a, b in zip(first, outputs)), name
+
+
+@pytest.mark.gpu
+def test_packed_calls_of_two_threads_on_streams_of_their_own():
+    """Backward passes, some with a deferred join, beside packing and restoring on another thread and stream: the bits of the calls
+    made one after the other."""
+    import threading
+    import torch
+    work, expected = [], []
+    for i, (name, n, ci, h, w, co, k, stride) in enumerate(AT_ONCE):
+        call, outputs = _call(I.LayerSpec(name, n, ci, h, w, co, k, k, stride=stride, pad=k // 2, dtype="f16" if i % 2 else "bf16"), i)
+        call()
+        work.append((call, outputs))
+        expected.append([o.clone() for o in outputs])
+    x = torch.randn(3_000_001, device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(torch.bfloat16)
+    codes, steps, back = torch.empty(x.numel(), dtype=torch.int8, device="cuda"), torch.empty(-(-x.numel() // 32), dtype=torch.uint8, device="cuda"), torch.empty_like(x)
+    C.convbn_pack(x, codes, steps)
+    C.convbn_unpack(codes, steps, back)
+    packed = (codes.clone(), steps.clone(), back.clone())
+    for _, outputs in work:
+        for o in outputs:
+            o.fill_(float("nan"))
+    C.convbn_check()
+    torch.cuda.synchronize()
+    failed = []
+
+    def run(mine):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for turn in range(12):
+                    for i in mine:
+                        work[i][0](turn % 2 == 1)
+                        if turn % 2:
+                            C.convbn_tune_bwd_join()
+                    if 0 in mine:
+                        C.convbn_pack(x, codes, steps)
+                        C.convbn_unpack(codes, steps, back)
+            stream.synchronize()
+        except Exception as e:                                           # (shown by the main thread)
+            failed.append(e)
+
+    threads = [threading.Thread(target=run, args=(mine,)) for mine in ((0, 1), (2, 3))]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not failed, failed
+    C.convbn_check()
+    for (_, outputs), want in zip(work, expected):
+        assert all(torch.equal(a, b) for a, b in zip(outputs, want))
+    assert all(torch.equal(a, b) for a, b in zip((codes, steps, back), packed))

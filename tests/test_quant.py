@@ -206,6 +206,17 @@ def test_strided_shortcuts(size, stride):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size,stride,kernel", [((14, 256, 111, 114, 64), 2, "umma-fused"), ((7, 96, 160, 161, 40), 2, "umma"),
+                                                ((2, 256, 15, 14, 512), 3, "mma")], ids=lambda s: "x".join(map(str, s)) if type(s) is tuple else s)
+def test_strided_shortcuts_in_half(size, stride, kernel):
+    n, ci, h, w, co = size
+    t = _draw(n, ci, h, w, co, "f16", stride, True, True)
+    got = _run(t, _desc(n, ci, h, w, co, "f16", stride), "f16", True)
+    assert C.convbn_last_kernel(C.PHASE_DEPLOY_FWD_QUANT) == kernel
+    _check(got, t, "f16", stride, True)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,ci", [(40, 64), (20000, 64), (20000, 256), (3000, 512)])
 def test_strides_that_leave_no_pixel_out(rows, ci, dtype):
@@ -329,3 +340,45 @@ def test_inputs_of_more_than_two_to_the_31_elements(rows, ci, co):
         C.convbn_check()
         out.append(z[part.shape[0] - tail:].clone())
     assert torch.equal(out[0], out[1]) and bool(out[0].float().abs().sum() > 0)
+
+
+@pytest.mark.gpu
+def test_calls_of_two_threads_on_streams_of_their_own():
+    """Each kernel beside each other one, with workspaces of their own: the bits of the calls made one after the other."""
+    import threading
+    import torch
+    from paper_2305_11624_b200.harness import Block
+    blocks = [Block(I.LayerSpec("t%d" % i, *s, 1, 1), modes=("quant",)) for i, s in
+              enumerate([(60, 256, 28, 28, 64), (40, 512, 20, 20, 640), (40, 64, 28, 28, 256), (1, 2048, 1, 1, 1000)])]
+    expected = []
+    for k, b in enumerate(blocks):
+        b.randomize(k)
+        b.deploy_prepare_quant()
+        b.deploy_fwd_quant(relu=True)
+        expected.append((b.z.clone(), b.w_codes.clone(), b.w_scale.clone(), b.b_fused.clone()))
+        b.z.fill_(float("nan"))
+    C.convbn_check()
+    torch.cuda.synchronize()
+    failed = []
+
+    def run(mine):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(30):
+                    for b in mine:
+                        b.deploy_prepare_quant()
+                        b.deploy_fwd_quant(relu=True)
+            stream.synchronize()
+        except Exception as e:                                           # (shown by the main thread)
+            failed.append(e)
+
+    threads = [threading.Thread(target=run, args=(mine,)) for mine in (blocks[:2], blocks[2:])]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not failed, failed
+    C.convbn_check()
+    for b, want in zip(blocks, expected):
+        assert all(torch.equal(a, e) for a, e in zip((b.z, b.w_codes, b.w_scale, b.b_fused), want))
