@@ -758,9 +758,13 @@ typedef CUresult (*EncodeIm2colFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_
                                    const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                    CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeTiledFn g_encode_tiled = nullptr;
+typedef CUresult (*ContextFn)(CUcontext *);
 EncodeIm2colFn g_encode_im2col = nullptr;
+ContextFn g_current_context = nullptr;
 std::once_flag g_encode_once;
 
+// The driver encodes a tensor map in a thread that has a context.  One whose first CUDA call this is has none yet (the runtime binds the
+// device's with the first call that needs it): it gets the current device's here.
 bool load_encoders() {
     std::call_once(g_encode_once, [] {
         void *f = nullptr;
@@ -772,8 +776,15 @@ bool load_encoders() {
         if (cudaGetDriverEntryPoint("cuTensorMapEncodeIm2col", &f, cudaEnableDefault, &q) == cudaSuccess &&
             q == cudaDriverEntryPointSuccess)
             g_encode_im2col = (EncodeIm2colFn)f;
+        f = nullptr;
+        if (cudaGetDriverEntryPoint("cuCtxGetCurrent", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+            g_current_context = (ContextFn)f;
     });
-    return g_encode_tiled && g_encode_im2col;
+    if (!g_encode_tiled || !g_encode_im2col || !g_current_context) return false;
+    CUcontext context = nullptr;
+    if (g_current_context(&context) == CUDA_SUCCESS && context) return true;
+    int device = 0;
+    return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess;
 }
 
 }  // namespace

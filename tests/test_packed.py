@@ -781,3 +781,62 @@ def test_packed_calls_of_two_threads_on_streams_of_their_own():
     for (_, outputs), want in zip(work, expected):
         assert all(torch.equal(a, b) for a, b in zip(outputs, want))
     assert all(torch.equal(a, b) for a, b in zip((codes, steps, back), packed))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("what", ["umma-fused-bwd", "umma", "unpack", "tune_fwd", "tune_bwd", "strip", "stem", "grouped", "depthwise", "conv_transposed",
+                                  "quant-mma", "quant-umma", "quant-umma-fused", "deploy"])
+def test_the_first_cuda_call_of_a_thread(what):
+    """A thread that has made no CUDA call has no context: the library's first call there makes the device's current."""
+    import threading
+    import torch
+    from paper_2305_11624_b200.harness import Block
+    sizes = {"umma-fused-bwd": (3, 256, 20, 15, 64, 1, 1), "umma": (3, 512, 9, 8, 128, 1, 1), "unpack": (3, 128, 9, 8, 512, 1, 1),
+             "tune_fwd": (3, 512, 9, 8, 128, 1, 1), "tune_bwd": (3, 256, 20, 15, 64, 1, 1), "strip": (2, 64, 20, 24, 64, 3, 1),
+             "stem": (2, 3, 64, 64, 64, 7, 2), "grouped": (2, 64, 10, 12, 64, 3, 1), "depthwise": (2, 96, 12, 11, 96, 3, 1),
+             "conv_transposed": (2, 128, 14, 14, 64, 3, 2), "quant-mma": (7, 64, 1, 1, 64, 1, 1), "quant-umma": (64, 2048, 1, 1, 64, 1, 1),
+             "quant-umma-fused": (20000, 64, 1, 1, 64, 1, 1), "deploy": (3, 512, 9, 8, 128, 1, 1)}
+    n, ci, h, w, co, k, stride = sizes[what]
+    groups = {"grouped": 8, "depthwise": 96}.get(what, 1)
+    mode = ("quant",) if what.startswith("quant") else ("deploy",) if what == "deploy" else ("tune", "packed")
+    blk = Block(I.LayerSpec("first", n, ci, h, w, co, k, k, stride=stride, pad=k // 2, groups=groups), modes=mode)
+    blk.randomize(1)
+    stream = torch.cuda.Stream()
+    if mode == ("quant",):
+        call, outputs = lambda: blk.deploy_fwd_quant(stream=stream.cuda_stream), ("z",)
+        blk.deploy_prepare_quant()
+    elif mode == ("deploy",):
+        call, outputs = lambda: blk.deploy_fwd(stream=stream.cuda_stream), ("z",)
+        blk.deploy_prepare()
+    else:
+        blk.tune_fwd()
+        blk.pack_x()
+        if what in ("umma-fused-bwd", "umma", "unpack"):
+            call = lambda: blk.tune_bwd_packed(stream=stream.cuda_stream)
+        elif what in ("tune_fwd", "strip", "stem", "grouped", "depthwise"):
+            call = lambda: blk.tune_fwd(stream=stream.cuda_stream)
+        else:
+            call = lambda: blk.tune_bwd(stream=stream.cuda_stream)
+        outputs = ("z",) if what in ("tune_fwd", "strip", "stem", "grouped", "depthwise") else ("dx", "dw", "dgamma", "dbeta")
+    torch.cuda.synchronize()
+    call()                                                               # (set-up that is made once a process is done)
+    stream.synchronize()
+    want = [getattr(blk, o).clone() for o in outputs]
+    for o in outputs:
+        getattr(blk, o).fill_(float("nan"))
+    torch.cuda.synchronize()
+    failed = []
+
+    def run():
+        try:
+            call()
+        except Exception as e:
+            failed.append(e)
+
+    thread = threading.Thread(target=run)
+    thread.start()
+    thread.join()
+    assert not failed, failed
+    stream.synchronize()
+    C.convbn_check()
+    assert all(torch.equal(getattr(blk, o), e) for o, e in zip(outputs, want))
