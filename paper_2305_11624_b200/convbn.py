@@ -420,17 +420,23 @@ def _packed_pair(x, codes, steps, where):
 
 def convbn_pack(x, codes, steps, stream=None):
     """x in 8 bits: a signed code per element, a step byte per 32 consecutive ones, in the order of x in memory."""
-    kind = _storage(x)
-    _packed_pair(x, codes, steps, "convbn_pack")
-    status = (_native or _calls()).convbn_pack(kind, x, codes, steps, x.numel(), stream)
+    native = _native or _calls()
+    status = native.pack(x, codes, steps, stream)
+    if status is None:           # what is wrong, or else addresses or another order of the dimensions
+        kind = _storage(x)
+        _packed_pair(x, codes, steps, "convbn_pack")
+        status = native.convbn_pack(kind, x, codes, steps, x.numel(), stream)
     if status:
         _raise(status, "convbn_pack")
 
 
 def convbn_unpack(codes, steps, out, stream=None):
-    kind = _storage(out)
-    _packed_pair(out, codes, steps, "convbn_unpack")
-    status = (_native or _calls()).convbn_unpack(kind, codes, steps, out, out.numel(), stream)
+    native = _native or _calls()
+    status = native.unpack(codes, steps, out, stream)
+    if status is None:
+        kind = _storage(out)
+        _packed_pair(out, codes, steps, "convbn_unpack")
+        status = native.convbn_unpack(kind, codes, steps, out, out.numel(), stream)
     if status:
         _raise(status, "convbn_unpack")
 
@@ -440,11 +446,13 @@ def convbn_tune_bwd_packed(desc, dz, codes, steps, w, b, run_mean, saved, dx, dw
     """convbn_tune_bwd_glue with X as convbn_pack left it."""
     if type(desc) is not Desc:
         desc = _desc(desc)
-    if desc is not None:
+    native = _native or _calls()
+    args = (desc, dz, codes, steps, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta, add, 1 if relu_mask else 0, 1 if begin else 0,
+            workspace, workspace_bytes, stream)
+    status = native.tune_bwd_packed(*args)
+    if status is None:           # (too short, or addresses)
         _packed_room(codes, steps, desc.n * desc.c_in * desc.h_in * desc.w_in, "convbn_tune_bwd_packed")
-    status = (_native or _calls()).convbn_tune_bwd_packed(desc, dz, codes, steps, w, b, run_mean, saved, dx, dw, db, dgamma, dbeta,
-                                                          add, 1 if relu_mask else 0, 1 if begin else 0, workspace,
-                                                          workspace_bytes, stream)
+        status = native.convbn_tune_bwd_packed(*args)
     if status:
         _raise(status, "convbn_tune_bwd_packed")
 

@@ -230,6 +230,28 @@ def test_pack_and_unpack_are_exact(dtype, count):
 
 
 @pytest.mark.gpu
+def test_packing_takes_channels_last_tensors_and_addresses():
+    """In the order of memory: an NCHW tensor stored as NHWC is packed as NHWC."""
+    import torch
+    x = torch.randn(2, 24, 7, 9, device="cuda").to(torch.bfloat16).to(memory_format=torch.channels_last)
+    codes, steps = torch.full((x.numel(),), 99, dtype=torch.int8, device="cuda"), torch.full((95,), 99, dtype=torch.uint8, device="cuda")
+    q, s = P.pack(x.permute(0, 2, 3, 1).float().cpu().numpy().ravel(), "bf16")
+    for c, t in ((codes, steps), (codes.data_ptr(), steps.data_ptr()), (codes.view(torch.uint8), steps.data_ptr())):
+        codes.fill_(99)
+        C.convbn_pack(x, c, t)
+        C.convbn_check()
+        assert np.array_equal(codes.cpu().numpy(), q) and np.array_equal(steps.cpu().numpy(), s)
+        out = torch.empty_like(x)
+        C.convbn_unpack(c, t, out)
+        C.convbn_check()
+        np.testing.assert_array_equal(out.permute(0, 2, 3, 1).float().cpu().numpy().ravel().astype(np.float64), P.unpack(q, s))
+    with pytest.raises(C.ConvBNError):
+        C.convbn_pack(x, codes.cpu(), steps)
+    with pytest.raises(C.ConvBNError):
+        C.convbn_unpack(codes, steps, x.cpu())
+
+
+@pytest.mark.gpu
 def test_a_type_that_is_not_a_storage_type_is_refused():
     import torch
     x = torch.zeros(64, dtype=torch.float64, device="cuda")
