@@ -224,7 +224,12 @@ int convbn_unpack(int dtype, const void *codes, const void *steps, void *out, lo
  * of desc.layout): the values of that call for the restored X, but that dX + add may be rounded once instead of twice, and that
  * the parameter gradients' sums over many pixels are cut into shorter ones; relu_mask: dx = 0 where the code is not positive.
  * Codes and steps belong to the library like X does (begin != 0: until the join).
- * Workspace: convbn_workspace_bytes(desc, CONVBN_PHASE_TUNE_BWD_PACKED).  Errors as for convbn_tune_bwd_glue. */
+ * Workspace: convbn_workspace_bytes(desc, CONVBN_PHASE_TUNE_BWD_PACKED).  Errors as for convbn_tune_bwd_glue.
+ * What packing saves is what is kept between the two passes, in a chain of layers whose calls share a workspace.  The call itself takes
+ * X as it is packed for dense 16-bit layers of unit stride, channels in multiples of 64 and few weights per input channel (kh kw
+ * ceil(C_out / 128) <= 2, from 1024 input channels on <= 4): codes, steps and workspace are then 0.5 to 0.8 of X and the workspace of
+ * convbn_tune_bwd.  All other layers have X restored whole in the workspace, and bf16 1x1 layers of many pixels have a partial tensor of the
+ * weights there for every 6144 of them: 1.1 to 2.1 times X and that workspace, for the length of the call. */
 int convbn_tune_bwd_packed(const convbn_desc *desc, const void *dz, const void *codes, const void *steps, const void *w,
                            const float *b, const float *run_mean, const void *saved, void *dx, float *dw, float *db,
                            float *dgamma, float *dbeta, const void *add, int relu_mask, int begin, void *workspace,
@@ -273,9 +278,13 @@ int convbn_deploy_bwd(const convbn_desc *desc, const void *dz, const void *x,
  *               z = (sum_k xq w_codes) (a / 127) w_scale + b_fused,   with `add` z + add, with relu != 0 max(z, 0)
  * with i = fl(127 fl(1 / a)) in fp32 and the product rounded once, to the nearest integer (ties to even).
  * The BatchNorm scale s is part of the channel scale: the codes are omega's own.  Products are exact, sums exact in 32 bits;
- * one rounding to the storage type, when z is written.  z is formed in fp32 from the left to the right: where |sum| (a / 127) passes
- * fp32's range it is infinite, whatever w_scale is.  A row or a channel whose largest magnitude is below 2^-100 counts as zero; one
- * with an infinity or a NaN gives NaN (which max(., 0) turns into 0, as convbn_relu does).
+ * one rounding to the storage type, when z is written.
+ * z is formed in fp32 from the left to the right: where |sum| (a / 127) passes fp32's range it is infinite, whatever w_scale is.
+ * A row or a channel whose largest magnitude is below 2^-100 counts as zero; one with an infinity or a NaN gives NaN (which max(., 0)
+ * turns into 0, as convbn_relu does).
+ * It is the faster call for few rows, for wide products, and where convbn_deploy_fwd has no tensor-core form (fp32 rows, channel counts
+ * that are no multiple of 64), and its weights have half the bytes.  For 1x1 layers that are bound by X and Z, which stay in the
+ * storage type, the conversion is extra work and convbn_deploy_fwd the faster call (a ResNet's: by 10 to 50 %, strided ones up to twice).
  * w_codes: signed bytes [C_out][C_in rounded up to a multiple of 16], the added columns zero.  w_scale, b_fused [C_out] fp32.
  * Layers: kh = kw = 1, no padding, groups = 1, any stride, C_in <= 131072, fewer than 2^31 - 256 output pixels; NHWC 16-bit storage,
  * or fp32 with one pixel per image (convbn_linear_desc).  Others: CONVBN_EUNSUPPORTED, workspace size 0.

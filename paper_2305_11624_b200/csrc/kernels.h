@@ -347,9 +347,9 @@ cudaError_t launch_unpack(int dtype, const void *codes, const void *steps, void 
 // length: against 64 bits, relative error of domega per 1000 pixels of a slice 0.7 to 1.5e-6 for half values (1024 -> 512 at 63 x 100: N = 4,
 // 2800 pixels 1.9e-6; N = 23, 16100 pixels 2.0e-5), a quarter of that for bf16.  Slices themselves are added in order by the finishing
 // kernels.  Where accumulators are emptied every 1024 pixels instead, by additions that round, it is 2e-7 (bf16) to 8e-7: with half values
-// in umma_wgrad.cu (SEG) and umma_bwd1x1_packed.cu, with both types for long slices of several taps and stems on a packed copy (3 -> 64 at 225 x 225, N = 256: 43000 pixels
-// a slice 5.0e-5 before in half, 2.6e-5 in bf16).  A stem's window kernel and groups of eight stay at this limit: 5.2e-6 in half (3 -> 64
-// at 224 x 224, N = 256; one accumulator per SM for all rows 1.1e-5; 350 -> 360 us a call).
+// in umma_wgrad.cu (SEG) and umma_bwd1x1_packed.cu, with both types for long slices of several taps and for stems on a packed copy (3 -> 64
+// at 225 x 225, N = 256: 43000 pixels a slice 5.0e-5 before in half, 2.6e-5 in bf16).  A stem's window kernel and groups of eight stay at
+// this limit: 5.2e-6 in half (3 -> 64 at 224 x 224, N = 256; one accumulator per SM for all rows 1.1e-5; 350 -> 360 us a call).
 constexpr long long kExactPixels = 6144;
 
 // The fused backward of a 1x1 layer (fused_bwd1x1_eligible) from packed X: umma_bwd1x1_packed.cu.  partials, bsum: one per CTA

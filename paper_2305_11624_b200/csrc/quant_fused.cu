@@ -5,8 +5,8 @@
 // CTA = 19 warps: 0 weight tiles (TMA), 1 MMA issuer and owner of tensor memory, 2-9 epilogue (two groups of four, an accumulator
 // each), 10-17 rows to codes, 18 brings the rows by TMA into a ring.  A unit of work is 128 rows: they are read whole, a row by 8, 16 or
 // 32 lanes, for their largest magnitudes and again for the codes, which are written as the K-major A operand (128-byte swizzle).
-// Bound by those two readings for long rows, by the epilogue for wide outputs: 256 -> 64 at 56 x 56, N = 256 107 us (78.5 at the
-// measured copy bandwidth), 64 -> 256, N = 128 55.5 (39.3), 128 -> 128, N = 128 40.3 (31.4).
+// Bound by those two readings for long rows, by the epilogue for wide outputs: 256 -> 64 at 56 x 56, N = 256 109 us (78.5 at the
+// measured copy bandwidth), 64 -> 256, N = 128 56.1 (39.3), 128 -> 128, N = 128 41.7 (31.4).
 #include "kernels.h"
 #include "quant8.cuh"
 
@@ -39,7 +39,8 @@ struct QuantFused {
 };
 
 struct QuantCtl {
-    uint64_t rows_full[2][kQMaxDepth], rows_empty[2][kQMaxDepth], full[kQMaxStages], empty[kQMaxStages], wfull, a_full[2], a_empty[2], xs_full[kQSlots], acc_full[2], acc_empty[2], add_full[8];
+    uint64_t rows_full[2][kQMaxDepth], rows_empty[2][kQMaxDepth], full[kQMaxStages], empty[kQMaxStages], wfull, a_full[2], a_empty[2];
+    uint64_t xs_full[kQSlots], acc_full[2], acc_empty[2], add_full[8];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -87,7 +88,10 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         for (int s = 0; s < 8; ++s) {
             mbar_init(&ctl->add_full[s], 1);
         }
-        for (int s = 0; s < 2 * kQMaxDepth; ++s) { mbar_init(&ctl->rows_full[0][0] + s, 1); mbar_init(&ctl->rows_empty[0][0] + s, RowSets<T, LPR>::WARPS); }
+        for (int s = 0; s < 2 * kQMaxDepth; ++s) {
+            mbar_init(&ctl->rows_full[0][0] + s, 1);
+            mbar_init(&ctl->rows_empty[0][0] + s, RowSets<T, LPR>::WARPS);
+        }
         ctl->abort_flag = 0;
         fence_barrier_init();
     }
@@ -208,7 +212,8 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
         // ---- rows to codes ----
         // What a unit costs beside its elements (waits, scales, the hand-over) is most of it where rows are short: two groups, each with an A
         // buffer of its own, halve that and run beside each other, 64 -> 64 at 56 x 56, N = 256 62 -> 51 us; longer rows want the ring in
-        // one piece, 256 -> 64 132 us and 157 by groups (sixteen warps in two groups: 133 where eight in one took 118).  A batch's rows are
+        // one piece, 256 -> 64 132 us and 157 by groups (sixteen warps in two groups: 133 where eight in one took 118; all of these before
+        // row addresses were formed once and waiting warps parked, which took 118 to 109).  A batch's rows are
         // read twice: for their largest magnitudes, and after these have become scales, which each lane works out for one row (a scale
         // per four rows, and the rows kept in registers between: 192 us).
         using R = RowSets<T, LPR>;
@@ -281,7 +286,8 @@ __global__ void __launch_bounds__(kQThreads) quant_fused_kernel(const __grid_con
                     ok = __all_sync(0xffffffffu, mbar_wait_parked(&ctl->a_empty[ab], (use & 1u) ^ 1u, abort_flag));
                     if (!ok) break;
                 }
-                if ((sub & (LPR / BATCH - 1)) == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(xs + (uint32_t)row_of(batch, sub / (LPR / BATCH)) * 4u), "f"(rs.scale) : "memory");
+                if ((sub & (LPR / BATCH - 1)) == 0)
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(xs + (uint32_t)row_of(batch, sub / (LPR / BATCH)) * 4u), "f"(rs.scale) : "memory");
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (!there[h]) continue;
@@ -413,8 +419,9 @@ static bool skips_pixels(const Problem &pb) { return pb.h_out != pb.h_in || pb.w
 
 // Rows enough for every SM, short ones that start on 16-byte boundaries, and not too many channels for two accumulators to drain.  This
 // kernel and the two of quant_gemm.cu, us: 100352 rows 64 -> 256 18.8 and 25.9, 256 -> 64 19.5 and 28.1, 128 -> 128 14.7 and 22.4,
-// 256 -> 1024 75.3 and 79.1, 64 -> 2048 143 and 123; 19200 rows 64 -> 256 7.8 and 9.6, 256 -> 64 8.3 and 8.7; an earlier form of it
-// 512 -> 1024 122.9 and 100.8, and below a unit per SM, 6272 rows 256 -> 64, 7.2 and 6.1: a warp per row beats sixteen rows a warp.
+// 256 -> 1024 75.3 and 79.1, 64 -> 2048 143 and 123; 19200 rows 64 -> 256 7.8 and 9.6, 256 -> 64 8.3 and 8.7; below a unit per SM, 6272
+// rows 256 -> 64, 7.2 and 6.1: a warp per row beats sixteen rows a warp.  256 channels are what 32 lanes read at once; an earlier form,
+// slower by a fifth, that took longer rows in pieces was behind there (512 -> 1024 122.9 and 100.8; this form has not been tried).
 bool quant_fused_eligible(const Problem &pb, int elem_bytes) {
     const bool beside = !skips_pixels(pb);                               // (otherwise im2col boxes of 64 channels)
     return pb.c_in <= 256 && pb.c_in % 8 == 0 && (size_t)pb.c_in * elem_bytes % 16 == 0 && pb.c_out <= 1024 &&

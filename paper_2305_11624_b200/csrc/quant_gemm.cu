@@ -1,13 +1,14 @@
 // The deployed 8-bit product of rows that the kernel of quant_fused.cu does not take (more than 256 channels, ragged ones, wide results)
-// and that are too many for quant_small.cu, as two kernels: rows to codes in the workspace, then a tensor-core GEMM of codes, both operands by TMA, 32-bit integer sums in tensor
-// memory (kind::i8), the epilogue of quant8.cuh.
+// and that are too many for quant_small.cu, as two kernels: rows to codes in the workspace, then a tensor-core GEMM of codes, both
+// operands by TMA, 32-bit integer sums in tensor memory (kind::i8), the epilogue of quant8.cuh.
 //
 // GEMM: CTA = 10 warps: 0 loads, 1 MMA issuer and owner of tensor memory, 2-9 epilogue (two groups of four, an accumulator each).
 // Persistent, tiles of 128 rows x BN channels dealt round-robin, the channel tiles of a row on neighbouring CTAs, so that codes
 // come from L2 after their first reading.  PAIR: two CTAs share a 256 x BN product (cta_group::2), each brings its 128 rows and half of
 // the channels: half the weight bytes into every SM.
-// Bound by the MMAs (kind::i8 runs at twice the 16-bit rate) and the power cap: 65536 rows 2048 -> 2048 227 us, 2.42 POP/s, 0.74 of twice
-// the measured 16-bit rate; the tensor pipe is busy 75 % of 16384 rows' time.
+// Bound by the MMAs (kind::i8 runs at twice the 16-bit rate), and in long runs by the power cap: 65536 rows 2048 -> 2048 166 us with the clock
+// up, 3.3 POP/s, twice the measured 16-bit rate; 199 us at the 1.3 GHz of the cap.  The rows' pass in front of it, in which no MMA runs, takes
+// 52 us: 230 us a call, 268 under the cap.
 #include "kernels.h"
 #include "quant8.cuh"
 

@@ -147,7 +147,8 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
                      mbar_wait_bounded(&ctl->dx_empty[buf], (use & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
                 tc_fence_after_sync();
-                const uint32_t dz_at = smem_u32(dz_tiles + (size_t)s * S::kDzBoxes * kPbBox), x_at = smem_u32(x_tiles + (size_t)s * S::kXBoxes * kPbBox);
+                const uint32_t dz_at = smem_u32(dz_tiles + (size_t)s * S::kDzBoxes * kPbBox);
+                const uint32_t x_at = smem_u32(x_tiles + (size_t)s * S::kXBoxes * kPbBox);
                 const uint32_t dz_k = smem_desc_lo(dz_at, 16), dz_mn = smem_desc_lo(dz_at, kPbBox), x_mn = smem_desc_lo(x_at, kPbBox);
                 // dX tile = dZ tile x omega': K = C_out in steps of 16
                 const uint32_t d_dx = tmem_base + buf * (uint32_t)CI;
@@ -171,7 +172,8 @@ __global__ void __launch_bounds__(kPbThreads) packed_bwd1x1_kernel(const __grid_
 #pragma unroll
                     for (int mb = 0; mb < S::kMBlocks; ++mb) {
                         const uint32_t d = tmem_base + (uint32_t)(S::kDwCol0 + mb * S::kNarrow);
-                        const uint32_t a_lo = (S::kWideIn ? x_mn : dz_mn) + (uint32_t)(2 * mb) * kBox16 + koff, b_lo = (S::kWideIn ? dz_mn : x_mn) + koff;
+                        const uint32_t a_lo = (S::kWideIn ? x_mn : dz_mn) + (uint32_t)(2 * mb) * kBox16 + koff;
+                        const uint32_t b_lo = (S::kWideIn ? dz_mn : x_mn) + koff;
                         umma_bf16_ss_sel(d, a_lo, hi, b_lo, hi, idesc_dw, !first);
                         if (!S::kWideIn)
                             umma_bf16_ss_sel(tmem_base + (uint32_t)(S::kSumCol0 + mb * 16), a_lo, hi, ones_lo, ones_hi, idesc_sum, !first);

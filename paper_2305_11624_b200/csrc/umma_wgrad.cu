@@ -347,7 +347,8 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
                 };
                 const uint32_t raw0 = smem_u32(&ctl->raw[0]), row = tiles0 + (uint32_t)slice * kChunkBytes;
                 // 64-byte swizzle of the codes, 128-byte swizzle of the values
-                const uint32_t codes_at = row + (uint32_t)r * 64u, values_at = row + (uint32_t)r * 128u, cx = (uint32_t)(r >> 1) & 3u, vx = (uint32_t)r & 7u;
+                const uint32_t codes_at = row + (uint32_t)r * 64u, cx = (uint32_t)(r >> 1) & 3u;
+                const uint32_t values_at = row + (uint32_t)r * 128u, vx = (uint32_t)r & 7u;
                 uint32_t at = 0, sb2 = 0, ph2 = 0, now = steps_of(0), next = steps_of(1), after = steps_of(2);
                 bool fine = true;
                 auto restore = [&](auto half_tag) {
@@ -378,8 +379,8 @@ __global__ void __launch_bounds__(kWThreads) umma_wgrad_kernel(const __grid_cons
                                 o[2 * h] = narrow_t<H>(f[0]);
                                 o[2 * h + 1] = narrow_t<H>(f[1]);
                             }
-                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(values_at + at + ((q ^ vx) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
-                                         : "memory");
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
+                                         ::"r"(values_at + at + ((q ^ vx) << 4)), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
                         }
                         fence_proxy_async_smem();
                         __syncwarp();

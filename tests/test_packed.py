@@ -645,6 +645,7 @@ LONG_SUMS = [("stem_window", 512, 3, 224, 224, 64, 7, 2, 1, "umma-stem", (False,
              ("stem_packed_wide", 256, 3, 64, 64, 256, 5, 2, 1, "umma-stem", (True, True)),
              ("groups_of_8", 256, 2048, 28, 28, 2048, 3, 1, 256, "grouped-mma", (False, False)),
              ("groups_of_32", 128, 64, 56, 56, 64, 3, 1, 2, "grouped-umma", (True, False)),
+             ("four_taps", 16, 1024, 80, 80, 64, 2, 1, 1, "umma", (True, True)),
              ("conv3", 64, 128, 56, 56, 128, 3, 1, 1, "umma", (True, False))]
 
 
