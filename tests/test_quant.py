@@ -279,6 +279,29 @@ def test_rows_and_channels_near_the_largest_value(rows, ci, kernel, dtype, large
     _check(got, t, dtype, 1, False)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 300])
+@pytest.mark.parametrize("ci", [131072, 131071])
+def test_the_longest_sums(rows, ci):
+    """All codes 127: 127^2 131072 is below 2^31 by 1.6 %.  x = 1 and omega = -1, then 1 in every other channel."""
+    import torch
+    co = 72
+    d = _desc(rows, ci, 1, 1, co)
+    x, w = torch.ones(rows, ci, dtype=torch.bfloat16, device="cuda"), torch.ones(co, ci, dtype=torch.bfloat16, device="cuda")
+    w[::2] = -1
+    one, zero = torch.ones(co, device="cuda"), torch.zeros(co, device="cuda")
+    codes = torch.empty(co * 131072, dtype=torch.int8, device="cuda")
+    scale, shift = torch.empty(co, device="cuda"), torch.empty(co, device="cuda")
+    C.convbn_deploy_prepare_quant(d, w, None, one, zero, zero, one - 1e-5, codes, scale, shift)
+    z = torch.empty(rows, co, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(max(256, C.convbn_workspace_bytes(d, C.PHASE_DEPLOY_FWD_QUANT)), dtype=torch.uint8, device="cuda")
+    C.convbn_deploy_fwd_quant(d, x, codes, scale, shift, z, None, False, ws)
+    C.convbn_check()
+    sign = torch.ones(co, device="cuda")
+    sign[::2] = -1
+    assert bool((z.float() == sign * 131072.0).all())              # (131071 too, rounded to bf16)
+
+
 # ---- together, as a deployed network uses them ---------------------------------------------------------------------------
 @pytest.mark.gpu
 def test_a_deployed_bottleneck_of_three_calls_captured_and_replayed():
