@@ -396,6 +396,35 @@ int convbn_add_relu(int dtype, const void *a, const void *b, void *out, long lon
 int convbn_relu_bwd(int dtype, const void *a, const void *y, void *out, long long count, void *stream);
 int convbn_add(int dtype, const void *a, const void *b, void *out, long long count, void *stream);
 
+/* ---- group norm with an activation, channels last (what a block without tracked statistics has in BatchNorm's place) ----------------
+ *
+ * X [n][h][w][c], c / groups neighbouring channels to a group.  Over the h w c / groups values of a group of a sample:
+ *     mean, var (biased)       r = 1 / sqrt(var + eps)       y = gamma (x - mean) r + beta       z = act(y)
+ * act: none, max(y, 0), or y / (1 + exp(-y)).  gamma, beta [c] fp32.  saved: means [n][groups], then r [n][groups], fp32.
+ * Backward, with dy = dz act'(y) and E the mean over a group's values:
+ *     dbeta = sum dy      dgamma = sum dy xhat      dx = r (gamma dy - E(gamma dy) - xhat E(gamma dy xhat)),   xhat = (x - mean) r
+ * y is formed again from x and saved; ReLU passes dz where y > 0, decided by the value in 64 bits.
+ * Variances are sums of squared distances from values of the group, not a difference of two large numbers; fp32, fixed order.  A group that
+ * holds a NaN or an infinity is NaN (which ReLU's max(., 0) turns into 0, as convbn_relu does); other groups are not touched by it.
+ * Layout CONVBN_NHWC with any of the three storage types; CONVBN_NCHW: CONVBN_EUNSUPPORTED, sizes 0.  Any h, w (1 x 1: a matrix [n][c]);
+ * at most 2^40 elements, 2^20 channels, 65535 groups, 2^30 samples.  z may be x and dx may be dz (in place), but nothing overlaps otherwise.
+ * X, Z, dZ, dX 16-byte, vectors 4-byte, saved 4-byte, workspace 256-byte aligned.  One workspace size serves both calls; query it with the
+ * device that will run the call current. */
+typedef enum { CONVBN_ACT_NONE = 0, CONVBN_ACT_RELU = 1, CONVBN_ACT_SILU = 2 } convbn_act;
+typedef struct convbn_group_norm_desc {
+    int n, c, h, w, groups;
+    int act;                   /* convbn_act */
+    int dtype;                 /* convbn_dtype of the activations */
+    int layout;                /* convbn_layout */
+    double eps;
+} convbn_group_norm_desc;
+size_t convbn_group_norm_saved_bytes(const convbn_group_norm_desc *desc);
+size_t convbn_group_norm_workspace_bytes(const convbn_group_norm_desc *desc);
+int convbn_group_norm_fwd(const convbn_group_norm_desc *desc, const void *x, const float *gamma, const float *beta, void *z, float *saved,
+                          void *workspace, size_t workspace_bytes, void *stream);
+int convbn_group_norm_bwd(const convbn_group_norm_desc *desc, const void *dz, const void *x, const float *gamma, const float *beta,
+                          const float *saved, void *dx, float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- measurement aid (the paper has no counterpart) ------------------------------------------ */
 
 /* After convbn_profile_begin(), every kernel this library launches (from any thread) is bracketed

@@ -19,6 +19,7 @@ OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EALIGN, ECUDA, ETIMEOUT, ECAPACITY = range
 F32, BF16, F16 = 0, 1, 2
 NCHW, NHWC = 0, 1
 MODE_TUNE, MODE_EVAL, MODE_DEPLOY = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 (PHASE_TUNE_FWD, PHASE_TUNE_BWD_DATA, PHASE_TUNE_BWD_WEIGHT, PHASE_EVAL_FWD, PHASE_EVAL_BWD,
  PHASE_DEPLOY_FWD, PHASE_DEPLOY_BWD, PHASE_TUNE_BWD, PHASE_TUNE_BWD_PACKED, PHASE_DEPLOY_FWD_QUANT) = range(10)
 
@@ -32,6 +33,7 @@ EXPORTS = (
     "convbn_tune_bwd_begin", "convbn_tune_bwd_join", "convbn_tune_fwd_glue", "convbn_tune_bwd_glue",
     "convbn_tconv_out_shape", "convbn_tconv_workspace_bytes", "convbn_tconv_tune_fwd", "convbn_tconv_tune_bwd",
     "convbn_pack", "convbn_unpack", "convbn_tune_bwd_packed", "convbn_deploy_prepare_quant", "convbn_deploy_fwd_quant",
+    "convbn_group_norm_saved_bytes", "convbn_group_norm_workspace_bytes", "convbn_group_norm_fwd", "convbn_group_norm_bwd",
 )
 
 
@@ -54,14 +56,23 @@ class Desc(ctypes.Structure):
                    dil_w, groups, dtype, layout, float(eps))
 
 
+class NormDesc(ctypes.Structure):
+    """Mirror of ``convbn_group_norm_desc``."""
+    _fields_ = [(k, ctypes.c_int) for k in ("n", "c", "h", "w", "groups", "act", "dtype", "layout")] + [("eps", ctypes.c_double)]
+
+    @classmethod
+    def make(cls, n, c, h=1, w=1, groups=32, act=ACT_NONE, dtype=BF16, layout=NHWC, eps=1e-5):
+        return cls(n, c, h, w, groups, act, dtype, layout, float(eps))
+
+
 _lib = None
 
 
 def _signatures():
     """argtypes of the entry points that take pointers: ctypes then converts plain integers itself, without an object per
-    argument, and to their full width (d: descriptor, p: pointer or stream, z: size, i: int, q: long long, f: double).  The
+    argument, and to their full width (d: descriptor, n: that of a group norm, p: pointer or stream, z: size, i: int, q: long long, f: double).  The
     calls of a training step go through _binding here; whoever takes them from lib() gets them typed all the same."""
-    kinds = {"d": ctypes.POINTER(Desc), "p": ctypes.c_void_p, "z": ctypes.c_size_t, "i": ctypes.c_int,
+    kinds = {"d": ctypes.POINTER(Desc), "n": ctypes.POINTER(NormDesc), "p": ctypes.c_void_p, "z": ctypes.c_size_t, "i": ctypes.c_int,
              "q": ctypes.c_longlong, "f": ctypes.c_double}
     table = {
         "convbn_tune_fwd": "dppppppppppzp", "convbn_tune_bwd_data": "dpppppzp", "convbn_tune_bwd_weight": "dppppppppppp" "zp",
@@ -74,6 +85,8 @@ def _signatures():
         "convbn_relu": "ippqp", "convbn_add_relu": "ipppqp", "convbn_relu_bwd": "ipppqp",
         "convbn_pack": "ipppqp", "convbn_unpack": "ipppqp", "convbn_tune_bwd_packed": "dppppppppppppp" "iipzp",
         "convbn_deploy_prepare_quant": "dppppppppp" "p", "convbn_deploy_fwd_quant": "dppppppipzp",
+        "convbn_group_norm_saved_bytes": "n", "convbn_group_norm_workspace_bytes": "n",
+        "convbn_group_norm_fwd": "nppppppzp", "convbn_group_norm_bwd": "npppppppppzp",
         "convbn_add": "ipppqp", "convbn_workspace_bytes": "di", "convbn_saved_bytes": "di", "convbn_check": "p",
     }
     return {name: [kinds[k] for k in sig] for name, sig in table.items()}
@@ -90,6 +103,7 @@ def lib():
         L.convbn_saved_bytes.restype = ctypes.c_size_t
         L.convbn_workspace_bytes.restype = ctypes.c_size_t
         L.convbn_host_step_arena_bytes.restype = ctypes.c_size_t
+        L.convbn_group_norm_saved_bytes.restype = L.convbn_group_norm_workspace_bytes.restype = ctypes.c_size_t
         L.convbn_status_string.restype = ctypes.c_char_p
         L.convbn_last_kernel.restype = ctypes.c_char_p
         for name in EXPORTS:
@@ -473,6 +487,55 @@ def convbn_deploy_fwd_quant(desc, x, w_codes, w_scale, b_fused, z, add, relu, wo
                                                            workspace_bytes, stream)
     if status:
         _raise(status, "convbn_deploy_fwd_quant")
+
+
+def convbn_group_norm_saved_bytes(desc: NormDesc) -> int:
+    return int(lib().convbn_group_norm_saved_bytes(desc))
+
+
+def convbn_group_norm_workspace_bytes(desc: NormDesc) -> int:
+    return int(lib().convbn_group_norm_workspace_bytes(desc))
+
+
+def _norm_tensors(desc, where, activations, vectors, saved):
+    """EINVAL for tensors (not addresses, not None) that are not what the descriptor says: another type or size, in several pieces,
+    channels not last, not on the current GPU."""
+    import torch
+    if type(desc) is not NormDesc:
+        raise TypeError("a NormDesc is expected")
+    current = None
+    for tensors, kind, count in ((activations, desc.dtype, desc.n * desc.c * desc.h * desc.w), (vectors, F32, desc.c),
+                                 ((saved,), F32, 2 * desc.n * desc.groups)):
+        for t in tensors:
+            if t is None or isinstance(t, int):
+                continue
+            if t.dim() == 4 and tensors is activations and t.shape != (desc.n, desc.h, desc.w, desc.c):
+                fits = t.shape == (desc.n, desc.c, desc.h, desc.w) and t.is_contiguous(memory_format=torch.channels_last)
+            else:
+                fits = t.is_contiguous()
+            if not fits or _storage(t) != kind or t.numel() != count:
+                _raise(EINVAL, "%s: %d elements of the descriptor's type, channels last, in one piece are needed" % (where, count))
+            if current is None:
+                current = torch.cuda.current_device() if t.is_cuda else -1
+            if not t.is_cuda or t.get_device() != current:
+                _raise(EINVAL, "%s: tensors of the current GPU are needed" % where)
+
+
+def convbn_group_norm_fwd(desc, x, gamma, beta, z, saved, workspace=None, workspace_bytes: Optional[int] = None, stream=None):
+    """z = act(group norm of x), channels last; saved: what the backward call needs beside x."""
+    _norm_tensors(desc, "convbn_group_norm_fwd", (x, z), (gamma, beta), saved)
+    status = (_native or _calls()).convbn_group_norm_fwd(desc, x, gamma, beta, z, saved, workspace, workspace_bytes, stream)
+    if status:
+        _raise(status, "convbn_group_norm_fwd")
+
+
+def convbn_group_norm_bwd(desc, dz, x, gamma, beta, saved, dx, dgamma, dbeta, workspace=None, workspace_bytes: Optional[int] = None,
+                          stream=None):
+    _norm_tensors(desc, "convbn_group_norm_bwd", (dz, x, dx), (gamma, beta, dgamma, dbeta), saved)
+    status = (_native or _calls()).convbn_group_norm_bwd(desc, dz, x, gamma, beta, saved, dx, dgamma, dbeta, workspace,
+                                                         workspace_bytes, stream)
+    if status:
+        _raise(status, "convbn_group_norm_bwd")
 
 
 def convbn_check(stream=None) -> None:

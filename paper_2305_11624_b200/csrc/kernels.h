@@ -378,4 +378,26 @@ cudaError_t launch_quant_rows(const Problem &pb, int dtype, const void *x, void 
 cudaError_t launch_quant_gemm(const Problem &pb, int dtype, const void *xq, const float *xs, const void *wq, const float *ws,
                               const float *shift, const void *add, int relu, void *z, cudaStream_t st);
 
+// ---- group norm with an activation, channels last (group_norm.cu) ----------------------------------------------------------
+constexpr int kNormMaxSlabGroups = 128;     // groups of a block's slab
+constexpr int kNormMaxBatch = 16384;        // samples of a launch
+struct GroupNormShape {
+    int n, c, g, cg;               // samples, channels, groups, channels of a group
+    int act, dtype;
+    int vec;                       // elements per access
+    int slab_g, slab_c, cols;      // groups, channels, accesses of a slab's pixel
+    int tx, ty;                    // threads side by side along a pixel; pixels side by side
+    int one_group;                 // every thread's channels belong to one group
+    int splits;                    // runs of pixels a sample is cut into ...
+    long long rows, pixels;        // ... pixels of a run, of a sample
+    int n0, batch;                 // samples of a launch
+    float eps;
+};
+GroupNormShape group_norm_shape(const convbn_group_norm_desc *d);     // (of a valid descriptor)
+size_t group_norm_workspace(const GroupNormShape &s);
+cudaError_t launch_group_norm_fwd(const GroupNormShape &s, const void *x, const float *gamma, const float *beta, void *z, float *saved,
+                                  void *workspace, cudaStream_t st);
+cudaError_t launch_group_norm_bwd(const GroupNormShape &s, const void *dz, const void *x, const float *gamma, const float *beta,
+                                  const float *saved, void *dx, float *dgamma, float *dbeta, void *workspace, cudaStream_t st);
+
 }  // namespace convbn
