@@ -425,6 +425,42 @@ int convbn_group_norm_fwd(const convbn_group_norm_desc *desc, const void *x, con
 int convbn_group_norm_bwd(const convbn_group_norm_desc *desc, const void *dz, const void *x, const float *gamma, const float *beta,
                           const float *saved, void *dx, float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- orthogonal updates of weights (what an optimiser makes of dw) -----------------------------------------------------------------------
+ *
+ * convbn_orthogonalise: of each of `count` matrices g [rows][cols], one after the other in memory,
+ *     X = g / (|g|_F + eps);   `steps` times  X <- 3.4445 X - 4.7750 (X X^T) X + 2.0315 (X X^T)^2 X;   out = X
+ * Newton-Schulz steps that bring every singular value near 1 and keep the singular vectors (five of them: to 0.7 .. 1.2).  g and out have
+ * `dtype`; out may be g.  Products are formed from pairs of halves (22 significant bits) with fp32 sums, squares of the norm in 64 bits; one
+ * rounding, to `dtype`, at the end.  fp32 results are as near to the formula as fp32 products bring them: 1e-6 (2-norm) for a matrix of noise, 1e-5
+ * for one of a few strong directions, whose noise the steps lift.
+ * A zero matrix gives zeros; one that holds a NaN or an infinity gives NaN, others are not touched by it.
+ *
+ * convbn_muon_step: one step of the optimiser over `count` layers of C_out = rows and cols weights per output channel (any weight layout of
+ * this library), in one call:
+ *     v = momentum v + grad        u = grad + momentum v  (nesterov != 0)  or  v        X = u made orthogonal as above
+ *     master = (1 - lr weight_decay) master - lr sqrt(max(1, rows / cols)) X            weight = master, rounded to `dtype`
+ * grad, momentum (v), master: fp32, device; weight: the storage type, or NULL.  `layers` and `params` are read on the host during the call.
+ * Every tensor belongs to one layer, once: nothing may overlap.  grad is left as it is.
+ *
+ * rows, cols >= 1, rows cols <= 2^31, count >= 0 (0: nothing is done, no other pointer is looked at), 1 <= steps <= 64, eps >= 0.  Pointers
+ * aligned to their element; workspace 256.  All memory of the current device.  CONVBN_EINVAL, CONVBN_EALIGN, CONVBN_EWORKSPACE, CONVBN_ECUDA. */
+typedef struct convbn_muon_layer {
+    int rows, cols;
+    const float *grad;
+    float *momentum, *master;
+    void *weight;
+} convbn_muon_layer;
+typedef struct convbn_muon_params {
+    double lr, momentum, weight_decay, eps;
+    int nesterov, steps;
+} convbn_muon_params;
+size_t convbn_orthogonalise_workspace_bytes(int rows, int cols, int count);
+int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols, int count, int steps, double eps, void *workspace,
+                         size_t workspace_bytes, void *stream);
+size_t convbn_muon_workspace_bytes(const convbn_muon_layer *layers, int count);
+int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, const convbn_muon_params *params, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
 /* ---- measurement aid (the paper has no counterpart) ------------------------------------------ */
 
 /* After convbn_profile_begin(), every kernel this library launches (from any thread) is bracketed

@@ -34,6 +34,7 @@ EXPORTS = (
     "convbn_tconv_out_shape", "convbn_tconv_workspace_bytes", "convbn_tconv_tune_fwd", "convbn_tconv_tune_bwd",
     "convbn_pack", "convbn_unpack", "convbn_tune_bwd_packed", "convbn_deploy_prepare_quant", "convbn_deploy_fwd_quant",
     "convbn_group_norm_saved_bytes", "convbn_group_norm_workspace_bytes", "convbn_group_norm_fwd", "convbn_group_norm_bwd",
+    "convbn_orthogonalise_workspace_bytes", "convbn_orthogonalise", "convbn_muon_workspace_bytes", "convbn_muon_step",
 )
 
 
@@ -65,14 +66,28 @@ class NormDesc(ctypes.Structure):
         return cls(n, c, h, w, groups, act, dtype, layout, float(eps))
 
 
+class _MuonLayer(ctypes.Structure):
+    """Mirror of ``convbn_muon_layer``."""
+    _fields_ = [("rows", ctypes.c_int), ("cols", ctypes.c_int)] + [(k, ctypes.c_void_p) for k in ("grad", "momentum", "master", "weight")]
+
+
+class MuonParams(ctypes.Structure):
+    """Mirror of ``convbn_muon_params``."""
+    _fields_ = [(k, ctypes.c_double) for k in ("lr", "momentum", "weight_decay", "eps")] + [(k, ctypes.c_int) for k in ("nesterov", "steps")]
+
+    @classmethod
+    def make(cls, lr=0.02, momentum=0.95, weight_decay=0.0, eps=1e-7, nesterov=True, steps=5):
+        return cls(float(lr), float(momentum), float(weight_decay), float(eps), 1 if nesterov else 0, steps)
+
+
 _lib = None
 
 
 def _signatures():
     """argtypes of the entry points that take pointers: ctypes then converts plain integers itself, without an object per
-    argument, and to their full width (d: descriptor, n: that of a group norm, p: pointer or stream, z: size, i: int, q: long long, f: double).  The
+    argument, and to their full width (d: descriptor, n: that of a group norm, m: an optimiser's parameters, p: pointer or stream, z: size, i: int, q: long long, f: double).  The
     calls of a training step go through _binding here; whoever takes them from lib() gets them typed all the same."""
-    kinds = {"d": ctypes.POINTER(Desc), "n": ctypes.POINTER(NormDesc), "p": ctypes.c_void_p, "z": ctypes.c_size_t, "i": ctypes.c_int,
+    kinds = {"d": ctypes.POINTER(Desc), "n": ctypes.POINTER(NormDesc), "m": ctypes.POINTER(MuonParams), "p": ctypes.c_void_p, "z": ctypes.c_size_t, "i": ctypes.c_int,
              "q": ctypes.c_longlong, "f": ctypes.c_double}
     table = {
         "convbn_tune_fwd": "dppppppppppzp", "convbn_tune_bwd_data": "dpppppzp", "convbn_tune_bwd_weight": "dppppppppppp" "zp",
@@ -87,6 +102,8 @@ def _signatures():
         "convbn_deploy_prepare_quant": "dppppppppp" "p", "convbn_deploy_fwd_quant": "dppppppipzp",
         "convbn_group_norm_saved_bytes": "n", "convbn_group_norm_workspace_bytes": "n",
         "convbn_group_norm_fwd": "nppppppzp", "convbn_group_norm_bwd": "npppppppppzp",
+        "convbn_orthogonalise_workspace_bytes": "iii", "convbn_orthogonalise": "ippiiiifpzp",
+        "convbn_muon_workspace_bytes": "pi", "convbn_muon_step": "piimpzp",
         "convbn_add": "ipppqp", "convbn_workspace_bytes": "di", "convbn_saved_bytes": "di", "convbn_check": "p",
     }
     return {name: [kinds[k] for k in sig] for name, sig in table.items()}
@@ -103,6 +120,7 @@ def lib():
         L.convbn_saved_bytes.restype = ctypes.c_size_t
         L.convbn_workspace_bytes.restype = ctypes.c_size_t
         L.convbn_host_step_arena_bytes.restype = ctypes.c_size_t
+        L.convbn_orthogonalise_workspace_bytes.restype = L.convbn_muon_workspace_bytes.restype = ctypes.c_size_t
         L.convbn_group_norm_saved_bytes.restype = L.convbn_group_norm_workspace_bytes.restype = ctypes.c_size_t
         L.convbn_status_string.restype = ctypes.c_char_p
         L.convbn_last_kernel.restype = ctypes.c_char_p
@@ -536,6 +554,78 @@ def convbn_group_norm_bwd(desc, dz, x, gamma, beta, saved, dx, dgamma, dbeta, wo
                                                          workspace_bytes, stream)
     if status:
         _raise(status, "convbn_group_norm_bwd")
+
+
+def _on_current_gpu(tensors, where):
+    import torch
+    if any(not t.is_cuda for t in tensors) or any(t.get_device() != torch.cuda.current_device() for t in tensors):
+        _raise(EINVAL, "%s: tensors of the current GPU are needed" % where)
+
+
+def convbn_orthogonalise_workspace_bytes(rows: int, cols: int, count: int = 1) -> int:
+    return int(lib().convbn_orthogonalise_workspace_bytes(rows, cols, count))
+
+
+def convbn_orthogonalise(g, out, steps: int = 5, eps: float = 1e-7, workspace=None, workspace_bytes: Optional[int] = None, stream=None):
+    """out = g ([rows, cols], or a stack [count, rows, cols]) made orthogonal by Newton-Schulz steps; out may be g."""
+    where = "convbn_orthogonalise"
+    if g.dim() not in (2, 3) or out.shape != g.shape or out.dtype != g.dtype or not (g.is_contiguous() and out.is_contiguous()):
+        _raise(EINVAL, "%s: two matrices, or stacks of them, of one shape and type are needed, each in one piece" % where)
+    kind = _storage(g)
+    _on_current_gpu((g, out), where)
+    rows, cols = g.shape[-2:]
+    status = (_native or _calls()).convbn_orthogonalise(kind, g, out, rows, cols, g.shape[0] if g.dim() == 3 else 1, steps, float(eps),
+                                                        workspace, workspace_bytes, stream)
+    if status:
+        _raise(status, where)
+
+
+class MuonLayers:
+    """The layers that convbn_muon_step updates: (gradient, momentum, master weights, weights in storage type or None) each, fp32 but the
+    last, of one shape whose first extent is C_out.  Made once; the tensors are kept."""
+
+    def __init__(self, layers):
+        import torch
+        where, self.tensors = "MuonLayers", [tuple(l) for l in layers]
+        self.dtype, kinds, spans = F32, set(), []
+        self.array = (_MuonLayer * len(self.tensors))()
+        for entry, (grad, momentum, master, weight) in zip(self.array, self.tensors):
+            whole = [t for t in (grad, momentum, master, weight) if t is not None]
+            if any(t is None or t.dtype != torch.float32 for t in (grad, momentum, master)):
+                _raise(EINVAL, "%s: gradients, momentum and master weights in fp32 are needed" % where)
+            if master.dim() < 1 or master.numel() < 1 or any(t.numel() != master.numel() or not t.is_contiguous() for t in whole):
+                _raise(EINVAL, "%s: a layer's tensors have one size and are in one piece each" % where)
+            _on_current_gpu(whole, where)
+            entry.rows, entry.cols = master.shape[0], master.numel() // master.shape[0]
+            entry.grad, entry.momentum, entry.master, entry.weight = (_ptr(t) for t in (grad, momentum, master, weight))
+            if weight is not None:
+                kinds.add(_storage(weight))
+            spans += [(t.data_ptr(), t.data_ptr() + t.nbytes) for t in whole]
+        spans.sort()
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            _raise(EINVAL, "%s: two tensors overlap" % where)
+        if len(kinds) > 1:
+            _raise(EINVAL, "%s: weights of one storage type are needed" % where)
+        if kinds:
+            self.dtype = kinds.pop()
+        self.device = self.tensors[0][0].device if self.tensors else None
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def convbn_muon_workspace_bytes(layers: MuonLayers) -> int:
+    return int(lib().convbn_muon_workspace_bytes(ctypes.addressof(layers.array), len(layers)))
+
+
+def convbn_muon_step(layers: MuonLayers, params: MuonParams, workspace=None, workspace_bytes: Optional[int] = None, stream=None):
+    """Momentum, orthogonal update and new weights of every layer."""
+    if layers.device is not None:
+        _on_current_gpu((layers.tensors[0][0],), "convbn_muon_step")
+    status = (_native or _calls()).convbn_muon_step(ctypes.addressof(layers.array), len(layers), layers.dtype, params, workspace,
+                                                    workspace_bytes, stream)
+    if status:
+        _raise(status, "convbn_muon_step")
 
 
 def convbn_check(stream=None) -> None:

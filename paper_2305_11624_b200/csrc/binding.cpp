@@ -61,20 +61,23 @@ bool stream(PyObject *o, void **out) {
 
 template <class T>
 bool convert(PyObject *o, T *out) {
-    if constexpr (std::is_same_v<T, const convbn_desc *> || std::is_same_v<T, const convbn_group_norm_desc *>) {
+    if constexpr (std::is_same_v<T, const convbn_desc *> || std::is_same_v<T, const convbn_group_norm_desc *> || std::is_same_v<T, const convbn_muon_params *>) {
         if (o == Py_None) { *out = nullptr; return true; }
         Py_buffer b;
         if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) return false;
         const bool fits = (size_t)b.len == sizeof(**out);
         *out = (T)b.buf;                              // (the caller holds the descriptor for the length of the call)
         PyBuffer_Release(&b);
-        if (!fits) PyErr_SetString(PyExc_TypeError, "a descriptor of this call's kind is expected");
+        if (!fits) PyErr_SetString(PyExc_TypeError, "another kind of structure is expected");
         return fits;
     } else if constexpr (std::is_pointer_v<T>) {
         void *p = nullptr;
         if (!address(o, &p)) return false;
         *out = (T)p;
         return true;
+    } else if constexpr (std::is_floating_point_v<T>) {
+        *out = (T)PyFloat_AsDouble(o);
+        return *out != (T)-1 || !PyErr_Occurred();
     } else {
         // (as ctypes does: integers only, and cut to the parameter's width)
         if (!PyLong_Check(o)) {
@@ -205,6 +208,7 @@ PyMethodDef g_methods[] = {
     ENTRY(convbn_tconv_tune_fwd), ENTRY(convbn_tconv_tune_bwd), ENTRY(convbn_eval_fwd), ENTRY(convbn_eval_bwd),
     ENTRY(convbn_deploy_fwd), ENTRY(convbn_deploy_bwd), ENTRY(convbn_pack), ENTRY(convbn_unpack), ENTRY(convbn_tune_bwd_packed),
     ENTRY(convbn_deploy_fwd_quant), ENTRY(convbn_group_norm_fwd), ENTRY(convbn_group_norm_bwd),
+    ENTRY(convbn_orthogonalise), ENTRY(convbn_muon_step),
     {"pack", (PyCFunction)(void (*)(void))packed<&convbn_pack, false>, METH_FASTCALL, nullptr},
     {"unpack", (PyCFunction)(void (*)(void))packed<&convbn_unpack, true>, METH_FASTCALL, nullptr},
     {"tune_bwd_packed", (PyCFunction)(void (*)(void))packed_bwd, METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};

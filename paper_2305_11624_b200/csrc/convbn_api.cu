@@ -5,6 +5,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <cmath>
 #include <map>
 #include <mutex>
 #include <new>
@@ -1797,6 +1798,121 @@ int convbn_group_norm_bwd(const convbn_group_norm_desc *desc, const void *dz, co
     cudaStream_t st = (cudaStream_t)stream;
     t_prof_phase = "group_norm_bwd";
     LAUNCH("group_norm", launch_group_norm_bwd(s, dz, x, gamma, beta, saved, dx, dgamma, dbeta, workspace, st));
+    return CONVBN_OK;
+}
+
+// Matrices that an update takes, in tasks that an int counts.
+static bool ortho_sizes(long long rows, long long cols, long long count) {
+    if (rows < 1 || cols < 1 || count < 0 || rows > (1LL << 31) / cols) return false;
+    const long long tiles = ((rows + 127) / 128) * ((cols + 127) / 128) * 2;
+    return (count * tiles) < (1LL << 30);
+}
+static int ortho_room(size_t need, const void *workspace, size_t bytes) {
+    if (!workspace || bytes < need) return CONVBN_EWORKSPACE;
+    return aligned(workspace, 256) ? CONVBN_OK : CONVBN_EALIGN;
+}
+
+size_t convbn_orthogonalise_workspace_bytes(int rows, int cols, int count) {
+    return ortho_sizes(rows, cols, count) ? (size_t)count * ortho_matrix_bytes(rows, cols) : 0;
+}
+
+int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols, int count, int steps, double eps, void *workspace,
+                         size_t workspace_bytes, void *stream) {
+    if (dtype != CONVBN_F32 && dtype != CONVBN_BF16 && dtype != CONVBN_F16) return CONVBN_EINVAL;
+    if (!ortho_sizes(rows, cols, count) || steps < 1 || steps > 64 || !(eps >= 0.)) return CONVBN_EINVAL;
+    if (count == 0) return CONVBN_OK;
+    if (!g || !out) return CONVBN_EINVAL;
+    if (!aligned(g, elem_size(dtype)) || !aligned(out, elem_size(dtype))) return CONVBN_EALIGN;
+    CK(ortho_room((size_t)count * ortho_matrix_bytes(rows, cols), workspace, workspace_bytes));
+    OrthoTable t = {};
+    t.items = 1;
+    t.steps = steps;
+    t.dtype = dtype;
+    t.eps = eps;
+    t.item[0].g = g;
+    t.item[0].out = out;
+    t.item[0].rows = rows;
+    t.item[0].cols = cols;
+    t.item[0].count = count;
+    ortho_place(t, 0, 0);
+    cudaStream_t st = (cudaStream_t)stream;
+    t_prof_phase = "orthogonalise";
+    LAUNCH("ortho", launch_ortho(t, workspace, st));
+    return CONVBN_OK;
+}
+
+// Layers first .. of a launch: as many as it takes and an int counts the tasks of.  Returns the next launch's first.
+static int muon_launch(const convbn_muon_layer *layers, int count, int first, size_t *bytes) {
+    long long tiles = 0;
+    int i = first;
+    for (*bytes = 0; i < count && i - first < kOrthoItems; ++i) {
+        tiles += (((long long)layers[i].rows + 127) / 128) * (((long long)layers[i].cols + 127) / 128) * 2;
+        if (tiles >= (1LL << 30)) break;
+        *bytes += ortho_matrix_bytes(layers[i].rows, layers[i].cols);
+    }
+    return i;
+}
+static bool muon_sizes(const convbn_muon_layer *layers, int count) {
+    if (count < 0 || (count > 0 && !layers)) return false;
+    for (int i = 0; i < count; ++i)
+        if (!ortho_sizes(layers[i].rows, layers[i].cols, 1)) return false;
+    return true;
+}
+
+size_t convbn_muon_workspace_bytes(const convbn_muon_layer *layers, int count) {
+    if (!muon_sizes(layers, count)) return 0;
+    size_t most = 0, bytes;
+    for (int i = 0; i < count;) {
+        i = muon_launch(layers, count, i, &bytes);
+        if (bytes > most) most = bytes;
+    }
+    return most;
+}
+
+int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, const convbn_muon_params *params, void *workspace,
+                     size_t workspace_bytes, void *stream) {
+    if (!params || (dtype != CONVBN_F32 && dtype != CONVBN_BF16 && dtype != CONVBN_F16) || !muon_sizes(layers, count)) return CONVBN_EINVAL;
+    if (params->steps < 1 || params->steps > 64 || !(params->eps >= 0.)) return CONVBN_EINVAL;
+    if (!std::isfinite(params->lr) || !std::isfinite(params->momentum) || !std::isfinite(params->weight_decay)) return CONVBN_EINVAL;
+    if (count == 0) return CONVBN_OK;
+    for (int i = 0; i < count; ++i)
+        if (!layers[i].grad || !layers[i].momentum || !layers[i].master) return CONVBN_EINVAL;
+    for (int i = 0; i < count; ++i)
+        if (!aligned(layers[i].grad, 4) || !aligned(layers[i].momentum, 4) || !aligned(layers[i].master, 4) ||
+            !aligned(layers[i].weight, elem_size(dtype)))
+            return CONVBN_EALIGN;
+    CK(ortho_room(convbn_muon_workspace_bytes(layers, count), workspace, workspace_bytes));
+    cudaStream_t st = (cudaStream_t)stream;
+    t_prof_phase = "muon";
+    for (int first = 0; first < count;) {
+        size_t bytes;
+        const int next = muon_launch(layers, count, first, &bytes);
+        OrthoTable t = {};
+        t.items = next - first;
+        t.steps = params->steps;
+        t.dtype = dtype;
+        t.muon = 1;
+        t.nesterov = params->nesterov != 0;
+        t.momentum = (float)params->momentum;
+        t.keep = (float)(1. - params->lr * params->weight_decay);
+        t.eps = params->eps;
+        long long end = 0;
+        for (int i = 0; i < t.items; ++i) {
+            const convbn_muon_layer &l = layers[first + i];
+            OrthoItem &it = t.item[i];
+            it.g = l.grad;
+            it.momentum = l.momentum;
+            it.master = l.master;
+            it.out = l.weight;
+            it.rows = l.rows;
+            it.cols = l.cols;
+            it.count = 1;
+            it.scale = (float)(params->lr * (l.rows > l.cols ? std::sqrt((double)l.rows / l.cols) : 1.));
+            end = ortho_place(t, i, end);
+        }
+        LAUNCH("ortho", launch_ortho(t, workspace, st));
+        first = next;
+    }
     return CONVBN_OK;
 }
 

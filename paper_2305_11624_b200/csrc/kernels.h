@@ -400,4 +400,30 @@ cudaError_t launch_group_norm_fwd(const GroupNormShape &s, const void *x, const 
 cudaError_t launch_group_norm_bwd(const GroupNormShape &s, const void *dz, const void *x, const float *gamma, const float *beta,
                                   const float *saved, void *dx, float *dgamma, float *dbeta, void *workspace, cudaStream_t st);
 
+// ---- orthogonal updates (ortho_kernels.cu; formulas and layout: ortho.cuh) ------------------------------------------------------
+constexpr int kOrthoItems = 64;             // matrices (or stacks of like ones) of a launch
+struct OrthoItem {
+    const void *g;                          // gradient or matrix ...
+    float *momentum, *master;               // muon only
+    void *out;                              // the orthogonal matrix, or the weights in storage type (may be NULL)
+    int rows, cols, count;                  // count like matrices, one after the other in g and out
+    int rt, ct;                             // tiles of 128 rows, of 128 columns
+    int first_sum, first_tile, first_gram, first_update;      // tasks of the items before
+    float scale;                            // of the update (muon)
+    long long base, bytes;                  // its first matrix's place in the workspace; of one matrix
+};
+struct OrthoTable {
+    int items, steps;
+    int sums, tiles, grams, updates;        // tasks in all
+    int dtype;                              // of g and out (muon: of out; g is fp32)
+    int muon, nesterov;
+    float momentum, keep, lr;               // keep = 1 - lr weight_decay
+    double eps;
+    OrthoItem item[kOrthoItems];
+};
+size_t ortho_matrix_bytes(int rows, int cols);        // of one matrix in the workspace
+// Fills rt .. bytes of t.item[i] behind its predecessors; returns the workspace's end.
+long long ortho_place(OrthoTable &t, int i, long long end);
+cudaError_t launch_ortho(const OrthoTable &t, void *workspace, cudaStream_t st);
+
 }  // namespace convbn
