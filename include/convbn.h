@@ -442,7 +442,7 @@ int convbn_group_norm_bwd(const convbn_group_norm_desc *desc, const void *dz, co
  * grad, momentum (v), master: fp32, device; weight: the storage type, or NULL.  `layers` and `params` are read on the host during the call.
  * Every tensor belongs to one layer, once: nothing may overlap.  grad is left as it is.
  *
- * rows, cols >= 1, rows cols <= 2^31, count >= 0 (0: nothing is done, no other pointer is looked at), 1 <= steps <= 64, eps >= 0.  Pointers
+ * rows, cols >= 1, rows cols <= 2^31, fewer than 2^23 tiles of 128 x 64 a matrix (a stack), count >= 0 (0: nothing is done, no other pointer is looked at), 1 <= steps <= 64, eps >= 0.  Pointers
  * aligned to their element; workspace 256.  All memory of the current device.  CONVBN_EINVAL, CONVBN_EALIGN, CONVBN_EWORKSPACE, CONVBN_ECUDA. */
 typedef struct convbn_muon_layer {
     int rows, cols;

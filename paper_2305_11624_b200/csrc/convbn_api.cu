@@ -1805,15 +1805,26 @@ int convbn_group_norm_bwd(const convbn_group_norm_desc *desc, const void *dz, co
 static bool ortho_sizes(long long rows, long long cols, long long count) {
     if (rows < 1 || cols < 1 || count < 0 || rows > (1LL << 31) / cols) return false;
     const long long tiles = ((rows + 127) / 128) * ((cols + 127) / 128) * 2;
-    return (count * tiles) < (1LL << 30);
+    return count * tiles < (1LL << 23);
 }
 static int ortho_room(size_t need, const void *workspace, size_t bytes) {
     if (!workspace || bytes < need) return CONVBN_EWORKSPACE;
     return aligned(workspace, 256) ? CONVBN_OK : CONVBN_EALIGN;
 }
 
+static OrthoTable ortho_stack(int rows, int cols, int count) {
+    OrthoTable t = {};
+    t.items = 1;
+    t.item[0].rows = rows;
+    t.item[0].cols = cols;
+    t.item[0].count = count;
+    return t;
+}
+
 size_t convbn_orthogonalise_workspace_bytes(int rows, int cols, int count) {
-    return ortho_sizes(rows, cols, count) ? (size_t)count * ortho_matrix_bytes(rows, cols) : 0;
+    if (!ortho_sizes(rows, cols, count) || count == 0) return 0;
+    OrthoTable t = ortho_stack(rows, cols, count);
+    return ortho_plan(t);
 }
 
 int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols, int count, int steps, double eps, void *workspace,
@@ -1823,33 +1834,32 @@ int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols
     if (count == 0) return CONVBN_OK;
     if (!g || !out) return CONVBN_EINVAL;
     if (!aligned(g, elem_size(dtype)) || !aligned(out, elem_size(dtype))) return CONVBN_EALIGN;
-    CK(ortho_room((size_t)count * ortho_matrix_bytes(rows, cols), workspace, workspace_bytes));
-    OrthoTable t = {};
-    t.items = 1;
+    OrthoTable t = ortho_stack(rows, cols, count);
+    CK(ortho_room(ortho_plan(t), workspace, workspace_bytes));
     t.steps = steps;
     t.dtype = dtype;
     t.eps = eps;
     t.item[0].g = g;
     t.item[0].out = out;
-    t.item[0].rows = rows;
-    t.item[0].cols = cols;
-    t.item[0].count = count;
-    ortho_place(t, 0, 0);
     cudaStream_t st = (cudaStream_t)stream;
     t_prof_phase = "orthogonalise";
     LAUNCH("ortho", launch_ortho(t, workspace, st));
     return CONVBN_OK;
 }
 
-// Layers first .. of a launch: as many as it takes and an int counts the tasks of.  Returns the next launch's first.
-static int muon_launch(const convbn_muon_layer *layers, int count, int first, size_t *bytes) {
+// The launch that begins with layer `first`: as many layers as it takes and an int counts the tasks of.  Returns the next one's first.
+static int muon_launch(const convbn_muon_layer *layers, int count, int first, OrthoTable *t) {
     long long tiles = 0;
     int i = first;
-    for (*bytes = 0; i < count && i - first < kOrthoItems; ++i) {
+    for (; i < count && i - first < kOrthoItems; ++i) {
         tiles += (((long long)layers[i].rows + 127) / 128) * (((long long)layers[i].cols + 127) / 128) * 2;
-        if (tiles >= (1LL << 30)) break;
-        *bytes += ortho_matrix_bytes(layers[i].rows, layers[i].cols);
+        if (tiles >= (1LL << 23) && i > first) break;
+        OrthoItem &it = t->item[i - first];
+        it.rows = layers[i].rows;
+        it.cols = layers[i].cols;
+        it.count = 1;
     }
+    t->items = i - first;
     return i;
 }
 static bool muon_sizes(const convbn_muon_layer *layers, int count) {
@@ -1861,9 +1871,11 @@ static bool muon_sizes(const convbn_muon_layer *layers, int count) {
 
 size_t convbn_muon_workspace_bytes(const convbn_muon_layer *layers, int count) {
     if (!muon_sizes(layers, count)) return 0;
-    size_t most = 0, bytes;
+    size_t most = 0;
     for (int i = 0; i < count;) {
-        i = muon_launch(layers, count, i, &bytes);
+        OrthoTable t = {};
+        i = muon_launch(layers, count, i, &t);
+        const size_t bytes = ortho_plan(t);
         if (bytes > most) most = bytes;
     }
     return most;
@@ -1881,14 +1893,13 @@ int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, cons
         if (!aligned(layers[i].grad, 4) || !aligned(layers[i].momentum, 4) || !aligned(layers[i].master, 4) ||
             !aligned(layers[i].weight, elem_size(dtype)))
             return CONVBN_EALIGN;
-    CK(ortho_room(convbn_muon_workspace_bytes(layers, count), workspace, workspace_bytes));
+    if (count > kOrthoItems) CK(ortho_room(convbn_muon_workspace_bytes(layers, count), workspace, workspace_bytes));    // (before anything is launched)
     cudaStream_t st = (cudaStream_t)stream;
     t_prof_phase = "muon";
     for (int first = 0; first < count;) {
-        size_t bytes;
-        const int next = muon_launch(layers, count, first, &bytes);
         OrthoTable t = {};
-        t.items = next - first;
+        const int next = muon_launch(layers, count, first, &t);
+        CK(ortho_room(ortho_plan(t), workspace, workspace_bytes));
         t.steps = params->steps;
         t.dtype = dtype;
         t.muon = 1;
@@ -1896,7 +1907,6 @@ int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, cons
         t.momentum = (float)params->momentum;
         t.keep = (float)(1. - params->lr * params->weight_decay);
         t.eps = params->eps;
-        long long end = 0;
         for (int i = 0; i < t.items; ++i) {
             const convbn_muon_layer &l = layers[first + i];
             OrthoItem &it = t.item[i];
@@ -1904,11 +1914,7 @@ int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, cons
             it.momentum = l.momentum;
             it.master = l.master;
             it.out = l.weight;
-            it.rows = l.rows;
-            it.cols = l.cols;
-            it.count = 1;
             it.scale = (float)(params->lr * (l.rows > l.cols ? std::sqrt((double)l.rows / l.cols) : 1.));
-            end = ortho_place(t, i, end);
         }
         LAUNCH("ortho", launch_ortho(t, workspace, st));
         first = next;

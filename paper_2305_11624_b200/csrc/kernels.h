@@ -408,22 +408,22 @@ struct OrthoItem {
     void *out;                              // the orthogonal matrix, or the weights in storage type (may be NULL)
     int rows, cols, count;                  // count like matrices, one after the other in g and out
     int rt, ct;                             // tiles of 128 rows, of 128 columns
-    int first_sum, first_tile, first_gram, first_update;      // tasks of the items before
+    int splits, per_split;                  // pieces that the sums of X X^T are cut into, steps of 64 of each
+    int first_sum, first_tile, first_gram, first_square, first_update, first_matrix;       // tasks, matrices of the items before
     float scale;                            // of the update (muon)
     long long base, bytes;                  // its first matrix's place in the workspace; of one matrix
 };
 struct OrthoTable {
     int items, steps;
-    int sums, tiles, grams, updates;        // tasks in all
+    int sums, tiles, grams, squares, updates, matrices;       // in all
     int dtype;                              // of g and out (muon: of out; g is fp32)
     int muon, nesterov;
     float momentum, keep, lr;               // keep = 1 - lr weight_decay
     double eps;
     OrthoItem item[kOrthoItems];
 };
-size_t ortho_matrix_bytes(int rows, int cols);        // of one matrix in the workspace
-// Fills rt .. bytes of t.item[i] behind its predecessors; returns the workspace's end.
-long long ortho_place(OrthoTable &t, int i, long long end);
+// Fills rt .. bytes of all items from rows, cols, count; returns the bytes of the workspace.
+size_t ortho_plan(OrthoTable &t);
 cudaError_t launch_ortho(const OrthoTable &t, void *workspace, cudaStream_t st);
 
 }  // namespace convbn

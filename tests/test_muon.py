@@ -87,7 +87,7 @@ def test_muon_refusals():
     assert raw(None, 0, C.BF16, None, None, 0, 0) == C.EINVAL
     # a launch takes 64 layers: the workspace is that of the largest launch
     many = (C._MuonLayer * 130)(*[_layer() for _ in range(130)])
-    assert size(ctypes.addressof(many), 130) == size(ctypes.addressof(many), 64) == 64 * size(ctypes.addressof(many), 1)
+    assert size(ctypes.addressof(many), 130) == size(ctypes.addressof(many), 64) <= 64 * size(ctypes.addressof(many), 1)
 
 
 def test_muon_layers_are_looked_at():
