@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__
 // ---- products ---------------------------------------------------------------------------------------------------------------------
 // All products of all steps in one launch.  CTA = 10 warps: 0 takes tasks and loads, 1 MMA issuer and owner of tensor memory, 2-9 epilogue.
 // A task is a 128 x 128 tile of A, P or X (or a piece of the k of one of A's); k in steps of 64.  A step's four tiles (hi and lo of both
-// operands) are 64 KB and feed twelve MMAs.  hi hi is summed apart from the other two products: the tensor core's sums drift towards zero
+// operands) are 64 KB and feed twelve MMAs.  What a task adds to its product (P: A's tile, X: X's) is brought by bulk copies too: read by the
+// rows' own threads it took 7000 clocks of a task, 32 lines an instruction.  hi hi is summed apart from the other two products: the tensor core's sums drift towards zero
 // with their length, and those of small numbers do not notice.  For the same reason a sum over more than 1024 k is cut: the epilogue adds
 // the pieces up in registers, in fp32 with rounding.
 //
@@ -128,23 +129,24 @@ __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__
 // matrix's earlier tasks are done, which a counter of the matrix tells.  What it waits for has a lower number, so it has been taken by a CTA
 // that runs: however few CTAs run at a time, one of them can go on.
 constexpr int kOThreads = 320;
-constexpr int kOStages = 3;
+constexpr int kOSlots = 5;                                 // of two tiles: the hi, or the lo, of both operands of a step
 constexpr int kORing = 4;                                  // tasks between the warps
-constexpr uint32_t kOStage = 4 * kOrthoTile;
+constexpr uint32_t kOSlot = 2 * kOrthoTile;
 constexpr int kOSegment = 16;                              // steps of a sum
-constexpr uint32_t kOStaging = 8 * 4096;                   // an epilogue warp's 32 rows x 64 columns, hi or lo; or 32 x 32 in fp32
+constexpr uint32_t kOStaging = 8 * 8192;                   // an epilogue warp's 32 rows x 64 columns, hi and lo, or fp32
 
 struct OrthoCtl {
-    uint64_t full[kOStages], empty[kOStages], acc_full[2], acc_empty[2], ring_full[kORing], ring_empty[kORing];
+    uint64_t full[kOSlots], empty[kOSlots], acc_full[2], acc_empty[2], ring_full[kORing], ring_empty[kORing], old_full[8];
     int ring[kORing];
     uint32_t tmem_base;
     int abort_flag;
 };
 
-// Where an operand of a step lies: one tile (K-major), or the halves of two (MN-major).
+// An operand's tiles: steps below `turn` are whole tiles side by side from `rows` on, the k along them (K-major); the others halves of
+// two tiles, the k down them (MN-major), from `cols` on.
 struct OrthoOperand {
-    long long first, second;
-    bool mn;
+    long long rows, cols, pitch, lo;           // pitch: of a row of tiles; lo: from hi to lo
+    int turn;
 };
 
 struct OrthoTask {
@@ -203,46 +205,28 @@ __device__ __forceinline__ OrthoTask ortho_task(const OrthoTable &tab, uint8_t *
     return k;
 }
 
-__device__ __forceinline__ OrthoOperand symmetric_operand(long long at, int d, int block, int step) {
-    const int j = step >> 1;
-    if (j <= block) return {at + ((long long)block * 2 * d + step) * kOrthoTile, 0, false};
-    const long long first = at + ((long long)j * 2 * d + 2 * block) * kOrthoTile + (step & 1) * (kOrthoTile / 2);
-    return {first, first + kOrthoTile, true};
+__device__ __forceinline__ OrthoOperand ortho_operand(long long at, int tiles, int block, int turn, long long lo) {
+    const long long pitch = 2LL * tiles * kOrthoTile;
+    return {at + block * pitch, at + 2LL * block * kOrthoTile, pitch, lo, turn};
 }
-__device__ __forceinline__ OrthoOperand rows_operand(long long at, int ct, int block, int step) {          // k along X's rows
-    return {at + ((long long)block * 2 * ct + step) * kOrthoTile, 0, false};
-}
-__device__ __forceinline__ OrthoOperand cols_operand(long long at, int ct, int block, int step) {          // k down X's columns
-    const long long first = at + ((long long)(step >> 1) * 2 * ct + 2 * block) * kOrthoTile + (step & 1) * (kOrthoTile / 2);
-    return {first, first + kOrthoTile, true};
-}
-
-// Operands of step `step` of a task (offsets in the matrix's part; lo lies half_a, half_b behind).
-__device__ __forceinline__ void ortho_operands(const OrthoTask &k, int step, OrthoOperand &a, OrthoOperand &b, long long &half_a, long long &half_b) {
+__device__ __forceinline__ void ortho_operands(const OrthoTask &k, OrthoOperand &a, OrthoOperand &b) {
     const OrthoItem &it = *k.it;
-    const int phase = k.phase, which = k.index & 1;
     const OrthoPlace place(it.rt, it.ct);
-    const int d = min(it.rt, it.ct);
+    const int d = min(it.rt, it.ct), never = 1 << 30;
     const bool tall = it.rows > it.cols;
-    const long long x = place.x(which);
-    if (phase == kOrthoGram) {
-        half_a = half_b = place.x_bytes;
-        a = tall ? cols_operand(x, it.ct, k.i, step) : rows_operand(x, it.ct, k.i, step);
-        b = tall ? cols_operand(x, it.ct, k.j, step) : rows_operand(x, it.ct, k.j, step);
-    } else if (phase == kOrthoSquare) {
-        half_a = half_b = place.s_bytes;
-        a = symmetric_operand(place.a(), d, k.i, step);
-        b = symmetric_operand(place.a(), d, k.j, step);
+    const long long x = place.x(k.index & 1);
+    if (k.phase == kOrthoGram) {
+        a = ortho_operand(x, it.ct, k.i, tall ? 0 : never, place.x_bytes);
+        b = ortho_operand(x, it.ct, k.j, tall ? 0 : never, place.x_bytes);
+    } else if (k.phase == kOrthoSquare) {
+        a = ortho_operand(place.a(), d, k.i, 2 * (k.i + 1), place.s_bytes);
+        b = ortho_operand(place.a(), d, k.j, 2 * (k.j + 1), place.s_bytes);
     } else if (tall) {
-        half_a = place.x_bytes;
-        half_b = place.s_bytes;
-        a = rows_operand(x, it.ct, k.i, step);
-        b = symmetric_operand(place.p(), d, k.j, step);
+        a = ortho_operand(x, it.ct, k.i, never, place.x_bytes);
+        b = ortho_operand(place.p(), d, k.j, 2 * (k.j + 1), place.s_bytes);
     } else {
-        half_a = place.s_bytes;
-        half_b = place.x_bytes;
-        a = symmetric_operand(place.p(), d, k.i, step);
-        b = cols_operand(x, it.ct, k.j, step);
+        a = ortho_operand(place.p(), d, k.i, 2 * (k.i + 1), place.s_bytes);
+        b = ortho_operand(x, it.ct, k.j, 0, place.x_bytes);
     }
 }
 
@@ -266,13 +250,13 @@ __device__ __forceinline__ int load_acquire(const int *p) {
 }
 __device__ __forceinline__ void add_release(int *p, int v) { asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory"); }
 // Between ordinary accesses to global memory and those of bulk copies.
-__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+__device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 
 template <class T>
 __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __grid_constant__ OrthoTable tab, uint8_t *__restrict__ ws, int *err) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t *staging = tiles + kOStages * kOStage;
+    uint8_t *staging = tiles + kOSlots * kOSlot;
     OrthoCtl *ctl = (OrthoCtl *)(staging + kOStaging);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *abort_flag = &ctl->abort_flag;
@@ -280,7 +264,8 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
     auto give_up = [&]() { atomicOr(err, ERRW_TIMEOUT); ctl->abort_flag = 1; };
 
     if (threadIdx.x == 64) {
-        for (int s = 0; s < kOStages; ++s) { mbar_init(&ctl->full[s], 1); mbar_init(&ctl->empty[s], 1); }
+        for (int s = 0; s < kOSlots; ++s) { mbar_init(&ctl->full[s], 1); mbar_init(&ctl->empty[s], 1); }
+        for (int w = 0; w < 8; ++w) mbar_init(&ctl->old_full[w], 1);
         for (int a = 0; a < 2; ++a) { mbar_init(&ctl->acc_full[a], 1); mbar_init(&ctl->acc_empty[a], 8); }
         for (int r = 0; r < kORing; ++r) { mbar_init(&ctl->ring_full[r], 1); mbar_init(&ctl->ring_empty[r], 9); }
         ctl->abort_flag = 0;
@@ -328,37 +313,37 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                     }
                     if (!ok) break;
                 }
-                fence_proxy_async_all();
+                fence_proxy_async_global();
                 ctl->ring[r] = t;
                 mbar_arrive(&ctl->ring_full[r]);
-                for (int s = k.from; s < k.to; ++s, ++it) {
-                    const uint32_t slot = it % kOStages;
-                    ok = mbar_wait_bounded(&ctl->empty[slot], ((it / kOStages) & 1u) ^ 1u, abort_flag);
-                    if (!ok) break;
-                    OrthoOperand a, b;
-                    long long ha, hb;
-                    ortho_operands(k, s, a, b, ha, hb);
-                    const uint32_t bar = smem_u32(&ctl->full[slot]), dst = smem_u32(tiles) + slot * kOStage;
-                    mbar_arrive_expect_tx(bar, kOStage);
-                    auto bring = [&](const OrthoOperand &o, long long half, uint32_t to) {
-                        if (o.mn) {
-                            bulk_load(to, k.m + o.first + half, kOrthoTile / 2, bar);
-                            bulk_load(to + kOrthoTile / 2, k.m + o.second + half, kOrthoTile / 2, bar);
-                        } else {
-                            bulk_load(to, k.m + o.first + half, kOrthoTile, bar);
-                        }
-                    };
-                    bring(a, 0, dst);
-                    bring(b, 0, dst + 2 * kOrthoTile);
-                    bring(a, ha, dst + kOrthoTile);
-                    bring(b, hb, dst + 3 * kOrthoTile);
-                }
+                OrthoOperand a, b;
+                ortho_operands(k, a, b);
+                auto bring = [&](const OrthoOperand &o, int s, long long lo, uint32_t to, uint32_t bar) {
+                    if (s >= o.turn) {
+                        const uint8_t *p = k.m + o.cols + (s >> 1) * o.pitch + (s & 1) * (kOrthoTile / 2) + lo;
+                        bulk_load(to, p, kOrthoTile / 2, bar);
+                        bulk_load(to + kOrthoTile / 2, p + kOrthoTile, kOrthoTile / 2, bar);
+                    } else {
+                        bulk_load(to, k.m + o.rows + (long long)s * kOrthoTile + lo, kOrthoTile, bar);
+                    }
+                };
+                for (int s = k.from; ok && s < k.to; ++s)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part, ++it) {
+                        const uint32_t slot = it % kOSlots;
+                        ok = ok && mbar_wait_bounded(&ctl->empty[slot], ((it / kOSlots) & 1u) ^ 1u, abort_flag);
+                        if (!ok) break;
+                        const uint32_t bar = smem_u32(&ctl->full[slot]), dst = smem_u32(tiles) + slot * kOSlot;
+                        mbar_arrive_expect_tx(bar, kOSlot);
+                        bring(a, s, part ? a.lo : 0, dst, bar);
+                        bring(b, s, part ? b.lo : 0, dst + kOrthoTile, bar);
+                    }
                 if (!ok) break;
             }
             if (!ok) {
                 give_up();
-                for (uint32_t j = it > kOStages ? it - kOStages : 0; j < it; ++j)          // let the copies in flight land
-                    mbar_wait_bounded(&ctl->full[j % kOStages], (j / kOStages) & 1u, nullptr, 200000000ull);
+                for (uint32_t j = it > kOSlots ? it - kOSlots : 0; j < it; ++j)          // let the copies in flight land
+                    mbar_wait_bounded(&ctl->full[j % kOSlots], (j / kOSlots) & 1u, nullptr, 200000000ull);
             }
         }
     } else if (warp == 1) {
@@ -374,31 +359,36 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 mbar_arrive(&ctl->ring_empty[r]);
                 if (t < 0) break;
                 const OrthoTask k = ortho_task(tab, ws, t);
-                for (int s = k.from; s < k.to; ++s, ++it) {
+                OrthoOperand a, b;
+                ortho_operands(k, a, b);
+                for (int s = k.from; s < k.to; ++s, it += 2) {
                     const uint32_t acc = acc_it & 1u, d = tmem_base + acc * 256u, first = (uint32_t)(s - k.from) % kOSegment;
                     if (first == 0) {
                         ok = mbar_wait_bounded(&ctl->acc_empty[acc], ((acc_it >> 1) & 1u) ^ 1u, abort_flag);
                         if (!ok) break;
                         tc_fence_after_sync();
                     }
-                    const uint32_t slot = it % kOStages;
-                    ok = mbar_wait_bounded(&ctl->full[slot], (it / kOStages) & 1u, abort_flag);
+                    const uint32_t slot = it % kOSlots, slot2 = (it + 1) % kOSlots;
+                    ok = mbar_wait_bounded(&ctl->full[slot], (it / kOSlots) & 1u, abort_flag);
                     if (!ok) break;
-                    OrthoOperand a, b;
-                    long long ha, hb;
-                    ortho_operands(k, s, a, b, ha, hb);
-                    const uint32_t idesc = idesc_h16_f32(128, 128, a.mn, b.mn, 1), base = smem_u32(tiles) + slot * kOStage;
-                    const uint32_t a_hi = smem_desc_lo(base, a.mn ? 8192 : 16), a_lo = a_hi + (kOrthoTile >> 4);
-                    const uint32_t b_hi = smem_desc_lo(base + 2 * kOrthoTile, b.mn ? 8192 : 16), b_lo = b_hi + (kOrthoTile >> 4);
-                    const uint32_t sa = a.mn ? 128u : 2u, sb = b.mn ? 128u : 2u;
+                    const bool a_mn = s >= a.turn, b_mn = s >= b.turn;
+                    const uint32_t idesc = idesc_h16_f32(128, 128, a_mn, b_mn, 1), base = smem_u32(tiles) + slot * kOSlot,
+                                   base2 = smem_u32(tiles) + slot2 * kOSlot;
+                    const uint32_t a_hi = smem_desc_lo(base, a_mn ? 8192 : 16), b_hi = smem_desc_lo(base + kOrthoTile, b_mn ? 8192 : 16);
+                    const uint32_t a_lo = smem_desc_lo(base2, a_mn ? 8192 : 16);
+                    const uint32_t b_lo = smem_desc_lo(base2 + kOrthoTile, b_mn ? 8192 : 16);
+                    const uint32_t sa = a_mn ? 128u : 2u, sb = b_mn ? 128u : 2u;
 #pragma unroll
                     for (uint32_t q = 0; q < 4; ++q) umma_bf16_ss_sel(d, a_hi + q * sa, hi, b_hi + q * sb, hi, idesc, first + q);
+                    ok = mbar_wait_bounded(&ctl->full[slot2], ((it + 1) / kOSlots) & 1u, abort_flag);
+                    if (!ok) break;
 #pragma unroll
                     for (uint32_t q = 0; q < 4; ++q) {
                         umma_bf16_ss_sel(d + 128, a_hi + q * sa, hi, b_lo + q * sb, hi, idesc, first + q);
                         umma_bf16_ss_halves<true>(d + 128, a_lo + q * sa, hi, b_hi + q * sb, hi, idesc);
                     }
                     umma_commit(&ctl->empty[slot]);
+                    umma_commit(&ctl->empty[slot2]);
                     if (s + 1 == k.to || first == kOSegment - 1) { umma_commit(&ctl->acc_full[acc]); ++acc_it; }
                 }
                 if (!ok) break;
@@ -408,9 +398,9 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
     } else {
         // A warp has 32 rows of 64 columns: a quarter of a tile of the workspace, 4 KB side by side there.
         const int quarter = warp & 3, half = (warp - 2) >> 2;
-        uint8_t *buf = staging + (warp - 2) * 4096;
+        uint8_t *buf = staging + (warp - 2) * 8192;
         const uint32_t row = quarter * 32 + lane;
-        uint32_t acc_it = 0;
+        uint32_t acc_it = 0, old_ph = 0;
         bool ok = true;
         for (uint32_t n = 0;; ++n) {
             const uint32_t r = n % kORing;
@@ -434,20 +424,29 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 for (int i = 0; i < 64; ++i) v[i] = 0.f;
             } else {
                 const bool square = k.phase == kOrthoSquare;
-                const uint8_t *old = k.m + (square ? place.a() + s_at : place.x(which) + x_at);
-                const long long old_half = square ? place.s_bytes : place.x_bytes;
+                const uint8_t *old = k.m + (square ? place.a() + s_at : place.x(which) + x_at) + quarter * 4096;
+                const long long old_lo = square ? place.s_bytes : place.x_bytes;
                 const float f_old = square ? kOrthoB : kOrthoA;
                 if (square) f_new = kOrthoC / kOrthoScale;
-                uint4 oh[8], ol[8];
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    oh[c] = __ldcg((const uint4 *)(old + ortho_chunk(row, c)));
-                    ol[c] = __ldcg((const uint4 *)(old + old_half + ortho_chunk(row, c)));
+                if (lane == 0) {
+                    fence_proxy_async_global();                 // (the producer saw the counter)
+                    fence_proxy_async_smem();
+                    const uint32_t bar = smem_u32(&ctl->old_full[warp - 2]);
+                    mbar_arrive_expect_tx(bar, 8192);
+                    bulk_load(smem_u32(buf), old, 4096, bar);
+                    bulk_load(smem_u32(buf) + 4096, old + old_lo, 4096, bar);
                 }
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->old_full[warp - 2], old_ph, abort_flag));
+                if (!ok) {                                      // (the copy in flight lands before the block ends)
+                    if (lane == 0) mbar_wait_bounded(&ctl->old_full[warp - 2], old_ph, nullptr, 200000000ull);
+                    __syncwarp();
+                    break;
+                }
+                old_ph ^= 1u;
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
-                    const float2 o[4] = {half_pair(oh[c].x, ol[c].x), half_pair(oh[c].y, ol[c].y), half_pair(oh[c].z, ol[c].z),
-                                         half_pair(oh[c].w, ol[c].w)};
+                    const uint4 oh = *(const uint4 *)(buf + ortho_chunk(lane, c)), ol = *(const uint4 *)(buf + 4096 + ortho_chunk(lane, c));
+                    const float2 o[4] = {half_pair(oh.x, ol.x), half_pair(oh.y, ol.y), half_pair(oh.z, ol.z), half_pair(oh.w, ol.w)};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) { v[8 * c + 2 * e] = f_old * o[e].x; v[8 * c + 2 * e + 1] = f_old * o[e].y; }
                 }
@@ -503,72 +502,61 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 if (k.phase == kOrthoUpdate) { to = k.m + place.x(which ^ 1) + x_at; lo_at = place.x_bytes; }
                 else { to = k.m + (k.phase == kOrthoGram ? place.a() : place.p()) + s_at; lo_at = place.s_bytes; }
                 to += quarter * 4096;
-                // hi, then what is left; each through the warp's 4 KB, which is a quarter of a tile as it lies in memory
+                // through the warp's staging, where its share of a tile lies as it does in memory
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    if (lane == 0) tma_store_wait_read<0>();
-                    __syncwarp();
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t wh[4], wl[4];
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float &x0 = v[8 * c + 2 * e], &x1 = v[8 * c + 2 * e + 1];
-                            const __half2 h = __floats2half2_rn(x0, x1);
-                            const float2 back = __half22float2(h);
-                            x0 -= back.x;
-                            x1 -= back.y;
-                            w[e] = *reinterpret_cast<const uint32_t *>(&h);
-                        }
-                        *(uint4 *)(buf + ortho_chunk(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);      // (its rows start on a multiple of 8)
+                    for (int e = 0; e < 4; ++e) {
+                        const __half2 h = __floats2half2_rn(v[8 * c + 2 * e], v[8 * c + 2 * e + 1]);
+                        const float2 back = __half22float2(h);
+                        const __half2 l = __floats2half2_rn(v[8 * c + 2 * e] - back.x, v[8 * c + 2 * e + 1] - back.y);
+                        wh[e] = *reinterpret_cast<const uint32_t *>(&h);
+                        wl[e] = *reinterpret_cast<const uint32_t *>(&l);
                     }
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        bulk_store(to + part * lo_at, buf, 4096);
-                        tma_store_commit();
-                    }
+                    *(uint4 *)(buf + ortho_chunk(lane, c)) = make_uint4(wh[0], wh[1], wh[2], wh[3]);      // (its rows start on a multiple of 8)
+                    *(uint4 *)(buf + 4096 + ortho_chunk(lane, c)) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
                 }
+                fence_proxy_async_smem();
+                __syncwarp();
                 if (lane == 0) {
-                    tma_store_wait_all<0>();
-                    fence_proxy_async_all();
-                    __threadfence();
+                    bulk_store(to, buf, 4096);
+                    bulk_store(to + lo_at, buf + 4096, 4096);
+                    tma_store_commit();
+                    tma_store_wait_all<0>();                    // (written, and seen by this thread, whose release passes that on)
                     add_release(done + it.first_matrix + k.copy, 1);
                 }
+                __syncwarp();
             } else {
-                // 32 columns at a time through the warp's 4 KB, chunks of four in an order that spreads a column over the banks, then row by row
+                // through the staging, chunks of four in an order that spreads a column over the banks, then row by row
                 const int r0 = k.i * 128 + quarter * 32, rows = min(32, it.rows - r0);
                 const long long base = k.copy * ((long long)it.rows * it.cols) + (long long)r0 * it.cols;
-                if (lane == 0) tma_store_wait_read<0>();
+#pragma unroll
+                for (int c = 0; c < 16; ++c)
+                    *(float4 *)(buf + lane * 256 + ((c ^ (lane & 15)) << 4)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+                __syncwarp();
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    __syncwarp();
-#pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        *(float4 *)(buf + lane * 128 + ((c ^ (lane & 7)) << 4)) =
-                            make_float4(v[32 * h + 4 * c], v[32 * h + 4 * c + 1], v[32 * h + 4 * c + 2], v[32 * h + 4 * c + 3]);
-                    __syncwarp();
                     const int c = k.j * 128 + half * 64 + h * 32 + lane;
-                    if (c < it.cols) {
-                        auto at = [&](int i) { return *(const float *)(buf + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) * (1.f / kOrthoScale); };
-                        T *out = (T *)it.out;
-                        if (tab.muon) {
-                            float *master = it.master + base + c;
-                            for (int i0 = 0; i0 < rows; i0 += 16) {
-                                float w[16];
+                    if (c >= it.cols) continue;
+                    auto at = [&](int i) { return *(const float *)(buf + i * 256 + (((h * 8 + (lane >> 2)) ^ (i & 15)) << 4) + (lane & 3) * 4) * (1.f / kOrthoScale); };
+                    T *out = (T *)it.out;
+                    if (tab.muon) {
+                        float *master = it.master + base + c;
+                        for (int i0 = 0; i0 < rows; i0 += 16) {
+                            float w[16];
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) w[i] = i0 + i < rows ? master[(long long)(i0 + i) * it.cols] : 0.f;
+                            for (int i = 0; i < 16; ++i) w[i] = i0 + i < rows ? master[(long long)(i0 + i) * it.cols] : 0.f;
 #pragma unroll
-                                for (int i = 0; i < 16; ++i)
-                                    if (i0 + i < rows) {
-                                        const float x = fmaf(-it.scale, at(i0 + i), tab.keep * w[i]);
-                                        master[(long long)(i0 + i) * it.cols] = x;
-                                        if (out) out[base + (long long)(i0 + i) * it.cols + c] = from_f32<T>(x);
-                                    }
-                            }
-                        } else {
-                            for (int i = 0; i < rows; ++i) out[base + (long long)i * it.cols + c] = from_f32<T>(at(i));
+                            for (int i = 0; i < 16; ++i)
+                                if (i0 + i < rows) {
+                                    const float x = fmaf(-it.scale, at(i0 + i), tab.keep * w[i]);
+                                    master[(long long)(i0 + i) * it.cols] = x;
+                                    if (out) out[base + (long long)(i0 + i) * it.cols + c] = from_f32<T>(x);
+                                }
                         }
+                    } else {
+                        for (int i = 0; i < rows; ++i) out[base + (long long)i * it.cols + c] = from_f32<T>(at(i));
                     }
                 }
                 __syncwarp();
@@ -591,7 +579,7 @@ cudaError_t launch_ortho_t(const OrthoTable &t, uint8_t *ws, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     auto kernel = ortho_product_kernel<T>;
     static PerDevice attr, carve;
-    constexpr int smem = 1024 + kOStages * kOStage + kOStaging + sizeof(OrthoCtl);
+    constexpr int smem = 1024 + kOSlots * kOSlot + kOStaging + sizeof(OrthoCtl);
     if (e = max_dynamic_smem_once(kernel, smem, &attr); e != cudaSuccess) return e;
     prefer_max_shared_once(kernel, &carve);
     const int sms = device_sm_count(), widest = t.updates > t.grams ? t.updates : t.grams;
