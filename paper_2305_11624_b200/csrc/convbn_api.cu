@@ -5,6 +5,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <cmath>
 #include <map>
 #include <mutex>
@@ -1748,7 +1749,7 @@ int convbn_add(int dtype, const void *a, const void *b, void *out, long long cou
     return glue_call(3, dtype, a, b, out, count, stream);
 }
 
-static int group_norm_open(const convbn_group_norm_desc *d, GroupNormShape *s) {
+static int group_norm_open(const convbn_group_norm_desc *d, GroupNormShape *s, bool backward) {
     if (!d || d->n <= 0 || d->c <= 0 || d->h <= 0 || d->w <= 0 || d->groups <= 0 || d->c % d->groups || !(d->eps >= 0.)) return CONVBN_EINVAL;
     if (d->act < CONVBN_ACT_NONE || d->act > CONVBN_ACT_SILU) return CONVBN_EINVAL;
     if (d->dtype != CONVBN_F32 && d->dtype != CONVBN_BF16 && d->dtype != CONVBN_F16) return CONVBN_EINVAL;
@@ -1756,31 +1757,32 @@ static int group_norm_open(const convbn_group_norm_desc *d, GroupNormShape *s) {
     const long long most = 1LL << 40, hw = (long long)d->h * d->w;
     if (d->n > (1 << 30) || d->c > (1 << 20) || d->groups > 65535 || hw > most || hw > most / d->c || hw * d->c > most / d->n) return CONVBN_EINVAL;
     if (d->layout != CONVBN_NHWC) return CONVBN_EUNSUPPORTED;
-    *s = group_norm_shape(d);
+    *s = group_norm_shape(d, backward);
     return CONVBN_OK;
 }
-static int group_norm_room(const GroupNormShape &s, const void *workspace, size_t bytes) {
-    if (!workspace || bytes < group_norm_workspace(s)) return CONVBN_EWORKSPACE;
+static int group_norm_room(const convbn_group_norm_desc *d, const void *workspace, size_t bytes) {
+    if (!workspace || bytes < convbn_group_norm_workspace_bytes(d)) return CONVBN_EWORKSPACE;
     return aligned(workspace, 256) ? CONVBN_OK : CONVBN_EALIGN;
 }
 
 size_t convbn_group_norm_saved_bytes(const convbn_group_norm_desc *desc) {
     GroupNormShape s;
-    return group_norm_open(desc, &s) == CONVBN_OK ? 2 * sizeof(float) * (size_t)s.n * s.g : 0;
+    return group_norm_open(desc, &s, false) == CONVBN_OK ? 2 * sizeof(float) * (size_t)s.n * s.g : 0;
 }
 
 size_t convbn_group_norm_workspace_bytes(const convbn_group_norm_desc *desc) {
-    GroupNormShape s;
-    return group_norm_open(desc, &s) == CONVBN_OK ? group_norm_workspace(s) : 0;
+    GroupNormShape fwd, bwd;
+    if (group_norm_open(desc, &fwd, false) != CONVBN_OK || group_norm_open(desc, &bwd, true) != CONVBN_OK) return 0;
+    return std::max(group_norm_workspace(fwd, false), group_norm_workspace(bwd, true));
 }
 
 int convbn_group_norm_fwd(const convbn_group_norm_desc *desc, const void *x, const float *gamma, const float *beta, void *z, float *saved,
                           void *workspace, size_t workspace_bytes, void *stream) {
     GroupNormShape s;
-    CK(group_norm_open(desc, &s));
+    CK(group_norm_open(desc, &s, false));
     if (!x || !gamma || !beta || !z || !saved) return CONVBN_EINVAL;
     if (!aligned(x, 16) || !aligned(z, 16) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(saved, 4)) return CONVBN_EALIGN;
-    CK(group_norm_room(s, workspace, workspace_bytes));
+    CK(group_norm_room(desc, workspace, workspace_bytes));
     cudaStream_t st = (cudaStream_t)stream;
     t_prof_phase = "group_norm_fwd";
     LAUNCH("group_norm", launch_group_norm_fwd(s, x, gamma, beta, z, saved, workspace, st));
@@ -1790,11 +1792,11 @@ int convbn_group_norm_fwd(const convbn_group_norm_desc *desc, const void *x, con
 int convbn_group_norm_bwd(const convbn_group_norm_desc *desc, const void *dz, const void *x, const float *gamma, const float *beta,
                           const float *saved, void *dx, float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream) {
     GroupNormShape s;
-    CK(group_norm_open(desc, &s));
+    CK(group_norm_open(desc, &s, true));
     if (!dz || !x || !gamma || !beta || !saved || !dx || !dgamma || !dbeta) return CONVBN_EINVAL;
     if (!aligned(dz, 16) || !aligned(x, 16) || !aligned(dx, 16)) return CONVBN_EALIGN;
     if (!aligned(gamma, 4) || !aligned(beta, 4) || !aligned(saved, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4)) return CONVBN_EALIGN;
-    CK(group_norm_room(s, workspace, workspace_bytes));
+    CK(group_norm_room(desc, workspace, workspace_bytes));
     cudaStream_t st = (cudaStream_t)stream;
     t_prof_phase = "group_norm_bwd";
     LAUNCH("group_norm", launch_group_norm_bwd(s, dz, x, gamma, beta, saved, dx, dgamma, dbeta, workspace, st));

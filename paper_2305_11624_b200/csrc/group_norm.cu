@@ -4,6 +4,7 @@
 // groups, 128 bytes of a pixel or more, so that every access of a warp is whole lines) of a run of pixels of one sample; a thread keeps its
 // channels, so what belongs to a channel stays in registers.
 #include "group_norm.cuh"
+#include "sm100_ptx.cuh"
 
 namespace convbn {
 
@@ -313,41 +314,41 @@ __global__ void __launch_bounds__(kThreads) group_norm_bwd_sums_kernel(const Gro
     }
 }
 
-// dx = r (gamma dy - E[gamma dy] - xhat E[gamma dy xhat]).  Blocks behind the last sample of the last call (blockIdx.z = batch) add up dgamma
-// and dbeta over samples and runs instead.
+// dgamma and dbeta: chan [runs][c] added up, 32 channels a block.
+__global__ void __launch_bounds__(1024) group_norm_finish_kernel(long long runs, int c, const float2 *__restrict__ chan, float *__restrict__ dgamma,
+                                                                 float *__restrict__ dbeta) {
+    __shared__ float2 sums[1024];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, channel = blockIdx.x * 32 + lane;
+    float2 t = make_float2(0.f, 0.f);
+    if (channel < c) {
+#pragma unroll 4
+        for (long long i = warp; i < runs; i += 32) {
+            const float2 v = chan[i * c + channel];
+            t.x += v.x;
+            t.y += v.y;
+        }
+    }
+    sums[threadIdx.x] = t;
+    __syncthreads();
+    if (warp == 0 && channel < c) {
+        for (int k = 1; k < 32; ++k) { t.x += sums[k * 32 + lane].x; t.y += sums[k * 32 + lane].y; }
+        dbeta[channel] = t.x;
+        dgamma[channel] = t.y;
+    }
+}
+
+// dx = r (gamma dy - E[gamma dy] - xhat E[gamma dy xhat]).
 template <class T, int V, int ACT>
 __global__ void __launch_bounds__(kThreads) group_norm_bwd_apply_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
                                                                         const float *__restrict__ gamma, const float *__restrict__ beta,
-                                                                        const float *__restrict__ saved, const float2 *__restrict__ chan,
-                                                                        const float2 *__restrict__ part, T *__restrict__ dx,
-                                                                        float *__restrict__ dgamma, float *__restrict__ dbeta) {
+                                                                        const float *__restrict__ saved, const float2 *__restrict__ part,
+                                                                        T *__restrict__ dx) {
     __shared__ float2 stat[kNormMaxSlabGroups];
-    __shared__ float2 sums[kThreads];
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if ((int)blockIdx.z == s.batch) {
-        // 32 channels a block, eight threads a channel
-        const long long runs = (long long)s.n * s.splits;
-        for (int c0 = (blockIdx.y * gridDim.x + blockIdx.x) * 32; c0 < s.c; c0 += gridDim.x * gridDim.y * 32) {
-            float2 t = make_float2(0.f, 0.f);
-            if (c0 + lane < s.c)
-                for (long long i = warp; i < runs; i += kThreads / 32) {
-                    const float2 v = chan[i * s.c + c0 + lane];
-                    t.x += v.x;
-                    t.y += v.y;
-                }
-            sums[threadIdx.x] = t;
-            __syncthreads();
-            if (warp == 0 && c0 + lane < s.c) {
-                for (int k = 1; k < kThreads / 32; ++k) { t.x += sums[k * 32 + lane].x; t.y += sums[k * 32 + lane].y; }
-                dbeta[c0 + lane] = t.x;
-                dgamma[c0 + lane] = t.y;
-            }
-            __syncthreads();
-        }
-        return;
-    }
     const int slab = blockIdx.y, split = blockIdx.x;
     const int n = s.n0 + blockIdx.z;
     const float *mean_p = saved + (long long)n * s.g + (long long)slab * s.slab_g, *rstd_p = mean_p + (long long)s.n * s.g;
@@ -413,6 +414,275 @@ __global__ void __launch_bounds__(kThreads) group_norm_bwd_apply_kernel(const Gr
     }
 }
 
+// ---- one pass: a sample's slab is kept on chip by a cluster of blocks -----------------------------------------------------------------
+// A block has a run of the sample's pixels, a thread `keep` of them, 16 bytes each, in places of shared memory that are its own: the copies
+// need no registers while they are under way and no barrier.  Sums go over the cluster through shared memory.
+constexpr int kFusedMax = 8;                   // blocks of a cluster
+constexpr int kFusedBytes = 72 * 1024;         // of a block: three blocks an SM
+
+__device__ __forceinline__ void copy16(void *dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+
+// ONE: all channels of a thread belong to one group.
+template <class T, int ACT, bool ONE>
+__global__ void __launch_bounds__(kThreads, 3) group_norm_fused_fwd_kernel(const GroupNormShape s, const T *__restrict__ x, const float *__restrict__ gamma,
+                                                                           const float *__restrict__ beta, float *__restrict__ saved, T *__restrict__ z) {
+    constexpr int V = 16 / (int)sizeof(T), W = ONE ? 1 : V;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    using Vec = NormVec<T, V>;
+    Vec *kept = (Vec *)smem_raw + threadIdx.x;
+    __shared__ float red[kThreads * W];
+    __shared__ float mu[kNormMaxSlabGroups];
+    __shared__ float2 part[kNormMaxSlabGroups], stat[kNormMaxSlabGroups];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int rank = blockIdx.x % s.splits, slab = blockIdx.x / s.splits, n = s.n0 + blockIdx.y;
+    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
+    const int first = rank * (int)s.rows, rows = max(0, min((int)s.rows, (int)s.pixels - first));
+    const long long base = ((long long)n * s.pixels + first) * s.c + (long long)slab * s.slab_c + tx * V;
+    const int mine = ty < s.ty && ty < rows ? (rows - ty + s.ty - 1) / s.ty : 0;
+    const long long pitch = (long long)s.ty * s.c;
+    {
+        const T *p = x + base + (long long)ty * s.c;
+        for (int k = 0; k < mine; ++k, p += pitch) copy16(kept + k * kThreads, p);
+    }
+    const int group = ONE ? (s.slab_g == 1 ? 0 : tx * V / s.cg) : 0, per = ONE ? (s.slab_g == 1 ? s.tx : s.cg / V) : s.cg;
+    const int width = s.tx * W;
+    const float inv = rows > 0 ? 1.f / ((float)rows * (float)s.cg) : 0.f;
+    copies_wait();
+    // the block's means, then the distances from them
+    float sum[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) sum[i] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < mine; ++k) {
+        float f[V];
+        kept[k * kThreads].get(f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[ONE ? 0 : i] += f[i];
+    }
+    if (ty < s.ty)
+#pragma unroll
+        for (int i = 0; i < W; ++i) red[ty * width + tx * W + i] = sum[i];
+    __syncthreads();
+    group_sums(red, s.ty, width, per, s.slab_g, [&](int g, float v) { mu[g] = v * inv; });
+    __syncthreads();
+    float m[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) { m[i] = mu[ONE ? group : (tx * V + i) / s.cg]; sum[i] = 0.f; }
+#pragma unroll 4
+    for (int k = 0; k < mine; ++k) {
+        float f[V];
+        kept[k * kThreads].get(f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) { const float d = f[i] - m[ONE ? 0 : i]; sum[ONE ? 0 : i] = fmaf(d, d, sum[ONE ? 0 : i]); }
+    }
+    if (ty < s.ty)
+#pragma unroll
+        for (int i = 0; i < W; ++i) red[ty * width + tx * W + i] = sum[i];
+    __syncthreads();
+    group_sums(red, s.ty, width, per, s.slab_g, [&](int g, float v) { part[g] = make_float2(mu[g], v); });
+    if (s.splits > 1) ptx::cluster_sync_all(); else __syncthreads();
+    for (int g = threadIdx.x; g < s.slab_g; g += kThreads) {
+        // the blocks' runs joined (pairwise update of mean and squared distances)
+        float2 all = part[g];
+        if (s.splits > 1) {
+            float cnt = 0.f;
+            all = make_float2(0.f, 0.f);
+            for (int b = 0; b < s.splits; ++b) {
+                const float2 v = ld_cluster_f2(ptx::cluster_addr(&part[g], b));
+                const float add = (float)max(0, min((int)s.rows, (int)s.pixels - b * (int)s.rows)), share = add / (cnt + add), d = v.x - all.x;
+                all.x = fmaf(d, share, all.x);
+                all.y += fmaf(d * d, cnt * share * (float)s.cg, v.y);
+                cnt += add;
+            }
+        }
+        const float r = 1.f / sqrtf(all.y / ((float)s.pixels * (float)s.cg) + s.eps);
+        stat[g] = make_float2(all.x, r);
+        if (rank == 0) {
+            const long long at = (long long)n * s.g + (long long)slab * s.slab_g + g;
+            saved[at] = all.x;
+            saved[(long long)s.n * s.g + at] = r;
+        }
+    }
+    if (s.splits > 1) ptx::cluster_arrive_started();             // (done with the others' shared memory)
+    __syncthreads();
+    if (mine > 0) {
+        float sub[W], mul[V], add[V];
+        const int c0 = slab * s.slab_c + tx * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float2 st = stat[ONE ? group : (tx * V + i) / s.cg];
+            sub[ONE ? 0 : i] = st.x;
+            mul[i] = __ldg(gamma + c0 + i) * st.y;
+            add[i] = __ldg(beta + c0 + i);
+        }
+        T *p = z + base + (long long)ty * s.c;
+#pragma unroll 2
+        for (int k = 0; k < mine; ++k, p += pitch) {
+            Vec v = kept[k * kThreads];
+            float f[V];
+            v.get(f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] = norm_act<ACT>(fmaf(f[i] - sub[ONE ? 0 : i], mul[i], add[i]));
+            v.put(f);
+            v.store(p);
+        }
+    }
+    if (s.splits > 1) ptx::cluster_wait_started();               // no block ends while another may read from it
+}
+
+template <class T, int ACT, bool ONE>
+__global__ void __launch_bounds__(kThreads, 2) group_norm_fused_bwd_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
+                                                                           const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                                           const float *__restrict__ saved, float2 *__restrict__ chan,
+                                                                           T *__restrict__ dx) {
+    constexpr int V = 16 / (int)sizeof(T), W = ONE ? 1 : V;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    using Vec = NormVec<T, V>;
+    Vec *kept = (Vec *)smem_raw + threadIdx.x;                   // x and dz of a pixel in turn
+    __shared__ float red_a[kThreads * V], red_b[kThreads * V];
+    __shared__ float2 part[kNormMaxSlabGroups], stat[kNormMaxSlabGroups];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int rank = blockIdx.x % s.splits, slab = blockIdx.x / s.splits, n = s.n0 + blockIdx.y;
+    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
+    const int first = rank * (int)s.rows, rows = max(0, min((int)s.rows, (int)s.pixels - first));
+    const long long base = ((long long)n * s.pixels + first) * s.c + (long long)slab * s.slab_c + tx * V;
+    const int mine = ty < s.ty && ty < rows ? (rows - ty + s.ty - 1) / s.ty : 0;
+    const long long pitch = (long long)s.ty * s.c;
+    {
+        long long at = base + (long long)ty * s.c;
+        for (int k = 0; k < mine; ++k, at += pitch) {
+            copy16(kept + 2 * k * kThreads, x + at);
+            copy16(kept + (2 * k + 1) * kThreads, dz + at);
+        }
+    }
+    float mean[W], rstd[W], gm[V], bt[V], a[V], b[V];
+    const int c0 = slab * s.slab_c + tx * V;
+    const float *mean_p = saved + (long long)n * s.g + (long long)slab * s.slab_g, *rstd_p = mean_p + (long long)s.n * s.g;
+    if (ty < s.ty) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int g = (tx * V + i) / s.cg;
+            if (!ONE || i == 0) { mean[ONE ? 0 : i] = __ldg(mean_p + g); rstd[ONE ? 0 : i] = __ldg(rstd_p + g); }
+            gm[i] = __ldg(gamma + c0 + i);
+            bt[i] = __ldg(beta + c0 + i);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) a[i] = b[i] = 0.f;
+    copies_wait();
+#pragma unroll 2
+    for (int k = 0; k < mine; ++k) {
+        float fx[V], fz[V];
+        kept[2 * k * kThreads].get(fx);
+        kept[(2 * k + 1) * kThreads].get(fz);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float mn = mean[ONE ? 0 : i], rs = rstd[ONE ? 0 : i], xc = fx[i] - mn;
+            const float dy = norm_act_grad<ACT>(fz[i], xc, fx[i], mn, rs, gm[i], gm[i] * rs, bt[i]);
+            a[i] += dy;
+            b[i] = fmaf(dy, xc, b[i]);
+        }
+    }
+    const int width = s.tx * V;
+    if (ty < s.ty)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            red_a[ty * width + tx * V + i] = a[i];
+            red_b[ty * width + tx * V + i] = mine > 0 ? b[i] * rstd[ONE ? 0 : i] : 0.f;
+        }
+    __syncthreads();
+    for (int c = threadIdx.x; c < width; c += kThreads) {
+        float sa = 0.f, sb = 0.f;
+        for (int k = 0; k < s.ty; ++k) { sa += red_a[k * width + c]; sb += red_b[k * width + c]; }
+        chan[((long long)n * s.splits + rank) * s.c + slab * s.slab_c + c] = make_float2(sa, sb);
+        const float g = __ldg(gamma + slab * s.slab_c + c);
+        red_a[c] = g * sa;                       // (row 0 of this column has been read by this thread)
+        red_b[c] = g * sb;
+    }
+    __syncthreads();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int g = warp; g < s.slab_g; g += kThreads / 32) {
+        float sa = 0.f, sb = 0.f;
+        for (int i = lane; i < s.cg; i += 32) { sa += red_a[g * s.cg + i]; sb += red_b[g * s.cg + i]; }
+        sa = warp_sum(sa);
+        sb = warp_sum(sb);
+        if (lane == 0) part[g] = make_float2(sa, sb);
+    }
+    if (s.splits > 1) ptx::cluster_sync_all(); else __syncthreads();
+    for (int g = threadIdx.x; g < s.slab_g; g += kThreads) {
+        float2 all = part[g];
+        if (s.splits > 1) {
+            all = make_float2(0.f, 0.f);
+            for (int k = 0; k < s.splits; ++k) {
+                const float2 v = ld_cluster_f2(ptx::cluster_addr(&part[g], k));
+                all.x += v.x;
+                all.y += v.y;
+            }
+        }
+        const float inv = 1.f / ((float)s.pixels * (float)s.cg), r = __ldg(rstd_p + g);
+        stat[g] = make_float2(all.x * inv * r, all.y * inv * r * r);
+    }
+    if (s.splits > 1) ptx::cluster_arrive_started();
+    __syncthreads();
+    if (mine > 0) {
+        float k1[W], k2[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float2 st = stat[(tx * V + i) / s.cg];
+            k1[i] = st.x;
+            k2[i] = st.y;
+        }
+        T *p = dx + base + (long long)ty * s.c;
+#pragma unroll 2
+        for (int k = 0; k < mine; ++k, p += pitch) {
+            float fx[V], fz[V];
+            kept[2 * k * kThreads].get(fx);
+            kept[(2 * k + 1) * kThreads].get(fz);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int o = ONE ? 0 : i;
+                const float xc = fx[i] - mean[o], scale = gm[i] * rstd[o];
+                const float dy = norm_act_grad<ACT>(fz[i], xc, fx[i], mean[o], rstd[o], gm[i], scale, bt[i]);
+                fx[i] = fmaf(dy, scale, fmaf(-xc, k2[o], -k1[o]));
+            }
+            Vec v;
+            v.put(fx);
+            v.store(p);
+        }
+    }
+    if (s.splits > 1) ptx::cluster_wait_started();
+}
+
+template <class K, class... Args>
+cudaError_t launch_fused(K kernel, PerDevice *attr, const GroupNormShape &s, int per_pixel, cudaStream_t st, Args... args) {
+    const int smem = s.keep * kThreads * per_pixel;
+    if (cudaError_t e = max_dynamic_smem_once(kernel, kFusedBytes, attr); e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(s.splits * (s.g / s.slab_g)), (unsigned)s.batch);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = s.splits;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = s.splits > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, s, args...);
+}
+
 // f(a value of the storage type, elements per access, activation)
 template <class F>
 cudaError_t dispatch(const GroupNormShape &s, F &&f) {
@@ -437,7 +707,7 @@ cudaError_t dispatch(const GroupNormShape &s, F &&f) {
 
 }  // namespace
 
-GroupNormShape group_norm_shape(const convbn_group_norm_desc *d) {
+GroupNormShape group_norm_shape(const convbn_group_norm_desc *d, bool backward) {
     GroupNormShape s;
     s.n = d->n; s.c = d->c; s.g = d->groups; s.cg = d->c / d->groups; s.act = d->act; s.dtype = d->dtype;
     s.pixels = (long long)d->h * d->w;
@@ -460,22 +730,47 @@ GroupNormShape group_norm_shape(const convbn_group_norm_desc *d) {
     s.tx = s.cols < kThreads ? s.cols : kThreads;
     s.ty = kThreads / s.tx;
     s.one_group = s.slab_g == 1 || s.cg % s.vec == 0;
+    s.n0 = 0;
+    s.batch = s.n;
+    // Kept on chip: as few blocks as hold the sample's slab, more of them where that leaves SMs idle.
+    const long long slabs = s.g / s.slab_g;
+    const int sms = device_sm_count(), per_pixel = backward ? 32 : 16, most_kept = kFusedBytes / (kThreads * per_pixel);
+    s.keep = 0;
+    if (s.vec * es == 16 && s.cols <= kThreads && s.pixels <= (long long)kFusedMax * most_kept * s.ty) {
+        int splits = (int)((s.pixels + (long long)most_kept * s.ty - 1) / ((long long)most_kept * s.ty));
+        while (splits < kFusedMax && slabs * s.n * splits < 4LL * sms && s.pixels > 2LL * s.ty * splits) ++splits;
+        s.rows = (s.pixels + splits - 1) / splits;
+        s.splits = (int)((s.pixels + s.rows - 1) / s.rows);
+        s.keep = (int)((s.rows + s.ty - 1) / s.ty);
+        return s;
+    }
     // Runs of pixels: four blocks an SM over the whole batch, each thread at least eight pixels.
-    const long long slabs = s.g / s.slab_g, want = (4LL * device_sm_count() + slabs * s.n - 1) / (slabs * s.n);
+    const long long want = (4LL * sms + slabs * s.n - 1) / (slabs * s.n);
     const long long most = (s.pixels + 8 * s.ty - 1) / (8 * s.ty);
     s.splits = (int)(want < most ? want : most);
     if (s.splits > 1024) s.splits = 1024;
     s.rows = (s.pixels + s.splits - 1) / s.splits;
     s.splits = (int)((s.pixels + s.rows - 1) / s.rows);
-    s.n0 = 0;
-    s.batch = s.n;
     return s;
 }
 
-// [runs][groups] pairs, then (backward) [runs][channels] pairs
-size_t group_norm_workspace(const GroupNormShape &s) {
+// Two passes: [runs][groups] pairs.  Backward: [runs][channels] pairs behind them.
+size_t group_norm_workspace(const GroupNormShape &s, bool backward) {
     const size_t runs = (size_t)s.n * s.splits;
-    return align_up(runs * s.g * sizeof(float2), 256) + align_up(runs * s.c * sizeof(float2), 256);
+    return align_up(runs * s.g * sizeof(float2), 256) + (backward ? align_up(runs * s.c * sizeof(float2), 256) : 0);
+}
+
+// f(first sample, samples) for every launch's share of the batch
+template <class F>
+static cudaError_t by_batch(const GroupNormShape &shape, F &&f) {
+    GroupNormShape s = shape;
+    cudaError_t e = cudaSuccess;
+    for (int n0 = 0; n0 < shape.n && e == cudaSuccess; n0 += kNormMaxBatch) {
+        s.n0 = n0;
+        s.batch = shape.n - n0 < kNormMaxBatch ? shape.n - n0 : kNormMaxBatch;
+        e = f(s);
+    }
+    return e;
 }
 
 cudaError_t launch_group_norm_fwd(const GroupNormShape &shape, const void *x, const float *gamma, const float *beta, void *z, float *saved,
@@ -483,43 +778,51 @@ cudaError_t launch_group_norm_fwd(const GroupNormShape &shape, const void *x, co
     return dispatch(shape, [&](auto t, auto v, auto act) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, ACT = decltype(act)::value;
-        GroupNormShape s = shape;
-        cudaError_t e = cudaSuccess;
-        for (int n0 = 0; n0 < shape.n && e == cudaSuccess; n0 += kNormMaxBatch) {
-            s.n0 = n0;
-            s.batch = shape.n - n0 < kNormMaxBatch ? shape.n - n0 : kNormMaxBatch;
-            const dim3 grid((unsigned)s.splits, (unsigned)(s.g / s.slab_g), (unsigned)s.batch);
-            e = launch_pdl(group_norm_stats_kernel<T, V>, grid, dim3(kThreads), 0, st, s, (const T *)x, (float2 *)workspace);
-            if (e == cudaSuccess)
-                e = launch_pdl(group_norm_apply_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)x, gamma, beta, (const float2 *)workspace,
-                               saved, (T *)z);
+        if constexpr (V * sizeof(T) == 16) {
+            static PerDevice attr[2];
+            if (shape.keep)
+                return by_batch(shape, [&](const GroupNormShape &s) {
+                    auto kernel = s.one_group ? group_norm_fused_fwd_kernel<T, ACT, true> : group_norm_fused_fwd_kernel<T, ACT, false>;
+                    return launch_fused(kernel, &attr[s.one_group], s, 16, st, (const T *)x, gamma, beta, saved, (T *)z);
+                });
         }
-        return e;
+        return by_batch(shape, [&](const GroupNormShape &s) {
+            const dim3 grid((unsigned)s.splits, (unsigned)(s.g / s.slab_g), (unsigned)s.batch);
+            const cudaError_t e = launch_pdl(group_norm_stats_kernel<T, V>, grid, dim3(kThreads), 0, st, s, (const T *)x, (float2 *)workspace);
+            if (e != cudaSuccess) return e;
+            return launch_pdl(group_norm_apply_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)x, gamma, beta, (const float2 *)workspace,
+                              saved, (T *)z);
+        });
     });
 }
 
 cudaError_t launch_group_norm_bwd(const GroupNormShape &shape, const void *dz, const void *x, const float *gamma, const float *beta,
                                   const float *saved, void *dx, float *dgamma, float *dbeta, void *workspace, cudaStream_t st) {
-    return dispatch(shape, [&](auto t, auto v, auto act) {
+    float2 *part = (float2 *)workspace;
+    float2 *chan = (float2 *)((char *)workspace + align_up((size_t)shape.n * shape.splits * shape.g * sizeof(float2), 256));
+    const cudaError_t e = dispatch(shape, [&](auto t, auto v, auto act) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, ACT = decltype(act)::value;
-        GroupNormShape s = shape;
-        float2 *part = (float2 *)workspace;
-        float2 *chan = (float2 *)((char *)workspace + align_up((size_t)s.n * s.splits * s.g * sizeof(float2), 256));
-        cudaError_t e = cudaSuccess;
-        for (int n0 = 0; n0 < shape.n && e == cudaSuccess; n0 += kNormMaxBatch) {
-            s.n0 = n0;
-            s.batch = shape.n - n0 < kNormMaxBatch ? shape.n - n0 : kNormMaxBatch;
-            const bool final = n0 + s.batch == shape.n;
-            dim3 grid((unsigned)s.splits, (unsigned)(s.g / s.slab_g), (unsigned)s.batch);
-            e = launch_pdl(group_norm_bwd_sums_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)dz, (const T *)x, gamma, beta, saved, chan, part);
-            if (e != cudaSuccess) break;
-            grid.z += final ? 1 : 0;
-            e = launch_pdl(group_norm_bwd_apply_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)dz, (const T *)x, gamma, beta, saved,
-                           (const float2 *)chan, (const float2 *)part, (T *)dx, dgamma, dbeta);
+        if constexpr (V * sizeof(T) == 16) {
+            static PerDevice attr[2];
+            if (shape.keep)
+                return by_batch(shape, [&](const GroupNormShape &s) {
+                    auto kernel = s.one_group ? group_norm_fused_bwd_kernel<T, ACT, true> : group_norm_fused_bwd_kernel<T, ACT, false>;
+                    return launch_fused(kernel, &attr[s.one_group], s, 32, st, (const T *)dz, (const T *)x, gamma, beta, saved, chan, (T *)dx);
+                });
         }
-        return e;
+        return by_batch(shape, [&](const GroupNormShape &s) {
+            const dim3 grid((unsigned)s.splits, (unsigned)(s.g / s.slab_g), (unsigned)s.batch);
+            const cudaError_t e = launch_pdl(group_norm_bwd_sums_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)dz, (const T *)x, gamma, beta,
+                                             saved, chan, part);
+            if (e != cudaSuccess) return e;
+            return launch_pdl(group_norm_bwd_apply_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)dz, (const T *)x, gamma, beta, saved,
+                              (const float2 *)part, (T *)dx);
+        });
     });
+    if (e != cudaSuccess) return e;
+    return launch_pdl(group_norm_finish_kernel, dim3((unsigned)((shape.c + 31) / 32)), dim3(1024), 0, st, (long long)shape.n * shape.splits, shape.c,
+                      (const float2 *)chan, dgamma, dbeta);
 }
 
 }  // namespace convbn

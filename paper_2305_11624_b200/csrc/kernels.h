@@ -391,10 +391,11 @@ struct GroupNormShape {
     int splits;                    // runs of pixels a sample is cut into ...
     long long rows, pixels;        // ... pixels of a run, of a sample
     int n0, batch;                 // samples of a launch
+    int keep;                      // pixels that a thread keeps in shared memory: a run is a block of a cluster (0: two passes over memory)
     float eps;
 };
-GroupNormShape group_norm_shape(const convbn_group_norm_desc *d);     // (of a valid descriptor)
-size_t group_norm_workspace(const GroupNormShape &s);
+GroupNormShape group_norm_shape(const convbn_group_norm_desc *d, bool backward);     // (of a valid descriptor)
+size_t group_norm_workspace(const GroupNormShape &s, bool backward);
 cudaError_t launch_group_norm_fwd(const GroupNormShape &s, const void *x, const float *gamma, const float *beta, void *z, float *saved,
                                   void *workspace, cudaStream_t st);
 cudaError_t launch_group_norm_bwd(const GroupNormShape &s, const void *dz, const void *x, const float *gamma, const float *beta,
