@@ -1,218 +1,319 @@
 // Group norm with its activation over channels-last activations, forward and backward (formulas: group_norm.cuh).
 //
-// Two passes each way.  The first sums, the second reads the same tensors again and writes.  A block takes a slab of channels (whole
-// groups, 128 bytes of a pixel or more, so that every access of a warp is whole lines) of a run of pixels of one sample; a thread keeps its
-// channels, so what belongs to a channel stays in registers.
+// A block takes a slab of channels (whole groups, 128 bytes of a pixel or more, so that every access of a warp is whole lines) and a run of
+// pixels of one sample; a thread keeps its channels, so what belongs to a channel stays in registers.
+//   on chip     where one block holds the slab of a sample in shared memory (or a cluster does, where there are few slabs): read once.
+//   two passes  otherwise: the first sums, the second reads the same tensors again, the latest first, from L2 as far as that has them, and
+//               writes.
+// Bound by memory; what is lost are the ends of passes, where sums go round.  So a run is long, its sums are shared by warp shuffles first,
+// and few runs are left for the second pass to join: clusters of eight blocks join theirs.
 #include "group_norm.cuh"
+
+#include <algorithm>
+
 #include "sm100_ptx.cuh"
 
 namespace convbn {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;                  // of the two passes' blocks
+constexpr int kKept = 224;                     // bytes of shared memory that a thread keeps pixels in: 1024 threads' share is the SM's
+constexpr int kMaxKeptThreads = 512;
 
-// Sums of a block: of the elements that its warps hold in `red`, [rows][width] with `rows` thread rows; groups of `size` neighbours.
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+template <int V>
+__device__ __forceinline__ float at(const f32x2 (&v)[(V + 1) / 2], int i) {
+    const float2 f = split2(v[i / 2]);
+    return i % 2 ? f.y : f.x;
+}
+// Sums over a warp's rows of threads, where tx divides 32 (lanes below tx have them).
+__device__ __forceinline__ float fold(const GroupNormShape &s, float v) {
+    if (s.fold)
+        for (int o = s.tx; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// Where a thread's sums go in a block's table [rows][tx]: rows are warps after fold(), else rows of threads; -1: nowhere.
+__device__ __forceinline__ int table_row(const GroupNormShape &s) {
+    const int lane = threadIdx.x & 31;
+    if (s.fold) return lane < s.tx ? (int)threadIdx.x >> 5 : -1;
+    const int ty = threadIdx.x / s.tx;
+    return ty < s.ty ? ty : -1;
+}
+__device__ __forceinline__ int table_rows(const GroupNormShape &s) { return s.fold ? (int)blockDim.x >> 5 : s.ty; }
+// Sums of `red`, [rows][width], over its rows and over groups of `size` neighbours: out(group, sum).
 template <class F>
 __device__ __forceinline__ void group_sums(const float *red, int rows, int width, int size, int groups, F &&out) {
+    if (rows * size <= 8) {                                           // a thread per group
+        for (int g = threadIdx.x; g < groups; g += blockDim.x) {
+            float s = 0.f;
+            for (int r = 0; r < rows; ++r)
+                for (int i = 0; i < size; ++i) s += red[r * width + g * size + i];
+            out(g, s);
+        }
+        return;
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int g = warp; g < groups; g += kThreads / 32) {
+    for (int g = warp; g < groups; g += blockDim.x >> 5) {
         float s = 0.f;
-        for (int i = lane; i < rows * size; i += 32) s += red[(i / size) * width + g * size + i % size];
+        for (int r = 0; r < rows; ++r)
+            for (int i = lane; i < size; i += 32) s += red[r * width + g * size + i];
         s = warp_sum(s);
         if (lane == 0) out(g, s);
     }
 }
 
-// Mean and sum of squared distances of a run of pixels, per group: part[(n splits + split) groups + g].
-// Every thread sums distances from its channel's first value, which is one of the values: what those sums lose by rounding is small against
-// the spread that the value itself brings in, however far the mean is from zero.
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+// Means and squared distances of runs, joined: run b has weight(b) values a channel, pair(b) its numbers.
+template <class W, class P>
+__device__ __forceinline__ float2 join_runs(int runs, float total, float cg, W &&weight, P &&pair_of) {
+    float m = 0.f, q = 0.f;
+    for (int b = 0; b < runs; ++b) m = fmaf(weight(b) / total, pair_of(b).x, m);
+    for (int b = 0; b < runs; ++b) {
+        const float2 v = pair_of(b);
+        const float d = v.x - m;
+        q += fmaf(weight(b) * cg * d, d, v.y);
+    }
+    return make_float2(m, q);
+}
+
+// minus_mean, scale, beta of the V channels from c0 on (c0 and stat: within the slab); what lies beside V = 1's channel is zero.
+template <int V, bool ONE, class F>
+__device__ __forceinline__ void set_channels(NormChannels<V, ONE> &k, int c0, int cg, const float *gamma, const float *beta, F &&stat) {
+    float2 one;
+    if constexpr (ONE) one = stat(c0 / cg);
+#pragma unroll
+    for (int i = 0; i < NormChannels<V, ONE>::P; ++i) {
+        float m[2] = {0.f, 0.f}, sc[2] = {0.f, 0.f}, b[2] = {0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < (V > 1 ? 2 : 1); ++e) {
+            const int c = c0 + 2 * i + e;
+            const float2 st = ONE ? one : stat(c / cg);
+            m[e] = -st.x;
+            sc[e] = __ldg(gamma + c) * st.y;
+            b[e] = __ldg(beta + c);
+        }
+        if (!ONE || i == 0) k.minus_mean[ONE ? 0 : i] = pair(m[0], m[1]);
+        k.scale[i] = pair(sc[0], sc[1]);
+        k.beta[i] = pair(b[0], b[1]);
+    }
+}
+template <int V, bool ONE>
+__device__ __forceinline__ float near_zero(const NormChannels<V, ONE> &k) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) top = fmaxf(top, fabsf(at<V>(k.beta, i)));
+    return top * 0x1p-20f;
+}
+
+// ---- sums of a run ------------------------------------------------------------------------------------------------------------------------
+// A thread's values as distances from its channel's first one, which is one of the values: what the sums lose by rounding is small against the
+// spread that the value itself brings in, however far the mean is from zero.
 template <class T, int V>
-__global__ void __launch_bounds__(kThreads) group_norm_stats_kernel(const GroupNormShape s, const T *__restrict__ x, float2 *__restrict__ part) {
+struct Spread {
+    static constexpr int P = (V + 1) / 2;
+    f32x2 ck[P], cs[P], cq[P];                       // per channel: minus the first value, sums of distances and of their squares
+    __device__ __forceinline__ void none() {
+#pragma unroll
+        for (int i = 0; i < P; ++i) ck[i] = cs[i] = cq[i] = 0ull;
+    }
+    __device__ __forceinline__ void first(const NormVec<T, V> &v) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) { ck[i] = mul2(v.get(i), both(-1.f)); cs[i] = cq[i] = 0ull; }
+    }
+    __device__ __forceinline__ void add(const NormVec<T, V> &v) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) { const f32x2 d = add2(v.get(i), ck[i]); cs[i] = add2(cs[i], d); cq[i] = fma2(d, d, cq[i]); }
+    }
+    __device__ __forceinline__ float mean(int i, float inv) const { return fmaf(at<V>(cs, i), inv, -at<V>(ck, i)); }
+    // squared distances from m
+    __device__ __forceinline__ float square(int i, float k, float inv, float m) const {
+        const float c = at<V>(cs, i), d = fmaf(c, inv, -at<V>(ck, i)) - m;
+        return fmaf(-c * inv, c, at<V>(cq, i)) + k * d * d;
+    }
+};
+// Of a thread's columns, where they belong to one group: count, mean, squared distances (Chan, Golub, LeVeque: pairwise updates of a variance).
+struct Moments {
+    float cnt = 0.f, mean = 0.f, m2 = 0.f;
+    template <class T, int V>
+    __device__ __forceinline__ void join(const Spread<T, V> &p, int seen) {
+        const float k = (float)seen, inv = 1.f / k;
+        float m = 0.f, q = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) m += p.mean(i, inv);
+        m *= 1.f / V;
+#pragma unroll
+        for (int i = 0; i < V; ++i) q += p.square(i, k, inv, m);
+        const float add = k * V, all = cnt + add, d = m - mean, share = add / all;
+        mean = fmaf(d, share, mean);
+        m2 += q + d * d * (cnt * share);
+        cnt = all;
+    }
+};
+// The block's groups: out(group, (mean, squared distances)).  `one`: m holds the thread's values, else p does, `seen` of each channel.
+template <class T, int V, class F>
+__device__ __forceinline__ void block_moments(const GroupNormShape &s, float *red, float *mu, bool one, const Moments &m, const Spread<T, V> &p, int seen,
+                                              float rows, F &&out) {
+    const int tx = threadIdx.x % s.tx, to = table_row(s), lines = table_rows(s);
+    const float total = 1.f / (rows * (float)s.cg);
+    if (one) {
+        // threads' columns of a group are neighbours
+        const int per = s.slab_g == 1 ? s.tx : s.cg / V, g = s.slab_g == 1 ? 0 : tx / per;
+        const float a = fold(s, m.cnt * m.mean);
+        if (to >= 0) red[to * s.tx + tx] = a;
+        __syncthreads();
+        group_sums(red, lines, s.tx, per, s.slab_g, [&](int k, float v) { mu[k] = v * total; });
+        __syncthreads();
+        const float d = m.mean - mu[g], b = fold(s, m.cnt > 0.f ? m.m2 + m.cnt * d * d : 0.f);
+        if (to >= 0) red[to * s.tx + tx] = b;
+        __syncthreads();
+        group_sums(red, lines, s.tx, per, s.slab_g, [&](int k, float v) { out(k, make_float2(mu[k], v)); });
+    } else {
+        const float k = (float)seen, inv = seen ? 1.f / k : 0.f;
+        const int width = s.tx * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float a = fold(s, k * p.mean(i, inv));
+            if (to >= 0) red[to * width + tx * V + i] = a;
+        }
+        __syncthreads();
+        group_sums(red, lines, width, s.cg, s.slab_g, [&](int g, float v) { mu[g] = v * total; });
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float b = fold(s, seen ? p.square(i, k, inv, mu[(tx * V + i) / s.cg]) : 0.f);
+            if (to >= 0) red[to * width + tx * V + i] = b;
+        }
+        __syncthreads();
+        group_sums(red, lines, width, s.cg, s.slab_g, [&](int g, float v) { out(g, make_float2(mu[g], v)); });
+    }
+}
+
+// ---- two passes -----------------------------------------------------------------------------------------------------------------------
+// Mean and sum of squared distances of a cluster's runs of pixels, per group: part[(n runs + run) groups + g], runs = splits / cluster.
+template <class T, int V>
+__global__ void __launch_bounds__(kThreads, 3) group_norm_stats_kernel(const GroupNormShape s, const T *__restrict__ x, float2 *__restrict__ part) {
     __shared__ float red[kThreads * V];
     __shared__ float mu[kNormMaxSlabGroups];
+    __shared__ float2 own[kNormMaxSlabGroups];
     pdl_wait();
     pdl_launch_dependents();
     const int slab = blockIdx.y, split = blockIdx.x;
     const int n = s.n0 + blockIdx.z;
     const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
-    const long long first = (long long)split * s.rows, last = min(first + s.rows, s.pixels);
-    const T *base = x + ((long long)n * s.pixels) * s.c + (long long)slab * s.slab_c;
-    const bool live = ty < s.ty;
-    float cnt = 0.f, mean = 0.f, m2 = 0.f;            // of all the thread's values (channels of one group)
-    float ck[V], cs[V], cq[V];                        // per channel: first value, sums of distances and squares
-    int seen = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) ck[i] = cs[i] = cq[i] = 0.f;
-    for (int col = tx; col < s.cols; col += s.tx) {
-        const T *p = base + (long long)col * V;
-        seen = 0;
-        long long r = first + ty;
-        if (live && r < last) {
+    const long long first = (long long)split * s.rows, rows = max(0LL, min(s.rows, s.pixels - first));
+    const T *base = x + ((long long)n * s.pixels + first) * s.c + (long long)slab * s.slab_c;
+    const int seen = ty < s.ty && ty < rows ? (int)((rows - ty + s.ty - 1) / s.ty) : 0;
+    Moments m;
+    Spread<T, V> sp;
+    sp.none();
+    if (seen > 0)
+        for (int col = tx; col < s.cols; col += s.tx) {
+            const T *p = base + (long long)ty * s.c + (long long)col * V;
+            const long long pitch = (long long)s.ty * s.c;
             NormVec<T, V> v;
-            v.load(p + r * s.c);
-            v.get(ck);
-#pragma unroll
-            for (int i = 0; i < V; ++i) cs[i] = cq[i] = 0.f;
-            seen = 1;
-            r += s.ty;
-            constexpr int U = 4;
-            for (; r + (long long)(U - 1) * s.ty < last; r += (long long)U * s.ty) {
+            v.load(p);
+            sp.first(v);
+            constexpr int U = 8;
+            int r = 1;
+            p += pitch;
+            for (; r + U <= seen; r += U, p += U * pitch) {
                 NormVec<T, V> u[U];
 #pragma unroll
-                for (int k = 0; k < U; ++k) u[k].load(p + (r + (long long)k * s.ty) * s.c);
+                for (int k = 0; k < U; ++k) u[k].load(p + k * pitch);
 #pragma unroll
-                for (int k = 0; k < U; ++k) {
-                    float f[V];
-                    u[k].get(f);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) { const float d = f[i] - ck[i]; cs[i] += d; cq[i] = fmaf(d, d, cq[i]); }
-                }
-                seen += U;
+                for (int k = 0; k < U; ++k) sp.add(u[k]);
             }
-            for (; r < last; r += s.ty) {
-                v.load(p + r * s.c);
-                float f[V];
-                v.get(f);
-#pragma unroll
-                for (int i = 0; i < V; ++i) { const float d = f[i] - ck[i]; cs[i] += d; cq[i] = fmaf(d, d, cq[i]); }
-                ++seen;
-            }
-            if (s.one_group) {
-                // the column's values, joined with what the thread has (Chan, Golub, LeVeque: pairwise updates of a variance)
-                const float k = (float)seen, inv = 1.f / k;
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < V; ++i) sum += fmaf(cs[i], inv, ck[i]);
-                const float m = sum * (1.f / V);
-                float q = 0.f;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = fmaf(cs[i], inv, ck[i]) - m;
-                    q += fmaf(-cs[i] * inv, cs[i], cq[i]) + k * d * d;
-                }
-                const float add = k * V, all = cnt + add, d = m - mean;
-                mean += d * (add / all);
-                m2 += q + d * d * (cnt * (add / all));
-                cnt = all;
-            }
+            for (; r < seen; ++r, p += pitch) { v.load(p); sp.add(v); }
+            if (s.one_group) m.join(sp, seen);
+        }
+    block_moments(s, red, mu, s.one_group, m, sp, seen, (float)max(rows, 1LL), [&](int g, float2 v) { own[g] = v; });
+    if (s.cluster > 1) ptx::cluster_sync_all(); else __syncthreads();
+    const int rank = s.cluster > 1 ? (int)ptx::cluster_rank() : 0, run = split / s.cluster;
+    if (rank == 0) {
+        const long long from = (long long)run * s.cluster * s.rows;
+        const float all = (float)max(1LL, min(s.rows * s.cluster, s.pixels - from));
+        float2 *to = part + (((long long)n * (s.splits / s.cluster) + run) * s.g + (long long)slab * s.slab_g);
+        for (int g = threadIdx.x; g < s.slab_g; g += kThreads) {
+            float2 v = own[g];
+            if (s.cluster > 1)
+                v = join_runs(s.cluster, all, (float)s.cg, [&](int b) { return (float)max(0LL, min(s.rows, s.pixels - from - b * s.rows)); },
+                              [&](int b) { return ld_cluster_f2(ptx::cluster_addr(&own[g], b)); });
+            to[g] = v;
         }
     }
-    const long long rows = last - first;
-    const float total = (float)rows * (float)s.cg;      // (an integer below 2^24 or rounded: the weights of a mean)
-    float2 *out = part + (((long long)n * s.splits + split) * s.g + (long long)slab * s.slab_g);
-    if (s.one_group) {
-        // threads' columns of a group are neighbours: [ty][tx], V channels each
-        const int per = s.slab_g == 1 ? s.tx : s.cg / V;
-        if (live) red[ty * s.tx + tx] = cnt * mean;
-        __syncthreads();
-        group_sums(red, s.ty, s.tx, per, s.slab_g, [&](int g, float v) { mu[g] = v / total; });
-        __syncthreads();
-        const int g = s.slab_g == 1 ? 0 : tx / per;
-        if (live) { const float d = mean - mu[g]; red[ty * s.tx + tx] = m2 + cnt * d * d; }
-        __syncthreads();
-        group_sums(red, s.ty, s.tx, per, s.slab_g, [&](int g, float v) { out[g] = make_float2(mu[g], v); });
-    } else {
-        const float k = (float)seen, inv = seen ? 1.f / k : 0.f;
-        const int width = s.tx * V;
-        if (live)
-#pragma unroll
-            for (int i = 0; i < V; ++i) red[ty * width + tx * V + i] = fmaf(k, ck[i], cs[i]);
-        __syncthreads();
-        group_sums(red, s.ty, width, s.cg, s.slab_g, [&](int g, float v) { mu[g] = v / total; });
-        __syncthreads();
-        if (live)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = fmaf(cs[i], inv, ck[i]) - mu[(tx * V + i) / s.cg];
-                red[ty * width + tx * V + i] = fmaf(-cs[i] * inv, cs[i], cq[i]) + k * d * d;
-            }
-        __syncthreads();
-        group_sums(red, s.ty, width, s.cg, s.slab_g, [&](int g, float v) { out[g] = make_float2(mu[g], v); });
-    }
+    if (s.cluster > 1) ptx::cluster_sync_all();                     // no block ends while another may read from it
 }
 
-// z = act(gamma (x - mean) r + beta).  Each block joins its groups' runs first; the first run's block writes saved.
+// z = act(gamma (x - mean) r + beta).  Each block joins its groups' runs first; the first run's block writes saved.  Runs are taken from the last
+// one on: what the pass before has read last is the likeliest in L2.
 template <class T, int V, int ACT>
-__global__ void __launch_bounds__(kThreads) group_norm_apply_kernel(const GroupNormShape s, const T *__restrict__ x, const float *__restrict__ gamma,
-                                                                    const float *__restrict__ beta, const float2 *__restrict__ part,
-                                                                    float *__restrict__ saved, T *__restrict__ z) {
+__global__ void __launch_bounds__(kThreads, 3) group_norm_apply_kernel(const GroupNormShape s, const T *__restrict__ x, const float *__restrict__ gamma,
+                                                                       const float *__restrict__ beta, const float2 *__restrict__ part,
+                                                                       float *__restrict__ saved, T *__restrict__ z) {
     __shared__ float2 stat[kNormMaxSlabGroups];
     pdl_wait();
     pdl_launch_dependents();
-    const int slab = blockIdx.y, split = blockIdx.x;
-    const int n = s.n0 + blockIdx.z;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int slab = gridDim.y - 1 - blockIdx.y, split = s.splits - 1 - blockIdx.x;
+    const int n = s.n0 + gridDim.z - 1 - blockIdx.z;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, runs = s.splits / s.cluster;
+    const long long run_rows = s.rows * s.cluster;
     for (int g = warp; g < s.slab_g; g += kThreads / 32) {
-        const float2 *p = part + (long long)n * s.splits * s.g + (long long)slab * s.slab_g + g;
+        const float2 *p = part + (long long)n * runs * s.g + (long long)slab * s.slab_g + g;
         const float all = (float)s.pixels;
-        float m = 0.f;
-        for (int i = lane; i < s.splits; i += 32) {
-            const float rows = (float)min(s.rows, s.pixels - (long long)i * s.rows);
-            m = fmaf(rows / all, p[(long long)i * s.g].x, m);
-        }
+        float m = 0.f, q = 0.f;
+        auto weight = [&](int i) { return (float)max(0LL, min(run_rows, s.pixels - i * run_rows)); };
+        for (int i = lane; i < runs; i += 32) m = fmaf(weight(i) / all, p[(long long)i * s.g].x, m);
         m = warp_sum(m);
-        float q = 0.f;
-        for (int i = lane; i < s.splits; i += 32) {
-            const float rows = (float)min(s.rows, s.pixels - (long long)i * s.rows);
+        for (int i = lane; i < runs; i += 32) {
             const float2 v = p[(long long)i * s.g];
             const float d = v.x - m;
-            q += fmaf(rows * s.cg * d, d, v.y);
+            q += fmaf(weight(i) * s.cg * d, d, v.y);
         }
         q = warp_sum(q);
         if (lane == 0) {
             const float r = 1.f / sqrtf(q / (all * s.cg) + s.eps);
             stat[g] = make_float2(m, r);
             if (split == 0) {
-                const long long at = (long long)n * s.g + (long long)slab * s.slab_g + g;
-                saved[at] = m;
-                saved[(long long)s.n * s.g + at] = r;
+                const long long to = (long long)n * s.g + (long long)slab * s.slab_g + g;
+                saved[to] = m;
+                saved[(long long)s.n * s.g + to] = r;
             }
         }
     }
     __syncthreads();
     const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
-    if (ty >= s.ty) return;
-    const long long first = (long long)split * s.rows, last = min(first + s.rows, s.pixels);
-    const long long base = ((long long)n * s.pixels) * s.c + (long long)slab * s.slab_c;
+    const long long first = (long long)split * s.rows, rows = min(s.rows, s.pixels - first);
+    if (ty >= s.ty || ty >= rows) return;
+    const int mine = (int)((rows - ty + s.ty - 1) / s.ty);
+    const long long base = ((long long)n * s.pixels + first + ty) * s.c + (long long)slab * s.slab_c, pitch = (long long)s.ty * s.c;
     for (int col = tx; col < s.cols; col += s.tx) {
-        float sub[V], mul[V], add[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = col * V + i;
-            const float2 st = stat[c / s.cg];
-            sub[i] = st.x;
-            mul[i] = __ldg(gamma + slab * s.slab_c + c) * st.y;
-            add[i] = __ldg(beta + slab * s.slab_c + c);
-        }
-        const T *src = x + base + (long long)col * V;
-        T *dst = z + base + (long long)col * V;
-        auto one = [&](NormVec<T, V> v, long long r) {
-            float f[V];
-            v.get(f);
-#pragma unroll
-            for (int i = 0; i < V; ++i) f[i] = norm_act<ACT>(fmaf(f[i] - sub[i], mul[i], add[i]));
-            v.put(f);
-            v.store(dst + r * s.c);
-        };
-        constexpr int U = 4;
-        long long r = first + ty;
-        for (; r + (long long)(U - 1) * s.ty < last; r += (long long)U * s.ty) {
+        NormChannels<V, false> k;
+        set_channels(k, col * V, s.cg, gamma + slab * s.slab_c, beta + slab * s.slab_c, [&](int g) { return stat[g]; });
+        // from the last pixel on, too
+        const T *src = x + base + (long long)col * V + (mine - 1) * pitch;
+        T *dst = z + base + (long long)col * V + (mine - 1) * pitch;
+        constexpr int U = 8;
+        int r = 0;
+        for (; r + U <= mine; r += U, src -= U * pitch, dst -= U * pitch) {
             NormVec<T, V> v[U];
 #pragma unroll
-            for (int k = 0; k < U; ++k) v[k].load_last(src + (r + (long long)k * s.ty) * s.c);
+            for (int i = 0; i < U; ++i) v[i].load_last(src - i * pitch);
 #pragma unroll
-            for (int k = 0; k < U; ++k) one(v[k], r + (long long)k * s.ty);
+            for (int i = 0; i < U; ++i) norm_forward<T, V, ACT, false>(v[i], k).store_last(dst - i * pitch);
         }
-        for (; r < last; r += s.ty) {
+        for (; r < mine; ++r, src -= pitch, dst -= pitch) {
             NormVec<T, V> v;
-            v.load_last(src + r * s.c);
-            one(v, r);
+            v.load_last(src);
+            norm_forward<T, V, ACT, false>(v, k).store_last(dst);
         }
     }
 }
@@ -220,82 +321,70 @@ __global__ void __launch_bounds__(kThreads) group_norm_apply_kernel(const GroupN
 // Sums of the backward pass over a run of pixels: per channel dy and dy xhat, chan[(n splits + split) c + channel]; per group those two
 // times gamma, part[(n splits + split) g + group].
 template <class T, int V, int ACT>
-__global__ void __launch_bounds__(kThreads) group_norm_bwd_sums_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
-                                                                       const float *__restrict__ gamma, const float *__restrict__ beta,
-                                                                       const float *__restrict__ saved, float2 *__restrict__ chan,
-                                                                       float2 *__restrict__ part) {
+__global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_sums_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
+                                                                          const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                                          const float *__restrict__ saved, float2 *__restrict__ chan,
+                                                                          float2 *__restrict__ part) {
+    constexpr int P = (V + 1) / 2;
     __shared__ float red_a[kThreads * V], red_b[kThreads * V];
     pdl_wait();
     pdl_launch_dependents();
     const int slab = blockIdx.y, split = blockIdx.x;
     const int n = s.n0 + blockIdx.z;
-    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
-    const bool live = ty < s.ty;
-    const long long first = (long long)split * s.rows, last = min(first + s.rows, s.pixels);
-    const long long base = ((long long)n * s.pixels) * s.c + (long long)slab * s.slab_c;
+    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx, line = table_row(s), lines = table_rows(s);
+    const long long first = (long long)split * s.rows, rows = min(s.rows, s.pixels - first);
+    const int mine = ty < s.ty && ty < rows ? (int)((rows - ty + s.ty - 1) / s.ty) : 0;
+    const long long base = ((long long)n * s.pixels + first + ty) * s.c + (long long)slab * s.slab_c, pitch = (long long)s.ty * s.c;
     const float *mean_p = saved + (long long)n * s.g + (long long)slab * s.slab_g, *rstd_p = mean_p + (long long)s.n * s.g;
+    const float *gamma_p = gamma + slab * s.slab_c, *beta_p = beta + slab * s.slab_c;
     const long long run = (long long)n * s.splits + split;
     const int width = s.tx * V;
-    float ga = 0.f, gb = 0.f;                      // the only group's sums, where there is one (thread 0)
+    float ga = 0.f, gb = 0.f;                      // the only group's sums, where there is one (warp 0)
     for (int col0 = 0; col0 < s.cols; col0 += s.tx) {
         const int col = col0 + tx, cols = min(s.tx, s.cols - col0);
-        float a[V], b[V];
+        f32x2 a[P], b[P];
 #pragma unroll
-        for (int i = 0; i < V; ++i) a[i] = b[i] = 0.f;
-        if (live && tx < cols) {
-            float mean[V], rstd[V], gm[V], bt[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = col * V + i;
-                mean[i] = __ldg(mean_p + c / s.cg);
-                rstd[i] = __ldg(rstd_p + c / s.cg);
-                gm[i] = __ldg(gamma + slab * s.slab_c + c);
-                bt[i] = __ldg(beta + slab * s.slab_c + c);
-            }
+        for (int i = 0; i < P; ++i) a[i] = b[i] = 0ull;
+        if (mine > 0 && tx < cols) {
+            NormChannels<V, false> k;
+            set_channels(k, col * V, s.cg, gamma_p, beta_p, [&](int g) { return make_float2(__ldg(mean_p + g), __ldg(rstd_p + g)); });
+            const NormExact exact{mean_p, rstd_p, gamma_p, beta_p, col * V, s.cg, near_zero(k)};
             const T *px = x + base + (long long)col * V, *pz = dz + base + (long long)col * V;
             auto one = [&](const NormVec<T, V> &vx, const NormVec<T, V> &vz) {
-                float fx[V], fz[V];
-                vx.get(fx);
-                vz.get(fz);
+                f32x2 xc[P], dy[P];
+                norm_grad<T, V, ACT, false>(vx, vz, k, exact, xc, dy);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float xc = fx[i] - mean[i];
-                    const float dy = norm_act_grad<ACT>(fz[i], xc, fx[i], mean[i], rstd[i], gm[i], gm[i] * rstd[i], bt[i]);
-                    a[i] += dy;
-                    b[i] = fmaf(dy, xc, b[i]);
-                }
+                for (int i = 0; i < P; ++i) { a[i] = add2(a[i], dy[i]); b[i] = fma2(dy[i], xc[i], b[i]); }
             };
-            constexpr int U = 2;
-            long long r = first + ty;
-            for (; r + (long long)(U - 1) * s.ty < last; r += (long long)U * s.ty) {
+            constexpr int U = 4;
+            int r = 0;
+            for (; r + U <= mine; r += U, px += U * pitch, pz += U * pitch) {
                 NormVec<T, V> vx[U], vz[U];
 #pragma unroll
-                for (int k = 0; k < U; ++k) {
-                    vx[k].load(px + (r + (long long)k * s.ty) * s.c);
-                    vz[k].load(pz + (r + (long long)k * s.ty) * s.c);
-                }
+                for (int i = 0; i < U; ++i) { vx[i].load(px + i * pitch); vz[i].load(pz + i * pitch); }
 #pragma unroll
-                for (int k = 0; k < U; ++k) one(vx[k], vz[k]);
+                for (int i = 0; i < U; ++i) one(vx[i], vz[i]);
             }
-            for (; r < last; r += s.ty) {
+            for (; r < mine; ++r, px += pitch, pz += pitch) {
                 NormVec<T, V> vx, vz;
-                vx.load(px + r * s.c);
-                vz.load(pz + r * s.c);
+                vx.load(px);
+                vz.load(pz);
                 one(vx, vz);
             }
-#pragma unroll
-            for (int i = 0; i < V; ++i) b[i] *= rstd[i];
         }
-        if (live)
 #pragma unroll
-            for (int i = 0; i < V; ++i) { red_a[ty * width + tx * V + i] = a[i]; red_b[ty * width + tx * V + i] = b[i]; }
+        for (int i = 0; i < V; ++i) {
+            const float fa = fold(s, at<V>(a, i)), fb = fold(s, at<V>(b, i));
+            if (line >= 0) { red_a[line * width + tx * V + i] = fa; red_b[line * width + tx * V + i] = fb; }
+        }
         __syncthreads();
         for (int c = threadIdx.x; c < cols * V; c += kThreads) {
             float sa = 0.f, sb = 0.f;
-            for (int k = 0; k < s.ty; ++k) { sa += red_a[k * width + c]; sb += red_b[k * width + c]; }
-            const int channel = slab * s.slab_c + col0 * V + c;
-            chan[run * s.c + channel] = make_float2(sa, sb);
-            const float g = __ldg(gamma + channel);
+            for (int k = 0; k < lines; ++k) { sa += red_a[k * width + c]; sb += red_b[k * width + c]; }
+            const int channel = col0 * V + c;
+            sb *= __ldg(rstd_p + channel / s.cg);
+            chan[run * s.c + slab * s.slab_c + channel] = make_float2(sa, sb);
+            const float g = __ldg(gamma_p + channel);
             red_a[c] = g * sa;                       // (row 0 of this column has been read by this thread)
             red_b[c] = g * sb;
         }
@@ -339,18 +428,19 @@ __global__ void __launch_bounds__(1024) group_norm_finish_kernel(long long runs,
     }
 }
 
-// dx = r (gamma dy - E[gamma dy] - xhat E[gamma dy xhat]).
+// dx = r (gamma dy - E[gamma dy] - xhat E[gamma dy xhat]) = scale dy + k1 + k2 (x - mean)
 template <class T, int V, int ACT>
-__global__ void __launch_bounds__(kThreads) group_norm_bwd_apply_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
-                                                                        const float *__restrict__ gamma, const float *__restrict__ beta,
-                                                                        const float *__restrict__ saved, const float2 *__restrict__ part,
-                                                                        T *__restrict__ dx) {
+__global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_apply_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
+                                                                           const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                                           const float *__restrict__ saved, const float2 *__restrict__ part,
+                                                                           T *__restrict__ dx) {
+    constexpr int P = (V + 1) / 2;
     __shared__ float2 stat[kNormMaxSlabGroups];
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int slab = blockIdx.y, split = blockIdx.x;
-    const int n = s.n0 + blockIdx.z;
+    const int slab = gridDim.y - 1 - blockIdx.y, split = s.splits - 1 - blockIdx.x;
+    const int n = s.n0 + gridDim.z - 1 - blockIdx.z;
     const float *mean_p = saved + (long long)n * s.g + (long long)slab * s.slab_g, *rstd_p = mean_p + (long long)s.n * s.g;
     for (int g = warp; g < s.slab_g; g += kThreads / 32) {
         const float2 *p = part + (long long)n * s.splits * s.g + (long long)slab * s.slab_g + g;
@@ -359,327 +449,246 @@ __global__ void __launch_bounds__(kThreads) group_norm_bwd_apply_kernel(const Gr
         sa = warp_sum(sa);
         sb = warp_sum(sb);
         const float inv = 1.f / ((float)s.pixels * (float)s.cg), r = __ldg(rstd_p + g);
-        if (lane == 0) stat[g] = make_float2(sa * inv * r, sb * inv * r * r);
+        if (lane == 0) stat[g] = make_float2(-sa * inv * r, -sb * inv * r * r);
     }
     __syncthreads();
     const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
-    if (ty >= s.ty) return;
-    const long long first = (long long)split * s.rows, last = min(first + s.rows, s.pixels);
-    const long long base = ((long long)n * s.pixels) * s.c + (long long)slab * s.slab_c;
+    const long long first = (long long)split * s.rows, rows = min(s.rows, s.pixels - first);
+    if (ty >= s.ty || ty >= rows) return;
+    const int mine = (int)((rows - ty + s.ty - 1) / s.ty);
+    const long long base = ((long long)n * s.pixels + first + ty) * s.c + (long long)slab * s.slab_c, pitch = (long long)s.ty * s.c;
+    const float *gamma_p = gamma + slab * s.slab_c, *beta_p = beta + slab * s.slab_c;
     for (int col = tx; col < s.cols; col += s.tx) {
-        float mean[V], rstd[V], gm[V], bt[V], k1[V], k2[V];
+        NormChannels<V, false> k;
+        set_channels(k, col * V, s.cg, gamma_p, beta_p, [&](int g) { return make_float2(__ldg(mean_p + g), __ldg(rstd_p + g)); });
+        const NormExact exact{mean_p, rstd_p, gamma_p, beta_p, col * V, s.cg, near_zero(k)};
+        f32x2 k1[P], k2[P];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = col * V + i, g = c / s.cg;
-            mean[i] = __ldg(mean_p + g);
-            rstd[i] = __ldg(rstd_p + g);
-            gm[i] = __ldg(gamma + slab * s.slab_c + c);
-            bt[i] = __ldg(beta + slab * s.slab_c + c);
-            k1[i] = stat[g].x;
-            k2[i] = stat[g].y;
+        for (int i = 0; i < P; ++i) {
+            const float2 u = stat[(col * V + 2 * i) / s.cg], w = V > 1 ? stat[(col * V + 2 * i + 1) / s.cg] : make_float2(0.f, 0.f);
+            k1[i] = pair(u.x, w.x);
+            k2[i] = pair(u.y, w.y);
         }
-        const long long at = base + (long long)col * V;
-        auto one = [&](const NormVec<T, V> &vx, const NormVec<T, V> &vz, long long r) {
-            float fx[V], fz[V];
-            vx.get(fx);
-            vz.get(fz);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float xc = fx[i] - mean[i], scale = gm[i] * rstd[i];
-                const float dy = norm_act_grad<ACT>(fz[i], xc, fx[i], mean[i], rstd[i], gm[i], scale, bt[i]);
-                fx[i] = fmaf(dy, scale, fmaf(-xc, k2[i], -k1[i]));
-            }
+        const long long last = base + (long long)col * V + (mine - 1) * pitch;
+        const T *px = x + last, *pz = dz + last;
+        T *to = dx + last;
+        auto one = [&](const NormVec<T, V> &vx, const NormVec<T, V> &vz, T *p) {
+            f32x2 xc[P], dy[P];
+            norm_grad<T, V, ACT, false>(vx, vz, k, exact, xc, dy);
             NormVec<T, V> v;
-            v.put(fx);
-            v.store(dx + at + r * s.c);
+#pragma unroll
+            for (int i = 0; i < P; ++i) v.put(i, fma2(dy[i], k.scale[i], fma2(xc[i], k2[i], k1[i])));
+            v.store_last(p);
         };
-        constexpr int U = 2;
-        long long r = first + ty;
-        for (; r + (long long)(U - 1) * s.ty < last; r += (long long)U * s.ty) {
+        constexpr int U = 4;
+        int r = 0;
+        for (; r + U <= mine; r += U, px -= U * pitch, pz -= U * pitch, to -= U * pitch) {
             NormVec<T, V> vx[U], vz[U];
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                vx[k].load_last(x + at + (r + (long long)k * s.ty) * s.c);
-                vz[k].load_last(dz + at + (r + (long long)k * s.ty) * s.c);
-            }
+            for (int i = 0; i < U; ++i) { vx[i].load_last(px - i * pitch); vz[i].load_last(pz - i * pitch); }
 #pragma unroll
-            for (int k = 0; k < U; ++k) one(vx[k], vz[k], r + (long long)k * s.ty);
+            for (int i = 0; i < U; ++i) one(vx[i], vz[i], to - i * pitch);
         }
-        for (; r < last; r += s.ty) {
+        for (; r < mine; ++r, px -= pitch, pz -= pitch, to -= pitch) {
             NormVec<T, V> vx, vz;
-            vx.load_last(x + at + r * s.c);
-            vz.load_last(dz + at + r * s.c);
-            one(vx, vz, r);
+            vx.load_last(px);
+            vz.load_last(pz);
+            one(vx, vz, to);
         }
     }
 }
 
-// ---- one pass: a sample's slab is kept on chip by a cluster of blocks -----------------------------------------------------------------
-// A block has a run of the sample's pixels, a thread `keep` of them, 16 bytes each, in places of shared memory that are its own: the copies
-// need no registers while they are under way and no barrier.  Sums go over the cluster through shared memory.
-constexpr int kFusedMax = 8;                   // blocks of a cluster
-constexpr int kFusedBytes = 72 * 1024;         // of a block: three blocks an SM
-
-__device__ __forceinline__ void copy16(void *dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(dst)), "l"(src) : "memory");
+// ---- on chip --------------------------------------------------------------------------------------------------------------------------
+// A block has the slab of a sample, or a run of its pixels and its cluster the slab; a thread keeps `keep` of them, 16 bytes each, in places
+// of shared memory that are its own: the copies need no registers while they are under way and no barrier.  Blocks are as small as hold
+// their pixels: many run on an SM, and one's copies are under way beside another's sums.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+template <class T, int V>
+__device__ __forceinline__ NormVec<T, V> kept_vec(uint32_t addr) {
+    uint4 q;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(addr) : "memory");
+    NormVec<T, V> v;
+    v.w = q;
     return v;
 }
 
 // ONE: all channels of a thread belong to one group.
 template <class T, int ACT, bool ONE>
-__global__ void __launch_bounds__(kThreads, 3) group_norm_fused_fwd_kernel(const GroupNormShape s, const T *__restrict__ x, const float *__restrict__ gamma,
-                                                                           const float *__restrict__ beta, float *__restrict__ saved, T *__restrict__ z) {
-    constexpr int V = 16 / (int)sizeof(T), W = ONE ? 1 : V;
+__global__ void __launch_bounds__(kMaxKeptThreads) group_norm_kept_fwd_kernel(const GroupNormShape s, const T *__restrict__ x,
+                                                                              const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                                              float *__restrict__ saved, T *__restrict__ z) {
+    constexpr int V = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    using Vec = NormVec<T, V>;
-    Vec *kept = (Vec *)smem_raw + threadIdx.x;
-    __shared__ float red[kThreads * W];
     __shared__ float mu[kNormMaxSlabGroups];
-    __shared__ float2 part[kNormMaxSlabGroups], stat[kNormMaxSlabGroups];
+    __shared__ float2 own[kNormMaxSlabGroups], stat[kNormMaxSlabGroups];
+    const uint32_t step = blockDim.x * 16, kept = ptx::smem_u32(smem_raw) + threadIdx.x * 16;
+    float *red = (float *)(smem_raw + (size_t)s.keep * step);
+    const int split = blockIdx.x, slab = blockIdx.y;
+    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
+    const int first = split * (int)s.rows, rows = max(0, min((int)s.rows, (int)s.pixels - first));
+    const int mine = ty < s.ty && ty < rows ? (rows - ty + s.ty - 1) / s.ty : 0;
+    const long long pitch = (long long)s.ty * s.c, inside = (long long)(first + ty) * s.c + (long long)slab * s.slab_c + tx * V;
+    const float *gamma_p = gamma + slab * s.slab_c, *beta_p = beta + slab * s.slab_c;
     pdl_wait();
     pdl_launch_dependents();
-    const int rank = blockIdx.x % s.splits, slab = blockIdx.x / s.splits, n = s.n0 + blockIdx.y;
-    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
-    const int first = rank * (int)s.rows, rows = max(0, min((int)s.rows, (int)s.pixels - first));
-    const long long base = ((long long)n * s.pixels + first) * s.c + (long long)slab * s.slab_c + tx * V;
-    const int mine = ty < s.ty && ty < rows ? (rows - ty + s.ty - 1) / s.ty : 0;
-    const long long pitch = (long long)s.ty * s.c;
-    {
-        const T *p = x + base + (long long)ty * s.c;
-        for (int k = 0; k < mine; ++k, p += pitch) copy16(kept + k * kThreads, p);
-    }
-    const int group = ONE ? (s.slab_g == 1 ? 0 : tx * V / s.cg) : 0, per = ONE ? (s.slab_g == 1 ? s.tx : s.cg / V) : s.cg;
-    const int width = s.tx * W;
-    const float inv = rows > 0 ? 1.f / ((float)rows * (float)s.cg) : 0.f;
-    copies_wait();
-    // the block's means, then the distances from them
-    float sum[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) sum[i] = 0.f;
+    for (int n = blockIdx.z; n < s.n; n += gridDim.z) {                  // (more samples than a grid has)
+        const T *from = x + n * s.pixels * s.c + inside;
+        for (int k = 0; k < mine; ++k) copy16(kept + k * step, from + k * pitch);
+        copies_wait();
+        Spread<T, V> sp;
+        sp.none();
+        if (mine > 0) sp.first(kept_vec<T, V>(kept));
 #pragma unroll 4
-    for (int k = 0; k < mine; ++k) {
-        float f[V];
-        kept[k * kThreads].get(f);
-#pragma unroll
-        for (int i = 0; i < V; ++i) sum[ONE ? 0 : i] += f[i];
-    }
-    if (ty < s.ty)
-#pragma unroll
-        for (int i = 0; i < W; ++i) red[ty * width + tx * W + i] = sum[i];
-    __syncthreads();
-    group_sums(red, s.ty, width, per, s.slab_g, [&](int g, float v) { mu[g] = v * inv; });
-    __syncthreads();
-    float m[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) { m[i] = mu[ONE ? group : (tx * V + i) / s.cg]; sum[i] = 0.f; }
-#pragma unroll 4
-    for (int k = 0; k < mine; ++k) {
-        float f[V];
-        kept[k * kThreads].get(f);
-#pragma unroll
-        for (int i = 0; i < V; ++i) { const float d = f[i] - m[ONE ? 0 : i]; sum[ONE ? 0 : i] = fmaf(d, d, sum[ONE ? 0 : i]); }
-    }
-    if (ty < s.ty)
-#pragma unroll
-        for (int i = 0; i < W; ++i) red[ty * width + tx * W + i] = sum[i];
-    __syncthreads();
-    group_sums(red, s.ty, width, per, s.slab_g, [&](int g, float v) { part[g] = make_float2(mu[g], v); });
-    if (s.splits > 1) ptx::cluster_sync_all(); else __syncthreads();
-    for (int g = threadIdx.x; g < s.slab_g; g += kThreads) {
-        // the blocks' runs joined (pairwise update of mean and squared distances)
-        float2 all = part[g];
-        if (s.splits > 1) {
-            float cnt = 0.f;
-            all = make_float2(0.f, 0.f);
-            for (int b = 0; b < s.splits; ++b) {
-                const float2 v = ld_cluster_f2(ptx::cluster_addr(&part[g], b));
-                const float add = (float)max(0, min((int)s.rows, (int)s.pixels - b * (int)s.rows)), share = add / (cnt + add), d = v.x - all.x;
-                all.x = fmaf(d, share, all.x);
-                all.y += fmaf(d * d, cnt * share * (float)s.cg, v.y);
-                cnt += add;
+        for (int k = 1; k < mine; ++k) sp.add(kept_vec<T, V>(kept + k * step));
+        Moments m;
+        if (ONE && mine > 0) m.join(sp, mine);
+        block_moments(s, red, mu, ONE, m, sp, mine, (float)max(rows, 1), [&](int g, float2 v) { own[g] = v; });
+        if (s.cluster > 1) ptx::cluster_sync_all(); else __syncthreads();
+        for (int g = threadIdx.x; g < s.slab_g; g += blockDim.x) {
+            float2 v = own[g];
+            if (s.cluster > 1)
+                v = join_runs(s.cluster, (float)s.pixels, (float)s.cg, [&](int b) { return (float)max(0, min((int)s.rows, (int)s.pixels - b * (int)s.rows)); },
+                              [&](int b) { return ld_cluster_f2(ptx::cluster_addr(&own[g], b)); });
+            const float r = 1.f / sqrtf(v.y / ((float)s.pixels * (float)s.cg) + s.eps);
+            stat[g] = make_float2(v.x, r);
+            if (split == 0) {
+                const long long to = (long long)n * s.g + (long long)slab * s.slab_g + g;
+                saved[to] = v.x;
+                saved[(long long)s.n * s.g + to] = r;
             }
         }
-        const float r = 1.f / sqrtf(all.y / ((float)s.pixels * (float)s.cg) + s.eps);
-        stat[g] = make_float2(all.x, r);
-        if (rank == 0) {
-            const long long at = (long long)n * s.g + (long long)slab * s.slab_g + g;
-            saved[at] = all.x;
-            saved[(long long)s.n * s.g + at] = r;
-        }
-    }
-    if (s.splits > 1) ptx::cluster_arrive_started();             // (done with the others' shared memory)
-    __syncthreads();
-    if (mine > 0) {
-        float sub[W], mul[V], add[V];
-        const int c0 = slab * s.slab_c + tx * V;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float2 st = stat[ONE ? group : (tx * V + i) / s.cg];
-            sub[ONE ? 0 : i] = st.x;
-            mul[i] = __ldg(gamma + c0 + i) * st.y;
-            add[i] = __ldg(beta + c0 + i);
-        }
-        T *p = z + base + (long long)ty * s.c;
+        __syncthreads();
+        if (mine > 0) {
+            NormChannels<V, ONE> ch;
+            set_channels(ch, tx * V, s.cg, gamma_p, beta_p, [&](int g) { return stat[g]; });
+            T *to = z + n * s.pixels * s.c + inside;
 #pragma unroll 2
-        for (int k = 0; k < mine; ++k, p += pitch) {
-            Vec v = kept[k * kThreads];
-            float f[V];
-            v.get(f);
-#pragma unroll
-            for (int i = 0; i < V; ++i) f[i] = norm_act<ACT>(fmaf(f[i] - sub[ONE ? 0 : i], mul[i], add[i]));
-            v.put(f);
-            v.store(p);
+            for (int k = 0; k < mine; ++k) norm_forward<T, V, ACT, ONE>(kept_vec<T, V>(kept + k * step), ch).store(to + k * pitch);
         }
+        if (s.cluster > 1) ptx::cluster_sync_all();               // no block ends, or sums the next sample, while another may read from it
     }
-    if (s.splits > 1) ptx::cluster_wait_started();               // no block ends while another may read from it
 }
 
 template <class T, int ACT, bool ONE>
-__global__ void __launch_bounds__(kThreads, 2) group_norm_fused_bwd_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
-                                                                           const float *__restrict__ gamma, const float *__restrict__ beta,
-                                                                           const float *__restrict__ saved, float2 *__restrict__ chan,
-                                                                           T *__restrict__ dx) {
-    constexpr int V = 16 / (int)sizeof(T), W = ONE ? 1 : V;
+__global__ void __launch_bounds__(kMaxKeptThreads) group_norm_kept_bwd_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
+                                                                              const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                                              const float *__restrict__ saved, float2 *__restrict__ chan,
+                                                                              T *__restrict__ dx) {
+    constexpr int V = 16 / (int)sizeof(T), P = V / 2;
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    using Vec = NormVec<T, V>;
-    Vec *kept = (Vec *)smem_raw + threadIdx.x;                   // x and dz of a pixel in turn
-    __shared__ float red_a[kThreads * V], red_b[kThreads * V];
-    __shared__ float2 part[kNormMaxSlabGroups], stat[kNormMaxSlabGroups];
+    __shared__ float2 own[kNormMaxSlabGroups], stat[kNormMaxSlabGroups];
+    const uint32_t step = blockDim.x * 16, kept = ptx::smem_u32(smem_raw) + threadIdx.x * 16;      // x and dz of a pixel in turn
+    const int split = blockIdx.x, slab = blockIdx.y, width = s.tx * V;
+    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx, line = table_row(s), lines = table_rows(s);
+    float *red_a = (float *)(smem_raw + (size_t)s.keep * 2 * step), *red_b = red_a + lines * width;
+    const int first = split * (int)s.rows, rows = max(0, min((int)s.rows, (int)s.pixels - first));
+    const int mine = ty < s.ty && ty < rows ? (rows - ty + s.ty - 1) / s.ty : 0;
+    const long long pitch = (long long)s.ty * s.c, inside = (long long)(first + ty) * s.c + (long long)slab * s.slab_c + tx * V;
+    const float *gamma_p = gamma + slab * s.slab_c, *beta_p = beta + slab * s.slab_c;
     pdl_wait();
     pdl_launch_dependents();
-    const int rank = blockIdx.x % s.splits, slab = blockIdx.x / s.splits, n = s.n0 + blockIdx.y;
-    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
-    const int first = rank * (int)s.rows, rows = max(0, min((int)s.rows, (int)s.pixels - first));
-    const long long base = ((long long)n * s.pixels + first) * s.c + (long long)slab * s.slab_c + tx * V;
-    const int mine = ty < s.ty && ty < rows ? (rows - ty + s.ty - 1) / s.ty : 0;
-    const long long pitch = (long long)s.ty * s.c;
-    {
-        long long at = base + (long long)ty * s.c;
-        for (int k = 0; k < mine; ++k, at += pitch) {
-            copy16(kept + 2 * k * kThreads, x + at);
-            copy16(kept + (2 * k + 1) * kThreads, dz + at);
+    for (int n = blockIdx.z; n < s.n; n += gridDim.z) {
+        const long long sample = n * s.pixels * s.c + inside;
+        for (int k = 0; k < mine; ++k) {
+            copy16(kept + 2 * k * step, x + sample + k * pitch);
+            copy16(kept + (2 * k + 1) * step, dz + sample + k * pitch);
         }
-    }
-    float mean[W], rstd[W], gm[V], bt[V], a[V], b[V];
-    const int c0 = slab * s.slab_c + tx * V;
-    const float *mean_p = saved + (long long)n * s.g + (long long)slab * s.slab_g, *rstd_p = mean_p + (long long)s.n * s.g;
-    if (ty < s.ty) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int g = (tx * V + i) / s.cg;
-            if (!ONE || i == 0) { mean[ONE ? 0 : i] = __ldg(mean_p + g); rstd[ONE ? 0 : i] = __ldg(rstd_p + g); }
-            gm[i] = __ldg(gamma + c0 + i);
-            bt[i] = __ldg(beta + c0 + i);
+        const float *mean_p = saved + (long long)n * s.g + (long long)slab * s.slab_g, *rstd_p = mean_p + (long long)s.n * s.g;
+        NormChannels<V, ONE> ch;
+        f32x2 a[P], b[P];
+        NormExact exact{mean_p, rstd_p, gamma_p, beta_p, tx * V, s.cg, 0.f};
+        if (mine > 0) {
+            set_channels(ch, tx * V, s.cg, gamma_p, beta_p, [&](int g) { return make_float2(__ldg(mean_p + g), __ldg(rstd_p + g)); });
+            exact.near = near_zero(ch);
         }
-    }
 #pragma unroll
-    for (int i = 0; i < V; ++i) a[i] = b[i] = 0.f;
-    copies_wait();
+        for (int i = 0; i < P; ++i) a[i] = b[i] = 0ull;
+        copies_wait();
 #pragma unroll 2
-    for (int k = 0; k < mine; ++k) {
-        float fx[V], fz[V];
-        kept[2 * k * kThreads].get(fx);
-        kept[(2 * k + 1) * kThreads].get(fz);
+        for (int k = 0; k < mine; ++k) {
+            f32x2 xc[P], dy[P];
+            norm_grad<T, V, ACT, ONE>(kept_vec<T, V>(kept + 2 * k * step), kept_vec<T, V>(kept + (2 * k + 1) * step), ch, exact, xc, dy);
+#pragma unroll
+            for (int i = 0; i < P; ++i) { a[i] = add2(a[i], dy[i]); b[i] = fma2(dy[i], xc[i], b[i]); }
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float mn = mean[ONE ? 0 : i], rs = rstd[ONE ? 0 : i], xc = fx[i] - mn;
-            const float dy = norm_act_grad<ACT>(fz[i], xc, fx[i], mn, rs, gm[i], gm[i] * rs, bt[i]);
-            a[i] += dy;
-            b[i] = fmaf(dy, xc, b[i]);
+            const float fa = fold(s, at<V>(a, i)), fb = fold(s, at<V>(b, i));
+            if (line >= 0) { red_a[line * width + tx * V + i] = fa; red_b[line * width + tx * V + i] = fb; }
         }
-    }
-    const int width = s.tx * V;
-    if (ty < s.ty)
+        __syncthreads();
+        for (int c = threadIdx.x; c < width; c += blockDim.x) {
+            float sa = 0.f, sb = 0.f;
+            for (int k = 0; k < lines; ++k) { sa += red_a[k * width + c]; sb += red_b[k * width + c]; }
+            sb *= __ldg(rstd_p + c / s.cg);
+            chan[((long long)n * s.splits + split) * s.c + slab * s.slab_c + c] = make_float2(sa, sb);
+            const float g = __ldg(gamma_p + c);
+            red_a[c] = g * sa;                       // (row 0 of this column has been read by this thread)
+            red_b[c] = g * sb;
+        }
+        __syncthreads();
+        group_sums(red_a, 1, width, s.cg, s.slab_g, [&](int g, float v) { own[g].x = v; });
+        group_sums(red_b, 1, width, s.cg, s.slab_g, [&](int g, float v) { own[g].y = v; });
+        if (s.cluster > 1) ptx::cluster_sync_all(); else __syncthreads();
+        for (int g = threadIdx.x; g < s.slab_g; g += blockDim.x) {
+            float2 all = own[g];
+            if (s.cluster > 1) {
+                all = make_float2(0.f, 0.f);
+                for (int k = 0; k < s.cluster; ++k) {
+                    const float2 v = ld_cluster_f2(ptx::cluster_addr(&own[g], k));
+                    all.x += v.x;
+                    all.y += v.y;
+                }
+            }
+            const float inv = 1.f / ((float)s.pixels * (float)s.cg), r = __ldg(rstd_p + g);
+            stat[g] = make_float2(-all.x * inv * r, -all.y * inv * r * r);
+        }
+        __syncthreads();
+        if (mine > 0) {
+            f32x2 k1[ONE ? 1 : P], k2[ONE ? 1 : P];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            red_a[ty * width + tx * V + i] = a[i];
-            red_b[ty * width + tx * V + i] = mine > 0 ? b[i] * rstd[ONE ? 0 : i] : 0.f;
-        }
-    __syncthreads();
-    for (int c = threadIdx.x; c < width; c += kThreads) {
-        float sa = 0.f, sb = 0.f;
-        for (int k = 0; k < s.ty; ++k) { sa += red_a[k * width + c]; sb += red_b[k * width + c]; }
-        chan[((long long)n * s.splits + rank) * s.c + slab * s.slab_c + c] = make_float2(sa, sb);
-        const float g = __ldg(gamma + slab * s.slab_c + c);
-        red_a[c] = g * sa;                       // (row 0 of this column has been read by this thread)
-        red_b[c] = g * sb;
-    }
-    __syncthreads();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int g = warp; g < s.slab_g; g += kThreads / 32) {
-        float sa = 0.f, sb = 0.f;
-        for (int i = lane; i < s.cg; i += 32) { sa += red_a[g * s.cg + i]; sb += red_b[g * s.cg + i]; }
-        sa = warp_sum(sa);
-        sb = warp_sum(sb);
-        if (lane == 0) part[g] = make_float2(sa, sb);
-    }
-    if (s.splits > 1) ptx::cluster_sync_all(); else __syncthreads();
-    for (int g = threadIdx.x; g < s.slab_g; g += kThreads) {
-        float2 all = part[g];
-        if (s.splits > 1) {
-            all = make_float2(0.f, 0.f);
-            for (int k = 0; k < s.splits; ++k) {
-                const float2 v = ld_cluster_f2(ptx::cluster_addr(&part[g], k));
-                all.x += v.x;
-                all.y += v.y;
+            for (int i = 0; i < (ONE ? 1 : P); ++i) {
+                const float2 f = stat[(tx * V + 2 * i) / s.cg], w = ONE ? f : stat[(tx * V + 2 * i + 1) / s.cg];
+                k1[i] = pair(f.x, w.x);
+                k2[i] = pair(f.y, w.y);
+            }
+#pragma unroll 2
+            for (int k = 0; k < mine; ++k) {
+                f32x2 xc[P], dy[P];
+                norm_grad<T, V, ACT, ONE>(kept_vec<T, V>(kept + 2 * k * step), kept_vec<T, V>(kept + (2 * k + 1) * step), ch, exact, xc, dy);
+                NormVec<T, V> v;
+#pragma unroll
+                for (int i = 0; i < P; ++i) v.put(i, fma2(dy[i], ch.scale[i], fma2(xc[i], k2[ONE ? 0 : i], k1[ONE ? 0 : i])));
+                v.store(dx + sample + k * pitch);
             }
         }
-        const float inv = 1.f / ((float)s.pixels * (float)s.cg), r = __ldg(rstd_p + g);
-        stat[g] = make_float2(all.x * inv * r, all.y * inv * r * r);
+        if (s.cluster > 1) ptx::cluster_sync_all();
     }
-    if (s.splits > 1) ptx::cluster_arrive_started();
-    __syncthreads();
-    if (mine > 0) {
-        float k1[W], k2[W];
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const float2 st = stat[(tx * V + i) / s.cg];
-            k1[i] = st.x;
-            k2[i] = st.y;
-        }
-        T *p = dx + base + (long long)ty * s.c;
-#pragma unroll 2
-        for (int k = 0; k < mine; ++k, p += pitch) {
-            float fx[V], fz[V];
-            kept[2 * k * kThreads].get(fx);
-            kept[(2 * k + 1) * kThreads].get(fz);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int o = ONE ? 0 : i;
-                const float xc = fx[i] - mean[o], scale = gm[i] * rstd[o];
-                const float dy = norm_act_grad<ACT>(fz[i], xc, fx[i], mean[o], rstd[o], gm[i], scale, bt[i]);
-                fx[i] = fmaf(dy, scale, fmaf(-xc, k2[o], -k1[o]));
-            }
-            Vec v;
-            v.put(fx);
-            v.store(p);
-        }
-    }
-    if (s.splits > 1) ptx::cluster_wait_started();
 }
 
+// Dynamic shared memory of a block: its pixels and its table of sums.
+int kept_smem(const GroupNormShape &s, bool backward) {
+    const int lines = s.fold ? s.threads / 32 : s.ty, wide = backward ? 2 * s.vec : s.one_group ? 1 : s.vec;
+    return s.keep * s.threads * (backward ? 32 : 16) + lines * s.tx * wide * 4;
+}
 template <class K, class... Args>
-cudaError_t launch_fused(K kernel, PerDevice *attr, const GroupNormShape &s, int per_pixel, cudaStream_t st, Args... args) {
-    const int smem = s.keep * kThreads * per_pixel;
-    if (cudaError_t e = max_dynamic_smem_once(kernel, kFusedBytes, attr); e != cudaSuccess) return e;
+cudaError_t launch_clusters(K kernel, const GroupNormShape &s, dim3 grid, int smem, cudaStream_t st, Args... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(s.splits * (s.g / s.slab_g)), (unsigned)s.batch);
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)s.threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = s.splits;
+    at[1].val.clusterDim.x = s.cluster;
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = s.splits > 1 ? 2 : 1;
+    cfg.numAttrs = s.cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, s, args...);
 }
 
@@ -705,6 +714,48 @@ cudaError_t dispatch(const GroupNormShape &s, F &&f) {
     return s.dtype == CONVBN_F32 ? by_width(float()) : s.dtype == CONVBN_F16 ? by_width(__half()) : by_width(__nv_bfloat16());
 }
 
+// The narrowest slab of whole groups that starts on an access of s.vec elements and has 128 bytes a pixel, or as many as a block can take.
+int slab_groups(const GroupNormShape &s, int es, int threads) {
+    int groups = 0;
+    for (int k = 1; k <= s.g && k <= kNormMaxSlabGroups; ++k) {
+        if (s.g % k || k * s.cg % s.vec || (k > 1 && k * s.cg / s.vec > threads)) continue;
+        groups = k;
+        if ((long long)k * s.cg * es >= 128) break;
+    }
+    return groups;
+}
+void set_slab(GroupNormShape &s, int groups, int threads) {
+    s.slab_g = groups;
+    s.slab_c = groups * s.cg;
+    s.cols = s.slab_c / s.vec;
+    s.threads = threads;
+    s.tx = s.cols < threads ? s.cols : threads;
+    s.ty = threads / s.tx;
+    s.one_group = groups == 1 || s.cg % s.vec == 0;
+    s.fold = s.tx <= 32 && 32 % s.tx == 0;
+}
+
+// On chip: the fewest threads that hold the slab.
+bool kept_plan(GroupNormShape &s, int es, bool backward) {
+    if (s.vec * es != 16) return false;
+    const int sms = device_sm_count(), most = kKept / (backward ? 32 : 16);
+    for (int threads = 32; threads <= kMaxKeptThreads; threads *= 2) {
+        const int groups = slab_groups(s, es, threads);
+        if (!groups) continue;
+        set_slab(s, groups, threads);
+        if (s.cols > threads || s.pixels > (long long)s.ty * most) continue;
+        const long long units = (long long)(s.g / s.slab_g) * s.n;
+        long long splits = 1;                            // (few slabs: a cluster each)
+        if (units * 2 <= sms) splits = std::max(1LL, std::min(std::min(sms / units, 8LL), s.pixels / s.ty));
+        s.splits = s.cluster = (int)splits;
+        s.rows = (s.pixels + splits - 1) / splits;
+        s.keep = (int)((s.rows + s.ty - 1) / s.ty);
+        s.batch = std::min(s.n, 65535);
+        return true;
+    }
+    return false;
+}
+
 }  // namespace
 
 GroupNormShape group_norm_shape(const convbn_group_norm_desc *d, bool backward) {
@@ -712,62 +763,41 @@ GroupNormShape group_norm_shape(const convbn_group_norm_desc *d, bool backward) 
     s.n = d->n; s.c = d->c; s.g = d->groups; s.cg = d->c / d->groups; s.act = d->act; s.dtype = d->dtype;
     s.pixels = (long long)d->h * d->w;
     s.eps = (float)d->eps;
-    const int es = d->dtype == CONVBN_F32 ? 4 : 2;
-    // The widest access that rows allow, and the narrowest slab of whole groups that starts on such an access and has 128 bytes a pixel, or
-    // as many as a block can take.
-    for (s.vec = 16 / es;; s.vec /= 2) {
-        if (s.c % s.vec) continue;
-        s.slab_g = 0;
-        for (int k = 1; k <= s.g && k <= kNormMaxSlabGroups; ++k) {
-            if (s.g % k || k * s.cg % s.vec || (k > 1 && k * s.cg / s.vec > kThreads)) continue;
-            s.slab_g = k;
-            if ((long long)k * s.cg * es >= 128) break;
-        }
-        if (s.slab_g) break;                       // (one element: k = 1 always is)
-    }
-    s.slab_c = s.slab_g * s.cg;
-    s.cols = s.slab_c / s.vec;
-    s.tx = s.cols < kThreads ? s.cols : kThreads;
-    s.ty = kThreads / s.tx;
-    s.one_group = s.slab_g == 1 || s.cg % s.vec == 0;
     s.n0 = 0;
-    s.batch = s.n;
-    // Kept on chip: as few blocks as hold the sample's slab, more of them where that leaves SMs idle.
-    const long long slabs = s.g / s.slab_g;
-    const int sms = device_sm_count(), per_pixel = backward ? 32 : 16, most_kept = kFusedBytes / (kThreads * per_pixel);
+    const int es = d->dtype == CONVBN_F32 ? 4 : 2;
+    for (s.vec = 16 / es; s.c % s.vec || !slab_groups(s, es, kThreads); s.vec /= 2) {}       // (one element: one group always is)
+    if (kept_plan(s, es, backward)) return s;
     s.keep = 0;
-    if (s.vec * es == 16 && s.cols <= kThreads && s.pixels <= (long long)kFusedMax * most_kept * s.ty) {
-        int splits = (int)((s.pixels + (long long)most_kept * s.ty - 1) / ((long long)most_kept * s.ty));
-        while (splits < kFusedMax && slabs * s.n * splits < 4LL * sms && s.pixels > 2LL * s.ty * splits) ++splits;
-        s.rows = (s.pixels + splits - 1) / splits;
-        s.splits = (int)((s.pixels + s.rows - 1) / s.rows);
-        s.keep = (int)((s.rows + s.ty - 1) / s.ty);
-        return s;
-    }
-    // Runs of pixels: four blocks an SM over the whole batch, each thread at least eight pixels.
-    const long long want = (4LL * sms + slabs * s.n - 1) / (slabs * s.n);
-    const long long most = (s.pixels + 8 * s.ty - 1) / (8 * s.ty);
-    s.splits = (int)(want < most ? want : most);
-    if (s.splits > 1024) s.splits = 1024;
-    s.rows = (s.pixels + s.splits - 1) / s.splits;
-    s.splits = (int)((s.pixels + s.rows - 1) / s.rows);
+    set_slab(s, slab_groups(s, es, kThreads), kThreads);
+    s.batch = std::min(s.n, kNormMaxBatch);
+    // Runs of pixels: as many as blocks run at a time (three an SM forward, two backward), each thread at least sixteen pixels.
+    const long long units = (long long)(s.g / s.slab_g) * s.batch, most = (s.pixels + 16 * s.ty - 1) / (16 * s.ty);
+    const long long room = (backward ? 2LL : 3LL) * device_sm_count();
+    long long splits = std::min(std::max(1LL, room / units), std::min(most, 1024LL));
+    s.cluster = 1;
+    if (!backward && splits > 8) { s.cluster = 8; splits -= splits % 8; }
+    s.splits = (int)splits;
+    s.rows = (s.pixels + splits - 1) / splits;
+    if (s.cluster == 1) s.splits = (int)((s.pixels + s.rows - 1) / s.rows);
     return s;
 }
 
 // Two passes: [runs][groups] pairs.  Backward: [runs][channels] pairs behind them.
+static long long runs_of(const GroupNormShape &s) { return (long long)s.n * s.splits; }
+static size_t part_bytes(const GroupNormShape &s) { return s.keep ? 0 : align_up((size_t)runs_of(s) * s.g * sizeof(float2), 256); }
 size_t group_norm_workspace(const GroupNormShape &s, bool backward) {
-    const size_t runs = (size_t)s.n * s.splits;
-    return align_up(runs * s.g * sizeof(float2), 256) + (backward ? align_up(runs * s.c * sizeof(float2), 256) : 0);
+    const size_t bytes = part_bytes(s) + (backward ? align_up((size_t)runs_of(s) * s.c * sizeof(float2), 256) : 0);
+    return bytes ? bytes : 256;
 }
 
-// f(first sample, samples) for every launch's share of the batch
+// f(share of the batch) for every launch's
 template <class F>
 static cudaError_t by_batch(const GroupNormShape &shape, F &&f) {
     GroupNormShape s = shape;
     cudaError_t e = cudaSuccess;
-    for (int n0 = 0; n0 < shape.n && e == cudaSuccess; n0 += kNormMaxBatch) {
+    for (int n0 = 0; n0 < shape.n && e == cudaSuccess; n0 += shape.batch) {
         s.n0 = n0;
-        s.batch = shape.n - n0 < kNormMaxBatch ? shape.n - n0 : kNormMaxBatch;
+        s.batch = shape.n - n0 < shape.batch ? shape.n - n0 : shape.batch;
         e = f(s);
     }
     return e;
@@ -778,17 +808,19 @@ cudaError_t launch_group_norm_fwd(const GroupNormShape &shape, const void *x, co
     return dispatch(shape, [&](auto t, auto v, auto act) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, ACT = decltype(act)::value;
+        const unsigned slabs = (unsigned)(shape.g / shape.slab_g);
         if constexpr (V * sizeof(T) == 16) {
             static PerDevice attr[2];
-            if (shape.keep)
-                return by_batch(shape, [&](const GroupNormShape &s) {
-                    auto kernel = s.one_group ? group_norm_fused_fwd_kernel<T, ACT, true> : group_norm_fused_fwd_kernel<T, ACT, false>;
-                    return launch_fused(kernel, &attr[s.one_group], s, 16, st, (const T *)x, gamma, beta, saved, (T *)z);
-                });
+            if (shape.keep) {
+                auto kernel = shape.one_group ? group_norm_kept_fwd_kernel<T, ACT, true> : group_norm_kept_fwd_kernel<T, ACT, false>;
+                if (cudaError_t e = max_dynamic_smem_once(kernel, 200 * 1024, &attr[shape.one_group]); e != cudaSuccess) return e;
+                return launch_clusters(kernel, shape, dim3((unsigned)shape.splits, slabs, (unsigned)shape.batch), kept_smem(shape, false), st,
+                                       (const T *)x, gamma, beta, saved, (T *)z);
+            }
         }
         return by_batch(shape, [&](const GroupNormShape &s) {
-            const dim3 grid((unsigned)s.splits, (unsigned)(s.g / s.slab_g), (unsigned)s.batch);
-            const cudaError_t e = launch_pdl(group_norm_stats_kernel<T, V>, grid, dim3(kThreads), 0, st, s, (const T *)x, (float2 *)workspace);
+            const dim3 grid((unsigned)s.splits, slabs, (unsigned)s.batch);
+            const cudaError_t e = launch_clusters(group_norm_stats_kernel<T, V>, s, grid, 0, st, (const T *)x, (float2 *)workspace);
             if (e != cudaSuccess) return e;
             return launch_pdl(group_norm_apply_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)x, gamma, beta, (const float2 *)workspace,
                               saved, (T *)z);
@@ -798,21 +830,22 @@ cudaError_t launch_group_norm_fwd(const GroupNormShape &shape, const void *x, co
 
 cudaError_t launch_group_norm_bwd(const GroupNormShape &shape, const void *dz, const void *x, const float *gamma, const float *beta,
                                   const float *saved, void *dx, float *dgamma, float *dbeta, void *workspace, cudaStream_t st) {
-    float2 *part = (float2 *)workspace;
-    float2 *chan = (float2 *)((char *)workspace + align_up((size_t)shape.n * shape.splits * shape.g * sizeof(float2), 256));
+    float2 *part = (float2 *)workspace, *chan = (float2 *)((char *)workspace + part_bytes(shape));
     const cudaError_t e = dispatch(shape, [&](auto t, auto v, auto act) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, ACT = decltype(act)::value;
+        const unsigned slabs = (unsigned)(shape.g / shape.slab_g);
         if constexpr (V * sizeof(T) == 16) {
             static PerDevice attr[2];
-            if (shape.keep)
-                return by_batch(shape, [&](const GroupNormShape &s) {
-                    auto kernel = s.one_group ? group_norm_fused_bwd_kernel<T, ACT, true> : group_norm_fused_bwd_kernel<T, ACT, false>;
-                    return launch_fused(kernel, &attr[s.one_group], s, 32, st, (const T *)dz, (const T *)x, gamma, beta, saved, chan, (T *)dx);
-                });
+            if (shape.keep) {
+                auto kernel = shape.one_group ? group_norm_kept_bwd_kernel<T, ACT, true> : group_norm_kept_bwd_kernel<T, ACT, false>;
+                if (cudaError_t e = max_dynamic_smem_once(kernel, 200 * 1024, &attr[shape.one_group]); e != cudaSuccess) return e;
+                return launch_clusters(kernel, shape, dim3((unsigned)shape.splits, slabs, (unsigned)shape.batch), kept_smem(shape, true), st,
+                                       (const T *)dz, (const T *)x, gamma, beta, saved, chan, (T *)dx);
+            }
         }
         return by_batch(shape, [&](const GroupNormShape &s) {
-            const dim3 grid((unsigned)s.splits, (unsigned)(s.g / s.slab_g), (unsigned)s.batch);
+            const dim3 grid((unsigned)s.splits, slabs, (unsigned)s.batch);
             const cudaError_t e = launch_pdl(group_norm_bwd_sums_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)dz, (const T *)x, gamma, beta,
                                              saved, chan, part);
             if (e != cudaSuccess) return e;
@@ -821,8 +854,8 @@ cudaError_t launch_group_norm_bwd(const GroupNormShape &shape, const void *dz, c
         });
     });
     if (e != cudaSuccess) return e;
-    return launch_pdl(group_norm_finish_kernel, dim3((unsigned)((shape.c + 31) / 32)), dim3(1024), 0, st, (long long)shape.n * shape.splits, shape.c,
-                      (const float2 *)chan, dgamma, dbeta);
+    return launch_pdl(group_norm_finish_kernel, dim3((unsigned)((shape.c + 31) / 32)), dim3(1024), 0, st, runs_of(shape), shape.c, (const float2 *)chan,
+                      dgamma, dbeta);
 }
 
 }  // namespace convbn

@@ -386,12 +386,15 @@ struct GroupNormShape {
     int act, dtype;
     int vec;                       // elements per access
     int slab_g, slab_c, cols;      // groups, channels, accesses of a slab's pixel
+    int threads;                   // of a block
     int tx, ty;                    // threads side by side along a pixel; pixels side by side
     int one_group;                 // every thread's channels belong to one group
+    int fold;                      // rows of threads in a warp are added up there (tx divides 32)
     int splits;                    // runs of pixels a sample is cut into ...
-    long long rows, pixels;        // ... pixels of a run, of a sample
+    int cluster;                   // ... so many of them to a cluster
+    long long rows, pixels;        // pixels of a run, of a sample
     int n0, batch;                 // samples of a launch
-    int keep;                      // pixels that a thread keeps in shared memory: a run is a block of a cluster (0: two passes over memory)
+    int keep;                      // pixels that a thread keeps on chip (0: two passes over memory)
     float eps;
 };
 GroupNormShape group_norm_shape(const convbn_group_norm_desc *d, bool backward);     // (of a valid descriptor)
