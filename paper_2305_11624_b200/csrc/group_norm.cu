@@ -45,25 +45,33 @@ __device__ __forceinline__ int table_row(const GroupNormShape &s) {
     return ty < s.ty ? ty : -1;
 }
 __device__ __forceinline__ int table_rows(const GroupNormShape &s) { return s.fold ? (int)blockDim.x >> 5 : s.ty; }
-// Sums of `red`, [rows][width], over its rows and over groups of `size` neighbours: out(group, sum).
+// Sums of `red`, [rows][width], over its rows (they end up in the first) and over groups of `size` neighbours: out(group, sum).
 template <class F>
-__device__ __forceinline__ void group_sums(const float *red, int rows, int width, int size, int groups, F &&out) {
-    if (rows * size <= 8) {                                           // a thread per group
+__device__ __forceinline__ void group_sums(float *red, int rows, int width, int size, int groups, F &&out) {
+    if (rows > 1 && size > 1) {
+        for (int c = threadIdx.x; c < width; c += blockDim.x) {
+            float v = red[c];
+            for (int r = 1; r < rows; ++r) v += red[r * width + c];
+            red[c] = v;
+        }
+        rows = 1;
+        __syncthreads();
+    }
+    if (size <= 16) {                                           // a thread per group
         for (int g = threadIdx.x; g < groups; g += blockDim.x) {
-            float s = 0.f;
+            float v = 0.f;
             for (int r = 0; r < rows; ++r)
-                for (int i = 0; i < size; ++i) s += red[r * width + g * size + i];
-            out(g, s);
+                for (int i = 0; i < size; ++i) v += red[r * width + g * size + i];
+            out(g, v);
         }
         return;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int g = warp; g < groups; g += blockDim.x >> 5) {
-        float s = 0.f;
-        for (int r = 0; r < rows; ++r)
-            for (int i = lane; i < size; i += 32) s += red[r * width + g * size + i];
-        s = warp_sum(s);
-        if (lane == 0) out(g, s);
+        float v = 0.f;
+        for (int i = lane; i < size; i += 32) v += red[g * size + i];
+        v = warp_sum(v);
+        if (lane == 0) out(g, v);
     }
 }
 
@@ -197,13 +205,92 @@ __device__ __forceinline__ void block_moments(const GroupNormShape &s, float *re
     }
 }
 
+// ---- copies into a thread's own places of shared memory: they need no registers while they are under way, and no barrier ----------------------
+template <class T, int V>
+__device__ __forceinline__ void copy_in(uint32_t dst, const T *src) {
+    if constexpr (V * sizeof(T) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else if constexpr (V * sizeof(T) == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+    else if constexpr (V * sizeof(T) == 4) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst), "h"(*(const uint16_t *)src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <class T, int V>
+__device__ __forceinline__ NormVec<T, V> kept_vec(uint32_t addr) {
+    NormVec<T, V> v;
+    if constexpr (V * sizeof(T) == 16) {
+        uint4 q;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(addr) : "memory");
+        v.w = q;
+    } else if constexpr (V * sizeof(T) == 8) {
+        uint2 q;
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(q.x), "=r"(q.y) : "r"(addr) : "memory");
+        v.w = q;
+    } else if constexpr (V * sizeof(T) == 4) {
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v.w) : "r"(addr) : "memory");
+    } else {
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v.w) : "r"(addr) : "memory");
+    }
+    return v;
+}
+// A column's pixels through a ring of kRing places, NT tensors side by side: f(its vectors) for pixel after pixel.  What is under way
+// at a time, 48 KB a block, does not depend on how long a pixel takes; with a batch of loads in registers between one wait and the next the
+// passes read 2.6 to 3.5 TB/s.
+constexpr int kRing = 12;
+template <class T, int V, int NT>
+struct Ring {
+    static constexpr int kPlaces = kRing / NT, kBatch = 2, kBatches = kPlaces / kBatch;
+    uint32_t slot;
+    long long pitch;
+    int mine;
+    const T *from[NT];
+    __device__ __forceinline__ void batch(int place, int left) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if (i < left)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) copy_in<T, V>(slot + ((place * kBatch + i) * NT + t) * (kThreads * 16), from[t]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) from[t] += pitch;
+        }
+        copies_commit();
+    }
+    __device__ __forceinline__ void start() {
+#pragma unroll
+        for (int b = 0; b < kBatches; ++b) batch(b, mine - b * kBatch);
+    }
+    template <class F>
+    __device__ __forceinline__ void run(F &&f) {
+        for (int left = mine; left > 0; left -= kPlaces) {
+#pragma unroll
+            for (int b = 0; b < kBatches; ++b) {
+                copies_wait<kBatches - 1>();
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i)
+                    if (b * kBatch + i < left) {
+                        NormVec<T, V> v[NT];
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) v[t] = kept_vec<T, V>(slot + ((b * kBatch + i) * NT + t) * (kThreads * 16));
+                        f(v);
+                    }
+                batch(b, left - kPlaces - b * kBatch);
+            }
+        }
+        copies_wait<0>();
+    }
+};
+constexpr int kRingBytes = kRing * kThreads * 16;
+
 // ---- two passes -----------------------------------------------------------------------------------------------------------------------
 // Mean and sum of squared distances of a cluster's runs of pixels, per group: part[(n runs + run) groups + g], runs = splits / cluster.
 template <class T, int V>
 __global__ void __launch_bounds__(kThreads, 3) group_norm_stats_kernel(const GroupNormShape s, const T *__restrict__ x, float2 *__restrict__ part) {
+    extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ float red[kThreads * V];
     __shared__ float mu[kNormMaxSlabGroups];
     __shared__ float2 own[kNormMaxSlabGroups];
+    const uint32_t slot = ptx::smem_u32(smem_raw) + threadIdx.x * 16;
     pdl_wait();
     pdl_launch_dependents();
     const int slab = blockIdx.y, split = blockIdx.x;
@@ -217,22 +304,14 @@ __global__ void __launch_bounds__(kThreads, 3) group_norm_stats_kernel(const Gro
     sp.none();
     if (seen > 0)
         for (int col = tx; col < s.cols; col += s.tx) {
-            const T *p = base + (long long)ty * s.c + (long long)col * V;
-            const long long pitch = (long long)s.ty * s.c;
-            NormVec<T, V> v;
-            v.load(p);
-            sp.first(v);
-            constexpr int U = 8;
-            int r = 1;
-            p += pitch;
-            for (; r + U <= seen; r += U, p += U * pitch) {
-                NormVec<T, V> u[U];
-#pragma unroll
-                for (int k = 0; k < U; ++k) u[k].load(p + k * pitch);
-#pragma unroll
-                for (int k = 0; k < U; ++k) sp.add(u[k]);
-            }
-            for (; r < seen; ++r, p += pitch) { v.load(p); sp.add(v); }
+            Ring<T, V, 1> ring{slot, (long long)s.ty * s.c, seen, {base + (long long)ty * s.c + (long long)col * V}};
+            ring.start();
+            bool begun = false;
+            ring.run([&](const NormVec<T, V> (&v)[1]) {
+                if (!begun) sp.first(v[0]);
+                begun = true;
+                sp.add(v[0]);
+            });
             if (s.one_group) m.join(sp, seen);
         }
     block_moments(s, red, mu, s.one_group, m, sp, seen, (float)max(rows, 1LL), [&](int g, float2 v) { own[g] = v; });
@@ -259,12 +338,21 @@ template <class T, int V, int ACT>
 __global__ void __launch_bounds__(kThreads, 3) group_norm_apply_kernel(const GroupNormShape s, const T *__restrict__ x, const float *__restrict__ gamma,
                                                                        const float *__restrict__ beta, const float2 *__restrict__ part,
                                                                        float *__restrict__ saved, T *__restrict__ z) {
+    extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ float2 stat[kNormMaxSlabGroups];
     pdl_wait();
     pdl_launch_dependents();
     const int slab = gridDim.y - 1 - blockIdx.y, split = s.splits - 1 - blockIdx.x;
     const int n = s.n0 + gridDim.z - 1 - blockIdx.z;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, runs = s.splits / s.cluster;
+    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
+    const long long first = (long long)split * s.rows, rows = min(s.rows, s.pixels - first);
+    const int mine = ty < s.ty && ty < rows ? (int)((rows - ty + s.ty - 1) / s.ty) : 0;
+    // from the last pixel on, too; the first ones are on their way while the runs are joined
+    const long long last = ((long long)n * s.pixels + first + ty) * s.c + (long long)slab * s.slab_c + (mine - 1) * (long long)s.ty * s.c;
+    const long long pitch = (long long)s.ty * s.c;
+    Ring<T, V, 1> ring{ptx::smem_u32(smem_raw) + threadIdx.x * 16, -pitch, mine, {x + last + (long long)tx * V}};
+    ring.start();
     const long long run_rows = s.rows * s.cluster;
     for (int g = warp; g < s.slab_g; g += kThreads / 32) {
         const float2 *p = part + (long long)n * runs * s.g + (long long)slab * s.slab_g + g;
@@ -290,31 +378,19 @@ __global__ void __launch_bounds__(kThreads, 3) group_norm_apply_kernel(const Gro
         }
     }
     __syncthreads();
-    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
-    const long long first = (long long)split * s.rows, rows = min(s.rows, s.pixels - first);
-    if (ty >= s.ty || ty >= rows) return;
-    const int mine = (int)((rows - ty + s.ty - 1) / s.ty);
-    const long long base = ((long long)n * s.pixels + first + ty) * s.c + (long long)slab * s.slab_c, pitch = (long long)s.ty * s.c;
+    if (mine == 0) return;
     for (int col = tx; col < s.cols; col += s.tx) {
         NormChannels<V, false> k;
         set_channels(k, col * V, s.cg, gamma + slab * s.slab_c, beta + slab * s.slab_c, [&](int g) { return stat[g]; });
-        // from the last pixel on, too
-        const T *src = x + base + (long long)col * V + (mine - 1) * pitch;
-        T *dst = z + base + (long long)col * V + (mine - 1) * pitch;
-        constexpr int U = 8;
-        int r = 0;
-        for (; r + U <= mine; r += U, src -= U * pitch, dst -= U * pitch) {
-            NormVec<T, V> v[U];
-#pragma unroll
-            for (int i = 0; i < U; ++i) v[i].load_last(src - i * pitch);
-#pragma unroll
-            for (int i = 0; i < U; ++i) norm_forward<T, V, ACT, false>(v[i], k).store_last(dst - i * pitch);
+        T *dst = z + last + (long long)col * V;
+        if (col != tx) {
+            ring.from[0] = x + last + (long long)col * V;
+            ring.start();
         }
-        for (; r < mine; ++r, src -= pitch, dst -= pitch) {
-            NormVec<T, V> v;
-            v.load_last(src);
-            norm_forward<T, V, ACT, false>(v, k).store_last(dst);
-        }
+        ring.run([&](const NormVec<T, V> (&v)[1]) {
+            norm_forward<T, V, ACT, false>(v[0], k).store_last(dst);
+            dst -= pitch;
+        });
     }
 }
 
@@ -326,7 +402,9 @@ __global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_sums_kernel(const 
                                                                           const float *__restrict__ saved, float2 *__restrict__ chan,
                                                                           float2 *__restrict__ part) {
     constexpr int P = (V + 1) / 2;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ float red_a[kThreads * V], red_b[kThreads * V];
+    const uint32_t slot = ptx::smem_u32(smem_raw) + threadIdx.x * 16;
     pdl_wait();
     pdl_launch_dependents();
     const int slab = blockIdx.y, split = blockIdx.x;
@@ -349,28 +427,14 @@ __global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_sums_kernel(const 
             NormChannels<V, false> k;
             set_channels(k, col * V, s.cg, gamma_p, beta_p, [&](int g) { return make_float2(__ldg(mean_p + g), __ldg(rstd_p + g)); });
             const NormExact exact{mean_p, rstd_p, gamma_p, beta_p, col * V, s.cg, near_zero(k)};
-            const T *px = x + base + (long long)col * V, *pz = dz + base + (long long)col * V;
-            auto one = [&](const NormVec<T, V> &vx, const NormVec<T, V> &vz) {
+            Ring<T, V, 2> ring{slot, pitch, mine, {x + base + (long long)col * V, dz + base + (long long)col * V}};
+            ring.start();
+            ring.run([&](const NormVec<T, V> (&v)[2]) {
                 f32x2 xc[P], dy[P];
-                norm_grad<T, V, ACT, false>(vx, vz, k, exact, xc, dy);
+                norm_grad<T, V, ACT, false>(v[0], v[1], k, exact, xc, dy);
 #pragma unroll
                 for (int i = 0; i < P; ++i) { a[i] = add2(a[i], dy[i]); b[i] = fma2(dy[i], xc[i], b[i]); }
-            };
-            constexpr int U = 4;
-            int r = 0;
-            for (; r + U <= mine; r += U, px += U * pitch, pz += U * pitch) {
-                NormVec<T, V> vx[U], vz[U];
-#pragma unroll
-                for (int i = 0; i < U; ++i) { vx[i].load(px + i * pitch); vz[i].load(pz + i * pitch); }
-#pragma unroll
-                for (int i = 0; i < U; ++i) one(vx[i], vz[i]);
-            }
-            for (; r < mine; ++r, px += pitch, pz += pitch) {
-                NormVec<T, V> vx, vz;
-                vx.load(px);
-                vz.load(pz);
-                one(vx, vz);
-            }
+            });
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -435,12 +499,19 @@ __global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_apply_kernel(const
                                                                            const float *__restrict__ saved, const float2 *__restrict__ part,
                                                                            T *__restrict__ dx) {
     constexpr int P = (V + 1) / 2;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ float2 stat[kNormMaxSlabGroups];
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int slab = gridDim.y - 1 - blockIdx.y, split = s.splits - 1 - blockIdx.x;
     const int n = s.n0 + gridDim.z - 1 - blockIdx.z;
+    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
+    const long long first = (long long)split * s.rows, rows = min(s.rows, s.pixels - first), pitch = (long long)s.ty * s.c;
+    const int mine = ty < s.ty && ty < rows ? (int)((rows - ty + s.ty - 1) / s.ty) : 0;
+    const long long last = ((long long)n * s.pixels + first + ty) * s.c + (long long)slab * s.slab_c + (mine - 1) * pitch;
+    Ring<T, V, 2> ring{ptx::smem_u32(smem_raw) + threadIdx.x * 16, -pitch, mine, {x + last + (long long)tx * V, dz + last + (long long)tx * V}};
+    ring.start();
     const float *mean_p = saved + (long long)n * s.g + (long long)slab * s.slab_g, *rstd_p = mean_p + (long long)s.n * s.g;
     for (int g = warp; g < s.slab_g; g += kThreads / 32) {
         const float2 *p = part + (long long)n * s.splits * s.g + (long long)slab * s.slab_g + g;
@@ -452,11 +523,7 @@ __global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_apply_kernel(const
         if (lane == 0) stat[g] = make_float2(-sa * inv * r, -sb * inv * r * r);
     }
     __syncthreads();
-    const int tx = threadIdx.x % s.tx, ty = threadIdx.x / s.tx;
-    const long long first = (long long)split * s.rows, rows = min(s.rows, s.pixels - first);
-    if (ty >= s.ty || ty >= rows) return;
-    const int mine = (int)((rows - ty + s.ty - 1) / s.ty);
-    const long long base = ((long long)n * s.pixels + first + ty) * s.c + (long long)slab * s.slab_c, pitch = (long long)s.ty * s.c;
+    if (mine == 0) return;
     const float *gamma_p = gamma + slab * s.slab_c, *beta_p = beta + slab * s.slab_c;
     for (int col = tx; col < s.cols; col += s.tx) {
         NormChannels<V, false> k;
@@ -469,32 +536,22 @@ __global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_apply_kernel(const
             k1[i] = pair(u.x, w.x);
             k2[i] = pair(u.y, w.y);
         }
-        const long long last = base + (long long)col * V + (mine - 1) * pitch;
-        const T *px = x + last, *pz = dz + last;
-        T *to = dx + last;
-        auto one = [&](const NormVec<T, V> &vx, const NormVec<T, V> &vz, T *p) {
+        const long long from = last + (long long)col * V;
+        if (col != tx) {
+            ring.from[0] = x + from;
+            ring.from[1] = dz + from;
+            ring.start();
+        }
+        T *to = dx + from;
+        ring.run([&](const NormVec<T, V> (&in)[2]) {
             f32x2 xc[P], dy[P];
-            norm_grad<T, V, ACT, false>(vx, vz, k, exact, xc, dy);
+            norm_grad<T, V, ACT, false>(in[0], in[1], k, exact, xc, dy);
             NormVec<T, V> v;
 #pragma unroll
             for (int i = 0; i < P; ++i) v.put(i, fma2(dy[i], k.scale[i], fma2(xc[i], k2[i], k1[i])));
-            v.store_last(p);
-        };
-        constexpr int U = 4;
-        int r = 0;
-        for (; r + U <= mine; r += U, px -= U * pitch, pz -= U * pitch, to -= U * pitch) {
-            NormVec<T, V> vx[U], vz[U];
-#pragma unroll
-            for (int i = 0; i < U; ++i) { vx[i].load_last(px - i * pitch); vz[i].load_last(pz - i * pitch); }
-#pragma unroll
-            for (int i = 0; i < U; ++i) one(vx[i], vz[i], to - i * pitch);
-        }
-        for (; r < mine; ++r, px -= pitch, pz -= pitch, to -= pitch) {
-            NormVec<T, V> vx, vz;
-            vx.load_last(px);
-            vz.load_last(pz);
-            one(vx, vz, to);
-        }
+            v.store_last(to);
+            to -= pitch;
+        });
     }
 }
 
@@ -502,19 +559,6 @@ __global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_apply_kernel(const
 // A block has the slab of a sample, or a run of its pixels and its cluster the slab; a thread keeps `keep` of them, 16 bytes each, in places
 // of shared memory that are its own: the copies need no registers while they are under way and no barrier.  Blocks are as small as hold
 // their pixels: many run on an SM, and one's copies are under way beside another's sums.
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-template <class T, int V>
-__device__ __forceinline__ NormVec<T, V> kept_vec(uint32_t addr) {
-    uint4 q;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(addr) : "memory");
-    NormVec<T, V> v;
-    v.w = q;
-    return v;
-}
-
 // ONE: all channels of a thread belong to one group.
 template <class T, int ACT, bool ONE>
 __global__ void __launch_bounds__(kMaxKeptThreads) group_norm_kept_fwd_kernel(const GroupNormShape s, const T *__restrict__ x,
@@ -536,8 +580,9 @@ __global__ void __launch_bounds__(kMaxKeptThreads) group_norm_kept_fwd_kernel(co
     pdl_launch_dependents();
     for (int n = blockIdx.z; n < s.n; n += gridDim.z) {                  // (more samples than a grid has)
         const T *from = x + n * s.pixels * s.c + inside;
-        for (int k = 0; k < mine; ++k) copy16(kept + k * step, from + k * pitch);
-        copies_wait();
+        for (int k = 0; k < mine; ++k) copy_in<T, V>(kept + k * step, from + k * pitch);
+        copies_commit();
+        copies_wait<0>();
         Spread<T, V> sp;
         sp.none();
         if (mine > 0) sp.first(kept_vec<T, V>(kept));
@@ -593,9 +638,10 @@ __global__ void __launch_bounds__(kMaxKeptThreads) group_norm_kept_bwd_kernel(co
     for (int n = blockIdx.z; n < s.n; n += gridDim.z) {
         const long long sample = n * s.pixels * s.c + inside;
         for (int k = 0; k < mine; ++k) {
-            copy16(kept + 2 * k * step, x + sample + k * pitch);
-            copy16(kept + (2 * k + 1) * step, dz + sample + k * pitch);
+            copy_in<T, V>(kept + 2 * k * step, x + sample + k * pitch);
+            copy_in<T, V>(kept + (2 * k + 1) * step, dz + sample + k * pitch);
         }
+        copies_commit();
         const float *mean_p = saved + (long long)n * s.g + (long long)slab * s.slab_g, *rstd_p = mean_p + (long long)s.n * s.g;
         NormChannels<V, ONE> ch;
         f32x2 a[P], b[P];
@@ -606,7 +652,7 @@ __global__ void __launch_bounds__(kMaxKeptThreads) group_norm_kept_bwd_kernel(co
         }
 #pragma unroll
         for (int i = 0; i < P; ++i) a[i] = b[i] = 0ull;
-        copies_wait();
+        copies_wait<0>();
 #pragma unroll 2
         for (int k = 0; k < mine; ++k) {
             f32x2 xc[P], dy[P];
@@ -820,9 +866,13 @@ cudaError_t launch_group_norm_fwd(const GroupNormShape &shape, const void *x, co
         }
         return by_batch(shape, [&](const GroupNormShape &s) {
             const dim3 grid((unsigned)s.splits, slabs, (unsigned)s.batch);
-            const cudaError_t e = launch_clusters(group_norm_stats_kernel<T, V>, s, grid, 0, st, (const T *)x, (float2 *)workspace);
+            static PerDevice ring[2];
+            cudaError_t e = max_dynamic_smem_once(group_norm_stats_kernel<T, V>, kRingBytes, &ring[0]);
+            if (e == cudaSuccess) e = max_dynamic_smem_once(group_norm_apply_kernel<T, V, ACT>, kRingBytes, &ring[1]);
             if (e != cudaSuccess) return e;
-            return launch_pdl(group_norm_apply_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)x, gamma, beta, (const float2 *)workspace,
+            e = launch_clusters(group_norm_stats_kernel<T, V>, s, grid, kRingBytes, st, (const T *)x, (float2 *)workspace);
+            if (e != cudaSuccess) return e;
+            return launch_pdl(group_norm_apply_kernel<T, V, ACT>, grid, dim3(kThreads), kRingBytes, st, s, (const T *)x, gamma, beta, (const float2 *)workspace,
                               saved, (T *)z);
         });
     });
@@ -846,10 +896,14 @@ cudaError_t launch_group_norm_bwd(const GroupNormShape &shape, const void *dz, c
         }
         return by_batch(shape, [&](const GroupNormShape &s) {
             const dim3 grid((unsigned)s.splits, slabs, (unsigned)s.batch);
-            const cudaError_t e = launch_pdl(group_norm_bwd_sums_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)dz, (const T *)x, gamma, beta,
+            static PerDevice ring[2];
+            cudaError_t e = max_dynamic_smem_once(group_norm_bwd_sums_kernel<T, V, ACT>, kRingBytes, &ring[0]);
+            if (e == cudaSuccess) e = max_dynamic_smem_once(group_norm_bwd_apply_kernel<T, V, ACT>, kRingBytes, &ring[1]);
+            if (e != cudaSuccess) return e;
+            e = launch_pdl(group_norm_bwd_sums_kernel<T, V, ACT>, grid, dim3(kThreads), kRingBytes, st, s, (const T *)dz, (const T *)x, gamma, beta,
                                              saved, chan, part);
             if (e != cudaSuccess) return e;
-            return launch_pdl(group_norm_bwd_apply_kernel<T, V, ACT>, grid, dim3(kThreads), 0, st, s, (const T *)dz, (const T *)x, gamma, beta, saved,
+            return launch_pdl(group_norm_bwd_apply_kernel<T, V, ACT>, grid, dim3(kThreads), kRingBytes, st, s, (const T *)dz, (const T *)x, gamma, beta, saved,
                               (const float2 *)part, (T *)dx);
         });
     });

@@ -124,9 +124,16 @@ struct NormChannels {
     __device__ __forceinline__ f32x2 y(f32x2 xc, int i) const { return fma2(xc, scale[i], beta[i]); }
 };
 
+// 1 / (1 + exp(-y)); exp(-y) = infinity gives 0.
 __device__ __forceinline__ f32x2 sigmoid2(f32x2 y) {
-    const float2 s = split2(y);
-    return pair(__fdividef(1.f, 1.f + __expf(-s.x)), __fdividef(1.f, 1.f + __expf(-s.y)));
+    const float2 t = split2(mul2(y, both(-1.44269504f)));
+    float e0, e1, r0, r1;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t.y));
+    const float2 d = split2(add2(pair(e0, e1), both(1.f)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(d.y));
+    return pair(r0, r1);
 }
 
 template <class T, int V, int ACT, bool ONE>
