@@ -519,8 +519,6 @@ def _norm_tensors(desc, where, activations, vectors, saved):
     """EINVAL for tensors (not addresses, not None) that are not what the descriptor says: another type or size, in several pieces,
     channels not last, not on the current GPU."""
     import torch
-    if type(desc) is not NormDesc:
-        raise TypeError("a NormDesc is expected")
     current = None
     for tensors, kind, count in ((activations, desc.dtype, desc.n * desc.c * desc.h * desc.w), (vectors, F32, desc.c),
                                  ((saved,), F32, 2 * desc.n * desc.groups)):
@@ -541,17 +539,27 @@ def _norm_tensors(desc, where, activations, vectors, saved):
 
 def convbn_group_norm_fwd(desc, x, gamma, beta, z, saved, workspace=None, workspace_bytes: Optional[int] = None, stream=None):
     """z = act(group norm of x), channels last; saved: what the backward call needs beside x."""
-    _norm_tensors(desc, "convbn_group_norm_fwd", (x, z), (gamma, beta), saved)
-    status = (_native or _calls()).convbn_group_norm_fwd(desc, x, gamma, beta, z, saved, workspace, workspace_bytes, stream)
+    if type(desc) is not NormDesc:
+        raise TypeError("a NormDesc is expected")
+    native = _native or _calls()
+    status = native.group_norm_fwd(desc, x, gamma, beta, z, saved, workspace, workspace_bytes, stream)
+    if status is None:           # what is wrong, or else addresses or another order of the dimensions
+        _norm_tensors(desc, "convbn_group_norm_fwd", (x, z), (gamma, beta), saved)
+        status = native.convbn_group_norm_fwd(desc, x, gamma, beta, z, saved, workspace, workspace_bytes, stream)
     if status:
         _raise(status, "convbn_group_norm_fwd")
 
 
 def convbn_group_norm_bwd(desc, dz, x, gamma, beta, saved, dx, dgamma, dbeta, workspace=None, workspace_bytes: Optional[int] = None,
                           stream=None):
-    _norm_tensors(desc, "convbn_group_norm_bwd", (dz, x, dx), (gamma, beta, dgamma, dbeta), saved)
-    status = (_native or _calls()).convbn_group_norm_bwd(desc, dz, x, gamma, beta, saved, dx, dgamma, dbeta, workspace,
-                                                         workspace_bytes, stream)
+    if type(desc) is not NormDesc:
+        raise TypeError("a NormDesc is expected")
+    native = _native or _calls()
+    args = (desc, dz, x, gamma, beta, saved, dx, dgamma, dbeta, workspace, workspace_bytes, stream)
+    status = native.group_norm_bwd(*args)
+    if status is None:
+        _norm_tensors(desc, "convbn_group_norm_bwd", (dz, x, dx), (gamma, beta, dgamma, dbeta), saved)
+        status = native.convbn_group_norm_bwd(*args)
     if status:
         _raise(status, "convbn_group_norm_bwd")
 

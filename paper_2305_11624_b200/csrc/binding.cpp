@@ -18,7 +18,7 @@
 
 namespace {
 
-PyObject *s_data_ptr, *s_nbytes, *s_cuda_stream, *s_dtype, *s_numel, *s_itemsize, *s_is_contiguous, *s_get_device;      // attribute names
+PyObject *s_data_ptr, *s_nbytes, *s_cuda_stream, *s_dtype, *s_numel, *s_itemsize, *s_is_contiguous, *s_get_device, *s_dim, *s_shape;      // attribute names
 PyObject *g_get_device, *g_get_stream;                // torch._C._cuda_getDevice, _cuda_getCurrentRawStream
 
 bool address(PyObject *o, void **out) {
@@ -34,18 +34,21 @@ bool address(PyObject *o, void **out) {
     return *out || !PyErr_Occurred();
 }
 
+bool torch_calls() {
+    if (g_get_stream) return true;
+    PyObject *m = PyImport_ImportModule("torch._C");
+    if (!m) return false;
+    g_get_device = PyObject_GetAttrString(m, "_cuda_getDevice");
+    if (g_get_device) g_get_stream = PyObject_GetAttrString(m, "_cuda_getCurrentRawStream");
+    Py_DECREF(m);
+    return g_get_stream != nullptr;
+}
+
 bool stream(PyObject *o, void **out) {
     if (PyLong_Check(o)) { *out = PyLong_AsVoidPtr(o); return *out || !PyErr_Occurred(); }
     PyObject *v;
     if (o == Py_None) {
-        if (!g_get_stream) {
-            PyObject *m = PyImport_ImportModule("torch._C");
-            if (!m) return false;
-            g_get_device = PyObject_GetAttrString(m, "_cuda_getDevice");
-            if (g_get_device) g_get_stream = PyObject_GetAttrString(m, "_cuda_getCurrentRawStream");
-            Py_DECREF(m);
-            if (!g_get_stream) return false;
-        }
+        if (!torch_calls()) return false;
         PyObject *d = PyObject_CallNoArgs(g_get_device);
         if (!d) return false;
         v = PyObject_CallOneArg(g_get_stream, d);
@@ -201,6 +204,44 @@ PyObject *packed_bwd(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     return Entry<&convbn_tune_bwd_packed>::go(self, a, n);
 }
 
+// The current GPU; -1 where there is none.
+long long current_device() {
+    PyObject *v = torch_calls() ? PyObject_CallNoArgs(g_get_device) : nullptr;
+    long long r = -1;
+    if (v) r = PyLong_AsLongLong(v);
+    Py_XDECREF(v);
+    PyErr_Clear();
+    return r;
+}
+// convbn_group_norm_fwd and _bwd for tensors that are what the descriptor says: contiguous (channels last by shape), of its type and sizes, on
+// the current GPU; None for anything else, which convbn.py then looks at.  (The checks in Python took 5 us of a call of 9.)
+// kinds: of the arguments behind the descriptor: a activation, v a vector of c, s saved.
+bool norm_argument(PyObject *o, char kind, const convbn_group_norm_desc *d, long long device) {
+    const long long want = kind == 'a' ? (long long)d->n * d->c * d->h * d->w : kind == 'v' ? d->c : 2LL * d->n * d->groups;
+    if (storage_type(o) != (kind == 'a' ? d->dtype : CONVBN_F32) || number(o, s_numel, true) != want || !contiguous(o) ||
+        number(o, s_get_device, true) != device)
+        return false;
+    if (kind != 'a' || number(o, s_dim, true) != 4) return true;
+    PyObject *shape = PyObject_GetAttr(o, s_shape), *last = shape && PyTuple_Check(shape) ? PyTuple_GetItem(shape, 3) : nullptr,
+             *second = last ? PyTuple_GetItem(shape, 1) : nullptr;
+    const bool fits = second && PyLong_Check(last) && PyLong_AsLong(last) == d->c && PyLong_AsLong(second) == d->h;
+    Py_XDECREF(shape);
+    PyErr_Clear();
+    return fits;
+}
+template <auto F>
+PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n, const char *kinds) {
+    const convbn_group_norm_desc *d = nullptr;
+    if (n > 1 && !convert(a[0], &d)) return nullptr;
+    const long long device = d ? current_device() : -1;
+    if (device < 0) Py_RETURN_NONE;
+    for (Py_ssize_t i = 1; kinds[i - 1]; ++i)
+        if (i >= n || !norm_argument(a[i], kinds[i - 1], d, device)) Py_RETURN_NONE;
+    return Entry<F>::go(self, a, n);
+}
+PyObject *norm_fwd(PyObject *self, PyObject *const *a, Py_ssize_t n) { return norm<&convbn_group_norm_fwd>(self, a, n, "avvas"); }
+PyObject *norm_bwd(PyObject *self, PyObject *const *a, Py_ssize_t n) { return norm<&convbn_group_norm_bwd>(self, a, n, "aavvsavv"); }
+
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))Entry<&name>::go, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     ENTRY(convbn_tune_fwd), ENTRY(convbn_tune_bwd_data), ENTRY(convbn_tune_bwd_weight), ENTRY(convbn_tune_bwd),
@@ -211,7 +252,9 @@ PyMethodDef g_methods[] = {
     ENTRY(convbn_orthogonalise), ENTRY(convbn_muon_step),
     {"pack", (PyCFunction)(void (*)(void))packed<&convbn_pack, false>, METH_FASTCALL, nullptr},
     {"unpack", (PyCFunction)(void (*)(void))packed<&convbn_unpack, true>, METH_FASTCALL, nullptr},
-    {"tune_bwd_packed", (PyCFunction)(void (*)(void))packed_bwd, METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    {"tune_bwd_packed", (PyCFunction)(void (*)(void))packed_bwd, METH_FASTCALL, nullptr},
+    {"group_norm_fwd", (PyCFunction)(void (*)(void))norm_fwd, METH_FASTCALL, nullptr},
+    {"group_norm_bwd", (PyCFunction)(void (*)(void))norm_bwd, METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -225,6 +268,8 @@ PyMODINIT_FUNC PyInit__binding(void) {
     s_itemsize = PyUnicode_InternFromString("itemsize");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_get_device = PyUnicode_InternFromString("get_device");
-    return s_data_ptr && s_nbytes && s_cuda_stream && s_dtype && s_numel && s_itemsize && s_is_contiguous && s_get_device
+    s_dim = PyUnicode_InternFromString("dim");
+    s_shape = PyUnicode_InternFromString("shape");
+    return s_data_ptr && s_nbytes && s_cuda_stream && s_dtype && s_numel && s_itemsize && s_is_contiguous && s_get_device && s_dim && s_shape
                ? PyModule_Create(&g_module) : nullptr;
 }

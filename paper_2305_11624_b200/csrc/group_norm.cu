@@ -75,21 +75,31 @@ __device__ __forceinline__ void group_sums(float *red, int rows, int width, int 
     }
 }
 
-__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-    return v;
+// Element g of the table `own` of each block of a cluster of `blocks`; all loads are on their way before the first is waited for (one after the
+// other they took 4 us of a pass).
+constexpr int kMaxCluster = 8;
+__device__ __forceinline__ void cluster_pairs(const float2 *own, int blocks, float2 (&v)[kMaxCluster]) {
+    uint32_t at[kMaxCluster];
+#pragma unroll
+    for (int b = 0; b < kMaxCluster; ++b) at[b] = ptx::cluster_addr(own, b < blocks ? b : 0);
+#pragma unroll
+    for (int b = 0; b < kMaxCluster; ++b) asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[b].x), "=f"(v[b].y) : "r"(at[b]) : "memory");
 }
-// Means and squared distances of runs, joined: run b has weight(b) values a channel, pair(b) its numbers.
-template <class W, class P>
-__device__ __forceinline__ float2 join_runs(int runs, float total, float cg, W &&weight, P &&pair_of) {
+// Means and squared distances of the blocks' runs, joined: run b has weight(b) values a channel (none: zero).
+template <class W>
+__device__ __forceinline__ float2 join_runs(const float2 *own, int blocks, float total, float cg, W &&weight) {
+    float2 v[kMaxCluster];
+    cluster_pairs(own, blocks, v);
     float m = 0.f, q = 0.f;
-    for (int b = 0; b < runs; ++b) m = fmaf(weight(b) / total, pair_of(b).x, m);
-    for (int b = 0; b < runs; ++b) {
-        const float2 v = pair_of(b);
-        const float d = v.x - m;
-        q += fmaf(weight(b) * cg * d, d, v.y);
-    }
+#pragma unroll
+    for (int b = 0; b < kMaxCluster; ++b)
+        if (b < blocks) m = fmaf(weight(b) / total, v[b].x, m);
+#pragma unroll
+    for (int b = 0; b < kMaxCluster; ++b)
+        if (b < blocks) {
+            const float d = v[b].x - m;
+            q += fmaf(weight(b) * cg * d, d, v[b].y);
+        }
     return make_float2(m, q);
 }
 
@@ -237,10 +247,11 @@ __device__ __forceinline__ NormVec<T, V> kept_vec(uint32_t addr) {
 // A column's pixels through a ring of kRing places, NT tensors side by side: f(its vectors) for pixel after pixel.  What is under way
 // at a time, 48 KB a block, does not depend on how long a pixel takes; with a batch of loads in registers between one wait and the next the
 // passes read 2.6 to 3.5 TB/s.
-constexpr int kRing = 12;
+constexpr int kRing = 12, kBlocks1 = 3, kBlocks2 = 2;        // places; blocks of an SM, with one tensor and with two
 template <class T, int V, int NT>
 struct Ring {
     static constexpr int kPlaces = kRing / NT, kBatch = 2, kBatches = kPlaces / kBatch;
+    static_assert(kBatches * kBatch == kPlaces, "whole batches");
     uint32_t slot;
     long long pitch;
     int mine;
@@ -285,7 +296,7 @@ constexpr int kRingBytes = kRing * kThreads * 16;
 // ---- two passes -----------------------------------------------------------------------------------------------------------------------
 // Mean and sum of squared distances of a cluster's runs of pixels, per group: part[(n runs + run) groups + g], runs = splits / cluster.
 template <class T, int V>
-__global__ void __launch_bounds__(kThreads, 3) group_norm_stats_kernel(const GroupNormShape s, const T *__restrict__ x, float2 *__restrict__ part) {
+__global__ void __launch_bounds__(kThreads, kBlocks1) group_norm_stats_kernel(const GroupNormShape s, const T *__restrict__ x, float2 *__restrict__ part) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ float red[kThreads * V];
     __shared__ float mu[kNormMaxSlabGroups];
@@ -324,8 +335,7 @@ __global__ void __launch_bounds__(kThreads, 3) group_norm_stats_kernel(const Gro
         for (int g = threadIdx.x; g < s.slab_g; g += kThreads) {
             float2 v = own[g];
             if (s.cluster > 1)
-                v = join_runs(s.cluster, all, (float)s.cg, [&](int b) { return (float)max(0LL, min(s.rows, s.pixels - from - b * s.rows)); },
-                              [&](int b) { return ld_cluster_f2(ptx::cluster_addr(&own[g], b)); });
+                v = join_runs(&own[g], s.cluster, all, (float)s.cg, [&](int b) { return (float)max(0LL, min(s.rows, s.pixels - from - b * s.rows)); });
             to[g] = v;
         }
     }
@@ -335,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 3) group_norm_stats_kernel(const Gro
 // z = act(gamma (x - mean) r + beta).  Each block joins its groups' runs first; the first run's block writes saved.  Runs are taken from the last
 // one on: what the pass before has read last is the likeliest in L2.
 template <class T, int V, int ACT>
-__global__ void __launch_bounds__(kThreads, 3) group_norm_apply_kernel(const GroupNormShape s, const T *__restrict__ x, const float *__restrict__ gamma,
+__global__ void __launch_bounds__(kThreads, kBlocks1) group_norm_apply_kernel(const GroupNormShape s, const T *__restrict__ x, const float *__restrict__ gamma,
                                                                        const float *__restrict__ beta, const float2 *__restrict__ part,
                                                                        float *__restrict__ saved, T *__restrict__ z) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -397,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 3) group_norm_apply_kernel(const Gro
 // Sums of the backward pass over a run of pixels: per channel dy and dy xhat, chan[(n splits + split) c + channel]; per group those two
 // times gamma, part[(n splits + split) g + group].
 template <class T, int V, int ACT>
-__global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_sums_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
+__global__ void __launch_bounds__(kThreads, kBlocks2) group_norm_bwd_sums_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
                                                                           const float *__restrict__ gamma, const float *__restrict__ beta,
                                                                           const float *__restrict__ saved, float2 *__restrict__ chan,
                                                                           float2 *__restrict__ part) {
@@ -494,7 +504,7 @@ __global__ void __launch_bounds__(1024) group_norm_finish_kernel(long long runs,
 
 // dx = r (gamma dy - E[gamma dy] - xhat E[gamma dy xhat]) = scale dy + k1 + k2 (x - mean)
 template <class T, int V, int ACT>
-__global__ void __launch_bounds__(kThreads, 2) group_norm_bwd_apply_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
+__global__ void __launch_bounds__(kThreads, kBlocks2) group_norm_bwd_apply_kernel(const GroupNormShape s, const T *__restrict__ dz, const T *__restrict__ x,
                                                                            const float *__restrict__ gamma, const float *__restrict__ beta,
                                                                            const float *__restrict__ saved, const float2 *__restrict__ part,
                                                                            T *__restrict__ dx) {
@@ -595,8 +605,8 @@ __global__ void __launch_bounds__(kMaxKeptThreads) group_norm_kept_fwd_kernel(co
         for (int g = threadIdx.x; g < s.slab_g; g += blockDim.x) {
             float2 v = own[g];
             if (s.cluster > 1)
-                v = join_runs(s.cluster, (float)s.pixels, (float)s.cg, [&](int b) { return (float)max(0, min((int)s.rows, (int)s.pixels - b * (int)s.rows)); },
-                              [&](int b) { return ld_cluster_f2(ptx::cluster_addr(&own[g], b)); });
+                v = join_runs(&own[g], s.cluster, (float)s.pixels, (float)s.cg,
+                              [&](int b) { return (float)max(0, min((int)s.rows, (int)s.pixels - b * (int)s.rows)); });
             const float r = 1.f / sqrtf(v.y / ((float)s.pixels * (float)s.cg) + s.eps);
             stat[g] = make_float2(v.x, r);
             if (split == 0) {
@@ -682,12 +692,12 @@ __global__ void __launch_bounds__(kMaxKeptThreads) group_norm_kept_bwd_kernel(co
         for (int g = threadIdx.x; g < s.slab_g; g += blockDim.x) {
             float2 all = own[g];
             if (s.cluster > 1) {
-                all = make_float2(0.f, 0.f);
-                for (int k = 0; k < s.cluster; ++k) {
-                    const float2 v = ld_cluster_f2(ptx::cluster_addr(&own[g], k));
-                    all.x += v.x;
-                    all.y += v.y;
-                }
+                float2 v[kMaxCluster];
+                cluster_pairs(&own[g], s.cluster, v);
+                all = v[0];
+#pragma unroll
+                for (int k = 1; k < kMaxCluster; ++k)
+                    if (k < s.cluster) { all.x += v[k].x; all.y += v[k].y; }
             }
             const float inv = 1.f / ((float)s.pixels * (float)s.cg), r = __ldg(rstd_p + g);
             stat[g] = make_float2(-all.x * inv * r, -all.y * inv * r * r);
@@ -816,9 +826,9 @@ GroupNormShape group_norm_shape(const convbn_group_norm_desc *d, bool backward) 
     s.keep = 0;
     set_slab(s, slab_groups(s, es, kThreads), kThreads);
     s.batch = std::min(s.n, kNormMaxBatch);
-    // Runs of pixels: as many as blocks run at a time (three an SM forward, two backward), each thread at least sixteen pixels.
+    // Runs of pixels: as many as blocks run at a time, each thread at least sixteen pixels.
     const long long units = (long long)(s.g / s.slab_g) * s.batch, most = (s.pixels + 16 * s.ty - 1) / (16 * s.ty);
-    const long long room = (backward ? 2LL : 3LL) * device_sm_count();
+    const long long room = (long long)(backward ? kBlocks2 : kBlocks1) * device_sm_count();
     long long splits = std::min(std::max(1LL, room / units), std::min(most, 1024LL));
     s.cluster = 1;
     if (!backward && splits > 8) { s.cluster = 8; splits -= splits % 8; }
