@@ -440,7 +440,8 @@ int convbn_group_norm_bwd(const convbn_group_norm_desc *desc, const void *dz, co
  *     v = momentum v + grad        u = grad + momentum v  (nesterov != 0)  or  v        X = u made orthogonal as above
  *     master = (1 - lr weight_decay) master - lr sqrt(max(1, rows / cols)) X            weight = master, rounded to `dtype`
  * grad, momentum (v), master: fp32, device; weight: the storage type, or NULL.  `layers` and `params` are read on the host during the call.
- * Every tensor belongs to one layer, once: nothing may overlap.  grad is left as it is.
+ * Every tensor belongs to one layer, once: nothing may overlap.  grad is left as it is.  The same list gives the same bits; what else is in
+ * the list may change a layer's rounding (how its sums are cut).
  *
  * rows, cols >= 1, rows cols <= 2^31, fewer than 2^23 tiles of 128 x 64 a matrix (a stack), count >= 0 (0: nothing is done, no other pointer is looked at), 1 <= steps <= 64, eps >= 0.  Pointers
  * aligned to their element; workspace 256.  All memory of the current device.  CONVBN_EINVAL, CONVBN_EALIGN, CONVBN_EWORKSPACE, CONVBN_ECUDA. */

@@ -429,5 +429,8 @@ struct OrthoTable {
 // Fills rt .. bytes of all items from rows, cols, count; returns the bytes of the workspace.
 size_t ortho_plan(OrthoTable &t);
 cudaError_t launch_ortho(const OrthoTable &t, void *workspace, cudaStream_t st);
+// All matrices with a shorter side of at most 128, kept on chip (ortho_small.cu).
+bool ortho_small_eligible(const OrthoTable &t);
+cudaError_t launch_ortho_small(const OrthoTable &t, cudaStream_t st);
 
 }  // namespace convbn

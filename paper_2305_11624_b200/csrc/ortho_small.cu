@@ -1,0 +1,435 @@
+// Orthogonal updates of matrices whose shorter side is at most 128 (formulas, pairs of halves: ortho.cuh), in one launch without a round through
+// memory: a cluster of blocks keeps X, each block `width` columns of it, and its own copy of A and P.
+//
+// What such a matrix costs is not its products (a step's are 2 us of one tensor core) but the ways between them.  On chip a product, its sums
+// from tensor memory and the rounding to pairs follow one another with a barrier in between; only A, whose sums run over all columns, goes
+// round the cluster: every block sends its part's rows to the block that adds them up, which hands the result to all.  (64 x 64 83 us by the
+// kernel for large matrices, eight microseconds a product, and two launches before it.)
+// X lies as m rows x n columns whichever side is the shorter: a tall matrix is transposed on its way in and out.
+#include <algorithm>
+
+#include "ortho.cuh"
+#include "sm100_ptx.cuh"
+
+namespace convbn {
+
+using namespace ptx;
+
+namespace {
+
+constexpr int kSThreads = 256;
+constexpr uint32_t kSTile = 2 * kOrthoTile;            // 128 rows x 64 columns, hi and lo
+constexpr int kSMaxWidth = 256;
+constexpr int kSMaxCluster = 8;
+
+struct SmallCtl {
+    uint64_t done;
+    double sum, part[8];
+    uint32_t tmem_base;
+};
+
+// A launch's matrices: one cluster each.
+struct SmallShape {
+    int blocks, width;                                 // of a cluster; columns of a block (a multiple of 64)
+};
+
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint4 v) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
+    double v;
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void fence_proxy_async_any() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+// Eight numbers (2^10 times what they stand for) as pairs of halves.
+__device__ __forceinline__ void to_pairs(const float (&v)[8], uint4 &hi, uint4 &lo) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const __half2 a = __floats2half2_rn(v[2 * e], v[2 * e + 1]);
+        const float2 back = __half22float2(a);
+        const __half2 b = __floats2half2_rn(v[2 * e] - back.x, v[2 * e + 1] - back.y);
+        h[e] = *reinterpret_cast<const uint32_t *>(&a);
+        l[e] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+__device__ __forceinline__ float2 from_pair(uint32_t hi, uint32_t lo) {
+    const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&hi)), l = __half22float2(*reinterpret_cast<const __half2 *>(&lo));
+    return make_float2(h.x + l.x, h.y + l.y);
+}
+__device__ __forceinline__ void from_pairs(uint4 hi, uint4 lo, float (&v)[8]) {
+    const float2 a = from_pair(hi.x, lo.x), b = from_pair(hi.y, lo.y), c = from_pair(hi.z, lo.z), d = from_pair(hi.w, lo.w);
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
+}
+
+template <class T>
+__global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_constant__ OrthoTable tab, const SmallShape sh, int *err) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *x = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);          // [width / 64] tiles
+    uint8_t *ap = x + (size_t)(sh.width / 64) * kSTile;                                // two tiles: A, then P; parts of A's sums before
+    SmallCtl *ctl = (SmallCtl *)(ap + 2 * kSTile);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
+    const int blocks = sh.blocks, rank = blocks > 1 ? (int)cluster_rank() : 0;
+    const int matrix = blockIdx.x / blocks;
+    int which = 0;
+    while (which + 1 < tab.items && tab.item[which + 1].first_matrix <= matrix) ++which;
+    const OrthoItem &it = tab.item[which];
+    const bool tall = it.rows > it.cols;
+    const int m = min(it.rows, it.cols), n = max(it.rows, it.cols);
+    const int col0 = rank * sh.width, cols = max(0, min(sh.width, n - col0));          // this block's columns
+    const int m16 = (m + 15) & ~15, n16 = (cols + 15) & ~15, tiles = (cols + 63) / 64;
+    const long long base = (long long)(matrix - it.first_matrix) * it.rows * it.cols;
+    // element (i, j) of X, j within the block
+    auto place = [&](int i, int j) { return base + (tall ? (long long)(col0 + j) * it.cols + i : (long long)i * it.cols + col0 + j); };
+
+    if (threadIdx.x == 0) {
+        mbar_init(&ctl->done, 1);
+        fence_barrier_init();
+    }
+    if (warp == 0) {
+        tmem_alloc(&ctl->tmem_base, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (blocks > 1) cluster_sync_all();
+    pdl_wait();
+    pdl_launch_dependents();
+    const uint32_t tmem = ctl->tmem_base;
+
+    // ---- X = G / (|G| + eps); muon: the momentum's step on the way ----
+    auto update = [&](long long at) -> float {
+        if (tab.muon) {
+            const float v = it.momentum[at];
+            return tab.nesterov ? fmaf(tab.momentum, v, ((const float *)it.g)[at]) : v;
+        }
+        return to_f32(((const T *)it.g)[at]);
+    };
+    const int fast = tall ? m : cols, slow = tall ? cols : m;           // lines of the block's part as it lies in memory
+    double s = 0.;
+    for (int b = warp; b < slow; b += kSThreads / 32)
+        for (int a = lane; a < fast; a += 32) {
+            const long long at = tall ? place(a, b) : place(b, a);
+            if (tab.muon) it.momentum[at] = fmaf(tab.momentum, it.momentum[at], ((const float *)it.g)[at]);
+            const double u = update(at);
+            s += u * u;
+        }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) ctl->part[warp] = s;
+    // (the block's tiles: zeros beyond the matrix)
+    for (int i = threadIdx.x; i < tiles * (int)(kSTile / 16); i += kSThreads) ((uint4 *)x)[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = ctl->part[0];
+        for (int i = 1; i < 8; ++i) s += ctl->part[i];
+        ctl->sum = s;
+    }
+    if (blocks > 1) cluster_sync_all(); else __syncthreads();
+    s = 0.;
+    if (blocks > 1) for (int b = 0; b < blocks; ++b) s += ld_cluster_f64(cluster_addr(&ctl->sum, b));
+    else s = ctl->sum;
+    const double inv = (double)kOrthoScale / (sqrt(s) + tab.eps);
+    for (int b = warp; b < slow; b += kSThreads / 32)
+        for (int a = lane; a < fast; a += 32) {
+            const int i = tall ? a : b, j = tall ? b : a;
+            const float v = (float)(update(place(i, j)) * inv);
+            const __half h = __float2half_rn(v);
+            uint8_t *to = x + (size_t)(j >> 6) * kSTile + ortho_chunk(i, (j & 63) >> 3) + (j & 7) * 2;
+            *(__half *)to = h;
+            *(__half *)(to + kOrthoTile) = __float2half_rn(v - __half2float(h));
+        }
+
+    uint32_t ph = 0;
+    const uint32_t x_at = smem_u32(x), ap_at = smem_u32(ap), hi_word = smem_desc_hi_sw128(1024);
+    // d (+ 256: the products with a lo) = A-operand x B-operand over k steps of 16; tiles of 64 k or 64 n are kSTile apart
+    auto product = [&](uint32_t a_at, uint32_t b_at, bool b_mn, int nn, int steps) {
+        fence_proxy_async_any();
+        if (blocks > 1) cluster_sync_all(); else __syncthreads();
+        if (warp == 0 && steps > 0 && elect_one()) {
+            tc_fence_after_sync();
+            fence_proxy_async_any();
+            const uint32_t idesc = idesc_h16_f32(128, nn, 0, b_mn, 1);
+            for (int k = 0; k < steps; ++k) {
+                const uint32_t a = smem_desc_lo(a_at + (k >> 2) * kSTile, 16) + (k & 3) * 2u;
+                const uint32_t b = b_mn ? smem_desc_lo(b_at, kSTile) + k * 128u : smem_desc_lo(b_at + (k >> 2) * kSTile, 16) + (k & 3) * 2u;
+                umma_bf16_ss_sel(tmem, a, hi_word, b, hi_word, idesc, k);
+                umma_bf16_ss_sel(tmem + 256, a, hi_word, b + (kOrthoTile >> 4), hi_word, idesc, k);
+                umma_bf16_ss_halves<true>(tmem + 256, a + (kOrthoTile >> 4), hi_word, b, hi_word, idesc);
+            }
+            umma_commit(&ctl->done);
+        }
+        if (steps > 0) {
+            if (!mbar_wait_bounded(&ctl->done, ph, nullptr) && threadIdx.x == 0) atomicOr(err, ERRW_TIMEOUT);
+            ph ^= 1u;
+        }
+        tc_fence_after_sync();
+    };
+    const uint32_t row = quarter * 32 + lane, t_row = tmem + ((uint32_t)(quarter * 32) << 16);
+    // 32 sums of this thread's row from column c on
+    auto sums = [&](int c, float (&v)[32]) {
+        uint32_t p[32], q[32];
+        tmem_ld_32x32(t_row + c, p);
+        tmem_ld_32x32(t_row + 256 + c, q);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(p[i]) + __uint_as_float(q[i]);
+    };
+    auto chunk_of = [&](uint8_t *at, int c) { return at + (size_t)(c >> 6) * kSTile + ortho_chunk(row, (c & 63) >> 3); };
+    const bool rows_here = quarter * 32 < m16;                        // (whole warps)
+
+    for (int step = 0; step < tab.steps; ++step) {
+        // ---- A = X X^T ----
+        product(x_at, x_at, false, m16, n16 / 16);
+        if (blocks == 1) {
+            if (rows_here)
+                for (int c = half * 32; c < m16; c += 64) {
+                    float v[32];
+                    sums(c, v);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (c + 8 * q >= m16) break;
+                        float w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = v[8 * q + e] * (1.f / kOrthoScale);
+                        uint4 h, l;
+                        to_pairs(w, h, l);
+                        uint8_t *to = chunk_of(ap, c + 8 * q);
+                        *(uint4 *)to = h;
+                        *(uint4 *)(to + kOrthoTile) = l;
+                    }
+                }
+        } else {
+            // part by part to the block that has the row: [block][its rows][128] in fp32, where P was
+            const int share = 128 / blocks;                           // (blocks: a power of two)
+            if (rows_here) {
+                const uint32_t to = cluster_addr(ap, row / share) + ((rank * share + row % share) * 128) * 4;
+                for (int c = half * 32; c < m16; c += 64) {
+                    float v[32];
+                    if (n16 > 0) sums(c, v);
+                    else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                    }
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        st_cluster_v4(to + (c + 4 * q) * 4, make_uint4(__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]),
+                                                                     __float_as_uint(v[4 * q + 3])));
+                }
+            }
+            tc_fence_before_sync();
+            cluster_sync_all();
+            // each thread eight columns of a row of the share, in turn
+            const int per_row = 16;
+            float w[8][8];
+            const int sets = share * per_row / kSThreads;             // (share 64: 4, 32: 2, 16: 1)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (k >= sets) break;
+                const int idx = threadIdx.x + k * kSThreads, r = idx / per_row, c = idx % per_row * 8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[k][e] = 0.f;
+                if (c < m16)
+                    for (int b = 0; b < blocks; ++b) {
+                        const float4 *f = (const float4 *)(ap + ((size_t)(b * share + r) * 128 + c) * 4);
+                        const float4 f0 = f[0], f1 = f[1];
+                        w[k][0] += f0.x; w[k][1] += f0.y; w[k][2] += f0.z; w[k][3] += f0.w;
+                        w[k][4] += f1.x; w[k][5] += f1.y; w[k][6] += f1.z; w[k][7] += f1.w;
+                    }
+            }
+            cluster_sync_all();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (k >= sets) break;
+                const int idx = threadIdx.x + k * kSThreads, r = rank * share + idx / per_row, c = idx % per_row * 8;
+                if (c >= m16 || r >= m16) continue;
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = w[k][e] * (1.f / kOrthoScale);
+                uint4 h, l;
+                to_pairs(f, h, l);
+                const uint32_t at = (uint32_t)(c >> 6) * kSTile + ortho_chunk(r, (c & 63) >> 3);
+                for (int b = 0; b < blocks; ++b) {
+                    const uint32_t to = cluster_addr(ap, b) + at;
+                    st_cluster_v4(to, h);
+                    st_cluster_v4(to + kOrthoTile, l);
+                }
+            }
+        }
+        tc_fence_before_sync();
+        // ---- P = b A + c A A, where A is ----
+        product(ap_at, ap_at, false, m16, m16 / 16);
+        if (rows_here)
+            for (int c = half * 32; c < m16; c += 64) {
+                float v[32];
+                sums(c, v);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (c + 8 * q >= m16) break;
+                    uint8_t *at = chunk_of(ap, c + 8 * q);
+                    float w[8];
+                    from_pairs(*(const uint4 *)at, *(const uint4 *)(at + kOrthoTile), w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = fmaf(kOrthoB, w[e], v[8 * q + e] * (kOrthoC / kOrthoScale));
+                    uint4 h, l;
+                    to_pairs(w, h, l);
+                    *(uint4 *)at = h;
+                    *(uint4 *)(at + kOrthoTile) = l;
+                }
+            }
+        tc_fence_before_sync();
+        // ---- X <- a X + P X, in place ----
+        product(ap_at, x_at, true, n16, n16 > 0 ? m16 / 16 : 0);
+        const bool last = step + 1 == tab.steps;
+        if (rows_here)
+            for (int t = half; t < tiles; t += 2) {
+                uint8_t *tile = x + (size_t)t * kSTile;
+                float v[64];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float f[32];
+                    if (t * 64 + h * 32 < n16) sums(t * 64 + h * 32, f);
+                    else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) f[i] = 0.f;
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint8_t *at = tile + ortho_chunk(row, h * 4 + q);
+                        float w[8];
+                        from_pairs(*(const uint4 *)at, *(const uint4 *)(at + kOrthoTile), w);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[h * 32 + q * 8 + e] = fmaf(kOrthoA, w[e], f[q * 8 + e] * (1.f / kOrthoScale));
+                    }
+                }
+                if (!last) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        if ((int)row >= m || t * 64 + q * 8 >= n16) continue;       // (rows and columns beyond stay zero)
+                        float w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = v[8 * q + e];
+                        uint4 hh, ll;
+                        to_pairs(w, hh, ll);
+                        uint8_t *at = tile + ortho_chunk(row, q);
+                        *(uint4 *)at = hh;
+                        *(uint4 *)(at + kOrthoTile) = ll;
+                    }
+                    continue;
+                }
+                auto give = [&](long long at, float o, float old) {
+                    if (tab.muon) {
+                        const float w = fmaf(-it.scale, o, tab.keep * old);
+                        it.master[at] = w;
+                        if (it.out) ((T *)it.out)[at] = from_f32<T>(w);
+                    } else {
+                        ((T *)it.out)[at] = from_f32<T>(o);
+                    }
+                };
+                if (tall) {
+                    // a column of X is a line in memory: a warp's rows side by side
+                    if ((int)row < m)
+#pragma unroll
+                        for (int j0 = 0; j0 < 64; j0 += 16) {
+                            float old[16];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) old[j] = tab.muon && t * 64 + j0 + j < cols ? it.master[place(row, t * 64 + j0 + j)] : 0.f;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                if (t * 64 + j0 + j < cols) give(place(row, t * 64 + j0 + j), v[j0 + j] * (1.f / kOrthoScale), old[j]);
+                        }
+                    continue;
+                }
+                // through the warp's quarters of the tile (rows 0 .. 15 where hi was, 16 .. 31 where lo was), then line by line
+                auto spot = [&](int r, int c4) { return tile + (r >= 16 ? kOrthoTile : 0) + quarter * 4096 + (r & 15) * 256 + ((c4 ^ (r & 15)) << 4); };
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < 16; ++c) *(float4 *)spot(lane, c) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+                __syncwarp();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int j = t * 64 + h * 32 + lane;
+                    if (j >= cols) continue;
+                    for (int i0 = 0; i0 < 32; i0 += 16) {
+                        float old[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) old[i] = tab.muon && quarter * 32 + i0 + i < m ? it.master[place(quarter * 32 + i0 + i, j)] : 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (quarter * 32 + i0 + i < m)
+                                give(place(quarter * 32 + i0 + i, j), *(const float *)(spot(i0 + i, h * 8 + (lane >> 2)) + (lane & 3) * 4) * (1.f / kOrthoScale),
+                                     old[i]);
+                    }
+                }
+                __syncwarp();
+            }
+        tc_fence_before_sync();
+    }
+    __syncthreads();
+    if (blocks > 1) cluster_sync_all();
+    if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+// One shape for all of a launch's matrices: as wide as the longest needs.
+bool small_shape(const OrthoTable &t, SmallShape *s) {
+    int longest = 0;
+    for (int i = 0; i < t.items; ++i) {
+        const int m = std::min(t.item[i].rows, t.item[i].cols), n = std::max(t.item[i].rows, t.item[i].cols);
+        if (m > 128 || n > kSMaxCluster * kSMaxWidth) return false;
+        longest = std::max(longest, n);
+    }
+    s->blocks = 1;
+    while (s->blocks < kSMaxCluster && longest > s->blocks * 128) s->blocks *= 2;
+    s->width = ((longest + s->blocks - 1) / s->blocks + 63) / 64 * 64;
+    return true;
+}
+
+template <class T>
+cudaError_t launch_small_t(const OrthoTable &t, const SmallShape &s, cudaStream_t st) {
+    int *err = nullptr;
+    if (cudaError_t e = error_word_address(&err); e != cudaSuccess) return e;
+    auto kernel = ortho_small_kernel<T>;
+    static PerDevice attr;
+    // The whole shared memory whatever the width: blocks of two clusters on one SM could each hold the tensor memory that the other cluster
+    // waits for.
+    const int smem = 1024 + (kSMaxWidth / 64 + 2) * (int)kSTile + (int)sizeof(SmallCtl);
+    if (cudaError_t e = max_dynamic_smem_once(kernel, smem, &attr); e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(t.matrices * s.blocks));
+    cfg.blockDim = dim3(kSThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = s.blocks;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = s.blocks > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, t, s, err);
+}
+
+}  // namespace
+
+bool ortho_small_eligible(const OrthoTable &t) {
+    SmallShape s;
+    return small_shape(t, &s);
+}
+
+cudaError_t launch_ortho_small(const OrthoTable &t, cudaStream_t st) {
+    SmallShape s;
+    if (!small_shape(t, &s)) return cudaErrorInvalidValue;
+    switch (t.dtype) {
+        case CONVBN_F32: return launch_small_t<float>(t, s, st);
+        case CONVBN_F16: return launch_small_t<__half>(t, s, st);
+        default: return launch_small_t<__nv_bfloat16>(t, s, st);
+    }
+}
+
+}  // namespace convbn

@@ -128,7 +128,7 @@ def orthogonalise(g, steps=5, eps=EPS, in_place=False, stream=None):
 
 
 SHAPES = [(1, 1), (1, 7), (7, 1), (64, 64), (64, 147), (147, 64), (100, 33), (96, 9), (128, 128), (129, 257), (257, 129), (384, 128), (130, 2100),
-          (2100, 130), (513, 70), (300, 1030)]
+          (2100, 130), (513, 70), (300, 1030), (128, 2048), (2048, 127), (17, 1025), (3, 4000), (33, 300), (129, 129)]
 
 
 @pytest.mark.gpu
@@ -248,14 +248,15 @@ def test_muon_more_layers_than_a_launch_takes():
 
 @pytest.mark.gpu
 def test_muon_repeats_itself():
-    """The same bits from the same inputs, whatever else is in the list; a captured step is the eager one."""
+    """The same bits from the same list; a layer by itself is right too (what else is in the list decides the kernel and how sums are cut); a
+    captured step is the eager one."""
     import torch
     layers = some_layers([(64, 147), (130, 300), (512, 128)])
     p = C.MuonParams.make(lr=0.02, weight_decay=0.01)
     both = muon(layers, "bf16", p)
-    for i, layer in enumerate(layers):
-        alone = muon([layer], "bf16", p)[0]
-        assert all(torch.equal(a, b) for a, b in zip(alone, both[i]))
+    assert all(torch.equal(a, b) for x, y in zip(muon(layers, "bf16", p), both) for a, b in zip(x, y))
+    for layer in layers:
+        check_muon([layer], muon([layer], "bf16", p), "bf16", p)
     twice = muon(layers, "bf16", p, repeat=2)
     dev = [(g.cuda(), v.cuda().clone(), m.cuda().clone(), m.cuda().to(torch.bfloat16)) for g, v, m in layers]
     table = C.MuonLayers(dev)
