@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <functional>
 #include <map>
 #include <mutex>
 #include <new>
@@ -1814,19 +1815,19 @@ static int ortho_room(size_t need, const void *workspace, size_t bytes) {
     return aligned(workspace, 256) ? CONVBN_OK : CONVBN_EALIGN;
 }
 
-static OrthoTable ortho_stack(int rows, int cols, int count) {
-    OrthoTable t = {};
+static size_t ortho_stack(OrthoTable &t, int rows, int cols, int count, int steps) {
     t.items = 1;
+    t.steps = steps;
     t.item[0].rows = rows;
     t.item[0].cols = cols;
     t.item[0].count = count;
-    return t;
+    return ortho_plan(t, ortho_wide(rows, cols));
 }
 
 size_t convbn_orthogonalise_workspace_bytes(int rows, int cols, int count) {
     if (!ortho_sizes(rows, cols, count) || count == 0) return 0;
-    OrthoTable t = ortho_stack(rows, cols, count);
-    return ortho_plan(t);
+    OrthoTable t = {};
+    return ortho_stack(t, rows, cols, count, 1);         // (the steps' number does not enter the size)
 }
 
 int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols, int count, int steps, double eps, void *workspace,
@@ -1836,9 +1837,8 @@ int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols
     if (count == 0) return CONVBN_OK;
     if (!g || !out) return CONVBN_EINVAL;
     if (!aligned(g, elem_size(dtype)) || !aligned(out, elem_size(dtype))) return CONVBN_EALIGN;
-    OrthoTable t = ortho_stack(rows, cols, count);
-    CK(ortho_room(ortho_plan(t), workspace, workspace_bytes));
-    t.steps = steps;
+    OrthoTable t = {};
+    CK(ortho_room(ortho_stack(t, rows, cols, count, steps), workspace, workspace_bytes));
     t.dtype = dtype;
     t.eps = eps;
     t.item[0].g = g;
@@ -1849,20 +1849,40 @@ int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols
     return CONVBN_OK;
 }
 
-// The launch that begins with layer `first`: as many layers as it takes and an int counts the tasks of.  Returns the next one's first.
-static int muon_launch(const convbn_muon_layer *layers, int count, int first, OrthoTable *t) {
+// A launch's layers: from `from` on, those whose steps go over X (wide = false) or over m x m matrices, as many as a launch takes and an int
+// counts the tasks of; their numbers in `taken`.  Returns where the next launch of the kind begins.  Small layers go with the wide ones if
+// there are any: beside those they cost nothing, by themselves a launch's latency.
+static bool muon_wide(const convbn_muon_layer &l, bool any) { return ortho_wide(l.rows, l.cols) || (any && std::min(l.rows, l.cols) <= 256); }
+static int muon_launch(const convbn_muon_layer *layers, int count, int from, bool wide, bool any, OrthoTable *t, int *taken) {
     long long tiles = 0;
-    int i = first;
-    for (; i < count && i - first < kOrthoItems; ++i) {
+    int i = from;
+    for (t->items = 0; i < count && t->items < kOrthoItems; ++i) {
+        if (muon_wide(layers[i], any) != wide) continue;
         tiles += (((long long)layers[i].rows + 127) / 128) * (((long long)layers[i].cols + 127) / 128) * 2;
-        if (tiles >= (1LL << 23) && i > first) break;
-        OrthoItem &it = t->item[i - first];
+        if (tiles >= (1LL << 23) && t->items > 0) break;
+        OrthoItem &it = t->item[t->items];
         it.rows = layers[i].rows;
         it.cols = layers[i].cols;
         it.count = 1;
+        taken[t->items++] = i;
     }
-    t->items = i - first;
     return i;
+}
+// f(table, its workspace's bytes, its layers' numbers) for every launch
+static int muon_launches(const convbn_muon_layer *layers, int count, int steps, const std::function<int(OrthoTable &, size_t, const int *)> &f) {
+    bool any = false;
+    for (int i = 0; i < count; ++i) any |= ortho_wide(layers[i].rows, layers[i].cols);
+    for (int wide = 1; wide >= 0; --wide)
+        for (int from = 0; from < count;) {
+            OrthoTable t = {};
+            int taken[kOrthoItems];
+            from = muon_launch(layers, count, from, wide, any, &t, taken);
+            if (t.items == 0) break;
+            t.steps = steps;
+            const size_t bytes = ortho_plan(t, wide);
+            CK(f(t, bytes, taken));
+        }
+    return CONVBN_OK;
 }
 static bool muon_sizes(const convbn_muon_layer *layers, int count) {
     if (count < 0 || (count > 0 && !layers)) return false;
@@ -1874,12 +1894,7 @@ static bool muon_sizes(const convbn_muon_layer *layers, int count) {
 size_t convbn_muon_workspace_bytes(const convbn_muon_layer *layers, int count) {
     if (!muon_sizes(layers, count)) return 0;
     size_t most = 0;
-    for (int i = 0; i < count;) {
-        OrthoTable t = {};
-        i = muon_launch(layers, count, i, &t);
-        const size_t bytes = ortho_plan(t);
-        if (bytes > most) most = bytes;
-    }
+    muon_launches(layers, count, 1, [&](OrthoTable &, size_t bytes, const int *) { most = std::max(most, bytes); return (int)CONVBN_OK; });
     return most;
 }
 
@@ -1895,14 +1910,11 @@ int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, cons
         if (!aligned(layers[i].grad, 4) || !aligned(layers[i].momentum, 4) || !aligned(layers[i].master, 4) ||
             !aligned(layers[i].weight, elem_size(dtype)))
             return CONVBN_EALIGN;
-    if (count > kOrthoItems) CK(ortho_room(convbn_muon_workspace_bytes(layers, count), workspace, workspace_bytes));    // (before anything is launched)
+    // (before anything is launched)
+    CK(muon_launches(layers, count, params->steps, [&](OrthoTable &, size_t bytes, const int *) { return ortho_room(bytes, workspace, workspace_bytes); }));
     cudaStream_t st = (cudaStream_t)stream;
     t_prof_phase = "muon";
-    for (int first = 0; first < count;) {
-        OrthoTable t = {};
-        const int next = muon_launch(layers, count, first, &t);
-        CK(ortho_room(ortho_plan(t), workspace, workspace_bytes));
-        t.steps = params->steps;
+    return muon_launches(layers, count, params->steps, [&](OrthoTable &t, size_t, const int *taken) -> int {
         t.dtype = dtype;
         t.muon = 1;
         t.nesterov = params->nesterov != 0;
@@ -1910,7 +1922,7 @@ int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, cons
         t.keep = (float)(1. - params->lr * params->weight_decay);
         t.eps = params->eps;
         for (int i = 0; i < t.items; ++i) {
-            const convbn_muon_layer &l = layers[first + i];
+            const convbn_muon_layer &l = layers[taken[i]];
             OrthoItem &it = t.item[i];
             it.g = l.grad;
             it.momentum = l.momentum;
@@ -1919,9 +1931,8 @@ int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, cons
             it.scale = (float)(params->lr * (l.rows > l.cols ? std::sqrt((double)l.rows / l.cols) : 1.));
         }
         LAUNCH("ortho", launch_ortho(t, workspace, st));
-        first = next;
-    }
-    return CONVBN_OK;
+        return CONVBN_OK;
+    });
 }
 
 int convbn_selftest_wait_timeout(void *stream) {

@@ -412,22 +412,30 @@ struct OrthoItem {
     void *out;                              // the orthogonal matrix, or the weights in storage type (may be NULL)
     int rows, cols, count;                  // count like matrices, one after the other in g and out
     int rt, ct;                             // tiles of 128 rows, of 128 columns
+    int wide;                               // its steps go over m x m matrices
     int splits, per_split;                  // pieces that the sums of X X^T are cut into, steps of 64 of each
     int first_sum, first_tile, first_gram, first_square, first_update, first_matrix;       // tasks, matrices of the items before
     float scale;                            // of the update (muon)
     long long base, bytes;                  // its first matrix's place in the workspace; of one matrix
 };
+constexpr int kOrthoPhases = 256;
 struct OrthoTable {
     int items, steps;
     int sums, tiles, grams, squares, updates, matrices;       // in all
+    int phases;                             // the products of all steps, one after the other ...
+    uint16_t op[kOrthoPhases];              // ... what each is (ortho.cuh) ...
+    uint16_t lowers[kOrthoPhases], xs[kOrthoPhases];          // ... after how many products of A's size and of X's ...
+    int first[kOrthoPhases + 1];            // ... and tasks
     int dtype;                              // of g and out (muon: of out; g is fp32)
     int muon, nesterov;
     float momentum, keep, lr;               // keep = 1 - lr weight_decay
     double eps;
     OrthoItem item[kOrthoItems];
 };
-// Fills rt .. bytes of all items from rows, cols, count; returns the bytes of the workspace.
-size_t ortho_plan(OrthoTable &t);
+// Whether the items' steps go over m x m matrices (ortho.cuh) rather than over X.
+bool ortho_wide(int rows, int cols);
+// Fills rt .. bytes of all items from rows, cols, count, and the phases; returns the bytes of the workspace.
+size_t ortho_plan(OrthoTable &t, bool wide);
 cudaError_t launch_ortho(const OrthoTable &t, void *workspace, cudaStream_t st);
 // All matrices with a shorter side of at most 128, kept on chip (ortho_small.cu).
 bool ortho_small_eligible(const OrthoTable &t);

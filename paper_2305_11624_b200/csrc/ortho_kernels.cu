@@ -1,4 +1,6 @@
 // Orthogonal updates (formulas, pairs of halves, tiles: ortho.cuh): the matrices' norms, their way into tiles, and the products.
+#include <algorithm>
+
 #include "ortho.cuh"
 #include "sm100_ptx.cuh"
 
@@ -17,15 +19,18 @@ struct OrthoPlace {
         s_bytes = (long long)d * d * 2 * kOrthoTile;
     }
     __host__ __device__ long long x(int which) const { return which * 2 * x_bytes; }        // X before and after a step, in turn
+    // A, R, then, where X is long, B and Q in its two places
     __host__ __device__ long long a() const { return 4 * x_bytes; }
-    __host__ __device__ long long p() const { return 4 * x_bytes + 2 * s_bytes; }
-    __host__ __device__ long long parts() const { return 4 * x_bytes + 4 * s_bytes; }       // fp32 pieces of A's tiles, 64 KB each
+    __host__ __device__ long long r() const { return 4 * x_bytes + 2 * s_bytes; }
+    __host__ __device__ long long b() const { return 4 * x_bytes + 4 * s_bytes; }
+    __host__ __device__ long long q(int which) const { return 4 * x_bytes + (6 + 2 * which) * s_bytes; }
+    __host__ __device__ long long parts(bool wide) const { return 4 * x_bytes + (wide ? 10 : 4) * s_bytes; }       // fp32 pieces of A's tiles, 64 KB each
 };
 __host__ __device__ inline int ortho_chunks(const OrthoItem &it) { return (int)(((long long)it.rows * it.cols + kOrthoChunk - 1) / kOrthoChunk); }
 __host__ __device__ inline int ortho_lower(int rt, int ct) { const int d = rt < ct ? rt : ct; return d * (d + 1) / 2; }
 __host__ __device__ inline long long ortho_sums_at(const OrthoItem &it) {
     const long long parts = it.splits > 1 ? (long long)ortho_lower(it.rt, it.ct) * it.splits * 65536 : 0;
-    return OrthoPlace(it.rt, it.ct).parts() + parts;
+    return OrthoPlace(it.rt, it.ct).parts(it.wide) + parts;
 }
 // In front of the matrices: [tasks taken | warps' shares done, per matrix | tickets of A's pieces, eight per tile], ints.
 __host__ __device__ inline int ortho_words(const OrthoTable &t) { return 1 + t.matrices + 8 * t.squares; }
@@ -118,14 +123,14 @@ __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__
 }
 
 // ---- products ---------------------------------------------------------------------------------------------------------------------
-// All products of all steps in one launch.  CTA = 10 warps: 0 takes tasks and loads, 1 MMA issuer and owner of tensor memory, 2-9 epilogue.
-// A task is a 128 x 128 tile of A, P or X (or a piece of the k of one of A's); k in steps of 64.  A step's four tiles (hi and lo of both
-// operands) are 64 KB and feed twelve MMAs.  What a task adds to its product (P: A's tile, X: X's) is brought by bulk copies too: read by the
+// All products of all steps in one launch (what they are: ortho.cuh).  CTA = 10 warps: 0 takes tasks and loads, 1 MMA issuer and owner of tensor memory, 2-9 epilogue.
+// A task is a 128 x 128 tile of a result (or a piece of the k of one of A's); k in steps of 64.  A step's four tiles (hi and lo of both
+// operands) are 64 KB and feed twelve MMAs.  What a task adds to its product is brought by bulk copies too: read by the
 // rows' own threads it took 7000 clocks of a task, 32 lines an instruction.  hi hi is summed apart from the other two products: the tensor core's sums drift towards zero
 // with their length, and those of small numbers do not notice.  For the same reason a sum over more than 1024 k is cut: the epilogue adds
 // the pieces up in registers, in fp32 with rounding.
 //
-// Order.  Tasks are numbered step by step, A's of all matrices, then P's, then X's, and taken one by one off a counter.  A task waits until its
+// Order.  Tasks are numbered product by product, those of all matrices together, and taken one by one off a counter.  A task waits until its
 // matrix's earlier tasks are done, which a counter of the matrix tells.  What it waits for has a lower number, so it has been taken by a CTA
 // that runs: however few CTAs run at a time, one of them can go on.
 constexpr int kOThreads = 320;
@@ -152,42 +157,56 @@ struct OrthoOperand {
 struct OrthoTask {
     const OrthoItem *it;
     uint8_t *m;                  // the matrix's part of the workspace
-    int phase, index;            // product, step
-    int copy;
+    int op, x, q;                // which product; X's and Q's places before it
+    bool update, last;           // of X's size; the last product
+    int phase, copy;
     int i, j;                    // row and column of the tile of 128 x 128
-    int lower;                   // its number in the lower half (A, P)
-    int split;                   // piece of its k (A)
+    int lower;                   // its number in the lower half
+    int split;                   // piece of its k (A = X X^T)
     int from, to;                // steps of k
 };
 
 __device__ __forceinline__ OrthoTask ortho_task(const OrthoTable &tab, uint8_t *ws, int t) {
     OrthoTask k;
-    const int per_step = tab.grams + tab.squares + tab.updates;
-    k.index = t / per_step;
-    t -= k.index * per_step;
-    k.phase = t < tab.grams ? kOrthoGram : t < tab.grams + tab.squares ? kOrthoSquare : kOrthoUpdate;
-    const int phase = k.phase;
-    if (phase != kOrthoGram) t -= tab.grams;
-    if (phase == kOrthoUpdate) t -= tab.squares;
-    auto first = [phase](const OrthoItem &i) { return phase == kOrthoUpdate ? i.first_update : phase == kOrthoSquare ? i.first_square : i.first_gram; };
+    int lo = 0, hi = tab.phases - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (tab.first[mid] <= t) lo = mid; else hi = mid - 1;
+    }
+    k.phase = lo;
+    t -= tab.first[lo];
+    const int word = tab.op[lo];
+    k.op = word & kOrthoOpMask;
+    k.x = word & kOrthoX ? 1 : 0;
+    k.q = word & kOrthoQSource ? 1 : 0;
+    k.last = word & kOrthoLast;
+    k.update = k.op >= kOrthoUpdate;
+    const int op = k.op;
+    auto first = [op](const OrthoItem &i) {
+        return op >= kOrthoUpdate ? i.first_update : op == kOrthoGram ? i.first_gram : op == kOrthoBQ ? 2 * i.first_square : i.first_square;
+    };
     k.it = &tab.item[find_item(tab, t, first)];
     const OrthoItem &it = *k.it;
     const int side = min(it.rows, it.cols);
     int local = t - first(it);
     k.split = k.lower = 0;
-    if (phase == kOrthoUpdate) {
+    if (k.update) {
         const int per = it.rt * it.ct;
         k.copy = local / per;
         local -= k.copy * per;
         k.i = local / it.ct;
         k.j = local - k.i * it.ct;
     } else {
-        if (phase == kOrthoGram) {
+        const int per = ortho_lower(it.rt, it.ct);
+        if (op == kOrthoGram) {
             const int whole = local / it.splits;
             k.split = local - whole * it.splits;
             local = whole;
+        } else if (op == kOrthoBQ) {               // a matrix's tiles of B, then those of Q
+            const int both = local / per;
+            k.op = both & 1 ? kOrthoQ : kOrthoB;
+            local -= both * per - (both >> 1) * per;
         }
-        const int per = ortho_lower(it.rt, it.ct);
         k.copy = local / per;
         local -= k.copy * per;
         k.lower = local;
@@ -199,9 +218,9 @@ __device__ __forceinline__ OrthoTask ortho_task(const OrthoTable &tab, uint8_t *
         k.j = local - i * (i + 1) / 2;
     }
     k.m = ws + it.base + k.copy * it.bytes;
-    k.from = phase == kOrthoGram ? k.split * it.per_split : 0;
-    k.to = ((phase == kOrthoGram ? max(it.rows, it.cols) : side) + 63) / 64;
-    if (phase == kOrthoGram) k.to = min(k.to, k.from + it.per_split);
+    k.from = op == kOrthoGram ? k.split * it.per_split : 0;
+    k.to = ((op == kOrthoGram ? max(it.rows, it.cols) : side) + 63) / 64;
+    if (op == kOrthoGram) k.to = min(k.to, k.from + it.per_split);
     return k;
 }
 
@@ -214,19 +233,25 @@ __device__ __forceinline__ void ortho_operands(const OrthoTask &k, OrthoOperand 
     const OrthoPlace place(it.rt, it.ct);
     const int d = min(it.rt, it.ct), never = 1 << 30;
     const bool tall = it.rows > it.cols;
-    const long long x = place.x(k.index & 1);
-    if (k.phase == kOrthoGram) {
+    const long long x = place.x(k.x);
+    if (k.op == kOrthoGram) {
         a = ortho_operand(x, it.ct, k.i, tall ? 0 : never, place.x_bytes);
         b = ortho_operand(x, it.ct, k.j, tall ? 0 : never, place.x_bytes);
-    } else if (k.phase == kOrthoSquare) {
-        a = ortho_operand(place.a(), d, k.i, 2 * (k.i + 1), place.s_bytes);
-        b = ortho_operand(place.a(), d, k.j, 2 * (k.j + 1), place.s_bytes);
-    } else if (tall) {
-        a = ortho_operand(x, it.ct, k.i, never, place.x_bytes);
-        b = ortho_operand(place.p(), d, k.j, 2 * (k.j + 1), place.s_bytes);
+    } else if (!k.update) {
+        const bool square = k.op == kOrthoSquare || k.op == kOrthoSquareQ;
+        const long long left = square ? place.a() : place.r();
+        const long long right = square || k.op == kOrthoB ? place.a() : k.op == kOrthoA ? place.b() : place.q(k.q);
+        a = ortho_operand(left, d, k.i, 2 * (k.i + 1), place.s_bytes);
+        b = ortho_operand(right, d, k.j, 2 * (k.j + 1), place.s_bytes);
     } else {
-        a = ortho_operand(place.p(), d, k.i, 2 * (k.i + 1), place.s_bytes);
-        b = ortho_operand(x, it.ct, k.j, 0, place.x_bytes);
+        const long long by = k.op == kOrthoUpdate ? place.r() : place.q(k.q);
+        if (tall) {
+            a = ortho_operand(x, it.ct, k.i, never, place.x_bytes);
+            b = ortho_operand(by, d, k.j, 2 * (k.j + 1), place.s_bytes);
+        } else {
+            a = ortho_operand(by, d, k.i, 2 * (k.i + 1), place.s_bytes);
+            b = ortho_operand(x, it.ct, k.j, 0, place.x_bytes);
+        }
     }
 }
 
@@ -284,7 +309,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
 
     if (warp == 0) {
         if (elect_one()) {
-            const int total = (tab.grams + tab.squares + tab.updates) * tab.steps;
+            const int total = tab.first[tab.phases];
             uint32_t it = 0, n = 0;
             bool ok = true;
             int next = atomicAdd(taken, 1);
@@ -301,8 +326,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 next = atomicAdd(taken, 1);
                 const OrthoTask k = ortho_task(tab, ws, t);
                 // the eight warps' shares of every earlier task of the matrix
-                const int lower = ortho_lower(k.it->rt, k.it->ct), per = 2 * lower + k.it->rt * k.it->ct;
-                const int need = 8 * (k.index * per + k.phase * lower);
+                const int need = 8 * (tab.lowers[k.phase] * ortho_lower(k.it->rt, k.it->ct) + tab.xs[k.phase] * k.it->rt * k.it->ct);
                 const int *flag = done + k.it->first_matrix + k.copy;
                 if (load_acquire(flag) < need) {
                     const uint64_t t0 = globaltimer_ns();
@@ -413,28 +437,34 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
             const OrthoTask k = ortho_task(tab, ws, t);
             const OrthoItem &it = *k.it;
             const OrthoPlace place(it.rt, it.ct);
-            const int which = k.index & 1;
-            const bool last = k.phase == kOrthoUpdate && k.index + 1 == tab.steps;
-            // numbers are 2^10 times what they stand for, sums of products 2^20 times
+            // numbers are 2^10 times what they stand for (Q's 2^8), sums of products 2^20 times (2^18)
             const long long x_at = ((long long)k.i * 2 * it.ct + 2 * k.j + half) * kOrthoTile;
             const long long s_at = ((long long)k.i * 2 * min(it.rt, it.ct) + 2 * k.j + half) * kOrthoTile;
-            float v[64], f_new = 1.f / kOrthoScale;
-            if (k.phase == kOrthoGram) {
+            const long long lo_at = k.update ? place.x_bytes : place.s_bytes;
+            long long old_at = -1, to_at;
+            float v[64], f_old = kOrthoCoefA, f_new = 1.f / kOrthoScale;
+            switch (k.op) {
+                case kOrthoGram: to_at = place.a() + s_at; break;
+                case kOrthoSquare: case kOrthoSquareQ:
+                    old_at = place.a() + s_at; to_at = place.r() + s_at; f_old = kOrthoCoefB; f_new = kOrthoCoefC / kOrthoScale; break;
+                case kOrthoB: old_at = place.a() + s_at; to_at = place.b() + s_at; break;
+                case kOrthoA: old_at = place.b() + s_at; to_at = place.a() + s_at; break;
+                case kOrthoQ: old_at = place.q(k.q) + s_at; to_at = place.q(k.q ^ 1) + s_at; break;
+                case kOrthoUpdate: old_at = place.x(k.x) + x_at; to_at = place.x(k.x ^ 1) + x_at; break;
+                default: to_at = place.x(k.x ^ 1) + x_at; f_new = 1.f / kOrthoQScale; break;
+            }
+            if (old_at < 0) {
 #pragma unroll
                 for (int i = 0; i < 64; ++i) v[i] = 0.f;
             } else {
-                const bool square = k.phase == kOrthoSquare;
-                const uint8_t *old = k.m + (square ? place.a() + s_at : place.x(which) + x_at) + quarter * 4096;
-                const long long old_lo = square ? place.s_bytes : place.x_bytes;
-                const float f_old = square ? kOrthoB : kOrthoA;
-                if (square) f_new = kOrthoC / kOrthoScale;
+                const uint8_t *old = k.m + old_at + quarter * 4096;
                 if (lane == 0) {
                     fence_proxy_async_global();                 // (the producer saw the counter)
                     fence_proxy_async_smem();
                     const uint32_t bar = smem_u32(&ctl->old_full[warp - 2]);
                     mbar_arrive_expect_tx(bar, 8192);
                     bulk_load(smem_u32(buf), old, 4096, bar);
-                    bulk_load(smem_u32(buf) + 4096, old + old_lo, 4096, bar);
+                    bulk_load(smem_u32(buf) + 4096, old + lo_at, 4096, bar);
                 }
                 ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->old_full[warp - 2], old_ph, abort_flag));
                 if (!ok) {                                      // (the copy in flight lands before the block ends)
@@ -472,10 +502,10 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 if (lane == 0) mbar_arrive(&ctl->acc_empty[acc]);
             }
             if (!ok) break;
-            if (k.phase == kOrthoGram && it.splits > 1) {
+            if (k.op == kOrthoGram && it.splits > 1) {
                 // The piece goes to memory, [4 columns][row] by chunks of 16 bytes; the warp whose piece is the last of this share of the
                 // tile adds all of them up, in their order.
-                float4 *part = (float4 *)(k.m + place.parts() + ((long long)k.lower * it.splits + k.split) * 65536) + half * 2048 + row;
+                float4 *part = (float4 *)(k.m + place.parts(it.wide) + ((long long)k.lower * it.splits + k.split) * 65536) + half * 2048 + row;
 #pragma unroll
                 for (int c = 0; c < 16; ++c) __stcg(part + c * 128, make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]));
                 __threadfence();
@@ -496,33 +526,41 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                     for (int c = 0; c < 16; ++c) { v[4 * c] += f[c].x; v[4 * c + 1] += f[c].y; v[4 * c + 2] += f[c].z; v[4 * c + 3] += f[c].w; }
                 }
             }
-            if (!last) {
-                uint8_t *to;
-                long long lo_at;
-                if (k.phase == kOrthoUpdate) { to = k.m + place.x(which ^ 1) + x_at; lo_at = place.x_bytes; }
-                else { to = k.m + (k.phase == kOrthoGram ? place.a() : place.p()) + s_at; lo_at = place.s_bytes; }
-                to += quarter * 4096;
+            if (!k.last) {
                 // through the warp's staging, where its share of a tile lies as it does in memory
+                auto put = [&](uint8_t *to) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    uint32_t wh[4], wl[4];
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t wh[4], wl[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const __half2 h = __floats2half2_rn(v[8 * c + 2 * e], v[8 * c + 2 * e + 1]);
-                        const float2 back = __half22float2(h);
-                        const __half2 l = __floats2half2_rn(v[8 * c + 2 * e] - back.x, v[8 * c + 2 * e + 1] - back.y);
-                        wh[e] = *reinterpret_cast<const uint32_t *>(&h);
-                        wl[e] = *reinterpret_cast<const uint32_t *>(&l);
+                        for (int e = 0; e < 4; ++e) {
+                            const __half2 h = __floats2half2_rn(v[8 * c + 2 * e], v[8 * c + 2 * e + 1]);
+                            const float2 back = __half22float2(h);
+                            const __half2 l = __floats2half2_rn(v[8 * c + 2 * e] - back.x, v[8 * c + 2 * e + 1] - back.y);
+                            wh[e] = *reinterpret_cast<const uint32_t *>(&h);
+                            wl[e] = *reinterpret_cast<const uint32_t *>(&l);
+                        }
+                        *(uint4 *)(buf + ortho_chunk(lane, c)) = make_uint4(wh[0], wh[1], wh[2], wh[3]);      // (its rows start on a multiple of 8)
+                        *(uint4 *)(buf + 4096 + ortho_chunk(lane, c)) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
                     }
-                    *(uint4 *)(buf + ortho_chunk(lane, c)) = make_uint4(wh[0], wh[1], wh[2], wh[3]);      // (its rows start on a multiple of 8)
-                    *(uint4 *)(buf + 4096 + ortho_chunk(lane, c)) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        bulk_store(to, buf, 4096);
+                        bulk_store(to + lo_at, buf + 4096, 4096);
+                        tma_store_commit();
+                    }
+                };
+                put(k.m + to_at + quarter * 4096);
+                if (k.op == kOrthoSquareQ) {
+                    const int diagonal = k.i == k.j ? (int)row - half * 64 : -1;
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) v[i] = v[i] * (kOrthoQScale / kOrthoScale) + (i == diagonal ? kOrthoCoefA * kOrthoQScale : 0.f);
+                    if (lane == 0) tma_store_wait_read<0>();
+                    __syncwarp();
+                    put(k.m + place.q(0) + s_at + quarter * 4096);
                 }
-                fence_proxy_async_smem();
-                __syncwarp();
                 if (lane == 0) {
-                    bulk_store(to, buf, 4096);
-                    bulk_store(to + lo_at, buf + 4096, 4096);
-                    tma_store_commit();
                     tma_store_wait_all<0>();                    // (written, and seen by this thread, whose release passes that on)
                     add_release(done + it.first_matrix + k.copy, 1);
                 }
@@ -588,11 +626,54 @@ cudaError_t launch_ortho_t(const OrthoTable &t, uint8_t *ws, cudaStream_t st) {
 
 }  // namespace
 
-size_t ortho_plan(OrthoTable &t) {
+// Two steps at a time or more pay where X is at least twice as long as it is high.
+bool ortho_wide(int rows, int cols) { return std::max(rows, cols) >= 2LL * std::min(rows, cols); }
+
+static void ortho_phases(OrthoTable &t, bool wide) {
+    int x = 0, lowers = 0, xs = 0, at = 0, n = 0;
+    auto add = [&](int op, int q = 0) {
+        const bool update = op >= kOrthoUpdate;
+        t.op[n] = (uint16_t)(op | (x ? kOrthoX : 0) | (q ? kOrthoQSource : 0));
+        t.lowers[n] = (uint16_t)lowers;
+        t.xs[n] = (uint16_t)xs;
+        t.first[n++] = at;
+        at += update ? t.updates : op == kOrthoGram ? t.grams : op == kOrthoBQ ? 2 * t.squares : t.squares;
+        if (update) { ++xs; x ^= 1; } else lowers += op == kOrthoBQ ? 2 : 1;
+    };
+    const int stages = wide ? (t.steps + 2) / 3 : t.steps;
+    for (int s = 0, left = t.steps; s < stages; ++s) {
+        const int k = (left + stages - s - 1) / (stages - s);          // 5: 3 and 2
+        left -= k;
+        add(kOrthoGram);
+        if (k == 1) {
+            add(kOrthoSquare);
+            add(kOrthoUpdate);
+            continue;
+        }
+        int q = 0;
+        for (int i = 0; i < k; ++i) {
+            add(i ? kOrthoSquare : kOrthoSquareQ);
+            if (i + 1 < k) {
+                add(i ? kOrthoBQ : kOrthoB, q);
+                add(kOrthoA);
+            } else {
+                add(kOrthoQ, q);
+            }
+            if (i) q ^= 1;
+        }
+        add(kOrthoUpdateQ, q);
+    }
+    t.op[n - 1] |= kOrthoLast;
+    t.first[n] = at;
+    t.phases = n;
+}
+
+size_t ortho_plan(OrthoTable &t, bool wide) {
     const int sms = device_sm_count();
     t.sums = t.tiles = t.grams = t.squares = t.updates = t.matrices = 0;
     for (int i = 0; i < t.items; ++i) {
         OrthoItem &it = t.item[i];
+        it.wide = wide;
         it.rt = (it.rows + 127) / 128;
         it.ct = (it.cols + 127) / 128;
         it.first_sum = t.sums; it.first_tile = t.tiles; it.first_square = t.squares; it.first_update = t.updates; it.first_matrix = t.matrices;
@@ -615,6 +696,7 @@ size_t ortho_plan(OrthoTable &t) {
         it.first_gram = t.grams;
         t.grams += it.count * ortho_lower(it.rt, it.ct) * it.splits;
     }
+    ortho_phases(t, wide);
     long long end = (long long)align_up((size_t)ortho_words(t) * sizeof(int), 1024);
     for (int i = 0; i < t.items; ++i) {
         OrthoItem &it = t.item[i];

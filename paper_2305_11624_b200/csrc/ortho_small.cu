@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
                     float w[8];
                     from_pairs(*(const uint4 *)at, *(const uint4 *)(at + kOrthoTile), w);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = fmaf(kOrthoB, w[e], v[8 * q + e] * (kOrthoC / kOrthoScale));
+                    for (int e = 0; e < 8; ++e) w[e] = fmaf(kOrthoCoefB, w[e], v[8 * q + e] * (kOrthoCoefC / kOrthoScale));
                     uint4 h, l;
                     to_pairs(w, h, l);
                     *(uint4 *)at = h;
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
                         float w[8];
                         from_pairs(*(const uint4 *)at, *(const uint4 *)(at + kOrthoTile), w);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[h * 32 + q * 8 + e] = fmaf(kOrthoA, w[e], f[q * 8 + e] * (1.f / kOrthoScale));
+                        for (int e = 0; e < 8; ++e) v[h * 32 + q * 8 + e] = fmaf(kOrthoCoefA, w[e], f[q * 8 + e] * (1.f / kOrthoScale));
                     }
                 }
                 if (!last) {
