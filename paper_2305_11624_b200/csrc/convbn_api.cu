@@ -1815,19 +1815,20 @@ static int ortho_room(size_t need, const void *workspace, size_t bytes) {
     return aligned(workspace, 256) ? CONVBN_OK : CONVBN_EALIGN;
 }
 
-static size_t ortho_stack(OrthoTable &t, int rows, int cols, int count, int steps) {
+static size_t ortho_stack(OrthoTable &t, int dtype, int rows, int cols, int count, int steps) {
     t.items = 1;
     t.steps = steps;
     t.item[0].rows = rows;
     t.item[0].cols = cols;
     t.item[0].count = count;
-    return ortho_plan(t, ortho_wide(rows, cols));
+    // (an fp32 result shows what several steps at a time lose, 2 to 3 times the direct ones' error; the others' rounding hides it)
+    return ortho_plan(t, dtype != CONVBN_F32 && ortho_wide(rows, cols));
 }
 
 size_t convbn_orthogonalise_workspace_bytes(int rows, int cols, int count) {
     if (!ortho_sizes(rows, cols, count) || count == 0) return 0;
     OrthoTable t = {};
-    return ortho_stack(t, rows, cols, count, 1);         // (the steps' number does not enter the size)
+    return ortho_stack(t, CONVBN_BF16, rows, cols, count, 1);         // (the larger of the types'; the steps' number does not enter)
 }
 
 int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols, int count, int steps, double eps, void *workspace,
@@ -1837,8 +1838,9 @@ int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols
     if (count == 0) return CONVBN_OK;
     if (!g || !out) return CONVBN_EINVAL;
     if (!aligned(g, elem_size(dtype)) || !aligned(out, elem_size(dtype))) return CONVBN_EALIGN;
+    CK(ortho_room(convbn_orthogonalise_workspace_bytes(rows, cols, count), workspace, workspace_bytes));
     OrthoTable t = {};
-    CK(ortho_room(ortho_stack(t, rows, cols, count, steps), workspace, workspace_bytes));
+    ortho_stack(t, dtype, rows, cols, count, steps);
     t.dtype = dtype;
     t.eps = eps;
     t.item[0].g = g;

@@ -422,6 +422,7 @@ constexpr int kOrthoPhases = 256;
 struct OrthoTable {
     int items, steps;
     int sums, tiles, grams, squares, updates, matrices;       // in all
+    int narrow;                             // m x m products in tiles of 128 x 64, not 128 x 128
     int phases;                             // the products of all steps, one after the other ...
     uint16_t op[kOrthoPhases];              // ... what each is (ortho.cuh) ...
     uint16_t lowers[kOrthoPhases], xs[kOrthoPhases];          // ... after how many products of A's size and of X's ...

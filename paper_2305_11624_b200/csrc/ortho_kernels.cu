@@ -124,20 +124,20 @@ __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__
 
 // ---- products ---------------------------------------------------------------------------------------------------------------------
 // All products of all steps in one launch (what they are: ortho.cuh).  CTA = 10 warps: 0 takes tasks and loads, 1 MMA issuer and owner of tensor memory, 2-9 epilogue.
-// A task is a 128 x 128 tile of a result (or a piece of the k of one of A's); k in steps of 64.  A step's four tiles (hi and lo of both
-// operands) are 64 KB and feed twelve MMAs.  What a task adds to its product is brought by bulk copies too: read by the
+// A task is a 128 x 128 (or 128 x 64) tile of a result (or a piece of the k of one of A's); k in steps of 64.  A step's four tiles (hi and lo of
+// both operands) are 64 KB and feed eight MMAs: hi of A with hi and lo of B, side by side as 256 columns, and lo of A with hi of B.  What a task adds to its product is brought by bulk copies too: read by the
 // rows' own threads it took 7000 clocks of a task, 32 lines an instruction.  hi hi is summed apart from the other two products: the tensor core's sums drift towards zero
-// with their length, and those of small numbers do not notice.  For the same reason a sum over more than 1024 k is cut: the epilogue adds
+// with their length, and those of small numbers do not notice.  For the same reason a sum over more than 512 k is cut: the epilogue adds
 // the pieces up in registers, in fp32 with rounding.
 //
 // Order.  Tasks are numbered product by product, those of all matrices together, and taken one by one off a counter.  A task waits until its
 // matrix's earlier tasks are done, which a counter of the matrix tells.  What it waits for has a lower number, so it has been taken by a CTA
 // that runs: however few CTAs run at a time, one of them can go on.
 constexpr int kOThreads = 320;
-constexpr int kOSlots = 5;                                 // of two tiles: the hi, or the lo, of both operands of a step
+constexpr int kOSlots = 5;                                 // of two tiles: hi and lo of an operand of a step
 constexpr int kORing = 4;                                  // tasks between the warps
 constexpr uint32_t kOSlot = 2 * kOrthoTile;
-constexpr int kOSegment = 16;                              // steps of a sum
+constexpr int kOSegment = 8;                               // steps of a sum
 constexpr uint32_t kOStaging = 8 * 8192;                   // an epilogue warp's 32 rows x 64 columns, hi and lo, or fp32
 
 struct OrthoCtl {
@@ -160,7 +160,8 @@ struct OrthoTask {
     int op, x, q;                // which product; X's and Q's places before it
     bool update, last;           // of X's size; the last product
     int phase, copy;
-    int i, j;                    // row and column of the tile of 128 x 128
+    bool narrow;                 // 64 columns
+    int i, j;                    // row and column of the tile of 128 x 128 (or 64)
     int lower;                   // its number in the lower half
     int split;                   // piece of its k (A = X X^T)
     int from, to;                // steps of k
@@ -182,8 +183,10 @@ __device__ __forceinline__ OrthoTask ortho_task(const OrthoTable &tab, uint8_t *
     k.last = word & kOrthoLast;
     k.update = k.op >= kOrthoUpdate;
     const int op = k.op;
-    auto first = [op](const OrthoItem &i) {
-        return op >= kOrthoUpdate ? i.first_update : op == kOrthoGram ? i.first_gram : op == kOrthoBQ ? 2 * i.first_square : i.first_square;
+    k.narrow = tab.narrow && !k.update;
+    const int squares = (op == kOrthoBQ ? 2 : 1) << tab.narrow;
+    auto first = [op, squares](const OrthoItem &i) {
+        return op >= kOrthoUpdate ? i.first_update : op == kOrthoGram ? i.first_gram : squares * i.first_square;
     };
     k.it = &tab.item[find_item(tab, t, first)];
     const OrthoItem &it = *k.it;
@@ -197,7 +200,7 @@ __device__ __forceinline__ OrthoTask ortho_task(const OrthoTable &tab, uint8_t *
         k.i = local / it.ct;
         k.j = local - k.i * it.ct;
     } else {
-        const int per = ortho_lower(it.rt, it.ct);
+        const int per = ortho_lower(it.rt, it.ct) << tab.narrow;
         if (op == kOrthoGram) {
             const int whole = local / it.splits;
             k.split = local - whole * it.splits;
@@ -210,12 +213,13 @@ __device__ __forceinline__ OrthoTask ortho_task(const OrthoTable &tab, uint8_t *
         k.copy = local / per;
         local -= k.copy * per;
         k.lower = local;
-        // row i of the lower half starts at i (i + 1) / 2
-        int i = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
-        while (i * (i + 1) / 2 > local) --i;
-        while ((i + 1) * (i + 2) / 2 <= local) ++i;
+        // row i of the lower half starts at i (i + 1) / 2, twice that where tiles are narrow
+        const int pair = local >> tab.narrow;
+        int i = (int)((sqrtf(8.f * (float)pair + 1.f) - 1.f) * 0.5f);
+        while (i * (i + 1) / 2 > pair) --i;
+        while ((i + 1) * (i + 2) / 2 <= pair) ++i;
         k.i = i;
-        k.j = local - i * (i + 1) / 2;
+        k.j = local - ((i * (i + 1) / 2) << tab.narrow);
     }
     k.m = ws + it.base + k.copy * it.bytes;
     k.from = op == kOrthoGram ? k.split * it.per_split : 0;
@@ -224,9 +228,12 @@ __device__ __forceinline__ OrthoTask ortho_task(const OrthoTable &tab, uint8_t *
     return k;
 }
 
-__device__ __forceinline__ OrthoOperand ortho_operand(long long at, int tiles, int block, int turn, long long lo) {
+// block: of 128 rows, or, narrow, of 64.  turn: never, 0 (always) or -1: where the symmetric matrix's upper half begins
+__device__ __forceinline__ OrthoOperand ortho_operand(long long at, int tiles, int block, bool narrow, int turn, long long lo) {
     const long long pitch = 2LL * tiles * kOrthoTile;
-    return {at + block * pitch, at + 2LL * block * kOrthoTile, pitch, lo, turn};
+    if (!narrow) return {at + block * pitch, at + 2LL * block * kOrthoTile, pitch, lo, turn < 0 ? 2 * (block + 1) : turn};
+    return {at + (block >> 1) * pitch + (block & 1) * (kOrthoTile / 2), at + (long long)block * kOrthoTile, pitch, lo,
+            turn < 0 ? 2 * ((block >> 1) + 1) : turn};
 }
 __device__ __forceinline__ void ortho_operands(const OrthoTask &k, OrthoOperand &a, OrthoOperand &b) {
     const OrthoItem &it = *k.it;
@@ -235,22 +242,22 @@ __device__ __forceinline__ void ortho_operands(const OrthoTask &k, OrthoOperand 
     const bool tall = it.rows > it.cols;
     const long long x = place.x(k.x);
     if (k.op == kOrthoGram) {
-        a = ortho_operand(x, it.ct, k.i, tall ? 0 : never, place.x_bytes);
-        b = ortho_operand(x, it.ct, k.j, tall ? 0 : never, place.x_bytes);
+        a = ortho_operand(x, it.ct, k.i, false, tall ? 0 : never, place.x_bytes);
+        b = ortho_operand(x, it.ct, k.j, k.narrow, tall ? 0 : never, place.x_bytes);
     } else if (!k.update) {
         const bool square = k.op == kOrthoSquare || k.op == kOrthoSquareQ;
         const long long left = square ? place.a() : place.r();
         const long long right = square || k.op == kOrthoB ? place.a() : k.op == kOrthoA ? place.b() : place.q(k.q);
-        a = ortho_operand(left, d, k.i, 2 * (k.i + 1), place.s_bytes);
-        b = ortho_operand(right, d, k.j, 2 * (k.j + 1), place.s_bytes);
+        a = ortho_operand(left, d, k.i, false, -1, place.s_bytes);
+        b = ortho_operand(right, d, k.j, k.narrow, -1, place.s_bytes);
     } else {
         const long long by = k.op == kOrthoUpdate ? place.r() : place.q(k.q);
         if (tall) {
-            a = ortho_operand(x, it.ct, k.i, never, place.x_bytes);
-            b = ortho_operand(by, d, k.j, 2 * (k.j + 1), place.s_bytes);
+            a = ortho_operand(x, it.ct, k.i, false, never, place.x_bytes);
+            b = ortho_operand(by, d, k.j, false, -1, place.s_bytes);
         } else {
-            a = ortho_operand(by, d, k.i, 2 * (k.i + 1), place.s_bytes);
-            b = ortho_operand(x, it.ct, k.j, 0, place.x_bytes);
+            a = ortho_operand(by, d, k.i, false, -1, place.s_bytes);
+            b = ortho_operand(x, it.ct, k.j, false, 0, place.x_bytes);
         }
     }
 }
@@ -312,9 +319,9 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
             const int total = tab.first[tab.phases];
             uint32_t it = 0, n = 0;
             bool ok = true;
-            int next = atomicAdd(taken, 1);
             for (;; ++n) {
-                const int t = next;
+                // (taken when its loads can begin: a task held in advance waits here while other CTAs have nothing to do)
+                const int t = atomicAdd(taken, 1);
                 const uint32_t r = n % kORing;
                 ok = mbar_wait_bounded(&ctl->ring_empty[r], ((n / kORing) & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
@@ -323,7 +330,6 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                     mbar_arrive(&ctl->ring_full[r]);
                     break;
                 }
-                next = atomicAdd(taken, 1);
                 const OrthoTask k = ortho_task(tab, ws, t);
                 // the eight warps' shares of every earlier task of the matrix
                 const int need = 8 * (tab.lowers[k.phase] * ortho_lower(k.it->rt, k.it->ct) + tab.xs[k.phase] * k.it->rt * k.it->ct);
@@ -342,13 +348,13 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 mbar_arrive(&ctl->ring_full[r]);
                 OrthoOperand a, b;
                 ortho_operands(k, a, b);
-                auto bring = [&](const OrthoOperand &o, int s, long long lo, uint32_t to, uint32_t bar) {
+                auto bring = [&](const OrthoOperand &o, bool narrow, int s, long long lo, uint32_t to, uint32_t bar) {
                     if (s >= o.turn) {
                         const uint8_t *p = k.m + o.cols + (s >> 1) * o.pitch + (s & 1) * (kOrthoTile / 2) + lo;
                         bulk_load(to, p, kOrthoTile / 2, bar);
-                        bulk_load(to + kOrthoTile / 2, p + kOrthoTile, kOrthoTile / 2, bar);
+                        if (!narrow) bulk_load(to + kOrthoTile / 2, p + kOrthoTile, kOrthoTile / 2, bar);
                     } else {
-                        bulk_load(to, k.m + o.rows + (long long)s * kOrthoTile + lo, kOrthoTile, bar);
+                        bulk_load(to, k.m + o.rows + (long long)s * kOrthoTile + lo, narrow ? kOrthoTile / 2 : kOrthoTile, bar);
                     }
                 };
                 for (int s = k.from; ok && s < k.to; ++s)
@@ -358,9 +364,12 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                         ok = ok && mbar_wait_bounded(&ctl->empty[slot], ((it / kOSlots) & 1u) ^ 1u, abort_flag);
                         if (!ok) break;
                         const uint32_t bar = smem_u32(&ctl->full[slot]), dst = smem_u32(tiles) + slot * kOSlot;
-                        mbar_arrive_expect_tx(bar, kOSlot);
-                        bring(a, s, part ? a.lo : 0, dst, bar);
-                        bring(b, s, part ? b.lo : 0, dst + kOrthoTile, bar);
+                        const OrthoOperand &o = part ? b : a;
+                        const bool narrow = part && k.narrow;
+                        const uint32_t half = narrow ? kOrthoTile / 2 : kOrthoTile;
+                        mbar_arrive_expect_tx(bar, 2 * half);
+                        bring(o, narrow, s, 0, dst, bar);
+                        bring(o, narrow, s, o.lo, dst + half, bar);
                     }
                 if (!ok) break;
             }
@@ -395,21 +404,18 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                     const uint32_t slot = it % kOSlots, slot2 = (it + 1) % kOSlots;
                     ok = mbar_wait_bounded(&ctl->full[slot], (it / kOSlots) & 1u, abort_flag);
                     if (!ok) break;
-                    const bool a_mn = s >= a.turn, b_mn = s >= b.turn;
-                    const uint32_t idesc = idesc_h16_f32(128, 128, a_mn, b_mn, 1), base = smem_u32(tiles) + slot * kOSlot,
-                                   base2 = smem_u32(tiles) + slot2 * kOSlot;
-                    const uint32_t a_hi = smem_desc_lo(base, a_mn ? 8192 : 16), b_hi = smem_desc_lo(base + kOrthoTile, b_mn ? 8192 : 16);
-                    const uint32_t a_lo = smem_desc_lo(base2, a_mn ? 8192 : 16);
-                    const uint32_t b_lo = smem_desc_lo(base2 + kOrthoTile, b_mn ? 8192 : 16);
-                    const uint32_t sa = a_mn ? 128u : 2u, sb = b_mn ? 128u : 2u;
-#pragma unroll
-                    for (uint32_t q = 0; q < 4; ++q) umma_bf16_ss_sel(d, a_hi + q * sa, hi, b_hi + q * sb, hi, idesc, first + q);
                     ok = mbar_wait_bounded(&ctl->full[slot2], ((it + 1) / kOSlots) & 1u, abort_flag);
                     if (!ok) break;
+                    const bool a_mn = s >= a.turn, b_mn = s >= b.turn;
+                    const int n = k.narrow ? 64 : 128;
+                    const uint32_t both = idesc_h16_f32(128, 2 * n, a_mn, b_mn, 1), one = idesc_h16_f32(128, n, a_mn, b_mn, 1);
+                    const uint32_t a_hi = smem_desc_lo(smem_u32(tiles) + slot * kOSlot, a_mn ? 8192 : 16), a_lo = a_hi + (kOrthoTile >> 4);
+                    const uint32_t b_hi = smem_desc_lo(smem_u32(tiles) + slot2 * kOSlot, b_mn ? 8192 : 16);
+                    const uint32_t sa = a_mn ? 128u : 2u, sb = b_mn ? 128u : 2u;
 #pragma unroll
                     for (uint32_t q = 0; q < 4; ++q) {
-                        umma_bf16_ss_sel(d + 128, a_hi + q * sa, hi, b_lo + q * sb, hi, idesc, first + q);
-                        umma_bf16_ss_halves<true>(d + 128, a_lo + q * sa, hi, b_hi + q * sb, hi, idesc);
+                        umma_bf16_ss_sel(d, a_hi + q * sa, hi, b_hi + q * sb, hi, both, first + q);
+                        umma_bf16_ss_halves<true>(d + n, a_lo + q * sa, hi, b_hi + q * sb, hi, one);
                     }
                     umma_commit(&ctl->empty[slot]);
                     umma_commit(&ctl->empty[slot2]);
@@ -437,9 +443,19 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
             const OrthoTask k = ortho_task(tab, ws, t);
             const OrthoItem &it = *k.it;
             const OrthoPlace place(it.rt, it.ct);
+            const int segments = (k.to - k.from + kOSegment - 1) / kOSegment;
+            if (k.narrow && half) {                             // (64 columns are four warps' work)
+                for (int g = 0; g < segments; ++g, ++acc_it) {
+                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->acc_full[acc_it & 1u], (acc_it >> 1) & 1u, abort_flag));
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive(&ctl->acc_empty[acc_it & 1u]);
+                }
+                if (!ok) break;
+                continue;
+            }
             // numbers are 2^10 times what they stand for (Q's 2^8), sums of products 2^20 times (2^18)
             const long long x_at = ((long long)k.i * 2 * it.ct + 2 * k.j + half) * kOrthoTile;
-            const long long s_at = ((long long)k.i * 2 * min(it.rt, it.ct) + 2 * k.j + half) * kOrthoTile;
+            const long long s_at = ((long long)k.i * 2 * min(it.rt, it.ct) + (k.narrow ? k.j : 2 * k.j + half)) * kOrthoTile;
             const long long lo_at = k.update ? place.x_bytes : place.s_bytes;
             long long old_at = -1, to_at;
             float v[64], f_old = kOrthoCoefA, f_new = 1.f / kOrthoScale;
@@ -481,7 +497,6 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                     for (int e = 0; e < 4; ++e) { v[8 * c + 2 * e] = f_old * o[e].x; v[8 * c + 2 * e + 1] = f_old * o[e].y; }
                 }
             }
-            const int segments = (k.to - k.from + kOSegment - 1) / kOSegment;
             for (int g = 0; g < segments; ++g, ++acc_it) {
                 const uint32_t acc = acc_it & 1u;
                 ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->acc_full[acc], (acc_it >> 1) & 1u, abort_flag));
@@ -492,7 +507,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 for (int h = 0; h < 2; ++h) {
                     uint32_t p[32], q[32];
                     tmem_ld_32x32(from + h * 32, p);
-                    tmem_ld_32x32(from + 128 + h * 32, q);
+                    tmem_ld_32x32(from + (k.narrow ? 64 : 128) + h * 32, q);
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[h * 32 + i] = fmaf(f_new, __uint_as_float(p[i]) + __uint_as_float(q[i]), v[h * 32 + i]);
@@ -505,23 +520,25 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
             if (k.op == kOrthoGram && it.splits > 1) {
                 // The piece goes to memory, [4 columns][row] by chunks of 16 bytes; the warp whose piece is the last of this share of the
                 // tile adds all of them up, in their order.
-                float4 *part = (float4 *)(k.m + place.parts(it.wide) + ((long long)k.lower * it.splits + k.split) * 65536) + half * 2048 + row;
+                const int part_bytes = k.narrow ? 32768 : 65536;
+                float4 *part = (float4 *)(k.m + place.parts(it.wide) + ((long long)k.lower * it.splits + k.split) * part_bytes) + half * 2048 + row;
 #pragma unroll
                 for (int c = 0; c < 16; ++c) __stcg(part + c * 128, make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]));
                 __threadfence();
                 __syncwarp();
                 int ticket = 0;
-                if (lane == 0) ticket = atomicAdd(tickets + 8 * (it.first_square + k.copy * ortho_lower(it.rt, it.ct) + k.lower) + (warp - 2), 1);
+                if (lane == 0)
+                    ticket = atomicAdd(tickets + 8 * (it.first_square + k.copy * ortho_lower(it.rt, it.ct)) + (k.narrow ? 4 : 8) * k.lower + (warp - 2), 1);
                 ticket = __shfl_sync(0xffffffffu, ticket, 0);
                 if ((ticket + 1) % it.splits != 0) continue;
                 __threadfence();
-                part -= (long long)k.split * 4096;
+                part -= (long long)k.split * (part_bytes / 16);
 #pragma unroll
                 for (int i = 0; i < 64; ++i) v[i] = 0.f;
                 for (int p = 0; p < it.splits; ++p) {
                     float4 f[16];
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) f[c] = __ldcg(part + (long long)p * 4096 + c * 128);
+                    for (int c = 0; c < 16; ++c) f[c] = __ldcg(part + (long long)p * (part_bytes / 16) + c * 128);
 #pragma unroll
                     for (int c = 0; c < 16; ++c) { v[4 * c] += f[c].x; v[4 * c + 1] += f[c].y; v[4 * c + 2] += f[c].z; v[4 * c + 3] += f[c].w; }
                 }
@@ -553,7 +570,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 };
                 put(k.m + to_at + quarter * 4096);
                 if (k.op == kOrthoSquareQ) {
-                    const int diagonal = k.i == k.j ? (int)row - half * 64 : -1;
+                    const int diagonal = (k.narrow ? k.j >> 1 : k.j) == k.i ? (int)row - (k.narrow ? k.j & 1 : half) * 64 : -1;
 #pragma unroll
                     for (int i = 0; i < 64; ++i) v[i] = v[i] * (kOrthoQScale / kOrthoScale) + (i == diagonal ? kOrthoCoefA * kOrthoQScale : 0.f);
                     if (lane == 0) tma_store_wait_read<0>();
@@ -637,7 +654,7 @@ static void ortho_phases(OrthoTable &t, bool wide) {
         t.lowers[n] = (uint16_t)lowers;
         t.xs[n] = (uint16_t)xs;
         t.first[n++] = at;
-        at += update ? t.updates : op == kOrthoGram ? t.grams : op == kOrthoBQ ? 2 * t.squares : t.squares;
+        at += update ? t.updates : op == kOrthoGram ? t.grams : t.squares << (t.narrow + (op == kOrthoBQ));
         if (update) { ++xs; x ^= 1; } else lowers += op == kOrthoBQ ? 2 : 1;
     };
     const int stages = wide ? (t.steps + 2) / 3 : t.steps;
@@ -683,18 +700,22 @@ size_t ortho_plan(OrthoTable &t, bool wide) {
         t.updates += it.count * it.rt * it.ct;
         t.matrices += it.count;
     }
-    // Where A has fewer tiles than there are SMs, its sums are cut.  A step of 64 takes 0.4 us, adding up a piece about 1 us.
+    // Where A's tiles leave half the SMs idle, they are halved: a step's copies, which come at some 52 bytes a clock, are what a product waits for
+    // (a step of 128 x 128 takes 1250 clocks, of 128 x 64 930).  Where they still leave SMs idle, A's sums are cut: a step takes 0.4 us, adding
+    // up a piece 0.7 us.
+    t.narrow = 2 * t.squares <= sms;
+    const int tiles_of_a = t.squares << t.narrow;
     for (int i = 0; i < t.items; ++i) {
         OrthoItem &it = t.item[i];
         const int steps = ((it.rows > it.cols ? it.rows : it.cols) + 63) / 64;
         int pieces = 1;
         while ((pieces + 1) * (pieces + 1) * 5 <= steps * 2) ++pieces;
-        if (pieces > sms / t.squares) pieces = sms / t.squares;
+        if (pieces > sms / tiles_of_a) pieces = sms / tiles_of_a;
         if (pieces < 1) pieces = 1;
         it.per_split = (steps + pieces - 1) / pieces;
         it.splits = (steps + it.per_split - 1) / it.per_split;
         it.first_gram = t.grams;
-        t.grams += it.count * ortho_lower(it.rt, it.ct) * it.splits;
+        t.grams += it.count * (ortho_lower(it.rt, it.ct) << t.narrow) * it.splits;
     }
     ortho_phases(t, wide);
     long long end = (long long)align_up((size_t)ortho_words(t) * sizeof(int), 1024);
