@@ -1,4 +1,5 @@
-"""Whole-backbone replay: forward + backward of a ResNet-50-shaped chain of ConvBN blocks in Tune, Eval or Deploy mode.
+"""Whole-backbone replay: forward + backward of a ResNet-50-shaped chain of ConvBN blocks in Tune, Eval or Deploy mode, or with group norms
+in the BatchNorms' place.
 
 This is the shape of the paper's efficiency experiment (Sec. 3.4, Fig. 3, App. D: time per iteration and peak
 memory of a ResNet-50 under the three modes) with synthetic weights and inputs: the 53 ConvBN blocks of the
@@ -11,6 +12,10 @@ ReLU's output; with `packed`, Tune mode, in 8 bits), the mode's extra state (Tun
 every block; Deploy: nothing), and nothing else.  Buffers are allocated with torch inside the pass and dropped
 as soon as the backward pass has used them, so `torch.cuda.max_memory_allocated` sees the peak a training
 framework would see.
+
+Mode "group" is the chain that a batch too small for statistics is trained with: the plain convolutions (the Deploy-mode calls on the
+weights as they are), each followed by a group norm that has its ReLU with it.  It keeps the normalisations' inputs, as Eval mode does, and a mean and a
+deviation per group.  `optimiser` gives the step that takes the gradients of a pass to new weights.
 
 The max-pool between the stem and the first stage is not a ConvBN block and has no counterpart in the library:
 the first stage is fed with a synthetic tensor of the pooled shape and the stem's backward pass with a synthetic
@@ -25,6 +30,7 @@ import torch
 from . import convbn as C
 from . import inputs as I
 from .harness import Block, packed_buffers
+from .muon import Muon
 
 
 @dataclass
@@ -52,7 +58,7 @@ def resnet50_plan(size: int = 224) -> Tuple[Optional[Tuple[int, int]], List[Bott
 class _Layer:
     """One ConvBN block of the chain: parameters, gradients, the calls of the chosen mode."""
 
-    def __init__(self, name, n, c_in, hw, c_out, k, stride, mode, device, seed, dtype="bf16", packed=False):
+    def __init__(self, name, n, c_in, hw, c_out, k, stride, mode, device, seed, dtype="bf16", packed=False, groups=32):
         spec = I.LayerSpec(name, n, c_in, hw[0], hw[1], c_out, k, k, stride=stride, pad=k // 2, dtype=dtype)
         self.blk = Block(spec, device=device, modes=(mode,), allocate="params")
         self.blk.randomize_params(seed)
@@ -69,6 +75,15 @@ class _Layer:
             b.dw_fused = torch.empty_like(b.dw)
             b.db_fused = torch.empty(spec.c_out, dtype=torch.float32, device=device)
             b.deploy_prepare()
+        if mode == "group":
+            b = self.blk
+            b.w_fused, b.dw_fused = b.w, b.dw                       # (Deploy mode's convolution, on weights nothing is folded into)
+            b.b_fused = torch.zeros(c_out, dtype=torch.float32, device=device)
+            b.db_fused = torch.empty(c_out, dtype=torch.float32, device=device)
+            self.norms = {act: C.NormDesc.make(n, c_out, b.h_out, b.w_out, groups, act=act, dtype=C.F16 if dtype == "f16" else C.BF16, eps=spec.eps)
+                          for act in (C.ACT_NONE, C.ACT_RELU)}
+            with torch.cuda.device(b.device):
+                self.norm_bytes = C.convbn_group_norm_workspace_bytes(self.norms[C.ACT_RELU])
         self.out_elems = n * c_out * self.blk.h_out * self.blk.w_out
         self.in_elems = n * c_in * hw[0] * hw[1]
 
@@ -84,6 +99,17 @@ class _Layer:
                                    self.fwd_bytes)
             return z
         b.z = z
+        if self.mode == "group":
+            y = b.z = torch.empty_like(z)
+            b.with_scratch(C.PHASE_DEPLOY_FWD, b.deploy_fwd)
+            b.z = None
+            norm = self.norms[C.ACT_RELU if relu and add is None else C.ACT_NONE]
+            kept = torch.empty(C.convbn_group_norm_saved_bytes(norm) // 4, dtype=torch.float32, device=b.device)
+            C.convbn_group_norm_fwd(norm, y, b.gamma, b.beta, z, kept, torch.empty(self.norm_bytes, dtype=torch.uint8, device=b.device))
+            self.kept = (norm, y, kept)
+            if add is not None:
+                (C.convbn_add_relu if relu else C.convbn_add)(z, add, z)
+            return z
         if self.mode == "eval":
             b.y_saved = torch.empty(C.convbn_saved_bytes(b.desc, C.MODE_EVAL), dtype=torch.uint8, device=b.device)
             b.with_scratch(C.PHASE_EVAL_FWD, b.eval_fwd)
@@ -117,6 +143,14 @@ class _Layer:
             if held is not None:
                 held.append((x, dz))
             return dx
+        if self.mode == "group":
+            # (a ReLU that belongs to a norm is that norm's: only where branches have met is there one of its own, which asks with `add`)
+            relu_mask = relu_mask and add is not None
+            (norm, y, kept), self.kept = self.kept, None
+            dy = torch.empty_like(y)
+            C.convbn_group_norm_bwd(norm, dz, y, b.gamma, b.beta, kept, dy, b.dgamma, b.dbeta,
+                                    torch.empty(self.norm_bytes, dtype=torch.uint8, device=b.device))
+            dz = dy
         b.dz, b.dx, b.x = dz, dx, x
         if self.mode == "eval":
             b.with_scratch(C.PHASE_EVAL_BWD, b.eval_bwd)
@@ -140,7 +174,7 @@ class BackboneReplay:
                  device="cuda:0", seed: int = 0, async_param_grads: bool = False, dtype: str = "bf16", packed: bool = False):
         """packed (Tune mode): the inputs of the bottlenecks' convolutions are kept for the backward pass in 8 bits
         (C.convbn_pack); their ReLUs decide as before, parameter gradients see the restored values."""
-        assert mode in ("tune", "eval", "deploy") and dtype in ("bf16", "f16") and (mode == "tune" or not packed)
+        assert mode in ("tune", "eval", "deploy", "group") and dtype in ("bf16", "f16") and (mode == "tune" or not packed)
         self.packed = packed
         self.async_param_grads = async_param_grads
         self.mode, self.batch, self.device = mode, batch, torch.device(device)
@@ -281,6 +315,12 @@ class BackboneReplay:
             if keep is not None:
                 keep["d_image"] = gi.clone()
         return g
+
+    def optimiser(self, **params) -> Muon:
+        """The optimiser over all convolutions' weights and the gradients that forward_backward leaves; step() after each pass.  (Deploy mode's
+        gradients belong to folded weights.)"""
+        assert self.mode != "deploy"
+        return Muon([(l.blk.w.view(l.blk.spec.c_out, -1), l.blk.dw) for l in self.layers], **params)
 
     # ---- measurements ------------------------------------------------------------------------------------
     def measure(self, iters: int = 5, warmup: int = 2):
