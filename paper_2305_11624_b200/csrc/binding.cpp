@@ -217,7 +217,9 @@ long long current_device() {
 // the current GPU; None for anything else, which convbn.py then looks at.  (The checks in Python took 5 us of a call of 9.)
 // kinds: of the arguments behind the descriptor: a activation, v a vector of c, s saved.
 bool norm_argument(PyObject *o, char kind, const convbn_group_norm_desc *d, long long device) {
-    const long long want = kind == 'a' ? (long long)d->n * d->c * d->h * d->w : kind == 'v' ? d->c : 2LL * d->n * d->groups;
+    const __int128 all = (__int128)d->n * d->c * ((__int128)d->h * d->w);
+    if (all > (1LL << 40)) return false;                 // (the library refuses it)
+    const long long want = kind == 'a' ? (long long)all : kind == 'v' ? d->c : 2LL * d->n * d->groups;
     if (storage_type(o) != (kind == 'a' ? d->dtype : CONVBN_F32) || number(o, s_numel, true) != want || !contiguous(o) ||
         number(o, s_get_device, true) != device)
         return false;

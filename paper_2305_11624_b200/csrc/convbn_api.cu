@@ -1851,39 +1851,33 @@ int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols
     return CONVBN_OK;
 }
 
-// A launch's layers: from `from` on, those whose steps go over X (wide = false) or over m x m matrices, as many as a launch takes and an int
-// counts the tasks of; their numbers in `taken`.  Returns where the next launch of the kind begins.  Small layers go with the wide ones if
-// there are any: beside those they cost nothing, by themselves a launch's latency.
-static bool muon_wide(const convbn_muon_layer &l, bool any) { return ortho_wide(l.rows, l.cols) || (any && std::min(l.rows, l.cols) <= 256); }
-static int muon_launch(const convbn_muon_layer *layers, int count, int from, bool wide, bool any, OrthoTable *t, int *taken) {
+// A launch's layers: from `from` on as many as it takes and an int counts the tasks of.  Returns the next launch's first.
+static int muon_launch(const convbn_muon_layer *layers, int count, int from, OrthoTable *t) {
     long long tiles = 0;
     int i = from;
     for (t->items = 0; i < count && t->items < kOrthoItems; ++i) {
-        if (muon_wide(layers[i], any) != wide) continue;
         tiles += (((long long)layers[i].rows + 127) / 128) * (((long long)layers[i].cols + 127) / 128) * 2;
         if (tiles >= (1LL << 23) && t->items > 0) break;
-        OrthoItem &it = t->item[t->items];
+        OrthoItem &it = t->item[t->items++];
         it.rows = layers[i].rows;
         it.cols = layers[i].cols;
         it.count = 1;
-        taken[t->items++] = i;
     }
     return i;
 }
-// f(table, its workspace's bytes, its layers' numbers) for every launch
-static int muon_launches(const convbn_muon_layer *layers, int count, int steps, const std::function<int(OrthoTable &, size_t, const int *)> &f) {
-    bool any = false;
-    for (int i = 0; i < count; ++i) any |= ortho_wide(layers[i].rows, layers[i].cols);
-    for (int wide = 1; wide >= 0; --wide)
-        for (int from = 0; from < count;) {
-            OrthoTable t = {};
-            int taken[kOrthoItems];
-            from = muon_launch(layers, count, from, wide, any, &t, taken);
-            if (t.items == 0) break;
-            t.steps = steps;
-            const size_t bytes = ortho_plan(t, wide);
-            CK(f(t, bytes, taken));
-        }
+// f(table, its workspace's bytes, its first layer) for every launch.  Steps go over m x m matrices for all layers if that pays for one: it is as
+// much work for square ones.
+static int muon_launches(const convbn_muon_layer *layers, int count, int steps, const std::function<int(OrthoTable &, size_t, int)> &f) {
+    bool wide = false;
+    for (int i = 0; i < count; ++i) wide |= ortho_wide(layers[i].rows, layers[i].cols);
+    for (int from = 0; from < count;) {
+        OrthoTable t = {};
+        const int next = muon_launch(layers, count, from, &t);
+        t.steps = steps;
+        const size_t bytes = ortho_plan(t, wide);
+        CK(f(t, bytes, from));
+        from = next;
+    }
     return CONVBN_OK;
 }
 static bool muon_sizes(const convbn_muon_layer *layers, int count) {
@@ -1896,7 +1890,7 @@ static bool muon_sizes(const convbn_muon_layer *layers, int count) {
 size_t convbn_muon_workspace_bytes(const convbn_muon_layer *layers, int count) {
     if (!muon_sizes(layers, count)) return 0;
     size_t most = 0;
-    muon_launches(layers, count, 1, [&](OrthoTable &, size_t bytes, const int *) { most = std::max(most, bytes); return (int)CONVBN_OK; });
+    muon_launches(layers, count, 1, [&](OrthoTable &, size_t bytes, int) { most = std::max(most, bytes); return (int)CONVBN_OK; });
     return most;
 }
 
@@ -1913,10 +1907,10 @@ int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, cons
             !aligned(layers[i].weight, elem_size(dtype)))
             return CONVBN_EALIGN;
     // (before anything is launched)
-    CK(muon_launches(layers, count, params->steps, [&](OrthoTable &, size_t bytes, const int *) { return ortho_room(bytes, workspace, workspace_bytes); }));
+    CK(muon_launches(layers, count, params->steps, [&](OrthoTable &, size_t bytes, int) { return ortho_room(bytes, workspace, workspace_bytes); }));
     cudaStream_t st = (cudaStream_t)stream;
     t_prof_phase = "muon";
-    return muon_launches(layers, count, params->steps, [&](OrthoTable &t, size_t, const int *taken) -> int {
+    return muon_launches(layers, count, params->steps, [&](OrthoTable &t, size_t, int first) -> int {
         t.dtype = dtype;
         t.muon = 1;
         t.nesterov = params->nesterov != 0;
@@ -1924,7 +1918,7 @@ int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, cons
         t.keep = (float)(1. - params->lr * params->weight_decay);
         t.eps = params->eps;
         for (int i = 0; i < t.items; ++i) {
-            const convbn_muon_layer &l = layers[taken[i]];
+            const convbn_muon_layer &l = layers[first + i];
             OrthoItem &it = t.item[i];
             it.g = l.grad;
             it.momentum = l.momentum;

@@ -248,7 +248,7 @@ __device__ __forceinline__ NormVec<T, V> kept_vec(uint32_t addr) {
 // at a time, 48 KB a block, does not depend on how long a pixel takes; with a batch of loads in registers between one wait and the next the
 // passes read 2.6 to 3.5 TB/s.
 constexpr int kRing = 12, kBlocks1 = 3, kBlocks2 = 2;        // places; blocks of an SM, with one tensor and with two
-template <class T, int V, int NT>
+template <class T, int V, int NT, bool COPIES = (V * sizeof(T) > 2)>
 struct Ring {
     static constexpr int kPlaces = kRing / NT, kBatch = 2, kBatches = kPlaces / kBatch;
     static_assert(kBatches * kBatch == kPlaces, "whole batches");
@@ -289,6 +289,31 @@ struct Ring {
             }
         }
         copies_wait<0>();
+    }
+};
+// The same for accesses of two bytes, which no asynchronous copy has: batches of loads in registers.
+template <class T, int V, int NT>
+struct Ring<T, V, NT, false> {
+    static constexpr int kBatch = 16 / NT;
+    uint32_t slot;
+    long long pitch;
+    int mine;
+    const T *from[NT];
+    __device__ __forceinline__ void start() {}
+    template <class F>
+    __device__ __forceinline__ void run(F &&f) {
+        for (int left = mine; left > 0; left -= kBatch) {
+            NormVec<T, V> v[kBatch][NT];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) v[i][t].load(from[t] + (i < left ? i : 0) * pitch);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (i < left) f(v[i]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) from[t] += kBatch * pitch;
+        }
     }
 };
 constexpr int kRingBytes = kRing * kThreads * 16;
@@ -799,10 +824,10 @@ bool kept_plan(GroupNormShape &s, int es, bool backward) {
         const int groups = slab_groups(s, es, threads);
         if (!groups) continue;
         set_slab(s, groups, threads);
-        if (s.cols > threads || s.pixels > (long long)s.ty * most) continue;
-        const long long units = (long long)(s.g / s.slab_g) * s.n;
-        long long splits = 1;                            // (few slabs: a cluster each)
-        if (units * 2 <= sms) splits = std::max(1LL, std::min(std::min(sms / units, 8LL), s.pixels / s.ty));
+        // (few slabs: a cluster each)
+        const long long units = (long long)(s.g / s.slab_g) * s.n, room = units * 2 <= sms ? std::min(sms / units, (long long)kMaxCluster) : 1;
+        if (s.cols > threads || s.pixels > room * s.ty * most) continue;
+        const long long splits = std::max(1LL, std::min(room, s.pixels / s.ty));
         s.splits = s.cluster = (int)splits;
         s.rows = (s.pixels + splits - 1) / splits;
         s.keep = (int)((s.rows + s.ty - 1) / s.ty);

@@ -103,27 +103,54 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     const uint32_t tmem = ctl->tmem_base;
 
     // ---- X = G / (|G| + eps); muon: the momentum's step on the way ----
-    auto update = [&](long long at) -> float {
-        if (tab.muon) {
-            const float v = it.momentum[at];
-            return tab.nesterov ? fmaf(tab.momentum, v, ((const float *)it.g)[at]) : v;
-        }
-        return to_f32(((const T *)it.g)[at]);
-    };
-    const int fast = tall ? m : cols, slow = tall ? cols : m;           // lines of the block's part as it lies in memory
+    // (the block's tiles: zeros beyond the matrix)
+    for (int i = threadIdx.x; i < tiles * (int)(kSTile / 16); i += kSThreads) ((uint4 *)x)[i] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+    // Once from memory, sixteen loads of a thread on their way: the sum of squares, and the number's two halves where hi and lo of it will be.
+    // (Line by line, and again for the scaling, this took two thirds of 189 x 37's 70 us.)
+    const int fast = tall ? m : cols, count = m * cols;              // (at most 2^15)
+    const float per_line = cols > 0 ? 1.f / (float)fast : 0.f;
     double s = 0.;
-    for (int b = warp; b < slow; b += kSThreads / 32)
-        for (int a = lane; a < fast; a += 32) {
-            const long long at = tall ? place(a, b) : place(b, a);
-            if (tab.muon) it.momentum[at] = fmaf(tab.momentum, it.momentum[at], ((const float *)it.g)[at]);
-            const double u = update(at);
-            s += u * u;
+    auto spot = [&](int i, int j) { return x + (size_t)(j >> 6) * kSTile + ortho_chunk(i, (j & 63) >> 3) + (j & 7) * 2; };
+    for (int e0 = threadIdx.x; e0 < count; e0 += 16 * kSThreads) {
+        float u[16];
+        long long at[16];
+        int where[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int e = min(e0 + k * kSThreads, count - 1), line = __float2int_rz(((float)e + 0.5f) * per_line), a = e - line * fast;
+            const int i = tall ? a : line, j = tall ? line : a;
+            at[k] = place(i, j);
+            where[k] = (int)(spot(i, j) - x);
         }
+        if (tab.muon) {
+            float v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) { u[k] = ((const float *)it.g)[at[k]]; v[k] = it.momentum[at[k]]; }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                v[k] = fmaf(tab.momentum, v[k], u[k]);
+                u[k] = tab.nesterov ? fmaf(tab.momentum, v[k], u[k]) : v[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (e0 + k * kSThreads < count) it.momentum[at[k]] = v[k];
+        } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) u[k] = to_f32(((const T *)it.g)[at[k]]);
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            if (e0 + k * kSThreads >= count) break;
+            s += (double)u[k] * (double)u[k];
+            const uint32_t bits = __float_as_uint(u[k]);
+            *(uint16_t *)(x + where[k]) = (uint16_t)(bits >> 16);
+            *(uint16_t *)(x + where[k] + kOrthoTile) = (uint16_t)bits;
+        }
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == 0) ctl->part[warp] = s;
-    // (the block's tiles: zeros beyond the matrix)
-    for (int i = threadIdx.x; i < tiles * (int)(kSTile / 16); i += kSThreads) ((uint4 *)x)[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
     if (threadIdx.x == 0) {
         s = ctl->part[0];
@@ -135,15 +162,22 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     if (blocks > 1) for (int b = 0; b < blocks; ++b) s += ld_cluster_f64(cluster_addr(&ctl->sum, b));
     else s = ctl->sum;
     const double inv = (double)kOrthoScale / (sqrt(s) + tab.eps);
-    for (int b = warp; b < slow; b += kSThreads / 32)
-        for (int a = lane; a < fast; a += 32) {
-            const int i = tall ? a : b, j = tall ? b : a;
-            const float v = (float)(update(place(i, j)) * inv);
-            const __half h = __float2half_rn(v);
-            uint8_t *to = x + (size_t)(j >> 6) * kSTile + ortho_chunk(i, (j & 63) >> 3) + (j & 7) * 2;
-            *(__half *)to = h;
-            *(__half *)(to + kOrthoTile) = __float2half_rn(v - __half2float(h));
+    // (rows beyond the matrix are zeros)
+    for (int c = threadIdx.x; c < tiles * m16 * 8; c += kSThreads) {
+        uint8_t *to = x + (size_t)(c / (m16 * 8)) * kSTile + c % (m16 * 8) * 16;
+        const uint4 top = *(const uint4 *)to, low = *(const uint4 *)(to + kOrthoTile);
+        const uint32_t a[4] = {top.x, top.y, top.z, top.w}, b[4] = {low.x, low.y, low.z, low.w};
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = (float)((double)__uint_as_float(a[e] << 16 | (b[e] & 0xFFFFu)) * inv);
+            v[2 * e + 1] = (float)((double)__uint_as_float((a[e] & 0xFFFF0000u) | b[e] >> 16) * inv);
         }
+        uint4 h, l;
+        to_pairs(v, h, l);
+        *(uint4 *)to = h;
+        *(uint4 *)(to + kOrthoTile) = l;
+    }
 
     uint32_t ph = 0;
     const uint32_t x_at = smem_u32(x), ap_at = smem_u32(ap), hi_word = smem_desc_hi_sw128(1024);
@@ -205,10 +239,11 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
                     }
                 }
         } else {
-            // part by part to the block that has the row: [block][its rows][128] in fp32, where P was
+            // part by part to the block that has the row: [block][4 columns][its rows] in fp32, where P was (rows side by side, as a warp has
+            // them: with a row's columns side by side the sums' round took 7 us)
             const int share = 128 / blocks;                           // (blocks: a power of two)
             if (rows_here) {
-                const uint32_t to = cluster_addr(ap, row / share) + ((rank * share + row % share) * 128) * 4;
+                const uint32_t to = cluster_addr(ap, row / share) + (rank * 32 * share + row % share) * 16;
                 for (int c = half * 32; c < m16; c += 64) {
                     float v[32];
                     if (n16 > 0) sums(c, v);
@@ -218,7 +253,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
                     }
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
-                        st_cluster_v4(to + (c + 4 * q) * 4, make_uint4(__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]),
+                        st_cluster_v4(to + (c / 4 + q) * share * 16, make_uint4(__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]),
                                                                      __float_as_uint(v[4 * q + 3])));
                 }
             }
@@ -231,13 +266,13 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (k >= sets) break;
-                const int idx = threadIdx.x + k * kSThreads, r = idx / per_row, c = idx % per_row * 8;
+                const int idx = threadIdx.x + k * kSThreads, r = idx % share, c = idx / share * 8;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[k][e] = 0.f;
                 if (c < m16)
                     for (int b = 0; b < blocks; ++b) {
-                        const float4 *f = (const float4 *)(ap + ((size_t)(b * share + r) * 128 + c) * 4);
-                        const float4 f0 = f[0], f1 = f[1];
+                        const float4 *f = (const float4 *)ap + (b * 32 + c / 4) * share + r;
+                        const float4 f0 = f[0], f1 = f[share];
                         w[k][0] += f0.x; w[k][1] += f0.y; w[k][2] += f0.z; w[k][3] += f0.w;
                         w[k][4] += f1.x; w[k][5] += f1.y; w[k][6] += f1.z; w[k][7] += f1.w;
                     }
@@ -246,7 +281,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (k >= sets) break;
-                const int idx = threadIdx.x + k * kSThreads, r = rank * share + idx / per_row, c = idx % per_row * 8;
+                const int idx = threadIdx.x + k * kSThreads, r = rank * share + idx % share, c = idx / share * 8;
                 if (c >= m16 || r >= m16) continue;
                 float f[8];
 #pragma unroll
@@ -384,7 +419,8 @@ bool small_shape(const OrthoTable &t, SmallShape *s) {
         longest = std::max(longest, n);
     }
     s->blocks = 1;
-    while (s->blocks < kSMaxCluster && longest > s->blocks * 128) s->blocks *= 2;
+    // (few wide blocks: 66 x 150 by two blocks of 128 columns took twice as long as by one)
+    while (longest > s->blocks * kSMaxWidth) s->blocks *= 2;
     s->width = ((longest + s->blocks - 1) / s->blocks + 63) / 64 * 64;
     return true;
 }
