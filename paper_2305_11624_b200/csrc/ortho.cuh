@@ -22,7 +22,6 @@ namespace convbn {
 constexpr uint32_t kOrthoTile = 16384;
 constexpr float kOrthoScale = 1024.f;
 constexpr float kOrthoCoefA = 3.4445f, kOrthoCoefB = -4.7750f, kOrthoCoefC = 2.0315f;
-constexpr int kOrthoChunk = 16384;                // elements that a block sums the squares of
 
 // Offset of the 16-byte chunk of 8 columns `chunk` of row `row` in a tile.
 __host__ __device__ __forceinline__ uint32_t ortho_chunk(uint32_t row, uint32_t chunk) { return row * 128u + ((chunk ^ (row & 7u)) << 4); }
