@@ -1841,6 +1841,7 @@ int convbn_orthogonalise(int dtype, const void *g, void *out, int rows, int cols
     CK(ortho_room(convbn_orthogonalise_workspace_bytes(rows, cols, count), workspace, workspace_bytes));
     OrthoTable t = {};
     ortho_stack(t, dtype, rows, cols, count, steps);
+    t.segment_mask = dtype == CONVBN_F32 ? 3 : 15;
     t.dtype = dtype;
     t.eps = eps;
     t.item[0].g = g;
@@ -1911,6 +1912,7 @@ int convbn_muon_step(const convbn_muon_layer *layers, int count, int dtype, cons
     cudaStream_t st = (cudaStream_t)stream;
     t_prof_phase = "muon";
     return muon_launches(layers, count, params->steps, [&](OrthoTable &t, size_t, int first) -> int {
+        t.segment_mask = 15;
         t.dtype = dtype;
         t.muon = 1;
         t.nesterov = params->nesterov != 0;

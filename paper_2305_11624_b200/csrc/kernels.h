@@ -422,6 +422,7 @@ constexpr int kOrthoPhases = 256;
 struct OrthoTable {
     int items, steps;
     int sums, tiles, grams, squares, updates, matrices;       // in all
+    int segment_mask;                       // steps of 64 k of a sum in tensor memory (a power of two), less one
     int narrow;                             // m x m products in tiles of 128 x 64, not 128 x 128
     int phases;                             // the products of all steps, one after the other ...
     uint16_t op[kOrthoPhases];              // ... what each is (ortho.cuh) ...

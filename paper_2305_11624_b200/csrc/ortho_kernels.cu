@@ -186,8 +186,9 @@ __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__
 // A task is a 128 x 128 (or 128 x 64) tile of a result (or a piece of the k of one of A's); k in steps of 64.  A step's four tiles (hi and lo of
 // both operands) are 64 KB and feed eight MMAs: hi of A with hi and lo of B, side by side as 256 columns, and lo of A with hi of B.  What a task adds to its product is brought by bulk copies too: read by the
 // rows' own threads it took 7000 clocks of a task, 32 lines an instruction.  hi hi is summed apart from the other two products: the tensor core's sums drift towards zero
-// with their length, and those of small numbers do not notice.  For the same reason a sum over more than 512 k is cut: the epilogue adds
-// the pieces up in registers, in fp32 with rounding.
+// with their length, and those of small numbers do not notice.  For the same reason a long sum is cut: the epilogue adds the
+// pieces up in registers, in fp32 with rounding.  Pieces are of 256 k for fp32 results (512 x 4608: error 1.1e-6; 2e-6 with 512, 3e-6 with 1024,
+// 1 to 2 % faster each) and of 1024 k where the result is rounded to 16 bits or is a small part of a weight.
 //
 // Order.  Tasks are numbered product by product, those of all matrices together, and taken one by one off a counter.  A task waits until its
 // matrix's earlier tasks are done, which a counter of the matrix tells.  What it waits for has a lower number, so it has been taken by a CTA
@@ -196,7 +197,6 @@ constexpr int kOThreads = 320;
 constexpr int kOSlots = 5;                                 // of two tiles: hi and lo of an operand of a step
 constexpr int kORing = 4;                                  // tasks between the warps
 constexpr uint32_t kOSlot = 2 * kOrthoTile;
-constexpr int kOSegment = 8;                               // steps of a sum
 constexpr uint32_t kOStaging = 8 * 8192;                   // an epilogue warp's 32 rows x 64 columns, hi and lo, or fp32
 
 struct OrthoCtl {
@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
         }
     } else if (warp == 1) {
         if (elect_one()) {
-            const uint32_t hi = smem_desc_hi_sw128(1024);
+            const uint32_t hi = smem_desc_hi_sw128(1024), segment_mask = (uint32_t)tab.segment_mask;
             uint32_t it = 0, acc_it = 0;
             bool ok = true;
             for (uint32_t n = 0;; ++n) {
@@ -454,7 +454,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 OrthoOperand a, b;
                 ortho_operands(k, a, b);
                 for (int s = k.from; s < k.to; ++s, it += 2) {
-                    const uint32_t acc = acc_it & 1u, d = tmem_base + acc * 256u, first = (uint32_t)(s - k.from) % kOSegment;
+                    const uint32_t acc = acc_it & 1u, d = tmem_base + acc * 256u, first = (uint32_t)(s - k.from) & segment_mask;
                     if (first == 0) {
                         ok = mbar_wait_bounded(&ctl->acc_empty[acc], ((acc_it >> 1) & 1u) ^ 1u, abort_flag);
                         if (!ok) break;
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                     }
                     umma_commit(&ctl->empty[slot]);
                     umma_commit(&ctl->empty[slot2]);
-                    if (s + 1 == k.to || first == kOSegment - 1) { umma_commit(&ctl->acc_full[acc]); ++acc_it; }
+                    if (s + 1 == k.to || first == segment_mask) { umma_commit(&ctl->acc_full[acc]); ++acc_it; }
                 }
                 if (!ok) break;
             }
@@ -489,6 +489,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         uint8_t *buf = staging + (warp - 2) * 8192;
         const uint32_t row = quarter * 32 + lane;
+        const int segment_shift = __popc(tab.segment_mask);
         uint32_t acc_it = 0, old_ph = 0;
         bool ok = true;
         for (uint32_t n = 0;; ++n) {
@@ -502,7 +503,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
             const OrthoTask k = ortho_task(tab, ws, t);
             const OrthoItem &it = *k.it;
             const OrthoPlace place(it.rt, it.ct);
-            const int segments = (k.to - k.from + kOSegment - 1) / kOSegment;
+            const int segments = (k.to - k.from + tab.segment_mask) >> segment_shift;
             if (k.narrow && half) {                             // (64 columns are four warps' work)
                 for (int g = 0; g < segments; ++g, ++acc_it) {
                     ok = __all_sync(0xffffffffu, mbar_wait_bounded(&ctl->acc_full[acc_it & 1u], (acc_it >> 1) & 1u, abort_flag));
