@@ -297,7 +297,7 @@ __device__ __forceinline__ OrthoOperand ortho_operand(long long at, int tiles, i
 __device__ __forceinline__ void ortho_operands(const OrthoTask &k, OrthoOperand &a, OrthoOperand &b) {
     const OrthoItem &it = *k.it;
     const OrthoPlace place(it.rt, it.ct);
-    const int d = min(it.rt, it.ct), never = 1 << 30;
+    const int d = min(it.rt, it.ct), never = 1 << 24;           // (a matrix has less than 2^23 tiles of two steps)
     const bool tall = it.rows > it.cols;
     const long long x = place.x(k.x);
     if (k.op == kOrthoGram) {
@@ -320,6 +320,23 @@ __device__ __forceinline__ void ortho_operands(const OrthoTask &k, OrthoOperand 
         }
     }
 }
+
+// Where the next step's hi lies; lo behind it.
+struct OrthoCursor {
+    const uint8_t *p, *cols;
+    long long pitch, lo;
+    int turn;
+    __device__ __forceinline__ OrthoCursor(const uint8_t *m, const OrthoOperand &o, int s)
+        : cols(m + o.cols + (o.turn >> 1) * o.pitch), pitch(o.pitch), lo(o.lo), turn(o.turn) {          // (turn is even)
+        p = s < turn ? m + o.rows + (long long)s * kOrthoTile : m + o.cols + (s >> 1) * pitch + (s & 1) * (kOrthoTile / 2);
+    }
+    __device__ __forceinline__ void next(int s) {
+        ++s;
+        if (s < turn) p += kOrthoTile;
+        else if (s == turn) p = cols;
+        else p += s & 1 ? (long long)(kOrthoTile / 2) : pitch - kOrthoTile / 2;
+    }
+};
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
@@ -378,6 +395,10 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
             const int total = tab.first[tab.phases];
             uint32_t it = 0, n = 0;
             bool ok = true;
+            // (issuing loops step addresses: what they form anew each step, they form at the price of a step's copies)
+            const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]), tiles0 = smem_u32(tiles);
+            uint32_t slot = 0, ph = 1;
+            bool free = false;
             for (;; ++n) {
                 // (taken when its loads can begin: a task held in advance waits here while other CTAs have nothing to do)
                 const int t = atomicAdd(taken, 1);
@@ -407,28 +428,30 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 mbar_arrive(&ctl->ring_full[r]);
                 OrthoOperand a, b;
                 ortho_operands(k, a, b);
-                auto bring = [&](const OrthoOperand &o, bool narrow, int s, long long lo, uint32_t to, uint32_t bar) {
-                    if (s >= o.turn) {
-                        const uint8_t *p = k.m + o.cols + (s >> 1) * o.pitch + (s & 1) * (kOrthoTile / 2) + lo;
-                        bulk_load(to, p, kOrthoTile / 2, bar);
-                        if (!narrow) bulk_load(to + kOrthoTile / 2, p + kOrthoTile, kOrthoTile / 2, bar);
-                    } else {
-                        bulk_load(to, k.m + o.rows + (long long)s * kOrthoTile + lo, narrow ? kOrthoTile / 2 : kOrthoTile, bar);
-                    }
-                };
+                OrthoCursor at[2] = {OrthoCursor(k.m, a, k.from), OrthoCursor(k.m, b, k.from)};
                 for (int s = k.from; ok && s < k.to; ++s)
 #pragma unroll
                     for (int part = 0; part < 2; ++part, ++it) {
-                        const uint32_t slot = it % kOSlots;
-                        ok = ok && mbar_wait_bounded(&ctl->empty[slot], ((it / kOSlots) & 1u) ^ 1u, abort_flag);
+                        if (!free) ok = ok && mbar_wait_bounded(empty0 + slot * 8, ph, abort_flag);
                         if (!ok) break;
-                        const uint32_t bar = smem_u32(&ctl->full[slot]), dst = smem_u32(tiles) + slot * kOSlot;
-                        const OrthoOperand &o = part ? b : a;
+                        const uint32_t bar = full0 + slot * 8, dst = tiles0 + slot * kOSlot;
+                        if (++slot == kOSlots) { slot = 0; ph ^= 1u; }
+                        free = mbar_test_wait(empty0 + slot * 8, ph);
                         const bool narrow = part && k.narrow;
-                        const uint32_t half = narrow ? kOrthoTile / 2 : kOrthoTile;
-                        mbar_arrive_expect_tx(bar, 2 * half);
-                        bring(o, narrow, s, 0, dst, bar);
-                        bring(o, narrow, s, o.lo, dst + half, bar);
+                        const uint32_t bytes = narrow ? kOrthoTile / 2 : kOrthoTile;
+                        mbar_arrive_expect_tx(bar, 2 * bytes);
+                        OrthoCursor &c = at[part];
+                        if (s < c.turn || narrow) {
+                            const uint32_t one = s < c.turn ? bytes : kOrthoTile / 2;
+                            bulk_load(dst, c.p, one, bar);
+                            bulk_load(dst + bytes, c.p + c.lo, one, bar);
+                        } else {
+                            bulk_load(dst, c.p, kOrthoTile / 2, bar);
+                            bulk_load(dst + kOrthoTile / 2, c.p + kOrthoTile, kOrthoTile / 2, bar);
+                            bulk_load(dst + kOrthoTile, c.p + c.lo, kOrthoTile / 2, bar);
+                            bulk_load(dst + 3 * kOrthoTile / 2, c.p + c.lo + kOrthoTile, kOrthoTile / 2, bar);
+                        }
+                        c.next(s);
                     }
                 if (!ok) break;
             }
@@ -441,7 +464,8 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
     } else if (warp == 1) {
         if (elect_one()) {
             const uint32_t hi = smem_desc_hi_sw128(1024), segment_mask = (uint32_t)tab.segment_mask;
-            uint32_t it = 0, acc_it = 0;
+            const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]), tiles_lo = smem_u32(tiles) >> 4;
+            uint32_t slot = 0, ph = 0, acc_it = 0;
             bool ok = true;
             for (uint32_t n = 0;; ++n) {
                 const uint32_t r = n % kORing;
@@ -453,31 +477,33 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 const OrthoTask k = ortho_task(tab, ws, t);
                 OrthoOperand a, b;
                 ortho_operands(k, a, b);
-                for (int s = k.from; s < k.to; ++s, it += 2) {
+                const uint32_t n_one = k.narrow ? 64 : 128, both0 = idesc_h16_f32(128, 2 * n_one, 0, 0, 1), one0 = idesc_h16_f32(128, n_one, 0, 0, 1);
+                for (int s = k.from; s < k.to; ++s) {
                     const uint32_t acc = acc_it & 1u, d = tmem_base + acc * 256u, first = (uint32_t)(s - k.from) & segment_mask;
                     if (first == 0) {
                         ok = mbar_wait_bounded(&ctl->acc_empty[acc], ((acc_it >> 1) & 1u) ^ 1u, abort_flag);
                         if (!ok) break;
                         tc_fence_after_sync();
                     }
-                    const uint32_t slot = it % kOSlots, slot2 = (it + 1) % kOSlots;
-                    ok = mbar_wait_bounded(&ctl->full[slot], (it / kOSlots) & 1u, abort_flag);
-                    if (!ok) break;
-                    ok = mbar_wait_bounded(&ctl->full[slot2], ((it + 1) / kOSlots) & 1u, abort_flag);
-                    if (!ok) break;
-                    const bool a_mn = s >= a.turn, b_mn = s >= b.turn;
-                    const int n = k.narrow ? 64 : 128;
-                    const uint32_t both = idesc_h16_f32(128, 2 * n, a_mn, b_mn, 1), one = idesc_h16_f32(128, n, a_mn, b_mn, 1);
-                    const uint32_t a_hi = smem_desc_lo(smem_u32(tiles) + slot * kOSlot, a_mn ? 8192 : 16), a_lo = a_hi + (kOrthoTile >> 4);
-                    const uint32_t b_hi = smem_desc_lo(smem_u32(tiles) + slot2 * kOSlot, b_mn ? 8192 : 16);
+                    // major: bit 15 of the descriptors A's, 16 B's; the leading byte offset is 8192 then, else 16
+                    const uint32_t a_mn = s >= a.turn, b_mn = s >= b.turn, major = a_mn << 15 | b_mn << 16;
                     const uint32_t sa = a_mn ? 128u : 2u, sb = b_mn ? 128u : 2u;
+                    ok = mbar_wait_bounded(full0 + slot * 8, ph, abort_flag);
+                    if (!ok) break;
+                    const uint32_t a_hi = tiles_lo + slot * (kOSlot >> 4) + (a_mn ? 512u << 16 : 1u << 16), a_lo = a_hi + (kOrthoTile >> 4);
+                    const uint32_t done_a = empty0 + slot * 8;
+                    if (++slot == kOSlots) { slot = 0; ph ^= 1u; }
+                    ok = mbar_wait_bounded(full0 + slot * 8, ph, abort_flag);
+                    if (!ok) break;
+                    const uint32_t b_hi = tiles_lo + slot * (kOSlot >> 4) + (b_mn ? 512u << 16 : 1u << 16), done_b = empty0 + slot * 8;
+                    if (++slot == kOSlots) { slot = 0; ph ^= 1u; }
 #pragma unroll
                     for (uint32_t q = 0; q < 4; ++q) {
-                        umma_bf16_ss_sel(d, a_hi + q * sa, hi, b_hi + q * sb, hi, both, first + q);
-                        umma_bf16_ss_halves<true>(d + n, a_lo + q * sa, hi, b_hi + q * sb, hi, one);
+                        umma_bf16_ss_sel(d, a_hi + q * sa, hi, b_hi + q * sb, hi, both0 | major, first + q);
+                        umma_bf16_ss_halves<true>(d + n_one, a_lo + q * sa, hi, b_hi + q * sb, hi, one0 | major);
                     }
-                    umma_commit(&ctl->empty[slot]);
-                    umma_commit(&ctl->empty[slot2]);
+                    umma_commit(done_a);
+                    umma_commit(done_b);
                     if (s + 1 == k.to || first == segment_mask) { umma_commit(&ctl->acc_full[acc]); ++acc_it; }
                 }
                 if (!ok) break;
