@@ -41,7 +41,8 @@ __device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
     asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ void fence_proxy_async_any() { asm volatile("fence.proxy.async;" ::: "memory"); }
+// (of all memory it takes 700 clocks, a fifth of a product)
+__device__ __forceinline__ void fence_proxy_async_cluster() { asm volatile("fence.proxy.async.shared::cluster;" ::: "memory"); }
 
 // Eight numbers (2^10 times what they stand for) as pairs of halves.
 __device__ __forceinline__ void to_pairs(const float (&v)[8], uint4 &hi, uint4 &lo) {
@@ -53,6 +54,18 @@ __device__ __forceinline__ void to_pairs(const float (&v)[8], uint4 &hi, uint4 &
         const __half2 b = __floats2half2_rn(v[2 * e] - back.x, v[2 * e + 1] - back.y);
         h[e] = *reinterpret_cast<const uint32_t *>(&a);
         l[e] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+// Eight numbers as they are, each in two words of 16 bits.
+__device__ __forceinline__ void split_words(const float (&v)[8], uint4 &hi, uint4 &lo) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t a = __float_as_uint(v[2 * e]), b = __float_as_uint(v[2 * e + 1]);
+        h[e] = a >> 16 | (b & 0xFFFF0000u);
+        l[e] = (a & 0xFFFFu) | b << 16;
     }
     hi = make_uint4(h[0], h[1], h[2], h[3]);
     lo = make_uint4(l[0], l[1], l[2], l[3]);
@@ -111,17 +124,19 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     const int fast = tall ? m : cols, count = m * cols;              // (at most 2^15)
     const float per_line = cols > 0 ? 1.f / (float)fast : 0.f;
     double s = 0.;
-    auto spot = [&](int i, int j) { return x + (size_t)(j >> 6) * kSTile + ortho_chunk(i, (j & 63) >> 3) + (j & 7) * 2; };
+    // the block's e-th element in the order of memory: where it lies there, and in the tiles
+    auto locate = [&](int e, long long &at) {
+        const int line = __float2int_rz(((float)e + 0.5f) * per_line), a = e - line * fast, i = tall ? a : line, j = tall ? line : a;
+        at = place(i, j);
+        return (j >> 6) * kSTile + ortho_chunk(i, (j & 63) >> 3) + (j & 7) * 2;
+    };
     for (int e0 = threadIdx.x; e0 < count; e0 += 16 * kSThreads) {
         float u[16];
         long long at[16];
-        int where[16];
+        uint32_t where[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-            const int e = min(e0 + k * kSThreads, count - 1), line = __float2int_rz(((float)e + 0.5f) * per_line), a = e - line * fast;
-            const int i = tall ? a : line, j = tall ? line : a;
-            at[k] = place(i, j);
-            where[k] = (int)(spot(i, j) - x);
+            where[k] = locate(min(e0 + k * kSThreads, count - 1), at[k]);
         }
         if (tab.muon) {
             float v[16];
@@ -161,7 +176,14 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     s = 0.;
     if (blocks > 1) for (int b = 0; b < blocks; ++b) s += ld_cluster_f64(cluster_addr(&ctl->sum, b));
     else s = ctl->sum;
-    const double inv = (double)kOrthoScale / (sqrt(s) + tab.eps);
+    // as a power of two, in two factors, and a fraction of 48 bits: a product in 64 bits per element is two conversions, sixteen a clock
+    int power;
+    const double part = frexp((double)kOrthoScale / (sqrt(s) + tab.eps), &power);
+    const float two_a = ldexpf(1.f, power / 2), two_b = ldexpf(1.f, power - power / 2), part_hi = (float)part, part_lo = (float)(part - (double)part_hi);
+    auto scaled = [&](uint32_t bits) {
+        const float u = __uint_as_float(bits) * two_a * two_b;
+        return fmaf(u, part_hi, u * part_lo);
+    };
     // (rows beyond the matrix are zeros)
     for (int c = threadIdx.x; c < tiles * m16 * 8; c += kSThreads) {
         uint8_t *to = x + (size_t)(c / (m16 * 8)) * kSTile + c % (m16 * 8) * 16;
@@ -170,8 +192,8 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
         float v[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            v[2 * e] = (float)((double)__uint_as_float(a[e] << 16 | (b[e] & 0xFFFFu)) * inv);
-            v[2 * e + 1] = (float)((double)__uint_as_float((a[e] & 0xFFFF0000u) | b[e] >> 16) * inv);
+            v[2 * e] = scaled(a[e] << 16 | (b[e] & 0xFFFFu));
+            v[2 * e + 1] = scaled((a[e] & 0xFFFF0000u) | b[e] >> 16);
         }
         uint4 h, l;
         to_pairs(v, h, l);
@@ -182,12 +204,18 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     uint32_t ph = 0;
     const uint32_t x_at = smem_u32(x), ap_at = smem_u32(ap), hi_word = smem_desc_hi_sw128(1024);
     // d (+ 256: the products with a lo) = A-operand x B-operand over k steps of 16; tiles of 64 k or 64 n are kSTile apart
-    auto product = [&](uint32_t a_at, uint32_t b_at, bool b_mn, int nn, int steps) {
-        fence_proxy_async_any();
-        if (blocks > 1) cluster_sync_all(); else __syncthreads();
+    // (wide: operands, or what the sums will lie on, are other blocks' doing)
+    auto product = [&](uint32_t a_at, uint32_t b_at, bool b_mn, int nn, int steps, bool wide) {
+        if (wide) {
+            fence_proxy_async_cluster();
+            cluster_sync_all();
+        } else {
+            fence_proxy_async_smem();
+            __syncthreads();
+        }
         if (warp == 0 && steps > 0 && elect_one()) {
             tc_fence_after_sync();
-            fence_proxy_async_any();
+            if (wide) fence_proxy_async_cluster();
             const uint32_t idesc = idesc_h16_f32(128, nn, 0, b_mn, 1);
             for (int k = 0; k < steps; ++k) {
                 const uint32_t a = smem_desc_lo(a_at + (k >> 2) * kSTile, 16) + (k & 3) * 2u;
@@ -219,7 +247,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
 
     for (int step = 0; step < tab.steps; ++step) {
         // ---- A = X X^T ----
-        product(x_at, x_at, false, m16, n16 / 16);
+        product(x_at, x_at, false, m16, n16 / 16, blocks > 1);
         if (blocks == 1) {
             if (rows_here)
                 for (int c = half * 32; c < m16; c += 64) {
@@ -298,7 +326,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
         }
         tc_fence_before_sync();
         // ---- P = b A + c A A, where A is ----
-        product(ap_at, ap_at, false, m16, m16 / 16);
+        product(ap_at, ap_at, false, m16, m16 / 16, blocks > 1);
         if (rows_here)
             for (int c = half * 32; c < m16; c += 64) {
                 float v[32];
@@ -319,91 +347,54 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
             }
         tc_fence_before_sync();
         // ---- X <- a X + P X, in place ----
-        product(ap_at, x_at, true, n16, n16 > 0 ? m16 / 16 : 0);
+        product(ap_at, x_at, true, n16, n16 > 0 ? m16 / 16 : 0, false);
         const bool last = step + 1 == tab.steps;
         if (rows_here)
-            for (int t = half; t < tiles; t += 2) {
-                uint8_t *tile = x + (size_t)t * kSTile;
-                float v[64];
+            for (int c0 = half * 32; c0 < n16; c0 += 64) {
+                float f[32];
+                sums(c0, f);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float f[32];
-                    if (t * 64 + h * 32 < n16) sums(t * 64 + h * 32, f);
-                    else {
+                for (int q = 0; q < 4; ++q) {
+                    if ((int)row >= m || c0 + q * 8 >= n16) continue;            // (rows and columns beyond stay zero)
+                    uint8_t *at = chunk_of(x, c0 + q * 8);
+                    float w[8];
+                    from_pairs(*(const uint4 *)at, *(const uint4 *)(at + kOrthoTile), w);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) f[i] = 0.f;
-                    }
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint8_t *at = tile + ortho_chunk(row, h * 4 + q);
-                        float w[8];
-                        from_pairs(*(const uint4 *)at, *(const uint4 *)(at + kOrthoTile), w);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[h * 32 + q * 8 + e] = fmaf(kOrthoCoefA, w[e], f[q * 8 + e] * (1.f / kOrthoScale));
-                    }
+                    for (int e = 0; e < 8; ++e) w[e] = fmaf(kOrthoCoefA, w[e], f[q * 8 + e] * (1.f / kOrthoScale));
+                    uint4 h, l;
+                    if (last) split_words(w, h, l); else to_pairs(w, h, l);
+                    *(uint4 *)at = h;
+                    *(uint4 *)(at + kOrthoTile) = l;
                 }
-                if (!last) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        if ((int)row >= m || t * 64 + q * 8 >= n16) continue;       // (rows and columns beyond stay zero)
-                        float w[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = v[8 * q + e];
-                        uint4 hh, ll;
-                        to_pairs(w, hh, ll);
-                        uint8_t *at = tile + ortho_chunk(row, q);
-                        *(uint4 *)at = hh;
-                        *(uint4 *)(at + kOrthoTile) = ll;
-                    }
-                    continue;
-                }
-                auto give = [&](long long at, float o, float old) {
-                    if (tab.muon) {
-                        const float w = fmaf(-it.scale, o, tab.keep * old);
-                        it.master[at] = w;
-                        if (it.out) ((T *)it.out)[at] = from_f32<T>(w);
-                    } else {
-                        ((T *)it.out)[at] = from_f32<T>(o);
-                    }
-                };
-                if (tall) {
-                    // a column of X is a line in memory: a warp's rows side by side
-                    if ((int)row < m)
-#pragma unroll
-                        for (int j0 = 0; j0 < 64; j0 += 16) {
-                            float old[16];
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) old[j] = tab.muon && t * 64 + j0 + j < cols ? it.master[place(row, t * 64 + j0 + j)] : 0.f;
-#pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                if (t * 64 + j0 + j < cols) give(place(row, t * 64 + j0 + j), v[j0 + j] * (1.f / kOrthoScale), old[j]);
-                        }
-                    continue;
-                }
-                // through the warp's quarters of the tile (rows 0 .. 15 where hi was, 16 .. 31 where lo was), then line by line
-                auto spot = [&](int r, int c4) { return tile + (r >= 16 ? kOrthoTile : 0) + quarter * 4096 + (r & 15) * 256 + ((c4 ^ (r & 15)) << 4); };
-                __syncwarp();
-#pragma unroll
-                for (int c = 0; c < 16; ++c) *(float4 *)spot(lane, c) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-                __syncwarp();
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int j = t * 64 + h * 32 + lane;
-                    if (j >= cols) continue;
-                    for (int i0 = 0; i0 < 32; i0 += 16) {
-                        float old[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) old[i] = tab.muon && quarter * 32 + i0 + i < m ? it.master[place(quarter * 32 + i0 + i, j)] : 0.f;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (quarter * 32 + i0 + i < m)
-                                give(place(quarter * 32 + i0 + i, j), *(const float *)(spot(i0 + i, h * 8 + (lane >> 2)) + (lane & 3) * 4) * (1.f / kOrthoScale),
-                                     old[i]);
-                    }
-                }
-                __syncwarp();
             }
         tc_fence_before_sync();
+    }
+    __syncthreads();
+    // ---- out, in the order of memory ----
+    for (int e0 = threadIdx.x; e0 < count; e0 += 16 * kSThreads) {
+        float o[16], old[16];
+        long long at[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const uint8_t *from = x + locate(min(e0 + k * kSThreads, count - 1), at[k]);
+            o[k] = __uint_as_float((uint32_t)*(const uint16_t *)from << 16 | *(const uint16_t *)(from + kOrthoTile)) * (1.f / kOrthoScale);
+        }
+        if (tab.muon) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) old[k] = it.master[at[k]];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                if (e0 + k * kSThreads >= count) break;
+                o[k] = fmaf(-it.scale, o[k], tab.keep * old[k]);
+                it.master[at[k]] = o[k];
+            }
+        }
+        if (it.out)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                if (e0 + k * kSThreads >= count) break;
+                ((T *)it.out)[at[k]] = from_f32<T>(o[k]);
+            }
     }
     __syncthreads();
     if (blocks > 1) cluster_sync_all();
