@@ -17,14 +17,14 @@ using namespace ptx;
 
 namespace {
 
-constexpr int kSThreads = 256;
+constexpr int kSThreads = 512;                          // sixteen warps: a row of sums is four threads' work
 constexpr uint32_t kSTile = 2 * kOrthoTile;            // 128 rows x 64 columns, hi and lo
 constexpr int kSMaxWidth = 256;
 constexpr int kSMaxCluster = 8;
 
 struct SmallCtl {
     uint64_t done;
-    double sum, part[8];
+    double sum, part[kSThreads / 32];
     uint32_t tmem_base;
 };
 
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     uint8_t *x = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);          // [width / 64] tiles
     uint8_t *ap = x + (size_t)(sh.width / 64) * kSTile;                                // two tiles: A, then P; parts of A's sums before
     SmallCtl *ctl = (SmallCtl *)(ap + 2 * kSTile);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, half = warp >> 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, fourth = warp >> 2;
     const int blocks = sh.blocks, rank = blocks > 1 ? (int)cluster_rank() : 0;
     const int matrix = blockIdx.x / blocks;
     int which = 0;
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     const int m16 = (m + 15) & ~15, n16 = (cols + 15) & ~15, tiles = (cols + 63) / 64;
     const long long base = (long long)(matrix - it.first_matrix) * it.rows * it.cols;
     // element (i, j) of X, j within the block
-    auto place = [&](int i, int j) { return base + (tall ? (long long)(col0 + j) * it.cols + i : (long long)i * it.cols + col0 + j); };
+    auto place = [&](int i, int j) { return tall ? (col0 + j) * it.cols + i : i * it.cols + col0 + j; };
 
     if (threadIdx.x == 0) {
         mbar_init(&ctl->done, 1);
@@ -125,14 +125,14 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     const float per_line = cols > 0 ? 1.f / (float)fast : 0.f;
     double s = 0.;
     // the block's e-th element in the order of memory: where it lies there, and in the tiles
-    auto locate = [&](int e, long long &at) {
+    auto locate = [&](int e, int &at) {
         const int line = __float2int_rz(((float)e + 0.5f) * per_line), a = e - line * fast, i = tall ? a : line, j = tall ? line : a;
         at = place(i, j);
         return (j >> 6) * kSTile + ortho_chunk(i, (j & 63) >> 3) + (j & 7) * 2;
     };
     for (int e0 = threadIdx.x; e0 < count; e0 += 16 * kSThreads) {
         float u[16];
-        long long at[16];
+        int at[16];
         uint32_t where[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
         if (tab.muon) {
             float v[16];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) { u[k] = ((const float *)it.g)[at[k]]; v[k] = it.momentum[at[k]]; }
+            for (int k = 0; k < 16; ++k) { u[k] = ((const float *)it.g + base)[at[k]]; v[k] = (it.momentum + base)[at[k]]; }
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
                 v[k] = fmaf(tab.momentum, v[k], u[k]);
@@ -149,10 +149,10 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
             }
 #pragma unroll
             for (int k = 0; k < 16; ++k)
-                if (e0 + k * kSThreads < count) it.momentum[at[k]] = v[k];
+                if (e0 + k * kSThreads < count) (it.momentum + base)[at[k]] = v[k];
         } else {
 #pragma unroll
-            for (int k = 0; k < 16; ++k) u[k] = to_f32(((const T *)it.g)[at[k]]);
+            for (int k = 0; k < 16; ++k) u[k] = to_f32(((const T *)it.g + base)[at[k]]);
         }
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     __syncthreads();
     if (threadIdx.x == 0) {
         s = ctl->part[0];
-        for (int i = 1; i < 8; ++i) s += ctl->part[i];
+        for (int i = 1; i < kSThreads / 32; ++i) s += ctl->part[i];
         ctl->sum = s;
     }
     if (blocks > 1) cluster_sync_all(); else __syncthreads();
@@ -226,6 +226,8 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
             }
             umma_commit(&ctl->done);
         }
+    };
+    auto finished = [&](int steps) {
         if (steps > 0) {
             if (!mbar_wait_bounded(&ctl->done, ph, nullptr) && threadIdx.x == 0) atomicOr(err, ERRW_TIMEOUT);
             ph ^= 1u;
@@ -233,38 +235,52 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
         tc_fence_after_sync();
     };
     const uint32_t row = quarter * 32 + lane, t_row = tmem + ((uint32_t)(quarter * 32) << 16);
-    // 32 sums of this thread's row from column c on
-    auto sums = [&](int c, float (&v)[32]) {
-        uint32_t p[32], q[32];
-        tmem_ld_32x32(t_row + c, p);
-        tmem_ld_32x32(t_row + 256 + c, q);
+    // 16 sums of this thread's row from column c on, times f
+    auto sums = [&](int c, float f, float (&v)[16]) {
+        uint32_t p[16], q[16];
+        tmem_ld_32x16(t_row + c, p);
+        tmem_ld_32x16(t_row + 256 + c, q);
         tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(p[i]) + __uint_as_float(q[i]);
+        for (int i = 0; i < 16; ++i) v[i] = f * (__uint_as_float(p[i]) + __uint_as_float(q[i]));
     };
     auto chunk_of = [&](uint8_t *at, int c) { return at + (size_t)(c >> 6) * kSTile + ortho_chunk(row, (c & 63) >> 3); };
+    // sixteen numbers of a row from column c on
+    auto read = [&](uint8_t *at, int c, float (&v)[16]) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const uint8_t *from = chunk_of(at, c + 8 * q);
+            float w[8];
+            from_pairs(*(const uint4 *)from, *(const uint4 *)(from + kOrthoTile), w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[8 * q + e] = w[e];
+        }
+    };
+    auto write = [&](uint8_t *at, int c, const float (&v)[16], bool whole) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            uint8_t *to = chunk_of(at, c + 8 * q);
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = v[8 * q + e];
+            uint4 h, l;
+            if (whole) split_words(w, h, l); else to_pairs(w, h, l);
+            *(uint4 *)to = h;
+            *(uint4 *)(to + kOrthoTile) = l;
+        }
+    };
     const bool rows_here = quarter * 32 < m16;                        // (whole warps)
 
     for (int step = 0; step < tab.steps; ++step) {
         // ---- A = X X^T ----
         product(x_at, x_at, false, m16, n16 / 16, blocks > 1);
+        finished(n16 / 16);
+        float v[16], old[16];
         if (blocks == 1) {
             if (rows_here)
-                for (int c = half * 32; c < m16; c += 64) {
-                    float v[32];
-                    sums(c, v);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (c + 8 * q >= m16) break;
-                        float w[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = v[8 * q + e] * (1.f / kOrthoScale);
-                        uint4 h, l;
-                        to_pairs(w, h, l);
-                        uint8_t *to = chunk_of(ap, c + 8 * q);
-                        *(uint4 *)to = h;
-                        *(uint4 *)(to + kOrthoTile) = l;
-                    }
+                for (int c = fourth * 16; c < m16; c += 64) {
+                    sums(c, 1.f / kOrthoScale, v);
+                    write(ap, c, v, false);
                 }
         } else {
             // part by part to the block that has the row: [block][4 columns][its rows] in fp32, where P was (rows side by side, as a warp has
@@ -272,15 +288,14 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
             const int share = 128 / blocks;                           // (blocks: a power of two)
             if (rows_here) {
                 const uint32_t to = cluster_addr(ap, row / share) + (rank * 32 * share + row % share) * 16;
-                for (int c = half * 32; c < m16; c += 64) {
-                    float v[32];
-                    if (n16 > 0) sums(c, v);
+                for (int c = fourth * 16; c < m16; c += 64) {
+                    if (n16 > 0) sums(c, 1.f, v);
                     else {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = 0.f;
+                        for (int i = 0; i < 16; ++i) v[i] = 0.f;
                     }
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
+                    for (int q = 0; q < 4; ++q)
                         st_cluster_v4(to + (c / 4 + q) * share * 16, make_uint4(__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]),
                                                                      __float_as_uint(v[4 * q + 3])));
                 }
@@ -288,12 +303,10 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
             tc_fence_before_sync();
             cluster_sync_all();
             // each thread eight columns of a row of the share, in turn
-            const int per_row = 16;
-            float w[8][8];
-            const int sets = share * per_row / kSThreads;             // (share 64: 4, 32: 2, 16: 1)
+            constexpr int kSets = 128 / 2 * 16 / kSThreads;           // of two blocks: their shares are the largest
+            float w[kSets][8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k >= sets) break;
+            for (int k = 0; k < kSets; ++k) {
                 const int idx = threadIdx.x + k * kSThreads, r = idx % share, c = idx / share * 8;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[k][e] = 0.f;
@@ -307,8 +320,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
             }
             cluster_sync_all();
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k >= sets) break;
+            for (int k = 0; k < kSets; ++k) {
                 const int idx = threadIdx.x + k * kSThreads, r = rank * share + idx % share, c = idx / share * 8;
                 if (c >= m16 || r >= m16) continue;
                 float f[8];
@@ -326,46 +338,32 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
         }
         tc_fence_before_sync();
         // ---- P = b A + c A A, where A is ----
+        // (the first of a thread's old numbers are read while the tensor core works)
+        const int c0 = fourth * 16;
         product(ap_at, ap_at, false, m16, m16 / 16, blocks > 1);
+        if (rows_here && c0 < m16) read(ap, c0, old);
+        finished(m16 / 16);
         if (rows_here)
-            for (int c = half * 32; c < m16; c += 64) {
-                float v[32];
-                sums(c, v);
+            for (int c = c0; c < m16; c += 64) {
+                if (c != c0) read(ap, c, old);
+                sums(c, kOrthoCoefC / kOrthoScale, v);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (c + 8 * q >= m16) break;
-                    uint8_t *at = chunk_of(ap, c + 8 * q);
-                    float w[8];
-                    from_pairs(*(const uint4 *)at, *(const uint4 *)(at + kOrthoTile), w);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = fmaf(kOrthoCoefB, w[e], v[8 * q + e] * (kOrthoCoefC / kOrthoScale));
-                    uint4 h, l;
-                    to_pairs(w, h, l);
-                    *(uint4 *)at = h;
-                    *(uint4 *)(at + kOrthoTile) = l;
-                }
+                for (int e = 0; e < 16; ++e) v[e] = fmaf(kOrthoCoefB, old[e], v[e]);
+                write(ap, c, v, false);
             }
         tc_fence_before_sync();
-        // ---- X <- a X + P X, in place ----
+        // ---- X <- a X + P X, in place (rows and columns beyond the matrix stay zero) ----
         product(ap_at, x_at, true, n16, n16 > 0 ? m16 / 16 : 0, false);
+        if (rows_here && c0 < n16) read(x, c0, old);
+        finished(n16);
         const bool last = step + 1 == tab.steps;
         if (rows_here)
-            for (int c0 = half * 32; c0 < n16; c0 += 64) {
-                float f[32];
-                sums(c0, f);
+            for (int c = c0; c < n16; c += 64) {
+                if (c != c0) read(x, c, old);
+                sums(c, 1.f / kOrthoScale, v);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if ((int)row >= m || c0 + q * 8 >= n16) continue;            // (rows and columns beyond stay zero)
-                    uint8_t *at = chunk_of(x, c0 + q * 8);
-                    float w[8];
-                    from_pairs(*(const uint4 *)at, *(const uint4 *)(at + kOrthoTile), w);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = fmaf(kOrthoCoefA, w[e], f[q * 8 + e] * (1.f / kOrthoScale));
-                    uint4 h, l;
-                    if (last) split_words(w, h, l); else to_pairs(w, h, l);
-                    *(uint4 *)at = h;
-                    *(uint4 *)(at + kOrthoTile) = l;
-                }
+                for (int e = 0; e < 16; ++e) v[e] = (int)row < m ? fmaf(kOrthoCoefA, old[e], v[e]) : 0.f;
+                write(x, c, v, last);
             }
         tc_fence_before_sync();
     }
@@ -373,7 +371,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     // ---- out, in the order of memory ----
     for (int e0 = threadIdx.x; e0 < count; e0 += 16 * kSThreads) {
         float o[16], old[16];
-        long long at[16];
+        int at[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             const uint8_t *from = x + locate(min(e0 + k * kSThreads, count - 1), at[k]);
@@ -381,19 +379,19 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
         }
         if (tab.muon) {
 #pragma unroll
-            for (int k = 0; k < 16; ++k) old[k] = it.master[at[k]];
+            for (int k = 0; k < 16; ++k) old[k] = (it.master + base)[at[k]];
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
                 if (e0 + k * kSThreads >= count) break;
                 o[k] = fmaf(-it.scale, o[k], tab.keep * old[k]);
-                it.master[at[k]] = o[k];
+                (it.master + base)[at[k]] = o[k];
             }
         }
         if (it.out)
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
                 if (e0 + k * kSThreads >= count) break;
-                ((T *)it.out)[at[k]] = from_f32<T>(o[k]);
+                ((T *)it.out + base)[at[k]] = from_f32<T>(o[k]);
             }
     }
     __syncthreads();
