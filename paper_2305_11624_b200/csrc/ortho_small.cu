@@ -7,6 +7,7 @@
 // kernel for large matrices, eight microseconds a product, and two launches before it.)
 // X lies as m rows x n columns whichever side is the shorter: a tall matrix is transposed on its way in and out.
 #include <algorithm>
+#include <type_traits>
 
 #include "ortho.cuh"
 #include "sm100_ptx.cuh"
@@ -23,7 +24,7 @@ constexpr int kSMaxWidth = 256;
 constexpr int kSMaxCluster = 8;
 
 struct SmallCtl {
-    uint64_t done;
+    uint64_t done, rows;                               // a product; the other blocks' rows of A
     double sum, part[kSThreads / 32];
     uint32_t tmem_base;
 };
@@ -43,6 +44,12 @@ __device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
 }
 // (of all memory it takes 700 clocks, a fifth of a product)
 __device__ __forceinline__ void fence_proxy_async_cluster() { asm volatile("fence.proxy.async.shared::cluster;" ::: "memory"); }
+
+// To another block of the cluster; its barrier counts the bytes.
+__device__ __forceinline__ void bulk_send(uint32_t dst, uint32_t src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "r"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
 
 // Eight numbers (2^10 times what they stand for) as pairs of halves.
 __device__ __forceinline__ void to_pairs(const float (&v)[8], uint4 &hi, uint4 &lo) {
@@ -79,6 +86,11 @@ __device__ __forceinline__ void from_pairs(uint4 hi, uint4 lo, float (&v)[8]) {
     v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
 }
 
+template <class U, int V>
+struct alignas(V * sizeof(U)) Few { U e[V]; };
+template <int V, class U>
+__device__ __forceinline__ Few<U, V> load(const U *p) { return *(const Few<U, V> *)p; }
+
 template <class T>
 __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_constant__ OrthoTable tab, const SmallShape sh, int *err) {
     extern __shared__ uint8_t smem_raw[];
@@ -96,11 +108,9 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     const int col0 = rank * sh.width, cols = max(0, min(sh.width, n - col0));          // this block's columns
     const int m16 = (m + 15) & ~15, n16 = (cols + 15) & ~15, tiles = (cols + 63) / 64;
     const long long base = (long long)(matrix - it.first_matrix) * it.rows * it.cols;
-    // element (i, j) of X, j within the block
-    auto place = [&](int i, int j) { return tall ? (col0 + j) * it.cols + i : i * it.cols + col0 + j; };
-
     if (threadIdx.x == 0) {
         mbar_init(&ctl->done, 1);
+        mbar_init(&ctl->rows, 1);
         fence_barrier_init();
     }
     if (warp == 0) {
@@ -119,50 +129,90 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     // (the block's tiles: zeros beyond the matrix)
     for (int i = threadIdx.x; i < tiles * (int)(kSTile / 16); i += kSThreads) ((uint4 *)x)[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
-    // Once from memory, sixteen loads of a thread on their way: the sum of squares, and the number's two halves where hi and lo of it will be.
-    // (Line by line, and again for the scaling, this took two thirds of 189 x 37's 70 us.)
-    const int fast = tall ? m : cols, count = m * cols;              // (at most 2^15)
-    const float per_line = cols > 0 ? 1.f / (float)fast : 0.f;
-    double s = 0.;
-    // the block's e-th element in the order of memory: where it lies there, and in the tiles
-    auto locate = [&](int e, int &at) {
-        const int line = __float2int_rz(((float)e + 0.5f) * per_line), a = e - line * fast, i = tall ? a : line, j = tall ? line : a;
-        at = place(i, j);
-        return (j >> 6) * kSTile + ortho_chunk(i, (j & 63) >> 3) + (j & 7) * 2;
-    };
-    for (int e0 = threadIdx.x; e0 < count; e0 += 16 * kSThreads) {
-        float u[16];
-        int at[16];
-        uint32_t where[16];
+    // The block's elements in the order of memory, a thread one to four side by side of every kSThreads', sixteen in all under way; f(where a unit lies
+    // in memory, and in the tiles, how many are there).  Four where a line's length and all addresses allow: 64 x 64 took 3700 clocks one by one.
+    const int fast = tall ? m : cols, lines = tall ? cols : m, start = tall ? col0 * it.cols : col0;
+    auto in_order = [&](auto side, auto &&f) {
+        constexpr int V = decltype(side)::value, B = 16 / V;
+        const int units = max(fast / V, 1), total = lines * (fast / V), dl = kSThreads / units, da = kSThreads - dl * units;
+        int line = threadIdx.x / units, a = threadIdx.x - line * units;
+        for (int e = threadIdx.x; e < total; e += B * kSThreads) {
+            int at[B];
+            uint32_t where[B];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            where[k] = locate(min(e0 + k * kSThreads, count - 1), at[k]);
+            for (int k = 0; k < B; ++k) {
+                const int i = tall ? a * V : line, j = tall ? line : a * V;
+                at[k] = start + line * it.cols + a * V;
+                where[k] = (j >> 6) * kSTile + ortho_chunk(i, (j & 63) >> 3) + (j & 7) * 2;
+                line += dl;
+                a += da;
+                if (a >= units) { a -= units; ++line; }
+            }
+            f(at, where, (total - e + kSThreads - 1) / kSThreads);
         }
-        if (tab.muon) {
-            float v[16];
+    };
+    // a unit lies along a row of a tile or, tall, down its rows (the first a multiple of V): the q-th's place
+    auto down = [&](uint32_t where, int q) { return (where + q * 128u) ^ (uint32_t)(q << 4); };
+    const bool fours = it.cols % 4 == 0 && ((uintptr_t)it.g | (uintptr_t)it.momentum | (uintptr_t)it.master) % 16 == 0 && (uintptr_t)it.out % (4 * sizeof(T)) == 0;
+    double s = 0.;
+    // Once from memory: the sum of squares, and the number's two halves where hi and lo of it will be.
+    // (Line by line, and again for the scaling, this took two thirds of 189 x 37's 70 us.)
+    auto take = [&](auto side) {
+        constexpr int V = decltype(side)::value, B = 16 / V;
+        in_order(side, [&](const int (&at)[B], const uint32_t (&where)[B], int here) {
+            float u[B][V];
+            if (tab.muon) {
+                Few<float, V> g[B], v[B];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) { u[k] = ((const float *)it.g + base)[at[k]]; v[k] = (it.momentum + base)[at[k]]; }
+                for (int k = 0; k < B; ++k)
+                    if (k < here) { g[k] = load<V>((const float *)it.g + base + at[k]); v[k] = load<V>(it.momentum + base + at[k]); }
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                v[k] = fmaf(tab.momentum, v[k], u[k]);
-                u[k] = tab.nesterov ? fmaf(tab.momentum, v[k], u[k]) : v[k];
+                for (int k = 0; k < B; ++k) {
+                    if (k >= here) break;
+#pragma unroll
+                    for (int q = 0; q < V; ++q) {
+                        v[k].e[q] = fmaf(tab.momentum, v[k].e[q], g[k].e[q]);
+                        u[k][q] = tab.nesterov ? fmaf(tab.momentum, v[k].e[q], g[k].e[q]) : v[k].e[q];
+                    }
+                    *(Few<float, V> *)(it.momentum + base + at[k]) = v[k];
+                }
+            } else {
+                Few<T, V> g[B];
+#pragma unroll
+                for (int k = 0; k < B; ++k)
+                    if (k < here) g[k] = load<V>((const T *)it.g + base + at[k]);
+#pragma unroll
+                for (int k = 0; k < B; ++k)
+#pragma unroll
+                    for (int q = 0; q < V; ++q)
+                        if (k < here) u[k][q] = to_f32(g[k].e[q]);
             }
 #pragma unroll
-            for (int k = 0; k < 16; ++k)
-                if (e0 + k * kSThreads < count) (it.momentum + base)[at[k]] = v[k];
-        } else {
+            for (int k = 0; k < B; ++k) {
+                if (k >= here) break;
+                Few<uint16_t, V> h, l;
 #pragma unroll
-            for (int k = 0; k < 16; ++k) u[k] = to_f32(((const T *)it.g + base)[at[k]]);
-        }
+                for (int q = 0; q < V; ++q) {
+                    s += (double)u[k][q] * (double)u[k][q];
+                    const uint32_t bits = __float_as_uint(u[k][q]);
+                    h.e[q] = (uint16_t)(bits >> 16);
+                    l.e[q] = (uint16_t)bits;
+                }
+                if (!tall) {
+                    *(Few<uint16_t, V> *)(x + where[k]) = h;
+                    *(Few<uint16_t, V> *)(x + where[k] + kOrthoTile) = l;
+                    continue;
+                }
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            if (e0 + k * kSThreads >= count) break;
-            s += (double)u[k] * (double)u[k];
-            const uint32_t bits = __float_as_uint(u[k]);
-            *(uint16_t *)(x + where[k]) = (uint16_t)(bits >> 16);
-            *(uint16_t *)(x + where[k] + kOrthoTile) = (uint16_t)bits;
-        }
-    }
+                for (int q = 0; q < V; ++q) {
+                    uint8_t *to = x + down(where[k], q);
+                    *(uint16_t *)to = h.e[q];
+                    *(uint16_t *)(to + kOrthoTile) = l.e[q];
+                }
+            }
+        });
+    };
+    if (fours) take(std::integral_constant<int, 4>()); else take(std::integral_constant<int, 1>());
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == 0) ctl->part[warp] = s;
@@ -318,6 +368,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
                         w[k][4] += f1.x; w[k][5] += f1.y; w[k][6] += f1.z; w[k][7] += f1.w;
                     }
             }
+            fence_proxy_async_cluster();
             cluster_sync_all();
 #pragma unroll
             for (int k = 0; k < kSets; ++k) {
@@ -328,19 +379,32 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
                 for (int e = 0; e < 8; ++e) f[e] = w[k][e] * (1.f / kOrthoScale);
                 uint4 h, l;
                 to_pairs(f, h, l);
-                const uint32_t at = (uint32_t)(c >> 6) * kSTile + ortho_chunk(r, (c & 63) >> 3);
-                for (int b = 0; b < blocks; ++b) {
-                    const uint32_t to = cluster_addr(ap, b) + at;
-                    st_cluster_v4(to, h);
-                    st_cluster_v4(to + kOrthoTile, l);
+                uint8_t *to = ap + (uint32_t)(c >> 6) * kSTile + ortho_chunk(r, (c & 63) >> 3);
+                *(uint4 *)to = h;
+                *(uint4 *)(to + kOrthoTile) = l;
+            }
+            // its rows, side by side in each tile, to every other block by bulk copies (by the threads' stores of 16 bytes, a line each, the
+            // round took 9400 clocks of 128 x 1152's 34000 a step)
+            fence_proxy_async_smem();
+            __syncthreads();
+            const int mine = max(0, min(share, m16 - rank * share)), parts = 2 * ((m16 + 63) / 64);
+            if (threadIdx.x == 0 && m16 > mine) mbar_arrive_expect_tx(&ctl->rows, (m16 - mine) * 128 * parts);
+            if (mine > 0)
+                for (int i = threadIdx.x; i < blocks * parts; i += kSThreads) {
+                    const int to = i / parts, part = i - to * parts;
+                    if (to == rank) continue;
+                    uint8_t *from = ap + part * kOrthoTile + rank * share * 128;
+                    bulk_send(cluster_addr(from, to), smem_u32(from), mine * 128, cluster_addr(&ctl->rows, to));
                 }
+            if (m16 > mine) {
+                if (!mbar_wait_bounded(&ctl->rows, step & 1, nullptr) && threadIdx.x == 0) atomicOr(err, ERRW_TIMEOUT);
             }
         }
         tc_fence_before_sync();
         // ---- P = b A + c A A, where A is ----
         // (the first of a thread's old numbers are read while the tensor core works)
         const int c0 = fourth * 16;
-        product(ap_at, ap_at, false, m16, m16 / 16, blocks > 1);
+        product(ap_at, ap_at, false, m16, m16 / 16, false);
         if (rows_here && c0 < m16) read(ap, c0, old);
         finished(m16 / 16);
         if (rows_here)
@@ -369,31 +433,40 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
     }
     __syncthreads();
     // ---- out, in the order of memory ----
-    for (int e0 = threadIdx.x; e0 < count; e0 += 16 * kSThreads) {
-        float o[16], old[16];
-        int at[16];
+    auto give = [&](auto side) {
+        constexpr int V = decltype(side)::value, B = 16 / V;
+        in_order(side, [&](const int (&at)[B], const uint32_t (&where)[B], int here) {
+            Few<float, V> o[B], old[B];
+            if (tab.muon)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const uint8_t *from = x + locate(min(e0 + k * kSThreads, count - 1), at[k]);
-            o[k] = __uint_as_float((uint32_t)*(const uint16_t *)from << 16 | *(const uint16_t *)(from + kOrthoTile)) * (1.f / kOrthoScale);
-        }
-        if (tab.muon) {
+                for (int k = 0; k < B; ++k)
+                    if (k < here) old[k] = load<V>(it.master + base + at[k]);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) old[k] = (it.master + base)[at[k]];
+            for (int k = 0; k < B; ++k)
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                if (e0 + k * kSThreads >= count) break;
-                o[k] = fmaf(-it.scale, o[k], tab.keep * old[k]);
-                (it.master + base)[at[k]] = o[k];
+                for (int q = 0; q < V; ++q) {
+                    if (k >= here) continue;
+                    const uint8_t *from = x + (tall ? down(where[k], q) : where[k] + q * 2u);
+                    o[k].e[q] = __uint_as_float((uint32_t)*(const uint16_t *)from << 16 | *(const uint16_t *)(from + kOrthoTile)) * (1.f / kOrthoScale);
+                }
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                if (k >= here) break;
+                if (tab.muon) {
+#pragma unroll
+                    for (int q = 0; q < V; ++q) o[k].e[q] = fmaf(-it.scale, o[k].e[q], tab.keep * old[k].e[q]);
+                    *(Few<float, V> *)(it.master + base + at[k]) = o[k];
+                }
+                if (it.out) {
+                    Few<T, V> r;
+#pragma unroll
+                    for (int q = 0; q < V; ++q) r.e[q] = from_f32<T>(o[k].e[q]);
+                    *(Few<T, V> *)((T *)it.out + base + at[k]) = r;
+                }
             }
-        }
-        if (it.out)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                if (e0 + k * kSThreads >= count) break;
-                ((T *)it.out + base)[at[k]] = from_f32<T>(o[k]);
-            }
-    }
+        });
+    };
+    if (fours) give(std::integral_constant<int, 4>()); else give(std::integral_constant<int, 1>());
     __syncthreads();
     if (blocks > 1) cluster_sync_all();
     if (warp == 0) tmem_dealloc(tmem, 512);
