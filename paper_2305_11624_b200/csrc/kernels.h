@@ -439,8 +439,8 @@ bool ortho_wide(int rows, int cols);
 // Fills rt .. bytes of all items from rows, cols, count, and the phases; returns the bytes of the workspace.
 size_t ortho_plan(OrthoTable &t, bool wide);
 cudaError_t launch_ortho(const OrthoTable &t, void *workspace, cudaStream_t st);
-// All matrices with a shorter side of at most 128, kept on chip (ortho_small.cu).
-bool ortho_small_eligible(const OrthoTable &t);
+// Matrices with a shorter side of at most 128 and a longer one of at most 4096, kept on chip: whether that is the shorter way (ortho_small.cu).
+bool ortho_small_pays(const OrthoTable &t);
 cudaError_t launch_ortho_small(const OrthoTable &t, cudaStream_t st);
 
 }  // namespace convbn

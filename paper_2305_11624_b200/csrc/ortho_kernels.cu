@@ -815,7 +815,7 @@ size_t ortho_plan(OrthoTable &t, bool wide) {
 }
 
 cudaError_t launch_ortho(const OrthoTable &t, void *workspace, cudaStream_t st) {
-    if (ortho_small_eligible(t)) return launch_ortho_small(t, st);
+    if (ortho_small_pays(t)) return launch_ortho_small(t, st);
     switch (t.dtype) {
         case CONVBN_F32: return launch_ortho_t<float>(t, (uint8_t *)workspace, st);
         case CONVBN_F16: return launch_ortho_t<__half>(t, (uint8_t *)workspace, st);

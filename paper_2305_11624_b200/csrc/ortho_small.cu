@@ -21,7 +21,7 @@ namespace {
 constexpr int kSThreads = 512;                          // sixteen warps: a row of sums is four threads' work
 constexpr uint32_t kSTile = 2 * kOrthoTile;            // 128 rows x 64 columns, hi and lo
 constexpr int kSMaxWidth = 256;
-constexpr int kSMaxCluster = 8;
+constexpr int kSMaxCluster = 16;                       // (more than eight where the device has room for such a cluster)
 
 struct SmallCtl {
     uint64_t done, rows;                               // a product; the other blocks' rows of A
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
         } else {
             // part by part to the block that has the row: [block][4 columns][its rows] in fp32, where P was (rows side by side, as a warp has
             // them: with a row's columns side by side the sums' round took 7 us)
-            const int share = 128 / blocks;                           // (blocks: a power of two)
+            const int share = 128 / blocks;                           // (blocks: a power of two, 16 at most)
             if (rows_here) {
                 const uint32_t to = cluster_addr(ap, row / share) + (rank * 32 * share + row % share) * 16;
                 for (int c = fourth * 16; c < m16; c += 64) {
@@ -488,21 +488,13 @@ bool small_shape(const OrthoTable &t, SmallShape *s) {
 }
 
 template <class T>
-cudaError_t launch_small_t(const OrthoTable &t, const SmallShape &s, cudaStream_t st) {
-    int *err = nullptr;
-    if (cudaError_t e = error_word_address(&err); e != cudaSuccess) return e;
-    auto kernel = ortho_small_kernel<T>;
-    static PerDevice attr;
-    // The whole shared memory whatever the width: blocks of two clusters on one SM could each hold the tensor memory that the other cluster
-    // waits for.
-    const int smem = 1024 + (kSMaxWidth / 64 + 2) * (int)kSTile + (int)sizeof(SmallCtl);
-    if (cudaError_t e = max_dynamic_smem_once(kernel, smem, &attr); e != cudaSuccess) return e;
+cudaLaunchConfig_t small_config(const OrthoTable &t, const SmallShape &s, cudaLaunchAttribute (&at)[2]) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(t.matrices * s.blocks));
     cfg.blockDim = dim3(kSThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute at[2];
+    // The whole shared memory whatever the width: blocks of two clusters on one SM could each hold the tensor memory that the other cluster
+    // waits for.
+    cfg.dynamicSmemBytes = 1024 + (kSMaxWidth / 64 + 2) * kSTile + sizeof(SmallCtl);
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
@@ -510,14 +502,74 @@ cudaError_t launch_small_t(const OrthoTable &t, const SmallShape &s, cudaStream_
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = s.blocks > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, t, s, err);
+    return cfg;
+}
+template <class T>
+cudaError_t small_attributes() {
+    static PerDevice smem, wide;
+    auto kernel = ortho_small_kernel<T>;
+    if (cudaError_t e = max_dynamic_smem_once(kernel, 1024 + (kSMaxWidth / 64 + 2) * (int)kSTile + (int)sizeof(SmallCtl), &smem); e != cudaSuccess) return e;
+    bool &done = wide.done[current_device_slot()];
+    if (done) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) done = true;
+    return e;
+}
+// Whether the device holds such clusters (of sixteen blocks not every one does), and this is the shorter way.  A B200 runs 7 clusters of sixteen blocks at
+// a time, 15 of eight, 33 of four, 74 of two; the next ones are another round, where the kernel for large matrices fills the SMs and its chain of
+// waits is paid once.  Estimates in us, five steps.  Measured, this kernel and the other, fp32: one 16 x 2268 44 and 119, one 128 x 4096 99 and 130; eight of those
+// 258 and 157; 128 x 2048 by 8 97 and 131, by 16 188 and 146; 64 x 64 by 512 78 and 276.
+template <class T>
+bool small_pays(const OrthoTable &t, const SmallShape &s) {
+    static int known[kMaxDevices][5];                  // clusters at a time + 1
+    int log = 0;
+    while (1 << log < s.blocks) ++log;
+    int &answer = known[current_device_slot()][log];
+    if (answer == 0 && s.blocks == 1) answer = device_sm_count() + 1;
+    if (answer == 0) {
+        cudaLaunchAttribute at[2];
+        const cudaLaunchConfig_t cfg = small_config<T>(t, s, at);
+        int fit = 0;
+        if (small_attributes<T>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&fit, ortho_small_kernel<T>, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            fit = 0;
+        }
+        answer = fit + 1;
+    }
+    const int fit = answer - 1;
+    if (fit < 1) return false;
+    int side = 0;
+    float other = 110.f;
+    for (int i = 0; i < t.items; ++i) {
+        const OrthoItem &it = t.item[i];
+        side = std::max(side, std::min(it.rows, it.cols));
+        other += (it.wide ? 0.037f : 0.06f) * (float)(3 * std::max(it.rt, it.ct) + 1) * (float)it.count;
+    }
+    const float round = 10.f + (float)side * (0.15f + 0.001f * (float)s.width) + (s.blocks > 1 ? 30.f : 0.f);
+    return t.matrices <= fit || round * (float)((t.matrices + fit - 1) / fit) <= other;
+}
+
+template <class T>
+cudaError_t launch_small_t(const OrthoTable &t, const SmallShape &s, cudaStream_t st) {
+    int *err = nullptr;
+    if (cudaError_t e = error_word_address(&err); e != cudaSuccess) return e;
+    if (cudaError_t e = small_attributes<T>(); e != cudaSuccess) return e;
+    cudaLaunchAttribute at[2];
+    cudaLaunchConfig_t cfg = small_config<T>(t, s, at);
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, ortho_small_kernel<T>, t, s, err);
 }
 
 }  // namespace
 
-bool ortho_small_eligible(const OrthoTable &t) {
+bool ortho_small_pays(const OrthoTable &t) {
     SmallShape s;
-    return small_shape(t, &s);
+    if (!small_shape(t, &s)) return false;
+    switch (t.dtype) {
+        case CONVBN_F32: return small_pays<float>(t, s);
+        case CONVBN_F16: return small_pays<__half>(t, s);
+        default: return small_pays<__nv_bfloat16>(t, s);
+    }
 }
 
 cudaError_t launch_ortho_small(const OrthoTable &t, cudaStream_t st) {

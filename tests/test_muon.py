@@ -143,6 +143,28 @@ def test_orthogonalise(shape, kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("count,rows,cols", [(1, 16, 2268), (2, 4096, 128), (1, 3001, 30), (9, 64, 2052), (1, 40, 4097), (16, 128, 1500), (40, 36, 1030), (300, 8, 12)])
+def test_lengths_and_stacks_on_either_side_of_the_choices(count, rows, cols):
+    """One matrix on chip in a cluster, as many as run at a time, and more; elements by fours, and one off where fours could lie."""
+    import torch
+    g = matrices("noise", count, rows, cols)
+    got = orthogonalise(g)
+    for i in {0, count // 2, count - 1}:
+        ref = M.orthogonalise(g[i].double().numpy(), 5, EPS)
+        assert np.linalg.norm(got[i].double().cpu().numpy() - ref) <= allowed(ref, "f32", 5)
+    room = torch.full((2, count * rows * cols + 2), 7.0, device="cuda")
+    room[0, 1:-1] = g.flatten().cuda()
+    views = [r[1:-1].view(count, rows, cols) for r in room]
+    ws = torch.empty(C.convbn_orthogonalise_workspace_bytes(rows, cols, count), dtype=torch.uint8, device="cuda")
+    C.convbn_orthogonalise(views[0], views[1], 5, EPS, ws)
+    C.convbn_check()
+    close = [np.linalg.norm((a - b).double().cpu().numpy()) for a, b in zip(views[1], got)]
+    # (the norm's squares are added up in another order, in 64 bits: at most a rounding of the scale)
+    assert max(close) <= 2 * allowed(M.orthogonalise(g[0].double().numpy(), 5, EPS), "f32", 5)
+    assert room[1, 0] == 7 and room[1, -1] == 7
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("shape", [(64, 64), (256, 1152), (1152, 256), (512, 2048)], ids=str)
 def test_as_near_as_documented(shape):
     """As near as the formula in fp32 comes.  That is 1e-5 for these matrices, whose noise, 2^-8 of the whole, becomes most of the result:
