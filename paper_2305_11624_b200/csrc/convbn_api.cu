@@ -1822,7 +1822,9 @@ static size_t ortho_stack(OrthoTable &t, int dtype, int rows, int cols, int coun
     t.item[0].cols = cols;
     t.item[0].count = count;
     // (an fp32 result shows what several steps at a time lose, 2 to 3 times the direct ones' error; the others' rounding hides it)
-    return ortho_plan(t, dtype != CONVBN_F32 && ortho_wide(rows, cols));
+    OrthoChoice choice;
+    choice.add(rows, cols, count);
+    return ortho_plan(t, dtype != CONVBN_F32 && choice.wide());
 }
 
 size_t convbn_orthogonalise_workspace_bytes(int rows, int cols, int count) {
@@ -1866,11 +1868,12 @@ static int muon_launch(const convbn_muon_layer *layers, int count, int from, Ort
     }
     return i;
 }
-// f(table, its workspace's bytes, its first layer) for every launch.  Steps go over m x m matrices for all layers if that pays for one: it is as
-// much work for square ones.
+// f(table, its workspace's bytes, its first layer) for every launch.  Steps go over m x m matrices for all layers or for
+// none: it is as much work for square ones.
 static int muon_launches(const convbn_muon_layer *layers, int count, int steps, const std::function<int(OrthoTable &, size_t, int)> &f) {
-    bool wide = false;
-    for (int i = 0; i < count; ++i) wide |= ortho_wide(layers[i].rows, layers[i].cols);
+    OrthoChoice choice;
+    for (int i = 0; i < count; ++i) choice.add(layers[i].rows, layers[i].cols, 1);
+    const bool wide = choice.wide();
     for (int from = 0; from < count;) {
         OrthoTable t = {};
         const int next = muon_launch(layers, count, from, &t);

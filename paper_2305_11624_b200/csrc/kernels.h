@@ -434,8 +434,13 @@ struct OrthoTable {
     double eps;
     OrthoItem item[kOrthoItems];
 };
-// Whether the items' steps go over m x m matrices (ortho.cuh) rather than over X.
-bool ortho_wide(int rows, int cols);
+// Whether the steps of a list's matrices go over m x m matrices (ortho.cuh) rather than over X.
+struct OrthoChoice {
+    bool longer = false;
+    double saved = 0.;
+    void add(int rows, int cols, int count);
+    bool wide() const;
+};
 // Fills rt .. bytes of all items from rows, cols, count, and the phases; returns the bytes of the workspace.
 size_t ortho_plan(OrthoTable &t, bool wide);
 cudaError_t launch_ortho(const OrthoTable &t, void *workspace, cudaStream_t st);

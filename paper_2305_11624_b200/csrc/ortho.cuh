@@ -26,11 +26,31 @@ constexpr float kOrthoCoefA = 3.4445f, kOrthoCoefB = -4.7750f, kOrthoCoefC = 2.0
 // Offset of the 16-byte chunk of 8 columns `chunk` of row `row` in a tile.
 __host__ __device__ __forceinline__ uint32_t ortho_chunk(uint32_t row, uint32_t chunk) { return row * 128u + ((chunk ^ (row & 7u)) << 4); }
 
+// 2^10 / (|G| + eps) as a power of two, in two factors, and a fraction of 48 bits: a product in 64 bits is two conversions an element, of
+// which an SM does sixteen a clock (a quarter of the time of putting a matrix into tiles).
+struct OrthoScaling {
+    float two_a, two_b, hi, lo;
+    __device__ __forceinline__ static OrthoScaling of(double squares, double eps) {
+        int power;
+        const double part = frexp((double)kOrthoScale / (sqrt(squares) + eps), &power);
+        OrthoScaling s;
+        s.two_a = ldexpf(1.f, power / 2);
+        s.two_b = ldexpf(1.f, power - power / 2);
+        s.hi = (float)part;
+        s.lo = (float)(part - (double)s.hi);
+        return s;
+    }
+    __device__ __forceinline__ float operator()(float g) const {
+        const float u = g * two_a * two_b;
+        return fmaf(u, hi, u * lo);
+    }
+};
+
 // The products.  All steps of X at a time, direct:
 //     A = X X^T        R = b A + c A A        X <- a X + R X
 // or, where X is long, on m x m matrices, all polynomials of one A, which commute and are symmetric: k steps are X <- Q X with
 //     A = X X^T;   k times:  R = b A + c A A;   Q <- (a + R) Q  (from 1);   B = (a + R) A;   A <- (a + R) B        then X <- Q X
-// For k = 3 and 2 five steps are 6 m^2 n + 14 m^3 multiplications (symmetric products half) where the direct ones are 15 m^2 n + 5 m^3, and two
+// For k = 3 and 2 five steps are 6 m^2 n + 14 m^3 operations (symmetric products half) where the direct ones are 15 m^2 n + 5 m^3, and two
 // sums over all of X's columns where they are five.  The price is precision: A's rounding, which belongs to all singular values alike, grows
 // by 3.4445^2 a step for the small ones.  After three steps X is formed and A from it anew; so the results are as near to the formula as fp32
 // products bring them (with stages of 2 and 3 steps it is twice to four times as far, with one of five ten times).

@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const __grid_constant__
 template <class T>
 __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__ OrthoTable tab, uint8_t *__restrict__ ws) {
     __shared__ double part[8];
+    __shared__ OrthoScaling scaling;
     pdl_wait();
     pdl_launch_dependents();
     const int task = blockIdx.x;
@@ -161,13 +162,17 @@ __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
     __syncthreads();
-    s = part[0];
-    for (int i = 1; i < 8; ++i) s += part[i];
-    const double inv = (double)kOrthoScale / (sqrt(s) + tab.eps);
+    if (threadIdx.x == 0) {
+        s = part[0];
+        for (int i = 1; i < 8; ++i) s += part[i];
+        scaling = OrthoScaling::of(s, tab.eps);
+    }
+    __syncthreads();
+    const OrthoScaling scaled = scaling;
     uint8_t *hi = m + place.x(0) + (long long)tile * kOrthoTile, *lo = hi + place.x_bytes;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const float x[4] = {(float)(u[k].x * inv), (float)(u[k].y * inv), (float)(u[k].z * inv), (float)(u[k].w * inv)};
+        const float x[4] = {scaled(u[k].x), scaled(u[k].y), scaled(u[k].z), scaled(u[k].w)};
         __half2 h[2], l[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -182,10 +187,15 @@ __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__
 }
 
 // ---- products ---------------------------------------------------------------------------------------------------------------------
-// All products of all steps in one launch (what they are: ortho.cuh).  CTA = 10 warps: 0 takes tasks and loads, 1 MMA issuer and owner of tensor memory, 2-9 epilogue.
+// All products of all steps in one launch (what they are: ortho.cuh).  CTA = 10 warps: 0 takes tasks and loads, 1 MMA issuer and owner of tensor
+// memory, 2-9 epilogue.
 // A task is a 128 x 128 (or 128 x 64) tile of a result (or a piece of the k of one of A's); k in steps of 64.  A step's four tiles (hi and lo of
-// both operands) are 64 KB and feed eight MMAs: hi of A with hi and lo of B, side by side as 256 columns, and lo of A with hi of B.  What a task adds to its product is brought by bulk copies too: read by the
-// rows' own threads it took 7000 clocks of a task, 32 lines an instruction.  hi hi is summed apart from the other two products: the tensor core's sums drift towards zero
+// both operands) are 64 KB and feed eight MMAs: hi of A with hi and lo of B, side by side as 256 columns, and lo of A with hi of B.  What a task
+// adds to its product is brought by bulk copies too: read by the rows' own threads it took 7000 clocks of a task, 32 lines an instruction.
+// Bound, where X is large, by these copies: a step takes 1150 to 1250 clocks, its MMAs 768, and 52 bytes a clock come from L2 to each SM.
+// Two 2048 x 8192 in bf16: MMAs busy 61 % of 1.73 ms.  Where X is small, by the chain of products: 512 x 4608 in fp32 (185 us) is fifteen of them one
+// after the other, each waiting for the last one's results (about 1 us from its last MMA to the next one's first tile) and its own sums.
+// hi hi is summed apart from the other two products: the tensor core's sums drift towards zero
 // with their length, and those of small numbers do not notice.  For the same reason a long sum is cut: the epilogue adds the
 // pieces up in registers, in fp32 with rounding.  Pieces are of 256 k for fp32 results (512 x 4608: error 1.1e-6; 2e-6 with 512, 3e-6 with 1024,
 // 1 to 2 % faster each) and of 1024 k where the result is rounded to 16 bits or is a small part of a weight.
@@ -729,8 +739,16 @@ cudaError_t launch_ortho_t(const OrthoTable &t, uint8_t *ws, cudaStream_t st) {
 
 }  // namespace
 
-// Two steps at a time or more pay where X is at least twice as long as it is high.
-bool ortho_wide(int rows, int cols) { return std::max(rows, cols) >= 2LL * std::min(rows, cols); }
+// Two steps at a time or more save 9 m^2 (n - m) operations of five steps', and cost two more products in the chain: they pay where X is long, so that the
+// chain is of shorter products, and where there is much to save.  us in bf16, directly and so: 512 x 4608 188 and 170, 256 x 1152 128 and 119, 512 x 1536
+// 152 and 153, 1000 x 2048 232 and 239, 512 x 768 144 and 148; 2048 x 2560 658 and 586, three of 1956 x 3501 2043 and 1665, two of 988 x 1865
+// (saved / 9: 1.7e9) 369 and 335, 1024 x 2048 (1.1e9) 233 and 239.
+void OrthoChoice::add(int rows, int cols, int count) {
+    const double m = std::min(rows, cols), n = std::max(rows, cols);
+    longer |= n >= 2.5 * m;
+    saved += m * m * (n - m) * count;
+}
+bool OrthoChoice::wide() const { return longer || saved > 1.3e9; }
 
 static void ortho_phases(OrthoTable &t, bool wide) {
     int x = 0, lowers = 0, xs = 0, at = 0, n = 0;
