@@ -190,7 +190,10 @@ __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__
 // All products of all steps in one launch (what they are: ortho.cuh).  CTA = 10 warps: 0 takes tasks and loads, 1 MMA issuer and owner of tensor
 // memory, 2-9 epilogue.
 // A task is a 128 x 128 (or 128 x 64) tile of a result (or a piece of the k of one of A's); k in steps of 64.  A step's four tiles (hi and lo of
-// both operands) are 64 KB and feed eight MMAs: hi of A with hi and lo of B, side by side as 256 columns, and lo of A with hi of B.  What a task
+// both operands) are 64 KB and feed twelve MMAs of one shape: hi hi into one half of the accumulator's 256 columns, hi lo and lo hi into the other.
+// MMAs keep the order of issue only where accumulator and shape are the same, so hi of A with hi and lo of B side by side, one MMA instead of
+// two, would need columns that lo hi does not touch.  128 x 64 tiles have them, and gain (A's rows come once less from shared memory: 512 x 4608
+// 194 us instead of 200); 128 x 128 ones do not, and would not: two 2048 x 8192 take 2126 us, 2110 with the two products on shared columns.  What a task
 // adds to its product is brought by bulk copies too: read by the rows' own threads it took 7000 clocks of a task, 32 lines an instruction.
 // Bound, where X is large, by these copies: a step takes 1150 to 1250 clocks, its MMAs 768, and 52 bytes a clock come from L2 to each SM.
 // Two 2048 x 8192 in bf16: MMAs busy 61 % of 1.73 ms.  Where X is small, by the chain of products: 512 x 4608 in fp32 (185 us) is fifteen of them one
@@ -487,7 +490,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                 const OrthoTask k = ortho_task(tab, ws, t);
                 OrthoOperand a, b;
                 ortho_operands(k, a, b);
-                const uint32_t n_one = k.narrow ? 64 : 128, both0 = idesc_h16_f32(128, 2 * n_one, 0, 0, 1), one0 = idesc_h16_f32(128, n_one, 0, 0, 1);
+                const uint32_t one0 = idesc_h16_f32(128, k.narrow ? 64 : 128, 0, 0, 1), b_lo = kOrthoTile >> 4;
                 for (int s = k.from; s < k.to; ++s) {
                     const uint32_t acc = acc_it & 1u, d = tmem_base + acc * 256u, first = (uint32_t)(s - k.from) & segment_mask;
                     if (first == 0) {
@@ -495,7 +498,7 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                         if (!ok) break;
                         tc_fence_after_sync();
                     }
-                    // major: bit 15 of the descriptors A's, 16 B's; the leading byte offset is 8192 then, else 16
+                    // bit 15 of the instruction's descriptor: A MN-major, 16: B; the leading byte offset is 8192 then, else 16
                     const uint32_t a_mn = s >= a.turn, b_mn = s >= b.turn, major = a_mn << 15 | b_mn << 16;
                     const uint32_t sa = a_mn ? 128u : 2u, sb = b_mn ? 128u : 2u;
                     ok = mbar_wait_bounded(full0 + slot * 8, ph, abort_flag);
@@ -507,10 +510,21 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
                     if (!ok) break;
                     const uint32_t b_hi = tiles_lo + slot * (kOSlot >> 4) + (b_mn ? 512u << 16 : 1u << 16), done_b = empty0 + slot * 8;
                     if (++slot == kOSlots) { slot = 0; ph ^= 1u; }
+                    if (k.narrow) {
+                        const uint32_t both = idesc_h16_f32(128, 128, 0, 0, 1) | major, one = one0 | major;
 #pragma unroll
-                    for (uint32_t q = 0; q < 4; ++q) {
-                        umma_bf16_ss_sel(d, a_hi + q * sa, hi, b_hi + q * sb, hi, both0 | major, first + q);
-                        umma_bf16_ss_halves<true>(d + n_one, a_lo + q * sa, hi, b_hi + q * sb, hi, one0 | major);
+                        for (uint32_t q = 0; q < 4; ++q) {
+                            umma_bf16_ss_sel(d, a_hi + q * sa, hi, b_hi + q * sb, hi, both, first + q);
+                            umma_bf16_ss_sel(d + 128, a_lo + q * sa, hi, b_hi + q * sb, hi, one, first + q);
+                        }
+                    } else {
+                        const uint32_t one = one0 | major;
+#pragma unroll
+                        for (uint32_t q = 0; q < 4; ++q) {
+                            umma_bf16_ss_sel(d, a_hi + q * sa, hi, b_hi + q * sb, hi, one, first + q);
+                            umma_bf16_ss_sel(d + 128, a_hi + q * sa, hi, b_hi + b_lo + q * sb, hi, one, first + q);
+                            umma_bf16_ss_halves<true>(d + 128, a_lo + q * sa, hi, b_hi + q * sb, hi, one);
+                        }
                     }
                     umma_commit(done_a);
                     umma_commit(done_b);
@@ -602,9 +616,15 @@ __global__ void __launch_bounds__(kOThreads, 1) ortho_product_kernel(const __gri
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t p[32], q[32];
-                    tmem_ld_32x32(from + h * 32, p);
-                    tmem_ld_32x32(from + (k.narrow ? 64 : 128) + h * 32, q);
+                    tmem_ld_32x32(from + (k.narrow ? 64 : 0) + h * 32, p);
+                    tmem_ld_32x32(from + 128 + h * 32, q);
                     tmem_ld_wait();
+                    if (k.narrow) {                             // hi hi | hi lo | lo hi
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) q[i] = __float_as_uint(__uint_as_float(p[i]) + __uint_as_float(q[i]));
+                        tmem_ld_32x32(from + h * 32, p);
+                        tmem_ld_wait();
+                    }
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[h * 32 + i] = fmaf(f_new, __uint_as_float(p[i]) + __uint_as_float(q[i]), v[h * 32 + i]);
                 }
