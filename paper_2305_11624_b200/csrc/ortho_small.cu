@@ -394,6 +394,9 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
             if (m16 > mine) {
                 if (!mbar_wait_bounded(&ctl->rows, step & 1, nullptr) && threadIdx.x == 0) atomicOr(err, ERRW_TIMEOUT);
             }
+            // (A's rows have come: said to the blocks they came from, which read them until then and write P over them below)
+            __syncwarp();
+            cluster_arrive_all();
         }
         tc_fence_before_sync();
         // ---- P = b A + c A A, where A is ----
@@ -402,6 +405,10 @@ __global__ void __launch_bounds__(kSThreads, 1) ortho_small_kernel(const __grid_
         product(ap_at, ap_at, false, m16, m16 / 16, false);
         if (rows_here && c0 < m16) read(ap, c0, old);
         finished(m16 / 16);
+        if (blocks > 1) {
+            __syncwarp();
+            cluster_wait_all();
+        }
         if (rows_here)
             for (int c = c0; c < m16; c += 64) {
                 if (c != c0) read(ap, c, old);

@@ -27,3 +27,36 @@ def same_bits(shape, dtype, steps=5, times=20):
                                          ((3, 300, 1030), "f32"), ((1, 1500, 1400), "f16")], ids=str)
 def test_large_matrices(shape, dtype):
     assert not any(same_bits(shape, dtype))
+
+
+# (clusters of 2, 4, 8 and 16 blocks; all of A's rows in one block's share, or in some; tall ones; more matrices than run at a time)
+CLUSTERS = [(1, 128, 1152), (1, 1152, 128), (1, 64, 300), (1, 16, 2268), (3, 100, 4000), (2, 4096, 128), (1, 33, 1025), (20, 128, 600)]
+
+
+@pytest.mark.parametrize("shape", CLUSTERS, ids=str)
+def test_clusters(shape):
+    """Blocks of a cluster send one another rows of A by copies that nothing in the sending block waits for, and write P where A was."""
+    assert not any(same_bits(shape, "f32", times=100))
+
+
+@pytest.mark.parametrize("kind", ["noise", "few"])
+@pytest.mark.parametrize("shape", CLUSTERS, ids=str)
+def test_clusters_are_as_near_as_the_formula_in_fp32(shape, kind):
+    """Tolerance, 2-norm.  X, A and P are rounded to 22 bits where the fp32 formula rounds these and what lies between them to 24: at most four
+    times its error.  An MMA cuts its sum below 2^-23, by half of that in the mean; 16 of them on an accumulator, of at most 256 columns, are
+    2^-20 of A, which moves X by at most 0.9 as much of itself, in each of five steps.  A row whose low halves were lost would be off by 2^-12."""
+    import numpy as np
+    from oracle import muon_oracle as M
+    from test_muon import matrices, orthogonalise
+    g = matrices(kind, *shape, seed=6)
+    got = orthogonalise(g).double().cpu().numpy()
+    a, b, c = (np.float32(v) for v in M.COEFFICIENTS)
+    for i in {0, shape[0] - 1}:
+        ref = M.orthogonalise(g[i].double().numpy(), 5, 1e-7)
+        x = g[i].numpy() / np.float32(np.linalg.norm(g[i].double().numpy()))
+        for _ in range(5):
+            s = x @ x.T if shape[1] <= shape[2] else x.T @ x
+            p = b * s + c * (s @ s)
+            x = a * x + (p @ x if shape[1] <= shape[2] else x @ p)
+        allowed = 4 * np.linalg.norm(x - ref) + 5 * 2.0 ** -20 * np.linalg.norm(ref)
+        assert np.linalg.norm(got[i] - ref) <= allowed, np.linalg.norm(got[i] - ref) / allowed
