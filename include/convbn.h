@@ -433,7 +433,7 @@ int convbn_group_norm_bwd(const convbn_group_norm_desc *desc, const void *dz, co
  * `dtype`; out may be g.  Products are formed from pairs of halves (22 significant bits) with fp32 sums, squares of the norm in 64 bits; one
  * rounding, to `dtype`, at the end.  fp32 results are as near to the formula as fp32 products bring them: 1e-6 (2-norm) for a matrix of noise, 1e-5
  * for one of a few strong directions, whose noise the steps lift.
- * A zero matrix gives zeros; one that holds a NaN or an infinity gives NaN, others are not touched by it.
+ * A zero matrix gives zeros, also with eps = 0; one that holds a NaN or an infinity gives NaN, others are not touched by it.
  *
  * convbn_muon_step: one step of the optimiser over `count` layers of C_out = rows and cols weights per output channel (any weight layout of
  * this library), in one call:

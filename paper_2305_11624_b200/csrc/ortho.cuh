@@ -30,7 +30,9 @@ __host__ __device__ __forceinline__ uint32_t ortho_chunk(uint32_t row, uint32_t 
 // which an SM does sixteen a clock (a quarter of the time of putting a matrix into tiles).
 struct OrthoScaling {
     float two_a, two_b, hi, lo;
+    // (a zero matrix has no quotient where eps is none either: zeros stay zeros; a sum that is no number passes through)
     __device__ __forceinline__ static OrthoScaling of(double squares, double eps) {
+        if (squares == 0.) return {1.f, 1.f, 0.f, 0.f};
         int power;
         const double part = frexp((double)kOrthoScale / (sqrt(squares) + eps), &power);
         OrthoScaling s;

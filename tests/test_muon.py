@@ -309,3 +309,31 @@ def test_two_streams_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     C.convbn_check()
     assert all(torch.equal(a, b) for a, b in zip(ref, out))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("eps", [0.0, 1e-300, 1e-7])
+@pytest.mark.parametrize("rows,cols", [(20, 30), (64, 700), (130, 200)])
+def test_a_zero_matrix_whatever_eps_is(rows, cols, eps):
+    """Zeros on chip, in a cluster and in tiles; beside it what is no number still is none, and the smallest numbers are as good as any."""
+    import torch
+    g = torch.zeros(4, rows, cols)
+    g[1] = matrices("noise", 1, rows, cols)[0] * 1e3
+    g[2] = (g[1].double() * 2.0 ** -126).float()
+    g[3, 1, 2] = float("nan")
+    got = orthogonalise(g, eps=eps)
+    assert bool((got[0] == 0).all()) and bool(torch.isnan(got[3]).all())
+    for i in (1, 2) if eps < 1e-7 else (1,):
+        ref = M.orthogonalise(g[i].double().numpy(), 5, eps)
+        assert np.linalg.norm(got[i].double().cpu().numpy() - ref) <= allowed(ref, "f32", 5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(20, 30), (130, 200)])
+def test_muon_step_of_nothing(rows, cols):
+    """A layer that had no gradient yet: its weights decay and stay numbers, also without eps."""
+    import torch
+    zero, master = torch.zeros(rows, cols), torch.randn(rows, cols, generator=torch.Generator().manual_seed(1))
+    p = C.MuonParams.make(lr=0.5, momentum=0.9, weight_decay=0.25, eps=0.0)
+    (v, m, w), = muon([(zero, zero, master)], "bf16", p)
+    assert bool((v == 0).all()) and torch.equal(m.cpu(), master * 0.875) and torch.equal(w, m.to(w.dtype))
