@@ -224,9 +224,10 @@ bool norm_argument(PyObject *o, char kind, const convbn_group_norm_desc *d, long
         number(o, s_get_device, true) != device)
         return false;
     if (kind != 'a' || number(o, s_dim, true) != 4) return true;
-    PyObject *shape = PyObject_GetAttr(o, s_shape), *last = shape && PyTuple_Check(shape) ? PyTuple_GetItem(shape, 3) : nullptr,
-             *second = last ? PyTuple_GetItem(shape, 1) : nullptr;
-    const bool fits = second && PyLong_Check(last) && PyLong_AsLong(last) == d->c && PyLong_AsLong(second) == d->h;
+    PyObject *shape = PyObject_GetAttr(o, s_shape);
+    bool fits = shape && PyTuple_Check(shape) && PyTuple_Size(shape) == 4;
+    const int extent[4] = {d->n, d->h, d->w, d->c};
+    for (int i = 0; fits && i < 4; ++i) fits = PyLong_AsLong(PyTuple_GetItem(shape, i)) == extent[i];
     Py_XDECREF(shape);
     PyErr_Clear();
     return fits;
