@@ -505,28 +505,49 @@ __global__ void __launch_bounds__(kThreads, kBlocks2) group_norm_bwd_sums_kernel
     }
 }
 
-// dgamma and dbeta: chan [runs][c] added up, 32 channels a block.
+// dgamma and dbeta: chan [runs][c] added up, 32 channels a block, in 64 bits: a batch has up to 2^30 runs, and after 2^24 like ones an fp32 sum
+// stands still.  (Sixteen of a warp's in fp32 first, their loads under way together.)
 __global__ void __launch_bounds__(1024) group_norm_finish_kernel(long long runs, int c, const float2 *__restrict__ chan, float *__restrict__ dgamma,
                                                                  float *__restrict__ dbeta) {
-    __shared__ float2 sums[1024];
+    __shared__ double2 sums[1024];
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, channel = blockIdx.x * 32 + lane;
-    float2 t = make_float2(0.f, 0.f);
+    double2 t = make_double2(0., 0.);
     if (channel < c) {
-#pragma unroll 4
-        for (long long i = warp; i < runs; i += 32) {
-            const float2 v = chan[i * c + channel];
-            t.x += v.x;
-            t.y += v.y;
+        constexpr int kBatch = 16;
+        const float2 *p = chan + (long long)warp * c + channel;
+        const long long pitch = 32LL * c;
+        long long left = (runs - warp + 31) / 32;                // of this warp
+        for (; left >= kBatch; left -= kBatch) {
+            float2 v[kBatch];
+#pragma unroll
+            for (int q = 0; q < kBatch; ++q) { v[q] = *p; p += pitch; }
+#pragma unroll
+            for (int q = 1; q < kBatch; ++q) { v[0].x += v[q].x; v[0].y += v[q].y; }
+            t.x += v[0].x;
+            t.y += v[0].y;
         }
+        float2 u = make_float2(0.f, 0.f);
+#pragma unroll 4
+        for (; left > 0; --left) {
+            u.x += p->x;
+            u.y += p->y;
+            p += pitch;
+        }
+        t.x += u.x;
+        t.y += u.y;
     }
     sums[threadIdx.x] = t;
     __syncthreads();
     if (warp == 0 && channel < c) {
-        for (int k = 1; k < 32; ++k) { t.x += sums[k * 32 + lane].x; t.y += sums[k * 32 + lane].y; }
-        dbeta[channel] = t.x;
-        dgamma[channel] = t.y;
+        double2 v[4] = {t, sums[32 + lane], sums[64 + lane], sums[96 + lane]};
+#pragma unroll
+        for (int k = 4; k < 32; ++k) { v[k % 4].x += sums[k * 32 + lane].x; v[k % 4].y += sums[k * 32 + lane].y; }
+        t.x = (v[0].x + v[1].x) + (v[2].x + v[3].x);
+        t.y = (v[0].y + v[1].y) + (v[2].y + v[3].y);
+        dbeta[channel] = (float)t.x;
+        dgamma[channel] = (float)t.y;
     }
 }
 

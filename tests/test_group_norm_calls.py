@@ -1,4 +1,4 @@
-"""Group norm's calls: what they refuse on the way to the kernels (GPU)."""
+"""Group norm's calls: what they refuse on the way to the kernels, and sums over many samples (GPU)."""
 import pytest
 
 from paper_2305_11624_b200 import convbn as C
@@ -38,3 +38,25 @@ def test_four_dimensions_in_another_order():
     dx, dg, db = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
     assert status(C.convbn_group_norm_bwd, d, z, x, gamma, beta, saved, other(dx), dg, db, ws) == C.EINVAL
     C.convbn_check()
+
+
+@pytest.mark.parametrize("c", [4, 6])                        # on chip; two passes
+def test_gradients_of_vectors_over_many_samples(c):
+    """Sums that fp32 additions one after the other lose: 32 large gradients, one for each warp, and many small ones.  Pairs of channels
+    hold (1, -1): xhat is that.  Tolerance: a value takes part in 15 fp32 additions at most, each off by half a step, 2^-24, of the
+    large ones' sum; then the result's own half step."""
+    import torch
+    n, groups = 65536 + 32, c // 2
+    d = C.NormDesc.make(n, c, 1, 1, groups, dtype=C.F32, eps=0.0)
+    sign = torch.tensor([1.0, -1.0], device="cuda").repeat(groups)
+    x, dx = sign.expand(n, 1, 1, c).contiguous(), torch.empty(n, 1, 1, c, device="cuda")
+    dz = torch.ones(n, 1, 1, c, device="cuda")
+    dz[:32] = 2.0 ** 24
+    gamma, beta, dgamma, dbeta = (torch.ones(c, device="cuda") for _ in range(4))
+    saved = torch.cat((torch.zeros(1, n, groups), torch.ones(1, n, groups))).cuda()
+    ws = torch.empty(C.convbn_group_norm_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    C.convbn_group_norm_bwd(d, dz, x, gamma, beta, saved, dx, dgamma, dbeta, ws)
+    C.convbn_check()
+    exact, allowed = 2.0 ** 29 + 65536, 15 * 2.0 ** -24 * 2.0 ** 29 + 32
+    assert bool(((dbeta - exact).abs() <= allowed).all()) and bool(((dgamma - exact * sign).abs() <= allowed).all())
+    assert allowed < 65536 / 16
