@@ -515,7 +515,22 @@ def convbn_group_norm_workspace_bytes(desc: NormDesc) -> int:
     return int(lib().convbn_group_norm_workspace_bytes(desc))
 
 
-def _norm_tensors(desc, where, activations, vectors, saved):
+def _on_current_gpu(tensors, where):
+    import torch
+    if any(not t.is_cuda for t in tensors) or any(t.get_device() != torch.cuda.current_device() for t in tensors):
+        _raise(EINVAL, "%s: tensors of the current GPU are needed" % where)
+
+
+def _room(workspace, where):
+    """EINVAL for a workspace (not an address, not None) whose bytes are not one piece of the current GPU's memory."""
+    if workspace is None or isinstance(workspace, int):
+        return
+    _on_current_gpu((workspace,), where)
+    if not workspace.is_contiguous():
+        _raise(EINVAL, "%s: a workspace in one piece is needed" % where)
+
+
+def _norm_tensors(desc, where, activations, vectors, saved, workspace):
     """EINVAL for tensors (not addresses, not None) that are not what the descriptor says: another type or size, in several pieces,
     channels not last, not on the current GPU."""
     import torch
@@ -535,6 +550,7 @@ def _norm_tensors(desc, where, activations, vectors, saved):
                 current = torch.cuda.current_device() if t.is_cuda else -1
             if not t.is_cuda or t.get_device() != current:
                 _raise(EINVAL, "%s: tensors of the current GPU are needed" % where)
+    _room(workspace, where)
 
 
 def convbn_group_norm_fwd(desc, x, gamma, beta, z, saved, workspace=None, workspace_bytes: Optional[int] = None, stream=None):
@@ -544,7 +560,7 @@ def convbn_group_norm_fwd(desc, x, gamma, beta, z, saved, workspace=None, worksp
     native = _native or _calls()
     status = native.group_norm_fwd(desc, x, gamma, beta, z, saved, workspace, workspace_bytes, stream)
     if status is None:           # what is wrong, or else addresses or another order of the dimensions
-        _norm_tensors(desc, "convbn_group_norm_fwd", (x, z), (gamma, beta), saved)
+        _norm_tensors(desc, "convbn_group_norm_fwd", (x, z), (gamma, beta), saved, workspace)
         status = native.convbn_group_norm_fwd(desc, x, gamma, beta, z, saved, workspace, workspace_bytes, stream)
     if status:
         _raise(status, "convbn_group_norm_fwd")
@@ -558,16 +574,10 @@ def convbn_group_norm_bwd(desc, dz, x, gamma, beta, saved, dx, dgamma, dbeta, wo
     args = (desc, dz, x, gamma, beta, saved, dx, dgamma, dbeta, workspace, workspace_bytes, stream)
     status = native.group_norm_bwd(*args)
     if status is None:
-        _norm_tensors(desc, "convbn_group_norm_bwd", (dz, x, dx), (gamma, beta, dgamma, dbeta), saved)
+        _norm_tensors(desc, "convbn_group_norm_bwd", (dz, x, dx), (gamma, beta, dgamma, dbeta), saved, workspace)
         status = native.convbn_group_norm_bwd(*args)
     if status:
         _raise(status, "convbn_group_norm_bwd")
-
-
-def _on_current_gpu(tensors, where):
-    import torch
-    if any(not t.is_cuda for t in tensors) or any(t.get_device() != torch.cuda.current_device() for t in tensors):
-        _raise(EINVAL, "%s: tensors of the current GPU are needed" % where)
 
 
 def convbn_orthogonalise_workspace_bytes(rows: int, cols: int, count: int = 1) -> int:
@@ -581,6 +591,7 @@ def convbn_orthogonalise(g, out, steps: int = 5, eps: float = 1e-7, workspace=No
         _raise(EINVAL, "%s: two matrices, or stacks of them, of one shape and type are needed, each in one piece" % where)
     kind = _storage(g)
     _on_current_gpu((g, out), where)
+    _room(workspace, where)
     rows, cols = g.shape[-2:]
     status = (_native or _calls()).convbn_orthogonalise(kind, g, out, rows, cols, g.shape[0] if g.dim() == 3 else 1, steps, float(eps),
                                                         workspace, workspace_bytes, stream)
@@ -630,6 +641,7 @@ def convbn_muon_step(layers: MuonLayers, params: MuonParams, workspace=None, wor
     """Momentum, orthogonal update and new weights of every layer."""
     if layers.device is not None:
         _on_current_gpu((layers.tensors[0][0],), "convbn_muon_step")
+        _room(workspace, "convbn_muon_step")
     status = (_native or _calls()).convbn_muon_step(ctypes.addressof(layers.array), len(layers), layers.dtype, params, workspace,
                                                     workspace_bytes, stream)
     if status:

@@ -18,7 +18,7 @@
 
 namespace {
 
-PyObject *s_data_ptr, *s_nbytes, *s_cuda_stream, *s_dtype, *s_numel, *s_itemsize, *s_is_contiguous, *s_get_device, *s_dim, *s_shape;      // attribute names
+PyObject *s_data_ptr, *s_nbytes, *s_cuda_stream, *s_dtype, *s_numel, *s_itemsize, *s_is_contiguous, *s_get_device, *s_shape;      // attribute names
 PyObject *g_get_device, *g_get_stream;                // torch._C._cuda_getDevice, _cuda_getCurrentRawStream
 
 bool address(PyObject *o, void **out) {
@@ -219,18 +219,18 @@ long long current_device() {
 bool norm_argument(PyObject *o, char kind, const convbn_group_norm_desc *d, long long device) {
     const __int128 all = (__int128)d->n * d->c * ((__int128)d->h * d->w);
     if (all > (1LL << 40)) return false;                 // (the library refuses it)
-    const long long want = kind == 'a' ? (long long)all : kind == 'v' ? d->c : 2LL * d->n * d->groups;
-    if (storage_type(o) != (kind == 'a' ? d->dtype : CONVBN_F32) || number(o, s_numel, true) != want || !contiguous(o) ||
-        number(o, s_get_device, true) != device)
-        return false;
-    if (kind != 'a' || number(o, s_dim, true) != 4) return true;
-    PyObject *shape = PyObject_GetAttr(o, s_shape);
-    bool fits = shape && PyTuple_Check(shape) && PyTuple_Size(shape) == 4;
-    const int extent[4] = {d->n, d->h, d->w, d->c};
-    for (int i = 0; fits && i < 4; ++i) fits = PyLong_AsLong(PyTuple_GetItem(shape, i)) == extent[i];
-    Py_XDECREF(shape);
-    PyErr_Clear();
-    return fits;
+    if (storage_type(o) != (kind == 'a' ? d->dtype : CONVBN_F32) || number(o, s_get_device, true) != device || !contiguous(o)) return false;
+    if (kind == 'a') {                                   // (four dimensions: those; others: as many elements)
+        PyObject *shape = PyObject_GetAttr(o, s_shape);
+        const bool four = shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 4;
+        const int extent[4] = {d->n, d->h, d->w, d->c};
+        bool fits = four;
+        for (int i = 0; fits && i < 4; ++i) fits = PyLong_AsLong(PyTuple_GET_ITEM(shape, i)) == extent[i];
+        Py_XDECREF(shape);
+        PyErr_Clear();
+        if (four) return fits;
+    }
+    return number(o, s_numel, true) == (kind == 'a' ? (long long)all : kind == 'v' ? d->c : 2LL * d->n * d->groups);
 }
 template <auto F>
 PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n, const char *kinds) {
@@ -238,8 +238,11 @@ PyObject *norm(PyObject *self, PyObject *const *a, Py_ssize_t n, const char *kin
     if (n > 1 && !convert(a[0], &d)) return nullptr;
     const long long device = d ? current_device() : -1;
     if (device < 0) Py_RETURN_NONE;
-    for (Py_ssize_t i = 1; kinds[i - 1]; ++i)
+    Py_ssize_t i = 1;
+    for (; kinds[i - 1]; ++i)
         if (i >= n || !norm_argument(a[i], kinds[i - 1], d, device)) Py_RETURN_NONE;
+    // (the workspace is written to by address alone too)
+    if (i < n && a[i] != Py_None && !PyLong_Check(a[i]) && (number(a[i], s_get_device, true) != device || !contiguous(a[i]))) Py_RETURN_NONE;
     return Entry<F>::go(self, a, n);
 }
 PyObject *norm_fwd(PyObject *self, PyObject *const *a, Py_ssize_t n) { return norm<&convbn_group_norm_fwd>(self, a, n, "avvas"); }
@@ -271,8 +274,7 @@ PyMODINIT_FUNC PyInit__binding(void) {
     s_itemsize = PyUnicode_InternFromString("itemsize");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_get_device = PyUnicode_InternFromString("get_device");
-    s_dim = PyUnicode_InternFromString("dim");
     s_shape = PyUnicode_InternFromString("shape");
-    return s_data_ptr && s_nbytes && s_cuda_stream && s_dtype && s_numel && s_itemsize && s_is_contiguous && s_get_device && s_dim && s_shape
+    return s_data_ptr && s_nbytes && s_cuda_stream && s_dtype && s_numel && s_itemsize && s_is_contiguous && s_get_device && s_shape
                ? PyModule_Create(&g_module) : nullptr;
 }
