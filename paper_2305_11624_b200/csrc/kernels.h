@@ -436,8 +436,8 @@ struct OrthoTable {
 };
 // Whether the steps of a list's matrices go over m x m matrices (ortho.cuh) rather than over X.
 struct OrthoChoice {
-    bool longer = false;
-    double saved = 0.;
+    bool longer = false;                    // the heaviest item's X is long
+    double heaviest = 0., saved = 0.;
     void add(int rows, int cols, int count);
     bool wide() const;
 };

@@ -763,9 +763,14 @@ cudaError_t launch_ortho_t(const OrthoTable &t, uint8_t *ws, cudaStream_t st) {
 // chain is of shorter products, and where there is much to save.  us in bf16, directly and so: 512 x 4608 188 and 170, 256 x 1152 128 and 119, 512 x 1536
 // 152 and 153, 1000 x 2048 232 and 239, 512 x 768 144 and 148; 2048 x 2560 658 and 586, three of 1956 x 3501 2043 and 1665, two of 988 x 1865
 // (saved / 9: 1.7e9) 369 and 335, 1024 x 2048 (1.1e9) 233 and 239.
+// In a list the heaviest matrix says whether X is long: 640 x 640, 700 x 640 and 5 x 1 take 176 us directly, 187 where 5 x 1 says it.
 void OrthoChoice::add(int rows, int cols, int count) {
     const double m = std::min(rows, cols), n = std::max(rows, cols);
-    longer |= n >= 2.5 * m;
+    const double work = m * m * (3. * n + m) * count;
+    if (work > heaviest) {                         // (whose chain the others of the list run beside)
+        heaviest = work;
+        longer = n >= 2.5 * m;
+    }
     saved += m * m * (n - m) * count;
 }
 bool OrthoChoice::wide() const { return longer || saved > 1.3e9; }

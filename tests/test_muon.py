@@ -337,3 +337,16 @@ def test_muon_step_of_nothing(rows, cols):
     p = C.MuonParams.make(lr=0.5, momentum=0.9, weight_decay=0.25, eps=0.0)
     (v, m, w), = muon([(zero, zero, master)], "bf16", p)
     assert bool((v == 0).all()) and torch.equal(m.cpu(), master * 0.875) and torch.equal(w, m.to(w.dtype))
+
+
+def test_a_small_long_layer_does_not_choose_for_the_list():
+    """Steps over m x m matrices have two more of them in the workspace (three places each): 6 x 9 tile pairs of 32 KB for sides of 300."""
+    def size(*shapes):
+        array = (C._MuonLayer * len(shapes))(*[_layer(*s) for s in shapes])
+        bytes_ = C.lib().convbn_muon_workspace_bytes(ctypes.addressof(array), len(shapes))
+        assert bytes_ > 0
+        return bytes_
+    direct, staged = size((300, 310)), size((300, 2000))
+    assert size((300, 310), (5, 1)) - direct < 6 * 9 * 32768 and size((5, 1), (300, 310)) - direct < 6 * 9 * 32768
+    # but a long layer that is most of the work does
+    assert size((300, 2000), (5, 5)) >= staged and size((300, 2000), (5, 5)) - staged < 6 * 9 * 32768
