@@ -9,6 +9,7 @@
 // at about the rate of distributed shared memory.
 // X lies as m rows x n columns whichever side is the shorter: a tall matrix is transposed on its way in and out.
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "ortho.cuh"
@@ -523,22 +524,24 @@ cudaError_t small_attributes() {
 // 258 and 157; 128 x 2048 by 8 97 and 131, by 16 188 and 146; 64 x 64 by 512 78 and 276.
 template <class T>
 bool small_pays(const OrthoTable &t, const SmallShape &s) {
-    static int known[kMaxDevices][5];                  // clusters at a time + 1
+    static std::atomic<int> known[kMaxDevices][5];     // clusters at a time + 1 (threads that ask at once find the same)
     int log = 0;
     while (1 << log < s.blocks) ++log;
-    int &answer = known[current_device_slot()][log];
-    if (answer == 0 && s.blocks == 1) answer = device_sm_count() + 1;
-    if (answer == 0) {
-        cudaLaunchAttribute at[2];
-        const cudaLaunchConfig_t cfg = small_config<T>(t, s, at);
-        int fit = 0;
-        if (small_attributes<T>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&fit, ortho_small_kernel<T>, &cfg) != cudaSuccess) {
-            cudaGetLastError();
-            fit = 0;
+    std::atomic<int> &answer = known[current_device_slot()][log];
+    int fit = answer.load(std::memory_order_relaxed) - 1;
+    if (fit < 0) {
+        if (s.blocks == 1) {
+            fit = device_sm_count();
+        } else {
+            cudaLaunchAttribute at[2];
+            const cudaLaunchConfig_t cfg = small_config<T>(t, s, at);
+            if (small_attributes<T>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&fit, ortho_small_kernel<T>, &cfg) != cudaSuccess) {
+                cudaGetLastError();
+                fit = 0;
+            }
         }
-        answer = fit + 1;
+        answer.store(fit + 1, std::memory_order_relaxed);
     }
-    const int fit = answer - 1;
     if (fit < 1) return false;
     int side = 0;
     float other = 110.f;

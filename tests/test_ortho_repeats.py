@@ -60,3 +60,31 @@ def test_clusters_are_as_near_as_the_formula_in_fp32(shape, kind):
             x = a * x + (p @ x if shape[1] <= shape[2] else x @ p)
         allowed = 4 * np.linalg.norm(x - ref) + 5 * 2.0 ** -20 * np.linalg.norm(ref)
         assert np.linalg.norm(got[i] - ref) <= allowed, np.linalg.norm(got[i] - ref) / allowed
+
+
+def test_threads_that_ask_at_once():
+    """The first calls of a process, made by four threads on streams of their own, choose the same kernel and give the same bits."""
+    import subprocess
+    import sys
+    import os
+    code = '''
+import threading, torch
+from paper_2305_11624_b200 import convbn as C
+g = torch.randn(100, 2000, device="cuda")
+out, ws = [torch.empty_like(g) for _ in range(5)], [torch.empty(C.convbn_orthogonalise_workspace_bytes(100, 2000), dtype=torch.uint8, device="cuda") for _ in range(5)]
+streams, gate = [torch.cuda.Stream() for _ in range(4)], threading.Barrier(4)
+torch.cuda.synchronize()
+def one(k):
+    gate.wait()
+    C.convbn_orthogonalise(g, out[k], 5, 1e-7, ws[k], stream=streams[k])
+threads = [threading.Thread(target=one, args=(k,)) for k in range(4)]
+for t in threads: t.start()
+for t in threads: t.join()
+torch.cuda.synchronize()
+C.convbn_orthogonalise(g, out[4], 5, 1e-7, ws[4])
+C.convbn_check()
+assert all(torch.equal(o, out[4]) for o in out[:4])
+'''
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
