@@ -39,12 +39,8 @@ struct NormVec {
                  typename std::conditional<kBytes == 4, uint32_t, uint16_t>::type>::type>::type;
     Word w;
     __device__ __forceinline__ void load(const T *p) { w = *reinterpret_cast<const Word *>(p); }
-    // the same for data that nothing reads again
-    __device__ __forceinline__ void load_last(const T *p) {
-        if constexpr (kBytes == 2) w = __ldcs(reinterpret_cast<const unsigned short *>(p));
-        else w = __ldcs(reinterpret_cast<const Word *>(p));
-    }
     __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<Word *>(p) = w; }
+    // the same for data that nothing reads again
     __device__ __forceinline__ void store_last(T *p) const {
         if constexpr (kBytes == 2) __stcs(reinterpret_cast<unsigned short *>(p), w);
         else __stcs(reinterpret_cast<Word *>(p), w);

@@ -430,7 +430,7 @@ struct OrthoTable {
     int first[kOrthoPhases + 1];            // ... and tasks
     int dtype;                              // of g and out (muon: of out; g is fp32)
     int muon, nesterov;
-    float momentum, keep, lr;               // keep = 1 - lr weight_decay
+    float momentum, keep;                   // keep = 1 - lr weight_decay
     double eps;
     OrthoItem item[kOrthoItems];
 };
