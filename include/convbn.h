@@ -403,7 +403,8 @@ int convbn_add(int dtype, const void *a, const void *b, void *out, long long cou
  * act: none, max(y, 0), or y / (1 + exp(-y)).  gamma, beta [c] fp32.  saved: means [n][groups], then r [n][groups], fp32.
  * Backward, with dy = dz act'(y) and E the mean over a group's values:
  *     dbeta = sum dy      dgamma = sum dy xhat      dx = r (gamma dy - E(gamma dy) - xhat E(gamma dy xhat)),   xhat = (x - mean) r
- * y is formed again from x and saved; ReLU passes dz where y > 0, decided by the value in 64 bits.
+ * y is formed again from x and saved; ReLU passes dz where y > 0, decided by the value in 64 bits (the forward call's y is fp32: next to zero its z may
+ * be a rounding above where the backward call sees y < 0, and the other way round).  dgamma and dbeta are added up over samples in 64 bits.
  * Variances are sums of squared distances from values of the group, not a difference of two large numbers; fp32, fixed order.  A group that
  * holds a NaN or an infinity is NaN (which ReLU's max(., 0) turns into 0, as convbn_relu does); other groups are not touched by it.
  * Layout CONVBN_NHWC with any of the three storage types; CONVBN_NCHW: CONVBN_EUNSUPPORTED, sizes 0.  Any h, w (1 x 1: a matrix [n][c]);

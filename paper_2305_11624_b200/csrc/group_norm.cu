@@ -9,7 +9,7 @@
 // and few runs are left for the second pass to join: clusters of eight blocks join theirs.
 // Measured, against each tensor once at the rate of a copy: forward 32 x 56 x 56 x 256 bf16 30.4 us (15.7; two plain passes, read and copied, take 27 to 31),
 // 2 x 200 x 334 x 256 43.7 (20.8), 64 x 112 x 112 x 96 half with SiLU 97 (47); backward 64 x 7 x 7 x 2048 on chip 18 to 20 (5.9), 2 x 200 x 334 x 256
-// 61 (31), 64 x 112 x 112 x 96 150 (70).  On chip from shared memory for these: 39 to 44 us for the first, where one cluster's sums wait for its loads.
+// 61 (31), 64 x 112 x 112 x 96 150 (70).  On chip the first took 27 in an early form of the kernel and 39 to 44 in a later one.
 #include "group_norm.cuh"
 
 #include <algorithm>

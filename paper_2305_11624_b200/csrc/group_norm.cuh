@@ -120,7 +120,8 @@ struct NormChannels {
     __device__ __forceinline__ f32x2 y(f32x2 xc, int i) const { return fma2(xc, scale[i], beta[i]); }
 };
 
-// 1 / (1 + exp(-y)); exp(-y) = infinity gives 0.
+// 1 / (1 + exp(-y)); exp(-y) = infinity gives 0.  The exponent is rounded once (|y| 2^-24 of the exponential), ex2.approx and rcp.approx add 2^-22
+// and 2^-23: for y = -20 1.5e-6 of the result, which is 2e-9 there; fp32 tensors have the same.
 __device__ __forceinline__ f32x2 sigmoid2(f32x2 y) {
     const float2 t = split2(mul2(y, both(-1.44269504f)));
     float e0, e1, r0, r1;
@@ -145,7 +146,8 @@ __device__ __forceinline__ NormVec<T, V> norm_forward(const NormVec<T, V> &x, co
     return z;
 }
 
-// ReLU: dz where y > 0.  The sign of y decides a whole gradient.  x - mean and gamma r are each off by half a step, so y in fp32 by less than
+// ReLU: dz where y > 0.  The sign of y decides a whole gradient.  (The forward call's max(y, 0) has nothing to decide: next to zero it is off by y's
+// own rounding, on either side.)  x - mean and gamma r are each off by half a step, so y in fp32 by less than
 // 4 * 2^-24 of gamma r (x - mean), which is next to |beta| where y is next to zero: if one of the V values is within `near` = 2^-20 max |beta|
 // (or no number), each sign is taken in 64 bits.
 template <class T, int V>

@@ -195,8 +195,8 @@ __global__ void __launch_bounds__(256) ortho_tile_kernel(const __grid_constant__
 // two, would need columns that lo hi does not touch.  128 x 64 tiles have them, and gain (A's rows come once less from shared memory: 512 x 4608
 // 194 us instead of 200); 128 x 128 ones do not, and would not: two 2048 x 8192 take 2126 us, 2110 with the two products on shared columns.  What a task
 // adds to its product is brought by bulk copies too: read by the rows' own threads it took 7000 clocks of a task, 32 lines an instruction.
-// Bound, where X is large, by these copies: a step takes 1150 to 1250 clocks, its MMAs 768, and 52 bytes a clock come from L2 to each SM.
-// Two 2048 x 8192 in bf16: MMAs busy 61 % of 1.73 ms.  Where X is small, by the chain of products: 512 x 4608 in fp32 (185 us) is fifteen of them one
+// Bound, where X is large, by these copies: a step takes about 1250 clocks, its MMAs 768, and 52 bytes a clock come from L2 to each SM.
+// Two 2048 x 8192 in bf16: MMAs busy 58 % of 1.77 ms.  Where X is small, by the chain of products: 512 x 4608 in fp32 (190 us) is fifteen of them one
 // after the other, each waiting for the last one's results (about 1 us from its last MMA to the next one's first tile) and its own sums.
 // hi hi is summed apart from the other two products: the tensor core's sums drift towards zero
 // with their length, and those of small numbers do not notice.  For the same reason a long sum is cut: the epilogue adds the
@@ -760,9 +760,9 @@ cudaError_t launch_ortho_t(const OrthoTable &t, uint8_t *ws, cudaStream_t st) {
 }  // namespace
 
 // Two steps at a time or more save 9 m^2 (n - m) operations of five steps', and cost two more products in the chain: they pay where X is long, so that the
-// chain is of shorter products, and where there is much to save.  us in bf16, directly and so: 512 x 4608 188 and 170, 256 x 1152 128 and 119, 512 x 1536
-// 152 and 153, 1000 x 2048 232 and 239, 512 x 768 144 and 148; 2048 x 2560 658 and 586, three of 1956 x 3501 2043 and 1665, two of 988 x 1865
-// (saved / 9: 1.7e9) 369 and 335, 1024 x 2048 (1.1e9) 233 and 239.
+// chain is of shorter products, and where there is much to save.  us in bf16, directly and so: 512 x 4608 199 and 179, 256 x 1152 138 and 130, 512 x 1536
+// 164 and 163, 1000 x 2048 248 and 251, 512 x 768 154 and 158; 2048 x 2560 695 and 627, three of 1956 x 3501 2131 and 1787, two of 988 x 1865
+// (saved / 9: 1.7e9) 380 and 349, 1024 x 2048 (1.1e9) 290 and 294.
 // In a list the heaviest matrix says whether X is long: 640 x 640, 700 x 640 and 5 x 1 take 176 us directly, 187 where 5 x 1 says it.
 void OrthoChoice::add(int rows, int cols, int count) {
     const double m = std::min(rows, cols), n = std::max(rows, cols);

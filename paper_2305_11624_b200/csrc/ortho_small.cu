@@ -5,7 +5,7 @@
 // from tensor memory and the rounding to pairs follow one another with a barrier in between; only A, whose sums run over all columns, goes
 // round the cluster: every block sends its part's rows to the block that adds them up, which hands the result to all.
 // 64 x 64 in fp32 takes 19 us, 75 by the kernel for large matrices: a product is 1650 clocks, 950 from the first MMA's issue to the last one's
-// end and 650 for sums and rounding, the way in 2 us, out 1.  128 x 1152 takes 75 us: 9000 of a step's 25000 clocks are A's round, 128 KB into each block
+// end and 650 for sums and rounding, the way in 2 us, out 1.  128 x 1152 takes 79 us: 9000 of a step's 25000 clocks are A's round, 128 KB into each block
 // at about the rate of distributed shared memory.
 // X lies as m rows x n columns whichever side is the shorter: a tall matrix is transposed on its way in and out.
 #include <algorithm>
@@ -520,8 +520,8 @@ cudaError_t small_attributes() {
 }
 // Whether the device holds such clusters (of sixteen blocks not every one does), and this is the shorter way.  A B200 runs 7 clusters of sixteen blocks at
 // a time, 15 of eight, 33 of four, 74 of two; the next ones are another round, where the kernel for large matrices fills the SMs and its chain of
-// waits is paid once.  Estimates in us, five steps.  Measured, this kernel and the other, fp32: one 16 x 2268 44 and 119, one 128 x 4096 99 and 130; eight of those
-// 258 and 157; 128 x 2048 by 8 97 and 131, by 16 188 and 146; 64 x 64 by 512 78 and 276.
+// waits is paid once.  Estimates in us, five steps.  Measured, this kernel and the other, fp32: one 16 x 2268 58 and 136, one 128 x 4096 116 and 148; eight of those
+// 216 and 170; 128 x 2048 by 8 108 and 145, by 16 206 and 160; 64 x 64 by 512 89 and 306.
 template <class T>
 bool small_pays(const OrthoTable &t, const SmallShape &s) {
     static std::atomic<int> known[kMaxDevices][5];     // clusters at a time + 1 (threads that ask at once find the same)

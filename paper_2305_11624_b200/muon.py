@@ -12,7 +12,8 @@ from . import convbn as C
 
 class Muon:
     """layers: (weight, gradient) pairs; weight: [C_out, ...] in its storage type, one piece, updated in place; gradient: fp32, as many
-    elements in the same order (a block's dw, a view of a GradientBucket), read at every step where it then is."""
+    elements in the same order (a block's dw, a view of a GradientBucket).  The very tensors given are read at every step: a gradient that is formed
+    anew elsewhere has to be copied into its own."""
 
     def __init__(self, layers: Iterable[Tuple[torch.Tensor, torch.Tensor]], lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, eps=1e-7):
         layers = [(w.detach(), g.detach()) for w, g in layers]
